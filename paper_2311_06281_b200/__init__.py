@@ -7,4 +7,4 @@ kernels, sources under ``csrc/``, declarations in ``include/heinsen_scan.h``).
 synthetic inputs.  Importing the package does not load the library; the first call
 does, and fails loudly if it has not been built.
 """
-__all__ = ["heinsen_scan", "workloads", "build_ext", "sharding"]
+__all__ = ["heinsen_scan", "heinsen_attention", "workloads", "build_ext", "sharding"]

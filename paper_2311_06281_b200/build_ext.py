@@ -4,14 +4,16 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libheinsen_scan.so")
-SOURCES = ["heinsen_scan.cu"]
-HEADERS = ["hs_device.cuh", "hs_kernels.cuh", "hs_pairs.cuh", os.path.join("..", "..", "include", "heinsen_scan.h")]
+SOURCES = ["heinsen_scan.cu", "heinsen_attention.cu", "heinsen_norms.cu"]
+HEADERS = ["hs_device.cuh", "hs_kernels.cuh", "hs_pairs.cuh", "hs_internal.h", "ha_simt.cuh", "hn_norms.cuh",
+           os.path.join("..", "..", "include", "heinsen_scan.h"), os.path.join("..", "..", "include", "heinsen_attention.h")]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-              "-shared", "-Xcompiler", "-fPIC"]
+              "-Xcompiler", "-fPIC"]
 
 
 def _nvcc() -> str:
@@ -39,13 +41,19 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     lib = DEBUG_LIB if debug else LIB
     if force or is_stale(lib):
         tmp = f"{lib}.{os.getpid()}.tmp"
-        cmd = [_nvcc(), *NVCC_FLAGS, *(["-DHEINSEN_DEBUG"] if debug else []), "-o", tmp,
-               *[os.path.join(CSRC, s) for s in SOURCES]]
-        if verbose:
-            cmd.insert(1, "-Xptxas")
-            cmd.insert(2, "-v")
-            print(" ".join(cmd), file=sys.stderr)
-        subprocess.check_call(cmd, cwd=CSRC)
+        with tempfile.TemporaryDirectory() as objs:  # one nvcc for each source, side by side
+            compiling = []
+            for src in SOURCES:
+                cmd = [_nvcc(), *NVCC_FLAGS, *(["-DHEINSEN_DEBUG"] if debug else []), "-c", os.path.join(CSRC, src),
+                       "-o", os.path.join(objs, src + ".o")]
+                if verbose:
+                    cmd[1:1] = ["-Xptxas", "-v"]
+                    print(" ".join(cmd), file=sys.stderr)
+                compiling.append((cmd, subprocess.Popen(cmd, cwd=CSRC)))
+            failed = [cmd for cmd, proc in compiling if proc.wait() != 0]
+            if failed:
+                raise subprocess.CalledProcessError(1, failed[0])
+            subprocess.check_call([_nvcc(), *NVCC_FLAGS, "-shared", "-o", tmp, *(cmd[-1] for cmd, _ in compiling)], cwd=CSRC)
         os.replace(tmp, lib)
     return lib
 

@@ -1,0 +1,271 @@
+// C ABI of the attention with a decay for each head: checks of the arguments, workspace layout, launches.
+#include "../../include/heinsen_attention.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "ha_simt.cuh"
+#include "hs_internal.h"
+
+namespace {
+
+using ha::Pass;
+using ha::Rows;
+
+constexpr long long kMaxTokens = (1ll << 31) - (1ll << 20);
+constexpr int kMaxHeadDim = 256;
+constexpr size_t kHeaderBytes = 256;
+
+size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+
+hs_status validate(const heinsen_attention_problem* p) {
+    if (!p || p->batch < 0 || p->tokens < 0 || p->tokens > kMaxTokens) return HS_ERR_INVALID_ARG;
+    if (p->heads < 0 || p->q_heads < 0 || p->k_heads < 0 || p->v_heads < 0) return HS_ERR_INVALID_ARG;
+    if (p->k_dim < 1 || p->k_dim > kMaxHeadDim || p->v_dim < 1 || p->v_dim > kMaxHeadDim) return HS_ERR_INVALID_ARG;
+    if (p->dtype != HS_F32 && p->dtype != HS_BF16) return HS_ERR_INVALID_ARG;
+    if (!std::isfinite(p->scale) || p->scale == 0.0f) return HS_ERR_INVALID_ARG;
+    if (p->heads > 0) {
+        if (!p->q_heads || !p->k_heads || !p->v_heads) return HS_ERR_INVALID_ARG;
+        if (p->heads % p->q_heads || p->heads % p->k_heads || p->heads % p->v_heads) return HS_ERR_INVALID_ARG;
+        if (p->batch > 0x7fffffffll / p->heads) return HS_ERR_INVALID_ARG;
+        if (p->tokens && p->batch > (1ll << 62) / p->tokens / p->heads / std::max(p->k_dim, p->v_dim)) return HS_ERR_INVALID_ARG;
+    }
+    return HS_OK;
+}
+bool nothing(const heinsen_attention_problem* p) { return p->batch == 0 || p->heads == 0; }
+hs_status validate_inputs(const heinsen_attention_problem* p) {
+    if (p->tokens && (!p->q.ptr || !p->k.ptr || !p->v.ptr || !p->log_a.ptr)) return HS_ERR_INVALID_ARG;
+    return HS_OK;
+}
+
+Rows rows_of(const heinsen_attention_tensor& t, int heads, int own) {
+    return {t.ptr, t.batch_stride, t.token_stride, t.head_stride, heads / own};
+}
+
+hs_status launched(const char* what) {
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return hs_internal::cuda_fail(what, e);
+    hs_internal::count_launches(1);
+    return HS_OK;
+}
+
+template <class T, bool kRev, class OutT>
+hs_status simt_pass(const Pass& ps, cudaStream_t stream) {
+    const size_t smem = ha::simt_pass_smem(ps.dx);
+    const auto fn = ha::simt_pass_kernel<T, kRev, OutT>;
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
+    const long long grid = (long long)ps.batch * ps.heads * ((ps.dz + ha::kSimtCols - 1) / ha::kSimtCols);
+    if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
+    fn<<<(unsigned)grid, ha::kSimtThreads, smem, stream>>>(ps);
+    return launched("simt_pass_kernel");
+}
+
+Pass common(const heinsen_attention_problem* p) {
+    Pass ps;
+    std::memset(&ps, 0, sizeof ps);
+    ps.log_a = static_cast<const float*>(p->log_a.ptr);
+    ps.ab = p->log_a.batch_stride; ps.at = p->log_a.token_stride; ps.ah = p->log_a.head_stride;
+    ps.lengths = p->lengths;
+    ps.batch = (int)p->batch; ps.tokens = (int)p->tokens; ps.heads = p->heads;
+    ps.scale = p->scale;
+    ps.s_in_mul = ps.s_out_mul = 1.0f;
+    return ps;
+}
+
+// Workspace of a backward pass: header | dq, dk, dv for each head, float32 | the states before every chunk and the gradients
+// of the states behind it | sums of the decay gradients.
+struct BackwardSpace {
+    size_t dq, dk, dv, before, behind, part, total;
+};
+BackwardSpace backward_space(const heinsen_attention_problem* p) {
+    BackwardSpace s;
+    const size_t rows = (size_t)p->batch * p->tokens * p->heads;
+    const size_t chunks = (size_t)p->batch * p->heads * ((p->tokens + ha::kSimtChunk - 1) / ha::kSimtChunk);
+    s.dq = kHeaderBytes;
+    s.dk = s.dq + up256(rows * p->k_dim * 4);
+    s.dv = s.dk + up256(rows * p->k_dim * 4);
+    s.before = s.dv + up256(rows * p->v_dim * 4);
+    s.behind = s.before + up256(chunks * p->k_dim * p->v_dim * 4);
+    s.part = s.behind + up256(chunks * p->k_dim * p->v_dim * 4);
+    s.total = s.part + up256(chunks * 8);
+    return s;
+}
+
+template <class T>
+hs_status forward_pass(const heinsen_attention_problem* p, const heinsen_attention_tensor* o, float* state, cudaStream_t stream) {
+    Pass ps = common(p);
+    ps.x = rows_of(p->q, p->heads, p->q_heads);
+    ps.y = rows_of(p->k, p->heads, p->k_heads);
+    ps.z = rows_of(p->v, p->heads, p->v_heads);
+    ps.dx = p->k_dim; ps.dz = p->v_dim;
+    ps.s_in = p->state0; ps.s_out = state;
+    ps.out = const_cast<void*>(o->ptr); ps.ob = o->batch_stride; ps.ot = o->token_stride; ps.oh = o->head_stride;
+    return simt_pass<T, false, T>(ps, stream);
+}
+
+template <class T>
+hs_status sum_heads(const float* src, void* dst, const heinsen_attention_problem* p, int groups, int dim, cudaStream_t stream) {
+    const long long total = (long long)p->batch * p->tokens * groups * dim;
+    if (total == 0) return HS_OK;
+    const long long grid = std::min<long long>((total + 255) / 256, 148 * 16);
+    ha::sum_heads_kernel<T><<<(unsigned)grid, 256, 0, stream>>>(src, static_cast<T*>(dst), p->lengths, (int)p->tokens, p->heads,
+                                                               groups, dim, total);
+    return launched("sum_heads_kernel");
+}
+
+template <class T>
+hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_attention_tensor* d_o, const float* d_state,
+                          void* dq, void* dk, void* dv, float* dlog_a, float* dstate0, uint8_t* ws,
+                          cudaStream_t stream) {
+    const BackwardSpace sp = backward_space(p);
+    float *wq = reinterpret_cast<float*>(ws + sp.dq), *wk = reinterpret_cast<float*>(ws + sp.dk),
+          *wv = reinterpret_cast<float*>(ws + sp.dv);
+    float *before = dlog_a ? reinterpret_cast<float*>(ws + sp.before) : nullptr,
+          *behind = dlog_a ? reinterpret_cast<float*>(ws + sp.behind) : nullptr;
+    double* part = reinterpret_cast<double*>(ws + sp.part);
+    const Rows q = rows_of(p->q, p->heads, p->q_heads), k = rows_of(p->k, p->heads, p->k_heads),
+               v = rows_of(p->v, p->heads, p->v_heads), g = rows_of(*d_o, p->heads, p->heads);
+    hs_status st;
+    auto to = [&](Pass& ps, float* w, int dim) {
+        ps.out = w; ps.oh = dim; ps.ot = (long long)p->heads * dim; ps.ob = p->tokens * ps.ot;
+    };
+    {
+        Pass ps = common(p);
+        ps.x = g; ps.y = v; ps.z = k; ps.dx = p->v_dim; ps.dz = p->k_dim;
+        ps.s_in = p->state0; ps.s_in_t = 1;
+        to(ps, wq, p->k_dim);
+        ps.dump = before;
+        if ((st = simt_pass<T, false, float>(ps, stream)) != HS_OK) return st;
+    }
+    {
+        Pass ps = common(p);
+        ps.x = v; ps.y = g; ps.z = q; ps.dx = p->v_dim; ps.dz = p->k_dim;
+        ps.s_in = d_state; ps.s_in_t = 1; ps.s_in_mul = 1.0f / p->scale;  // the scale comes back with the output
+        to(ps, wk, p->k_dim);
+        ps.dump = behind;
+        if ((st = simt_pass<T, true, float>(ps, stream)) != HS_OK) return st;
+    }
+    {
+        Pass ps = common(p);
+        ps.x = k; ps.y = q; ps.z = g; ps.dx = p->k_dim; ps.dz = p->v_dim;
+        ps.s_in = d_state; ps.s_in_mul = 1.0f / p->scale;
+        ps.s_out = dstate0; ps.s_out_mul = p->scale;
+        to(ps, wv, p->v_dim);
+        if ((st = simt_pass<T, true, float>(ps, stream)) != HS_OK) return st;
+    }
+    if ((st = sum_heads<T>(wq, dq, p, p->q_heads, p->k_dim, stream)) != HS_OK) return st;
+    if ((st = sum_heads<T>(wk, dk, p, p->k_heads, p->k_dim, stream)) != HS_OK) return st;
+    if ((st = sum_heads<T>(wv, dv, p, p->v_heads, p->v_dim, stream)) != HS_OK) return st;
+    if (dlog_a) {
+        ha::DecayGrad d;
+        d.q = q; d.k = k; d.v = v; d.g = g;
+        d.log_a = static_cast<const float*>(p->log_a.ptr);
+        d.ab = p->log_a.batch_stride; d.at = p->log_a.token_stride; d.ah = p->log_a.head_stride;
+        d.lengths = p->lengths; d.tokens = (int)p->tokens; d.heads = p->heads; d.dk = p->k_dim; d.dv = p->v_dim;
+        d.chunks = (int)((p->tokens + ha::kSimtChunk - 1) / ha::kSimtChunk);
+        d.scale = p->scale; d.before = before; d.behind = behind;
+        const bool fixed = p->log_a.batch_stride == 0 && p->log_a.token_stride == 0;
+        d.dlog_a = dlog_a; d.part = fixed ? part : nullptr;
+        const long long grid = p->batch * p->heads * d.chunks;
+        if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
+        if (grid) {
+            const size_t smem = ha::decay_grad_smem(p->k_dim, p->v_dim);
+            const cudaError_t e = cudaFuncSetAttribute(ha::decay_grad_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
+            ha::decay_grad_kernel<T><<<(unsigned)grid, ha::kDecayThreads, smem, stream>>>(d);
+            if ((st = launched("decay_grad_kernel")) != HS_OK) return st;
+        }
+        if (fixed) {
+            ha::decay_grad_sum_kernel<<<(unsigned)p->heads, 32, 0, stream>>>(part, (int)p->batch, p->heads, d.chunks, dlog_a);
+            if ((st = launched("decay_grad_sum_kernel")) != HS_OK) return st;
+        }
+    }
+    return HS_OK;
+}
+
+hs_status check_space(const heinsen_attention_problem* p, int backward, void* workspace, size_t bytes) {
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HS_ERR_INVALID_ARG;
+    return bytes < heinsen_attention_workspace_bytes(p, backward) ? HS_ERR_WORKSPACE_TOO_SMALL : HS_OK;
+}
+
+template <class T>
+hs_status step(const ha::Step& s, long long batch, cudaStream_t stream) {
+    const bool vec = s.dv % 4 == 0 && (reinterpret_cast<uintptr_t>(s.pool) & 15u) == 0;
+    auto go = [&](auto fn, int cols) {
+        const long long grid = batch * s.heads * ((s.dv + cols - 1) / cols);
+        if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
+        fn<<<(unsigned)grid, ha::kStepThreads, 0, stream>>>(s);
+        return launched("step_kernel");
+    };
+    if (!vec) return go(ha::step_kernel<T, 32, 1>, 32);
+    return go(ha::step_kernel<T, 32, 4>, 32);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t heinsen_attention_workspace_bytes(const heinsen_attention_problem* p, int backward) {
+    if (validate(p) != HS_OK) return 0;
+    if (!backward || nothing(p)) return kHeaderBytes;
+    return backward_space(p).total;
+}
+
+hs_status heinsen_attention_forward(const heinsen_attention_problem* p, const heinsen_attention_tensor* o, float* state,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+    hs_status st = validate(p);
+    if (st != HS_OK || nothing(p)) return st;
+    if ((st = validate_inputs(p)) != HS_OK) return st;
+    if (!o || (p->tokens && !o->ptr)) return HS_ERR_INVALID_ARG;
+    if ((st = check_space(p, 0, workspace, workspace_bytes)) != HS_OK) return st;
+    int sms;
+    if ((st = hs_internal::current_device(&sms)) != HS_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return p->dtype == HS_F32 ? forward_pass<float>(p, o, state, s) : forward_pass<__nv_bfloat16>(p, o, state, s);
+}
+
+hs_status heinsen_attention_backward(const heinsen_attention_problem* p, const heinsen_attention_tensor* d_o,
+                                     const float* d_state, void* dq, void* dk, void* dv,
+                                     float* dlog_a, float* dstate0, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+    hs_status st = validate(p);
+    if (st != HS_OK || nothing(p)) return st;
+    if ((st = validate_inputs(p)) != HS_OK) return st;
+    if (!d_o || (p->tokens && (!d_o->ptr || !dq || !dk || !dv))) return HS_ERR_INVALID_ARG;
+    if ((st = check_space(p, 1, workspace, workspace_bytes)) != HS_OK) return st;
+    int sms;
+    if ((st = hs_internal::current_device(&sms)) != HS_OK) return st;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return p->dtype == HS_F32
+               ? backward_passes<float>(p, d_o, d_state, dq, dk, dv, dlog_a, dstate0, ws, s)
+               : backward_passes<__nv_bfloat16>(p, d_o, d_state, dq, dk, dv, dlog_a, dstate0, ws, s);
+}
+
+hs_status heinsen_attention_step(const heinsen_attention_problem* p, const heinsen_attention_tensor* o, float* pool_state,
+                                 int64_t pool, const int32_t* slots, void* stream) {
+    hs_status st = validate(p);
+    if (st != HS_OK) return st;
+    if (p->tokens != 1 || p->lengths || p->state0 || pool < 0) return HS_ERR_INVALID_ARG;
+    if (!slots && pool < p->batch) return HS_ERR_INVALID_ARG;
+    if (nothing(p)) return HS_OK;
+    if ((st = validate_inputs(p)) != HS_OK) return st;
+    if (!o || !o->ptr || (pool && !pool_state)) return HS_ERR_INVALID_ARG;
+    int sms;
+    if ((st = hs_internal::current_device(&sms)) != HS_OK) return st;
+    ha::Step s;
+    s.q = p->q.ptr; s.k = p->k.ptr; s.v = p->v.ptr;
+    s.qb = p->q.batch_stride; s.qh = p->q.head_stride; s.qdiv = p->heads / p->q_heads;
+    s.kb = p->k.batch_stride; s.kh = p->k.head_stride; s.kdiv = p->heads / p->k_heads;
+    s.vb = p->v.batch_stride; s.vh = p->v.head_stride; s.vdiv = p->heads / p->v_heads;
+    s.log_a = static_cast<const float*>(p->log_a.ptr); s.ab = p->log_a.batch_stride; s.ah = p->log_a.head_stride;
+    s.pool = pool_state; s.slots = slots; s.pool_rows = pool;
+    s.heads = p->heads; s.dk = p->k_dim; s.dv = p->v_dim; s.scale = p->scale;
+    s.o = const_cast<void*>(o->ptr); s.ob = o->batch_stride; s.oh = o->head_stride;
+    cudaStream_t str = static_cast<cudaStream_t>(stream);
+    return p->dtype == HS_F32 ? step<float>(s, p->batch, str) : step<__nv_bfloat16>(s, p->batch, str);
+}
+
+}  // extern "C"

@@ -13,6 +13,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "hs_internal.h"
 #include "hs_kernels.cuh"
 
 namespace {
@@ -625,6 +626,20 @@ __global__ void __launch_bounds__(256) mufu_probe_kernel(int iterations, float s
 }  // namespace
 
 // =============================================================================================
+namespace hs_internal {
+hs_status cuda_fail(const char* what, cudaError_t e) { return ::cuda_fail(what, e); }
+hs_status current_device(int* sm_count) {
+    DeviceInfo di;
+    const hs_status st = device_info(di);
+    if (st != HS_OK) return st;
+    if (di.cc_major != 10) return HS_ERR_UNSUPPORTED_DEVICE;
+    *sm_count = di.sm_count;
+    return HS_OK;
+}
+void count_launches(int n) { g_launches.fetch_add(n); }
+unsigned long long call_id() { return next_call_id(); }
+}  // namespace hs_internal
+
 extern "C" {
 
 hs_status heinsen_scan_probe_mufu(int iterations, double* results, double* seconds) {
