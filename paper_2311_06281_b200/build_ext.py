@@ -10,7 +10,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libheinsen_scan.so")
 SOURCES = ["heinsen_scan.cu", "heinsen_attention.cu", "heinsen_norms.cu"]
-HEADERS = ["hs_device.cuh", "hs_kernels.cuh", "hs_pairs.cuh", "hs_internal.h", "ha_simt.cuh", "hn_norms.cuh",
+HEADERS = ["hs_device.cuh", "hs_kernels.cuh", "hs_pairs.cuh", "hs_internal.h", "ha_ptx.cuh", "ha_simt.cuh", "ha_mma.cuh", "hn_norms.cuh",
            os.path.join("..", "..", "include", "heinsen_scan.h"), os.path.join("..", "..", "include", "heinsen_attention.h")]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC"]

@@ -1,0 +1,657 @@
+// The passes of ha_simt.cuh on the tensor cores (tcgen05): bf16 tensors, head dimensions up to 128, chunks of 128 tokens.
+//
+// One CTA walks the chunks of one (batch, head), or of one segment of it, with the state S^T in registers.  Per chunk
+//     P   = mask(e^{c_i-c_j}) o (X Y^T)         X, Y from shared memory; P goes back to tensor memory as the next A operand
+//     out = scale (e^{c_i} X S + P Z)           the second product adds to the first, whose rows are scaled between them
+//     S^T = e^{c_C} S^T + (w Z)^T Y             Z^T reaches tensor memory by sixteen-column products with an identity: the
+//                                               tensor core transposes, the threads scale by the weights w_j and write the
+//                                               A operand back, no shared memory is spent on it
+// Warps 0-7 own the rows of P and out (two threads to a row), warps 8-15 the rows of S^T (likewise); the two chains meet only
+// in S.  One warp of the last four loads (TMA, two chunks ahead) and sums the decays, one thread of another issues the
+// products.
+//
+// Rounding.  A float32 factor enters a product as bf16 terms: w Z (and so the state, which is float32 to its owner) as three,
+// 24 bits, exact to float32's own rounding; P and the state in X S as kTerms: one where only the bf16 output depends on
+// it (its own rounding is as large), two where the decay gradients do, and then two for w Z as well.
+#pragma once
+#include <cuda.h>
+
+#include "ha_ptx.cuh"
+#include "ha_simt.cuh"
+
+namespace ha {
+
+constexpr int kChunk = 128;
+constexpr int kMmaThreads = 640;
+// Registers of a thread: 96 at launch (65536 over 20 warps); those that the feeding warps and the rows of out can spare go to
+// the rows of the state.  64 + 2 * 80 + 2 * 128 = 480 for a thread of each warpgroup, 5 * 96 as at launch.
+constexpr int kRowRegs = 80, kStateRegs = 128, kFeedRegs = 64;
+constexpr uint32_t kTile = 128 * 256;        // 128 rows of 128 bf16: two blocks of 64 columns, 128-byte swizzle
+constexpr uint32_t kBlock = kTile / 2;
+constexpr uint32_t kSpin = 1u << 21;         // polls of a barrier before a wait gives up
+
+struct Fault {  // the header that heinsen_scan_check() reads
+    unsigned long long started_id, error_id;
+    int error_code, error_where;
+};
+
+struct MmaPass {
+    const float* log_a;
+    long long ab, at, ah;
+    const int* lengths;
+    int tokens, heads, dx, dz;
+    int xdiv, ydiv, zdiv;
+    float scale;
+    const float* s_in;
+    float* s_out;
+    int s_in_t, s_out_t;
+    float s_in_mul, s_out_mul;
+    void* out;
+    long long ob, ot, oh;
+    // A sequence cut into segments: each starts from seg_state[bh][segment] ([dx, dz], formed by two kernels before this one)
+    int segments, seg_chunks;
+    float* seg_state;
+    float* seg_decay;
+    Fault* fault;
+    unsigned long long call_id;
+};
+
+template <int kTerms>
+struct MmaLayout {
+    static constexpr int kXs = 2, kYs = 2, kZs = kTerms == 1 ? 2 : 1;  // stages; a chunk's X tile also stages its output
+    static constexpr uint32_t x = 0, y = x + kXs * kTile, z = y + kYs * kTile, s = z + kZs * kTile, ident = s + kTerms * kTile,
+                              decays = ident + 512, whole = decays + 4 * kChunk * 4, bars = whole + 32, end = bars + 8 * 32;
+    // Tensor memory columns, all 512.  What is read out before the next product of its chain is due shares columns with it:
+    // Z^T with the state's update, the scores with the output.
+    static constexpr int kWeights = kTerms == 1 ? 3 : 2;       // terms of w Z
+    static constexpr uint32_t tw = 0;                          // the terms of (w Z)^T: A operand
+    static constexpr uint32_t tz = tw + 64 * kWeights;         // Z^T, then the state's update
+    static constexpr uint32_t to = tz + 128;                   // X Y^T, then X S, then P Z
+    static constexpr uint32_t tp = to + 128;                   // the terms of P: A operand
+    static_assert(tp + 64 * kTerms == 512, "tensor memory");
+    // where term t of 16 tokens q lies
+    static __device__ __forceinline__ constexpr uint32_t prob(int q, int t) { return tp + 8 * kTerms * q + 8 * t; }
+    static __device__ __forceinline__ constexpr uint32_t weighted(int q, int t) { return tw + 8 * kWeights * q + 8 * t; }
+};
+
+// Every barrier completes one phase per chunk (those with two entries: per chunk that uses the entry), and nobody who waits
+// for a phase can be overtaken by the next: it needs something of the waiter's own.
+enum Bar : int { kFullX = 0, kFullY = 2, kFullZ = 4, kFreeX = 6, kFreeY = 8, kFreeZ = 10, kPatchY = 12, kPatchZ, kDecays, kDecaysFree, kScores,
+                 kTransposed, kProbs, kFar, kFarRead, kNear, kStaged, kWeighted, kUpdate, kUpdateRead, kStateReady, kDrain,
+                 kBars };
+
+struct Waiter {
+    uint32_t bars;
+    volatile int* stop;  // in shared memory: some wait of this CTA gave up
+    __device__ __forceinline__ bool operator()(int bar, int turn) const {
+#pragma unroll 1
+        for (uint32_t i = 0; i < kSpin; ++i) {
+            if (bar_try(bars + 8 * bar, turn & 1)) return true;
+            if (*stop) return false;
+        }
+        *stop = 1 + bar;
+        return false;
+    }
+};
+
+// A pair of values as kTerms bf16 pairs whose sum is the pair.
+template <int kTerms>
+__device__ __forceinline__ void split(pair v, uint32_t (&t)[kTerms]) {
+    t[0] = pack_bf16(v);
+#pragma unroll
+    for (int i = 1; i < kTerms; ++i) {
+        v = minus_bf16(v, t[i - 1]);
+        t[i] = pack_bf16(v);
+    }
+}
+
+// Sixteen columns of one row, or the n that are left of it
+__device__ __forceinline__ void store_row16(float* to, const float (&v)[16], int n) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+        if (i < n) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+}
+__device__ __forceinline__ void store_row16(__nv_bfloat16* to, const float (&v)[16], int n) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 8)
+        if (i < n)
+            *reinterpret_cast<uint4*>(to + i) =
+                make_uint4(pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3]), pack_bf16(v[i + 4], v[i + 5]), pack_bf16(v[i + 6], v[i + 7]));
+}
+
+template <bool kRev, int kTerms, class Out, bool kStateOnly>
+__global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap my,
+                                                                  const __grid_constant__ CUtensorMap mz, const __grid_constant__ CUtensorMap mo,
+                                                                  const MmaPass p) {
+    using L = MmaLayout<kTerms>;
+    extern __shared__ __align__(1024) uint8_t sm8[];
+    const uint32_t base = smem_addr(sm8);
+    float* const c_hi = reinterpret_cast<float*>(sm8 + L::decays);
+    float* const c_lo = c_hi + kChunk;
+    float* const w_st = c_lo + kChunk;    // what a token's update still weighs at the chunk's end (reversed: its beginning)
+    float* const w_bt = w_st + kChunk;    // ... at the edge of its batch of 32
+    float* const s_whole = reinterpret_cast<float*>(sm8 + L::whole);  // the chunk's decay, and its logarithm in two parts
+    volatile int* const stop = reinterpret_cast<int*>(sm8 + L::whole + 16);
+    uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(sm8 + L::whole + 20);
+    const uint32_t bars = base + L::bars;
+    const Waiter wait{bars, stop};
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    const int cuts = kStateOnly ? p.segments - 1 : p.segments;  // the last segment's own state is not needed by another
+    const int segment = blockIdx.x % cuts, bh = blockIdx.x / cuts, b = bh / p.heads, h = bh % p.heads;
+    const int live = live_tokens(p.lengths, b, p.tokens);
+    const int chunks = (live + kChunk - 1) / kChunk;                       // that hold tokens
+    const int first = min(chunks, segment * p.seg_chunks), count = min(chunks, first + p.seg_chunks) - first;
+    auto chunk_at = [&](int it) { return kRev ? chunks - 1 - (first + it) : first + it; };
+
+    if (tid == 0) {
+        for (int i = 0; i < kBars; ++i) {
+            uint32_t arrivals = 1;
+            if (i >= kFreeY && i < kPatchY) arrivals = kStateOnly ? 1 : 2;
+            if (i == kDecays) arrivals = 32;
+            if (i == kDecaysFree) arrivals = kStateOnly ? 256 : 512;
+            if (i == kProbs || i == kFarRead || i == kStaged || i == kWeighted || i == kUpdateRead || i == kStateReady) arrivals = 256;
+            bar_init(bars + 8 * i, arrivals);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *stop = 0;
+        if (blockIdx.x == 0) p.fault->started_id = p.call_id;
+    }
+    if (tid < 256) {  // the identity, two 8 x 8 core matrices along each of k and n
+        const int n = tid >> 4, k = tid & 15;
+        *reinterpret_cast<__nv_bfloat16*>(sm8 + L::ident + (k >> 3) * 256 + (n >> 3) * 128 + (n & 7) * 16 + (k & 7) * 2) =
+            __float2bfloat16(n == k ? 1.0f : 0.0f);
+    }
+    fence_smem_to_async();
+    if (warp == 16) tmem_alloc(smem_addr(s_tmem), 512);
+    tmem_before_sync();
+    __syncthreads();
+    tmem_after_sync();
+    if (tid == 0 && *s_tmem != 0) *stop = 1 + kBars;  // all columns were asked for: they start at 0
+    constexpr uint32_t tmem = 0;
+
+    if (warp >= 16) {
+        give_registers<kFeedRegs>();
+        // The issuing thread shares a scheduler with the rows that have least to do: the first 32 (reversed: the last)
+        constexpr int kIssuer = kRev ? 19 : 16, kStorer = kRev ? 16 : 19, kLoader = 17, kDecayer = 18;
+        if (warp == kLoader) {
+            // ------------------------------------------------------------ loads
+            auto load = [&](const CUtensorMap* m, uint32_t to, int dim, int head, int t0, int full) {
+                bar_expect(bars + 8 * full, dim > 64 ? kTile : kBlock);
+                tma_load_4d(to, m, 0, head, t0, b, bars + 8 * full);
+                if (dim > 64) tma_load_4d(to + kBlock, m, 64, head, t0, b, bars + 8 * full);
+            };
+            bool ok = true;
+            int loads = 0;
+            for (int it = 0; it < count && ok; ++it) {
+                const int t0 = chunk_at(it) * kChunk;
+                // tokens behind the sequence's end are in memory and may hold anything: 0 * NaN must not reach a sum
+                const bool patch = live < p.tokens && t0 + kChunk > live;
+                const uint32_t Y = base + L::y + it % L::kYs * kTile, Z = base + L::z + it % L::kZs * kTile;
+                if (lane == 0) {
+                    if (!kStateOnly) {
+                        if (it >= L::kXs) ok = wait(kFreeX + it % L::kXs, it / L::kXs - 1);
+                        if (ok) load(&mx, base + L::x + it % L::kXs * kTile, p.dx, h / p.xdiv, t0, kFullX + it % L::kXs);
+                    }
+                    if (ok && it >= L::kYs) ok = wait(kFreeY + it % L::kYs, it / L::kYs - 1);
+                    if (ok) load(&my, Y, p.dx, h / p.ydiv, t0, patch ? kPatchY : kFullY + it % L::kYs);
+                    if (ok && it >= L::kZs) ok = wait(kFreeZ + it % L::kZs, it / L::kZs - 1);
+                    if (ok) {
+                        load(&mz, Z, p.dz, h / p.zdiv, t0, patch ? kPatchZ : kFullZ + it % L::kZs);
+                        loads = it + 1;
+                    }
+                }
+                if (patch) {
+                    ok = __shfl_sync(~0u, (int)ok, 0);
+                    ok = ok && wait(kPatchY, 0) && wait(kPatchZ, 0);
+                    ok = __all_sync(~0u, ok);
+                    const int rows = t0 + kChunk - live;
+                    for (int e = lane; ok && e < rows * 16; e += 32) {
+                        const uint32_t at = (e & 8 ? kBlock : 0) + (live - t0 + (e >> 4)) * 128 + (e & 7) * 16;
+                        if (!(e & 8) || p.dx > 64) *reinterpret_cast<uint4*>(sm8 + (Y - base) + at) = make_uint4(0, 0, 0, 0);
+                        if (!(e & 8) || p.dz > 64) *reinterpret_cast<uint4*>(sm8 + (Z - base) + at) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_smem_to_async();
+                    __syncwarp();
+                    if (lane == 0 && ok) {
+                        bar_arrive(bars + 8 * (kFullY + it % L::kYs));
+                        bar_arrive(bars + 8 * (kFullZ + it % L::kZs));
+                    }
+                }
+            }
+            if (*stop && lane == 0) {  // nothing may land in shared memory after the CTA has left
+                auto drain = [&](int full, int stages) {
+                    for (int it = max(0, loads - stages); it < loads; ++it)
+                        for (uint32_t i = 0; i < kSpin / 16 && !bar_try(bars + 8 * (full + it % stages), (it / stages) & 1); ++i) {}
+                };
+                if (!kStateOnly) drain(kFullX, L::kXs);
+                drain(kFullY, L::kYs);
+                drain(kFullZ, L::kZs);
+            }
+        } else if (warp == kDecayer) {
+            // ------------------------------------------------------------ decays, a lane has four tokens
+            const float* ga = p.log_a + b * p.ab + h * p.ah;
+            float a[4];
+            auto fetch = [&](int it) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = chunk_at(it) * kChunk + 4 * lane + i;
+                    a[i] = it < count && t < live ? ga[t * p.at] : 0.0f;
+                }
+            };
+            fetch(0);
+            bool ok = true;
+            double total = 0.0;
+            for (int it = 0; it < count && ok; ++it) {
+                double c[4], sum;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) c[i] = (i ? c[i - 1] : 0.0) + (double)(a[i] < kReset ? kReset : a[i]) * 1.4426950408889634;
+                fetch(it + 1);
+                sum = c[3];
+                for (int o = 1; o < 32; o *= 2) {
+                    const double u = __shfl_up_sync(~0u, sum, o);
+                    if (lane >= o) sum += u;
+                }
+                const double whole = __shfl_sync(~0u, sum, 31), before = sum - c[3];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) c[i] += before;
+                const double edge = kRev ? __shfl_sync(~0u, c[0], lane & ~7) : __shfl_sync(~0u, c[3], lane | 7);
+                float4 hi, lo, st, bt;
+                auto four = [&](int i, float& h4, float& l4, float& s4, float& b4) {
+                    h4 = (float)c[i];
+                    l4 = (float)(c[i] - (double)(float)c[i]);
+                    s4 = ex2((float)(kRev ? c[i] : whole - c[i]));
+                    b4 = ex2((float)(kRev ? c[i] - edge : edge - c[i]));
+                };
+                four(0, hi.x, lo.x, st.x, bt.x);
+                four(1, hi.y, lo.y, st.y, bt.y);
+                four(2, hi.z, lo.z, st.z, bt.z);
+                four(3, hi.w, lo.w, st.w, bt.w);
+                if (it > 0) ok = __all_sync(~0u, wait(kDecaysFree, it - 1));
+                if (!ok) break;
+                reinterpret_cast<float4*>(c_hi)[lane] = hi;
+                reinterpret_cast<float4*>(c_lo)[lane] = lo;
+                reinterpret_cast<float4*>(w_st)[lane] = st;
+                reinterpret_cast<float4*>(w_bt)[lane] = bt;
+                if (lane == 31) {
+                    s_whole[0] = ex2((float)whole);
+                    s_whole[1] = (float)whole;
+                    s_whole[2] = (float)(whole - (double)(float)whole);
+                }
+                total += whole;
+                bar_arrive(bars + 8 * kDecays);
+            }
+            if (kStateOnly && lane == 0) p.seg_decay[bh * p.segments + segment] = ex2((float)total);
+        } else if (warp == kStorer) {
+            // ------------------------------------------------------------ the output leaves by TMA from the chunk's X tile
+            if (!kStateOnly && lane == 0) {
+                bool ok = true;
+                for (int it = 0; it < count && ok; ++it) {
+                    if (!(ok = wait(kStaged, it))) break;
+                    if constexpr (sizeof(Out) == 2) {
+                        const uint32_t from = base + L::x + it % L::kXs * kTile;
+                        tma_store_4d(&mo, 0, h, chunk_at(it) * kChunk, b, from);
+                        if (p.dz > 64) tma_store_4d(&mo, 64, h, chunk_at(it) * kChunk, b, from + kBlock);
+                        tma_store_commit();
+                        tma_store_wait_read();
+                    }
+                    bar_arrive(bars + 8 * (kFreeX + it % L::kXs));
+                }
+                tma_store_wait_all();
+            }
+        } else if (warp == kIssuer) {
+            // ------------------------------------------------------------ the products
+            // Two chains share the tensor core, output (X Y^T; X S; P Z) and state (Z^T; its update); one thread watches
+            // the barriers of both and issues what is ready.  Nearly all that a product takes is a constant: what has to be
+            // computed between two products delays them (measured: 20 to 30 clocks for a product's issue so, 48 to 110 with
+            // every operand in a register; the tensor core needs 30 to 64).
+            if (elect_one()) {
+                const int kx = (p.dx + 15) / 16;
+                const uint32_t nz = (p.dz + 15) / 16 * 16;
+                const uint32_t shape_p = mma_shape(128, 0), shape_t = mma_shape(16, kColMajorA), shape_f = mma_shape(nz, 0),
+                               shape_n = mma_shape(nz, kColMajorB), shape_u = mma_shape(16 * kx, kColMajorB);
+                auto ready = [&](int bar, int turn) { return bar_test(bars + 8 * bar, turn & 1); };
+                auto k_step = [](int kk) { return (uint32_t)((kk >> 2) * (kBlock >> 4) + (kk & 3) * 2); };  // 32 bytes, then the next block
+                int a_it = kStateOnly ? count : 0, a_step = 0, b_it = 0, b_step = 0;
+                uint32_t idle = 0;
+                while (a_it < count || b_it < count) {
+                    bool moved = false;
+                    if (b_it < count) {
+                        const int it = b_it, steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32), zs = it % L::kZs, ys = it % L::kYs;
+                        if (b_step == 0) {
+                            if (ready(kFullZ + zs, it / L::kZs) && (it == 0 || ready(kUpdateRead, it - 1))) {
+                                tmem_after_sync();
+                                const uint32_t zo = operand(base + L::z + zs * kTile, kBlock), ident = operand(base + L::ident, 256);
+#pragma unroll
+                                for (int q = 0; q < 8; ++q)
+                                    if (q < steps) mma_ss<plain_layout(128)>(tmem + L::tz + 16 * q, zo + q * 128, ident, shape_t, false);
+                                mma_commit(bars + 8 * kTransposed);
+                                mma_commit(bars + 8 * (kFreeZ + zs));
+                                b_step = 1;
+                                moved = true;
+                            }
+                        } else if (ready(kWeighted, it) && ready(kFullY + ys, it / L::kYs)) {
+                            tmem_after_sync();
+                            const uint32_t yo = operand(base + L::y + ys * kTile, kBlock);
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                if (q < steps)
+#pragma unroll
+                                    for (int t = 0; t < L::kWeights; ++t)
+                                        mma_ts(tmem + L::weighted(q, t), yo + q * 128, shape_u, q + t > 0, tmem + L::tz);
+                            mma_commit(bars + 8 * kUpdate);
+                            mma_commit(bars + 8 * (kFreeY + ys));
+                            b_step = 0;
+                            ++b_it;
+                            moved = true;
+                        }
+                    }
+                    if (a_it < count) {
+                        const int it = a_it, xs = it % L::kXs, ys = it % L::kYs, zs = it % L::kZs;
+                        const uint32_t xo = operand(base + L::x + xs * kTile, kBlock);
+                        if (a_step == 0) {
+                            if (ready(kFullX + xs, it / L::kXs) && ready(kFullY + ys, it / L::kYs) && (it == 0 || ready(kStaged, it - 1))) {
+                                tmem_after_sync();
+                                const uint32_t yo = operand(base + L::y + ys * kTile, kBlock);
+#pragma unroll
+                                for (int kk = 0; kk < 8; ++kk)
+                                    if (kk < kx) mma_ss(tmem + L::to, xo + k_step(kk), yo + k_step(kk), shape_p, kk > 0);
+                                mma_commit(bars + 8 * kScores);
+                                mma_commit(bars + 8 * (kFreeY + ys));
+                                a_step = 1;
+                                moved = true;
+                            }
+                        } else if (a_step == 1) {
+                            if (ready(kProbs, it) && ready(kStateReady, it)) {
+                                tmem_after_sync();
+                                const uint32_t so = operand(base + L::s, kBlock);
+#pragma unroll
+                                for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+                                    for (int kk = 0; kk < 8; ++kk)
+                                        if (kk < kx)
+                                            mma_ss(tmem + L::to, xo + k_step(kk), so + t * (kTile >> 4) + k_step(kk), shape_f, t + kk > 0);
+                                mma_commit(bars + 8 * kFar);
+                                a_step = 2;
+                                moved = true;
+                            }
+                        } else if (ready(kFarRead, it) && ready(kFullZ + zs, it / L::kZs)) {
+                            tmem_after_sync();
+                            const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32);
+                            const uint32_t zo = operand(base + L::z + zs * kTile, kBlock);
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                if (q < steps)
+#pragma unroll
+                                    for (int t = 0; t < kTerms; ++t)
+                                        mma_ts(tmem + L::prob(q, t), zo + q * 128, shape_n, true, tmem + L::to);
+                            mma_commit(bars + 8 * kNear);
+                            mma_commit(bars + 8 * (kFreeZ + zs));
+                            a_step = 0;
+                            ++a_it;
+                            moved = true;
+                        }
+                    }
+                    idle = moved ? 0 : idle + 1;
+                    if (idle >= 16 * kSpin) *stop = 1 + kBars;
+                    if ((idle & 1023) == 1023 && *stop) break;
+                }
+                if (*stop) {
+                    mma_commit(bars + 8 * kDrain);
+                    for (uint32_t i = 0; i < kSpin / 16 && !bar_try(bars + 8 * kDrain, 0); ++i) {}
+                }
+            }
+            __syncwarp();
+        }
+    } else if (warp < 8) {
+        give_registers<kRowRegs>();
+        // ---------------------------------------------------------------- P and the output: two threads have one token's row
+        if (!kStateOnly) {
+            const int side = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+            const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
+            Out* go = static_cast<Out*>(p.out) + b * p.ob + h * p.oh;
+            const bool columns = 64 * side < p.dz;
+            bool ok = true;  // once a wait has given up, the rest runs on without waiting: its barriers need every thread
+            for (int it = 0; it < count; ++it) {
+                const int t0 = chunk_at(it) * kChunk, t = t0 + row;
+                const int batches = min(4, (live - t0 + 31) / 32);
+                ok = ok && wait(kDecays, it);
+                const float own_hi = c_hi[row], own_lo = c_lo[row];
+                const float far = p.scale * ex2(kRev ? (s_whole[1] - own_hi) + (s_whole[2] - own_lo) : own_hi + own_lo);
+                ok = ok && wait(kScores, it);
+                tmem_after_sync();
+#pragma unroll 1
+                for (int n = side; n < batches; n += 2) {  // a batch of 32 columns; the sides take turns
+                    if (kRev ? n < quarter : n > quarter) {
+                        const uint32_t zero[8] = {};
+#pragma unroll
+                        for (int i = 0; i < 2 * kTerms; ++i) tmem_st8(at + L::prob(2 * n, 0) + 8 * i, zero);
+                        continue;
+                    }
+                    const bool diagonal = n == quarter;
+                    // e^{c_i-c_j} = e^{c_i-c_m} e^{c_m-c_j} with m at the batch's edge between j and i: both exponents keep
+                    // their sign, and one exponential of the row serves the batch's columns
+                    const int m = kRev ? 32 * n : 32 * n + 31;
+                    const float f1 = p.scale * ex2(kRev ? (c_hi[m] - own_hi) + (c_lo[m] - own_lo) : (own_hi - c_hi[m]) + (own_lo - c_lo[m]));
+                    const pair f = make_pair2(f1, f1);
+#pragma unroll 1
+                    for (int q = 2 * n; q < 2 * n + 2; ++q) {
+                        uint32_t v[16], term[kTerms][8];
+                        tmem_ld16(v, at + L::to + 16 * q);
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) {
+                            pair w0, w1;
+                            if (!diagonal) {
+                                const float4 g = *reinterpret_cast<const float4*>(w_bt + 16 * q + j);
+                                w0 = mul2(f, make_pair2(g.x, g.y));
+                                w1 = mul2(f, make_pair2(g.z, g.w));
+                            } else {
+                                const float4 hi = *reinterpret_cast<const float4*>(c_hi + 16 * q + j);
+                                const float4 lo = *reinterpret_cast<const float4*>(c_lo + 16 * q + j);
+                                const int ahead = row - 16 * q - j;  // columns up to the diagonal
+                                auto weight = [&](int u, float h1, float l1) {
+                                    const float d = kRev ? (h1 - own_hi) + (l1 - own_lo) : (own_hi - h1) + (own_lo - l1);
+                                    return (kRev ? u >= ahead : u <= ahead) ? p.scale * ex2(d) : 0.0f;
+                                };
+                                w0 = make_pair2(weight(0, hi.x, lo.x), weight(1, hi.y, lo.y));
+                                w1 = make_pair2(weight(2, hi.z, lo.z), weight(3, hi.w, lo.w));
+                            }
+                            uint32_t s[kTerms];
+                            split<kTerms>(mul2(w0, make_pair2(v[j], v[j + 1])), s);
+#pragma unroll
+                            for (int i = 0; i < kTerms; ++i) term[i][j / 2] = s[i];
+                            split<kTerms>(mul2(w1, make_pair2(v[j + 2], v[j + 3])), s);
+#pragma unroll
+                            for (int i = 0; i < kTerms; ++i) term[i][j / 2 + 1] = s[i];
+                        }
+#pragma unroll
+                        for (int i = 0; i < kTerms; ++i) tmem_st8(at + L::prob(q, i), term[i]);
+                    }
+                }
+                bar_arrive(bars + 8 * kDecaysFree);
+                tmem_wait_st();
+                tmem_before_sync();
+                bar_arrive(bars + 8 * kProbs);
+                ok = ok && wait(kFar, it);
+                tmem_after_sync();
+                const int col0 = 64 * side, col1 = min(p.dz, col0 + 64);
+                const pair far2 = make_pair2(far, far);
+#pragma unroll 1
+                for (int col = col0; col < col1; col += 16) {  // X S with its row's weight, for P Z to be added to
+                    uint32_t v[16];
+                    tmem_ld16(v, at + L::to + col);
+#pragma unroll
+                    for (int u = 0; u < 16; u += 2) parts(mul2(far2, make_pair2(v[u], v[u + 1])), v[u], v[u + 1]);
+                    tmem_st16(at + L::to + col, v);
+                }
+                tmem_wait_st();
+                tmem_before_sync();
+                bar_arrive(bars + 8 * kFarRead);
+                ok = ok && wait(kNear, it);
+                tmem_after_sync();
+                uint8_t* const stage = sm8 + L::x + it % L::kXs * kTile + side * kBlock + row * 128;
+#pragma unroll 1
+                for (int col = col0; col < col1; col += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(v, at + L::to + col);
+                    if (t >= live)
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) v[u] = 0u;
+                    if constexpr (sizeof(Out) == 2) {
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+                            *reinterpret_cast<uint4*>(stage + ((((col - col0) / 8 + c) ^ (row & 7)) << 4)) =
+                                make_uint4(pack_bf16(make_pair2(v[8 * c], v[8 * c + 1])), pack_bf16(make_pair2(v[8 * c + 2], v[8 * c + 3])),
+                                           pack_bf16(make_pair2(v[8 * c + 4], v[8 * c + 5])), pack_bf16(make_pair2(v[8 * c + 6], v[8 * c + 7])));
+                    } else if (t < p.tokens) {
+                        float f[16];
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) f[u] = __uint_as_float(v[u]);
+                        store_row16(go + t * p.ot + col, f, p.dz - col);
+                    }
+                }
+                tmem_before_sync();
+                if (sizeof(Out) == 2) fence_smem_to_async();
+                bar_arrive(bars + 8 * kStaged);
+            }
+            // chunks without tokens
+            if (columns)
+                for (int c = max(chunks, segment * p.seg_chunks); c < (segment + 1) * p.seg_chunks; ++c) {
+                    const int t = c * kChunk + row;
+                    const float o[16] = {};
+                    for (int col = 64 * side; col < min(p.dz, 64 * side + 64) && t < p.tokens; col += 16) store_row16(go + t * p.ot + col, o, p.dz - col);
+                }
+        }
+    } else {
+        take_registers<kStateRegs>();
+        // ---------------------------------------------------------------- the state: two threads have one row of S^T
+        const int side = (warp - 8) >> 2, quarter = warp & 3, z = quarter * 32 + lane, k0 = 64 * side;
+        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
+        const bool columns = k0 < p.dx, mine = z < p.dz;
+        pair s[32];
+        const float* from = kStateOnly ? nullptr : p.segments > 1 ? p.seg_state + ((long long)bh * p.segments + segment) * p.dx * p.dz
+                                                 : p.s_in ? p.s_in + (long long)bh * p.dx * p.dz : nullptr;
+        const bool across = p.segments == 1 && p.s_in_t;
+        const float mul = p.segments == 1 ? p.s_in_mul : 1.0f;
+#pragma unroll
+        for (int k = 0; k < 64; k += 2) {  // dimensions are even: TMA could not load others
+            float s0 = 0.0f, s1 = 0.0f;
+            if (from && mine && k0 + k < p.dx) {
+                s0 = from[across ? z * p.dx + k0 + k : (k0 + k) * p.dz + z] * mul;
+                s1 = from[across ? z * p.dx + k0 + k + 1 : (k0 + k + 1) * p.dz + z] * mul;
+            }
+            s[k / 2] = make_pair2(s0, s1);
+        }
+        auto publish = [&]() {  // the state as the B operand of X S: row z, contiguous along k
+            if (columns) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t w[kTerms][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t t[kTerms];
+                        split<kTerms>(s[4 * c + j], t);
+#pragma unroll
+                        for (int i = 0; i < kTerms; ++i) w[i][j] = t[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < kTerms; ++i)
+                        *reinterpret_cast<uint4*>(sm8 + L::s + i * kTile + side * kBlock + z * 128 + ((c ^ (z & 7)) << 4)) =
+                            make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+                }
+                fence_smem_to_async();
+            }
+            bar_arrive(bars + 8 * kStateReady);
+        };
+        if (!kStateOnly && count > 0) publish();
+        bool ok = true;
+        for (int it = 0; it < count; ++it) {
+            const int t0 = chunk_at(it) * kChunk;
+            const int steps = 2 * min(4, (live - t0 + 31) / 32);
+            ok = ok && wait(kDecays, it);
+            const pair whole2 = make_pair2(s_whole[0], s_whole[0]);
+            ok = ok && wait(kTransposed, it);
+            tmem_after_sync();
+            uint32_t v[16];
+            if (4 * side < steps) tmem_ld16_early(v, at + L::tz + 64 * side);
+#pragma unroll 1
+            for (int q = 4 * side; q < min(steps, 4 * side + 4); ++q) {
+                uint32_t w[L::kWeights][8];
+                tmem_ready(v);
+#pragma unroll
+                for (int j = 0; j < 16; j += 4) {
+                    const float4 f = *reinterpret_cast<const float4*>(w_st + 16 * q + j);
+                    uint32_t t[L::kWeights];
+                    split<L::kWeights>(mul2(make_pair2(v[j], v[j + 1]), make_pair2(f.x, f.y)), t);
+#pragma unroll
+                    for (int i = 0; i < L::kWeights; ++i) w[i][j / 2] = t[i];
+                    split<L::kWeights>(mul2(make_pair2(v[j + 2], v[j + 3]), make_pair2(f.z, f.w)), t);
+#pragma unroll
+                    for (int i = 0; i < L::kWeights; ++i) w[i][j / 2 + 1] = t[i];
+                }
+                if (q + 1 < min(steps, 4 * side + 4)) tmem_ld16_early(v, at + L::tz + 16 * (q + 1));
+#pragma unroll
+                for (int i = 0; i < L::kWeights; ++i) tmem_st8(at + L::weighted(q, i), w[i]);
+            }
+            bar_arrive(bars + 8 * kDecaysFree);
+            tmem_wait_st();
+            tmem_before_sync();
+            bar_arrive(bars + 8 * kWeighted);
+            ok = ok && wait(kUpdate, it);
+            tmem_after_sync();
+            if (columns)
+#pragma unroll
+                for (int j = 0; j < 64; j += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(v, at + L::tz + k0 + j);
+#pragma unroll
+                    for (int u = 0; u < 16; u += 2) s[(j + u) / 2] = fma2(whole2, s[(j + u) / 2], make_pair2(v[u], v[u + 1]));
+                }
+            tmem_before_sync();
+            bar_arrive(bars + 8 * kUpdateRead);
+            if (!kStateOnly && it + 1 < count) {
+                ok = ok && wait(kFar, it);  // this chunk's X S has read the state it started from
+                publish();
+            }
+        }
+        float* to = kStateOnly ? p.seg_state + ((long long)bh * p.segments + segment) * p.dx * p.dz
+                               : p.s_out && segment == p.segments - 1 ? p.s_out + (long long)bh * p.dx * p.dz : nullptr;
+        const float out_mul = kStateOnly ? 1.0f : p.s_out_mul;
+#pragma unroll
+        for (int k = 0; k < 64; k += 2)
+            if (to && mine && k0 + k < p.dx) {
+                const bool turned = !kStateOnly && p.s_out_t;
+                float s0, s1;
+                parts(s[k / 2], s0, s1);
+                to[turned ? z * p.dx + k0 + k : (k0 + k) * p.dz + z] = s0 * out_mul;
+                to[turned ? z * p.dx + k0 + k + 1 : (k0 + k + 1) * p.dz + z] = s1 * out_mul;
+            }
+    }
+    tmem_before_sync();
+    __syncthreads();
+    if (warp == 16) tmem_free(tmem, 512);
+    if (tid == 0 && *stop) {
+        p.fault->error_code = 6;  // HS_ERR_COPY_TIMEOUT
+        p.fault->error_where = *stop;
+        __threadfence();
+        p.fault->error_id = p.call_id;
+    }
+}
+
+// What each segment starts from: the states that the segments would end at from zero (left by the state-only pass in
+// seg_state) joined in order.  A thread has one element; segments is small.
+__global__ void join_segments_kernel(const MmaPass p) {
+    const int plane = p.dx * p.dz, tiles = (plane + 255) / 256;
+    const int bh = blockIdx.x / tiles, e = blockIdx.x % tiles * 256 + threadIdx.x;
+    if (e >= plane) return;
+    const int k = e / p.dz, z = e % p.dz;
+    float cur = p.s_in ? p.s_in[(long long)bh * plane + (p.s_in_t ? z * p.dx + k : e)] * p.s_in_mul : 0.0f;
+    float* at = p.seg_state + (long long)bh * p.segments * plane + e;
+    for (int s = 0; s < p.segments; ++s) {
+        const float own = s + 1 < p.segments ? at[(long long)s * plane] : 0.0f;
+        at[(long long)s * plane] = cur;
+        if (s + 1 < p.segments) cur = fmaf(p.seg_decay[bh * p.segments + s], cur, own);
+    }
+}
+
+}  // namespace ha

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstring>
 
+#include "ha_mma.cuh"
 #include "ha_simt.cuh"
 #include "hs_internal.h"
 
@@ -74,6 +75,119 @@ Pass common(const heinsen_attention_problem* p) {
     return ps;
 }
 
+// ---- the tensor-core passes
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+    static EncodeFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<EncodeFn>(f);
+    }();
+    return fn;
+}
+
+struct View {  // one [batch, tokens, heads', dim] tensor of a pass
+    Rows rows;
+    int own_heads, dim;
+};
+
+// Can TMA address it?  16-byte base and strides; a stride of a dimension of one is never used.
+bool tma_fits(const View& v, long long batch, long long tokens) {
+    const long long s[3] = {v.own_heads > 1 ? v.rows.sh : 8, tokens > 1 ? v.rows.st : 8, batch > 1 ? v.rows.sb : 8};
+    for (long long x : s)
+        if (x <= 0 || x % 8 || x >= (1ll << 38)) return false;
+    return v.dim % 8 == 0 && v.dim <= 128 && (reinterpret_cast<uintptr_t>(v.rows.ptr) & 15u) == 0;
+}
+bool encode(CUtensorMap* m, const View& v, long long batch, long long tokens) {
+    const EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)v.dim, (cuuint64_t)v.own_heads, (cuuint64_t)tokens, (cuuint64_t)batch};
+    const cuuint64_t any = 256;
+    const cuuint64_t strides[3] = {v.own_heads > 1 ? (cuuint64_t)v.rows.sh * 2 : any, tokens > 1 ? (cuuint64_t)v.rows.st * 2 : any,
+                                   batch > 1 ? (cuuint64_t)v.rows.sb * 2 : any};
+    const cuuint32_t box[4] = {64, 1, (cuuint32_t)ha::kChunk, 1}, one[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(v.rows.ptr), dims, strides, box, one,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Segments of a sequence.  Fewer (batch, head) pairs than SMs leave the rest of the GPU idle, so sequences are cut until
+// there is about one segment for each SM; each keeps at least four chunks, since the cut reads keys and values twice.
+int segments_for(long long pairs, long long tokens, int sms) {
+    const long long chunks = (tokens + ha::kChunk - 1) / ha::kChunk;
+    if (pairs * 2 > sms) return 1;
+    return (int)std::max(1ll, std::min({sms / pairs, chunks / 4, 64ll}));
+}
+constexpr int kSms = 148;  // B200; sizes workspaces the same wherever they are asked for
+size_t segment_bytes(const heinsen_attention_problem* p) {
+    const long long pairs = p->batch * p->heads;
+    const int n = segments_for(pairs, p->tokens, kSms);
+    return n > 1 ? up256((size_t)pairs * n * p->k_dim * p->v_dim * 4) + up256((size_t)pairs * n * 4) : 0;
+}
+
+template <bool kRev, int kTerms, class Out, bool kStateOnly>
+hs_status mma_launch(const CUtensorMap& mx, const CUtensorMap& my, const CUtensorMap& mz, const CUtensorMap& mo,
+                     const ha::MmaPass& mp, long long pairs, cudaStream_t stream) {
+    const auto fn = ha::mma_pass_kernel<kRev, kTerms, Out, kStateOnly>;
+    const int smem = (int)ha::MmaLayout<kTerms>::end;
+    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
+    const long long grid = pairs * (kStateOnly ? mp.segments - 1 : mp.segments);
+    if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
+    fn<<<(unsigned)grid, ha::kMmaThreads, smem, stream>>>(mx, my, mz, mo, mp);
+    return launched("mma_pass_kernel");
+}
+
+// One pass, with its segments.  `ws`: workspace header, `space`: segment_bytes() of scratch.
+template <bool kRev, int kTerms, class Out>
+hs_status mma_pass(const Pass& ps, const View& x, const View& y, const View& z, const heinsen_attention_problem* p, uint8_t* ws,
+                   uint8_t* space, unsigned long long id, cudaStream_t stream) {
+    CUtensorMap mx, my, mz, mo;
+    const View o{{ps.out, ps.ob, ps.ot, ps.oh, 1}, ps.heads, ps.dz};
+    if (sizeof(Out) == 2 && !encode(&mo, o, ps.batch, ps.tokens))
+        return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
+    if (sizeof(Out) != 2) std::memset(&mo, 0, sizeof mo);  // not read
+    if (!encode(&mx, x, ps.batch, ps.tokens) || !encode(&my, y, ps.batch, ps.tokens) || !encode(&mz, z, ps.batch, ps.tokens))
+        return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
+    ha::MmaPass mp;
+    std::memset(&mp, 0, sizeof mp);
+    mp.log_a = ps.log_a; mp.ab = ps.ab; mp.at = ps.at; mp.ah = ps.ah; mp.lengths = ps.lengths;
+    mp.tokens = ps.tokens; mp.heads = ps.heads; mp.dx = ps.dx; mp.dz = ps.dz;
+    mp.xdiv = ps.x.div; mp.ydiv = ps.y.div; mp.zdiv = ps.z.div;
+    mp.scale = ps.scale;
+    mp.s_in = ps.s_in; mp.s_out = ps.s_out; mp.s_in_t = ps.s_in_t; mp.s_out_t = ps.s_out_t;
+    mp.s_in_mul = ps.s_in_mul; mp.s_out_mul = ps.s_out_mul;
+    mp.out = ps.out; mp.ob = ps.ob; mp.ot = ps.ot; mp.oh = ps.oh;
+    mp.fault = reinterpret_cast<ha::Fault*>(ws); mp.call_id = id;
+    const long long pairs = (long long)ps.batch * ps.heads, chunks = (ps.tokens + ha::kChunk - 1) / ha::kChunk;
+    mp.segments = segments_for(pairs, ps.tokens, kSms);
+    mp.seg_chunks = (int)((chunks + mp.segments - 1) / mp.segments);
+    if (mp.segments > 1) {
+        mp.seg_state = reinterpret_cast<float*>(space);
+        mp.seg_decay = reinterpret_cast<float*>(space + up256((size_t)pairs * mp.segments * ps.dx * ps.dz * 4));
+        hs_status st = mma_launch<kRev, 1, __nv_bfloat16, true>(mx, my, mz, mo, mp, pairs, stream);
+        if (st != HS_OK) return st;
+        ha::join_segments_kernel<<<(unsigned)(pairs * ((ps.dx * ps.dz + 255) / 256)), 256, 0, stream>>>(mp);
+        if ((st = launched("join_segments_kernel")) != HS_OK) return st;
+    }
+    return mma_launch<kRev, kTerms, Out, false>(mx, my, mz, mo, mp, pairs, stream);
+}
+
+// The rule for the tensor cores: bf16, head dimensions that TMA can load (multiples of 8, at most 128, 16-byte strides).
+bool mma_fits(const heinsen_attention_problem* p, const heinsen_attention_tensor* o) {
+    if (p->dtype != HS_BF16 || p->tokens == 0) return false;
+    if (!tma_fits({rows_of(p->q, p->heads, p->q_heads), p->q_heads, p->k_dim}, p->batch, p->tokens) ||
+        !tma_fits({rows_of(p->k, p->heads, p->k_heads), p->k_heads, p->k_dim}, p->batch, p->tokens) ||
+        !tma_fits({rows_of(p->v, p->heads, p->v_heads), p->v_heads, p->v_dim}, p->batch, p->tokens))
+        return false;
+    return tma_fits({rows_of(*o, p->heads, p->heads), p->heads, p->v_dim}, p->batch, p->tokens);
+}
+
 // Workspace of a backward pass: header | dq, dk, dv for each head, float32 | the states before every chunk and the gradients
 // of the states behind it | sums of the decay gradients.
 struct BackwardSpace {
@@ -94,7 +208,8 @@ BackwardSpace backward_space(const heinsen_attention_problem* p) {
 }
 
 template <class T>
-hs_status forward_pass(const heinsen_attention_problem* p, const heinsen_attention_tensor* o, float* state, cudaStream_t stream) {
+hs_status forward_pass(const heinsen_attention_problem* p, const heinsen_attention_tensor* o, float* state, uint8_t* ws,
+                       cudaStream_t stream) {
     Pass ps = common(p);
     ps.x = rows_of(p->q, p->heads, p->q_heads);
     ps.y = rows_of(p->k, p->heads, p->k_heads);
@@ -102,6 +217,9 @@ hs_status forward_pass(const heinsen_attention_problem* p, const heinsen_attenti
     ps.dx = p->k_dim; ps.dz = p->v_dim;
     ps.s_in = p->state0; ps.s_out = state;
     ps.out = const_cast<void*>(o->ptr); ps.ob = o->batch_stride; ps.ot = o->token_stride; ps.oh = o->head_stride;
+    if (mma_fits(p, o))
+        return mma_pass<false, 1, __nv_bfloat16>(ps, {ps.x, p->q_heads, p->k_dim}, {ps.y, p->k_heads, p->k_dim},
+                                                 {ps.z, p->v_heads, p->v_dim}, p, ws, ws + kHeaderBytes, hs_internal::call_id(), stream);
     return simt_pass<T, false, T>(ps, stream);
 }
 
@@ -209,8 +327,8 @@ extern "C" {
 
 size_t heinsen_attention_workspace_bytes(const heinsen_attention_problem* p, int backward) {
     if (validate(p) != HS_OK) return 0;
-    if (!backward || nothing(p)) return kHeaderBytes;
-    return backward_space(p).total;
+    if (nothing(p)) return kHeaderBytes;
+    return backward ? backward_space(p).total : kHeaderBytes + segment_bytes(p);
 }
 
 hs_status heinsen_attention_forward(const heinsen_attention_problem* p, const heinsen_attention_tensor* o, float* state,
@@ -222,8 +340,9 @@ hs_status heinsen_attention_forward(const heinsen_attention_problem* p, const he
     if ((st = check_space(p, 0, workspace, workspace_bytes)) != HS_OK) return st;
     int sms;
     if ((st = hs_internal::current_device(&sms)) != HS_OK) return st;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return p->dtype == HS_F32 ? forward_pass<float>(p, o, state, s) : forward_pass<__nv_bfloat16>(p, o, state, s);
+    return p->dtype == HS_F32 ? forward_pass<float>(p, o, state, ws, s) : forward_pass<__nv_bfloat16>(p, o, state, ws, s);
 }
 
 hs_status heinsen_attention_backward(const heinsen_attention_problem* p, const heinsen_attention_tensor* d_o,
