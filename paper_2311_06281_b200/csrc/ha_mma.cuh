@@ -11,8 +11,10 @@
 // products.
 //
 // Rounding.  A float32 factor enters a product as bf16 terms: w Z (and so the state, which is float32 to its owner) as three,
-// 24 bits, exact to float32's own rounding; P and the state in X S as kTerms: one where only the bf16 output depends on
-// it (its own rounding is as large), two where the decay gradients do, and then two for w Z as well.
+// 24 bits, exact to float32's own rounding; P and the state in X S as one, where only the bf16 output depends on them (its own
+// rounding is as large), and as three where the decay gradients do (kDots): they are float32, and sums over many tokens of
+// dots that cancel in part, to which two terms (17 bits) would leave errors of 2e-5 and more.  Tensor memory then holds two
+// terms at a time; the third is kept in registers and follows when the first two have been used.
 #pragma once
 #include <cuda.h>
 
@@ -23,12 +25,15 @@ namespace ha {
 
 constexpr int kChunk = 128;
 constexpr int kMmaThreads = 640;
-// Registers of a thread: 96 at launch (65536 over 20 warps); those that the feeding warps and the rows of out can spare go to
-// the rows of the state.  64 + 2 * 80 + 2 * 128 = 480 for a thread of each warpgroup, 5 * 96 as at launch.
-constexpr int kRowRegs = 80, kStateRegs = 128, kFeedRegs = 64;
+// Registers of a thread: 96 at launch (65536 over 20 warps).  What the feeding warps can spare goes to the rows of the state,
+// and to those of out where they hold two more rows for the decay gradients: 64 + 2 * 80 + 2 * 128 = 64 + 2 * 88 + 2 * 120 =
+// 480 for a thread of each warpgroup, 5 * 96 as at launch.
+constexpr int kFeedRegs = 64;
+template <bool kDots> constexpr int kRowRegs = kDots ? 88 : 80;
+template <bool kDots> constexpr int kStateRegs = kDots ? 120 : 128;
 constexpr uint32_t kTile = 128 * 256;        // 128 rows of 128 bf16: two blocks of 64 columns, 128-byte swizzle
 constexpr uint32_t kBlock = kTile / 2;
-constexpr uint32_t kSpin = 1u << 21;         // polls of a barrier before a wait gives up
+constexpr uint32_t kSpin = 1u << 20;         // polls of a barrier before a wait gives up (about a microsecond each)
 
 struct Fault {  // the header that heinsen_scan_check() reads
     unsigned long long started_id, error_id;
@@ -49,35 +54,52 @@ struct MmaPass {
     void* out;
     long long ob, ot, oh;
     // A sequence cut into segments: each starts from seg_state[bh][segment] ([dx, dz], formed by two kernels before this one)
-    int segments, seg_chunks;
+    int segments, seg_chunks, chunks;
     float* seg_state;
     float* seg_decay;
+    // For the decay gradients (kDots): w_i . out_i of every token without the token's own term, and of its X S part
+    // alone (reversed pass), by halves of the columns: [2][batch * heads][tokens].  The forward pass leaves the state before
+    // every chunk in `dump`, the reversed one multiplies it with its own: cross[batch * heads][chunks][8], a warp each.
+    Rows w;
+    float *dots, *dots_far;
+    float4* dump;
+    float* cross;
     Fault* fault;
     unsigned long long call_id;
 };
 
-template <int kTerms>
+// A chunk whose decay is below 2^-60 passes nothing on from before it that float32 could see beside what is in it.
+constexpr float kNothingCrosses = -60.0f;
+
+template <bool kDots>
 struct MmaLayout {
-    static constexpr int kXs = 2, kYs = 2, kZs = kTerms == 1 ? 2 : 1;  // stages; a chunk's X tile also stages its output
+    static constexpr int kTerms = kDots ? 3 : 1;               // of P and of the state in X S
+    static constexpr int kAtOnce = kDots ? 2 : 1;              // terms of P in the first product
+    static constexpr int kWeightsAtOnce = kDots ? 2 : 3;       // terms of w Z in the first product
+    // Stages.  A chunk's output leaves from its X tile, where X has two, else from its Y tile.
+    static constexpr int kXs = kDots ? 1 : 2, kYs = 2, kZs = kDots ? 1 : 2;
     static constexpr uint32_t x = 0, y = x + kXs * kTile, z = y + kYs * kTile, s = z + kZs * kTile, ident = s + kTerms * kTile,
-                              decays = ident + 512, whole = decays + 4 * kChunk * 4, bars = whole + 32, end = bars + 8 * 32;
+                              decays = ident + 512, whole = decays + 4 * kChunk * 4, bars = whole + 32, end = bars + 8 * 34;
     // Tensor memory columns, all 512.  What is read out before the next product of its chain is due shares columns with it:
     // Z^T with the state's update, the scores with the output.
-    static constexpr int kWeights = kTerms == 1 ? 3 : 2;       // terms of w Z
     static constexpr uint32_t tw = 0;                          // the terms of (w Z)^T: A operand
-    static constexpr uint32_t tz = tw + 64 * kWeights;         // Z^T, then the state's update
+    static constexpr uint32_t tz = tw + 64 * kWeightsAtOnce;   // Z^T, then the state's update
     static constexpr uint32_t to = tz + 128;                   // X Y^T, then X S, then P Z
     static constexpr uint32_t tp = to + 128;                   // the terms of P: A operand
-    static_assert(tp + 64 * kTerms == 512, "tensor memory");
+    static_assert(tp + 64 * kAtOnce == 512, "tensor memory");
+    static __device__ __forceinline__ uint32_t staged(uint32_t base, int it) {
+        return base + (kDots ? y + it % kYs * kTile : x + it % kXs * kTile);
+    }
     // where term t of 16 tokens q lies
-    static __device__ __forceinline__ constexpr uint32_t prob(int q, int t) { return tp + 8 * kTerms * q + 8 * t; }
-    static __device__ __forceinline__ constexpr uint32_t weighted(int q, int t) { return tw + 8 * kWeights * q + 8 * t; }
+    static __device__ __forceinline__ constexpr uint32_t prob(int q, int t) { return tp + 8 * kAtOnce * q + 8 * t; }
+    static __device__ __forceinline__ constexpr uint32_t weighted(int q, int t) { return tw + 8 * kWeightsAtOnce * q + 8 * t; }
 };
 
 // Every barrier completes one phase per chunk (those with two entries: per chunk that uses the entry), and nobody who waits
 // for a phase can be overtaken by the next: it needs something of the waiter's own.
 enum Bar : int { kFullX = 0, kFullY = 2, kFullZ = 4, kFreeX = 6, kFreeY = 8, kFreeZ = 10, kPatchY = 12, kPatchZ, kDecays, kDecaysFree, kScores,
-                 kTransposed, kProbs, kFar, kFarRead, kNear, kStaged, kWeighted, kUpdate, kUpdateRead, kStateReady, kDrain,
+                 kTransposed, kProbs, kFar, kFarRead, kNear, kStaged, kWeighted, kWeightedLast, kUpdateFirst,
+                 kUpdate, kUpdateRead, kStateReady, kNearFirst, kProbsLast, kYDone, kDrain = kYDone + 2,
                  kBars };
 
 struct Waiter {
@@ -105,6 +127,20 @@ __device__ __forceinline__ void split(pair v, uint32_t (&t)[kTerms]) {
     }
 }
 
+// sum + the products of sixteen float32 values and sixteen bf16
+__device__ __forceinline__ pair add_dot(pair sum, const uint32_t (&v)[16], const uint4& lo, const uint4& hi) {
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum = fma2(make_pair2(w[i] << 16, w[i] & 0xffff0000u), make_pair2(v[2 * i], v[2 * i + 1]), sum);
+    return sum;
+}
+__device__ __forceinline__ void add_scaled(uint32_t (&v)[16], float f, const uint4& lo, const uint4& hi) {
+    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        parts(fma2(make_pair2(w[i] << 16, w[i] & 0xffff0000u), make_pair2(f, f), make_pair2(v[2 * i], v[2 * i + 1])), v[2 * i], v[2 * i + 1]);
+}
+
 // Sixteen columns of one row, or the n that are left of it
 __device__ __forceinline__ void store_row16(float* to, const float (&v)[16], int n) {
 #pragma unroll
@@ -119,11 +155,14 @@ __device__ __forceinline__ void store_row16(__nv_bfloat16* to, const float (&v)[
                 make_uint4(pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3]), pack_bf16(v[i + 4], v[i + 5]), pack_bf16(v[i + 6], v[i + 7]));
 }
 
-template <bool kRev, int kTerms, class Out, bool kStateOnly>
+template <bool kRev, bool kDots, class Out, bool kStateOnly>
 __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap my,
                                                                   const __grid_constant__ CUtensorMap mz, const __grid_constant__ CUtensorMap mo,
                                                                   const MmaPass p) {
-    using L = MmaLayout<kTerms>;
+    using L = MmaLayout<kDots>;
+    // a group that asks for more than the others gave up would wait for ever
+    static_assert(kFeedRegs + 2 * kRowRegs<kDots> + 2 * kStateRegs<kDots> <= 5 * 96 && kRowRegs<kDots> <= 96, "registers");
+    constexpr int kTerms = L::kTerms;
     extern __shared__ __align__(1024) uint8_t sm8[];
     const uint32_t base = smem_addr(sm8);
     float* const c_hi = reinterpret_cast<float*>(sm8 + L::decays);
@@ -147,10 +186,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i) {
             uint32_t arrivals = 1;
-            if (i >= kFreeY && i < kPatchY) arrivals = kStateOnly ? 1 : 2;
+            if (i >= kFreeY && i < kPatchY) arrivals = kStateOnly ? 1 : kDots && i < kFreeZ ? 3 : 2;
             if (i == kDecays) arrivals = 32;
             if (i == kDecaysFree) arrivals = kStateOnly ? 256 : 512;
-            if (i == kProbs || i == kFarRead || i == kStaged || i == kWeighted || i == kUpdateRead || i == kStateReady) arrivals = 256;
+            if (i == kProbs || i == kFarRead || i == kStaged || i == kWeighted || i == kWeightedLast || i == kProbsLast || i == kUpdateRead || i == kStateReady) arrivals = 256;
             bar_init(bars + 8 * i, arrivals);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -283,19 +322,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             }
             if (kStateOnly && lane == 0) p.seg_decay[bh * p.segments + segment] = ex2((float)total);
         } else if (warp == kStorer) {
-            // ------------------------------------------------------------ the output leaves by TMA from the chunk's X tile
+            // ------------------------------------------------------------ the output leaves by TMA
             if (!kStateOnly && lane == 0) {
                 bool ok = true;
                 for (int it = 0; it < count && ok; ++it) {
                     if (!(ok = wait(kStaged, it))) break;
                     if constexpr (sizeof(Out) == 2) {
-                        const uint32_t from = base + L::x + it % L::kXs * kTile;
+                        const uint32_t from = L::staged(base, it);
                         tma_store_4d(&mo, 0, h, chunk_at(it) * kChunk, b, from);
                         if (p.dz > 64) tma_store_4d(&mo, 64, h, chunk_at(it) * kChunk, b, from + kBlock);
                         tma_store_commit();
                         tma_store_wait_read();
                     }
-                    bar_arrive(bars + 8 * (kFreeX + it % L::kXs));
+                    bar_arrive(bars + 8 * (kDots ? kFreeY + it % L::kYs : kFreeX + it % L::kXs));
                 }
                 tma_store_wait_all();
             }
@@ -330,19 +369,31 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                                 b_step = 1;
                                 moved = true;
                             }
-                        } else if (ready(kWeighted, it) && ready(kFullY + ys, it / L::kYs)) {
+                        } else if (b_step == 1 ? ready(kWeighted, it) && ready(kFullY + ys, it / L::kYs) : ready(kWeightedLast, it)) {
                             tmem_after_sync();
                             const uint32_t yo = operand(base + L::y + ys * kTile, kBlock);
+                            if (L::kWeightsAtOnce == 3 || b_step == 1) {
 #pragma unroll
-                            for (int q = 0; q < 8; ++q)
-                                if (q < steps)
+                                for (int q = 0; q < 8; ++q)
+                                    if (q < steps)
 #pragma unroll
-                                    for (int t = 0; t < L::kWeights; ++t)
-                                        mma_ts(tmem + L::weighted(q, t), yo + q * 128, shape_u, q + t > 0, tmem + L::tz);
-                            mma_commit(bars + 8 * kUpdate);
-                            mma_commit(bars + 8 * (kFreeY + ys));
-                            b_step = 0;
-                            ++b_it;
+                                        for (int t = 0; t < L::kWeightsAtOnce; ++t)
+                                            mma_ts(tmem + L::weighted(q, t), yo + q * 128, shape_u, q + t > 0, tmem + L::tz);
+                            } else {
+#pragma unroll
+                                for (int q = 0; q < 8; ++q)
+                                    if (q < steps) mma_ts(tmem + L::weighted(q, 0), yo + q * 128, shape_u, true, tmem + L::tz);
+                            }
+                            if (L::kWeightsAtOnce == 2 && b_step == 1) {
+                                mma_commit(bars + 8 * kUpdateFirst);
+                                b_step = 2;
+                            } else {
+                                mma_commit(bars + 8 * kUpdate);
+                                mma_commit(bars + 8 * (kFreeY + ys));
+                                if (kDots) mma_commit(bars + 8 * (kYDone + ys));
+                                b_step = 0;
+                                ++b_it;
+                            }
                             moved = true;
                         }
                     }
@@ -372,23 +423,35 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                                         if (kk < kx)
                                             mma_ss(tmem + L::to, xo + k_step(kk), so + t * (kTile >> 4) + k_step(kk), shape_f, t + kk > 0);
                                 mma_commit(bars + 8 * kFar);
+                                if (kDots) mma_commit(bars + 8 * (kFreeX + xs));
                                 a_step = 2;
                                 moved = true;
                             }
-                        } else if (ready(kFarRead, it) && ready(kFullZ + zs, it / L::kZs)) {
+                        } else if (a_step == 2 ? ready(kFarRead, it) && ready(kFullZ + zs, it / L::kZs) : ready(kProbsLast, it)) {
                             tmem_after_sync();
                             const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32);
                             const uint32_t zo = operand(base + L::z + zs * kTile, kBlock);
+                            if (!kDots || a_step == 2) {
 #pragma unroll
-                            for (int q = 0; q < 8; ++q)
-                                if (q < steps)
+                                for (int q = 0; q < 8; ++q)
+                                    if (q < steps)
 #pragma unroll
-                                    for (int t = 0; t < kTerms; ++t)
-                                        mma_ts(tmem + L::prob(q, t), zo + q * 128, shape_n, true, tmem + L::to);
-                            mma_commit(bars + 8 * kNear);
-                            mma_commit(bars + 8 * (kFreeZ + zs));
-                            a_step = 0;
-                            ++a_it;
+                                        for (int t = 0; t < L::kAtOnce; ++t)
+                                            mma_ts(tmem + L::prob(q, t), zo + q * 128, shape_n, true, tmem + L::to);
+                            } else {
+#pragma unroll
+                                for (int q = 0; q < 8; ++q)
+                                    if (q < steps) mma_ts(tmem + L::prob(q, 0), zo + q * 128, shape_n, true, tmem + L::to);
+                            }
+                            if (kDots && a_step == 2) {
+                                mma_commit(bars + 8 * kNearFirst);
+                                a_step = 3;
+                            } else {
+                                mma_commit(bars + 8 * kNear);
+                                mma_commit(bars + 8 * (kFreeZ + zs));
+                                a_step = 0;
+                                ++a_it;
+                            }
                             moved = true;
                         }
                     }
@@ -404,7 +467,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             __syncwarp();
         }
     } else if (warp < 8) {
-        give_registers<kRowRegs>();
+        give_registers<kRowRegs<kDots>>();
         // ---------------------------------------------------------------- P and the output: two threads have one token's row
         if (!kStateOnly) {
             const int side = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
@@ -416,84 +479,151 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 const int t0 = chunk_at(it) * kChunk, t = t0 + row;
                 const int batches = min(4, (live - t0 + 31) / 32);
                 ok = ok && wait(kDecays, it);
-                const float own_hi = c_hi[row], own_lo = c_lo[row];
-                const float far = p.scale * ex2(kRev ? (s_whole[1] - own_hi) + (s_whole[2] - own_lo) : own_hi + own_lo);
+                const float own_hi = read1(c_hi + row), own_lo = read1(c_lo + row);
+                float own = 0.0f;  // P_ii, where it is kept out of the product
+                const float far = p.scale * ex2(kRev ? (read1(s_whole + 1) - own_hi) + (read1(s_whole + 2) - own_lo) : own_hi + own_lo);
                 ok = ok && wait(kScores, it);
                 tmem_after_sync();
-#pragma unroll 1
-                for (int n = side; n < batches; n += 2) {  // a batch of 32 columns; the sides take turns
+                uint32_t last[2][2][8] = {};  // third terms: they wait for the first two
+#pragma unroll kDots ? 2 : 1
+                for (int i = 0; i < 2; ++i) {  // a batch of 32 columns; the sides take turns
+                    const int n = side + 2 * i;
+                    if (n >= batches) break;
                     if (kRev ? n < quarter : n > quarter) {
                         const uint32_t zero[8] = {};
 #pragma unroll
-                        for (int i = 0; i < 2 * kTerms; ++i) tmem_st8(at + L::prob(2 * n, 0) + 8 * i, zero);
+                        for (int i = 0; i < 2 * L::kAtOnce; ++i) tmem_st8(at + L::prob(2 * n, 0) + 8 * i, zero);
                         continue;
                     }
                     const bool diagonal = n == quarter;
                     // e^{c_i-c_j} = e^{c_i-c_m} e^{c_m-c_j} with m at the batch's edge between j and i: both exponents keep
                     // their sign, and one exponential of the row serves the batch's columns
                     const int m = kRev ? 32 * n : 32 * n + 31;
-                    const float f1 = p.scale * ex2(kRev ? (c_hi[m] - own_hi) + (c_lo[m] - own_lo) : (own_hi - c_hi[m]) + (own_lo - c_lo[m]));
+                    const float f1 = p.scale * ex2((kRev ? 1.0f : -1.0f) * ((read1(c_hi + m) - own_hi) + (read1(c_lo + m) - own_lo)));
                     const pair f = make_pair2(f1, f1);
-#pragma unroll 1
-                    for (int q = 2 * n; q < 2 * n + 2; ++q) {
+#pragma unroll kDots ? 2 : 1
+                    for (int e = 0; e < 2; ++e) {
+                        const int q = 2 * n + e;
                         uint32_t v[16], term[kTerms][8];
                         tmem_ld16(v, at + L::to + 16 * q);
 #pragma unroll
                         for (int j = 0; j < 16; j += 4) {
                             pair w0, w1;
                             if (!diagonal) {
-                                const float4 g = *reinterpret_cast<const float4*>(w_bt + 16 * q + j);
+                                const float4 g = read4(w_bt + 16 * q + j);
                                 w0 = mul2(f, make_pair2(g.x, g.y));
                                 w1 = mul2(f, make_pair2(g.z, g.w));
                             } else {
-                                const float4 hi = *reinterpret_cast<const float4*>(c_hi + 16 * q + j);
-                                const float4 lo = *reinterpret_cast<const float4*>(c_lo + 16 * q + j);
+                                const float4 hi = read4(c_hi + 16 * q + j);
+                                const float4 lo = read4(c_lo + 16 * q + j);
                                 const int ahead = row - 16 * q - j;  // columns up to the diagonal
                                 auto weight = [&](int u, float h1, float l1) {
                                     const float d = kRev ? (h1 - own_hi) + (l1 - own_lo) : (own_hi - h1) + (own_lo - l1);
-                                    return (kRev ? u >= ahead : u <= ahead) ? p.scale * ex2(d) : 0.0f;
+                                    return (kDots ? (kRev ? u > ahead : u < ahead) : (kRev ? u >= ahead : u <= ahead)) ? p.scale * ex2(d) : 0.0f;
                                 };
+                                if (kDots) {
+#pragma unroll
+                                    for (int u = 0; u < 4; ++u)
+                                        if (u == ahead) own = p.scale * __uint_as_float(v[j + u]);
+                                }
                                 w0 = make_pair2(weight(0, hi.x, lo.x), weight(1, hi.y, lo.y));
                                 w1 = make_pair2(weight(2, hi.z, lo.z), weight(3, hi.w, lo.w));
                             }
                             uint32_t s[kTerms];
                             split<kTerms>(mul2(w0, make_pair2(v[j], v[j + 1])), s);
 #pragma unroll
-                            for (int i = 0; i < kTerms; ++i) term[i][j / 2] = s[i];
+                            for (int u = 0; u < kTerms; ++u) term[u][j / 2] = s[u];
                             split<kTerms>(mul2(w1, make_pair2(v[j + 2], v[j + 3])), s);
 #pragma unroll
-                            for (int i = 0; i < kTerms; ++i) term[i][j / 2 + 1] = s[i];
+                            for (int u = 0; u < kTerms; ++u) term[u][j / 2 + 1] = s[u];
                         }
 #pragma unroll
-                        for (int i = 0; i < kTerms; ++i) tmem_st8(at + L::prob(q, i), term[i]);
+                        for (int u = 0; u < L::kAtOnce; ++u) tmem_st8(at + L::prob(q, u), term[u]);
+                        if constexpr (kDots)
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) last[i][e][u] = term[2][u];
                     }
                 }
+                release_reads();
                 bar_arrive(bars + 8 * kDecaysFree);
+                if (kDots && (quarter & 1) != side && quarter < batches) {  // the other side had the diagonal
+#pragma unroll 1
+                    for (int q = 2 * quarter; q < 2 * quarter + 2; ++q) {
+                        uint32_t v[16];
+                        tmem_ld16(v, at + L::to + 16 * q);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (16 * q + j == row) own = p.scale * __uint_as_float(v[j]);
+                    }
+                }
+                const int col0 = 64 * side, col1 = min(p.dz, col0 + 64);
+                auto own_row = [&](uint4 (&w4)[8]) {  // the row's own w, 8 columns each
+                    const __nv_bfloat16* gw = static_cast<const __nv_bfloat16*>(p.w.ptr) + b * p.w.sb + (h / p.w.div) * p.w.sh + t * p.w.st + col0;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        w4[c] = make_uint4(0, 0, 0, 0);
+                        if (t < live && col0 + 8 * c < p.dz) w4[c] = *reinterpret_cast<const uint4*>(gw + 8 * c);
+                    }
+                };
+                uint4 w4[8];
+                if (kDots && kRev) own_row(w4);
                 tmem_wait_st();
                 tmem_before_sync();
                 bar_arrive(bars + 8 * kProbs);
                 ok = ok && wait(kFar, it);
                 tmem_after_sync();
-                const int col0 = 64 * side, col1 = min(p.dz, col0 + 64);
                 const pair far2 = make_pair2(far, far);
-#pragma unroll 1
-                for (int col = col0; col < col1; col += 16) {  // X S with its row's weight, for P Z to be added to
+                pair dot = 0, dot_far = 0;
+#pragma unroll kDots ? 4 : 1
+                for (int c = 0; c < 4; ++c) {  // X S with its row's weight, for P Z to be added to
+                    const int col = col0 + 16 * c;
+                    if (col >= col1) break;
                     uint32_t v[16];
                     tmem_ld16(v, at + L::to + col);
 #pragma unroll
                     for (int u = 0; u < 16; u += 2) parts(mul2(far2, make_pair2(v[u], v[u + 1])), v[u], v[u + 1]);
+                    if constexpr (kDots && kRev) dot_far = add_dot(dot_far, v, w4[2 * c], w4[2 * c + 1]);
                     tmem_st16(at + L::to + col, v);
                 }
                 tmem_wait_st();
                 tmem_before_sync();
                 bar_arrive(bars + 8 * kFarRead);
+                uint4 z4[8];  // the row's own z, for its own term
+                if constexpr (kDots) {
+                    ok = ok && wait(kNearFirst, it);
+                    tmem_after_sync();
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (side + 2 * i < batches) tmem_st8(at + L::prob(2 * (side + 2 * i) + e, 0), last[i][e]);
+                    ok = ok && wait(kFullZ + it % L::kZs, it / L::kZs);
+                    const uint8_t* zt = sm8 + L::z + it % L::kZs * kTile + side * kBlock + row * 128;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        z4[c] = make_uint4(0, 0, 0, 0);
+                        if (col0 + 8 * c < p.dz) z4[c] = read4(zt + ((c ^ (row & 7)) << 4));
+                    }
+                    tmem_wait_st();
+                    tmem_before_sync();
+                    release_reads();
+                    bar_arrive(bars + 8 * kProbsLast);
+                    own_row(w4);
+                }
                 ok = ok && wait(kNear, it);
                 tmem_after_sync();
-                uint8_t* const stage = sm8 + L::x + it % L::kXs * kTile + side * kBlock + row * 128;
-#pragma unroll 1
-                for (int col = col0; col < col1; col += 16) {
+                uint8_t* const stage = sm8 + L::staged(0, it) + side * kBlock + row * 128;
+                if (kDots) ok = ok && wait(kYDone + it % L::kYs, it / L::kYs);  // the tile has been read (the scores were before)
+#pragma unroll kDots ? 4 : 1
+                for (int n = 0; n < 4; ++n) {
+                    const int col = col0 + 16 * n;
+                    if (col >= col1) break;
                     uint32_t v[16];
                     tmem_ld16(v, at + L::to + col);
+                    if constexpr (kDots) {
+                        dot = add_dot(dot, v, w4[2 * n], w4[2 * n + 1]);
+                        add_scaled(v, own, z4[2 * n], z4[2 * n + 1]);
+                    }
                     if (t >= live)
 #pragma unroll
                         for (int u = 0; u < 16; ++u) v[u] = 0u;
@@ -513,6 +643,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 tmem_before_sync();
                 if (sizeof(Out) == 2) fence_smem_to_async();
                 bar_arrive(bars + 8 * kStaged);
+                if constexpr (kDots) {
+                    const long long to = ((long long)side * gridDim.x / p.segments + bh) * p.tokens + t;
+                    float d0, d1;
+                    if (t < live) {
+                        parts(dot, d0, d1);
+                        p.dots[to] = columns ? d0 + d1 : 0.0f;
+                        if (kRev) {
+                            parts(dot_far, d0, d1);
+                            p.dots_far[to] = columns ? d0 + d1 : 0.0f;
+                        }
+                    }
+                }
             }
             // chunks without tokens
             if (columns)
@@ -523,7 +665,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 }
         }
     } else {
-        take_registers<kStateRegs>();
+        take_registers<kStateRegs<kDots>>();
         // ---------------------------------------------------------------- the state: two threads have one row of S^T
         const int side = (warp - 8) >> 2, quarter = warp & 3, z = quarter * 32 + lane, k0 = 64 * side;
         const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
@@ -569,39 +711,93 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             const int t0 = chunk_at(it) * kChunk;
             const int steps = 2 * min(4, (live - t0 + 31) / 32);
             ok = ok && wait(kDecays, it);
-            const pair whole2 = make_pair2(s_whole[0], s_whole[0]);
+            const float whole = read1(s_whole);
+            const pair whole2 = make_pair2(whole, whole);
+            const bool crosses = read1(s_whole + 1) > kNothingCrosses;
+            if constexpr (kDots && !kRev) {
+                if (crosses && columns && mine) {
+                    float4* to = p.dump + ((long long)bh * p.chunks + t0 / kChunk) * 4096 + side * 2048 + z;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float4 f;
+                        parts(s[2 * j], f.x, f.y);
+                        parts(s[2 * j + 1], f.z, f.w);
+                        to[j * 128] = f;
+                    }
+                }
+            }
             ok = ok && wait(kTransposed, it);
             tmem_after_sync();
             uint32_t v[16];
-            if (4 * side < steps) tmem_ld16_early(v, at + L::tz + 64 * side);
-#pragma unroll 1
-            for (int q = 4 * side; q < min(steps, 4 * side + 4); ++q) {
-                uint32_t w[L::kWeights][8];
+            uint32_t last[L::kWeightsAtOnce == 2 ? 4 : 1][8];  // third terms, where they have to wait
+            const int q0 = 4 * side, q1 = min(steps, q0 + 4);
+            if (q0 < q1) tmem_ld16_early(v, at + L::tz + 16 * q0);
+#pragma unroll L::kWeightsAtOnce == 2 ? 4 : 1
+            for (int i = 0; i < 4; ++i) {
+                const int q = q0 + i;
+                if (q >= q1) break;
+                uint32_t w[3][8];
                 tmem_ready(v);
 #pragma unroll
                 for (int j = 0; j < 16; j += 4) {
-                    const float4 f = *reinterpret_cast<const float4*>(w_st + 16 * q + j);
-                    uint32_t t[L::kWeights];
-                    split<L::kWeights>(mul2(make_pair2(v[j], v[j + 1]), make_pair2(f.x, f.y)), t);
+                    const float4 f = read4(w_st + 16 * q + j);
+                    uint32_t t[3];
+                    split<3>(mul2(make_pair2(v[j], v[j + 1]), make_pair2(f.x, f.y)), t);
 #pragma unroll
-                    for (int i = 0; i < L::kWeights; ++i) w[i][j / 2] = t[i];
-                    split<L::kWeights>(mul2(make_pair2(v[j + 2], v[j + 3]), make_pair2(f.z, f.w)), t);
+                    for (int u = 0; u < 3; ++u) w[u][j / 2] = t[u];
+                    split<3>(mul2(make_pair2(v[j + 2], v[j + 3]), make_pair2(f.z, f.w)), t);
 #pragma unroll
-                    for (int i = 0; i < L::kWeights; ++i) w[i][j / 2 + 1] = t[i];
+                    for (int u = 0; u < 3; ++u) w[u][j / 2 + 1] = t[u];
                 }
-                if (q + 1 < min(steps, 4 * side + 4)) tmem_ld16_early(v, at + L::tz + 16 * (q + 1));
+                if (q + 1 < q1) tmem_ld16_early(v, at + L::tz + 16 * (q + 1));
 #pragma unroll
-                for (int i = 0; i < L::kWeights; ++i) tmem_st8(at + L::weighted(q, i), w[i]);
+                for (int u = 0; u < L::kWeightsAtOnce; ++u) tmem_st8(at + L::weighted(q, u), w[u]);
+                if constexpr (L::kWeightsAtOnce == 2)
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) last[i][u] = w[2][u];
             }
+            release_reads();
             bar_arrive(bars + 8 * kDecaysFree);
             tmem_wait_st();
             tmem_before_sync();
             bar_arrive(bars + 8 * kWeighted);
+            if constexpr (L::kWeightsAtOnce == 2) {
+                ok = ok && wait(kUpdateFirst, it);
+                tmem_after_sync();
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (q0 + i < q1) tmem_st8(at + L::weighted(q0 + i, 0), last[i]);
+                tmem_wait_st();
+                tmem_before_sync();
+                bar_arrive(bars + 8 * kWeightedLast);
+            }
+            if constexpr (kDots && kRev) {  // <S, D> of this chunk, while its update is formed
+                pair sum = 0;
+                if (crosses && columns && mine) {
+                    const float4* from4 = p.dump + ((long long)bh * p.chunks + t0 / kChunk) * 4096 + side * 2048 + z;
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        float4 f[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) f[u] = from4[(j + u) * 128];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            sum = fma2(make_pair2(f[u].x, f[u].y), s[2 * (j + u)], sum);
+                            sum = fma2(make_pair2(f[u].z, f[u].w), s[2 * (j + u) + 1], sum);
+                        }
+                    }
+                }
+                float a, c;
+                parts(sum, a, c);
+                a += c;
+                for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(~0u, a, o);
+                if (lane == 0) p.cross[((long long)bh * p.chunks + t0 / kChunk) * 8 + warp - 8] = a;
+            }
             ok = ok && wait(kUpdate, it);
             tmem_after_sync();
-            if (columns)
 #pragma unroll
-                for (int j = 0; j < 64; j += 16) {
+            for (int j = 0; j < 64; j += 16)
+                if (k0 + j < p.dx) {  // the product has no further columns
                     uint32_t v[16];
                     tmem_ld16(v, at + L::tz + k0 + j);
 #pragma unroll
@@ -635,6 +831,72 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
         p.fault->error_where = *stop;
         __threadfence();
         p.fault->error_id = p.call_id;
+    }
+}
+
+// dlog_a of one chunk from what the two passes left (the formulas at the head of ha_simt.cuh): with r, u the dots of the dq
+// and the dk pass and f the far part of u,
+//     dlog_a_t = sum_{i>=t} (r_i - (u_i - f_i)) + sum_{j<t} f_j + e^{c_C} scale <S, D>.
+// u - f are pairs inside the chunk and cancel exactly against r where both lie behind t.  A thread has one token; sums in
+// 64 bits.  part (fixed decays): only the sum over the chunk's tokens.
+__global__ void __launch_bounds__(kChunk) join_decay_grad_kernel(const float* r, const float* u, const float* f, const float* cross,
+                                                                 const float* log_a, long long ab, long long at, long long ah,
+                                                                 const int* lengths, int tokens, int heads, int chunks, long long side,
+                                                                 float scale, float* dlog_a, double* part) {
+    __shared__ double sums[3][4];
+    const int n = blockIdx.x % chunks, bh = blockIdx.x / chunks, b = bh / heads, h = bh % heads, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int t = n * kChunk + threadIdx.x, live = live_tokens(lengths, b, tokens);
+    const long long e = (long long)bh * tokens + t;
+    double x = 0.0, y = 0.0, c = 0.0;
+    if (t < live) {
+        const double far = (double)f[e] + (double)f[side + e];
+        x = ((double)r[e] + (double)r[side + e]) - (((double)u[e] + (double)u[side + e]) - far);
+        y = far;
+        const float a = log_a[b * ab + t * at + h * ah];
+        c = (double)(a < kReset ? kReset : a) * 1.4426950408889634;
+    }
+    const double own_x = x;
+    for (int o = 1; o < 32; o *= 2) {  // running sums within a warp
+        const double p = __shfl_up_sync(~0u, x, o), q = __shfl_up_sync(~0u, y, o);
+        if (lane >= o) { x += p; y += q; }
+    }
+    for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(~0u, c, o);
+    if (lane == 31) { sums[0][warp] = x; sums[1][warp] = y; sums[2][warp] = c; }
+    __syncthreads();
+    double all = 0.0, whole = 0.0;
+    for (int w = 0; w < 4; ++w) {
+        if (w < warp) { x += sums[0][w]; y += sums[1][w]; }
+        all += sums[0][w];
+        whole += sums[2][w];
+    }
+    double g = all - (x - own_x);                     // sum_{i>=t}
+    const double before = __shfl_up_sync(~0u, y, 1);  // sum_{j<t}
+    double first = 0.0;
+    for (int w = 0; w < warp; ++w) first += sums[1][w];
+    g += lane ? before : first;
+    if (whole > (double)kNothingCrosses && n * kChunk < live) {
+        double s = 0.0;
+        for (int w = 0; w < 8; ++w) s += (double)cross[((long long)bh * chunks + n) * 8 + w];
+        g += s * (double)scale * exp2(whole);
+    }
+    if (t >= live) g = 0.0;
+    if (!part) {
+        if (t < tokens) dlog_a[((long long)b * tokens + t) * heads + h] = (float)g;
+        return;
+    }
+    for (int o = 16; o > 0; o >>= 1) g += __shfl_xor_sync(~0u, g, o);
+    __syncthreads();
+    if (lane == 0) sums[0][warp] = g;
+    __syncthreads();
+    if (threadIdx.x == 0) part[blockIdx.x] = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+}
+
+// A strided [batch, tokens, heads, dim] tensor laid out contiguously, for TMA.
+__global__ void pack_rows_kernel(const Rows from, __nv_bfloat16* to, int tokens, int heads, int dim, long long total) {
+    for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < total; e += (long long)gridDim.x * blockDim.x) {
+        const int d = (int)(e % dim);
+        const long long row = e / dim, bt = row / heads;
+        to[e] = static_cast<const __nv_bfloat16*>(from.ptr)[bt / tokens * from.sb + bt % tokens * from.st + row % heads * from.sh + d];
     }
 }
 

@@ -8,6 +8,26 @@ namespace ha {
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+// Shared memory that another warp or TMA will overwrite once this thread has arrived on a barrier is read with these, and
+// release_reads() stands before the arrival.  The arrival alone (a release) was seen not to hold the loads back: they were
+// made after it, where registers were short, and found what came next.
+__device__ __forceinline__ void release_reads() { asm volatile("fence.acq_rel.cta;" ::: "memory"); }
+__device__ __forceinline__ float4 read4(const float* p) {
+    float4 v;
+    asm volatile("ld.volatile.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(smem_addr(p)) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 read4(const uint8_t* p) {
+    uint4 v;
+    asm volatile("ld.volatile.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem_addr(p)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float read1(const float* p) {
+    float v;
+    asm volatile("ld.volatile.shared.f32 %0, [%1];" : "=f"(v) : "r"(smem_addr(p)) : "memory");
+    return v;
+}
+
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
 }

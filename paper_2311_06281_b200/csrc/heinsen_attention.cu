@@ -111,9 +111,13 @@ bool encode(CUtensorMap* m, const View& v, long long batch, long long tokens) {
     const cuuint64_t strides[3] = {v.own_heads > 1 ? (cuuint64_t)v.rows.sh * 2 : any, tokens > 1 ? (cuuint64_t)v.rows.st * 2 : any,
                                    batch > 1 ? (cuuint64_t)v.rows.sb * 2 : any};
     const cuuint32_t box[4] = {64, 1, (cuuint32_t)ha::kChunk, 1}, one[4] = {1, 1, 1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(v.rows.ptr), dims, strides, box, one,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    for (int again = 0;; ++again) {
+        const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(v.rows.ptr), dims, strides, box, one,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r == CUDA_SUCCESS || again) return r == CUDA_SUCCESS;
+        cudaFree(nullptr);  // a thread that has made no runtime call yet has no context for the driver's
+    }
 }
 
 // Segments of a sequence.  Fewer (batch, head) pairs than SMs leave the rest of the GPU idle, so sequences are cut until
@@ -130,11 +134,11 @@ size_t segment_bytes(const heinsen_attention_problem* p) {
     return n > 1 ? up256((size_t)pairs * n * p->k_dim * p->v_dim * 4) + up256((size_t)pairs * n * 4) : 0;
 }
 
-template <bool kRev, int kTerms, class Out, bool kStateOnly>
+template <bool kRev, bool kDots, class Out, bool kStateOnly>
 hs_status mma_launch(const CUtensorMap& mx, const CUtensorMap& my, const CUtensorMap& mz, const CUtensorMap& mo,
                      const ha::MmaPass& mp, long long pairs, cudaStream_t stream) {
-    const auto fn = ha::mma_pass_kernel<kRev, kTerms, Out, kStateOnly>;
-    const int smem = (int)ha::MmaLayout<kTerms>::end;
+    const auto fn = ha::mma_pass_kernel<kRev, kDots, Out, kStateOnly>;
+    const int smem = (int)ha::MmaLayout<kDots>::end;
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
     const long long grid = pairs * (kStateOnly ? mp.segments - 1 : mp.segments);
@@ -143,10 +147,18 @@ hs_status mma_launch(const CUtensorMap& mx, const CUtensorMap& my, const CUtenso
     return launched("mma_pass_kernel");
 }
 
+// What the passes leave for the decay gradients.
+struct Dots {
+    Rows w;
+    float *near, *far;
+    float4* dump;
+    float* cross;
+};
+
 // One pass, with its segments.  `ws`: workspace header, `space`: segment_bytes() of scratch.
-template <bool kRev, int kTerms, class Out>
-hs_status mma_pass(const Pass& ps, const View& x, const View& y, const View& z, const heinsen_attention_problem* p, uint8_t* ws,
-                   uint8_t* space, unsigned long long id, cudaStream_t stream) {
+template <bool kRev, bool kDots, class Out>
+hs_status mma_pass(const Pass& ps, const View& x, const View& y, const View& z, uint8_t* ws, uint8_t* space, unsigned long long id,
+                   cudaStream_t stream, const Dots* dots = nullptr) {
     CUtensorMap mx, my, mz, mo;
     const View o{{ps.out, ps.ob, ps.ot, ps.oh, 1}, ps.heads, ps.dz};
     if (sizeof(Out) == 2 && !encode(&mo, o, ps.batch, ps.tokens))
@@ -167,25 +179,51 @@ hs_status mma_pass(const Pass& ps, const View& x, const View& y, const View& z, 
     const long long pairs = (long long)ps.batch * ps.heads, chunks = (ps.tokens + ha::kChunk - 1) / ha::kChunk;
     mp.segments = segments_for(pairs, ps.tokens, kSms);
     mp.seg_chunks = (int)((chunks + mp.segments - 1) / mp.segments);
+    mp.chunks = (int)chunks;
+    if (dots) {
+        mp.w = dots->w; mp.dots = dots->near; mp.dots_far = dots->far; mp.dump = dots->dump; mp.cross = dots->cross;
+    }
     if (mp.segments > 1) {
         mp.seg_state = reinterpret_cast<float*>(space);
         mp.seg_decay = reinterpret_cast<float*>(space + up256((size_t)pairs * mp.segments * ps.dx * ps.dz * 4));
-        hs_status st = mma_launch<kRev, 1, __nv_bfloat16, true>(mx, my, mz, mo, mp, pairs, stream);
+        hs_status st = mma_launch<kRev, false, __nv_bfloat16, true>(mx, my, mz, mo, mp, pairs, stream);
         if (st != HS_OK) return st;
         ha::join_segments_kernel<<<(unsigned)(pairs * ((ps.dx * ps.dz + 255) / 256)), 256, 0, stream>>>(mp);
         if ((st = launched("join_segments_kernel")) != HS_OK) return st;
     }
-    return mma_launch<kRev, kTerms, Out, false>(mx, my, mz, mo, mp, pairs, stream);
+    return mma_launch<kRev, kDots, Out, false>(mx, my, mz, mo, mp, pairs, stream);
 }
 
 // The rule for the tensor cores: bf16, head dimensions that TMA can load (multiples of 8, at most 128, 16-byte strides).
-bool mma_fits(const heinsen_attention_problem* p, const heinsen_attention_tensor* o) {
+bool mma_fits(const heinsen_attention_problem* p) {
     if (p->dtype != HS_BF16 || p->tokens == 0) return false;
-    if (!tma_fits({rows_of(p->q, p->heads, p->q_heads), p->q_heads, p->k_dim}, p->batch, p->tokens) ||
-        !tma_fits({rows_of(p->k, p->heads, p->k_heads), p->k_heads, p->k_dim}, p->batch, p->tokens) ||
-        !tma_fits({rows_of(p->v, p->heads, p->v_heads), p->v_heads, p->v_dim}, p->batch, p->tokens))
-        return false;
-    return tma_fits({rows_of(*o, p->heads, p->heads), p->heads, p->v_dim}, p->batch, p->tokens);
+    return tma_fits({rows_of(p->q, p->heads, p->q_heads), p->q_heads, p->k_dim}, p->batch, p->tokens) &&
+           tma_fits({rows_of(p->k, p->heads, p->k_heads), p->k_heads, p->k_dim}, p->batch, p->tokens) &&
+           tma_fits({rows_of(p->v, p->heads, p->v_heads), p->v_heads, p->v_dim}, p->batch, p->tokens);
+}
+View view_of(const heinsen_attention_tensor& t, int heads, int own, int dim) { return {rows_of(t, heads, own), own, dim}; }
+
+// Workspace of a backward call on the tensor cores: header | segments of a pass | a contiguous dO where TMA cannot load the
+// given one | gradients of each head where heads are shared, float32 | dots of the tokens | states before the chunks | their
+// products with the gradients behind them | sums of the decay gradients.
+struct MmaSpace {
+    size_t segments, d_o, dq, dk, dv, dots, dump, cross, part, total;
+};
+MmaSpace mma_space(const heinsen_attention_problem* p) {
+    MmaSpace s;
+    const size_t rows = (size_t)p->batch * p->tokens * p->heads, pairs = (size_t)p->batch * p->heads;
+    const size_t chunks = pairs * ((p->tokens + ha::kChunk - 1) / ha::kChunk);
+    s.segments = kHeaderBytes;
+    s.d_o = s.segments + segment_bytes(p);
+    s.dq = s.d_o + up256(rows * p->v_dim * 2);
+    s.dk = s.dq + (p->q_heads == p->heads ? 0 : up256(rows * p->k_dim * 4));
+    s.dv = s.dk + (p->k_heads == p->heads ? 0 : up256(rows * p->k_dim * 4));
+    s.dots = s.dv + (p->v_heads == p->heads ? 0 : up256(rows * p->v_dim * 4));
+    s.dump = s.dots + up256(6 * rows * 4);
+    s.cross = s.dump + chunks * 65536;
+    s.part = s.cross + up256(chunks * 32);
+    s.total = s.part + up256(chunks * 8);
+    return s;
 }
 
 // Workspace of a backward pass: header | dq, dk, dv for each head, float32 | the states before every chunk and the gradients
@@ -217,9 +255,9 @@ hs_status forward_pass(const heinsen_attention_problem* p, const heinsen_attenti
     ps.dx = p->k_dim; ps.dz = p->v_dim;
     ps.s_in = p->state0; ps.s_out = state;
     ps.out = const_cast<void*>(o->ptr); ps.ob = o->batch_stride; ps.ot = o->token_stride; ps.oh = o->head_stride;
-    if (mma_fits(p, o))
-        return mma_pass<false, 1, __nv_bfloat16>(ps, {ps.x, p->q_heads, p->k_dim}, {ps.y, p->k_heads, p->k_dim},
-                                                 {ps.z, p->v_heads, p->v_dim}, p, ws, ws + kHeaderBytes, hs_internal::call_id(), stream);
+    if (mma_fits(p) && tma_fits(view_of(*o, p->heads, p->heads, p->v_dim), p->batch, p->tokens))
+        return mma_pass<false, false, __nv_bfloat16>(ps, {ps.x, p->q_heads, p->k_dim}, {ps.y, p->k_heads, p->k_dim},
+                                                 {ps.z, p->v_heads, p->v_dim}, ws, ws + kHeaderBytes, hs_internal::call_id(), stream);
     return simt_pass<T, false, T>(ps, stream);
 }
 
@@ -303,6 +341,79 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
     return HS_OK;
 }
 
+// One gradient: straight into `to` where no head is shared, else a float32 row for each head first.
+template <bool kRev, bool kDots>
+hs_status gradient(Pass ps, const View& x, const View& y, const View& z, const heinsen_attention_problem* p, int groups, void* to,
+                   float* each, uint8_t* ws, unsigned long long id, cudaStream_t stream, const Dots* dots = nullptr) {
+    ps.x = x.rows; ps.y = y.rows; ps.z = z.rows; ps.dx = x.dim; ps.dz = z.dim;
+    ps.oh = z.dim; ps.ot = (long long)p->heads * z.dim; ps.ob = p->tokens * ps.ot;
+    uint8_t* space = ws + kHeaderBytes;
+    if (groups == p->heads) {
+        ps.out = to;
+        return mma_pass<kRev, kDots, __nv_bfloat16>(ps, x, y, z, ws, space, id, stream, dots);
+    }
+    ps.out = each;
+    const hs_status st = mma_pass<kRev, kDots, float>(ps, x, y, z, ws, space, id, stream, dots);
+    return st != HS_OK ? st : sum_heads<__nv_bfloat16>(each, to, p, groups, z.dim, stream);
+}
+
+template <bool kDots>
+hs_status mma_backward(const heinsen_attention_problem* p, const heinsen_attention_tensor* d_o, const float* d_state, void* dq,
+                       void* dk, void* dv, float* dlog_a, float* dstate0, uint8_t* ws, cudaStream_t stream) {
+    const MmaSpace sp = mma_space(p);
+    const unsigned long long id = hs_internal::call_id();
+    const int chunks = (int)((p->tokens + ha::kChunk - 1) / ha::kChunk);
+    const long long rows = (long long)p->batch * p->tokens * p->heads, pairs = (long long)p->batch * p->heads;
+    if (pairs * chunks > 0x7fffffffll) return HS_ERR_INVALID_ARG;
+    hs_status st;
+    View g = view_of(*d_o, p->heads, p->heads, p->v_dim);
+    if (!tma_fits(g, p->batch, p->tokens)) {
+        __nv_bfloat16* packed = reinterpret_cast<__nv_bfloat16*>(ws + sp.d_o);
+        const long long total = rows * p->v_dim;
+        ha::pack_rows_kernel<<<(unsigned)std::min<long long>((total + 255) / 256, kSms * 16), 256, 0, stream>>>(
+            g.rows, packed, (int)p->tokens, p->heads, p->v_dim, total);
+        if ((st = launched("pack_rows_kernel")) != HS_OK) return st;
+        const long long sh = p->v_dim, stk = sh * p->heads;
+        g.rows = {packed, stk * p->tokens, stk, sh, 1};
+    }
+    const View q = view_of(p->q, p->heads, p->q_heads, p->k_dim), k = view_of(p->k, p->heads, p->k_heads, p->k_dim),
+               v = view_of(p->v, p->heads, p->v_heads, p->v_dim);
+    float* dots = reinterpret_cast<float*>(ws + sp.dots);
+    float4* dump = reinterpret_cast<float4*>(ws + sp.dump);
+    float* cross = reinterpret_cast<float*>(ws + sp.cross);
+    auto each = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
+    {
+        Pass ps = common(p);
+        ps.s_in = p->state0; ps.s_in_t = 1;
+        const Dots d{q.rows, dots, nullptr, dump, nullptr};
+        if ((st = gradient<false, kDots>(ps, g, v, k, p, p->q_heads, dq, each(sp.dq), ws, id, stream, kDots ? &d : nullptr)) != HS_OK)
+            return st;
+    }
+    {
+        Pass ps = common(p);
+        ps.s_in = d_state; ps.s_in_t = 1; ps.s_in_mul = 1.0f / p->scale;  // the scale comes back with the output
+        const Dots d{k.rows, dots + 2 * rows, dots + 4 * rows, dump, cross};
+        if ((st = gradient<true, kDots>(ps, v, g, q, p, p->k_heads, dk, each(sp.dk), ws, id, stream, kDots ? &d : nullptr)) != HS_OK)
+            return st;
+    }
+    {
+        Pass ps = common(p);
+        ps.s_in = d_state; ps.s_in_mul = 1.0f / p->scale;
+        ps.s_out = dstate0; ps.s_out_mul = p->scale;
+        if ((st = gradient<true, false>(ps, k, q, g, p, p->v_heads, dv, each(sp.dv), ws, id, stream)) != HS_OK) return st;
+    }
+    if (!dlog_a) return HS_OK;
+    const bool fixed = p->log_a.batch_stride == 0 && p->log_a.token_stride == 0;
+    double* part = reinterpret_cast<double*>(ws + sp.part);
+    ha::join_decay_grad_kernel<<<(unsigned)(pairs * chunks), ha::kChunk, 0, stream>>>(
+        dots, dots + 2 * rows, dots + 4 * rows, cross, static_cast<const float*>(p->log_a.ptr), p->log_a.batch_stride,
+        p->log_a.token_stride, p->log_a.head_stride, p->lengths, (int)p->tokens, p->heads, chunks, rows, p->scale,
+        fixed ? nullptr : dlog_a, fixed ? part : nullptr);
+    if ((st = launched("join_decay_grad_kernel")) != HS_OK || !fixed) return st;
+    ha::decay_grad_sum_kernel<<<(unsigned)p->heads, 32, 0, stream>>>(part, (int)p->batch, p->heads, chunks, dlog_a);
+    return launched("decay_grad_sum_kernel");
+}
+
 hs_status check_space(const heinsen_attention_problem* p, int backward, void* workspace, size_t bytes) {
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HS_ERR_INVALID_ARG;
     return bytes < heinsen_attention_workspace_bytes(p, backward) ? HS_ERR_WORKSPACE_TOO_SMALL : HS_OK;
@@ -328,7 +439,8 @@ extern "C" {
 size_t heinsen_attention_workspace_bytes(const heinsen_attention_problem* p, int backward) {
     if (validate(p) != HS_OK) return 0;
     if (nothing(p)) return kHeaderBytes;
-    return backward ? backward_space(p).total : kHeaderBytes + segment_bytes(p);
+    if (!backward) return kHeaderBytes + segment_bytes(p);
+    return mma_fits(p) ? mma_space(p).total : backward_space(p).total;
 }
 
 hs_status heinsen_attention_forward(const heinsen_attention_problem* p, const heinsen_attention_tensor* o, float* state,
@@ -358,6 +470,9 @@ hs_status heinsen_attention_backward(const heinsen_attention_problem* p, const h
     if ((st = hs_internal::current_device(&sms)) != HS_OK) return st;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (mma_fits(p))
+        return dlog_a ? mma_backward<true>(p, d_o, d_state, dq, dk, dv, dlog_a, dstate0, ws, s)
+                      : mma_backward<false>(p, d_o, d_state, dq, dk, dv, dlog_a, dstate0, ws, s);
     return p->dtype == HS_F32
                ? backward_passes<float>(p, d_o, d_state, dq, dk, dv, dlog_a, dstate0, ws, s)
                : backward_passes<__nv_bfloat16>(p, d_o, d_state, dq, dk, dv, dlog_a, dstate0, ws, s);
