@@ -12,9 +12,13 @@
 //
 // Rounding.  A float32 factor enters a product as bf16 terms: w Z (and so the state, which is float32 to its owner) as three,
 // 24 bits, exact to float32's own rounding; P and the state in X S as one, where only the bf16 output depends on them (its own
-// rounding is as large), and as three where the decay gradients do (kDots): they are float32, and sums over many tokens of
-// dots that cancel in part, to which two terms (17 bits) would leave errors of 2e-5 and more.  Tensor memory then holds two
-// terms at a time; the third is kept in registers and follows when the first two have been used.
+// rounding is as large).
+//
+// kDots: the pass also forms what the decay gradients need of it, in float32: the row sums of W = P o (w Z^T), w the fourth
+// tensor, from the unrounded P, and the dots w_i . (X S)_i, for which X S has the state in two terms.  W comes out of the two
+// passes that form it in the same bits (each exponential is taken of the same difference there), so that what cancels between
+// their sums cancels exactly.  Row sums from the outputs instead, w_i . out_i, were 1e-6 off in a common direction (the tensor
+// core's additions cut off), which sums over many tokens turn into 5e-5.
 #pragma once
 #include <cuda.h>
 
@@ -25,12 +29,10 @@ namespace ha {
 
 constexpr int kChunk = 128;
 constexpr int kMmaThreads = 640;
-// Registers of a thread: 96 at launch (65536 over 20 warps).  What the feeding warps can spare goes to the rows of the state,
-// and to those of out where they hold two more rows for the decay gradients: 64 + 2 * 80 + 2 * 128 = 64 + 2 * 88 + 2 * 120 =
-// 480 for a thread of each warpgroup, 5 * 96 as at launch.
+// Registers of a thread: 96 at launch (65536 over 20 warps); those that the feeding warps and the rows of out can spare go to
+// the rows of the state.  64 + 2 * 80 + 2 * 128 = 480 for a thread of each warpgroup, 5 * 96 as at launch.
 constexpr int kFeedRegs = 64;
-template <bool kDots> constexpr int kRowRegs = kDots ? 88 : 80;
-template <bool kDots> constexpr int kStateRegs = kDots ? 120 : 128;
+constexpr int kRowRegs = 80, kStateRegs = 128;
 constexpr uint32_t kTile = 128 * 256;        // 128 rows of 128 bf16: two blocks of 64 columns, 128-byte swizzle
 constexpr uint32_t kBlock = kTile / 2;
 constexpr uint32_t kSpin = 1u << 20;         // polls of a barrier before a wait gives up (about a microsecond each)
@@ -57,11 +59,12 @@ struct MmaPass {
     int segments, seg_chunks, chunks;
     float* seg_state;
     float* seg_decay;
-    // For the decay gradients (kDots): w_i . out_i of every token without the token's own term, and of its X S part
-    // alone (reversed pass), by halves of the columns: [2][batch * heads][tokens].  The forward pass leaves the state before
-    // every chunk in `dump`, the reversed one multiplies it with its own: cross[batch * heads][chunks][8], a warp each.
-    Rows w;
-    float *dots, *dots_far;
+    // For the decay gradients (kDots), by token and for each half of the columns, [2][batch * heads][tokens]: the row sums of
+    // W below (reversed: above) the diagonal, and w_i . (X S)_i.  The forward pass also leaves the state before every chunk in `dump`, the reversed one multiplies it with its own: cross[batch * heads][chunks][8], a warp
+    // each.
+    int wdiv;
+    double* dots;
+    float* dots_far;
     float4* dump;
     float* cross;
     Fault* fault;
@@ -73,34 +76,34 @@ constexpr float kNothingCrosses = -60.0f;
 
 template <bool kDots>
 struct MmaLayout {
-    static constexpr int kTerms = kDots ? 3 : 1;               // of P and of the state in X S
-    static constexpr int kAtOnce = kDots ? 2 : 1;              // terms of P in the first product
-    static constexpr int kWeightsAtOnce = kDots ? 2 : 3;       // terms of w Z in the first product
+    static constexpr int kTerms = kDots ? 2 : 1;               // of the state in X S
+    static constexpr int kWeightsAtOnce = kDots ? 2 : 3;       // terms of w Z in the first product; the third follows
     // Stages.  A chunk's output leaves from its X tile, where X has two, else from its Y tile.
-    static constexpr int kXs = kDots ? 1 : 2, kYs = 2, kZs = kDots ? 1 : 2;
-    static constexpr uint32_t x = 0, y = x + kXs * kTile, z = y + kYs * kTile, s = z + kZs * kTile, ident = s + kTerms * kTile,
-                              decays = ident + 512, whole = decays + 4 * kChunk * 4, bars = whole + 32, end = bars + 8 * 34;
+    static constexpr int kXs = kDots ? 1 : 2, kYs = 2, kZs = kDots ? 1 : 2, kWs = kDots ? 1 : 0;
+    static constexpr uint32_t x = 0, y = x + kXs * kTile, z = y + kYs * kTile, w = z + kZs * kTile, s = w + kWs * kTile,
+                              ident = s + kTerms * kTile, decays = ident + 512, whole = decays + 4 * kChunk * 4, bars = whole + 32,
+                              end = bars + 8 * 36;
     // Tensor memory columns, all 512.  What is read out before the next product of its chain is due shares columns with it:
     // Z^T with the state's update, the scores with the output.
     static constexpr uint32_t tw = 0;                          // the terms of (w Z)^T: A operand
     static constexpr uint32_t tz = tw + 64 * kWeightsAtOnce;   // Z^T, then the state's update
     static constexpr uint32_t to = tz + 128;                   // X Y^T, then X S, then P Z
-    static constexpr uint32_t tp = to + 128;                   // the terms of P: A operand
-    static_assert(tp + 64 * kAtOnce == 512, "tensor memory");
+    static constexpr uint32_t tp = to + 128;                   // P: A operand
+    static constexpr uint32_t tt = tp + 64;                    // half of w Z^T (kDots)
+    static_assert(tt + (kDots ? 64 : 0) == 512, "tensor memory");
     static __device__ __forceinline__ uint32_t staged(uint32_t base, int it) {
         return base + (kDots ? y + it % kYs * kTile : x + it % kXs * kTile);
     }
-    // where term t of 16 tokens q lies
-    static __device__ __forceinline__ constexpr uint32_t prob(int q, int t) { return tp + 8 * kAtOnce * q + 8 * t; }
+    // where 16 tokens q, and term t of them, lie
+    static __device__ __forceinline__ constexpr uint32_t prob(int q) { return tp + 8 * q; }
     static __device__ __forceinline__ constexpr uint32_t weighted(int q, int t) { return tw + 8 * kWeightsAtOnce * q + 8 * t; }
 };
 
 // Every barrier completes one phase per chunk (those with two entries: per chunk that uses the entry), and nobody who waits
 // for a phase can be overtaken by the next: it needs something of the waiter's own.
 enum Bar : int { kFullX = 0, kFullY = 2, kFullZ = 4, kFreeX = 6, kFreeY = 8, kFreeZ = 10, kPatchY = 12, kPatchZ, kDecays, kDecaysFree, kScores,
-                 kTransposed, kProbs, kFar, kFarRead, kNear, kStaged, kWeighted, kWeightedLast, kUpdateFirst,
-                 kUpdate, kUpdateRead, kStateReady, kNearFirst, kProbsLast, kYDone, kDrain = kYDone + 2,
-                 kBars };
+                 kTransposed, kProbs, kFar, kFarRead, kNear, kStaged, kWeighted, kWeightedLast, kUpdateFirst, kUpdate, kUpdateRead,
+                 kStateReady, kFullW, kFreeW, kHalfRead, kHalf, kYDone, kDrain = kYDone + 2, kBars };
 
 struct Waiter {
     uint32_t bars;
@@ -134,13 +137,6 @@ __device__ __forceinline__ pair add_dot(pair sum, const uint32_t (&v)[16], const
     for (int i = 0; i < 8; ++i) sum = fma2(make_pair2(w[i] << 16, w[i] & 0xffff0000u), make_pair2(v[2 * i], v[2 * i + 1]), sum);
     return sum;
 }
-__device__ __forceinline__ void add_scaled(uint32_t (&v)[16], float f, const uint4& lo, const uint4& hi) {
-    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        parts(fma2(make_pair2(w[i] << 16, w[i] & 0xffff0000u), make_pair2(f, f), make_pair2(v[2 * i], v[2 * i + 1])), v[2 * i], v[2 * i + 1]);
-}
-
 // Sixteen columns of one row, or the n that are left of it
 __device__ __forceinline__ void store_row16(float* to, const float (&v)[16], int n) {
 #pragma unroll
@@ -158,10 +154,11 @@ __device__ __forceinline__ void store_row16(__nv_bfloat16* to, const float (&v)[
 template <bool kRev, bool kDots, class Out, bool kStateOnly>
 __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_constant__ CUtensorMap mx, const __grid_constant__ CUtensorMap my,
                                                                   const __grid_constant__ CUtensorMap mz, const __grid_constant__ CUtensorMap mo,
+                                                                  const __grid_constant__ CUtensorMap mw,
                                                                   const MmaPass p) {
     using L = MmaLayout<kDots>;
     // a group that asks for more than the others gave up would wait for ever
-    static_assert(kFeedRegs + 2 * kRowRegs<kDots> + 2 * kStateRegs<kDots> <= 5 * 96 && kRowRegs<kDots> <= 96, "registers");
+    static_assert(kFeedRegs + 2 * kRowRegs + 2 * kStateRegs <= 5 * 96 && kRowRegs <= 96, "registers");
     constexpr int kTerms = L::kTerms;
     extern __shared__ __align__(1024) uint8_t sm8[];
     const uint32_t base = smem_addr(sm8);
@@ -189,7 +186,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             if (i >= kFreeY && i < kPatchY) arrivals = kStateOnly ? 1 : kDots && i < kFreeZ ? 3 : 2;
             if (i == kDecays) arrivals = 32;
             if (i == kDecaysFree) arrivals = kStateOnly ? 256 : 512;
-            if (i == kProbs || i == kFarRead || i == kStaged || i == kWeighted || i == kWeightedLast || i == kProbsLast || i == kUpdateRead || i == kStateReady) arrivals = 256;
+            if (i == kProbs || i == kFarRead || i == kStaged || i == kWeighted || i == kWeightedLast || i == kHalfRead || i == kUpdateRead ||
+                i == kStateReady)
+                arrivals = 256;
+            if (i == kFreeW) arrivals = 257;
             bar_init(bars + 8 * i, arrivals);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 if (dim > 64) tma_load_4d(to + kBlock, m, 64, head, t0, b, bars + 8 * full);
             };
             bool ok = true;
-            int loads = 0;
+            int loads = 0, loads_w = 0;
             for (int it = 0; it < count && ok; ++it) {
                 const int t0 = chunk_at(it) * kChunk;
                 // tokens behind the sequence's end are in memory and may hold anything: 0 * NaN must not reach a sum
@@ -238,6 +238,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     if (ok) {
                         load(&mz, Z, p.dz, h / p.zdiv, t0, patch ? kPatchZ : kFullZ + it % L::kZs);
                         loads = it + 1;
+                    }
+                    if (kDots) {
+                        if (ok && it >= 1) ok = wait(kFreeW, it - 1);
+                        if (ok) load(&mw, base + L::w, p.dz, h / p.wdiv, t0, kFullW);
+                        if (ok) loads_w = it + 1;
                     }
                 }
                 if (patch) {
@@ -266,6 +271,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 if (!kStateOnly) drain(kFullX, L::kXs);
                 drain(kFullY, L::kYs);
                 drain(kFullZ, L::kZs);
+                loads = loads_w;
+                if (kDots) drain(kFullW, 1);
             }
         } else if (warp == kDecayer) {
             // ------------------------------------------------------------ decays, a lane has four tokens
@@ -351,6 +358,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                                shape_n = mma_shape(nz, kColMajorB), shape_u = mma_shape(16 * kx, kColMajorB);
                 auto ready = [&](int bar, int turn) { return bar_test(bars + 8 * bar, turn & 1); };
                 auto k_step = [](int kk) { return (uint32_t)((kk >> 2) * (kBlock >> 4) + (kk & 3) * 2); };  // 32 bytes, then the next block
+                // w Z^T for 64 of the chunk's tokens as columns
+                auto half_scores = [&](int half) {
+                    const uint32_t wo = operand(base + L::w, kBlock), zo = operand(base + L::z, kBlock) + half * (64 * 128 >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        if (16 * kk < p.dz) mma_ss(tmem + L::tt, wo + k_step(kk), zo + k_step(kk), mma_shape(64, 0), kk > 0);
+                };
                 int a_it = kStateOnly ? count : 0, a_step = 0, b_it = 0, b_step = 0;
                 uint32_t idle = 0;
                 while (a_it < count || b_it < count) {
@@ -374,11 +388,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                             const uint32_t yo = operand(base + L::y + ys * kTile, kBlock);
                             if (L::kWeightsAtOnce == 3 || b_step == 1) {
 #pragma unroll
-                                for (int q = 0; q < 8; ++q)
-                                    if (q < steps)
+                                for (int t = 0; t < L::kWeightsAtOnce; ++t)
 #pragma unroll
-                                        for (int t = 0; t < L::kWeightsAtOnce; ++t)
-                                            mma_ts(tmem + L::weighted(q, t), yo + q * 128, shape_u, q + t > 0, tmem + L::tz);
+                                    for (int q = 0; q < 8; ++q)
+                                        if (q < steps) mma_ts(tmem + L::weighted(q, t), yo + q * 128, shape_u, q + t > 0, tmem + L::tz);
                             } else {
 #pragma unroll
                                 for (int q = 0; q < 8; ++q)
@@ -401,14 +414,25 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                         const int it = a_it, xs = it % L::kXs, ys = it % L::kYs, zs = it % L::kZs;
                         const uint32_t xo = operand(base + L::x + xs * kTile, kBlock);
                         if (a_step == 0) {
-                            if (ready(kFullX + xs, it / L::kXs) && ready(kFullY + ys, it / L::kYs) && (it == 0 || ready(kStaged, it - 1))) {
+                            if (ready(kFullX + xs, it / L::kXs) && ready(kFullY + ys, it / L::kYs) && (it == 0 || ready(kStaged, it - 1)) &&
+                                (!kDots || (ready(kFullZ, it) && ready(kFullW, it)))) {
                                 tmem_after_sync();
                                 const uint32_t yo = operand(base + L::y + ys * kTile, kBlock);
 #pragma unroll
                                 for (int kk = 0; kk < 8; ++kk)
                                     if (kk < kx) mma_ss(tmem + L::to, xo + k_step(kk), yo + k_step(kk), shape_p, kk > 0);
+                                if (kDots) half_scores(0);
                                 mma_commit(bars + 8 * kScores);
                                 mma_commit(bars + 8 * (kFreeY + ys));
+                                a_step = kDots ? 4 : 1;
+                                moved = true;
+                            }
+                        } else if (kDots && a_step == 4) {
+                            if (ready(kHalfRead, it)) {
+                                tmem_after_sync();
+                                half_scores(1);
+                                mma_commit(bars + 8 * kHalf);
+                                mma_commit(bars + 8 * kFreeW);
                                 a_step = 1;
                                 moved = true;
                             }
@@ -417,41 +441,28 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                                 tmem_after_sync();
                                 const uint32_t so = operand(base + L::s, kBlock);
 #pragma unroll
-                                for (int t = 0; t < kTerms; ++t)
+                                for (int t = kTerms - 1; t >= 0; --t)  // small terms first: every addition rounds the sum so far
 #pragma unroll
                                     for (int kk = 0; kk < 8; ++kk)
                                         if (kk < kx)
-                                            mma_ss(tmem + L::to, xo + k_step(kk), so + t * (kTile >> 4) + k_step(kk), shape_f, t + kk > 0);
+                                            mma_ss(tmem + L::to, xo + k_step(kk), so + t * (kTile >> 4) + k_step(kk), shape_f,
+                                                   t < kTerms - 1 || kk > 0);
                                 mma_commit(bars + 8 * kFar);
                                 if (kDots) mma_commit(bars + 8 * (kFreeX + xs));
                                 a_step = 2;
                                 moved = true;
                             }
-                        } else if (a_step == 2 ? ready(kFarRead, it) && ready(kFullZ + zs, it / L::kZs) : ready(kProbsLast, it)) {
+                        } else if (ready(kFarRead, it) && ready(kFullZ + zs, it / L::kZs)) {
                             tmem_after_sync();
                             const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32);
                             const uint32_t zo = operand(base + L::z + zs * kTile, kBlock);
-                            if (!kDots || a_step == 2) {
 #pragma unroll
-                                for (int q = 0; q < 8; ++q)
-                                    if (q < steps)
-#pragma unroll
-                                        for (int t = 0; t < L::kAtOnce; ++t)
-                                            mma_ts(tmem + L::prob(q, t), zo + q * 128, shape_n, true, tmem + L::to);
-                            } else {
-#pragma unroll
-                                for (int q = 0; q < 8; ++q)
-                                    if (q < steps) mma_ts(tmem + L::prob(q, 0), zo + q * 128, shape_n, true, tmem + L::to);
-                            }
-                            if (kDots && a_step == 2) {
-                                mma_commit(bars + 8 * kNearFirst);
-                                a_step = 3;
-                            } else {
-                                mma_commit(bars + 8 * kNear);
-                                mma_commit(bars + 8 * (kFreeZ + zs));
-                                a_step = 0;
-                                ++a_it;
-                            }
+                            for (int q = 0; q < 8; ++q)
+                                if (q < steps) mma_ts(tmem + L::prob(q), zo + q * 128, shape_n, true, tmem + L::to);
+                            mma_commit(bars + 8 * kNear);
+                            mma_commit(bars + 8 * (kFreeZ + zs));
+                            a_step = 0;
+                            ++a_it;
                             moved = true;
                         }
                     }
@@ -467,7 +478,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             __syncwarp();
         }
     } else if (warp < 8) {
-        give_registers<kRowRegs<kDots>>();
+        give_registers<kRowRegs>();
         // ---------------------------------------------------------------- P and the output: two threads have one token's row
         if (!kStateOnly) {
             const int side = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
@@ -480,19 +491,25 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 const int batches = min(4, (live - t0 + 31) / 32);
                 ok = ok && wait(kDecays, it);
                 const float own_hi = read1(c_hi + row), own_lo = read1(c_lo + row);
-                float own = 0.0f;  // P_ii, where it is kept out of the product
                 const float far = p.scale * ex2(kRev ? (read1(s_whole + 1) - own_hi) + (read1(s_whole + 2) - own_lo) : own_hi + own_lo);
                 ok = ok && wait(kScores, it);
                 tmem_after_sync();
-                uint32_t last[2][2][8] = {};  // third terms: they wait for the first two
-#pragma unroll kDots ? 2 : 1
+                double sum = 0.0;  // of W's row; joined in 64 bits, since two such sums will be subtracted
+                pair sum_far = 0;
+#pragma unroll 1
                 for (int i = 0; i < 2; ++i) {  // a batch of 32 columns; the sides take turns
                     const int n = side + 2 * i;
-                    if (n >= batches) break;
+                    if (kDots && i == 1) {  // the first half of w Z^T has been read by this thread
+                        tmem_before_sync();
+                        bar_arrive(bars + 8 * kHalfRead);
+                        ok = ok && wait(kHalf, it);
+                        tmem_after_sync();
+                    }
+                    if (n >= batches) continue;
                     if (kRev ? n < quarter : n > quarter) {
                         const uint32_t zero[8] = {};
 #pragma unroll
-                        for (int i = 0; i < 2 * L::kAtOnce; ++i) tmem_st8(at + L::prob(2 * n, 0) + 8 * i, zero);
+                        for (int e = 0; e < 2; ++e) tmem_st8(at + L::prob(2 * n + e), zero);
                         continue;
                     }
                     const bool diagonal = n == quarter;
@@ -501,80 +518,66 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     const int m = kRev ? 32 * n : 32 * n + 31;
                     const float f1 = p.scale * ex2((kRev ? 1.0f : -1.0f) * ((read1(c_hi + m) - own_hi) + (read1(c_lo + m) - own_lo)));
                     const pair f = make_pair2(f1, f1);
-#pragma unroll kDots ? 2 : 1
+#pragma unroll 1
                     for (int e = 0; e < 2; ++e) {
                         const int q = 2 * n + e;
-                        uint32_t v[16], term[kTerms][8];
+                        uint32_t v[16], term[8];
                         tmem_ld16(v, at + L::to + 16 * q);
 #pragma unroll
                         for (int j = 0; j < 16; j += 4) {
                             pair w0, w1;
-                            if (!diagonal) {
+                            if (!kDots && !diagonal) {
                                 const float4 g = read4(w_bt + 16 * q + j);
                                 w0 = mul2(f, make_pair2(g.x, g.y));
                                 w1 = mul2(f, make_pair2(g.z, g.w));
                             } else {
                                 const float4 hi = read4(c_hi + 16 * q + j);
                                 const float4 lo = read4(c_lo + 16 * q + j);
-                                const int ahead = row - 16 * q - j;  // columns up to the diagonal
+                                const int ahead = diagonal ? row - 16 * q - j : kRev ? -1 : 16;  // columns up to the diagonal
                                 auto weight = [&](int u, float h1, float l1) {
                                     const float d = kRev ? (h1 - own_hi) + (l1 - own_lo) : (own_hi - h1) + (own_lo - l1);
-                                    return (kDots ? (kRev ? u > ahead : u < ahead) : (kRev ? u >= ahead : u <= ahead)) ? p.scale * ex2(d) : 0.0f;
+                                    return (kRev ? u >= ahead : u <= ahead) ? p.scale * ex2(d) : 0.0f;
                                 };
-                                if (kDots) {
-#pragma unroll
-                                    for (int u = 0; u < 4; ++u)
-                                        if (u == ahead) own = p.scale * __uint_as_float(v[j + u]);
-                                }
                                 w0 = make_pair2(weight(0, hi.x, lo.x), weight(1, hi.y, lo.y));
                                 w1 = make_pair2(weight(2, hi.z, lo.z), weight(3, hi.w, lo.w));
                             }
-                            uint32_t s[kTerms];
-                            split<kTerms>(mul2(w0, make_pair2(v[j], v[j + 1])), s);
+                            w0 = mul2(w0, make_pair2(v[j], v[j + 1]));
+                            w1 = mul2(w1, make_pair2(v[j + 2], v[j + 3]));
+                            term[j / 2] = pack_bf16(w0);
+                            term[j / 2 + 1] = pack_bf16(w1);
+                            if constexpr (kDots) {  // kept for the row sum, without the token itself
+                                parts(w0, v[j], v[j + 1]);
+                                parts(w1, v[j + 2], v[j + 3]);
 #pragma unroll
-                            for (int u = 0; u < kTerms; ++u) term[u][j / 2] = s[u];
-                            split<kTerms>(mul2(w1, make_pair2(v[j + 2], v[j + 3])), s);
-#pragma unroll
-                            for (int u = 0; u < kTerms; ++u) term[u][j / 2 + 1] = s[u];
+                                for (int u = 0; u < 4; ++u)
+                                    if (16 * q + j + u == row) v[j + u] = 0u;
+                            }
                         }
+                        tmem_st8(at + L::prob(q), term);
+                        if constexpr (kDots) {
+                            uint32_t t16[16];
+                            tmem_ld16(t16, at + L::tt + 16 * (q & 3));
 #pragma unroll
-                        for (int u = 0; u < L::kAtOnce; ++u) tmem_st8(at + L::prob(q, u), term[u]);
-                        if constexpr (kDots)
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) last[i][e][u] = term[2][u];
+                            for (int j = 0; j < 16; j += 4) {
+                                float a, c;
+                                parts(fma2(make_pair2(v[j], v[j + 1]), make_pair2(t16[j], t16[j + 1]),
+                                           mul2(make_pair2(v[j + 2], v[j + 3]), make_pair2(t16[j + 2], t16[j + 3]))), a, c);
+                                sum += (double)(a + c);
+                            }
+                        }
                     }
                 }
                 release_reads();
                 bar_arrive(bars + 8 * kDecaysFree);
-                if (kDots && (quarter & 1) != side && quarter < batches) {  // the other side had the diagonal
-#pragma unroll 1
-                    for (int q = 2 * quarter; q < 2 * quarter + 2; ++q) {
-                        uint32_t v[16];
-                        tmem_ld16(v, at + L::to + 16 * q);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (16 * q + j == row) own = p.scale * __uint_as_float(v[j]);
-                    }
-                }
-                const int col0 = 64 * side, col1 = min(p.dz, col0 + 64);
-                auto own_row = [&](uint4 (&w4)[8]) {  // the row's own w, 8 columns each
-                    const __nv_bfloat16* gw = static_cast<const __nv_bfloat16*>(p.w.ptr) + b * p.w.sb + (h / p.w.div) * p.w.sh + t * p.w.st + col0;
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        w4[c] = make_uint4(0, 0, 0, 0);
-                        if (t < live && col0 + 8 * c < p.dz) w4[c] = *reinterpret_cast<const uint4*>(gw + 8 * c);
-                    }
-                };
-                uint4 w4[8];
-                if (kDots && kRev) own_row(w4);
                 tmem_wait_st();
                 tmem_before_sync();
                 bar_arrive(bars + 8 * kProbs);
                 ok = ok && wait(kFar, it);
                 tmem_after_sync();
+                const int col0 = 64 * side, col1 = min(p.dz, col0 + 64);
                 const pair far2 = make_pair2(far, far);
-                pair dot = 0, dot_far = 0;
-#pragma unroll kDots ? 4 : 1
+                const uint8_t* const own_w = sm8 + L::w + side * kBlock + row * 128;
+#pragma unroll 1
                 for (int c = 0; c < 4; ++c) {  // X S with its row's weight, for P Z to be added to
                     const int col = col0 + 16 * c;
                     if (col >= col1) break;
@@ -582,48 +585,27 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     tmem_ld16(v, at + L::to + col);
 #pragma unroll
                     for (int u = 0; u < 16; u += 2) parts(mul2(far2, make_pair2(v[u], v[u + 1])), v[u], v[u + 1]);
-                    if constexpr (kDots && kRev) dot_far = add_dot(dot_far, v, w4[2 * c], w4[2 * c + 1]);
                     tmem_st16(at + L::to + col, v);
+                    if constexpr (kDots) {
+                        const uint4 lo = read4(own_w + (((2 * c) ^ (row & 7)) << 4)), hi = read4(own_w + (((2 * c + 1) ^ (row & 7)) << 4));
+                        sum_far = add_dot(sum_far, v, lo, hi);
+                    }
+                }
+                if constexpr (kDots) {
+                    release_reads();
+                    bar_arrive(bars + 8 * kFreeW);
                 }
                 tmem_wait_st();
                 tmem_before_sync();
                 bar_arrive(bars + 8 * kFarRead);
-                uint4 z4[8];  // the row's own z, for its own term
-                if constexpr (kDots) {
-                    ok = ok && wait(kNearFirst, it);
-                    tmem_after_sync();
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            if (side + 2 * i < batches) tmem_st8(at + L::prob(2 * (side + 2 * i) + e, 0), last[i][e]);
-                    ok = ok && wait(kFullZ + it % L::kZs, it / L::kZs);
-                    const uint8_t* zt = sm8 + L::z + it % L::kZs * kTile + side * kBlock + row * 128;
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        z4[c] = make_uint4(0, 0, 0, 0);
-                        if (col0 + 8 * c < p.dz) z4[c] = read4(zt + ((c ^ (row & 7)) << 4));
-                    }
-                    tmem_wait_st();
-                    tmem_before_sync();
-                    release_reads();
-                    bar_arrive(bars + 8 * kProbsLast);
-                    own_row(w4);
-                }
                 ok = ok && wait(kNear, it);
                 tmem_after_sync();
                 uint8_t* const stage = sm8 + L::staged(0, it) + side * kBlock + row * 128;
                 if (kDots) ok = ok && wait(kYDone + it % L::kYs, it / L::kYs);  // the tile has been read (the scores were before)
-#pragma unroll kDots ? 4 : 1
-                for (int n = 0; n < 4; ++n) {
-                    const int col = col0 + 16 * n;
-                    if (col >= col1) break;
+#pragma unroll 1
+                for (int col = col0; col < col1; col += 16) {
                     uint32_t v[16];
                     tmem_ld16(v, at + L::to + col);
-                    if constexpr (kDots) {
-                        dot = add_dot(dot, v, w4[2 * n], w4[2 * n + 1]);
-                        add_scaled(v, own, z4[2 * n], z4[2 * n + 1]);
-                    }
                     if (t >= live)
 #pragma unroll
                         for (int u = 0; u < 16; ++u) v[u] = 0u;
@@ -645,14 +627,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 bar_arrive(bars + 8 * kStaged);
                 if constexpr (kDots) {
                     const long long to = ((long long)side * gridDim.x / p.segments + bh) * p.tokens + t;
-                    float d0, d1;
+                    float a, c;
+                    parts(sum_far, a, c);
                     if (t < live) {
-                        parts(dot, d0, d1);
-                        p.dots[to] = columns ? d0 + d1 : 0.0f;
-                        if (kRev) {
-                            parts(dot_far, d0, d1);
-                            p.dots_far[to] = columns ? d0 + d1 : 0.0f;
-                        }
+                        p.dots[to] = sum;
+                        p.dots_far[to] = columns ? a + c : 0.0f;
                     }
                 }
             }
@@ -665,7 +644,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 }
         }
     } else {
-        take_registers<kStateRegs<kDots>>();
+        take_registers<kStateRegs>();
         // ---------------------------------------------------------------- the state: two threads have one row of S^T
         const int side = (warp - 8) >> 2, quarter = warp & 3, z = quarter * 32 + lane, k0 = 64 * side;
         const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
@@ -729,7 +708,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             ok = ok && wait(kTransposed, it);
             tmem_after_sync();
             uint32_t v[16];
-            uint32_t last[L::kWeightsAtOnce == 2 ? 4 : 1][8];  // third terms, where they have to wait
+            uint32_t last[L::kWeightsAtOnce == 2 ? 4 : 1][8];  // first terms, where they have to wait
             const int q0 = 4 * side, q1 = min(steps, q0 + 4);
             if (q0 < q1) tmem_ld16_early(v, at + L::tz + 16 * q0);
 #pragma unroll L::kWeightsAtOnce == 2 ? 4 : 1
@@ -751,10 +730,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 }
                 if (q + 1 < q1) tmem_ld16_early(v, at + L::tz + 16 * (q + 1));
 #pragma unroll
-                for (int u = 0; u < L::kWeightsAtOnce; ++u) tmem_st8(at + L::weighted(q, u), w[u]);
+                for (int u = 0; u < L::kWeightsAtOnce; ++u) tmem_st8(at + L::weighted(q, u), w[2 - u]);  // the smallest first
                 if constexpr (L::kWeightsAtOnce == 2)
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) last[i][u] = w[2][u];
+                    for (int u = 0; u < 8; ++u) last[i][u] = w[0][u];
             }
             release_reads();
             bar_arrive(bars + 8 * kDecaysFree);
@@ -834,12 +813,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
     }
 }
 
-// dlog_a of one chunk from what the two passes left (the formulas at the head of ha_simt.cuh): with r, u the dots of the dq
-// and the dk pass and f the far part of u,
-//     dlog_a_t = sum_{i>=t} (r_i - (u_i - f_i)) + sum_{j<t} f_j + e^{c_C} scale <S, D>.
-// u - f are pairs inside the chunk and cancel exactly against r where both lie behind t.  A thread has one token; sums in
-// 64 bits.  part (fixed decays): only the sum over the chunk's tokens.
-__global__ void __launch_bounds__(kChunk) join_decay_grad_kernel(const float* r, const float* u, const float* f, const float* cross,
+// dlog_a of one chunk from what the two passes left (the formulas at the head of ha_simt.cuh): with r and r', u and u' the row
+// sums and the far dots of the dq and the dk pass,
+//     dlog_a_t = sum_{i>=t} (r_i - u_i + r'_i) + sum_{j<t} u'_j + e^{c_C} scale <S, D>.
+// Pairs inside the chunk that both lie behind t are in r and in u and cancel.  A thread has one token; sums in 64 bits.  part (fixed decays): only the sum over the chunk's tokens.
+__global__ void __launch_bounds__(kChunk) join_decay_grad_kernel(const double* r, const double* u, const float* rf, const float* uf, const float* cross,
                                                                  const float* log_a, long long ab, long long at, long long ah,
                                                                  const int* lengths, int tokens, int heads, int chunks, long long side,
                                                                  float scale, float* dlog_a, double* part) {
@@ -849,9 +827,8 @@ __global__ void __launch_bounds__(kChunk) join_decay_grad_kernel(const float* r,
     const long long e = (long long)bh * tokens + t;
     double x = 0.0, y = 0.0, c = 0.0;
     if (t < live) {
-        const double far = (double)f[e] + (double)f[side + e];
-        x = ((double)r[e] + (double)r[side + e]) - (((double)u[e] + (double)u[side + e]) - far);
-        y = far;
+        x = (r[e] + r[side + e]) - (u[e] + u[side + e]) + ((double)rf[e] + (double)rf[side + e]);
+        y = (double)uf[e] + (double)uf[side + e];
         const float a = log_a[b * ab + t * at + h * ah];
         c = (double)(a < kReset ? kReset : a) * 1.4426950408889634;
     }

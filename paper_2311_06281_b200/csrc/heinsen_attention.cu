@@ -136,21 +136,22 @@ size_t segment_bytes(const heinsen_attention_problem* p) {
 
 template <bool kRev, bool kDots, class Out, bool kStateOnly>
 hs_status mma_launch(const CUtensorMap& mx, const CUtensorMap& my, const CUtensorMap& mz, const CUtensorMap& mo,
-                     const ha::MmaPass& mp, long long pairs, cudaStream_t stream) {
+                     const CUtensorMap& mw, const ha::MmaPass& mp, long long pairs, cudaStream_t stream) {
     const auto fn = ha::mma_pass_kernel<kRev, kDots, Out, kStateOnly>;
     const int smem = (int)ha::MmaLayout<kDots>::end;
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
     const long long grid = pairs * (kStateOnly ? mp.segments - 1 : mp.segments);
     if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
-    fn<<<(unsigned)grid, ha::kMmaThreads, smem, stream>>>(mx, my, mz, mo, mp);
+    fn<<<(unsigned)grid, ha::kMmaThreads, smem, stream>>>(mx, my, mz, mo, mw, mp);
     return launched("mma_pass_kernel");
 }
 
 // What the passes leave for the decay gradients.
 struct Dots {
-    Rows w;
-    float *near, *far;
+    View w;
+    double* near;
+    float* far;
     float4* dump;
     float* cross;
 };
@@ -159,11 +160,13 @@ struct Dots {
 template <bool kRev, bool kDots, class Out>
 hs_status mma_pass(const Pass& ps, const View& x, const View& y, const View& z, uint8_t* ws, uint8_t* space, unsigned long long id,
                    cudaStream_t stream, const Dots* dots = nullptr) {
-    CUtensorMap mx, my, mz, mo;
+    CUtensorMap mx, my, mz, mo, mw;
     const View o{{ps.out, ps.ob, ps.ot, ps.oh, 1}, ps.heads, ps.dz};
     if (sizeof(Out) == 2 && !encode(&mo, o, ps.batch, ps.tokens))
         return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
     if (sizeof(Out) != 2) std::memset(&mo, 0, sizeof mo);  // not read
+    if (!dots) std::memset(&mw, 0, sizeof mw);
+    else if (!encode(&mw, dots->w, ps.batch, ps.tokens)) return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
     if (!encode(&mx, x, ps.batch, ps.tokens) || !encode(&my, y, ps.batch, ps.tokens) || !encode(&mz, z, ps.batch, ps.tokens))
         return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
     ha::MmaPass mp;
@@ -181,17 +184,17 @@ hs_status mma_pass(const Pass& ps, const View& x, const View& y, const View& z, 
     mp.seg_chunks = (int)((chunks + mp.segments - 1) / mp.segments);
     mp.chunks = (int)chunks;
     if (dots) {
-        mp.w = dots->w; mp.dots = dots->near; mp.dots_far = dots->far; mp.dump = dots->dump; mp.cross = dots->cross;
+        mp.wdiv = dots->w.rows.div; mp.dots = dots->near; mp.dots_far = dots->far; mp.dump = dots->dump; mp.cross = dots->cross;
     }
     if (mp.segments > 1) {
         mp.seg_state = reinterpret_cast<float*>(space);
         mp.seg_decay = reinterpret_cast<float*>(space + up256((size_t)pairs * mp.segments * ps.dx * ps.dz * 4));
-        hs_status st = mma_launch<kRev, false, __nv_bfloat16, true>(mx, my, mz, mo, mp, pairs, stream);
+        hs_status st = mma_launch<kRev, false, __nv_bfloat16, true>(mx, my, mz, mo, mw, mp, pairs, stream);
         if (st != HS_OK) return st;
         ha::join_segments_kernel<<<(unsigned)(pairs * ((ps.dx * ps.dz + 255) / 256)), 256, 0, stream>>>(mp);
         if ((st = launched("join_segments_kernel")) != HS_OK) return st;
     }
-    return mma_launch<kRev, kDots, Out, false>(mx, my, mz, mo, mp, pairs, stream);
+    return mma_launch<kRev, kDots, Out, false>(mx, my, mz, mo, mw, mp, pairs, stream);
 }
 
 // The rule for the tensor cores: bf16, head dimensions that TMA can load (multiples of 8, at most 128, 16-byte strides).
@@ -219,7 +222,7 @@ MmaSpace mma_space(const heinsen_attention_problem* p) {
     s.dk = s.dq + (p->q_heads == p->heads ? 0 : up256(rows * p->k_dim * 4));
     s.dv = s.dk + (p->k_heads == p->heads ? 0 : up256(rows * p->k_dim * 4));
     s.dots = s.dv + (p->v_heads == p->heads ? 0 : up256(rows * p->v_dim * 4));
-    s.dump = s.dots + up256(6 * rows * 4);
+    s.dump = s.dots + up256(4 * rows * 8 + 4 * rows * 4);
     s.cross = s.dump + chunks * 65536;
     s.part = s.cross + up256(chunks * 32);
     s.total = s.part + up256(chunks * 8);
@@ -378,21 +381,22 @@ hs_status mma_backward(const heinsen_attention_problem* p, const heinsen_attenti
     }
     const View q = view_of(p->q, p->heads, p->q_heads, p->k_dim), k = view_of(p->k, p->heads, p->k_heads, p->k_dim),
                v = view_of(p->v, p->heads, p->v_heads, p->v_dim);
-    float* dots = reinterpret_cast<float*>(ws + sp.dots);
+    double* near = reinterpret_cast<double*>(ws + sp.dots);  // [pass][half][token]
+    float* far = reinterpret_cast<float*>(near + 4 * rows);
     float4* dump = reinterpret_cast<float4*>(ws + sp.dump);
     float* cross = reinterpret_cast<float*>(ws + sp.cross);
     auto each = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
     {
         Pass ps = common(p);
         ps.s_in = p->state0; ps.s_in_t = 1;
-        const Dots d{q.rows, dots, nullptr, dump, nullptr};
+        const Dots d{q, near, far, dump, nullptr};
         if ((st = gradient<false, kDots>(ps, g, v, k, p, p->q_heads, dq, each(sp.dq), ws, id, stream, kDots ? &d : nullptr)) != HS_OK)
             return st;
     }
     {
         Pass ps = common(p);
         ps.s_in = d_state; ps.s_in_t = 1; ps.s_in_mul = 1.0f / p->scale;  // the scale comes back with the output
-        const Dots d{k.rows, dots + 2 * rows, dots + 4 * rows, dump, cross};
+        const Dots d{k, near + 2 * rows, far + 2 * rows, dump, cross};
         if ((st = gradient<true, kDots>(ps, v, g, q, p, p->k_heads, dk, each(sp.dk), ws, id, stream, kDots ? &d : nullptr)) != HS_OK)
             return st;
     }
@@ -406,7 +410,7 @@ hs_status mma_backward(const heinsen_attention_problem* p, const heinsen_attenti
     const bool fixed = p->log_a.batch_stride == 0 && p->log_a.token_stride == 0;
     double* part = reinterpret_cast<double*>(ws + sp.part);
     ha::join_decay_grad_kernel<<<(unsigned)(pairs * chunks), ha::kChunk, 0, stream>>>(
-        dots, dots + 2 * rows, dots + 4 * rows, cross, static_cast<const float*>(p->log_a.ptr), p->log_a.batch_stride,
+        near, near + 2 * rows, far, far + 2 * rows, cross, static_cast<const float*>(p->log_a.ptr), p->log_a.batch_stride,
         p->log_a.token_stride, p->log_a.head_stride, p->lengths, (int)p->tokens, p->heads, chunks, rows, p->scale,
         fixed ? nullptr : dlog_a, fixed ? part : nullptr);
     if ((st = launched("join_decay_grad_kernel")) != HS_OK || !fixed) return st;

@@ -127,6 +127,7 @@ def test_strides_and_offsets(ha, dtype):
 
 
 def test_gradients_of_views_and_expanded_decays(ha):
+    torch.manual_seed(0)
     b, t, h, d = 2, 100, 2, 64
     fused = torch.randn(b, t, 3, h, d, device=DEV).to(BF16).requires_grad_()
     log_a = (-torch.rand(h, device=DEV)).requires_grad_()
