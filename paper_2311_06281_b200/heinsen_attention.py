@@ -10,10 +10,11 @@ differentiable in every tensor argument (once: their gradients are not different
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
-from .heinsen_scan import HeinsenScanError, _check, _dtype_code, _on_device, _ptr, _stream_ptr, lib as _scan_lib  # noqa: F401
+from .heinsen_scan import HeinsenScanError, _check, _dtype_code, _on_device, lib as _scan_lib  # noqa: F401
 
 EXPORTS = [
     "heinsen_attention_forward", "heinsen_attention_backward", "heinsen_attention_workspace_bytes",
@@ -42,7 +43,44 @@ class _Norms(ctypes.Structure):
                 ("post_weight", ctypes.c_void_p)]
 
 
+_PROBLEM = struct.Struct("@qqiiiiiiif" + "Pqqq" * 4 + "PP")
+_ROWS = struct.Struct("@Pqqq")
+_NORMS = struct.Struct("@qqiiiffPPPPP0q")
+assert (_PROBLEM.size, _ROWS.size, _NORMS.size) == tuple(ctypes.sizeof(t) for t in (_Problem, _Tensor, _Norms))
+
 _lib = None
+_calls = None
+
+
+class _Calls:
+    """The functions once more, taking structures as packed bytes and pointers as integers: filling in ctypes structures
+    field by field costs more than a small call does on the GPU."""
+
+    def __init__(self, L):
+        vp, sz, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64
+
+        def of(name, args, res=ctypes.c_int):
+            f = L[name]
+            f.argtypes, f.restype = args, res
+            return f
+
+        self.forward = of("heinsen_attention_forward", [vp, vp, vp, vp, sz, vp])
+        self.backward = of("heinsen_attention_backward", [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])
+        self.space = of("heinsen_attention_workspace_bytes", [vp, ctypes.c_int], sz)
+        self.step = of("heinsen_attention_step", [vp, vp, vp, i64, vp, vp])
+        self.block_forward = of("heinsen_block_norms_forward", [vp, vp, vp, vp])
+        self.block_backward = of("heinsen_block_norms_backward", [vp] * 9 + [sz, vp])
+        self.block_space = of("heinsen_block_norms_workspace_bytes", [vp], sz)
+        self.gated_forward = of("heinsen_gated_norm_forward", [vp, vp, vp])
+        self.gated_backward = of("heinsen_gated_norm_backward", [vp] * 6 + [sz, vp])
+        self.gated_space = of("heinsen_gated_norm_workspace_bytes", [vp], sz)
+
+
+def _call() -> _Calls:
+    global _calls
+    if _calls is None:
+        _calls = _Calls(lib())
+    return _calls
 
 
 def lib() -> ctypes.CDLL:
@@ -68,14 +106,36 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-def _cuda(name: str, device=None, **tensors):
+def _cuda(name: str, device, **tensors):
     for n, t in tensors.items():
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError(f"{n} must be a CUDA tensor (there is no CPU path)")
-        if device is not None and t.device != device:
+        if t is not None and t.device != device:
             raise ValueError(f"{name}: {n} is on {t.device}, not on {device}")
+
+
+def _on_gpu(t: torch.Tensor, name: str):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor (there is no CPU path)")
+
+
+def _dtype(t: torch.Tensor) -> int:
+    d = t.dtype
+    return 1 if d is torch.bfloat16 else 0 if d is torch.float32 else _dtype_code(t)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _launch(device, fn, *args):
+    """Calls fn(*args, stream) on `device` and its current stream."""
+    index = device.index
+    if index == torch.cuda.current_device():
+        status = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with _on_device(device):
+            status = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if status:
+        _check(status)
 
 
 def _space(nbytes: int, device) -> torch.Tensor:
@@ -86,64 +146,81 @@ def _space(nbytes: int, device) -> torch.Tensor:
 
 def _tensor(t: torch.Tensor, name: str) -> _Tensor:
     """[batch, tokens, heads, dim] of any strides, the last dimension contiguous."""
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    return _Tensor(*_rows(t, name))
+
+
+def _rows(t: torch.Tensor, name: str):
+    s = t.stride()
+    if s[3] != 1 and t.shape[3] > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return _Tensor(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return t.data_ptr(), s[0], s[1], s[2]
 
 
 def _state_ok(t, shape, name):
-    if t is None:
-        return
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype != torch.float32:
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    if t.dtype is not torch.float32:
         raise TypeError(f"{name} must be float32")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
 
 
-def _problem(q, k, v, log_a, state0, scale, lengths) -> _Problem:
+def _heads(h, hq, hk, hv):
+    if hq < 1 or hk < 1 or hv < 1 or h % hq or h % hk or h % hv:
+        raise ValueError(f"the {h} heads of log_a must be a multiple of the heads of q ({hq}), k ({hk}) and v ({hv})")
+
+
+class _Sizes:
+    __slots__ = ("batch", "tokens", "heads", "k_dim", "v_dim", "packed")
+
+
+def _problem(q, k, v, log_a, state0, scale, lengths) -> _Sizes:
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         raise ValueError("q, k, v are [batch, tokens, heads, dim]")
     b, t, hq, kd = q.shape
-    hk, hv, vd = k.shape[2], v.shape[2], v.shape[3]
-    if k.shape[:2] != (b, t) or v.shape[:2] != (b, t) or k.shape[3] != kd:
+    bk, tk, hk, kk = k.shape
+    bv, tv, hv, vd = v.shape
+    if bk != b or bv != b or tk != t or tv != t or kk != kd:
         raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
-    if not (q.dtype == k.dtype == v.dtype):
+    if q.dtype is not k.dtype or q.dtype is not v.dtype:
         raise TypeError("q, k, v must share one dtype")
-    if log_a.dtype != torch.float32:
+    if log_a.dtype is not torch.float32:
         raise TypeError("log_a must be float32")
     if log_a.dim() == 1:
-        h, la = log_a.shape[0], _Tensor(log_a.data_ptr(), 0, 0, log_a.stride(0))
+        h, la = log_a.shape[0], (log_a.data_ptr(), 0, 0, log_a.stride(0))
     elif log_a.dim() == 3 and log_a.shape[:2] == (b, t):
-        h, la = log_a.shape[2], _Tensor(log_a.data_ptr(), *log_a.stride())
+        h, la = log_a.shape[2], (log_a.data_ptr(), *log_a.stride())
     else:
         raise ValueError(f"log_a: expected shape [heads] or {(b, t, 'heads')}, got {tuple(log_a.shape)}")
-    if any(n < 1 or h % n for n in (hq, hk, hv)):
-        raise ValueError(f"the {h} heads of log_a must be a multiple of the heads of q ({hq}), k ({hk}) and v ({hv})")
-    _state_ok(state0, (b, h, kd, vd), "state0")
+    _heads(h, hq, hk, hv)
+    if state0 is not None:
+        _state_ok(state0, (b, h, kd, vd), "state0")
     if lengths is not None and (lengths.dtype != torch.int32 or tuple(lengths.shape) != (b,) or not lengths.is_contiguous()):
         raise ValueError("lengths must be a contiguous int32 tensor [batch]")
-    _cuda("decay_attention", q.device, q=q, k=k, v=v, log_a=log_a, state0=state0, lengths=lengths)
-    return _Problem(b, t, h, hq, hk, hv, kd, vd, _dtype_code(q), scale, _tensor(q, "q"), _tensor(k, "k"), _tensor(v, "v"), la,
-                    state0.data_ptr() if state0 is not None else None, lengths.data_ptr() if lengths is not None else None)
+    _on_gpu(q, "q")
+    _cuda("decay_attention", q.device, k=k, v=v, log_a=log_a, state0=state0, lengths=lengths)
+    p = _Sizes()
+    p.batch, p.tokens, p.heads, p.k_dim, p.v_dim = b, t, h, kd, vd
+    p.packed = _PROBLEM.pack(b, t, h, hq, hk, hv, kd, vd, _dtype(q), scale, *_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), *la,
+                             0 if state0 is None else state0.data_ptr(), 0 if lengths is None else lengths.data_ptr())
+    return p
 
 
-def _attention_forward(p: _Problem, q: torch.Tensor):
+def _attention_forward(p: _Sizes, q: torch.Tensor, workspace: torch.Tensor | None):
     dev = q.device
     o = torch.empty((p.batch, p.tokens, p.heads, p.v_dim), dtype=q.dtype, device=dev)
     state = torch.empty((p.batch, p.heads, p.k_dim, p.v_dim), dtype=torch.float32, device=dev)
-    ws = _space(int(lib().heinsen_attention_workspace_bytes(p, 0)), dev)
-    with _on_device(dev):
-        _check(lib().heinsen_attention_forward(p, _tensor(o, "o"), _ptr(state), _ptr(ws), ws.numel(), _stream_ptr(dev)))
+    call = _call()
+    if workspace is None:
+        workspace = _space(call.space(p.packed, 0), dev)
+    _launch(dev, call.forward, p.packed, _ROWS.pack(*_rows(o, "o")), state.data_ptr(), workspace.data_ptr(), workspace.numel())
     return o, state
 
 
 class _DecayAttention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, log_a, state0, scale, lengths):
-        p = _problem(q, k, v, log_a, state0, scale, lengths)
-        o, state = _attention_forward(p, q)
+    def forward(ctx, q, k, v, log_a, state0, scale, lengths, workspace):
+        o, state = _attention_forward(_problem(q, k, v, log_a, state0, scale, lengths), q, workspace)
         ctx.save_for_backward(q, k, v, log_a, state0, lengths)
         ctx.scale = scale
         ctx.set_materialize_grads(False)
@@ -153,8 +230,11 @@ class _DecayAttention(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_o, d_state):
         q, k, v, log_a, state0, lengths = ctx.saved_tensors
-        p = _problem(q, k, v, log_a, state0, ctx.scale, lengths)
         dev = q.device
+        need_decays = ctx.needs_input_grad[3]
+        if need_decays and log_a.dim() == 3 and log_a.stride(0) == 0 and log_a.stride(1) == 0 and q.numel():
+            log_a = log_a.contiguous()  # an expanded [heads]: its gradient is still asked for every token
+        p = _problem(q, k, v, log_a, state0, ctx.scale, lengths)
         if d_o is None:
             d_o = torch.zeros((p.batch, p.tokens, p.heads, p.v_dim), dtype=q.dtype, device=dev)
         if d_o.shape[-1] > 1 and d_o.stride(-1) != 1:
@@ -162,21 +242,23 @@ class _DecayAttention(torch.autograd.Function):
         if d_state is not None:
             d_state = d_state.contiguous()
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v))
-        dla = torch.empty(log_a.shape, dtype=torch.float32, device=dev) if ctx.needs_input_grad[3] else None
-        if dla is not None and log_a.dim() == 3 and log_a.stride(0) == 0 and log_a.stride(1) == 0 and p.tokens * p.batch:
-            log_a = log_a.contiguous()  # an expanded [heads]: its gradient is still asked for every token
-            p.log_a = _tensor(log_a, "log_a")
+        dla = torch.empty(log_a.shape, dtype=torch.float32, device=dev) if need_decays else None
         ds0 = torch.empty(state0.shape, dtype=torch.float32, device=dev) if ctx.needs_input_grad[4] else None
-        ws = _space(int(lib().heinsen_attention_workspace_bytes(p, 1)), dev)
-        with _on_device(dev):
-            _check(lib().heinsen_attention_backward(p, _tensor(d_o, "d_o"), _ptr(d_state), _ptr(dq), _ptr(dk), _ptr(dv),
-                                                    _ptr(dla), _ptr(ds0), _ptr(ws), ws.numel(), _stream_ptr(dev)))
-        return dq, dk, dv, dla, ds0, None, None
+        call = _call()
+        ws = _space(call.space(p.packed, 1), dev)
+        _launch(dev, call.backward, p.packed, _ROWS.pack(*_rows(d_o, "d_o")), _addr(d_state), dq.data_ptr(), dk.data_ptr(),
+                dv.data_ptr(), _addr(dla), _addr(ds0), ws.data_ptr(), ws.numel())
+        return dq, dk, dv, dla, ds0, None, None, None
+
+
+def workspace(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: torch.Tensor) -> torch.Tensor:
+    """Uninitialised scratch for ``decay_attention`` calls of these shapes, one at a time."""
+    return _space(_call().space(_problem(q, k, v, log_a, None, 1.0, None).packed, 0), q.device)
 
 
 def decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: torch.Tensor,
                     state0: torch.Tensor | None = None, *, scale: float | None = None,
-                    lengths: torch.Tensor | None = None):
+                    lengths: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """Attention with a decay for each head over whole sequences; returns (o, state).  Asynchronous, differentiable.
 
     q [B, T, Hq, K], k [B, T, Hk, K], v [B, T, Hv, V]: float32 or bfloat16, last dimension contiguous, any other strides;
@@ -184,11 +266,14 @@ def decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: to
     state0 [B, H, K, V] float32 continues earlier tokens; lengths [B] int32 ends row b after lengths[b] tokens.
     scale defaults to K ** -0.5.  o [B, T, H, V] has q's dtype, state [B, H, K, V] is float32 (what the next call or
     ``decay_attention_step`` takes).  log_a = -inf forgets the state at that token: packed sequences start so.
+    workspace: scratch from ``workspace()``, kept by the caller; ``heinsen_scan.check(workspace)`` then reports what the
+    device recorded (a bounded wait that ran out).  Without it each call takes its own.
     """
     scale = float(q.shape[-1] ** -0.5 if scale is None else scale)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, log_a, state0)):
-        return _DecayAttention.apply(q, k, v, log_a, state0, scale, lengths)
-    return _attention_forward(_problem(q, k, v, log_a, state0, scale, lengths), q)
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or log_a.requires_grad or
+                                    (state0 is not None and state0.requires_grad)):
+        return _DecayAttention.apply(q, k, v, log_a, state0, scale, lengths, workspace)
+    return _attention_forward(_problem(q, k, v, log_a, state0, scale, lengths), q, workspace)
 
 
 def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: torch.Tensor, state: torch.Tensor, *,
@@ -201,63 +286,83 @@ def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
     """
     if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise ValueError("q, k, v are [batch, heads, dim]")
-    b, kd = q.shape[0], q.shape[2]
-    la = log_a if log_a.dim() == 1 else log_a.unsqueeze(1)
-    p = _problem(q.unsqueeze(1), k.unsqueeze(1), v.unsqueeze(1), la, None, float(kd ** -0.5 if scale is None else scale), None)
-    _state_ok(state, (state.shape[0], p.heads, kd, p.v_dim), "state")
+    b, hq, kd = q.shape
+    bk, hk, kk = k.shape
+    bv, hv, vd = v.shape
+    if bk != b or bv != b or kk != kd:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
+    if q.dtype is not k.dtype or q.dtype is not v.dtype:
+        raise TypeError("q, k, v must share one dtype")
+    if log_a.dtype is not torch.float32:
+        raise TypeError("log_a must be float32")
+    if log_a.dim() == 1:
+        h, ab, ah = log_a.shape[0], 0, log_a.stride(0)
+    elif log_a.dim() == 2 and log_a.shape[0] == b:
+        h, (ab, ah) = log_a.shape[1], log_a.stride()
+    else:
+        raise ValueError(f"log_a: expected shape [heads] or {(b, 'heads')}, got {tuple(log_a.shape)}")
+    _heads(h, hq, hk, hv)
+    n = state.shape[0]
+    _state_ok(state, (n, h, kd, vd), "state")
+    (qb, qh, q1), (kb, kh, k1), (vb, vh, v1) = q.stride(), k.stride(), v.stride()
+    if (q1 != 1 or k1 != 1) and kd > 1 or v1 != 1 and vd > 1:
+        raise ValueError("q, k, v: the last dimension must be contiguous")
     if slots is None:
-        if state.shape[0] < b:
-            raise ValueError(f"state has {state.shape[0]} rows for {b} sequences")
-    elif slots.dtype != torch.int32 or tuple(slots.shape) != (b,) or not slots.is_contiguous():
+        if n < b:
+            raise ValueError(f"state has {n} rows for {b} sequences")
+    elif slots.dtype is not torch.int32 or tuple(slots.shape) != (b,) or not slots.is_contiguous():
         raise ValueError("slots must be a contiguous int32 tensor [batch]")
+    dev = q.device
+    _on_gpu(q, "q")
     if out is None:
-        out = torch.empty((b, p.heads, p.v_dim), dtype=q.dtype, device=q.device)
-    elif tuple(out.shape) != (b, p.heads, p.v_dim) or out.dtype != q.dtype:
-        raise ValueError("out must be [batch, heads, v_dim] of q's dtype")
-    _cuda("decay_attention_step", q.device, state=state, slots=slots, out=out)
-    with _on_device(q.device):
-        _check(lib().heinsen_attention_step(p, _tensor(out.unsqueeze(1), "out"), _ptr(state), state.shape[0], _ptr(slots),
-                                            _stream_ptr(q.device)))
+        out = torch.empty((b, h, vd), dtype=q.dtype, device=dev)
+    elif tuple(out.shape) != (b, h, vd) or out.dtype is not q.dtype or out.stride(2) != 1 and vd > 1:
+        raise ValueError("out must be [batch, heads, v_dim] of q's dtype, the last dimension contiguous")
+    _cuda("decay_attention_step", dev, k=k, v=v, log_a=log_a, state=state, slots=slots, out=out)
+    ob, oh, _ = out.stride()
+    packed = _PROBLEM.pack(b, 1, h, hq, hk, hv, kd, vd, _dtype(q), float(kd ** -0.5 if scale is None else scale),
+                           q.data_ptr(), qb, 0, qh, k.data_ptr(), kb, 0, kh, v.data_ptr(), vb, 0, vh, log_a.data_ptr(), ab, 0, ah, 0, 0)
+    _launch(dev, _call().step, packed, _ROWS.pack(out.data_ptr(), ob, 0, oh), state.data_ptr(), n, _addr(slots))
     return out
 
 
 # ------------------------------------------------------------------------------------------------------------- norms
 
-def _norms_problem(name, x, weight, eps, scale=1.0, branch=None, gate=None, post=None) -> _Norms:
-    dim = x.shape[-1]
+def _norms_problem(name, x, weight, eps, scale=1.0, branch=None, gate=None, post=None) -> bytes:
+    shape, dtype = x.shape, x.dtype
+    dim = shape[-1]
     rows, gate_rows = x.numel() // dim if dim else 0, 1
-    _dtype_code(x)
-    for n, t in (("branch", branch),):
-        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
-            raise ValueError(f"{name}: {n} must have the shape and dtype of x")
+    code = _dtype(x)
+    if branch is not None and (branch.shape != shape or branch.dtype is not dtype):
+        raise ValueError(f"{name}: branch must have the shape and dtype of x")
     if gate is not None:
-        if gate.dtype != x.dtype:
+        if gate.dtype is not dtype:
             raise TypeError(f"{name}: gate must have the dtype of x")
-        if gate.shape != x.shape:
+        if gate.shape != shape:
             # a gate for each sequence: [.., 1, dim] beside [.., tokens, dim]
-            if branch is None or x.dim() < 2 or gate.shape != (*x.shape[:-2], 1, dim):
-                raise ValueError(f"{name}: gate has shape {tuple(gate.shape)} beside {tuple(x.shape)}")
-            gate_rows = x.shape[-2]
+            if branch is None or x.dim() < 2 or gate.shape != (*shape[:-2], 1, dim):
+                raise ValueError(f"{name}: gate has shape {tuple(gate.shape)} beside {tuple(shape)}")
+            gate_rows = max(1, shape[-2])
     for n, t in (("weight", weight), ("post_weight", post)):
-        if t is not None and tuple(t.shape) != (dim,):
+        if t is not None and (t.dim() != 1 or t.shape[0] != dim):
             raise ValueError(f"{name}: {n} must be [{dim}]")
-        if t is not None and t.dtype != torch.float32 and t.dtype != x.dtype:
+        if t is not None and t.dtype is not torch.float32 and t.dtype is not dtype:
             raise TypeError(f"{name}: {n} must be float32 or of x's dtype")
-    if post is not None and post.dtype != weight.dtype:
+    if post is not None and post.dtype is not weight.dtype:
         raise TypeError(f"{name}: both weights must share one dtype")
     for n, t in (("x", x), ("branch", branch), ("gate", gate), ("weight", weight), ("post_weight", post)):
         if t is not None and not t.is_contiguous():
             raise ValueError(f"{name}: {n} must be contiguous")
-    _cuda(name, x.device, x=x, branch=branch, gate=gate, weight=weight, post_weight=post)
-    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    return _Norms(rows, max(1, gate_rows), dim, _dtype_code(x), _dtype_code(weight), scale, eps, ptr(x), ptr(branch), ptr(gate),
-                  ptr(weight), ptr(post))
+    _on_gpu(x, "x")
+    _cuda(name, x.device, branch=branch, gate=gate, weight=weight, post_weight=post)
+    ptr = lambda t: t.data_ptr() if t is not None else 0  # noqa: E731
+    return _NORMS.pack(rows, gate_rows, dim, code, _dtype(weight), scale, eps, x.data_ptr(), ptr(branch), ptr(gate), weight.data_ptr(),
+                       ptr(post))
 
 
-def _block_norms_forward(p: _Norms, x):
+def _block_norms_forward(p: bytes, x):
     r, y = torch.empty_like(x), torch.empty_like(x)
-    with _on_device(x.device):
-        _check(lib().heinsen_block_norms_forward(p, _ptr(r), _ptr(y), _stream_ptr(x.device)))
+    _launch(x.device, _call().block_forward, p, r.data_ptr(), y.data_ptr())
     return r, y
 
 
@@ -266,7 +371,7 @@ class _BlockNorms(torch.autograd.Function):
     def forward(ctx, x, branch, pre, post, gate, scale, eps):
         p = _norms_problem("block_norms", x, pre, eps, scale, branch, gate, post)
         ctx.save_for_backward(x, branch, pre, post, gate)
-        ctx.numbers = (eps, scale)
+        ctx.problem = p  # the saved tensors keep its pointers alive
         ctx.set_materialize_grads(False)
         return _block_norms_forward(p, x)
 
@@ -274,16 +379,15 @@ class _BlockNorms(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_r, d_y):
         x, branch, pre, post, gate = ctx.saved_tensors
-        eps, scale = ctx.numbers
-        p = _norms_problem("block_norms", x, pre, eps, scale, branch, gate, post)
+        p = ctx.problem
         d_y = torch.zeros_like(x) if d_y is None else d_y.contiguous()
         d_r = None if d_r is None else d_r.contiguous()
         new = lambda t: None if t is None else torch.empty_like(t)  # noqa: E731
         dx, dh, dpre, dpost, dgate = new(x), new(branch), new(pre), new(post), new(gate)
-        ws = _space(int(lib().heinsen_block_norms_workspace_bytes(p)), x.device)
-        with _on_device(x.device):
-            _check(lib().heinsen_block_norms_backward(p, _ptr(d_r), _ptr(d_y), _ptr(dx), _ptr(dh), _ptr(dgate), _ptr(dpre),
-                                                      _ptr(dpost), _ptr(ws), ws.numel(), _stream_ptr(x.device)))
+        call = _call()
+        ws = _space(call.block_space(p), x.device)
+        _launch(x.device, call.block_backward, p, _addr(d_r), d_y.data_ptr(), dx.data_ptr(), dh.data_ptr(), _addr(dgate),
+                dpre.data_ptr(), _addr(dpost), ws.data_ptr(), ws.numel())
         return dx, dh, dpre, dpost, dgate, None, None
 
 
@@ -295,35 +399,33 @@ def block_norms(x: torch.Tensor, branch: torch.Tensor, pre_weight: torch.Tensor,
     y = r / sqrt(mean(r^2) + eps) * pre_weight.  x, branch: contiguous [..., dim] of one dtype (float32 or bfloat16);
     gate: as x, or [..., 1, dim] for one gate per sequence; weights [dim], float32 or x's dtype.
     """
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, branch, pre_weight, post_weight, gate)):
+    if torch.is_grad_enabled() and (x.requires_grad or branch.requires_grad or pre_weight.requires_grad or
+                                    (post_weight is not None and post_weight.requires_grad) or
+                                    (gate is not None and gate.requires_grad)):
         return _BlockNorms.apply(x, branch, pre_weight, post_weight, gate, float(scale), float(eps))
-    p = _norms_problem("block_norms", x, pre_weight, float(eps), float(scale), branch, gate, post_weight)
-    return _block_norms_forward(p, x)
+    return _block_norms_forward(_norms_problem("block_norms", x, pre_weight, float(eps), float(scale), branch, gate, post_weight), x)
 
 
 class _GatedNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gate, weight, eps):
-        p = _norms_problem("gated_norm", x, weight, eps, gate=gate)
+        ctx.problem = p = _norms_problem("gated_norm", x, weight, eps, gate=gate)
         ctx.save_for_backward(x, gate, weight)
-        ctx.eps = eps
         y = torch.empty_like(x)
-        with _on_device(x.device):
-            _check(lib().heinsen_gated_norm_forward(p, _ptr(y), _stream_ptr(x.device)))
+        _launch(x.device, _call().gated_forward, p, y.data_ptr())
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_y):
         x, gate, weight = ctx.saved_tensors
-        p = _norms_problem("gated_norm", x, weight, ctx.eps, gate=gate)
         d_y = d_y.contiguous()
         dx, dweight = torch.empty_like(x), torch.empty_like(weight)
         dgate = None if gate is None else torch.empty_like(gate)
-        ws = _space(int(lib().heinsen_gated_norm_workspace_bytes(p)), x.device)
-        with _on_device(x.device):
-            _check(lib().heinsen_gated_norm_backward(p, _ptr(d_y), _ptr(dx), _ptr(dgate), _ptr(dweight), _ptr(ws), ws.numel(),
-                                                     _stream_ptr(x.device)))
+        call = _call()
+        ws = _space(call.gated_space(ctx.problem), x.device)
+        _launch(x.device, call.gated_backward, ctx.problem, d_y.data_ptr(), dx.data_ptr(), _addr(dgate), dweight.data_ptr(),
+                ws.data_ptr(), ws.numel())
         return dx, dgate, dweight, None
 
 
@@ -331,10 +433,9 @@ def gated_norm(x: torch.Tensor, gate: torch.Tensor | None, weight: torch.Tensor,
     """x / sqrt(mean(x^2) + eps) * weight * silu(gate) over the last dimension (a head).  Asynchronous, differentiable.
 
     x, gate: contiguous [..., dim] of one dtype (float32 or bfloat16); gate None: no factor; weight [dim], float32 or x's."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, gate, weight)):
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (gate is not None and gate.requires_grad)):
         return _GatedNorm.apply(x, gate, weight, float(eps))
     p = _norms_problem("gated_norm", x, weight, float(eps), gate=gate)
     y = torch.empty_like(x)
-    with _on_device(x.device):
-        _check(lib().heinsen_gated_norm_forward(p, _ptr(y), _stream_ptr(x.device)))
+    _launch(x.device, _call().gated_forward, p, y.data_ptr())
     return y
