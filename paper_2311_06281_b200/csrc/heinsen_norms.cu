@@ -118,11 +118,11 @@ Norms make(const heinsen_norms_problem* p) {
     return n;
 }
 
-// CTAs of the backward kernels, which stay and sum over their rows.  Every CTA leaves one row of partial sums behind, so
-// there are no more than fill the GPU a few times over: 8 CTAs of 128 threads, 1 of 1024 for each of 148 SMs.
+// CTAs of the backward kernels, which stay and sum over their rows: as many as are resident at once.  Every CTA leaves one row
+// of partial sums behind.
 long long stay(long long rows, const Layout& l) {
     const int threads = std::max(128, l.threads), per_cta = threads / l.threads;
-    const long long most = 148ll * std::max(1, 1024 / threads);
+    const long long most = 148ll * std::max(1, hn::resident(l.vec * l.nv, l.threads));
     return std::max(1ll, std::min(most, (rows + per_cta - 1) / per_cta));
 }
 
@@ -132,12 +132,12 @@ void cut(const heinsen_norms_problem* p, const Layout& l, long long* units, int*
     const bool wide = p->gate && p->gate_rows > 1;
     const long long gates = wide ? p->rows / p->gate_rows : 1, per_gate = wide ? p->gate_rows : p->rows;
     // whole rows of the gate to each CTA where there are enough of them, else each is split
-    long long s = gates >= want ? 1 : std::min(per_gate, (want + gates - 1) / gates);
+    long long s = gates >= want ? 1 : std::min(per_gate, want / gates);
     const long long per_unit = (per_gate + s - 1) / s;
     s = (per_gate + per_unit - 1) / per_unit;  // no empty units
     *splits = (int)s;
     *units = gates * s;
-    *grid = std::min(*units, std::max(want, gates * s <= 2 * want ? gates * s : want));
+    *grid = std::min(*units, want);
 }
 
 size_t block_parts(const heinsen_norms_problem* p, const Layout& l, size_t* gate_at) {
@@ -149,11 +149,18 @@ size_t block_parts(const heinsen_norms_problem* p, const Layout& l, size_t* gate
     return weights + (p->gate && p->gate_rows > 1 ? up256((size_t)units * p->dim * 4) : 0);
 }
 
-hs_status sum_parts(const float* part, long long groups, long long per, int dim, void* out, bool f32, cudaStream_t stream) {
+// One or two (out2 not NULL) sums of the same shape.
+hs_status sum_parts(const float* part, void* out, const float* part2, void* out2, long long groups, long long per, int dim, bool f32,
+                    cudaStream_t stream) {
     const long long grid = groups * ((dim + 31) / 32);
     if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
-    if (f32) hn::sum_parts_kernel<float><<<(unsigned)grid, 256, 0, stream>>>(part, per, dim, static_cast<float*>(out));
-    else hn::sum_parts_kernel<__nv_bfloat16><<<(unsigned)grid, 256, 0, stream>>>(part, per, dim, static_cast<__nv_bfloat16*>(out));
+    const hn::Parts parts{{part, part2}, {out, out2}, per, dim};
+    const dim3 g((unsigned)grid, out2 ? 2 : 1);
+    const bool few = per <= 64;
+    if (f32 && few) hn::sum_parts_kernel<float, 8><<<g, 256, 0, stream>>>(parts);
+    else if (f32) hn::sum_parts_kernel<float, 32><<<g, 1024, 0, stream>>>(parts);
+    else if (few) hn::sum_parts_kernel<__nv_bfloat16, 8><<<g, 256, 0, stream>>>(parts);
+    else hn::sum_parts_kernel<__nv_bfloat16, 32><<<g, 1024, 0, stream>>>(parts);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return hs_internal::cuda_fail("cudaLaunchKernel (sum of parts)", e);
     hs_internal::count_launches(1);
@@ -233,9 +240,10 @@ hs_status heinsen_block_norms_backward(const heinsen_norms_problem* p, const voi
     n.part_gate = n.part_pre + gate_at / 4;
     const int threads = std::max(128, l.threads), sub = threads / l.threads;
     st = launch(kernel_for(kBlockBackward, l, f32), n, grid, threads, sub > 1 ? (size_t)sub * p->dim * 4 : 0, stream);
-    if (st == HS_OK) st = sum_parts(n.part_pre, 1, grid, p->dim, dpre, w32, stream);
-    if (st == HS_OK && p->post_weight) st = sum_parts(n.part_post, 1, grid, p->dim, dpost, w32, stream);
-    if (st == HS_OK && wide) st = sum_parts(n.part_gate, p->rows / p->gate_rows, n.splits, p->dim, dgate, f32, stream);
+    if (st == HS_OK)
+        st = sum_parts(n.part_pre, dpre, n.part_post, p->post_weight ? dpost : nullptr, 1, grid, p->dim, w32, stream);
+    if (st == HS_OK && wide)
+        st = sum_parts(n.part_gate, dgate, nullptr, nullptr, p->rows / p->gate_rows, n.splits, p->dim, f32, stream);
     return st;
 }
 
@@ -272,7 +280,7 @@ hs_status heinsen_gated_norm_backward(const heinsen_norms_problem* p, const void
     const long long grid = stay(p->rows, l);
     const int threads = std::max(128, l.threads), sub = threads / l.threads;
     st = launch(kernel_for(kGatedBackward, l, f32), n, grid, threads, sub > 1 ? (size_t)sub * p->dim * 4 : 0, stream);
-    if (st == HS_OK) st = sum_parts(n.part_pre, 1, grid, p->dim, dweight, w32, stream);
+    if (st == HS_OK) st = sum_parts(n.part_pre, dweight, nullptr, nullptr, 1, grid, p->dim, w32, stream);
     return st;
 }
 

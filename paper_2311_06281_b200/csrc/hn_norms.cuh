@@ -12,6 +12,13 @@ namespace hn {
 // at most 16 bytes aligned: float32 weights and sums beside 8 bf16 elements are read as two 16-byte halves
 template <class T, int kVec> struct alignas(sizeof(T) * kVec < 16 ? sizeof(T) * kVec : 16) Vec { T v[kVec]; };
 
+// CTAs of a backward kernel that shall be resident on an SM beside one another: 768 threads where a thread has 8 elements of a
+// row (84 registers each), so that there are rows in flight while others are at their barriers.
+__host__ __device__ constexpr int resident(int elems, int row_threads) {
+    const int threads = row_threads < 128 ? 128 : row_threads;
+    return threads * 2 > 1024 ? 1 : (elems > 8 ? 512 : 768) / threads;
+}
+
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 template <class T> __device__ __forceinline__ T from_f(float v);
@@ -104,7 +111,8 @@ __device__ __forceinline__ float norm_back(float d, float n, float mean, float r
     return dim == 1 ? rs * d * (eps * rs * rs) : rs * fmaf(-n, mean, d);
 }
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.0f / (1.0f + __expf(-z)); }
+// one exponential and one reciprocal, each good to about an ulp
+__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
 template <class T, int kVec, int kNv, int kRowThreads>
 __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) block_norms_forward_kernel(const Norms p) {
@@ -154,7 +162,7 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) block_n
 // gate).  A CTA takes a contiguous run of units and keeps the weights' sums over all of them; only the gate's sum starts
 // anew with each unit.
 template <class T, int kVec, int kNv, int kRowThreads>
-__global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) block_norms_backward_kernel(const Norms p) {
+__global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, resident(kVec * kNv, kRowThreads)) block_norms_backward_kernel(const Norms p) {
     using S = Slice<T, kVec, kNv, kRowThreads>;
     constexpr int kE = S::kElems, kRowsPerCta = kRowThreads < 128 ? 128 / kRowThreads : 1;
     __shared__ float red[3 * 64];
@@ -301,7 +309,7 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) gated_n
 }
 
 template <class T, int kVec, int kNv, int kRowThreads>
-__global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) gated_norm_backward_kernel(const Norms p) {
+__global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, resident(kVec * kNv, kRowThreads)) gated_norm_backward_kernel(const Norms p) {
     using S = Slice<T, kVec, kNv, kRowThreads>;
     constexpr int kE = S::kElems, kRowsPerCta = kRowThreads < 128 ? 128 / kRowThreads : 1;
     __shared__ float red[3 * 64];
@@ -360,21 +368,33 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) gated_n
     }
 }
 
-// out[g, c] = sum over the `per` rows of part that belong to g; a CTA has 32 columns, 8 warps share the rows in a fixed order.
-template <class T>
-__global__ void __launch_bounds__(256) sum_parts_kernel(const float* part, long long per, int dim, T* out) {
-    __shared__ float s_part[8][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tiles = (dim + 31) / 32;
+// out[g, c] = sum over the `per` rows of part that belong to g; a CTA has 32 columns, its warps share the rows in a fixed
+// order (32 of them, or 8 where there are few rows).  Two such sums of one shape go in one launch (blockIdx.y).
+struct Parts {
+    const float* part[2];
+    void* out[2];
+    long long per;
+    int dim;
+};
+template <class T, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps) sum_parts_kernel(const Parts p) {
+    __shared__ float s_part[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tiles = (p.dim + 31) / 32;
     const int c = blockIdx.x % tiles * 32 + lane;
     const long long g = blockIdx.x / tiles;
+    const float* part = p.part[blockIdx.y];
     float s = 0.0f;
-    if (c < dim)
-        for (long long i = warp; i < per; i += 8) s += part[(g * per + i) * dim + c];
+    if (c < p.dim) {
+#pragma unroll 4
+        for (long long i = warp; i < p.per; i += kWarps) s += part[(g * p.per + i) * p.dim + c];
+    }
     s_part[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && c < dim) {
-        for (int i = 1; i < 8; ++i) s += s_part[i][lane];
-        out[g * dim + c] = from_f<T>(s);
+    for (int w = warp; w < 32; w += kWarps) {  // a column each
+        s = lane < kWarps ? s_part[lane][w] : 0.0f;
+        for (int o = kWarps / 2; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+        const int col = blockIdx.x % tiles * 32 + w;
+        if (lane == 0 && col < p.dim) static_cast<T*>(p.out[blockIdx.y])[g * p.dim + col] = from_f<T>(s);
     }
 }
 
