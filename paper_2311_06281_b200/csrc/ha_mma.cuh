@@ -7,8 +7,8 @@
 //                                               tensor core transposes, the threads scale by the weights w_j and write the
 //                                               A operand back, no shared memory is spent on it
 // Warps 0-7 own the rows of P and out (two threads to a row), warps 8-15 the rows of S^T (likewise); the two chains meet only
-// in S.  One warp of the last four loads (TMA, two chunks ahead) and sums the decays, one thread of another issues the
-// products.
+// in S.  Of the last four warps one loads (TMA, two chunks ahead), one sums the decays, and one thread of each of the others
+// issues the products of a chain.
 //
 // Rounding.  A float32 factor enters a product as bf16 terms: w Z (and so the state, which is float32 to its owner) as three,
 // 24 bits, exact to float32's own rounding; P and the state in X S as one, where only the bf16 output depends on them (its own
@@ -30,9 +30,9 @@ namespace ha {
 constexpr int kChunk = 128;
 constexpr int kMmaThreads = 640;
 // Registers of a thread: 96 at launch (65536 over 20 warps); those that the feeding warps and the rows of out can spare go to
-// the rows of the state.  64 + 2 * 80 + 2 * 128 = 480 for a thread of each warpgroup, 5 * 96 as at launch.
-constexpr int kFeedRegs = 64;
-constexpr int kRowRegs = 80, kStateRegs = 128;
+// the rows of the state.  80 + 2 * 64 + 2 * 136 = 480 for a thread of each warpgroup, 5 * 96 as at launch.
+constexpr int kFeedRegs = 80;
+constexpr int kRowRegs = 64, kStateRegs = 136;
 constexpr uint32_t kTile = 128 * 256;        // 128 rows of 128 bf16: two blocks of 64 columns, 128-byte swizzle
 constexpr uint32_t kBlock = kTile / 2;
 constexpr uint32_t kSpin = 1u << 20;         // polls of a barrier before a wait gives up (about a microsecond each)
@@ -78,11 +78,12 @@ template <bool kDots>
 struct MmaLayout {
     static constexpr int kTerms = kDots ? 2 : 1;               // of the state in X S
     static constexpr int kWeightsAtOnce = kDots ? 2 : 3;       // terms of w Z in the first product; the third follows
-    // Stages.  A chunk's output leaves from its X tile, where X has two, else from its Y tile.
+    // Stages.  A chunk's output leaves by TMA from its Z tile, the one that the next chunk needs last, or from its Y tile where Z
+    // has one stage.  (Stores of a thread's own row took 2200 clocks a chunk instead of 760.)
     static constexpr int kXs = kDots ? 1 : 2, kYs = 2, kZs = kDots ? 1 : 2, kWs = kDots ? 1 : 0;
     static constexpr uint32_t x = 0, y = x + kXs * kTile, z = y + kYs * kTile, w = z + kZs * kTile, s = w + kWs * kTile,
                               ident = s + kTerms * kTile, decays = ident + 512, whole = decays + 4 * kChunk * 4, bars = whole + 32,
-                              end = bars + 8 * 36;
+                              end = bars + 8 * 38;
     // Tensor memory columns, all 512.  What is read out before the next product of its chain is due shares columns with it:
     // Z^T with the state's update, the scores with the output.
     static constexpr uint32_t tw = 0;                          // the terms of (w Z)^T: A operand
@@ -92,7 +93,7 @@ struct MmaLayout {
     static constexpr uint32_t tt = tp + 64;                    // half of w Z^T (kDots)
     static_assert(tt + (kDots ? 64 : 0) == 512, "tensor memory");
     static __device__ __forceinline__ uint32_t staged(uint32_t base, int it) {
-        return base + (kDots ? y + it % kYs * kTile : x + it % kXs * kTile);
+        return base + (kDots ? y + it % kYs * kTile : z + it % kZs * kTile);
     }
     // where 16 tokens q, and term t of them, lie
     static __device__ __forceinline__ constexpr uint32_t prob(int q) { return tp + 8 * q; }
@@ -102,8 +103,12 @@ struct MmaLayout {
 // Every barrier completes one phase per chunk (those with two entries: per chunk that uses the entry), and nobody who waits
 // for a phase can be overtaken by the next: it needs something of the waiter's own.
 enum Bar : int { kFullX = 0, kFullY = 2, kFullZ = 4, kFreeX = 6, kFreeY = 8, kFreeZ = 10, kPatchY = 12, kPatchZ, kDecays, kDecaysFree, kScores,
-                 kTransposed, kProbs, kFar, kFarRead, kNear, kStaged, kWeighted, kWeightedLast, kUpdateFirst, kUpdate, kUpdateRead,
-                 kStateReady, kFullW, kFreeW, kHalfRead, kHalf, kYDone, kDrain = kYDone + 2, kBars };
+                 kTransposed, kProbs, kFar, kFarRead, kNear, kOutRead, kWeighted, kWeightedLast, kUpdateFirst, kUpdate, kUpdateRead,
+                 kStateReady, kFullW, kFreeW, kHalfRead, kHalf, kTileDone, kDrain = kTileDone + 2,
+                 kBars = kDrain + 2 };
+static_assert(kBars <= 38, "barriers");
+
+template <int kValue> struct Int { static constexpr int value = kValue; };
 
 struct Waiter {
     uint32_t bars;
@@ -137,18 +142,19 @@ __device__ __forceinline__ pair add_dot(pair sum, const uint32_t (&v)[16], const
     for (int i = 0; i < 8; ++i) sum = fma2(make_pair2(w[i] << 16, w[i] & 0xffff0000u), make_pair2(v[2 * i], v[2 * i + 1]), sum);
     return sum;
 }
-// Sixteen columns of one row, or the n that are left of it
-__device__ __forceinline__ void store_row16(float* to, const float (&v)[16], int n) {
+// Sixteen columns of one row, or the n (a multiple of 8) that are left of it
+__device__ __forceinline__ void store16(float* to, const uint32_t (&v)[16], int n) {
 #pragma unroll
     for (int i = 0; i < 16; i += 4)
-        if (i < n) *reinterpret_cast<float4*>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        if (i < n) *reinterpret_cast<uint4*>(to + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
 }
-__device__ __forceinline__ void store_row16(__nv_bfloat16* to, const float (&v)[16], int n) {
+__device__ __forceinline__ void store16(__nv_bfloat16* to, const uint32_t (&v)[16], int n) {
 #pragma unroll
     for (int i = 0; i < 16; i += 8)
         if (i < n)
             *reinterpret_cast<uint4*>(to + i) =
-                make_uint4(pack_bf16(v[i], v[i + 1]), pack_bf16(v[i + 2], v[i + 3]), pack_bf16(v[i + 4], v[i + 5]), pack_bf16(v[i + 6], v[i + 7]));
+                make_uint4(pack_bf16(make_pair2(v[i], v[i + 1])), pack_bf16(make_pair2(v[i + 2], v[i + 3])),
+                           pack_bf16(make_pair2(v[i + 4], v[i + 5])), pack_bf16(make_pair2(v[i + 6], v[i + 7])));
 }
 
 template <bool kRev, bool kDots, class Out, bool kStateOnly>
@@ -183,10 +189,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i) {
             uint32_t arrivals = 1;
-            if (i >= kFreeY && i < kPatchY) arrivals = kStateOnly ? 1 : kDots && i < kFreeZ ? 3 : 2;
+            if (i >= kFreeY && i < kFreeZ) arrivals = kStateOnly ? 1 : kDots ? 3 : 2;
+            if (i >= kFreeZ && i < kPatchY) arrivals = kDots ? 2 : 1;
             if (i == kDecays) arrivals = 32;
             if (i == kDecaysFree) arrivals = kStateOnly ? 256 : 512;
-            if (i == kProbs || i == kFarRead || i == kStaged || i == kWeighted || i == kWeightedLast || i == kHalfRead || i == kUpdateRead ||
+            if (i == kProbs || i == kFarRead || i == kOutRead || i == kWeighted || i == kWeightedLast || i == kHalfRead || i == kUpdateRead ||
                 i == kStateReady)
                 arrivals = 256;
             if (i == kFreeW) arrivals = 257;
@@ -211,8 +218,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
 
     if (warp >= 16) {
         give_registers<kFeedRegs>();
-        // The issuing thread shares a scheduler with the rows that have least to do: the first 32 (reversed: the last)
-        constexpr int kIssuer = kRev ? 19 : 16, kStorer = kRev ? 16 : 19, kLoader = 17, kDecayer = 18;
+        // The thread that issues the output's products shares a scheduler with the rows that have least to do: the first 32
+        // (reversed: the last)
+        constexpr int kOutIssuer = kRev ? 19 : 16, kStateIssuer = kRev ? 16 : 19, kLoader = 17, kDecayer = 18;
         if (warp == kLoader) {
             // ------------------------------------------------------------ loads
             auto load = [&](const CUtensorMap* m, uint32_t to, int dim, int head, int t0, int full) {
@@ -221,29 +229,29 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 if (dim > 64) tma_load_4d(to + kBlock, m, 64, head, t0, b, bars + 8 * full);
             };
             bool ok = true;
-            int loads = 0, loads_w = 0;
+            int loads_x = 0, loads_y = 0, loads_z = 0, loads_w = 0;
             for (int it = 0; it < count && ok; ++it) {
                 const int t0 = chunk_at(it) * kChunk;
                 // tokens behind the sequence's end are in memory and may hold anything: 0 * NaN must not reach a sum
                 const bool patch = live < p.tokens && t0 + kChunk > live;
                 const uint32_t Y = base + L::y + it % L::kYs * kTile, Z = base + L::z + it % L::kZs * kTile;
-                if (lane == 0) {
-                    if (!kStateOnly) {
-                        if (it >= L::kXs) ok = wait(kFreeX + it % L::kXs, it / L::kXs - 1);
-                        if (ok) load(&mx, base + L::x + it % L::kXs * kTile, p.dx, h / p.xdiv, t0, kFullX + it % L::kXs);
-                    }
-                    if (ok && it >= L::kYs) ok = wait(kFreeY + it % L::kYs, it / L::kYs - 1);
+                if (lane == 0) {  // in the order in which tiles become free
+                    if (it >= L::kYs) ok = wait(kFreeY + it % L::kYs, it / L::kYs - 1);
                     if (ok) load(&my, Y, p.dx, h / p.ydiv, t0, patch ? kPatchY : kFullY + it % L::kYs);
-                    if (ok && it >= L::kZs) ok = wait(kFreeZ + it % L::kZs, it / L::kZs - 1);
-                    if (ok) {
-                        load(&mz, Z, p.dz, h / p.zdiv, t0, patch ? kPatchZ : kFullZ + it % L::kZs);
-                        loads = it + 1;
+                    if (ok) loads_y = it + 1;
+                    if (!kStateOnly) {
+                        if (ok && it >= L::kXs) ok = wait(kFreeX + it % L::kXs, it / L::kXs - 1);
+                        if (ok) load(&mx, base + L::x + it % L::kXs * kTile, p.dx, h / p.xdiv, t0, kFullX + it % L::kXs);
+                        if (ok) loads_x = it + 1;
                     }
                     if (kDots) {
                         if (ok && it >= 1) ok = wait(kFreeW, it - 1);
                         if (ok) load(&mw, base + L::w, p.dz, h / p.wdiv, t0, kFullW);
                         if (ok) loads_w = it + 1;
                     }
+                    if (ok && it >= L::kZs) ok = wait(kFreeZ + it % L::kZs, it / L::kZs - 1);
+                    if (ok) load(&mz, Z, p.dz, h / p.zdiv, t0, patch ? kPatchZ : kFullZ + it % L::kZs);
+                    if (ok) loads_z = it + 1;
                 }
                 if (patch) {
                     ok = __shfl_sync(~0u, (int)ok, 0);
@@ -262,17 +270,17 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                         bar_arrive(bars + 8 * (kFullZ + it % L::kZs));
                     }
                 }
+                ok = __shfl_sync(~0u, (int)ok, 0);
             }
             if (*stop && lane == 0) {  // nothing may land in shared memory after the CTA has left
-                auto drain = [&](int full, int stages) {
+                auto drain = [&](int full, int stages, int loads) {
                     for (int it = max(0, loads - stages); it < loads; ++it)
                         for (uint32_t i = 0; i < kSpin / 16 && !bar_try(bars + 8 * (full + it % stages), (it / stages) & 1); ++i) {}
                 };
-                if (!kStateOnly) drain(kFullX, L::kXs);
-                drain(kFullY, L::kYs);
-                drain(kFullZ, L::kZs);
-                loads = loads_w;
-                if (kDots) drain(kFullW, 1);
+                drain(kFullY, L::kYs, loads_y);
+                drain(kFullZ, L::kZs, loads_z);
+                if (kDots) drain(kFullW, 1, loads_w);
+                if (!kStateOnly) drain(kFullX, L::kXs, loads_x);
             }
         } else if (warp == kDecayer) {
             // ------------------------------------------------------------ decays, a lane has four tokens
@@ -328,152 +336,136 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 bar_arrive(bars + 8 * kDecays);
             }
             if (kStateOnly && lane == 0) p.seg_decay[bh * p.segments + segment] = ex2((float)total);
-        } else if (warp == kStorer) {
-            // ------------------------------------------------------------ the output leaves by TMA
-            if (!kStateOnly && lane == 0) {
+        } else if (warp == kStateIssuer) {
+            // ------------------------------------------------------------ the products of the state's chain: Z^T; its update
+            // Two warps issue, one for each chain, and wait for one barrier at a time: a thread that watched both chains took
+            // 600 clocks from a barrier to the last of eight products.  Nearly all that a product takes is a constant (measured:
+            // 20 to 30 clocks for a product's issue so, 48 to 110 with every operand in a register; the tensor core needs 30
+            // to 64).
+            if (elect_one()) {
+                const uint32_t shape_t = mma_shape(16, kColMajorA), shape_u = mma_shape((p.dx + 15) / 16 * 16, kColMajorB);
                 bool ok = true;
-                for (int it = 0; it < count && ok; ++it) {
-                    if (!(ok = wait(kStaged, it))) break;
-                    if constexpr (sizeof(Out) == 2) {
-                        const uint32_t from = L::staged(base, it);
-                        tma_store_4d(&mo, 0, h, chunk_at(it) * kChunk, b, from);
-                        if (p.dz > 64) tma_store_4d(&mo, 64, h, chunk_at(it) * kChunk, b, from + kBlock);
-                        tma_store_commit();
-                        tma_store_wait_read();
+                for (int it = 0; it < count; ++it) {
+                    const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32), zs = it % L::kZs, ys = it % L::kYs;
+                    const uint32_t zo = operand(base + L::z + zs * kTile, kBlock), yo = operand(base + L::y + ys * kTile, kBlock),
+                                   ident = operand(base + L::ident, 256);
+                    ok = wait(kFullZ + zs, it / L::kZs) && (it == 0 || wait(kUpdateRead, it - 1));
+                    if (!ok) break;
+                    tmem_after_sync();
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (q < steps) mma_ss<plain_layout(128)>(tmem + L::tz + 16 * q, zo + q * 128, ident, shape_t, false);
+                    mma_commit(bars + 8 * kTransposed);
+                    if (kDots || kStateOnly) mma_commit(bars + 8 * (kFreeZ + zs));
+                    else mma_commit(bars + 8 * (kTileDone + zs));
+                    if (!(ok = wait(kFullY + ys, it / L::kYs) && wait(kWeighted, it))) break;
+                    tmem_after_sync();
+#pragma unroll
+                    for (int t = 0; t < L::kWeightsAtOnce; ++t)
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (q < steps) mma_ts(tmem + L::weighted(q, t), yo + q * 128, shape_u, q + t > 0, tmem + L::tz);
+                    if (L::kWeightsAtOnce == 2) {
+                        mma_commit(bars + 8 * kUpdateFirst);
+                        if (!(ok = wait(kWeightedLast, it))) break;
+                        tmem_after_sync();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (q < steps) mma_ts(tmem + L::weighted(q, 0), yo + q * 128, shape_u, true, tmem + L::tz);
                     }
-                    bar_arrive(bars + 8 * (kDots ? kFreeY + it % L::kYs : kFreeX + it % L::kXs));
+                    mma_commit(bars + 8 * kUpdate);
+                    mma_commit(bars + 8 * (kFreeY + ys));
+                    if (kDots) mma_commit(bars + 8 * (kTileDone + ys));
                 }
-                tma_store_wait_all();
+                if (!ok) {
+                    mma_commit(bars + 8 * kDrain);
+                    for (uint32_t i = 0; i < kSpin / 16 && !bar_try(bars + 8 * kDrain, 0); ++i) {}
+                }
             }
-        } else if (warp == kIssuer) {
-            // ------------------------------------------------------------ the products
-            // Two chains share the tensor core, output (X Y^T; X S; P Z) and state (Z^T; its update); one thread watches
-            // the barriers of both and issues what is ready.  Nearly all that a product takes is a constant: what has to be
-            // computed between two products delays them (measured: 20 to 30 clocks for a product's issue so, 48 to 110 with
-            // every operand in a register; the tensor core needs 30 to 64).
+            __syncwarp();
+        } else if (!kStateOnly && warp == kOutIssuer) {
+            // ------------------------------------------------------------ the products of the output's chain: X Y^T (w Z^T in
+            // two halves); X S; P Z.  The output leaves in between.
             if (elect_one()) {
                 const int kx = (p.dx + 15) / 16;
                 const uint32_t nz = (p.dz + 15) / 16 * 16;
-                const uint32_t shape_p = mma_shape(128, 0), shape_t = mma_shape(16, kColMajorA), shape_f = mma_shape(nz, 0),
-                               shape_n = mma_shape(nz, kColMajorB), shape_u = mma_shape(16 * kx, kColMajorB);
-                auto ready = [&](int bar, int turn) { return bar_test(bars + 8 * bar, turn & 1); };
+                const uint32_t shape_p = mma_shape(128, 0), shape_f = mma_shape(nz, 0), shape_n = mma_shape(nz, kColMajorB);
+                const uint32_t so = operand(base + L::s, kBlock);
                 auto k_step = [](int kk) { return (uint32_t)((kk >> 2) * (kBlock >> 4) + (kk & 3) * 2); };  // 32 bytes, then the next block
-                // w Z^T for 64 of the chunk's tokens as columns
-                auto half_scores = [&](int half) {
+                auto half_scores = [&](int half) {  // w Z^T for 64 of the chunk's tokens as columns
                     const uint32_t wo = operand(base + L::w, kBlock), zo = operand(base + L::z, kBlock) + half * (64 * 128 >> 4);
 #pragma unroll
                     for (int kk = 0; kk < 8; ++kk)
                         if (16 * kk < p.dz) mma_ss(tmem + L::tt, wo + k_step(kk), zo + k_step(kk), mma_shape(64, 0), kk > 0);
                 };
-                int a_it = kStateOnly ? count : 0, a_step = 0, b_it = 0, b_step = 0;
-                uint32_t idle = 0;
-                while (a_it < count || b_it < count) {
-                    bool moved = false;
-                    if (b_it < count) {
-                        const int it = b_it, steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32), zs = it % L::kZs, ys = it % L::kYs;
-                        if (b_step == 0) {
-                            if (ready(kFullZ + zs, it / L::kZs) && (it == 0 || ready(kUpdateRead, it - 1))) {
-                                tmem_after_sync();
-                                const uint32_t zo = operand(base + L::z + zs * kTile, kBlock), ident = operand(base + L::ident, 256);
-#pragma unroll
-                                for (int q = 0; q < 8; ++q)
-                                    if (q < steps) mma_ss<plain_layout(128)>(tmem + L::tz + 16 * q, zo + q * 128, ident, shape_t, false);
-                                mma_commit(bars + 8 * kTransposed);
-                                mma_commit(bars + 8 * (kFreeZ + zs));
-                                b_step = 1;
-                                moved = true;
-                            }
-                        } else if (b_step == 1 ? ready(kWeighted, it) && ready(kFullY + ys, it / L::kYs) : ready(kWeightedLast, it)) {
-                            tmem_after_sync();
-                            const uint32_t yo = operand(base + L::y + ys * kTile, kBlock);
-                            if (L::kWeightsAtOnce == 3 || b_step == 1) {
-#pragma unroll
-                                for (int t = 0; t < L::kWeightsAtOnce; ++t)
-#pragma unroll
-                                    for (int q = 0; q < 8; ++q)
-                                        if (q < steps) mma_ts(tmem + L::weighted(q, t), yo + q * 128, shape_u, q + t > 0, tmem + L::tz);
-                            } else {
-#pragma unroll
-                                for (int q = 0; q < 8; ++q)
-                                    if (q < steps) mma_ts(tmem + L::weighted(q, 0), yo + q * 128, shape_u, true, tmem + L::tz);
-                            }
-                            if (L::kWeightsAtOnce == 2 && b_step == 1) {
-                                mma_commit(bars + 8 * kUpdateFirst);
-                                b_step = 2;
-                            } else {
-                                mma_commit(bars + 8 * kUpdate);
-                                mma_commit(bars + 8 * (kFreeY + ys));
-                                if (kDots) mma_commit(bars + 8 * (kYDone + ys));
-                                b_step = 0;
-                                ++b_it;
-                            }
-                            moved = true;
-                        }
+                auto send = [&](int it) {  // a chunk's output is in shared memory
+                    if constexpr (sizeof(Out) == 2) {
+                        const uint32_t from = L::staged(base, it);
+                        tma_store_4d(&mo, 0, h, chunk_at(it) * kChunk, b, from);
+                        if (p.dz > 64) tma_store_4d(&mo, 64, h, chunk_at(it) * kChunk, b, from + kBlock);
+                        tma_store_commit();
                     }
-                    if (a_it < count) {
-                        const int it = a_it, xs = it % L::kXs, ys = it % L::kYs, zs = it % L::kZs;
-                        const uint32_t xo = operand(base + L::x + xs * kTile, kBlock);
-                        if (a_step == 0) {
-                            if (ready(kFullX + xs, it / L::kXs) && ready(kFullY + ys, it / L::kYs) && (it == 0 || ready(kStaged, it - 1)) &&
-                                (!kDots || (ready(kFullZ, it) && ready(kFullW, it)))) {
-                                tmem_after_sync();
-                                const uint32_t yo = operand(base + L::y + ys * kTile, kBlock);
+                };
+                auto sent = [&](int it) {  // ... and has been read from there
+                    if constexpr (sizeof(Out) == 2) tma_store_wait_read();
+                    bar_arrive(bars + 8 * (kDots ? kFreeY + it % L::kYs : kFreeZ + it % L::kZs));
+                };
+                auto chunk = [&](int it, auto odd) {  // a copy for each stage: their addresses are constants
+                    constexpr int xs = odd.value % L::kXs, ys = odd.value % L::kYs, zs = odd.value % L::kZs;
+                    const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32);
+                    const uint32_t xo = operand(base + L::x + xs * kTile, kBlock), yo = operand(base + L::y + ys * kTile, kBlock),
+                                   zo = operand(base + L::z + zs * kTile, kBlock);
+                    if (!(wait(kFullX + xs, it / L::kXs) && wait(kFullY + ys, it / L::kYs) &&
+                          (!kDots || (wait(kFullZ, it) && wait(kFullW, it))) && (it == 0 || wait(kOutRead, it - 1))))
+                        return false;
+                    tmem_after_sync();
 #pragma unroll
-                                for (int kk = 0; kk < 8; ++kk)
-                                    if (kk < kx) mma_ss(tmem + L::to, xo + k_step(kk), yo + k_step(kk), shape_p, kk > 0);
-                                if (kDots) half_scores(0);
-                                mma_commit(bars + 8 * kScores);
-                                mma_commit(bars + 8 * (kFreeY + ys));
-                                a_step = kDots ? 4 : 1;
-                                moved = true;
-                            }
-                        } else if (kDots && a_step == 4) {
-                            if (ready(kHalfRead, it)) {
-                                tmem_after_sync();
-                                half_scores(1);
-                                mma_commit(bars + 8 * kHalf);
-                                mma_commit(bars + 8 * kFreeW);
-                                a_step = 1;
-                                moved = true;
-                            }
-                        } else if (a_step == 1) {
-                            if (ready(kProbs, it) && ready(kStateReady, it)) {
-                                tmem_after_sync();
-                                const uint32_t so = operand(base + L::s, kBlock);
-#pragma unroll
-                                for (int t = kTerms - 1; t >= 0; --t)  // small terms first: every addition rounds the sum so far
-#pragma unroll
-                                    for (int kk = 0; kk < 8; ++kk)
-                                        if (kk < kx)
-                                            mma_ss(tmem + L::to, xo + k_step(kk), so + t * (kTile >> 4) + k_step(kk), shape_f,
-                                                   t < kTerms - 1 || kk > 0);
-                                mma_commit(bars + 8 * kFar);
-                                if (kDots) mma_commit(bars + 8 * (kFreeX + xs));
-                                a_step = 2;
-                                moved = true;
-                            }
-                        } else if (ready(kFarRead, it) && ready(kFullZ + zs, it / L::kZs)) {
-                            tmem_after_sync();
-                            const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32);
-                            const uint32_t zo = operand(base + L::z + zs * kTile, kBlock);
-#pragma unroll
-                            for (int q = 0; q < 8; ++q)
-                                if (q < steps) mma_ts(tmem + L::prob(q), zo + q * 128, shape_n, true, tmem + L::to);
-                            mma_commit(bars + 8 * kNear);
-                            mma_commit(bars + 8 * (kFreeZ + zs));
-                            a_step = 0;
-                            ++a_it;
-                            moved = true;
-                        }
+                    for (int kk = 0; kk < 8; ++kk)
+                        if (kk < kx) mma_ss(tmem + L::to, xo + k_step(kk), yo + k_step(kk), shape_p, kk > 0);
+                    if (kDots) half_scores(0);
+                    mma_commit(bars + 8 * kScores);
+                    mma_commit(bars + 8 * (kFreeY + ys));
+                    if (it > 0) {
+                        send(it - 1);
+                        sent(it - 1);
                     }
-                    idle = moved ? 0 : idle + 1;
-                    if (idle >= 16 * kSpin) *stop = 1 + kBars;
-                    if ((idle & 1023) == 1023 && *stop) break;
+                    if (kDots) {
+                        if (!wait(kHalfRead, it)) return false;
+                        tmem_after_sync();
+                        half_scores(1);
+                        mma_commit(bars + 8 * kHalf);
+                        mma_commit(bars + 8 * kFreeW);
+                    }
+                    if (!(wait(kStateReady, it) && wait(kProbs, it))) return false;
+                    tmem_after_sync();
+#pragma unroll
+                    for (int t = kTerms - 1; t >= 0; --t)  // small terms first: every addition rounds the sum so far
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)
+                            if (kk < kx)
+                                mma_ss(tmem + L::to, xo + k_step(kk), so + t * (kTile >> 4) + k_step(kk), shape_f, t < kTerms - 1 || kk > 0);
+                    mma_commit(bars + 8 * kFar);
+                    mma_commit(bars + 8 * (kFreeX + xs));
+                    if (!(wait(kFullZ + zs, it / L::kZs) && wait(kFarRead, it))) return false;
+                    tmem_after_sync();
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (q < steps) mma_ts(tmem + L::prob(q), zo + q * 128, shape_n, true, tmem + L::to);
+                    mma_commit(bars + 8 * kNear);
+                    if (kDots) mma_commit(bars + 8 * (kFreeZ + zs));
+                    return true;
+                };
+                bool ok = true;
+                for (int it = 0; it < count && ok; it += 2) {
+                    ok = chunk(it, Int<0>{});
+                    if (ok && it + 1 < count) ok = chunk(it + 1, Int<1>{});
                 }
-                if (*stop) {
-                    mma_commit(bars + 8 * kDrain);
-                    for (uint32_t i = 0; i < kSpin / 16 && !bar_try(bars + 8 * kDrain, 0); ++i) {}
+                if (ok && count > 0 && (ok = wait(kOutRead, count - 1))) send(count - 1);
+                if (!ok) {
+                    mma_commit(bars + 8 * (kDrain + 1));
+                    for (uint32_t i = 0; i < kSpin / 16 && !bar_try(bars + 8 * (kDrain + 1), 0); ++i) {}
                 }
+                tma_store_wait_all();
             }
             __syncwarp();
         }
@@ -485,6 +477,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
             Out* go = static_cast<Out*>(p.out) + b * p.ob + h * p.oh;
             const bool columns = 64 * side < p.dz;
+            {   // P starts as zeros
+                const uint32_t zero[8] = {};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_st8(at + L::tp + 32 * side + 8 * i, zero);
+                tmem_wait_st();
+            }
             bool ok = true;  // once a wait has given up, the rest runs on without waiting: its barriers need every thread
             for (int it = 0; it < count; ++it) {
                 const int t0 = chunk_at(it) * kChunk, t = t0 + row;
@@ -496,74 +494,70 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 tmem_after_sync();
                 double sum = 0.0;  // of W's row; joined in 64 bits, since two such sums will be subtracted
                 pair sum_far = 0;
+                const pair minus = make_pair2(-1.0f, -1.0f), scale2 = make_pair2(p.scale, p.scale);
+                const float to_late = kRev ? 1.0f : -1.0f;
+                // A side has 16 columns of every batch of 32; batches on the empty side of the diagonal stay zero from the start.
 #pragma unroll 1
-                for (int i = 0; i < 2; ++i) {  // a batch of 32 columns; the sides take turns
-                    const int n = side + 2 * i;
-                    if (kDots && i == 1) {  // the first half of w Z^T has been read by this thread
+                for (int n = 0; n < 4; ++n) {
+                    if (kDots && n == 2) {  // the first half of w Z^T has been read by this thread
                         tmem_before_sync();
                         bar_arrive(bars + 8 * kHalfRead);
                         ok = ok && wait(kHalf, it);
                         tmem_after_sync();
                     }
-                    if (n >= batches) continue;
-                    if (kRev ? n < quarter : n > quarter) {
-                        const uint32_t zero[8] = {};
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) tmem_st8(at + L::prob(2 * n + e), zero);
-                        continue;
-                    }
-                    const bool diagonal = n == quarter;
-                    // e^{c_i-c_j} = e^{c_i-c_m} e^{c_m-c_j} with m at the batch's edge between j and i: both exponents keep
-                    // their sign, and one exponential of the row serves the batch's columns
-                    const int m = kRev ? 32 * n : 32 * n + 31;
-                    const float f1 = p.scale * ex2((kRev ? 1.0f : -1.0f) * ((read1(c_hi + m) - own_hi) + (read1(c_lo + m) - own_lo)));
-                    const pair f = make_pair2(f1, f1);
-#pragma unroll 1
-                    for (int e = 0; e < 2; ++e) {
-                        const int q = 2 * n + e;
-                        uint32_t v[16], term[8];
-                        tmem_ld16(v, at + L::to + 16 * q);
+                    if (n >= batches || (kRev ? n < quarter : n > quarter)) continue;
+                    const int q = 2 * n + side;
+                    uint32_t v[16], term[8];
+                    tmem_ld16(v, at + L::to + 16 * q);
+                    auto keep = [&](int j, pair w) {  // two columns of P
+                        w = mul2(w, make_pair2(v[j], v[j + 1]));
+                        term[j / 2] = pack_bf16(w);
+                        if constexpr (kDots) parts(w, v[j], v[j + 1]);
+                    };
+                    if (!kDots && n != quarter) {
+                        // e^{c_i-c_j} = e^{c_i-c_m} e^{c_m-c_j} with m at the batch's edge between j and i: both exponents keep
+                        // their sign, and one exponential of the row serves the batch's columns
+                        const int m = kRev ? 32 * n : 32 * n + 31;
+                        const float f1 = p.scale * ex2(to_late * ((read1(c_hi + m) - own_hi) + (read1(c_lo + m) - own_lo)));
+                        const pair f = make_pair2(f1, f1);
 #pragma unroll
                         for (int j = 0; j < 16; j += 4) {
-                            pair w0, w1;
-                            if (!kDots && !diagonal) {
-                                const float4 g = read4(w_bt + 16 * q + j);
-                                w0 = mul2(f, make_pair2(g.x, g.y));
-                                w1 = mul2(f, make_pair2(g.z, g.w));
-                            } else {
-                                const float4 hi = read4(c_hi + 16 * q + j);
-                                const float4 lo = read4(c_lo + 16 * q + j);
-                                const int ahead = diagonal ? row - 16 * q - j : kRev ? -1 : 16;  // columns up to the diagonal
-                                auto weight = [&](int u, float h1, float l1) {
-                                    const float d = kRev ? (h1 - own_hi) + (l1 - own_lo) : (own_hi - h1) + (own_lo - l1);
-                                    return (kRev ? u >= ahead : u <= ahead) ? p.scale * ex2(d) : 0.0f;
-                                };
-                                w0 = make_pair2(weight(0, hi.x, lo.x), weight(1, hi.y, lo.y));
-                                w1 = make_pair2(weight(2, hi.z, lo.z), weight(3, hi.w, lo.w));
-                            }
-                            w0 = mul2(w0, make_pair2(v[j], v[j + 1]));
-                            w1 = mul2(w1, make_pair2(v[j + 2], v[j + 3]));
-                            term[j / 2] = pack_bf16(w0);
-                            term[j / 2 + 1] = pack_bf16(w1);
-                            if constexpr (kDots) {  // kept for the row sum, without the token itself
-                                parts(w0, v[j], v[j + 1]);
-                                parts(w1, v[j + 2], v[j + 3]);
-#pragma unroll
-                                for (int u = 0; u < 4; ++u)
-                                    if (16 * q + j + u == row) v[j + u] = 0u;
-                            }
+                            const float4 g = read4(w_bt + 16 * q + j);
+                            keep(j, mul2(f, make_pair2(g.x, g.y)));
+                            keep(j + 2, mul2(f, make_pair2(g.z, g.w)));
                         }
-                        tmem_st8(at + L::prob(q), term);
-                        if constexpr (kDots) {
-                            uint32_t t16[16];
-                            tmem_ld16(t16, at + L::tt + 16 * (q & 3));
+                    } else {
+                        const pair own_h = make_pair2(own_hi, own_hi), own_l = make_pair2(own_lo, own_lo);
+                        const int ahead = n == quarter ? row - 16 * q : kRev ? -1 : 16;  // columns up to the diagonal
+                        auto weights = [&](int j, float h0, float h1, float l0, float l1) {
+                            // differences of the two parts first, either way round the same bits
+                            float d0, d1;
+                            parts(add2(fma2(own_h, minus, make_pair2(h0, h1)), fma2(own_l, minus, make_pair2(l0, l1))), d0, d1);
+                            d0 = (kRev ? j >= ahead : j <= ahead) ? ex2(to_late * d0) : 0.0f;
+                            d1 = (kRev ? j + 1 >= ahead : j + 1 <= ahead) ? ex2(to_late * d1) : 0.0f;
+                            keep(j, mul2(scale2, make_pair2(d0, d1)));
+                        };
 #pragma unroll
-                            for (int j = 0; j < 16; j += 4) {
-                                float a, c;
-                                parts(fma2(make_pair2(v[j], v[j + 1]), make_pair2(t16[j], t16[j + 1]),
-                                           mul2(make_pair2(v[j + 2], v[j + 3]), make_pair2(t16[j + 2], t16[j + 3]))), a, c);
-                                sum += (double)(a + c);
-                            }
+                        for (int j = 0; j < 16; j += 4) {
+                            const float4 hi = read4(c_hi + 16 * q + j), lo = read4(c_lo + 16 * q + j);
+                            weights(j, hi.x, hi.y, lo.x, lo.y);
+                            weights(j + 2, hi.z, hi.w, lo.z, lo.w);
+                        }
+                    }
+                    tmem_st8(at + L::prob(q), term);
+                    if constexpr (kDots) {
+                        uint32_t t16[16];
+                        tmem_ld16(t16, at + L::tt + 16 * (q & 3));
+                        const int own = row - 16 * q;  // without the token itself
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (j == own) t16[j] = 0u;
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) {
+                            float a, c;
+                            parts(fma2(make_pair2(v[j], v[j + 1]), make_pair2(t16[j], t16[j + 1]),
+                                       mul2(make_pair2(v[j + 2], v[j + 3]), make_pair2(t16[j + 2], t16[j + 3]))), a, c);
+                            sum += (double)(a + c);
                         }
                     }
                 }
@@ -600,8 +594,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 bar_arrive(bars + 8 * kFarRead);
                 ok = ok && wait(kNear, it);
                 tmem_after_sync();
+                // products may still read the tile that the output leaves from
+                ok = ok && wait(kTileDone + it % 2, it / 2);
                 uint8_t* const stage = sm8 + L::staged(0, it) + side * kBlock + row * 128;
-                if (kDots) ok = ok && wait(kYDone + it % L::kYs, it / L::kYs);  // the tile has been read (the scores were before)
 #pragma unroll 1
                 for (int col = col0; col < col1; col += 16) {
                     uint32_t v[16];
@@ -616,15 +611,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                                 make_uint4(pack_bf16(make_pair2(v[8 * c], v[8 * c + 1])), pack_bf16(make_pair2(v[8 * c + 2], v[8 * c + 3])),
                                            pack_bf16(make_pair2(v[8 * c + 4], v[8 * c + 5])), pack_bf16(make_pair2(v[8 * c + 6], v[8 * c + 7])));
                     } else if (t < p.tokens) {
-                        float f[16];
-#pragma unroll
-                        for (int u = 0; u < 16; ++u) f[u] = __uint_as_float(v[u]);
-                        store_row16(go + t * p.ot + col, f, p.dz - col);
+                        store16(go + t * p.ot + col, v, p.dz - col);
                     }
                 }
-                tmem_before_sync();
                 if (sizeof(Out) == 2) fence_smem_to_async();
-                bar_arrive(bars + 8 * kStaged);
+                tmem_before_sync();
+                bar_arrive(bars + 8 * kOutRead);
                 if constexpr (kDots) {
                     const long long to = ((long long)side * gridDim.x / p.segments + bh) * p.tokens + t;
                     float a, c;
@@ -639,8 +631,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             if (columns)
                 for (int c = max(chunks, segment * p.seg_chunks); c < (segment + 1) * p.seg_chunks; ++c) {
                     const int t = c * kChunk + row;
-                    const float o[16] = {};
-                    for (int col = 64 * side; col < min(p.dz, 64 * side + 64) && t < p.tokens; col += 16) store_row16(go + t * p.ot + col, o, p.dz - col);
+                    const uint32_t o[16] = {};
+                    for (int col = 64 * side; col < min(p.dz, 64 * side + 64) && t < p.tokens; col += 16) store16(go + t * p.ot + col, o, p.dz - col);
                 }
         }
     } else {
