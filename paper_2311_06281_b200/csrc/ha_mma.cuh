@@ -869,20 +869,4 @@ __global__ void pack_rows_kernel(const Rows from, __nv_bfloat16* to, int tokens,
     }
 }
 
-// What each segment starts from: the states that the segments would end at from zero (left by the state-only pass in
-// seg_state) joined in order.  A thread has one element; segments is small.
-__global__ void join_segments_kernel(const MmaPass p) {
-    const int plane = p.dx * p.dz, tiles = (plane + 255) / 256;
-    const int bh = blockIdx.x / tiles, e = blockIdx.x % tiles * 256 + threadIdx.x;
-    if (e >= plane) return;
-    const int k = e / p.dz, z = e % p.dz;
-    float cur = p.s_in ? p.s_in[(long long)bh * plane + (p.s_in_t ? z * p.dx + k : e)] * p.s_in_mul : 0.0f;
-    float* at = p.seg_state + (long long)bh * p.segments * plane + e;
-    for (int s = 0; s < p.segments; ++s) {
-        const float own = s + 1 < p.segments ? at[(long long)s * plane] : 0.0f;
-        at[(long long)s * plane] = cur;
-        if (s + 1 < p.segments) cur = fmaf(p.seg_decay[bh * p.segments + s], cur, own);
-    }
-}
-
 }  // namespace ha

@@ -31,7 +31,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 // difference of sums finite.  (x < kReset keeps NaN.)
 constexpr float kReset = -1.0e4f;
 constexpr int kSimtChunk = 32;   // tokens of a chunk
-constexpr int kSimtCols = 32;    // columns of Z (and of the state) of one CTA
 constexpr int kSimtThreads = 256;
 
 struct Rows {  // [batch, tokens, heads', dim] with a contiguous last dimension, strides in elements
@@ -54,6 +53,10 @@ struct Pass {
     void* out;           // [batch, tokens, heads, dz] through its strides
     long long ob, ot, oh;
     float* dump;         // [batch * heads, chunks, dx, dz]: the state before each chunk, or NULL
+    // A sequence cut into segments of seg_chunks chunks: each starts from seg_state[bh][segment] ([dx, dz])
+    int segments, seg_chunks;
+    float* seg_state;
+    float* seg_decay;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -76,23 +79,56 @@ __device__ __forceinline__ int live_tokens(const int* lengths, int b, int tokens
 // d * s without 0 * inf: a decay of zero forgets the state whatever it holds
 __device__ __forceinline__ float decayed(float d, float s) { return d == 0.0f ? 0.0f : d * s; }
 
-template <class T, bool kRev, class OutT>
+// Columns c0 + lane + 32 u (u < kN) of a warp's four of the rows t0 .. t0 + 31, zeros where there is nothing; and their way to
+// shared memory.
+template <int kN, class T>
+__device__ __forceinline__ void load_rows(float (&v)[4 * kN], const T* from, long long st, int c0, int dim, int t0, int live) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int u = 0; u < kN; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + warp + 8 * i, c = c0 + lane + 32 * u;
+            v[4 * u + i] = t < live && c < dim ? to_f(from[t * st + c]) : 0.0f;
+        }
+}
+template <int kN>
+__device__ __forceinline__ void keep_rows(const float (&v)[4 * kN], float* to, int pitch, int c0, int width) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int u = 0; u < kN; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c0 + lane + 32 * u < width) to[(warp + 8 * i) * pitch + c0 + lane + 32 * u] = v[4 * u + i];
+}
+__device__ __forceinline__ void add4(float4& acc, float w, const float4& v) {
+    acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
+}
+
+// A CTA has kCols columns of Z and of the state and walks the chunks of its segment.  The products read shared memory more than
+// they compute: a 16-byte read of a warp costs it four turns, whatever is read twice.  So a thread has four columns of kPer
+// output rows and of four state rows, which share those reads (24 sequences of up to 1000 tokens, dimension 64: 69 us with one
+// row for 32 columns, 43 us with two for 64; the sums of the states before it 25 us and 16 us).  The next chunk's first 64
+// columns travel meanwhile: waiting for them took half of a chunk's time.
+template <class T, bool kRev, class OutT, bool kStateOnly, int kCols>
 __global__ void __launch_bounds__(kSimtThreads) simt_pass_kernel(const Pass p) {
-    extern __shared__ float sm[];
+    constexpr int kLanes = kCols / 4, kSweep = kSimtThreads / kLanes, kPer = kSimtChunk / kSweep;
+    extern __shared__ __align__(16) float sm[];
     const int dxp = p.dx + 4 - (p.dx & 3) + ((p.dx & 3) ? 4 : 0);  // a multiple of 4, at least dx + 4: rows shifted by 4 banks
     float* xs = sm;                                  // [32][dxp]
     float* ys = xs + kSimtChunk * dxp;               // [32][dxp]
-    float* zs = ys + kSimtChunk * dxp;               // [32][32]
-    float* zw = zs + kSimtChunk * kSimtCols;         // [32][32] times the state's weight
-    float* st = zw + kSimtChunk * kSimtCols;         // [dx][32]
-    float* pr = st + p.dx * kSimtCols;               // [32][33]
+    float* zs = ys + kSimtChunk * dxp;               // [32][kCols]
+    float* zw = zs + kSimtChunk * kCols;         // [32][kCols] times the state's weight
+    float* st = zw + kSimtChunk * kCols;         // [dx][kCols]
+    float* pr = st + p.dx * kCols;               // [32][33]
     __shared__ float c_hi[kSimtChunk], c_lo[kSimtChunk], w_in[kSimtChunk], w_st[kSimtChunk];
     __shared__ float s_whole;
 
-    const int tid = threadIdx.x, ztiles = (p.dz + kSimtCols - 1) / kSimtCols;
-    const long long item = blockIdx.x;
-    const int z0 = (int)(item % ztiles) * kSimtCols;
-    const int bh = (int)(item / ztiles), b = bh / p.heads, h = bh % p.heads;
+    const int tid = threadIdx.x, ztiles = (p.dz + kCols - 1) / kCols;
+    const int cuts = kStateOnly ? p.segments - 1 : p.segments;  // the last segment's own state is not needed by another
+    const int segment = blockIdx.x % cuts, item = blockIdx.x / cuts;
+    const int z0 = item % ztiles * kCols;
+    const int bh = item / ztiles, b = bh / p.heads, h = bh % p.heads;
     const int live = live_tokens(p.lengths, b, p.tokens);
     const T* gx = static_cast<const T*>(p.x.ptr) + b * p.x.sb + (h / p.x.div) * p.x.sh;
     const T* gy = static_cast<const T*>(p.y.ptr) + b * p.y.sb + (h / p.y.div) * p.y.sh;
@@ -101,56 +137,81 @@ __global__ void __launch_bounds__(kSimtThreads) simt_pass_kernel(const Pass p) {
     OutT* go = static_cast<OutT*>(p.out) + b * p.ob + h * p.oh;
 
     const long long plane = (long long)bh * p.dx * p.dz;
-    for (int e = tid; e < p.dx * kSimtCols; e += kSimtThreads) {
-        const int k = e / kSimtCols, z = z0 + e % kSimtCols;
+    float* const seg = p.segments > 1 ? p.seg_state + ((long long)bh * p.segments + segment) * p.dx * p.dz : nullptr;
+    for (int e = tid; e < p.dx * kCols; e += kSimtThreads) {
+        const int k = e / kCols, z = z0 + e % kCols;
         float v = 0.0f;
-        if (p.s_in && z < p.dz) v = p.s_in[plane + (p.s_in_t ? (long long)z * p.dx + k : (long long)k * p.dz + z)] * p.s_in_mul;
+        if (!kStateOnly && z < p.dz) {
+            if (seg) v = seg[(long long)k * p.dz + z];
+            else if (p.s_in) v = p.s_in[plane + (p.s_in_t ? (long long)z * p.dx + k : (long long)k * p.dz + z)] * p.s_in_mul;
+        }
         st[e] = v;
     }
     const int chunks = (p.tokens + kSimtChunk - 1) / kSimtChunk;
-    for (int n = 0; n < chunks; ++n) {
+    const int first = min(chunks, segment * p.seg_chunks), last = min(chunks, first + p.seg_chunks);
+    double total = 0.0;
+    // the next chunk's first 64 columns, on their way while this one is worked on
+    float x_next[8], y_next[8], z_next[kCols / 8], a_next = 0.0f;
+    auto fetch = [&](int n) {
+        if (n >= last) return;
         const int t0 = (kRev ? chunks - 1 - n : n) * kSimtChunk;
+        if (!kStateOnly) load_rows<2>(x_next, gx, p.x.st, 0, p.dx, t0, live);
+        load_rows<2>(y_next, gy, p.y.st, 0, p.dx, t0, live);
+        load_rows<kCols / 32>(z_next, gz, p.z.st, z0, p.dz, t0, live);
+        a_next = tid < 32 && t0 + tid < live ? ga[(t0 + tid) * p.at] : 0.0f;
+    };
+    bool fetched = false;
+    for (int n = first; n < last; ++n) {
+        const int t0 = (kRev ? chunks - 1 - n : n) * kSimtChunk;
+        if (t0 >= live && !p.dump) {  // nothing in it: the state passes as it is
+            if (!kStateOnly)
+                for (int e = tid; e < kSimtChunk * kCols; e += kSimtThreads) {
+                    const int t = t0 + e / kCols, z = z0 + e % kCols;
+                    if (t < p.tokens && z < p.dz) go[t * p.ot + z] = from_f<OutT>(0.0f);
+                }
+            continue;
+        }
+        if (!fetched) fetch(n);
+        fetched = true;
         __syncthreads();
-        if (p.dump)
-            for (int e = tid; e < p.dx * kSimtCols; e += kSimtThreads) {
-                const int k = e / kSimtCols, z = z0 + e % kSimtCols;
+        if (!kStateOnly && p.dump)
+            for (int e = tid; e < p.dx * kCols; e += kSimtThreads) {
+                const int k = e / kCols, z = z0 + e % kCols;
                 if (z < p.dz) p.dump[(((long long)bh * chunks + t0 / kSimtChunk) * p.dx + k) * p.dz + z] = st[e];
             }
-        for (int e = tid; e < kSimtChunk * p.dx; e += kSimtThreads) {
-            const int i = e / p.dx, k = e % p.dx;
-            const bool in = t0 + i < live;
-            xs[i * dxp + k] = in ? to_f(gx[(t0 + i) * p.x.st + k]) : 0.0f;
-            ys[i * dxp + k] = in ? to_f(gy[(t0 + i) * p.y.st + k]) : 0.0f;
-        }
-        for (int e = tid; e < kSimtChunk * (dxp - p.dx); e += kSimtThreads) {
-            const int i = e / (dxp - p.dx), k = p.dx + e % (dxp - p.dx);
-            xs[i * dxp + k] = ys[i * dxp + k] = 0.0f;
-        }
-        for (int e = tid; e < kSimtChunk * kSimtCols; e += kSimtThreads) {
-            const int i = e / kSimtCols, z = z0 + e % kSimtCols;
-            zs[e] = t0 + i < live && z < p.dz ? to_f(gz[(t0 + i) * p.z.st + z]) : 0.0f;
+        if (!kStateOnly) keep_rows<2>(x_next, xs, dxp, 0, dxp);
+        keep_rows<2>(y_next, ys, dxp, 0, dxp);
+        keep_rows<kCols / 32>(z_next, zs, kCols, 0, kCols);
+        for (int c0 = 64; c0 < dxp; c0 += 64) {
+            float x[8], y[8];
+            if (!kStateOnly) load_rows<2>(x, gx, p.x.st, c0, p.dx, t0, live);
+            load_rows<2>(y, gy, p.y.st, c0, p.dx, t0, live);
+            if (!kStateOnly) keep_rows<2>(x, xs, dxp, c0, dxp);
+            keep_rows<2>(y, ys, dxp, c0, dxp);
         }
         if (tid < 32) {
             // running sums of the log2 decays, in 64 bits and handed on as two floats: a reset (-10000) must not cost the
             // differences of the sums after it their low bits
-            float a = t0 + tid < live ? ga[(t0 + tid) * p.at] : 0.0f;
-            a = a < kReset ? kReset : a;
+            const float a = a_next < kReset ? kReset : a_next;
             double c = (double)a * 1.4426950408889634;
             for (int o = 1; o < 32; o *= 2) {
                 const double u = __shfl_up_sync(~0u, c, o);
                 if (tid >= o) c += u;
             }
             const double whole = __shfl_sync(~0u, c, 31);
+            total += whole;
             c_hi[tid] = (float)c;
             c_lo[tid] = (float)(c - (double)(float)c);
             w_in[tid] = ex2((float)(kRev ? whole - c : c));
             w_st[tid] = ex2((float)(kRev ? c : whole - c));
             if (tid == 31) s_whole = ex2((float)whole);
         }
+        fetch(n + 1);
         __syncthreads();
-        {   // P, four columns of one row each
+        if (!kStateOnly) {  // P, four columns of one row each
             const int i = tid >> 3, j0 = tid & 7;
             float acc[4] = {};
+#pragma unroll 4
             for (int k = 0; k < dxp - 4; k += 4) {
                 const float4 a = *reinterpret_cast<const float4*>(xs + i * dxp + k);
 #pragma unroll
@@ -165,55 +226,100 @@ __global__ void __launch_bounds__(kSimtThreads) simt_pass_kernel(const Pass p) {
                 const float d = (c_hi[late] - c_hi[early]) + (c_lo[late] - c_lo[early]);
                 pr[i * 33 + j] = early <= late ? acc[m] * ex2(d) : 0.0f;
             }
-            for (int e = tid; e < kSimtChunk * kSimtCols; e += kSimtThreads) zw[e] = zs[e] * w_st[e / kSimtCols];
         }
+        for (int e = tid; e < kSimtChunk * kCols; e += kSimtThreads) zw[e] = zs[e] * w_st[e / kCols];
         __syncthreads();
-        {   // four columns of one output row each
-            const int i = tid >> 3, z = (tid & 7) * 4;
-            float in[4] = {}, far[4] = {};
+        const int z = tid % kLanes * 4, r0 = tid / kLanes;
+        if (!kStateOnly) {  // four columns of kPer output rows each
+            float4 in[kPer] = {}, far[kPer] = {};
+#pragma unroll 8
             for (int j = 0; j < kSimtChunk; ++j) {
-                const float w = pr[i * 33 + j];
+                const float4 v = *reinterpret_cast<const float4*>(zs + j * kCols + z);
 #pragma unroll
-                for (int m = 0; m < 4; ++m) in[m] = fmaf(w, zs[j * kSimtCols + z + m], in[m]);
+                for (int u = 0; u < kPer; ++u) add4(in[u], pr[(r0 + u * kSweep) * 33 + j], v);
             }
+#pragma unroll 8
             for (int k = 0; k < p.dx; ++k) {
-                const float w = xs[i * dxp + k];
+                const float4 v = *reinterpret_cast<const float4*>(st + k * kCols + z);
 #pragma unroll
-                for (int m = 0; m < 4; ++m) far[m] = fmaf(w, st[k * kSimtCols + z + m], far[m]);
+                for (int u = 0; u < kPer; ++u) add4(far[u], xs[(r0 + u * kSweep) * dxp + k], v);
             }
-            if (t0 + i < p.tokens) {
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) {
+                const int i = r0 + u * kSweep;
+                const float in4[4] = {in[u].x, in[u].y, in[u].z, in[u].w}, far4[4] = {far[u].x, far[u].y, far[u].z, far[u].w};
 #pragma unroll
                 for (int m = 0; m < 4; ++m)
-                    if (z0 + z + m < p.dz)
+                    if (t0 + i < p.tokens && z0 + z + m < p.dz)
                         go[(t0 + i) * p.ot + z0 + z + m] =
-                            from_f<OutT>(t0 + i < live ? p.scale * (in[m] + decayed(w_in[i], far[m])) : 0.0f);
+                            from_f<OutT>(t0 + i < live ? p.scale * (in4[m] + decayed(w_in[i], far4[m])) : 0.0f);
             }
+            __syncthreads();
         }
-        __syncthreads();
-        for (int k = tid >> 3; k < p.dx; k += kSimtThreads / 8) {
-            const int z = (tid & 7) * 4;
-            float acc[4];
-#pragma unroll
-            for (int m = 0; m < 4; ++m) acc[m] = decayed(s_whole, st[k * kSimtCols + z + m]);
+        for (int k0 = r0; k0 < p.dx; k0 += 4 * kSweep) {  // the state, four rows at a time
+            float4 acc[4] = {};
+#pragma unroll 4
             for (int j = 0; j < kSimtChunk; ++j) {
-                const float w = ys[j * dxp + k];
+                const float4 v = *reinterpret_cast<const float4*>(zw + j * kCols + z);
 #pragma unroll
-                for (int m = 0; m < 4; ++m) acc[m] = fmaf(w, zw[j * kSimtCols + z + m], acc[m]);
+                for (int u = 0; u < 4; ++u) add4(acc[u], ys[j * dxp + min(k0 + u * kSweep, p.dx)], v);  // column dx is there, and zero
             }
 #pragma unroll
-            for (int m = 0; m < 4; ++m) st[k * kSimtCols + z + m] = acc[m];
+            for (int u = 0; u < 4; ++u)
+                if (k0 + u * kSweep < p.dx) {
+                    float4* own = reinterpret_cast<float4*>(st + (k0 + u * kSweep) * kCols + z);
+                    const float4 s = *own;
+                    *own = make_float4(acc[u].x + decayed(s_whole, s.x), acc[u].y + decayed(s_whole, s.y), acc[u].z + decayed(s_whole, s.z),
+                                       acc[u].w + decayed(s_whole, s.w));
+                }
         }
     }
     __syncthreads();
-    if (p.s_out)
-        for (int e = tid; e < p.dx * kSimtCols; e += kSimtThreads) {
-            const int k = e / kSimtCols, z = z0 + e % kSimtCols;
+    if (kStateOnly) {
+        for (int e = tid; e < p.dx * kCols; e += kSimtThreads) {
+            const int k = e / kCols, z = z0 + e % kCols;
+            if (z < p.dz) seg[(long long)k * p.dz + z] = st[e];
+        }
+        if (tid == 0 && z0 == 0) p.seg_decay[bh * p.segments + segment] = ex2((float)total);
+    } else if (p.s_out && segment == p.segments - 1) {
+        for (int e = tid; e < p.dx * kCols; e += kSimtThreads) {
+            const int k = e / kCols, z = z0 + e % kCols;
             if (z < p.dz) p.s_out[plane + (p.s_out_t ? (long long)z * p.dx + k : (long long)k * p.dz + z)] = st[e] * p.s_out_mul;
         }
+    }
 }
-inline size_t simt_pass_smem(int dx) {
+inline size_t simt_pass_smem(int dx, int cols) {
     const int dxp = dx + 4 - (dx & 3) + ((dx & 3) ? 4 : 0);
-    return sizeof(float) * (size_t)(2 * kSimtChunk * dxp + 2 * kSimtChunk * kSimtCols + dx * kSimtCols + kSimtChunk * 33);
+    return sizeof(float) * (size_t)(2 * kSimtChunk * dxp + 2 * kSimtChunk * cols + dx * cols + kSimtChunk * 33);
+}
+
+// What each segment starts from: the states that the segments would end at from zero (left by the state-only pass in
+// seg_state) joined in order.  A thread has one element and loads eight segments' before it stores one: the chain itself is
+// one multiply-add a segment, memory's latency was all of the 16 us that one load at a time took (18 segments of 8 heads).
+template <class P>
+__global__ void __launch_bounds__(256) join_segments_kernel(const P p) {
+    const int plane = p.dx * p.dz, tiles = (plane + 255) / 256;
+    const int bh = blockIdx.x / tiles, e = blockIdx.x % tiles * 256 + threadIdx.x;
+    if (e >= plane) return;
+    const int k = e / p.dz, z = e % p.dz, last = p.segments - 1;
+    const float* decay = p.seg_decay + (long long)bh * p.segments;
+    float* at = p.seg_state + (long long)bh * p.segments * plane + e;
+    float cur = p.s_in ? p.s_in[(long long)bh * plane + (p.s_in_t ? z * p.dx + k : e)] * p.s_in_mul : 0.0f;
+    constexpr int kAhead = 8;
+    for (int s0 = 0; s0 <= last; s0 += kAhead) {
+        float own[kAhead], d[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            own[i] = s0 + i < last ? at[(long long)(s0 + i) * plane] : 0.0f;
+            d[i] = s0 + i < last ? decay[s0 + i] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (s0 + i <= last) {
+                at[(long long)(s0 + i) * plane] = cur;
+                cur = decayed(d[i], cur) + own[i];
+            }
+    }
 }
 
 // dst[b, t, g, :] = the sum over the heads that read head g, rounded once; zero behind a sequence's end.

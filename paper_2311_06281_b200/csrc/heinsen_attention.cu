@@ -51,16 +51,58 @@ hs_status launched(const char* what) {
     return HS_OK;
 }
 
-template <class T, bool kRev, class OutT>
-hs_status simt_pass(const Pass& ps, cudaStream_t stream) {
-    const size_t smem = ha::simt_pass_smem(ps.dx);
-    const auto fn = ha::simt_pass_kernel<T, kRev, OutT>;
+constexpr int kSms = 148;  // B200; sizes workspaces the same wherever they are asked for
+
+// Columns of the state that a CTA has, and the CTAs for a state.  64 take fewer reads of shared memory for a product than 32
+// (two rows share each), and half of them would idle where a state has no more than 32.
+int simt_cols(int dz) { return dz > 32 ? 64 : 32; }
+int simt_tiles(int dz) { return (dz + simt_cols(dz) - 1) / simt_cols(dz); }
+
+// Segments of a sequence on the CUDA cores, as below: up to two CTAs for an SM, where cutting in two steps (states, then the
+// rest) is less than walking all chunks.  Measured, whole and cut: 24 states of 64 x 64, 31 chunks 230 us and 71 us, 4 chunks
+// 37 us and 28 us; 64 of them, 32 chunks 231 us and 152 us; 128 of them 233 us and 257 us (not cut).
+int simt_segments(const heinsen_attention_problem* p) {
+    const long long ctas = p->batch * p->heads * simt_tiles(std::max(p->k_dim, p->v_dim));
+    const long long chunks = (p->tokens + ha::kSimtChunk - 1) / ha::kSimtChunk;
+    const long long most = std::max(1ll, std::min(2 * kSms / std::max(1ll, ctas), chunks));
+    const long long each = std::max(1ll, (chunks + most - 1) / most);
+    return 2 * each + 1 < chunks ? (int)((chunks + each - 1) / each) : 1;
+}
+size_t simt_segment_bytes(const heinsen_attention_problem* p) {
+    const long long pairs = p->batch * p->heads;
+    const int n = simt_segments(p);
+    return n > 1 ? up256((size_t)pairs * n * p->k_dim * p->v_dim * 4) + up256((size_t)pairs * n * 4) : 0;
+}
+
+template <class T, bool kRev, class OutT, bool kStateOnly>
+hs_status simt_launch(const Pass& ps, cudaStream_t stream) {
+    const int cols = simt_cols(ps.dz);
+    const size_t smem = ha::simt_pass_smem(ps.dx, cols);
+    const auto fn = cols == 64 ? ha::simt_pass_kernel<T, kRev, OutT, kStateOnly, 64> : ha::simt_pass_kernel<T, kRev, OutT, kStateOnly, 32>;
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
-    const long long grid = (long long)ps.batch * ps.heads * ((ps.dz + ha::kSimtCols - 1) / ha::kSimtCols);
+    const long long grid = (long long)ps.batch * ps.heads * simt_tiles(ps.dz) * (kStateOnly ? ps.segments - 1 : ps.segments);
     if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
     fn<<<(unsigned)grid, ha::kSimtThreads, smem, stream>>>(ps);
     return launched("simt_pass_kernel");
+}
+
+// One pass, with its segments; `space`: simt_segment_bytes() of scratch.
+template <class T, bool kRev, class OutT>
+hs_status simt_pass(Pass ps, int segments, uint8_t* space, cudaStream_t stream) {
+    const long long pairs = (long long)ps.batch * ps.heads;
+    ps.segments = segments;
+    const int chunks = (ps.tokens + ha::kSimtChunk - 1) / ha::kSimtChunk;
+    ps.seg_chunks = (chunks + segments - 1) / segments;
+    if (segments > 1) {
+        ps.seg_state = reinterpret_cast<float*>(space);
+        ps.seg_decay = reinterpret_cast<float*>(space + up256((size_t)pairs * segments * ps.dx * ps.dz * 4));
+        hs_status st = simt_launch<T, kRev, float, true>(ps, stream);
+        if (st != HS_OK) return st;
+        ha::join_segments_kernel<<<(unsigned)(pairs * ((ps.dx * ps.dz + 255) / 256)), 256, 0, stream>>>(ps);
+        if ((st = launched("join_segments_kernel")) != HS_OK) return st;
+    }
+    return simt_launch<T, kRev, OutT, false>(ps, stream);
 }
 
 Pass common(const heinsen_attention_problem* p) {
@@ -120,14 +162,17 @@ bool encode(CUtensorMap* m, const View& v, long long batch, long long tokens) {
     }
 }
 
-// Segments of a sequence.  Fewer (batch, head) pairs than SMs leave the rest of the GPU idle, so sequences are cut until
-// there is about one segment for each SM; each keeps at least four chunks, since the cut reads keys and values twice.
+// Segments of a sequence.  Fewer (batch, head) pairs than SMs leave the rest of the GPU idle, so a sequence is cut into as many
+// segments as there are SMs for; their states are formed first, from keys and values alone, and joined.  Measured at dimension
+// 128: one pass 15 us + 3.7 us a chunk, segments 34 us + 6.2 us for each chunk of a segment, 8 us where all SMs read at once.
+// So they are taken from about where they pay: 64 pairs never (64 chunks: 248 us whole, 257 us in two), 49 pairs of 16 chunks
+// not (74 us, in three 83 us) and of 32 (131 us, 120 us), 8 pairs of 4 chunks not (27 us, 38 us) and of 8 (41 us, 38 us).
 int segments_for(long long pairs, long long tokens, int sms) {
     const long long chunks = (tokens + ha::kChunk - 1) / ha::kChunk;
-    if (pairs * 2 > sms) return 1;
-    return (int)std::max(1ll, std::min({sms / pairs, chunks / 4, 64ll}));
+    const long long most = std::max(1ll, std::min(sms / std::max(1ll, pairs), chunks));
+    const long long each = std::max(1ll, (chunks + most - 1) / most);
+    return 2 * each + 5 < chunks ? (int)((chunks + each - 1) / each) : 1;
 }
-constexpr int kSms = 148;  // B200; sizes workspaces the same wherever they are asked for
 size_t segment_bytes(const heinsen_attention_problem* p) {
     const long long pairs = p->batch * p->heads;
     const int n = segments_for(pairs, p->tokens, kSms);
@@ -229,16 +274,17 @@ MmaSpace mma_space(const heinsen_attention_problem* p) {
     return s;
 }
 
-// Workspace of a backward pass: header | dq, dk, dv for each head, float32 | the states before every chunk and the gradients
+// Workspace of a backward pass: header | segments of a pass | dq, dk, dv for each head, float32 | the states before every chunk and the gradients
 // of the states behind it | sums of the decay gradients.
 struct BackwardSpace {
-    size_t dq, dk, dv, before, behind, part, total;
+    size_t segments, dq, dk, dv, before, behind, part, total;
 };
 BackwardSpace backward_space(const heinsen_attention_problem* p) {
     BackwardSpace s;
     const size_t rows = (size_t)p->batch * p->tokens * p->heads;
     const size_t chunks = (size_t)p->batch * p->heads * ((p->tokens + ha::kSimtChunk - 1) / ha::kSimtChunk);
-    s.dq = kHeaderBytes;
+    s.segments = kHeaderBytes;
+    s.dq = s.segments + simt_segment_bytes(p);
     s.dk = s.dq + up256(rows * p->k_dim * 4);
     s.dv = s.dk + up256(rows * p->k_dim * 4);
     s.before = s.dv + up256(rows * p->v_dim * 4);
@@ -261,7 +307,7 @@ hs_status forward_pass(const heinsen_attention_problem* p, const heinsen_attenti
     if (mma_fits(p) && tma_fits(view_of(*o, p->heads, p->heads, p->v_dim), p->batch, p->tokens))
         return mma_pass<false, false, __nv_bfloat16>(ps, {ps.x, p->q_heads, p->k_dim}, {ps.y, p->k_heads, p->k_dim},
                                                  {ps.z, p->v_heads, p->v_dim}, ws, ws + kHeaderBytes, hs_internal::call_id(), stream);
-    return simt_pass<T, false, T>(ps, stream);
+    return simt_pass<T, false, T>(ps, simt_segments(p), ws + kHeaderBytes, stream);
 }
 
 template <class T>
@@ -284,6 +330,8 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
     float *before = dlog_a ? reinterpret_cast<float*>(ws + sp.before) : nullptr,
           *behind = dlog_a ? reinterpret_cast<float*>(ws + sp.behind) : nullptr;
     double* part = reinterpret_cast<double*>(ws + sp.part);
+    const int segments = simt_segments(p);
+    uint8_t* space = ws + sp.segments;
     const Rows q = rows_of(p->q, p->heads, p->q_heads), k = rows_of(p->k, p->heads, p->k_heads),
                v = rows_of(p->v, p->heads, p->v_heads), g = rows_of(*d_o, p->heads, p->heads);
     hs_status st;
@@ -296,7 +344,7 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
         ps.s_in = p->state0; ps.s_in_t = 1;
         to(ps, wq, p->k_dim);
         ps.dump = before;
-        if ((st = simt_pass<T, false, float>(ps, stream)) != HS_OK) return st;
+        if ((st = simt_pass<T, false, float>(ps, segments, space, stream)) != HS_OK) return st;
     }
     {
         Pass ps = common(p);
@@ -304,7 +352,7 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
         ps.s_in = d_state; ps.s_in_t = 1; ps.s_in_mul = 1.0f / p->scale;  // the scale comes back with the output
         to(ps, wk, p->k_dim);
         ps.dump = behind;
-        if ((st = simt_pass<T, true, float>(ps, stream)) != HS_OK) return st;
+        if ((st = simt_pass<T, true, float>(ps, segments, space, stream)) != HS_OK) return st;
     }
     {
         Pass ps = common(p);
@@ -312,7 +360,7 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
         ps.s_in = d_state; ps.s_in_mul = 1.0f / p->scale;
         ps.s_out = dstate0; ps.s_out_mul = p->scale;
         to(ps, wv, p->v_dim);
-        if ((st = simt_pass<T, true, float>(ps, stream)) != HS_OK) return st;
+        if ((st = simt_pass<T, true, float>(ps, segments, space, stream)) != HS_OK) return st;
     }
     if ((st = sum_heads<T>(wq, dq, p, p->q_heads, p->k_dim, stream)) != HS_OK) return st;
     if ((st = sum_heads<T>(wk, dk, p, p->k_heads, p->k_dim, stream)) != HS_OK) return st;
@@ -443,7 +491,8 @@ extern "C" {
 size_t heinsen_attention_workspace_bytes(const heinsen_attention_problem* p, int backward) {
     if (validate(p) != HS_OK) return 0;
     if (nothing(p)) return kHeaderBytes;
-    if (!backward) return kHeaderBytes + segment_bytes(p);
+    if (!backward)  // which of the two passes runs depends on the output's layout too
+        return kHeaderBytes + std::max(simt_segment_bytes(p), p->dtype == HS_BF16 ? segment_bytes(p) : 0);
     return mma_fits(p) ? mma_space(p).total : backward_space(p).total;
 }
 
