@@ -15,7 +15,7 @@
 // rounding is as large).
 //
 // kDots: the pass also forms what the decay gradients need of it, in float32: the row sums of W = P o (w Z^T), w the fourth
-// tensor, from the unrounded P, and the dots w_i . (X S)_i, for which X S has the state in two terms.  W comes out of the two
+// tensor, from the unrounded P, and the dots w_i . (X S)_i, for which X S has the state in three terms.  W comes out of the two
 // passes that form it in the same bits (each exponential is taken of the same difference there), so that what cancels between
 // their sums cancels exactly.  Row sums from the outputs instead, w_i . out_i, were 1e-6 off in a common direction (the tensor
 // core's additions cut off), which sums over many tokens turn into 5e-5.
@@ -76,14 +76,14 @@ constexpr float kNothingCrosses = -60.0f;
 
 template <bool kDots>
 struct MmaLayout {
-    static constexpr int kTerms = kDots ? 2 : 1;               // of the state in X S
+    static constexpr int kTerms = kDots ? 2 : 1;               // of the state in X S (kDots: a third in a Y tile)
     static constexpr int kWeightsAtOnce = kDots ? 2 : 3;       // terms of w Z in the first product; the third follows
     // Stages.  A chunk's output leaves by TMA from its Z tile, the one that the next chunk needs last, or from its Y tile where Z
     // has one stage.  (Stores of a thread's own row took 2200 clocks a chunk instead of 760.)
     static constexpr int kXs = kDots ? 1 : 2, kYs = 2, kZs = kDots ? 1 : 2, kWs = kDots ? 1 : 0;
     static constexpr uint32_t x = 0, y = x + kXs * kTile, z = y + kYs * kTile, w = z + kZs * kTile, s = w + kWs * kTile,
                               ident = s + kTerms * kTile, decays = ident + 512, whole = decays + 4 * kChunk * 4, bars = whole + 32,
-                              end = bars + 8 * 38;
+                              end = bars + 8 * 40;
     // Tensor memory columns, all 512.  What is read out before the next product of its chain is due shares columns with it:
     // Z^T with the state's update, the scores with the output.
     static constexpr uint32_t tw = 0;                          // the terms of (w Z)^T: A operand
@@ -104,9 +104,9 @@ struct MmaLayout {
 // for a phase can be overtaken by the next: it needs something of the waiter's own.
 enum Bar : int { kFullX = 0, kFullY = 2, kFullZ = 4, kFreeX = 6, kFreeY = 8, kFreeZ = 10, kPatchY = 12, kPatchZ, kDecays, kDecaysFree, kScores,
                  kTransposed, kProbs, kFar, kFarRead, kNear, kOutRead, kWeighted, kWeightedLast, kUpdateFirst, kUpdate, kUpdateRead,
-                 kStateReady, kFullW, kFreeW, kHalfRead, kHalf, kTileDone, kDrain = kTileDone + 2,
+                 kStateReady, kFullW, kFreeW, kHalfRead, kHalf, kTileDone, kSent = kTileDone + 2, kStateLast, kDrain,
                  kBars = kDrain + 2 };
-static_assert(kBars <= 38, "barriers");
+static_assert(kBars <= 40, "barriers");
 
 template <int kValue> struct Int { static constexpr int value = kValue; };
 
@@ -189,12 +189,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i) {
             uint32_t arrivals = 1;
-            if (i >= kFreeY && i < kFreeZ) arrivals = kStateOnly ? 1 : kDots ? 3 : 2;
+            if (i >= kFreeY && i < kFreeZ) arrivals = kStateOnly || kDots ? 1 : 2;
             if (i >= kFreeZ && i < kPatchY) arrivals = kDots ? 2 : 1;
             if (i == kDecays) arrivals = 32;
             if (i == kDecaysFree) arrivals = kStateOnly ? 256 : 512;
             if (i == kProbs || i == kFarRead || i == kOutRead || i == kWeighted || i == kWeightedLast || i == kHalfRead || i == kUpdateRead ||
-                i == kStateReady)
+                i == kStateReady || i == kStateLast)
                 arrivals = 256;
             if (i == kFreeW) arrivals = 257;
             bar_init(bars + 8 * i, arrivals);
@@ -236,7 +236,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 const bool patch = live < p.tokens && t0 + kChunk > live;
                 const uint32_t Y = base + L::y + it % L::kYs * kTile, Z = base + L::z + it % L::kZs * kTile;
                 if (lane == 0) {  // in the order in which tiles become free
-                    if (it >= L::kYs) ok = wait(kFreeY + it % L::kYs, it / L::kYs - 1);
+                    if (kDots && it >= 1) ok = wait(kFreeY + it % L::kYs, (it - 1) / L::kYs);  // the state's last term was in it
+                    if (!kDots && it >= L::kYs) ok = wait(kFreeY + it % L::kYs, it / L::kYs - 1);
                     if (ok) load(&my, Y, p.dx, h / p.ydiv, t0, patch ? kPatchY : kFullY + it % L::kYs);
                     if (ok) loads_y = it + 1;
                     if (!kStateOnly) {
@@ -374,8 +375,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                             if (q < steps) mma_ts(tmem + L::weighted(q, 0), yo + q * 128, shape_u, true, tmem + L::tz);
                     }
                     mma_commit(bars + 8 * kUpdate);
-                    mma_commit(bars + 8 * (kFreeY + ys));
-                    if (kDots) mma_commit(bars + 8 * (kTileDone + ys));
+                    mma_commit(bars + 8 * ((kDots ? kTileDone : kFreeY) + ys));
                 }
                 if (!ok) {
                     mma_commit(bars + 8 * kDrain);
@@ -408,13 +408,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 };
                 auto sent = [&](int it) {  // ... and has been read from there
                     if constexpr (sizeof(Out) == 2) tma_store_wait_read();
-                    bar_arrive(bars + 8 * (kDots ? kFreeY + it % L::kYs : kFreeZ + it % L::kZs));
+                    bar_arrive(bars + 8 * (kDots ? kSent : kFreeZ + it % L::kZs));
                 };
                 auto chunk = [&](int it, auto odd) {  // a copy for each stage: their addresses are constants
                     constexpr int xs = odd.value % L::kXs, ys = odd.value % L::kYs, zs = odd.value % L::kZs;
                     const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32);
                     const uint32_t xo = operand(base + L::x + xs * kTile, kBlock), yo = operand(base + L::y + ys * kTile, kBlock),
-                                   zo = operand(base + L::z + zs * kTile, kBlock);
+                                   zo = operand(base + L::z + zs * kTile, kBlock), last = operand(base + L::y + (ys ^ 1) * kTile, kBlock);
                     if (!(wait(kFullX + xs, it / L::kXs) && wait(kFullY + ys, it / L::kYs) &&
                           (!kDots || (wait(kFullZ, it) && wait(kFullW, it))) && (it == 0 || wait(kOutRead, it - 1))))
                         return false;
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                         if (kk < kx) mma_ss(tmem + L::to, xo + k_step(kk), yo + k_step(kk), shape_p, kk > 0);
                     if (kDots) half_scores(0);
                     mma_commit(bars + 8 * kScores);
-                    mma_commit(bars + 8 * (kFreeY + ys));
+                    if (!kDots) mma_commit(bars + 8 * (kFreeY + ys));
                     if (it > 0) {
                         send(it - 1);
                         sent(it - 1);
@@ -436,16 +436,21 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                         mma_commit(bars + 8 * kHalf);
                         mma_commit(bars + 8 * kFreeW);
                     }
-                    if (!(wait(kStateReady, it) && wait(kProbs, it))) return false;
+                    if (!(wait(kStateReady, it) && (!kDots || wait(kStateLast, it)) && wait(kProbs, it))) return false;
                     tmem_after_sync();
+                    if (kDots)
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk)
+                            if (kk < kx) mma_ss(tmem + L::to, xo + k_step(kk), last + k_step(kk), shape_f, kk > 0);
 #pragma unroll
                     for (int t = kTerms - 1; t >= 0; --t)  // small terms first: every addition rounds the sum so far
 #pragma unroll
                         for (int kk = 0; kk < 8; ++kk)
                             if (kk < kx)
-                                mma_ss(tmem + L::to, xo + k_step(kk), so + t * (kTile >> 4) + k_step(kk), shape_f, t < kTerms - 1 || kk > 0);
+                                mma_ss(tmem + L::to, xo + k_step(kk), so + t * (kTile >> 4) + k_step(kk), shape_f, kDots || t < kTerms - 1 || kk > 0);
                     mma_commit(bars + 8 * kFar);
                     mma_commit(bars + 8 * (kFreeX + xs));
+                    if (kDots) mma_commit(bars + 8 * (kFreeY + (ys ^ 1)));
                     if (!(wait(kFullZ + zs, it / L::kZs) && wait(kFarRead, it))) return false;
                     tmem_after_sync();
 #pragma unroll
@@ -676,6 +681,25 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             }
             bar_arrive(bars + 8 * kStateReady);
         };
+        // kDots: the state's third term goes where the output of the chunk before has left from
+        auto publish_last = [&](int it) {
+            if (columns) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t t[3];
+                        split<3>(s[4 * c + j], t);
+                        w[j] = t[2];
+                    }
+                    *reinterpret_cast<uint4*>(sm8 + L::y + (it + 1) % L::kYs * kTile + side * kBlock + z * 128 + ((c ^ (z & 7)) << 4)) =
+                        make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                fence_smem_to_async();
+            }
+            bar_arrive(bars + 8 * kStateLast);
+        };
         if (!kStateOnly && count > 0) publish();
         bool ok = true;
         for (int it = 0; it < count; ++it) {
@@ -732,6 +756,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             tmem_wait_st();
             tmem_before_sync();
             bar_arrive(bars + 8 * kWeighted);
+            if constexpr (kDots) {
+                if (it > 0) ok = ok && wait(kSent, it - 1);
+                publish_last(it);
+            }
             if constexpr (L::kWeightsAtOnce == 2) {
                 ok = ok && wait(kUpdateFirst, it);
                 tmem_after_sync();
