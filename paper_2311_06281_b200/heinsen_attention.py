@@ -369,17 +369,16 @@ def _block_norms_forward(p: bytes, x):
 class _BlockNorms(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, branch, pre, post, gate, scale, eps):
-        p = _norms_problem("block_norms", x, pre, eps, scale, branch, gate, post)
         ctx.save_for_backward(x, branch, pre, post, gate)
-        ctx.problem = p  # the saved tensors keep its pointers alive
+        ctx.scale, ctx.eps = scale, eps
         ctx.set_materialize_grads(False)
-        return _block_norms_forward(p, x)
+        return _block_norms_forward(_norms_problem("block_norms", x, pre, eps, scale, branch, gate, post), x)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_r, d_y):
         x, branch, pre, post, gate = ctx.saved_tensors
-        p = ctx.problem
+        p = _norms_problem("block_norms", x, pre, ctx.eps, ctx.scale, branch, gate, post)  # a hook may have moved what was saved
         d_y = torch.zeros_like(x) if d_y is None else d_y.contiguous()
         d_r = None if d_r is None else d_r.contiguous()
         new = lambda t: None if t is None else torch.empty_like(t)  # noqa: E731
@@ -409,22 +408,23 @@ def block_norms(x: torch.Tensor, branch: torch.Tensor, pre_weight: torch.Tensor,
 class _GatedNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gate, weight, eps):
-        ctx.problem = p = _norms_problem("gated_norm", x, weight, eps, gate=gate)
         ctx.save_for_backward(x, gate, weight)
+        ctx.eps = eps
         y = torch.empty_like(x)
-        _launch(x.device, _call().gated_forward, p, y.data_ptr())
+        _launch(x.device, _call().gated_forward, _norms_problem("gated_norm", x, weight, eps, gate=gate), y.data_ptr())
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_y):
         x, gate, weight = ctx.saved_tensors
+        p = _norms_problem("gated_norm", x, weight, ctx.eps, gate=gate)  # a hook may have moved what was saved
         d_y = d_y.contiguous()
         dx, dweight = torch.empty_like(x), torch.empty_like(weight)
         dgate = None if gate is None else torch.empty_like(gate)
         call = _call()
-        ws = _space(call.gated_space(ctx.problem), x.device)
-        _launch(x.device, call.gated_backward, ctx.problem, d_y.data_ptr(), dx.data_ptr(), _addr(dgate), dweight.data_ptr(),
+        ws = _space(call.gated_space(p), x.device)
+        _launch(x.device, call.gated_backward, p, d_y.data_ptr(), dx.data_ptr(), _addr(dgate), dweight.data_ptr(),
                 ws.data_ptr(), ws.numel())
         return dx, dgate, dweight, None
 
