@@ -51,18 +51,20 @@ Layout choose(int dim, bool f32, bool vectors) {
     return {vec, 4, 1024};
 }
 
+struct Kernel { const void* fn; size_t smem; };  // beside the rows that share a CTA
 template <class T, int kVec, int kNv, int kThreads>
-const void* pick(Which w) {
+Kernel pick(Which w) {
     switch (w) {
-        case kBlockForward: return (const void*)hn::block_norms_forward_kernel<T, kVec, kNv, kThreads>;
-        case kBlockBackward: return (const void*)hn::block_norms_backward_kernel<T, kVec, kNv, kThreads>;
-        case kGatedForward: return (const void*)hn::gated_norm_forward_kernel<T, kVec, kNv, kThreads>;
-        case kGatedBackward: return (const void*)hn::gated_norm_backward_kernel<T, kVec, kNv, kThreads>;
+        case kBlockForward: return {(const void*)hn::block_norms_forward_kernel<T, kVec, kNv, kThreads>, 0};
+        case kBlockBackward:
+            return {(const void*)hn::block_norms_backward_kernel<T, kVec, kNv, kThreads>, hn::Ahead<T, kVec, kNv, kThreads>::kBytes};
+        case kGatedForward: return {(const void*)hn::gated_norm_forward_kernel<T, kVec, kNv, kThreads>, 0};
+        case kGatedBackward: return {(const void*)hn::gated_norm_backward_kernel<T, kVec, kNv, kThreads>, 0};
     }
-    return nullptr;
+    return {nullptr, 0};
 }
 template <class T, int kVec>
-const void* kernel_for(Which w, const Layout& l) {
+Kernel kernel_for(Which w, const Layout& l) {
     if (l.vec == 1) {
         if (l.threads == 32) return pick<T, 1, 4, 32>(w);
         if (l.threads == 128) return pick<T, 1, 4, 128>(w);
@@ -78,16 +80,16 @@ const void* kernel_for(Which w, const Layout& l) {
         case 512: return l.nv == 2 ? pick<T, kVec, 2, 512>(w) : pick<T, kVec, 4, 512>(w);
     }
     if constexpr (kVec == 4) return pick<T, kVec, 4, 1024>(w);
-    return nullptr;  // 8 elements a vector: 512 threads of 4 already hold the widest row
+    return {nullptr, 0};  // 8 elements a vector: 512 threads of 4 already hold the widest row
 }
-const void* kernel_for(Which w, const Layout& l, bool f32) {
+Kernel kernel_for(Which w, const Layout& l, bool f32) {
     return f32 ? kernel_for<float, 4>(w, l) : kernel_for<__nv_bfloat16, 8>(w, l);
 }
 
-hs_status launch(const void* fn, const Norms& n, long long grid, int threads, size_t smem, cudaStream_t stream) {
+hs_status launch(const Kernel& k, const Norms& n, long long grid, int threads, size_t smem, cudaStream_t stream) {
     Norms copy = n;
     void* args[] = {&copy};
-    const cudaError_t e = cudaLaunchKernel(fn, dim3((unsigned)grid), dim3((unsigned)threads), args, smem, stream);
+    const cudaError_t e = cudaLaunchKernel(k.fn, dim3((unsigned)grid), dim3((unsigned)threads), args, smem + k.smem, stream);
     if (e != cudaSuccess) return hs_internal::cuda_fail("cudaLaunchKernel (norms)", e);
     hs_internal::count_launches(1);
     return HS_OK;
@@ -120,15 +122,15 @@ Norms make(const heinsen_norms_problem* p) {
 
 // CTAs of the backward kernels, which stay and sum over their rows: as many as are resident at once.  Every CTA leaves one row
 // of partial sums behind.
-long long stay(long long rows, const Layout& l) {
+long long stay(long long rows, const Layout& l, bool ahead) {
     const int threads = std::max(128, l.threads), per_cta = threads / l.threads;
-    const long long most = 148ll * std::max(1, hn::resident(l.vec * l.nv, l.threads));
+    const long long most = 148ll * std::max(1, hn::resident(l.vec * l.nv, l.threads, ahead));
     return std::max(1ll, std::min(most, (rows + per_cta - 1) / per_cta));
 }
 
 // How the rows of a block's backward pass are cut into units (see the kernel).
 void cut(const heinsen_norms_problem* p, const Layout& l, long long* units, int* splits, long long* grid) {
-    const long long want = stay(p->rows, l);
+    const long long want = stay(p->rows, l, hn::ahead_fits(l.vec, l.nv, l.threads, p->dtype == HS_F32 ? 4 : 2));
     const bool wide = p->gate && p->gate_rows > 1;
     const long long gates = wide ? p->rows / p->gate_rows : 1, per_gate = wide ? p->gate_rows : p->rows;
     // whole rows of the gate to each CTA where there are enough of them, else each is split
@@ -250,8 +252,8 @@ hs_status heinsen_block_norms_backward(const heinsen_norms_problem* p, const voi
 size_t heinsen_gated_norm_workspace_bytes(const heinsen_norms_problem* p) {
     if (!p || p->rows < 0 || p->dim < 1 || p->dim > kMaxDim) return 0;
     const bool f32 = p->dtype == HS_F32;
-    const long long grid = std::max(stay(p->rows, choose(p->dim, f32, false)),
-                                    p->dim * (f32 ? 4 : 2) % 16 ? 1 : stay(p->rows, choose(p->dim, f32, true)));
+    const long long grid = std::max(stay(p->rows, choose(p->dim, f32, false), false),
+                                    p->dim * (f32 ? 4 : 2) % 16 ? 1 : stay(p->rows, choose(p->dim, f32, true), false));
     return up256((size_t)grid * p->dim * 4);
 }
 
@@ -277,7 +279,7 @@ hs_status heinsen_gated_norm_backward(const heinsen_norms_problem* p, const void
     Norms n = make(p);
     n.d_y = d_y; n.dx = dx; n.dgate = dgate;
     n.part_pre = static_cast<float*>(workspace);
-    const long long grid = stay(p->rows, l);
+    const long long grid = stay(p->rows, l, false);
     const int threads = std::max(128, l.threads), sub = threads / l.threads;
     st = launch(kernel_for(kGatedBackward, l, f32), n, grid, threads, sub > 1 ? (size_t)sub * p->dim * 4 : 0, stream);
     if (st == HS_OK) st = sum_parts(n.part_pre, dweight, nullptr, nullptr, 1, grid, p->dim, w32, stream);

@@ -13,10 +13,11 @@ namespace hn {
 template <class T, int kVec> struct alignas(sizeof(T) * kVec < 16 ? sizeof(T) * kVec : 16) Vec { T v[kVec]; };
 
 // CTAs of a backward kernel that shall be resident on an SM beside one another: 768 threads where a thread has 8 elements of a
-// row (84 registers each), so that there are rows in flight while others are at their barriers.
-__host__ __device__ constexpr int resident(int elems, int row_threads) {
+// row (84 registers each), so that there are rows in flight while others are at their barriers; 512 where the next row is on
+// its way in any case (16384 rows of 2048 bf16: 154 us, 768 threads and their spills 233 us).
+__host__ __device__ constexpr int resident(int elems, int row_threads, bool ahead) {
     const int threads = row_threads < 128 ? 128 : row_threads;
-    return threads * 2 > 1024 ? 1 : (elems > 8 ? 512 : 768) / threads;
+    return threads * 2 > 1024 ? 1 : (elems > 8 || ahead ? 512 : 768) / threads;
 }
 
 __device__ __forceinline__ float to_f(float v) { return v; }
@@ -74,6 +75,48 @@ struct Slice {
                 for (int e = 0; e < kVec; ++e) f.v[e] = from_f<U>(from[v * kVec + e]);
                 *reinterpret_cast<Vec<U, kVec>*>(row + c) = f;
             }
+        }
+    }
+};
+
+// Do two stages of five tensors, beside the sums of rows that share a CTA, fit what a kernel has without asking for more?
+__host__ __device__ constexpr bool ahead_fits(int vec, int nv, int row_threads, int elem) {
+    const int threads = row_threads < 128 ? 128 : row_threads;
+    return vec * elem == 16 && 2 * 5 * nv * 16 * threads + (row_threads < 128 ? 128 * vec * nv * 4 : 0) <= 47 * 1024;
+}
+
+// The rows of a block's backward pass on their way while others are worked on: every thread copies its own 16-byte pieces of the
+// next row's tensors to shared memory and reads nobody else's, so no barrier belongs to it.  Two stages, as long as they leave
+// room for the CTAs of resident(); wider rows have enough in flight without it (8192 float32: 208 us so, 245 us with one stage).
+template <class T, int kVec, int kNv, int kRowThreads>
+struct Ahead {
+    static constexpr int kThreads = kRowThreads < 128 ? 128 : kRowThreads, kPiece = kNv * 16 * kThreads, kTensors = 5;
+    static constexpr bool kOn = ahead_fits(kVec, kNv, kRowThreads, sizeof(T));
+    static constexpr int kBytes = kOn ? 2 * kTensors * kPiece : 0;
+    static __device__ __forceinline__ void copy(uint8_t* sm, int stage, int tensor, const T* row, int t, int dim) {
+#pragma unroll
+        for (int v = 0; v < kNv; ++v) {
+            const int c = (v * kRowThreads + t) * kVec;
+            if (c < dim)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(
+                                 sm + (stage * kTensors + tensor) * kPiece + (v * kThreads + threadIdx.x) * 16)),
+                             "l"(row + c)
+                             : "memory");
+        }
+    }
+    static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    static __device__ __forceinline__ void arrived(bool next) {  // this row's, of which the next's may be behind
+        if (next) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+    static __device__ __forceinline__ void read(float (&to)[kVec * kNv], const uint8_t* sm, int stage, int tensor, int t, int dim) {
+#pragma unroll
+        for (int v = 0; v < kNv; ++v) {
+            const bool in = (v * kRowThreads + t) * kVec < dim;
+            Vec<T, kVec> f;
+            if (in) f = *reinterpret_cast<const Vec<T, kVec>*>(sm + (stage * kTensors + tensor) * kPiece + (v * kThreads + threadIdx.x) * 16);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) to[v * kVec + e] = in ? to_f(f.v[e]) : 0.0f;
         }
     }
 };
@@ -162,11 +205,13 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) block_n
 // gate).  A CTA takes a contiguous run of units and keeps the weights' sums over all of them; only the gate's sum starts
 // anew with each unit.
 template <class T, int kVec, int kNv, int kRowThreads>
-__global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, resident(kVec * kNv, kRowThreads)) block_norms_backward_kernel(const Norms p) {
+__global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, resident(kVec * kNv, kRowThreads, Ahead<T, kVec, kNv, kRowThreads>::kOn)) block_norms_backward_kernel(const Norms p) {
     using S = Slice<T, kVec, kNv, kRowThreads>;
     constexpr int kE = S::kElems, kRowsPerCta = kRowThreads < 128 ? 128 / kRowThreads : 1;
+    using A = Ahead<T, kVec, kNv, kRowThreads>;
     __shared__ float red[3 * 64];
-    extern __shared__ float join[];  // [kRowsPerCta][dim], only where rows share a CTA
+    extern __shared__ __align__(16) uint8_t sm[];
+    float* join = reinterpret_cast<float*>(sm + A::kBytes);  // [kRowsPerCta][dim], only where rows share a CTA
     int turn = 0;
     const int t = threadIdx.x % kRowThreads, sub = threadIdx.x / kRowThreads;
     const float inv = 1.0f / (float)p.dim;
@@ -195,17 +240,40 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, residen
         const long long last = first + per_unit < base + per_gate ? first + per_unit : base + per_gate;
 #pragma unroll
         for (int e = 0; e < kE; ++e) a_gate[e] = 0.0f;
+        auto fetch = [&](long long at, int stage) {
+            const long long row = at + sub < last ? at + sub : last - 1;
+            A::copy(sm, stage, 0, static_cast<const T*>(p.branch) + row * p.dim, t, p.dim);
+            A::copy(sm, stage, 1, static_cast<const T*>(p.x) + row * p.dim, t, p.dim);
+            A::copy(sm, stage, 2, static_cast<const T*>(p.d_y) + row * p.dim, t, p.dim);
+            if (p.gate) A::copy(sm, stage, 3, static_cast<const T*>(p.gate) + (row / p.gate_rows) * p.dim, t, p.dim);
+            if (p.d_r) A::copy(sm, stage, 4, static_cast<const T*>(p.d_r) + row * p.dim, t, p.dim);
+            A::commit();
+        };
+        if (A::kOn && first < last) fetch(first, 0);
+        int stage = 0;
         for (long long at = first; at < last; at += kRowsPerCta) {
-            const bool live = at + sub < last;
+            const bool live = at + sub < last, next = at + kRowsPerCta < last;
             const long long row = live ? at + sub : last - 1;
             float h[kE], x[kE], g[kE], dy[kE], w[kE];
-            S::load(h, static_cast<const T*>(p.branch) + row * p.dim, t, p.dim);
-            S::load(x, static_cast<const T*>(p.x) + row * p.dim, t, p.dim);
-            S::load(dy, static_cast<const T*>(p.d_y) + row * p.dim, t, p.dim);
-            if (p.gate) S::load(g, static_cast<const T*>(p.gate) + (row / p.gate_rows) * p.dim, t, p.dim);
-            else
+            if constexpr (A::kOn) {
+                if (next) fetch(at + kRowsPerCta, stage ^ 1);
+                A::arrived(next);
+                A::read(h, sm, stage, 0, t, p.dim);
+                A::read(x, sm, stage, 1, t, p.dim);
+                A::read(dy, sm, stage, 2, t, p.dim);
+                if (p.gate) A::read(g, sm, stage, 3, t, p.dim);
+                else
 #pragma unroll
-                for (int e = 0; e < kE; ++e) g[e] = 1.0f;
+                    for (int e = 0; e < kE; ++e) g[e] = 1.0f;
+            } else {
+                S::load(h, static_cast<const T*>(p.branch) + row * p.dim, t, p.dim);
+                S::load(x, static_cast<const T*>(p.x) + row * p.dim, t, p.dim);
+                S::load(dy, static_cast<const T*>(p.d_y) + row * p.dim, t, p.dim);
+                if (p.gate) S::load(g, static_cast<const T*>(p.gate) + (row / p.gate_rows) * p.dim, t, p.dim);
+                else
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) g[e] = 1.0f;
+            }
             float rs1 = 1.0f;
             if (p.post) {
                 float s[1] = {0.0f};
@@ -239,7 +307,8 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, residen
                 dy[e] = norm_back(dy[e] * w[e], m, mean, rs2, p.dim, p.eps);
             }
             if (p.d_r) {
-                S::load(w, static_cast<const T*>(p.d_r) + row * p.dim, t, p.dim);
+                if constexpr (A::kOn) A::read(w, sm, stage, 4, t, p.dim);
+                else S::load(w, static_cast<const T*>(p.d_r) + row * p.dim, t, p.dim);
 #pragma unroll
                 for (int e = 0; e < kE; ++e) dy[e] += w[e];
             }
@@ -274,6 +343,7 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, residen
                 for (int e = 0; e < kE; ++e) dy[e] = norm_back(dy[e], h[e], s1[0] * inv, rs1, p.dim, p.eps);
             }
             if (live) S::store(dy, static_cast<T*>(p.dbranch) + row * p.dim, t, p.dim);
+            stage ^= 1;
         }
         if (wide_gate) flush(a_gate, p.part_gate + u * p.dim);
     }
@@ -309,7 +379,7 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) gated_n
 }
 
 template <class T, int kVec, int kNv, int kRowThreads>
-__global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, resident(kVec * kNv, kRowThreads)) gated_norm_backward_kernel(const Norms p) {
+__global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, resident(kVec * kNv, kRowThreads, false)) gated_norm_backward_kernel(const Norms p) {
     using S = Slice<T, kVec, kNv, kRowThreads>;
     constexpr int kE = S::kElems, kRowsPerCta = kRowThreads < 128 ? 128 / kRowThreads : 1;
     __shared__ float red[3 * 64];
