@@ -43,13 +43,6 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// without a suspended wait, for a thread that has several barriers to watch
-__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
 __device__ __forceinline__ void tma_store_4d(const void* map, int x, int y, int z, int w, uint32_t from) {
     asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(map), "r"(x), "r"(y),
                  "r"(z), "r"(w), "r"(from)
@@ -85,11 +78,6 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ void tmem_ld16(uint32_t (&v)[16], uint32_t addr) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
                  : HA_R8(v, 0), HA_R8(v, 8) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void tmem_ld32(uint32_t (&v)[32], uint32_t addr) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
-                 : HA_R8(v, 0), HA_R8(v, 8), HA_R8(v, 16), HA_R8(v, 24) : "r"(addr) : "memory");
 }
 // The same without the wait, for a load that other work hides: tmem_ready() before the registers are used.
 __device__ __forceinline__ void tmem_ld16_early(uint32_t (&v)[16], uint32_t addr) {
@@ -158,8 +146,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float first, float second) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(second), "f"(first));
     return r;
 }
-__device__ __forceinline__ float low_bf16(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float high_bf16(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
 // ---- float32 pairs: one instruction for two elements
 using pair = unsigned long long;

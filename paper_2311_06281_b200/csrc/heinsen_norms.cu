@@ -28,7 +28,8 @@ bool vectors_fit(const heinsen_norms_problem* p, std::initializer_list<const voi
 
 // Rows are laid over threads so that one thread has 4 to 16 elements (float32) or 8 to 16 (bf16): fewer leave the sums
 // over a row's threads dominant, more do not fit the registers of the backward pass, which keeps three running sums and
-// four rows of its slice.
+// four rows of its slice.  Measured at 2048 bf16: 256 threads to a row 69 us forward and 168 us backward (without the copies
+// ahead), a warp to a row 102 us and 230 us.
 struct Layout { int vec, nv, threads; };
 Layout choose(int dim, bool f32, bool vectors) {
     if (!vectors) {

@@ -2,6 +2,11 @@
 // with its backward pass.  All are bound by HBM: every input element is read once and every output written once, the row
 // stays in registers between its reductions, and the gradients that are summed over rows are kept in registers by threads
 // that own the same columns of every row they see.
+//
+// Measured, bf16, and the time of the same bytes at a copy's rate: block, 16384 rows of 2048: forward 69 us (51), backward 154 us
+// (82); gated, 16384 x 16 rows of 128: forward 43 us (31), backward 69 us (51).  Between its loads and its stores a row waits for
+// two sums over its threads (three on the way back), each some 500 clocks: other rows of the SM have to cover that, and how many
+// fit is up to registers.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
