@@ -15,7 +15,7 @@
 // rounding is as large).
 //
 // Measured, [8 x 2048 tokens, 16 heads of 128] (128 CTAs): forward and dv 76 us each, 268 MB at 3.5 TB/s; with kDots 151 us (dk)
-// and 174 us (dq).  Neither memory (36% of a copy's rate) nor the tensor core (31% of its cycles) bounds it: a chunk's steps wait
+// and 171 us (dq).  Neither memory (36% of a copy's rate) nor the tensor core (31% of its cycles) bounds it: a chunk's steps wait
 // for each other, 7000 to 8000 clocks of them, and shared memory holds one CTA.  Of those the output's chain has: scores 520, P
 // 2000, X S 1100, scaling its rows 600, P Z 900, the output 760; the state's: Z^T 500, its terms 2400, the update 2000, reading
 // it 500, publishing it 500.  What did not help: the output from registers straight to memory (2200 clocks for 760), one warp that
@@ -717,18 +717,6 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             const float whole = read1(s_whole);
             const pair whole2 = make_pair2(whole, whole);
             const bool crosses = read1(s_whole + 1) > kNothingCrosses;
-            if constexpr (kDots && !kRev) {
-                if (crosses && columns && mine) {
-                    float4* to = p.dump + ((long long)bh * p.chunks + t0 / kChunk) * 4096 + side * 2048 + z;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        float4 f;
-                        parts(s[2 * j], f.x, f.y);
-                        parts(s[2 * j + 1], f.z, f.w);
-                        to[j * 128] = f;
-                    }
-                }
-            }
             ok = ok && wait(kTransposed, it);
             tmem_after_sync();
             uint32_t v[16];
@@ -777,6 +765,18 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 tmem_wait_st();
                 tmem_before_sync();
                 bar_arrive(bars + 8 * kWeightedLast);
+            }
+            if constexpr (kDots && !kRev) {  // the state from before this chunk, while its update is formed
+                if (crosses && columns && mine) {
+                    float4* to = p.dump + ((long long)bh * p.chunks + t0 / kChunk) * 4096 + side * 2048 + z;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float4 f;
+                        parts(s[2 * j], f.x, f.y);
+                        parts(s[2 * j + 1], f.z, f.w);
+                        to[j * 128] = f;
+                    }
+                }
             }
             if constexpr (kDots && kRev) {  // <S, D> of this chunk, while its update is formed
                 pair sum = 0;
