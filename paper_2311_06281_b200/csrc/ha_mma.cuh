@@ -200,10 +200,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             if (i >= kFreeY && i < kFreeZ) arrivals = kStateOnly || kDots ? 1 : 2;
             if (i >= kFreeZ && i < kPatchY) arrivals = kDots ? 2 : 1;
             if (i == kDecays) arrivals = 32;
-            if (i == kDecaysFree) arrivals = kStateOnly ? 256 : 512;
+            if (i == kDecaysFree) arrivals = 512;
             if (i == kProbs || i == kFarRead || i == kOutRead || i == kWeighted || i == kWeightedLast || i == kHalfRead || i == kUpdateRead ||
                 i == kStateReady || i == kStateLast)
-                arrivals = 256;
+                arrivals = kStateOnly && i == kWeighted ? 512 : 256;
             if (i == kFreeW) arrivals = 257;
             bar_init(bars + 8 * i, arrivals);
         }
@@ -224,6 +224,35 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
     if (tid == 0 && *s_tmem != 0) *stop = 1 + kBars;  // all columns were asked for: they start at 0
     constexpr uint32_t tmem = 0;
 
+    // (w Z)^T of tokens 16 q0 to 16 q1, for one z of it each thread: its terms, the smallest first
+    auto weigh = [&](uint32_t at, int q0, int q1, uint32_t (&last)[L::kWeightsAtOnce == 2 ? 4 : 1][8]) {
+        uint32_t v[16];
+        if (q0 < q1) tmem_ld16_early(v, at + L::tz + 16 * q0);
+#pragma unroll L::kWeightsAtOnce == 2 ? 4 : 1
+        for (int i = 0; i < 4; ++i) {
+            const int q = q0 + i;
+            if (q >= q1) break;
+            uint32_t w[3][8];
+            tmem_ready(v);
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                const float4 f = read4(w_st + 16 * q + j);
+                uint32_t t[3];
+                split<3>(mul2(make_pair2(v[j], v[j + 1]), make_pair2(f.x, f.y)), t);
+#pragma unroll
+                for (int u = 0; u < 3; ++u) w[u][j / 2] = t[u];
+                split<3>(mul2(make_pair2(v[j + 2], v[j + 3]), make_pair2(f.z, f.w)), t);
+#pragma unroll
+                for (int u = 0; u < 3; ++u) w[u][j / 2 + 1] = t[u];
+            }
+            if (q + 1 < q1) tmem_ld16_early(v, at + L::tz + 16 * (q + 1));
+#pragma unroll
+            for (int u = 0; u < L::kWeightsAtOnce; ++u) tmem_st8(at + L::weighted(q, u), w[2 - u]);
+            if constexpr (L::kWeightsAtOnce == 2)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) last[i][u] = w[0][u];
+        }
+    };
     if (warp >= 16) {
         give_registers<kFeedRegs>();
         // The thread that issues the output's products shares a scheduler with the rows that have least to do: the first 32
@@ -485,6 +514,23 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
     } else if (warp < 8) {
         give_registers<kRowRegs>();
         // ---------------------------------------------------------------- P and the output: two threads have one token's row
+        if (kStateOnly) {  // no output: half of the weighing
+            const int side = warp >> 2;
+            const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+            bool ok = true;
+            for (int it = 0; it < count; ++it) {
+                const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32);
+                uint32_t none[L::kWeightsAtOnce == 2 ? 4 : 1][8];
+                ok = ok && wait(kDecays, it) && wait(kTransposed, it);
+                tmem_after_sync();
+                weigh(at, 4 * side + 2, min(steps, 4 * side + 4), none);
+                release_reads();
+                bar_arrive(bars + 8 * kDecaysFree);
+                tmem_wait_st();
+                tmem_before_sync();
+                bar_arrive(bars + 8 * kWeighted);
+            }
+        }
         if (!kStateOnly) {
             const int side = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
             const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
@@ -719,34 +765,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             const bool crosses = read1(s_whole + 1) > kNothingCrosses;
             ok = ok && wait(kTransposed, it);
             tmem_after_sync();
-            uint32_t v[16];
             uint32_t last[L::kWeightsAtOnce == 2 ? 4 : 1][8];  // first terms, where they have to wait
-            const int q0 = 4 * side, q1 = min(steps, q0 + 4);
-            if (q0 < q1) tmem_ld16_early(v, at + L::tz + 16 * q0);
-#pragma unroll L::kWeightsAtOnce == 2 ? 4 : 1
-            for (int i = 0; i < 4; ++i) {
-                const int q = q0 + i;
-                if (q >= q1) break;
-                uint32_t w[3][8];
-                tmem_ready(v);
-#pragma unroll
-                for (int j = 0; j < 16; j += 4) {
-                    const float4 f = read4(w_st + 16 * q + j);
-                    uint32_t t[3];
-                    split<3>(mul2(make_pair2(v[j], v[j + 1]), make_pair2(f.x, f.y)), t);
-#pragma unroll
-                    for (int u = 0; u < 3; ++u) w[u][j / 2] = t[u];
-                    split<3>(mul2(make_pair2(v[j + 2], v[j + 3]), make_pair2(f.z, f.w)), t);
-#pragma unroll
-                    for (int u = 0; u < 3; ++u) w[u][j / 2 + 1] = t[u];
-                }
-                if (q + 1 < q1) tmem_ld16_early(v, at + L::tz + 16 * (q + 1));
-#pragma unroll
-                for (int u = 0; u < L::kWeightsAtOnce; ++u) tmem_st8(at + L::weighted(q, u), w[2 - u]);  // the smallest first
-                if constexpr (L::kWeightsAtOnce == 2)
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) last[i][u] = w[0][u];
-            }
+            const int q0 = 4 * side, q1 = min(steps, q0 + (kStateOnly ? 2 : 4));
+            weigh(at, q0, q1, last);
             release_reads();
             bar_arrive(bars + 8 * kDecaysFree);
             tmem_wait_st();
