@@ -223,11 +223,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
     tmem_after_sync();
     if (tid == 0 && *s_tmem != 0) *stop = 1 + kBars;  // all columns were asked for: they start at 0
     constexpr uint32_t tmem = 0;
+    // a pass without an output has its columns for Z^T: the next chunk's is formed behind this one's update
+    constexpr uint32_t zt = kStateOnly ? L::to : L::tz;
 
     // (w Z)^T of tokens 16 q0 to 16 q1, for one z of it each thread: its terms, the smallest first
     auto weigh = [&](uint32_t at, int q0, int q1, uint32_t (&last)[L::kWeightsAtOnce == 2 ? 4 : 1][8]) {
         uint32_t v[16];
-        if (q0 < q1) tmem_ld16_early(v, at + L::tz + 16 * q0);
+        if (q0 < q1) tmem_ld16_early(v, at + zt + 16 * q0);
 #pragma unroll L::kWeightsAtOnce == 2 ? 4 : 1
         for (int i = 0; i < 4; ++i) {
             const int q = q0 + i;
@@ -245,7 +247,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
 #pragma unroll
                 for (int u = 0; u < 3; ++u) w[u][j / 2 + 1] = t[u];
             }
-            if (q + 1 < q1) tmem_ld16_early(v, at + L::tz + 16 * (q + 1));
+            if (q + 1 < q1) tmem_ld16_early(v, at + zt + 16 * (q + 1));
 #pragma unroll
             for (int u = 0; u < L::kWeightsAtOnce; ++u) tmem_st8(at + L::weighted(q, u), w[2 - u]);
             if constexpr (L::kWeightsAtOnce == 2)
@@ -382,20 +384,25 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             // to 64).
             if (elect_one()) {
                 const uint32_t shape_t = mma_shape(16, kColMajorA), shape_u = mma_shape((p.dx + 15) / 16 * 16, kColMajorB);
-                bool ok = true;
-                for (int it = 0; it < count; ++it) {
-                    const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32), zs = it % L::kZs, ys = it % L::kYs;
-                    const uint32_t zo = operand(base + L::z + zs * kTile, kBlock), yo = operand(base + L::y + ys * kTile, kBlock),
-                                   ident = operand(base + L::ident, 256);
-                    ok = wait(kFullZ + zs, it / L::kZs) && (it == 0 || wait(kUpdateRead, it - 1));
-                    if (!ok) break;
+                auto transpose = [&](int it) {
+                    const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32), zs = it % L::kZs;
+                    const uint32_t zo = operand(base + L::z + zs * kTile, kBlock), ident = operand(base + L::ident, 256);
+                    if (!(wait(kFullZ + zs, it / L::kZs) && (kStateOnly || it == 0 || wait(kUpdateRead, it - 1)))) return false;
                     tmem_after_sync();
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
-                        if (q < steps) mma_ss<plain_layout(128)>(tmem + L::tz + 16 * q, zo + q * 128, ident, shape_t, false);
+                        if (q < steps) mma_ss<plain_layout(128)>(tmem + zt + 16 * q, zo + q * 128, ident, shape_t, false);
                     mma_commit(bars + 8 * kTransposed);
                     if (kDots || kStateOnly) mma_commit(bars + 8 * (kFreeZ + zs));
                     else mma_commit(bars + 8 * (kTileDone + zs));
+                    return true;
+                };
+                bool ok = !kStateOnly || count == 0 || transpose(0);
+                for (int it = 0; it < count && ok; ++it) {
+                    const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32), ys = it % L::kYs;
+                    const uint32_t yo = operand(base + L::y + ys * kTile, kBlock);
+                    if (!kStateOnly && !(ok = transpose(it))) break;
+                    if (kStateOnly && it > 0 && !(ok = wait(kUpdateRead, it - 1))) break;
                     if (!(ok = wait(kFullY + ys, it / L::kYs) && wait(kWeighted, it))) break;
                     tmem_after_sync();
 #pragma unroll
@@ -413,6 +420,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     }
                     mma_commit(bars + 8 * kUpdate);
                     mma_commit(bars + 8 * ((kDots ? kTileDone : kFreeY) + ys));
+                    if (kStateOnly && it + 1 < count) ok = transpose(it + 1);
                 }
                 if (!ok) {
                     mma_commit(bars + 8 * kDrain);
@@ -521,7 +529,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             for (int it = 0; it < count; ++it) {
                 const int steps = 2 * min(4, (live - chunk_at(it) * kChunk + 31) / 32);
                 uint32_t none[L::kWeightsAtOnce == 2 ? 4 : 1][8];
-                ok = ok && wait(kDecays, it) && wait(kTransposed, it);
+                ok = ok && wait(kDecays, it) && wait(kTransposed, it) && (it == 0 || wait(kUpdate, it - 1));
                 tmem_after_sync();
                 weigh(at, 4 * side + 2, min(steps, 4 * side + 4), none);
                 release_reads();
