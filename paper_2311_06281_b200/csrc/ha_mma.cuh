@@ -68,8 +68,8 @@ struct MmaPass {
     float* seg_state;
     float* seg_decay;
     // For the decay gradients (kDots), by token and for each half of the columns, [2][batch * heads][tokens]: the row sums of
-    // W below (reversed: above) the diagonal, and w_i . (X S)_i.  The forward pass also leaves the state before every chunk in `dump`, the reversed one multiplies it with its own: cross[batch * heads][chunks][8], a warp
-    // each.
+    // W below (reversed: above) the diagonal, and w_i . (X S)_i.  The forward pass also leaves the state before every chunk in
+    // `dump`, the reversed one multiplies it with its own: cross[batch * heads][chunks][8], one for each warp.
     int wdiv;
     double* dots;
     float* dots_far;
@@ -873,7 +873,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
 // dlog_a of one chunk from what the two passes left (the formulas at the head of ha_simt.cuh): with r and r', u and u' the row
 // sums and the far dots of the dq and the dk pass,
 //     dlog_a_t = sum_{i>=t} (r_i - u_i + r'_i) + sum_{j<t} u'_j + e^{c_C} scale <S, D>.
-// Pairs inside the chunk that both lie behind t are in r and in u and cancel.  A thread has one token; sums in 64 bits.  part (fixed decays): only the sum over the chunk's tokens.
+// Pairs inside the chunk that both lie behind t are in r and in u and cancel.  A thread has one token; sums in 64 bits.
+// part (fixed decays): only the sum over the chunk's tokens.
 __global__ void __launch_bounds__(kChunk) join_decay_grad_kernel(const double* r, const double* u, const float* rf, const float* uf, const float* cross,
                                                                  const float* log_a, long long ab, long long at, long long ah,
                                                                  const int* lengths, int tokens, int heads, int chunks, long long side,

@@ -88,3 +88,19 @@ def test_steps_of_few_and_many_states(ha, heads, kd, vd):  # noqa: F811
     o = ha.decay_attention_step(q, k, v, log_a, state)
     close(state, want, "state")
     close(o, kd ** -0.5 * (q.double().unsqueeze(-2) @ want).squeeze(-2), "o")
+
+
+@pytest.mark.parametrize("dtype,t", [(BF16, 1400), (BF16, 100), (F32, 100)])
+def test_a_kept_workspace_reports_no_fault(ha, dtype, t):  # noqa: F811
+    from paper_2311_06281_b200 import heinsen_scan
+    q, k, v, log_a, s0 = make(1, t, 2, 2, 2, 2, 64, 64, dtype, state=True)
+    ws = ha.workspace(q, k, v, log_a)
+    want = ha.decay_attention(q, k, v, log_a, s0)
+    for fill in (0, 0xFF):  # its contents do not matter
+        ws.fill_(fill)
+        for _ in range(2):
+            got = ha.decay_attention(q, k, v, log_a, s0, workspace=ws)
+            heinsen_scan.check(ws)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(Exception, match="(?i)workspace"):
+        ha.decay_attention(q, k, v, log_a, s0, workspace=ws[:256] if ws.numel() > 256 else ws[:0])
