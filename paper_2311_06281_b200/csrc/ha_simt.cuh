@@ -57,6 +57,11 @@ struct Pass {
     int segments, seg_chunks;
     float* seg_state;
     float* seg_decay;
+    int rev;
+};
+// Passes over the same sequences that do not depend on one another go in one launch, blockIdx.y each.
+struct Passes {
+    Pass p[3];
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -111,7 +116,7 @@ __device__ __forceinline__ void add4(float4& acc, float w, const float4& v) {
 // row for 32 columns, 43 us with two for 64; the sums of the states before it 25 us and 16 us).  The next chunk's first 64
 // columns travel meanwhile: waiting for them took half of a chunk's time.
 template <class T, bool kRev, class OutT, bool kStateOnly, int kCols>
-__global__ void __launch_bounds__(kSimtThreads) simt_pass_kernel(const Pass p) {
+__device__ __forceinline__ void simt_pass(const Pass& p) {
     constexpr int kLanes = kCols / 4, kSweep = kSimtThreads / kLanes, kPer = kSimtChunk / kSweep;
     extern __shared__ __align__(16) float sm[];
     const int dxp = p.dx + 4 - (p.dx & 3) + ((p.dx & 3) ? 4 : 0);  // a multiple of 4, at least dx + 4: rows shifted by 4 banks
@@ -129,6 +134,7 @@ __global__ void __launch_bounds__(kSimtThreads) simt_pass_kernel(const Pass p) {
     const int segment = blockIdx.x % cuts, item = blockIdx.x / cuts;
     const int z0 = item % ztiles * kCols;
     const int bh = item / ztiles, b = bh / p.heads, h = bh % p.heads;
+    if (bh >= p.batch * p.heads) return;  // another pass has more columns
     const int live = live_tokens(p.lengths, b, p.tokens);
     const T* gx = static_cast<const T*>(p.x.ptr) + b * p.x.sb + (h / p.x.div) * p.x.sh;
     const T* gy = static_cast<const T*>(p.y.ptr) + b * p.y.sb + (h / p.y.div) * p.y.sh;
@@ -288,6 +294,13 @@ __global__ void __launch_bounds__(kSimtThreads) simt_pass_kernel(const Pass p) {
         }
     }
 }
+// Both directions in one kernel: one register count, but no decision inside the loops (a direction read at run time took 6%).
+template <class T, class OutT, bool kStateOnly, int kCols>
+__global__ void __launch_bounds__(kSimtThreads, 2) simt_pass_kernel(const __grid_constant__ Passes passes) {
+    const Pass& p = passes.p[blockIdx.y];
+    if (p.rev) simt_pass<T, true, OutT, kStateOnly, kCols>(p);
+    else simt_pass<T, false, OutT, kStateOnly, kCols>(p);
+}
 inline size_t simt_pass_smem(int dx, int cols) {
     const int dxp = dx + 4 - (dx & 3) + ((dx & 3) ? 4 : 0);
     return sizeof(float) * (size_t)(2 * kSimtChunk * dxp + 2 * kSimtChunk * cols + dx * cols + kSimtChunk * 33);
@@ -297,7 +310,7 @@ inline size_t simt_pass_smem(int dx, int cols) {
 // seg_state) joined in order.  A thread has one element and loads eight segments' before it stores one: the chain itself is
 // one multiply-add a segment, memory's latency was all of the 16 us that one load at a time took (18 segments of 8 heads).
 template <class P>
-__global__ void __launch_bounds__(256) join_segments_kernel(const P p) {
+__device__ __forceinline__ void join_segments(const P& p) {
     const int plane = p.dx * p.dz, tiles = (plane + 255) / 256;
     const int bh = blockIdx.x / tiles, e = blockIdx.x % tiles * 256 + threadIdx.x;
     if (e >= plane) return;
@@ -321,6 +334,9 @@ __global__ void __launch_bounds__(256) join_segments_kernel(const P p) {
             }
     }
 }
+template <class P>
+__global__ void __launch_bounds__(256) join_segments_kernel(const __grid_constant__ P p) { join_segments(p); }
+__global__ void __launch_bounds__(256) join_passes_kernel(const __grid_constant__ Passes passes) { join_segments(passes.p[blockIdx.y]); }
 
 // dst[b, t, g, :] = the sum over the heads that read head g, rounded once; zero behind a sequence's end.
 template <class T>

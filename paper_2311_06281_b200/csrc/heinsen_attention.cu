@@ -62,17 +62,17 @@ int simt_tiles(int dz) { return (dz + simt_cols(dz) - 1) / simt_cols(dz); }
 // Segments of a sequence on the CUDA cores, as below: up to two CTAs for an SM, where cutting in two steps (states, then the
 // rest) is less than walking all chunks.  Measured, whole and cut: 24 states of 64 x 64, 31 chunks 230 us and 71 us, 4 chunks
 // 37 us and 28 us; 64 of them, 32 chunks 231 us and 152 us; 128 of them 233 us and 257 us (not cut).
-int simt_segments(const heinsen_attention_problem* p) {
-    const long long ctas = p->batch * p->heads * simt_tiles(std::max(p->k_dim, p->v_dim));
+int simt_segments(const heinsen_attention_problem* p, int passes) {
+    const long long ctas = passes * p->batch * p->heads * simt_tiles(std::max(p->k_dim, p->v_dim));
     const long long chunks = (p->tokens + ha::kSimtChunk - 1) / ha::kSimtChunk;
     const long long most = std::max(1ll, std::min(2 * kSms / std::max(1ll, ctas), chunks));
     const long long each = std::max(1ll, (chunks + most - 1) / most);
     return 2 * each + 1 < chunks ? (int)((chunks + each - 1) / each) : 1;
 }
-size_t simt_segment_bytes(const heinsen_attention_problem* p) {
+size_t simt_segment_bytes(const heinsen_attention_problem* p, int passes) {
     const long long pairs = p->batch * p->heads;
-    const int n = simt_segments(p);
-    return n > 1 ? up256((size_t)pairs * n * p->k_dim * p->v_dim * 4) + up256((size_t)pairs * n * 4) : 0;
+    const int n = simt_segments(p, passes);
+    return n > 1 ? passes * (up256((size_t)pairs * n * p->k_dim * p->v_dim * 4) + up256((size_t)pairs * n * 4)) : 0;
 }
 
 // Asks once for each kernel and device: a call costs more host time than a launch.  `done`: bits of the devices, the kernel's own.
@@ -88,35 +88,44 @@ hs_status allow_smem(const void* fn, int smem, std::atomic<unsigned long long>& 
     return HS_OK;
 }
 
-template <class T, bool kRev, class OutT, bool kStateOnly>
-hs_status simt_launch(const Pass& ps, cudaStream_t stream) {
-    const int cols = simt_cols(ps.dz);
-    const size_t smem = ha::simt_pass_smem(ps.dx, cols);
-    const auto fn = cols == 64 ? ha::simt_pass_kernel<T, kRev, OutT, kStateOnly, 64> : ha::simt_pass_kernel<T, kRev, OutT, kStateOnly, 32>;
+template <class T, class OutT, bool kStateOnly>
+hs_status simt_launch(const ha::Passes& ps, int n, cudaStream_t stream) {
+    int dx = 0, dz = 0;
+    for (int i = 0; i < n; ++i) {
+        dx = std::max(dx, ps.p[i].dx);
+        dz = std::max(dz, ps.p[i].dz);
+    }
+    const int cols = simt_cols(dz), segments = ps.p[0].segments;
+    const size_t smem = ha::simt_pass_smem(dx, cols);
+    const auto fn = cols == 64 ? ha::simt_pass_kernel<T, OutT, kStateOnly, 64> : ha::simt_pass_kernel<T, OutT, kStateOnly, 32>;
     const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
-    const long long grid = (long long)ps.batch * ps.heads * simt_tiles(ps.dz) * (kStateOnly ? ps.segments - 1 : ps.segments);
+    const long long grid = (long long)ps.p[0].batch * ps.p[0].heads * simt_tiles(dz) * (kStateOnly ? segments - 1 : segments);
     if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
-    fn<<<(unsigned)grid, ha::kSimtThreads, smem, stream>>>(ps);
+    fn<<<dim3((unsigned)grid, (unsigned)n), ha::kSimtThreads, smem, stream>>>(ps);
     return launched("simt_pass_kernel");
 }
 
-// One pass, with its segments; `space`: simt_segment_bytes() of scratch.
-template <class T, bool kRev, class OutT>
-hs_status simt_pass(Pass ps, int segments, uint8_t* space, cudaStream_t stream) {
-    const long long pairs = (long long)ps.batch * ps.heads;
-    ps.segments = segments;
-    const int chunks = (ps.tokens + ha::kSimtChunk - 1) / ha::kSimtChunk;
-    ps.seg_chunks = (chunks + segments - 1) / segments;
-    if (segments > 1) {
-        ps.seg_state = reinterpret_cast<float*>(space);
-        ps.seg_decay = reinterpret_cast<float*>(space + up256((size_t)pairs * segments * ps.dx * ps.dz * 4));
-        hs_status st = simt_launch<T, kRev, float, true>(ps, stream);
-        if (st != HS_OK) return st;
-        ha::join_segments_kernel<<<(unsigned)(pairs * ((ps.dx * ps.dz + 255) / 256)), 256, 0, stream>>>(ps);
-        if ((st = launched("join_segments_kernel")) != HS_OK) return st;
+// n passes over the same sequences, with their segments; `space`: n times simt_segment_bytes() of scratch.
+template <class T, class OutT>
+hs_status simt_passes(ha::Passes ps, int n, int segments, uint8_t* space, cudaStream_t stream) {
+    const long long pairs = (long long)ps.p[0].batch * ps.p[0].heads, plane = (long long)ps.p[0].dx * ps.p[0].dz;
+    const int chunks = (ps.p[0].tokens + ha::kSimtChunk - 1) / ha::kSimtChunk;
+    const size_t states = up256((size_t)pairs * segments * plane * 4), decays = up256((size_t)pairs * segments * 4);
+    for (int i = 0; i < n; ++i) {
+        Pass& p = ps.p[i];
+        p.segments = segments;
+        p.seg_chunks = (chunks + segments - 1) / segments;
+        p.seg_state = reinterpret_cast<float*>(space + i * (states + decays));
+        p.seg_decay = reinterpret_cast<float*>(space + i * (states + decays) + states);
     }
-    return simt_launch<T, kRev, OutT, false>(ps, stream);
+    if (segments > 1) {
+        hs_status st = simt_launch<T, float, true>(ps, n, stream);
+        if (st != HS_OK) return st;
+        ha::join_passes_kernel<<<dim3((unsigned)(pairs * ((plane + 255) / 256)), (unsigned)n), 256, 0, stream>>>(ps);
+        if ((st = launched("join_passes_kernel")) != HS_OK) return st;
+    }
+    return simt_launch<T, OutT, false>(ps, n, stream);
 }
 
 Pass common(const heinsen_attention_problem* p) {
@@ -299,7 +308,7 @@ BackwardSpace backward_space(const heinsen_attention_problem* p) {
     const size_t rows = (size_t)p->batch * p->tokens * p->heads;
     const size_t chunks = (size_t)p->batch * p->heads * ((p->tokens + ha::kSimtChunk - 1) / ha::kSimtChunk);
     s.segments = kHeaderBytes;
-    s.dq = s.segments + simt_segment_bytes(p);
+    s.dq = s.segments + simt_segment_bytes(p, 3);
     s.dk = s.dq + up256(rows * p->k_dim * 4);
     s.dv = s.dk + up256(rows * p->k_dim * 4);
     s.before = s.dv + up256(rows * p->v_dim * 4);
@@ -322,7 +331,10 @@ hs_status forward_pass(const heinsen_attention_problem* p, const heinsen_attenti
     if (mma_fits(p) && tma_fits(view_of(*o, p->heads, p->heads, p->v_dim), p->batch, p->tokens))
         return mma_pass<false, false, __nv_bfloat16>(ps, {ps.x, p->q_heads, p->k_dim}, {ps.y, p->k_heads, p->k_dim},
                                                  {ps.z, p->v_heads, p->v_dim}, ws, ws + kHeaderBytes, hs_internal::call_id(), stream);
-    return simt_pass<T, false, T>(ps, simt_segments(p), ws + kHeaderBytes, stream);
+    ha::Passes list;
+    std::memset(&list, 0, sizeof list);
+    list.p[0] = ps;
+    return simt_passes<T, T>(list, 1, simt_segments(p, 1), ws + kHeaderBytes, stream);
 }
 
 template <class T>
@@ -345,7 +357,7 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
     float *before = dlog_a ? reinterpret_cast<float*>(ws + sp.before) : nullptr,
           *behind = dlog_a ? reinterpret_cast<float*>(ws + sp.behind) : nullptr;
     double* part = reinterpret_cast<double*>(ws + sp.part);
-    const int segments = simt_segments(p);
+    ha::Passes list;  // dq, dk, dv
     uint8_t* space = ws + sp.segments;
     const Rows q = rows_of(p->q, p->heads, p->q_heads), k = rows_of(p->k, p->heads, p->k_heads),
                v = rows_of(p->v, p->heads, p->v_heads), g = rows_of(*d_o, p->heads, p->heads);
@@ -359,7 +371,7 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
         ps.s_in = p->state0; ps.s_in_t = 1;
         to(ps, wq, p->k_dim);
         ps.dump = before;
-        if ((st = simt_pass<T, false, float>(ps, segments, space, stream)) != HS_OK) return st;
+        list.p[0] = ps;
     }
     {
         Pass ps = common(p);
@@ -367,7 +379,8 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
         ps.s_in = d_state; ps.s_in_t = 1; ps.s_in_mul = 1.0f / p->scale;  // the scale comes back with the output
         to(ps, wk, p->k_dim);
         ps.dump = behind;
-        if ((st = simt_pass<T, true, float>(ps, segments, space, stream)) != HS_OK) return st;
+        ps.rev = 1;
+        list.p[1] = ps;
     }
     {
         Pass ps = common(p);
@@ -375,8 +388,10 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
         ps.s_in = d_state; ps.s_in_mul = 1.0f / p->scale;
         ps.s_out = dstate0; ps.s_out_mul = p->scale;
         to(ps, wv, p->v_dim);
-        if ((st = simt_pass<T, true, float>(ps, segments, space, stream)) != HS_OK) return st;
+        ps.rev = 1;
+        list.p[2] = ps;
     }
+    if ((st = simt_passes<T, float>(list, 3, simt_segments(p, 3), space, stream)) != HS_OK) return st;
     if ((st = sum_heads<T>(wq, dq, p, p->q_heads, p->k_dim, stream)) != HS_OK) return st;
     if ((st = sum_heads<T>(wk, dk, p, p->k_heads, p->k_dim, stream)) != HS_OK) return st;
     if ((st = sum_heads<T>(wv, dv, p, p->v_heads, p->v_dim, stream)) != HS_OK) return st;
@@ -511,7 +526,7 @@ size_t heinsen_attention_workspace_bytes(const heinsen_attention_problem* p, int
     if (validate(p) != HS_OK) return 0;
     if (nothing(p)) return kHeaderBytes;
     if (!backward)  // which of the two passes runs depends on the output's layout too
-        return kHeaderBytes + std::max(simt_segment_bytes(p), p->dtype == HS_BF16 ? segment_bytes(p) : 0);
+        return kHeaderBytes + std::max(simt_segment_bytes(p, 1), p->dtype == HS_BF16 ? segment_bytes(p) : 0);
     return mma_fits(p) ? mma_space(p).total : backward_space(p).total;
 }
 
