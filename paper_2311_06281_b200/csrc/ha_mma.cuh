@@ -15,7 +15,7 @@
 // rounding is as large).
 //
 // Measured, [8 x 2048 tokens, 16 heads of 128] (128 CTAs): forward and dv 75 us each, 268 MB at 3.6 TB/s; with kDots 150 us (dk)
-// and 169 us (dq).  Neither memory (36% of a copy's rate) nor the tensor core (31% of its cycles) bounds it: a chunk's steps wait
+// and 169 us (dq).  Neither memory (55% of a copy's rate) nor the tensor core (31% of its cycles) bounds it: a chunk's steps wait
 // for each other, 7000 to 8000 clocks of them, and shared memory holds one CTA.  Of those the output's chain has: scores 520, P
 // 2000, X S 1100, scaling its rows 600, P Z 900, the output 760; the state's: Z^T 500, its terms 2400, the update 2000, reading
 // it 500, publishing it 500.  What did not help: the output from registers straight to memory (2200 clocks for 760), one warp that
