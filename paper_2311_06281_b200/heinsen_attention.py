@@ -144,6 +144,14 @@ def _space(nbytes: int, device) -> torch.Tensor:
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+def _space_ok(workspace: torch.Tensor, device):
+    """A caller's own scratch: the kernels are given its address."""
+    if workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor")
+    if workspace.device != device:
+        raise ValueError(f"workspace is on {workspace.device}, not on {device}")
+
+
 def _tensor(t: torch.Tensor, name: str) -> _Tensor:
     """[batch, tokens, heads, dim] of any strides, the last dimension contiguous."""
     return _Tensor(*_rows(t, name))
@@ -213,6 +221,8 @@ def _attention_forward(p: _Sizes, q: torch.Tensor, workspace: torch.Tensor | Non
     call = _call()
     if workspace is None:
         workspace = _space(call.space(p.packed, 0), dev)
+    else:
+        _space_ok(workspace, dev)
     _launch(dev, call.forward, p.packed, _ROWS.pack(*_rows(o, "o")), state.data_ptr(), workspace.data_ptr(), workspace.numel())
     return o, state
 
