@@ -107,6 +107,7 @@ hs_status heinsen_block_norms_forward(const heinsen_norms_problem* p, void* r, v
 hs_status heinsen_block_norms_backward(const heinsen_norms_problem* p, const void* d_r, const void* d_y, void* dx,
                                        void* dbranch, void* dgate, void* dpre, void* dpost, void* workspace,
                                        size_t workspace_bytes, void* stream);
+/* 0 for sizes the library does not accept; of the pointers only whether there is a gate matters. */
 size_t heinsen_block_norms_workspace_bytes(const heinsen_norms_problem* p);
 
 /*

@@ -96,14 +96,19 @@ hs_status launch(const Kernel& k, const Norms& n, long long grid, int threads, s
     return HS_OK;
 }
 
-hs_status validate(const heinsen_norms_problem* p, bool block) {
+// What does not depend on the pointers, but for whether there is a gate.
+hs_status validate_sizes(const heinsen_norms_problem* p, bool block) {
     if (!p || p->rows < 0 || p->rows > kMaxRows || p->dim < 1 || p->dim > kMaxDim) return HS_ERR_INVALID_ARG;
     if ((p->dtype != HS_F32 && p->dtype != HS_BF16) || (p->weight_dtype != HS_F32 && p->weight_dtype != p->dtype))
         return HS_ERR_INVALID_ARG;
     if (!std::isfinite(p->eps) || p->eps < 0.0f || (block && !std::isfinite(p->scale))) return HS_ERR_INVALID_ARG;
     if (p->rows > (1ll << 46) / p->dim) return HS_ERR_INVALID_ARG;
     if (block && p->gate && (p->gate_rows < 1 || p->rows % p->gate_rows)) return HS_ERR_INVALID_ARG;
-    if (p->rows == 0) return HS_OK;
+    return HS_OK;
+}
+hs_status validate(const heinsen_norms_problem* p, bool block) {
+    const hs_status st = validate_sizes(p, block);
+    if (st != HS_OK || p->rows == 0) return st;
     if (!p->x || !p->pre_weight || (block && !p->branch)) return HS_ERR_INVALID_ARG;
     return HS_OK;
 }
@@ -200,8 +205,8 @@ hs_status heinsen_gated_norm_forward(const heinsen_norms_problem* p, void* y, vo
 }
 
 size_t heinsen_block_norms_workspace_bytes(const heinsen_norms_problem* p) {
-    if (validate(p, true) != HS_OK && !(p && p->rows > 0 && p->dim > 0 && p->dim <= kMaxDim)) return 0;
-    if (p->rows <= 0) return 256;
+    if (validate_sizes(p, true) != HS_OK) return 0;
+    if (p->rows == 0) return 256;
     // the larger of the two layouts the pointers may lead to
     size_t at;
     const bool f32 = p->dtype == HS_F32;
@@ -251,7 +256,7 @@ hs_status heinsen_block_norms_backward(const heinsen_norms_problem* p, const voi
 }
 
 size_t heinsen_gated_norm_workspace_bytes(const heinsen_norms_problem* p) {
-    if (!p || p->rows < 0 || p->dim < 1 || p->dim > kMaxDim) return 0;
+    if (validate_sizes(p, false) != HS_OK) return 0;
     const bool f32 = p->dtype == HS_F32;
     const long long grid = std::max(stay(p->rows, choose(p->dim, f32, false), false),
                                     p->dim * (f32 ? 4 : 2) % 16 ? 1 : stay(p->rows, choose(p->dim, f32, true), false));

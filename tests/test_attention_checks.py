@@ -22,3 +22,21 @@ def test_a_kept_workspace_is_contiguous_bytes_of_the_calls_device(ha):
     for bad in (ws.view(torch.float32), ws[::2], torch.empty(512, dtype=torch.int8)):
         with pytest.raises(ValueError, match="contiguous uint8"):
             ha._space_ok(bad, host)
+
+
+def norms(ha, **other):
+    d = dict(rows=6, gate_rows=3, dim=16, dtype=0, weight_dtype=0, scale=1.0, eps=1e-6, x=None, branch=None, gate=256, pre_weight=None,
+             post_weight=None)
+    d.update(other)
+    return ha._Norms(*[d[n] for n, _ in ha._Norms._fields_])
+
+
+def test_the_norms_scratch_is_zero_for_sizes_that_are_not_accepted(ha):
+    """A gate of more rows than there are ended the process with a division by zero."""
+    L = ha.lib()
+    for space, own in ((L.heinsen_block_norms_workspace_bytes, [dict(gate_rows=12), dict(gate_rows=4), dict(gate_rows=0), dict(gate_rows=-3)]),
+                       (L.heinsen_gated_norm_workspace_bytes, [])):
+        assert space(norms(ha)) > 0 and space(norms(ha, rows=0)) > 0 and space(norms(ha, gate=None, gate_rows=12)) > 0
+        for bad in (dict(rows=-1), dict(rows=1 << 62), dict(dim=0), dict(dim=16385), dict(dtype=7), dict(weight_dtype=1), dict(eps=-1.0), *own):
+            assert space(norms(ha, **bad)) == 0, bad
+        assert space(None) == 0
