@@ -497,6 +497,21 @@ hs_status mma_backward(const heinsen_attention_problem* p, const heinsen_attenti
     return launched("decay_grad_sum_kernel");
 }
 
+// The gradients of a call without sequences or without heads: zeros, wherever they have elements all the same.
+hs_status zero_gradients(const heinsen_attention_problem* p, void* dq, void* dk, void* dv, float* dlog_a, cudaStream_t stream) {
+    const size_t size = p->dtype == HS_F32 ? 4 : 2, rows = (size_t)p->batch * p->tokens;
+    const bool fixed = p->log_a.batch_stride == 0 && p->log_a.token_stride == 0;
+    const struct { void* to; size_t bytes; } all[] = {{dq, rows * p->q_heads * p->k_dim * size}, {dk, rows * p->k_heads * p->k_dim * size},
+                                                      {dv, rows * p->v_heads * p->v_dim * size},
+                                                      {dlog_a, fixed ? (size_t)p->heads * 4 : 0}};
+    for (const auto& z : all) {
+        if (!z.to || !z.bytes) continue;
+        const cudaError_t e = cudaMemsetAsync(z.to, 0, z.bytes, stream);
+        if (e != cudaSuccess) return hs_internal::cuda_fail("cudaMemsetAsync", e);
+    }
+    return HS_OK;
+}
+
 hs_status check_space(const heinsen_attention_problem* p, int backward, void* workspace, size_t bytes) {
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return HS_ERR_INVALID_ARG;
     return bytes < heinsen_attention_workspace_bytes(p, backward) ? HS_ERR_WORKSPACE_TOO_SMALL : HS_OK;
@@ -550,7 +565,8 @@ hs_status heinsen_attention_backward(const heinsen_attention_problem* p, const h
                                      float* dlog_a, float* dstate0, void* workspace, size_t workspace_bytes,
                                      void* stream) {
     hs_status st = validate(p);
-    if (st != HS_OK || nothing(p)) return st;
+    if (st != HS_OK) return st;
+    if (nothing(p)) return zero_gradients(p, dq, dk, dv, dlog_a, static_cast<cudaStream_t>(stream));
     if ((st = validate_inputs(p)) != HS_OK) return st;
     if (!d_o || (p->tokens && (!d_o->ptr || !dq || !dk || !dv))) return HS_ERR_INVALID_ARG;
     if ((st = check_space(p, 1, workspace, workspace_bytes)) != HS_OK) return st;

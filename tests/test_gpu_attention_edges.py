@@ -16,3 +16,32 @@ def test_a_workspace_of_the_host_is_refused(ha):  # noqa: F811
         for grad in (False, True):
             with pytest.raises(ValueError, match="workspace"):
                 ha.decay_attention(q.detach().requires_grad_(grad), k, v, log_a, s0, workspace=bad)
+
+
+def leave_nan_behind(*shapes):
+    """Fills what the allocator will hand out next: a result that nobody writes is NaN then, not a zero by chance."""
+    kept = [torch.full(s, float("nan"), device=DEV) for s in shapes for _ in range(16)]
+    torch.cuda.synchronize()
+    del kept
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gradients_of_an_empty_batch_are_zero(ha, dtype):  # noqa: F811
+    q = torch.empty(0, 5, 2, 64, device=DEV, dtype=dtype, requires_grad=True)
+    log_a = (-torch.rand(2, device=DEV)).requires_grad_()
+    o, s = ha.decay_attention(q, q, q, log_a)
+    leave_nan_behind((2,), (64,))
+    dq, da = torch.autograd.grad(o.sum() + s.sum(), (q, log_a))
+    assert dq.shape == q.shape and torch.equal(da, torch.zeros_like(log_a))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("fixed", [False, True])
+def test_gradients_without_heads_are_zero(ha, fixed, dtype):  # noqa: F811
+    q, k, v = (torch.randn(2, 3, 1, 16, device=DEV).to(dtype).requires_grad_() for _ in range(3))
+    log_a = torch.empty((0,) if fixed else (2, 3, 0), device=DEV, requires_grad=True)
+    o, s = ha.decay_attention(q, k, v, log_a)
+    assert o.shape == (2, 3, 0, 16) and s.shape == (2, 0, 16, 16)
+    leave_nan_behind(q.shape, (q.numel() // 2,))
+    for g, x in zip(torch.autograd.grad(o.sum() + s.sum(), (q, k, v, log_a)), (q, k, v, log_a)):
+        assert torch.equal(g, torch.zeros_like(x))
