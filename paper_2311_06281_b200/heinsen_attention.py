@@ -393,6 +393,8 @@ class _BlockNorms(torch.autograd.Function):
         d_r = None if d_r is None else d_r.contiguous()
         new = lambda t: None if t is None else torch.empty_like(t)  # noqa: E731
         dx, dh, dpre, dpost, dgate = new(x), new(branch), new(pre), new(post), new(gate)
+        if dgate is not None and x.numel() == 0:
+            dgate.zero_()  # gates of sequences without tokens: the library sees no rows, and so no gates
         call = _call()
         ws = _space(call.block_space(p), x.device)
         _launch(x.device, call.block_backward, p, _addr(d_r), d_y.data_ptr(), dx.data_ptr(), dh.data_ptr(), _addr(dgate),

@@ -45,3 +45,15 @@ def test_gradients_without_heads_are_zero(ha, fixed, dtype):  # noqa: F811
     leave_nan_behind(q.shape, (q.numel() // 2,))
     for g, x in zip(torch.autograd.grad(o.sum() + s.sum(), (q, k, v, log_a)), (q, k, v, log_a)):
         assert torch.equal(g, torch.zeros_like(x))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gates_of_sequences_without_tokens_have_zero_gradients(ha, dtype):  # noqa: F811
+    x, branch = (torch.empty(3, 0, 64, device=DEV, dtype=dtype, requires_grad=True) for _ in range(2))
+    gate = torch.randn(3, 1, 64, device=DEV).to(dtype).requires_grad_()
+    pre, post = (torch.ones(64, device=DEV, dtype=dtype, requires_grad=True) for _ in range(2))
+    r, y = ha.block_norms(x, branch, pre, post_weight=post, gate=gate)
+    leave_nan_behind((64,), (32,), (192,), (96,))
+    ins = (x, branch, gate, pre, post)
+    for g, t in zip(torch.autograd.grad(r.sum() + y.sum(), ins), ins):
+        assert torch.equal(g, torch.zeros_like(t))
