@@ -159,7 +159,7 @@ def _tensor(t: torch.Tensor, name: str) -> _Tensor:
 
 def _rows(t: torch.Tensor, name: str):
     s = t.stride()
-    if s[3] != 1 and t.shape[3] > 1:
+    if s[3] != 1 and t.shape[3] > 1 and t.numel():  # an empty tensor counts as contiguous whatever its strides
         raise ValueError(f"{name}: the last dimension must be contiguous")
     return t.data_ptr(), s[0], s[1], s[2]
 
@@ -315,7 +315,7 @@ def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
     n = state.shape[0]
     _state_ok(state, (n, h, kd, vd), "state")
     (qb, qh, q1), (kb, kh, k1), (vb, vh, v1) = q.stride(), k.stride(), v.stride()
-    if (q1 != 1 or k1 != 1) and kd > 1 or v1 != 1 and vd > 1:
+    if b and ((q1 != 1 or k1 != 1) and kd > 1 or v1 != 1 and vd > 1):
         raise ValueError("q, k, v: the last dimension must be contiguous")
     if slots is None:
         if n < b:
@@ -326,7 +326,7 @@ def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
     _on_gpu(q, "q")
     if out is None:
         out = torch.empty((b, h, vd), dtype=q.dtype, device=dev)
-    elif tuple(out.shape) != (b, h, vd) or out.dtype is not q.dtype or out.stride(2) != 1 and vd > 1:
+    elif tuple(out.shape) != (b, h, vd) or out.dtype is not q.dtype or b and out.stride(2) != 1 and vd > 1:
         raise ValueError("out must be [batch, heads, v_dim] of q's dtype, the last dimension contiguous")
     _cuda("decay_attention_step", dev, k=k, v=v, log_a=log_a, state=state, slots=slots, out=out)
     ob, oh, _ = out.stride()

@@ -40,3 +40,12 @@ def test_the_norms_scratch_is_zero_for_sizes_that_are_not_accepted(ha):
         for bad in (dict(rows=-1), dict(rows=1 << 62), dict(dim=0), dict(dim=16385), dict(dtype=7), dict(weight_dtype=1), dict(eps=-1.0), *own):
             assert space(norms(ha, **bad)) == 0, bad
         assert space(None) == 0
+
+
+def test_strides_of_empty_tensors_are_not_looked_at(ha):
+    """An expanded gradient without elements: PyTorch counts it as contiguous, so that no copy gives it other strides."""
+    one = torch.zeros(())
+    ha._rows(one.expand(0, 5, 2, 64).contiguous(), "d_o")
+    ha._rows(one.expand(2, 3, 0, 16).contiguous(), "d_o")
+    with pytest.raises(ValueError, match="contiguous"):
+        ha._rows(one.expand(2, 3, 4, 16), "d_o")
