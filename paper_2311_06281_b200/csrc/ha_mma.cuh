@@ -556,7 +556,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 const int batches = min(4, (live - t0 + 31) / 32);
                 ok = ok && wait(kDecays, it);
                 const float own_hi = read1(c_hi + row), own_lo = read1(c_lo + row);
-                const float far = p.scale * ex2(kRev ? (read1(s_whole + 1) - own_hi) + (read1(s_whole + 2) - own_lo) : own_hi + own_lo);
+                const float far1 = ex2(kRev ? (read1(s_whole + 1) - own_hi) + (read1(s_whole + 2) - own_lo) : own_hi + own_lo);
+                const float far = p.scale * far1;
+                const bool forgotten = far1 == 0.0f;  // a decay of zero forgets the state whatever it holds: no 0 * inf
                 ok = ok && wait(kScores, it);
                 tmem_after_sync();
                 double sum = 0.0;  // of W's row; joined in 64 bits, since two such sums will be subtracted
@@ -646,6 +648,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     tmem_ld16(v, at + L::to + col);
 #pragma unroll
                     for (int u = 0; u < 16; u += 2) parts(mul2(far2, make_pair2(v[u], v[u + 1])), v[u], v[u + 1]);
+                    if (forgotten)
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) v[u] = 0u;
                     tmem_st16(at + L::to + col, v);
                     if constexpr (kDots) {
                         const uint4 lo = read4(own_w + (((2 * c) ^ (row & 7)) << 4)), hi = read4(own_w + (((2 * c + 1) ^ (row & 7)) << 4));
@@ -829,6 +834,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(~0u, a, o);
                 if (lane == 0) p.cross[((long long)bh * p.chunks + t0 / kChunk) * 8 + warp - 8] = a;
             }
+            if (whole == 0.0f)  // likewise
+#pragma unroll
+                for (int j = 0; j < 32; ++j) s[j] = 0;
             ok = ok && wait(kUpdate, it);
             tmem_after_sync();
 #pragma unroll

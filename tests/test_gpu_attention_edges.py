@@ -57,3 +57,39 @@ def test_gates_of_sequences_without_tokens_have_zero_gradients(ha, dtype):  # no
     ins = (x, branch, gate, pre, post)
     for g, t in zip(torch.autograd.grad(r.sum() + y.sum(), ins), ins):
         assert torch.equal(g, torch.zeros_like(t))
+
+
+# (b, t, h, kd, vd): whole, and cut into segments (bf16 at multiples of 128 tokens, float32 of 32)
+FORGET = [(2, 300, 60, 64, 64), (2, 300, 2, 128, 72), (1, 1500, 2, 64, 128)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("at", [0, 50, 127, 128, 200])
+@pytest.mark.parametrize("b,t,h,kd,vd", FORGET)
+def test_a_decay_of_zero_forgets_whatever_the_state_holds(ha, b, t, h, kd, vd, at, dtype):  # noqa: F811
+    q, k, v, log_a, s0 = make(b, t, h, h, h, h, kd, vd, dtype, state=True, seed=at)
+    log_a[:, at] = -float("inf")
+    s0[:, :, 0] = float("nan")
+    s0[:, :, 1, 1:] = float("inf")
+    s0[:, :, 2, ::2] = -float("inf")
+    o, s = ha.decay_attention(q, k, v, log_a, s0)
+    want_o, want_s = attention64(*(x[:, at:] for x in (q, k, v, log_a)), None, kd ** -0.5)
+    close(o[:, at:], want_o, "o")
+    close(s, want_s, "state")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("b,t,h,kd,vd", FORGET[1:])
+def test_gradients_past_a_forgotten_state(ha, b, t, h, kd, vd, dtype):  # noqa: F811
+    q, k, v, log_a, s0 = make(b, t, h, h, h, h, kd, vd, dtype, state=True, seed=1)
+    log_a[:, 0] = -float("inf")
+    g = torch.Generator(device=DEV).manual_seed(3)
+    d_o, d_s = torch.randn(b, t, h, vd, device=DEV, generator=g).to(dtype), torch.randn(b, h, kd, vd, device=DEV, generator=g)
+    wide = [leaf64(x) for x in (q, k, v, log_a, s0)]
+    want = torch.autograd.grad(attention64(*wide, scale=0.25), wide, [d_o.double(), d_s.double()])
+    s0[:, :, 0], s0[:, :, 1, 1:] = float("nan"), float("inf")
+    ins = [x.requires_grad_() for x in (q, k, v, log_a, s0)]
+    got = torch.autograd.grad(ha.decay_attention(*ins, scale=0.25), ins, [d_o, d_s])
+    for name, x, y in zip(("dq", "dk", "dv", "dlog_a", "dstate0"), got, want):
+        close(x, y, name)
+    assert (got[4] == 0).all()
