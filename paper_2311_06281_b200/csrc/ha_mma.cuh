@@ -23,9 +23,11 @@
 // the state (spills).
 //
 // kDots: the pass also forms what the decay gradients need of it, in float32: the row sums of W = P o (w Z^T), w the fourth
-// tensor, from the unrounded P, and the dots w_i . (X S)_i, for which X S has the state in three terms.  W comes out of the two
-// passes that form it in the same bits (each exponential is taken of the same difference there), so that what cancels between
-// their sums cancels exactly.  Row sums from the outputs instead, w_i . out_i, were 1e-6 off in a common direction (the tensor
+// tensor, from the unrounded P, and the dots w_i . (X S)_i, for which X S has the state in three terms.  Each W_ij comes out of
+// the two passes that form it in the same bits (each exponential is taken of the same difference there, each product is rounded
+// once before it is added to anything) and is summed in 64 bits: what cancels between their sums leaves at most 2^-44 of the sum
+// of |W|, at tokens that forget everything too.  (Four products added in float32 first left 2^-28 there, 1e-5 to 1e-4 where
+// nothing belonged; 64 bits from the start cost 3% of a training step.)  Row sums from the outputs instead, w_i . out_i, were 1e-6 off in a common direction (the tensor
 // core's additions cut off), which sums over many tokens turn into 5e-5.
 #pragma once
 #include <cuda.h>
@@ -561,7 +563,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 const bool forgotten = far1 == 0.0f;  // a decay of zero forgets the state whatever it holds: no 0 * inf
                 ok = ok && wait(kScores, it);
                 tmem_after_sync();
-                double sum = 0.0;  // of W's row; joined in 64 bits, since two such sums will be subtracted
+                double sum = 0.0, sum_odd = 0.0;  // of W's row, in 64 bits, since two such sums will be subtracted
                 pair sum_far = 0;
                 const pair minus = make_pair2(-1.0f, -1.0f), scale2 = make_pair2(p.scale, p.scale);
                 const float to_late = kRev ? 1.0f : -1.0f;
@@ -622,11 +624,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                         for (int j = 0; j < 16; ++j)
                             if (j == own) t16[j] = 0u;
 #pragma unroll
-                        for (int j = 0; j < 16; j += 4) {
+                        for (int j = 0; j < 16; j += 2) {  // each W_ij rounded once, the same way in both passes, before any addition
                             float a, c;
-                            parts(fma2(make_pair2(v[j], v[j + 1]), make_pair2(t16[j], t16[j + 1]),
-                                       mul2(make_pair2(v[j + 2], v[j + 3]), make_pair2(t16[j + 2], t16[j + 3]))), a, c);
-                            sum += (double)(a + c);
+                            parts(mul2(make_pair2(v[j], v[j + 1]), make_pair2(t16[j], t16[j + 1])), a, c);
+                            sum += (double)a;
+                            sum_odd += (double)c;
                         }
                     }
                 }
@@ -694,7 +696,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     float a, c;
                     parts(sum_far, a, c);
                     if (t < live) {
-                        p.dots[to] = sum;
+                        p.dots[to] = sum + sum_odd;
                         p.dots_far[to] = columns ? a + c : 0.0f;
                     }
                 }

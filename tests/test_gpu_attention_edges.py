@@ -93,3 +93,40 @@ def test_gradients_past_a_forgotten_state(ha, b, t, h, kd, vd, dtype):  # noqa: 
     for name, x, y in zip(("dq", "dk", "dv", "dlog_a", "dstate0"), got, want):
         close(x, y, name)
     assert (got[4] == 0).all()
+
+
+def pairs_weight(q, k, v, log_a, d_o, scale, chunk):
+    """The sum of |W_ij| over the pairs i >= j of every chunk, for every token of it: what a sum over them can be off by."""
+    q, k, v, a, g = (x.double().transpose(1, 2) for x in (q, k, v, log_a.unsqueeze(-1), d_o))
+    out = torch.zeros(*log_a.shape, dtype=torch.float64, device=log_a.device)
+    for t0 in range(0, q.shape[2], chunk):
+        at = slice(t0, t0 + chunk)
+        c = a[:, :, at, 0].clamp(min=-1e4).cumsum(-1)
+        w = torch.exp((c[..., :, None] - c[..., None, :]).tril()).tril() * scale
+        w = (w * (q[:, :, at] @ k[:, :, at].mT) * (g[:, :, at] @ v[:, :, at].mT)).abs().sum((-1, -2))
+        out[:, at] = w[:, None]
+    return out
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("b,t,h,kd,vd", [(1, 128, 2, 64, 64), (2, 300, 60, 128, 128), (2, 300, 2, 128, 72), (1, 1500, 2, 64, 128)])
+def test_decay_gradients_where_decays_are_strong(ha, b, t, h, kd, vd, dtype):  # noqa: F811
+    """A few tokens forget all or nearly all (-inf, -20): their own gradients, not only those beside them.  Nothing crosses a
+    reset, so its gradient is zero but for the sums of what lies on both sides of it: with sums over up to 2 * 128 products
+    on each of two sides in 64 bits that is 512 * 2^-53 of the products' absolute sum.  The others are held to float32's
+    tolerance by themselves."""
+    q, k, v, log_a, s0 = make(b, t, h, h, h, h, kd, vd, dtype, state=True, seed=2)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    which = torch.rand(b, t, h, device=DEV, generator=g)
+    reset, strong = which < 0.02, (which >= 0.02) & (which < 0.04)
+    log_a = log_a.masked_fill(reset, -float("inf")).masked_fill(strong, -20.0)
+    d_o, d_s = torch.randn(b, t, h, vd, device=DEV, generator=g).to(dtype), torch.randn(b, h, kd, vd, device=DEV, generator=g)
+    ins, wide = [x.requires_grad_() for x in (q, k, v, log_a, s0)], [leaf64(x) for x in (q, k, v, log_a, s0)]
+    got, = torch.autograd.grad(ha.decay_attention(*ins, scale=0.25), log_a, [d_o, d_s])
+    want, = torch.autograd.grad(attention64(*wide, scale=0.25), wide[3], [d_o.double(), d_s.double()])
+    close(got, want, "dlog_a")
+    bound = pairs_weight(q.detach(), k.detach(), v.detach(), log_a.detach(), d_o, 0.25, 128) * 2.0 ** -44
+    assert reset.any() and strong.any() and (want[reset] == 0).all()
+    worst = float((got[reset].double().abs() / bound[reset]).max())
+    assert worst <= 1, f"at a reset: {float(got[reset].abs().max()):.3g}, {worst:.3g} times what sums in 64 bits may leave"
+    close(got[strong], want[strong], "dlog_a at strong decays")
