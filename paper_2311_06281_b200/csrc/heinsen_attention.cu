@@ -76,6 +76,8 @@ size_t simt_segment_bytes(const heinsen_attention_problem* p, int passes) {
 }
 
 // Asks once for each kernel and device: a call costs more host time than a launch.  `done`: bits of the devices, the kernel's own.
+// `smem` is the most that any launch of the kernel takes: the limit is the kernel's, and a smaller one set for this call would
+// refuse the launch of another thread's.
 hs_status allow_smem(const void* fn, int smem, std::atomic<unsigned long long>& done) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -98,8 +100,9 @@ hs_status simt_launch(const ha::Passes& ps, int n, cudaStream_t stream) {
     const int cols = simt_cols(dz), segments = ps.p[0].segments;
     const size_t smem = ha::simt_pass_smem(dx, cols);
     const auto fn = cols == 64 ? ha::simt_pass_kernel<T, OutT, kStateOnly, 64> : ha::simt_pass_kernel<T, OutT, kStateOnly, 32>;
-    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
+    static std::atomic<unsigned long long> done[2] = {};
+    const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)ha::simt_pass_smem(kMaxHeadDim, cols), done[cols == 64]);
+    if (st != HS_OK) return st;
     const long long grid = (long long)ps.p[0].batch * ps.p[0].heads * simt_tiles(dz) * (kStateOnly ? segments - 1 : segments);
     if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
     fn<<<dim3((unsigned)grid, (unsigned)n), ha::kSimtThreads, smem, stream>>>(ps);
@@ -410,8 +413,9 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
         if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
         if (grid) {
             const size_t smem = ha::decay_grad_smem(p->k_dim, p->v_dim);
-            const cudaError_t e = cudaFuncSetAttribute(ha::decay_grad_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-            if (e != cudaSuccess) return hs_internal::cuda_fail("cudaFuncSetAttribute", e);
+            static std::atomic<unsigned long long> done{0};
+            st = allow_smem(reinterpret_cast<const void*>(ha::decay_grad_kernel<T>), (int)ha::decay_grad_smem(kMaxHeadDim, kMaxHeadDim), done);
+            if (st != HS_OK) return st;
             ha::decay_grad_kernel<T><<<(unsigned)grid, ha::kDecayThreads, smem, stream>>>(d);
             if ((st = launched("decay_grad_kernel")) != HS_OK) return st;
         }
