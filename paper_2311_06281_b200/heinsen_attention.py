@@ -333,6 +333,8 @@ def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
     packed = _PROBLEM.pack(b, 1, h, hq, hk, hv, kd, vd, _dtype(q), float(kd ** -0.5 if scale is None else scale),
                            q.data_ptr(), qb, 0, qh, k.data_ptr(), kb, 0, kh, v.data_ptr(), vb, 0, vh, log_a.data_ptr(), ab, 0, ah, 0, 0)
     _launch(dev, _call().step, packed, _ROWS.pack(out.data_ptr(), ob, 0, oh), state.data_ptr(), n, _addr(slots))
+    # autograd sees no address being written to: a graph that kept either of them has to notice
+    torch.autograd.graph.increment_version((state, out))
     return out
 
 

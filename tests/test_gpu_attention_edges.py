@@ -130,3 +130,22 @@ def test_decay_gradients_where_decays_are_strong(ha, b, t, h, kd, vd, dtype):  #
     worst = float((got[reset].double().abs() / bound[reset]).max())
     assert worst <= 1, f"at a reset: {float(got[reset].abs().max()):.3g}, {worst:.3g} times what sums in 64 bits may leave"
     close(got[strong], want[strong], "dlog_a at strong decays")
+
+
+def test_a_step_on_a_state_that_a_graph_has_kept_is_noticed(ha):  # noqa: F811
+    q, k, v, log_a, s0 = make(2, 9, 2, 2, 2, 2, 64, 64, F32, state=True)
+    q.requires_grad_()
+    one = [x[:, 0].detach() for x in (q, k, v, log_a)]
+    o, _ = ha.decay_attention(q, k, v, log_a, s0)
+    before, out = s0._version, torch.empty(2, 2, 64, device=DEV)
+    ha.decay_attention_step(*one, s0, out=out)
+    assert s0._version > before and out._version > 0
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        torch.autograd.grad(o.sum(), q)
+    kept = (out.clone().requires_grad_() * out).sum()  # its backward needs `out`
+    ha.decay_attention_step(*one, s0, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        kept.backward()
+    with torch.inference_mode():  # tensors without a version
+        state = s0.clone()
+        ha.decay_attention_step(*one, state)
