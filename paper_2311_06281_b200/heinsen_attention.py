@@ -5,7 +5,8 @@ head), its one-token step, and the norms around a block built on it.
 
 As in ``heinsen_scan`` every step of the computation runs in the library's CUDA kernels; PyTorch provides device memory,
 streams and the autograd graph.  There is no CPU fallback.  ``decay_attention``, ``block_norms`` and ``gated_norm`` are
-differentiable in every tensor argument (once: their gradients are not differentiable again).
+differentiable in every tensor argument (once: their gradients are not differentiable again; backwards only: tangents of
+``torch.autograd.forward_ad`` are refused).
 """
 from __future__ import annotations
 
@@ -13,6 +14,7 @@ import ctypes
 import struct
 
 import torch
+from torch.autograd import forward_ad
 
 from .heinsen_scan import HeinsenScanError, _check, _dtype_code, _on_device, lib as _scan_lib  # noqa: F401
 
@@ -136,6 +138,21 @@ def _launch(device, fn, *args):
             status = fn(*args, torch.cuda.current_stream(device).cuda_stream)
     if status:
         _check(status)
+
+
+def _seen_by_autograd(*tensors) -> bool:
+    """Does a call have to go through its autograd function?  Where an input wants a gradient, and wherever tangents may be
+    about (a dual tensor wants no gradient): the function refuses those."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return getattr(forward_ad, "_current_level", 0) >= 0
+
+
+def _no_tangents(name, *tensors):
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError(f"{name} has no forward-mode derivative")
 
 
 def _space(nbytes: int, device) -> torch.Tensor:
@@ -280,8 +297,7 @@ def decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: to
     device recorded (a bounded wait that ran out).  Without it each call takes its own.
     """
     scale = float(q.shape[-1] ** -0.5 if scale is None else scale)
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or log_a.requires_grad or
-                                    (state0 is not None and state0.requires_grad)):
+    if _seen_by_autograd(q, k, v, log_a, state0):
         return _DecayAttention.apply(q, k, v, log_a, state0, scale, lengths, workspace)
     return _attention_forward(_problem(q, k, v, log_a, state0, scale, lengths), q, workspace)
 
@@ -329,6 +345,7 @@ def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
     elif tuple(out.shape) != (b, h, vd) or out.dtype is not q.dtype or b and out.stride(2) != 1 and vd > 1:
         raise ValueError("out must be [batch, heads, v_dim] of q's dtype, the last dimension contiguous")
     _cuda("decay_attention_step", dev, k=k, v=v, log_a=log_a, state=state, slots=slots, out=out)
+    _no_tangents("decay_attention_step", q, k, v, log_a, state, out)
     ob, oh, _ = out.stride()
     packed = _PROBLEM.pack(b, 1, h, hq, hk, hv, kd, vd, _dtype(q), float(kd ** -0.5 if scale is None else scale),
                            q.data_ptr(), qb, 0, qh, k.data_ptr(), kb, 0, kh, v.data_ptr(), vb, 0, vh, log_a.data_ptr(), ab, 0, ah, 0, 0)
@@ -412,9 +429,7 @@ def block_norms(x: torch.Tensor, branch: torch.Tensor, pre_weight: torch.Tensor,
     y = r / sqrt(mean(r^2) + eps) * pre_weight.  x, branch: contiguous [..., dim] of one dtype (float32 or bfloat16);
     gate: as x, or [..., 1, dim] for one gate per sequence; weights [dim], float32 or x's dtype.
     """
-    if torch.is_grad_enabled() and (x.requires_grad or branch.requires_grad or pre_weight.requires_grad or
-                                    (post_weight is not None and post_weight.requires_grad) or
-                                    (gate is not None and gate.requires_grad)):
+    if _seen_by_autograd(x, branch, pre_weight, post_weight, gate):
         return _BlockNorms.apply(x, branch, pre_weight, post_weight, gate, float(scale), float(eps))
     return _block_norms_forward(_norms_problem("block_norms", x, pre_weight, float(eps), float(scale), branch, gate, post_weight), x)
 
@@ -447,7 +462,7 @@ def gated_norm(x: torch.Tensor, gate: torch.Tensor | None, weight: torch.Tensor,
     """x / sqrt(mean(x^2) + eps) * weight * silu(gate) over the last dimension (a head).  Asynchronous, differentiable.
 
     x, gate: contiguous [..., dim] of one dtype (float32 or bfloat16); gate None: no factor; weight [dim], float32 or x's."""
-    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (gate is not None and gate.requires_grad)):
+    if _seen_by_autograd(x, gate, weight):
         return _GatedNorm.apply(x, gate, weight, float(eps))
     p = _norms_problem("gated_norm", x, weight, float(eps), gate=gate)
     y = torch.empty_like(x)

@@ -49,3 +49,18 @@ def test_strides_of_empty_tensors_are_not_looked_at(ha):
     ha._rows(one.expand(2, 3, 0, 16).contiguous(), "d_o")
     with pytest.raises(ValueError, match="contiguous"):
         ha._rows(one.expand(2, 3, 4, 16), "d_o")
+
+
+def test_what_autograd_has_to_see(ha):
+    from torch.autograd import forward_ad
+    x, leaf = torch.ones(3), torch.ones(3, requires_grad=True)
+    assert not ha._seen_by_autograd(x, None) and ha._seen_by_autograd(x, None, leaf)
+    with torch.no_grad():
+        assert not ha._seen_by_autograd(leaf)
+    ha._no_tangents("a call", x)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, x)
+        assert not dual.requires_grad and ha._seen_by_autograd(dual)
+        ha._no_tangents("a call", x, leaf)
+        with pytest.raises(NotImplementedError, match="a call"):
+            ha._no_tangents("a call", x, dual)

@@ -149,3 +149,25 @@ def test_a_step_on_a_state_that_a_graph_has_kept_is_noticed(ha):  # noqa: F811
     with torch.inference_mode():  # tensors without a version
         state = s0.clone()
         ha.decay_attention_step(*one, state)
+
+
+def test_tangents_are_refused_and_not_dropped(ha):  # noqa: F811
+    from torch.autograd import forward_ad
+    q, k, v, log_a, s0 = make(2, 9, 2, 2, 2, 2, 64, 64, F32, state=True)
+    x, w = torch.randn(4, 64, device=DEV), torch.ones(64, device=DEV)
+    want = [*ha.decay_attention(q, k, v, log_a, s0), *ha.block_norms(x, x, w), ha.gated_norm(x, x, w)]
+    with forward_ad.dual_level():
+        dual = lambda t: forward_ad.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for call in (lambda: ha.decay_attention(dual(q), k, v, log_a), lambda: ha.decay_attention(q, k, v, log_a, dual(s0)),
+                     lambda: ha.decay_attention_step(q[:, 0], k[:, 0], v[:, 0], dual(log_a[:, 0]), s0.clone()),
+                     lambda: ha.decay_attention_step(q[:, 0], k[:, 0], v[:, 0], log_a[:, 0], dual(s0.clone())),
+                     lambda: ha.block_norms(x, dual(x), w), lambda: ha.block_norms(x, x, w, gate=dual(x)),
+                     lambda: ha.gated_norm(x, x, dual(w))):
+            for grad in (True, False):
+                with torch.set_grad_enabled(grad), pytest.raises(NotImplementedError):
+                    call()
+        # without a tangent nothing changes while a level is active
+        got = [*ha.decay_attention(q, k, v, log_a, s0), *ha.block_norms(x, x, w), ha.gated_norm(x, x, w)]
+        ha.decay_attention_step(q[:, 0], k[:, 0], v[:, 0], log_a[:, 0], s0.clone())
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
