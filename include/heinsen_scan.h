@@ -246,6 +246,8 @@ hs_status heinsen_scan_set_path(hs_path path);
  * the carries and the tiles waiting for it run out of polls, record HS_ERR_LOOKBACK_TIMEOUT in the
  * workspace and leave;
  * -1 disables it.  Nothing faults or hangs: the kernel returns and the context stays usable.
+ * The tensor-core passes of heinsen_attention.h take the same two settings: their waits are bounded by the same number of
+ * polls, and the decays of chunk `mute_tile` (128 tokens) are not announced, so that the chunk's waits run out.
  */
 hs_status heinsen_scan_debug_config(uint32_t lookback_spin_limit, int64_t mute_tile);
 /*

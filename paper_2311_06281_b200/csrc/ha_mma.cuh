@@ -45,7 +45,7 @@ constexpr int kFeedRegs = 80;
 constexpr int kRowRegs = 64, kStateRegs = 136;
 constexpr uint32_t kTile = 128 * 256;        // 128 rows of 128 bf16: two blocks of 64 columns, 128-byte swizzle
 constexpr uint32_t kBlock = kTile / 2;
-constexpr uint32_t kSpin = 1u << 20;         // polls of a barrier before a wait gives up (about a microsecond each)
+constexpr uint32_t kDrainSpin = 1u << 16;    // polls for what is still in flight when a CTA leaves (about a microsecond each)
 
 struct Fault {  // the header that heinsen_scan_check() reads
     unsigned long long started_id, error_id;
@@ -79,6 +79,8 @@ struct MmaPass {
     float* cross;
     Fault* fault;
     unsigned long long call_id;
+    uint32_t spin;  // polls of a barrier before a wait gives up (about a microsecond each)
+    int mute;       // tests: the chunk whose decays are never announced, or -1
 };
 
 // A chunk whose decay is below 2^-60 passes nothing on from before it that float32 could see beside what is in it.
@@ -120,17 +122,26 @@ static_assert(kBars <= 40, "barriers");
 
 template <int kValue> struct Int { static constexpr int value = kValue; };
 
+// A thread whose wait has given up runs on without waiting (its warp's loads and stores of tensor memory need every lane), but
+// never arrives on a barrier again: nobody takes what it did not do for done, no barrier gets more arrivals in a phase than it
+// expects (one too many makes a fault), and the others' waits find `stop` set.
 struct Waiter {
     uint32_t bars;
     volatile int* stop;  // in shared memory: some wait of this CTA gave up
+    uint32_t limit;
     __device__ __forceinline__ bool operator()(int bar, int turn) const {
 #pragma unroll 1
-        for (uint32_t i = 0; i < kSpin; ++i) {
+        for (uint32_t i = 0; i < limit; ++i) {
             if (bar_try(bars + 8 * bar, turn & 1)) return true;
             if (*stop) return false;
         }
         *stop = 1 + bar;
         return false;
+    }
+    // What this thread has in flight on a barrier lands before it leaves, whoever has given up meanwhile.
+    __device__ __forceinline__ void drain(int bar, int turn) const {
+#pragma unroll 1
+        for (uint32_t i = 0; i < kDrainSpin && !bar_try(bars + 8 * bar, turn & 1); ++i) {}
     }
 };
 
@@ -186,7 +197,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
     volatile int* const stop = reinterpret_cast<int*>(sm8 + L::whole + 16);
     uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(sm8 + L::whole + 20);
     const uint32_t bars = base + L::bars;
-    const Waiter wait{bars, stop};
+    const Waiter wait{bars, stop, p.spin};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
     const int cuts = kStateOnly ? p.segments - 1 : p.segments;  // the last segment's own state is not needed by another
@@ -270,7 +281,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 if (dim > 64) tma_load_4d(to + kBlock, m, 64, head, t0, b, bars + 8 * full);
             };
             bool ok = true;
-            int loads_x = 0, loads_y = 0, loads_z = 0, loads_w = 0;
+            int loads_x = 0, loads_y = 0, loads_z = 0, loads_w = 0, patched = -1;
             for (int it = 0; it < count && ok; ++it) {
                 const int t0 = chunk_at(it) * kChunk;
                 // tokens behind the sequence's end are in memory and may hold anything: 0 * NaN must not reach a sum
@@ -279,6 +290,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 if (lane == 0) {  // in the order in which tiles become free
                     if (kDots && it >= 1) ok = wait(kFreeY + it % L::kYs, (it - 1) / L::kYs);  // the state's last term was in it
                     if (!kDots && it >= L::kYs) ok = wait(kFreeY + it % L::kYs, it / L::kYs - 1);
+                    if (ok && patch) patched = it;
                     if (ok) load(&my, Y, p.dx, h / p.ydiv, t0, patch ? kPatchY : kFullY + it % L::kYs);
                     if (ok) loads_y = it + 1;
                     if (!kStateOnly) {
@@ -314,15 +326,16 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 }
                 ok = __shfl_sync(~0u, (int)ok, 0);
             }
-            if (*stop && lane == 0) {  // nothing may land in shared memory after the CTA has left
-                auto drain = [&](int full, int stages, int loads) {
+            if (lane == 0) {  // nothing may land in shared memory after the CTA has left
+                auto drain = [&](int full, int stages, int loads, int patch) {
                     for (int it = max(0, loads - stages); it < loads; ++it)
-                        for (uint32_t i = 0; i < kSpin / 16 && !bar_try(bars + 8 * (full + it % stages), (it / stages) & 1); ++i) {}
+                        if (patch && it == patched) wait.drain(patch, 0);
+                        else wait.drain(full + it % stages, it / stages);
                 };
-                drain(kFullY, L::kYs, loads_y);
-                drain(kFullZ, L::kZs, loads_z);
-                if (kDots) drain(kFullW, 1, loads_w);
-                if (!kStateOnly) drain(kFullX, L::kXs, loads_x);
+                drain(kFullY, L::kYs, loads_y, kPatchY);
+                drain(kFullZ, L::kZs, loads_z, kPatchZ);
+                if (kDots) drain(kFullW, 1, loads_w, 0);
+                if (!kStateOnly) drain(kFullX, L::kXs, loads_x, 0);
             }
         } else if (warp == kDecayer) {
             // ------------------------------------------------------------ decays, a lane has four tokens
@@ -364,7 +377,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 four(2, hi.z, lo.z, st.z, bt.z);
                 four(3, hi.w, lo.w, st.w, bt.w);
                 if (it > 0) ok = __all_sync(~0u, wait(kDecaysFree, it - 1));
-                if (!ok) break;
+                if (!ok || chunk_at(it) == p.mute) break;
                 reinterpret_cast<float4*>(c_hi)[lane] = hi;
                 reinterpret_cast<float4*>(c_lo)[lane] = lo;
                 reinterpret_cast<float4*>(w_st)[lane] = st;
@@ -424,10 +437,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     mma_commit(bars + 8 * ((kDots ? kTileDone : kFreeY) + ys));
                     if (kStateOnly && it + 1 < count) ok = transpose(it + 1);
                 }
-                if (!ok) {
-                    mma_commit(bars + 8 * kDrain);
-                    for (uint32_t i = 0; i < kSpin / 16 && !bar_try(bars + 8 * kDrain, 0); ++i) {}
-                }
+                mma_commit(bars + 8 * kDrain);
+                wait.drain(kDrain, 0);
             }
             __syncwarp();
         } else if (!kStateOnly && warp == kOutIssuer) {
@@ -513,10 +524,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     if (ok && it + 1 < count) ok = chunk(it + 1, Int<1>{});
                 }
                 if (ok && count > 0 && (ok = wait(kOutRead, count - 1))) send(count - 1);
-                if (!ok) {
-                    mma_commit(bars + 8 * (kDrain + 1));
-                    for (uint32_t i = 0; i < kSpin / 16 && !bar_try(bars + 8 * (kDrain + 1), 0); ++i) {}
-                }
+                mma_commit(bars + 8 * (kDrain + 1));
+                wait.drain(kDrain + 1, 0);
                 tma_store_wait_all();
             }
             __syncwarp();
@@ -535,10 +544,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 tmem_after_sync();
                 weigh(at, 4 * side + 2, min(steps, 4 * side + 4), none);
                 release_reads();
-                bar_arrive(bars + 8 * kDecaysFree);
+                if (ok) bar_arrive(bars + 8 * kDecaysFree);
                 tmem_wait_st();
                 tmem_before_sync();
-                bar_arrive(bars + 8 * kWeighted);
+                if (ok) bar_arrive(bars + 8 * kWeighted);
             }
         }
         if (!kStateOnly) {
@@ -552,7 +561,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 for (int i = 0; i < 4; ++i) tmem_st8(at + L::tp + 32 * side + 8 * i, zero);
                 tmem_wait_st();
             }
-            bool ok = true;  // once a wait has given up, the rest runs on without waiting: its barriers need every thread
+            bool ok = true;
             for (int it = 0; it < count; ++it) {
                 const int t0 = chunk_at(it) * kChunk, t = t0 + row;
                 const int batches = min(4, (live - t0 + 31) / 32);
@@ -572,7 +581,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 for (int n = 0; n < 4; ++n) {
                     if (kDots && n == 2) {  // the first half of w Z^T has been read by this thread
                         tmem_before_sync();
-                        bar_arrive(bars + 8 * kHalfRead);
+                        if (ok) bar_arrive(bars + 8 * kHalfRead);
                         ok = ok && wait(kHalf, it);
                         tmem_after_sync();
                     }
@@ -633,10 +642,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     }
                 }
                 release_reads();
-                bar_arrive(bars + 8 * kDecaysFree);
+                if (ok) bar_arrive(bars + 8 * kDecaysFree);
                 tmem_wait_st();
                 tmem_before_sync();
-                bar_arrive(bars + 8 * kProbs);
+                if (ok) bar_arrive(bars + 8 * kProbs);
                 ok = ok && wait(kFar, it);
                 tmem_after_sync();
                 const int col0 = 64 * side, col1 = min(p.dz, col0 + 64);
@@ -661,11 +670,11 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 }
                 if constexpr (kDots) {
                     release_reads();
-                    bar_arrive(bars + 8 * kFreeW);
+                    if (ok) bar_arrive(bars + 8 * kFreeW);
                 }
                 tmem_wait_st();
                 tmem_before_sync();
-                bar_arrive(bars + 8 * kFarRead);
+                if (ok) bar_arrive(bars + 8 * kFarRead);
                 ok = ok && wait(kNear, it);
                 tmem_after_sync();
                 // products may still read the tile that the output leaves from
@@ -690,7 +699,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 }
                 if (sizeof(Out) == 2) fence_smem_to_async();
                 tmem_before_sync();
-                bar_arrive(bars + 8 * kOutRead);
+                if (ok) bar_arrive(bars + 8 * kOutRead);
                 if constexpr (kDots) {
                     const long long to = ((long long)side * gridDim.x / p.segments + bh) * p.tokens + t;
                     float a, c;
@@ -729,6 +738,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             }
             s[k / 2] = make_pair2(s0, s1);
         }
+        bool ok = true;
         auto publish = [&]() {  // the state as the B operand of X S: row z, contiguous along k
             if (columns) {
 #pragma unroll
@@ -748,7 +758,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 }
                 fence_smem_to_async();
             }
-            bar_arrive(bars + 8 * kStateReady);
+            if (ok) bar_arrive(bars + 8 * kStateReady);
         };
         // kDots: the state's third term goes where the output of the chunk before has left from
         auto publish_last = [&](int it) {
@@ -767,10 +777,9 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 }
                 fence_smem_to_async();
             }
-            bar_arrive(bars + 8 * kStateLast);
+            if (ok) bar_arrive(bars + 8 * kStateLast);
         };
         if (!kStateOnly && count > 0) publish();
-        bool ok = true;
         for (int it = 0; it < count; ++it) {
             const int t0 = chunk_at(it) * kChunk;
             const int steps = 2 * min(4, (live - t0 + 31) / 32);
@@ -784,10 +793,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
             const int q0 = 4 * side, q1 = min(steps, q0 + (kStateOnly ? 2 : 4));
             weigh(at, q0, q1, last);
             release_reads();
-            bar_arrive(bars + 8 * kDecaysFree);
+            if (ok) bar_arrive(bars + 8 * kDecaysFree);
             tmem_wait_st();
             tmem_before_sync();
-            bar_arrive(bars + 8 * kWeighted);
+            if (ok) bar_arrive(bars + 8 * kWeighted);
             if constexpr (kDots) {
                 if (it > 0) ok = ok && wait(kSent, it - 1);
                 publish_last(it);
@@ -800,7 +809,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     if (q0 + i < q1) tmem_st8(at + L::weighted(q0 + i, 0), last[i]);
                 tmem_wait_st();
                 tmem_before_sync();
-                bar_arrive(bars + 8 * kWeightedLast);
+                if (ok) bar_arrive(bars + 8 * kWeightedLast);
             }
             if constexpr (kDots && !kRev) {  // the state from before this chunk, while its update is formed
                 if (crosses && columns && mine) {
@@ -850,7 +859,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                     for (int u = 0; u < 16; u += 2) s[(j + u) / 2] = fma2(whole2, s[(j + u) / 2], make_pair2(v[u], v[u + 1]));
                 }
             tmem_before_sync();
-            bar_arrive(bars + 8 * kUpdateRead);
+            if (ok) bar_arrive(bars + 8 * kUpdateRead);
             if (!kStateOnly && it + 1 < count) {
                 ok = ok && wait(kFar, it);  // this chunk's X S has read the state it started from
                 publish();

@@ -252,6 +252,8 @@ hs_status mma_pass(const Pass& ps, const View& x, const View& y, const View& z, 
     mp.s_in_mul = ps.s_in_mul; mp.s_out_mul = ps.s_out_mul;
     mp.out = ps.out; mp.ob = ps.ob; mp.ot = ps.ot; mp.oh = ps.oh;
     mp.fault = reinterpret_cast<ha::Fault*>(ws); mp.call_id = id;
+    mp.spin = hs_internal::spin_limit();
+    mp.mute = (int)std::min<long long>(hs_internal::mute_tile(), 0x7fffffff);
     const long long pairs = (long long)ps.batch * ps.heads, chunks = (ps.tokens + ha::kChunk - 1) / ha::kChunk;
     mp.segments = segments_for(pairs, ps.tokens, kSms);
     mp.seg_chunks = (int)((chunks + mp.segments - 1) / mp.segments);

@@ -638,6 +638,8 @@ hs_status current_device(int* sm_count) {
 }
 void count_launches(int n) { g_launches.fetch_add(n); }
 unsigned long long call_id() { return next_call_id(); }
+unsigned int spin_limit() { return g_spin_limit.load(); }
+long long mute_tile() { return g_mute_tile.load(); }
 }  // namespace hs_internal
 
 extern "C" {

@@ -13,5 +13,8 @@ hs_status current_device(int* sm_count);
 void count_launches(int n);
 // Identifies one call in a workspace header; never 0, not repeated within a process.
 unsigned long long call_id();
+// What heinsen_scan_debug_config has set: polls of a bounded wait, and the tile (chunk) that is to be left unannounced, or -1.
+unsigned int spin_limit();
+long long mute_tile();
 #pragma GCC visibility pop
 }  // namespace hs_internal

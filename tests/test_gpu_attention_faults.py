@@ -1,0 +1,61 @@
+"""Bounded waits of the tensor-core passes that run out: the kernels return, the failure is reported, the next call is right.
+The failure is a signal that is not given (the decays of one chunk are never announced) under a small limit of polls; nothing
+faults or hangs."""
+import pytest
+import torch
+
+from test_gpu_attention import BF16, DEV, F32, ha, make  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+HS_ERR_COPY_TIMEOUT = 6
+
+
+@pytest.fixture
+def hs():
+    from paper_2311_06281_b200 import heinsen_scan
+    yield heinsen_scan
+    heinsen_scan.debug_config(0, -1)
+
+
+# (b, t, h), the silent chunk, lengths: whole and cut sequences, the first, a middle and the last, partly filled chunk
+CASES = [((2, 1000, 60), 3, None), ((1, 1500, 2), 2, None), ((1, 1500, 2), 11, None), ((3, 520, 40), 0, None),
+         ((2, 700, 50), 4, (600, 530)), ((1, 100, 1), 0, None)]
+
+
+@pytest.mark.parametrize("shape,silent,lengths", CASES, ids=str)
+def test_a_wait_that_runs_out_is_reported_in_the_workspace(ha, hs, shape, silent, lengths):  # noqa: F811
+    q, k, v, log_a, s0 = make(*shape, *[shape[2]] * 3, 128, 64, BF16, state=True)
+    ends = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    ws = ha.workspace(q, k, v, log_a)
+    want = ha.decay_attention(q, k, v, log_a, s0, lengths=ends, workspace=ws)
+    hs.check(ws)
+    for _ in range(2):
+        hs.debug_config(20000, silent)
+        ha.decay_attention(q, k, v, log_a, s0, lengths=ends, workspace=ws)
+        with pytest.raises(hs.HeinsenScanError) as e:
+            hs.check(ws)
+        assert e.value.status == HS_ERR_COPY_TIMEOUT
+        hs.debug_config(0, -1)
+        got = ha.decay_attention(q, k, v, log_a, s0, lengths=ends, workspace=ws)
+        hs.check(ws)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("shape,silent,lengths", CASES, ids=str)
+def test_gradients_are_right_again_after_a_wait_that_ran_out(ha, hs, shape, silent, lengths):  # noqa: F811
+    ins = [x.requires_grad_() for x in make(*shape, *[shape[2]] * 3, 128, 64, BF16, state=True)]
+    ends = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    d_o = torch.randn(*shape, 64, device=DEV).to(BF16)
+
+    def gradients(silence):
+        o, s = ha.decay_attention(*ins, lengths=ends)
+        if silence:
+            hs.debug_config(20000, silent)
+        got = torch.autograd.grad([o, s], ins, [d_o, torch.ones_like(s)])
+        torch.cuda.synchronize()
+        hs.debug_config(0, -1)
+        return got
+    want = gradients(False)
+    gradients(True)
+    assert all(torch.equal(a, b) for a, b in zip(gradients(False), want))
