@@ -51,7 +51,8 @@ typedef struct {
 /*
  * o_t for every token of every sequence, and the state after the last one (`state`, may be NULL).
  * `state` may be `state0` itself.  o.ptr is written through its strides.  Asynchronous on `stream`.
- * workspace: 256-byte aligned device scratch of heinsen_attention_workspace_bytes(p, 0) bytes.
+ * workspace: 256-byte aligned device scratch of heinsen_attention_workspace_bytes(p, 0) bytes.  heinsen_scan_check(workspace,
+ * stream) returns HS_ERR_COPY_TIMEOUT where a bounded wait of the last call on it ran out: its outputs are not valid then.
  */
 hs_status heinsen_attention_forward(const heinsen_attention_problem* p, const heinsen_attention_tensor* o, float* state,
                                     void* workspace, size_t workspace_bytes, void* stream);

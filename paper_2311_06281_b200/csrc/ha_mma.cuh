@@ -47,11 +47,6 @@ constexpr uint32_t kTile = 128 * 256;        // 128 rows of 128 bf16: two blocks
 constexpr uint32_t kBlock = kTile / 2;
 constexpr uint32_t kDrainSpin = 1u << 16;    // polls for what is still in flight when a CTA leaves (about a microsecond each)
 
-struct Fault {  // the header that heinsen_scan_check() reads
-    unsigned long long started_id, error_id;
-    int error_code, error_where;
-};
-
 struct MmaPass {
     const float* log_a;
     long long ab, at, ah;

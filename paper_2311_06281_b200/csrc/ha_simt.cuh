@@ -39,6 +39,11 @@ struct Rows {  // [batch, tokens, heads', dim] with a contiguous last dimension,
     int div;  // head h reads head h / div
 };
 
+struct Fault {  // the header that heinsen_scan_check() reads
+    unsigned long long started_id, error_id;
+    int error_code, error_where;
+};
+
 struct Pass {
     Rows x, y, z;
     const float* log_a;
@@ -58,6 +63,8 @@ struct Pass {
     float* seg_state;
     float* seg_decay;
     int rev;
+    Fault* fault;
+    unsigned long long call_id;
 };
 // Passes over the same sequences that do not depend on one another go in one launch, blockIdx.y each.
 struct Passes {
@@ -298,6 +305,8 @@ __device__ __forceinline__ void simt_pass(const Pass& p) {
 template <class T, class OutT, bool kStateOnly, int kCols>
 __global__ void __launch_bounds__(kSimtThreads, 2) simt_pass_kernel(const __grid_constant__ Passes passes) {
     const Pass& p = passes.p[blockIdx.y];
+    // nothing here waits, but the header of a kept workspace may still show what an earlier call met
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) p.fault->started_id = p.call_id;
     if (p.rev) simt_pass<T, true, OutT, kStateOnly, kCols>(p);
     else simt_pass<T, false, OutT, kStateOnly, kCols>(p);
 }

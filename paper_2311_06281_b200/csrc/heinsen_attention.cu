@@ -340,6 +340,8 @@ hs_status forward_pass(const heinsen_attention_problem* p, const heinsen_attenti
     ha::Passes list;
     std::memset(&list, 0, sizeof list);
     list.p[0] = ps;
+    list.p[0].fault = reinterpret_cast<ha::Fault*>(ws);
+    list.p[0].call_id = hs_internal::call_id();
     return simt_passes<T, T>(list, 1, simt_segments(p, 1), ws + kHeaderBytes, stream);
 }
 
@@ -397,6 +399,8 @@ hs_status backward_passes(const heinsen_attention_problem* p, const heinsen_atte
         ps.rev = 1;
         list.p[2] = ps;
     }
+    list.p[0].fault = reinterpret_cast<ha::Fault*>(ws);
+    list.p[0].call_id = hs_internal::call_id();
     if ((st = simt_passes<T, float>(list, 3, simt_segments(p, 3), space, stream)) != HS_OK) return st;
     if ((st = sum_heads<T>(wq, dq, p, p->q_heads, p->k_dim, stream)) != HS_OK) return st;
     if ((st = sum_heads<T>(wk, dk, p, p->k_heads, p->k_dim, stream)) != HS_OK) return st;

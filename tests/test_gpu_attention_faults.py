@@ -59,3 +59,17 @@ def test_gradients_are_right_again_after_a_wait_that_ran_out(ha, hs, shape, sile
     want = gradients(False)
     gradients(True)
     assert all(torch.equal(a, b) for a, b in zip(gradients(False), want))
+
+
+def test_a_call_on_the_cuda_cores_does_not_report_an_earlier_failure(ha, hs):  # noqa: F811
+    q, k, v, log_a, s0 = make(1, 700, 2, 2, 2, 2, 64, 64, BF16, state=True)
+    ws = torch.empty(max(ha.workspace(*x, log_a).numel() for x in ((q, k, v), (q.float(), k.float(), v.float()))),
+                     dtype=torch.uint8, device=DEV)
+    for other in ([q.float(), k.float(), v.float(), log_a, s0], [x[:, :5].float() for x in (q, k, v, log_a)]):
+        hs.debug_config(20000, 1)
+        ha.decay_attention(q, k, v, log_a, s0, workspace=ws)
+        with pytest.raises(hs.HeinsenScanError):
+            hs.check(ws)
+        hs.debug_config(0, -1)
+        ha.decay_attention(*other, workspace=ws)  # float32: another kernel, the same workspace
+        hs.check(ws)
