@@ -71,6 +71,13 @@ hs_status heinsen_attention_backward(const heinsen_attention_problem* p, const h
 size_t heinsen_attention_workspace_bytes(const heinsen_attention_problem* p, int backward);
 
 /*
+ * Synchronises `stream` and returns HS_ERR_COPY_TIMEOUT where a bounded wait of any forward or backward call on the current
+ * device, whatever its workspace, has run out since this was last asked (outputs of such calls are not valid); HS_OK otherwise.
+ * It finds what calls that completed before it have met.
+ */
+hs_status heinsen_attention_check(void* stream);
+
+/*
  * One token for each of `batch` sequences (problem with tokens == 1; lengths and state0 must be NULL).  The states are
  * rows of a pool [pool, heads, k_dim, v_dim] that is updated in place: sequence b uses row slots[b], or row b where
  * slots is NULL (pool >= batch).  A slot that is negative or >= pool has no state: nothing is read or written for it and

@@ -81,6 +81,9 @@ struct MmaPass {
 // A chunk whose decay is below 2^-60 passes nothing on from before it that float32 could see beside what is in it.
 constexpr float kNothingCrosses = -60.0f;
 
+// Where a bounded wait of any pass on this device has run out since the record was last read, plus one; 0: nowhere.
+__device__ int g_gave_up;
+
 template <bool kDots>
 struct MmaLayout {
     static constexpr int kTerms = kDots ? 2 : 1;               // of the state in X S (kDots: a third in a Y tile)
@@ -879,6 +882,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
     if (tid == 0 && *stop) {
         p.fault->error_code = 6;  // HS_ERR_COPY_TIMEOUT
         p.fault->error_where = *stop;
+        g_gave_up = *stop;
         __threadfence();
         p.fault->error_id = p.call_id;
     }

@@ -592,6 +592,20 @@ hs_status heinsen_attention_backward(const heinsen_attention_problem* p, const h
                : backward_passes<__nv_bfloat16>(p, d_o, d_state, dq, dk, dv, dlog_a, dstate0, ws, s);
 }
 
+hs_status heinsen_attention_check(void* stream) {
+    int sms, where = 0;
+    const hs_status st = hs_internal::current_device(&sms);
+    if (st != HS_OK) return st;
+    cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return hs_internal::cuda_fail("cudaStreamSynchronize", e);
+    e = cudaMemcpyFromSymbol(&where, ha::g_gave_up, sizeof where);
+    if (e != cudaSuccess) return hs_internal::cuda_fail("cudaMemcpyFromSymbol", e);
+    if (!where) return HS_OK;
+    const int none = 0;
+    e = cudaMemcpyToSymbol(ha::g_gave_up, &none, sizeof none);
+    return e == cudaSuccess ? HS_ERR_COPY_TIMEOUT : hs_internal::cuda_fail("cudaMemcpyToSymbol", e);
+}
+
 hs_status heinsen_attention_step(const heinsen_attention_problem* p, const heinsen_attention_tensor* o, float* pool_state,
                                  int64_t pool, const int32_t* slots, void* stream) {
     hs_status st = validate(p);

@@ -20,7 +20,7 @@ from .heinsen_scan import HeinsenScanError, _check, _dtype_code, _on_device, lib
 
 EXPORTS = [
     "heinsen_attention_forward", "heinsen_attention_backward", "heinsen_attention_workspace_bytes",
-    "heinsen_attention_step", "heinsen_block_norms_forward", "heinsen_block_norms_backward",
+    "heinsen_attention_step", "heinsen_attention_check", "heinsen_block_norms_forward", "heinsen_block_norms_backward",
     "heinsen_block_norms_workspace_bytes", "heinsen_gated_norm_forward", "heinsen_gated_norm_backward",
     "heinsen_gated_norm_workspace_bytes",
 ]
@@ -97,6 +97,7 @@ def lib() -> ctypes.CDLL:
                 ("heinsen_attention_backward", [pr, te, vp, vp, vp, vp, vp, vp, vp, sz, vp], ci),
                 ("heinsen_attention_workspace_bytes", [pr, ci], sz),
                 ("heinsen_attention_step", [pr, te, vp, i64, vp, vp], ci),
+                ("heinsen_attention_check", [vp], ci),
                 ("heinsen_block_norms_forward", [no, vp, vp, vp], ci),
                 ("heinsen_block_norms_backward", [no, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], ci),
                 ("heinsen_block_norms_workspace_bytes", [no], sz),
@@ -283,6 +284,14 @@ def workspace(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: torch.Te
     return _space(_call().space(_problem(q, k, v, log_a, None, 1.0, None).packed, 0), q.device)
 
 
+def check(device) -> None:
+    """Synchronises the current stream of `device` and raises if a bounded wait of any ``decay_attention`` call there, forward
+    or backward, has run out on the device since the last check: the results of such a call are not valid."""
+    device = torch.device(device)
+    with _on_device(device):
+        _check(lib().heinsen_attention_check(torch.cuda.current_stream(device).cuda_stream))
+
+
 def decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: torch.Tensor,
                     state0: torch.Tensor | None = None, *, scale: float | None = None,
                     lengths: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
@@ -294,7 +303,8 @@ def decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: to
     scale defaults to K ** -0.5.  o [B, T, H, V] has q's dtype, state [B, H, K, V] is float32 (what the next call or
     ``decay_attention_step`` takes).  log_a = -inf forgets the state at that token: packed sequences start so.
     workspace: scratch from ``workspace()``, kept by the caller; ``heinsen_scan.check(workspace)`` then reports what the
-    device recorded (a bounded wait that ran out).  Without it each call takes its own.
+    device recorded for the last call (a bounded wait that ran out).  Without it each call takes its own; ``check(device)``
+    reports for all calls, backward ones too.
     """
     scale = float(q.shape[-1] ** -0.5 if scale is None else scale)
     if _seen_by_autograd(q, k, v, log_a, state0):

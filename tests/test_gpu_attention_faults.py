@@ -73,3 +73,31 @@ def test_a_call_on_the_cuda_cores_does_not_report_an_earlier_failure(ha, hs):  #
         hs.debug_config(0, -1)
         ha.decay_attention(*other, workspace=ws)  # float32: another kernel, the same workspace
         hs.check(ws)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_failures_without_a_kept_workspace_are_found(ha, hs, backward):  # noqa: F811
+    ins = [x.requires_grad_(backward) for x in make(1, 1500, 2, 2, 2, 2, 128, 128, BF16, state=True)]
+    try:
+        ha.check(DEV)
+    except hs.HeinsenScanError:
+        pass  # what the tests before have left
+    ha.check(DEV)
+
+    def call(silence):
+        if silence and not backward:
+            hs.debug_config(20000, 5)
+        o, s = ha.decay_attention(*ins)
+        if backward:
+            if silence:
+                hs.debug_config(20000, 5)
+            torch.autograd.grad(o.float().sum(), ins)
+        hs.debug_config(0, -1)
+    for _ in range(2):
+        call(True)
+        with pytest.raises(hs.HeinsenScanError) as e:
+            ha.check(DEV)
+        assert e.value.status == HS_ERR_COPY_TIMEOUT
+        ha.check(DEV)  # told once
+        call(False)
+        ha.check(torch.device(DEV))
