@@ -59,9 +59,10 @@ hs_status heinsen_attention_forward(const heinsen_attention_problem* p, const he
 
 /*
  * The gradients of every input.  d_o is the gradient of o (strides as given); d_state that of the last state, or NULL.
- * Nothing of the forward call is needed again.  Outputs, all contiguous: dk, dv in the shapes of q, k, v (summed over the heads that share a head); dlog_a float32
- * [batch, tokens, heads], or [heads] where the decay is fixed (batch and token stride 0); dstate0 float32.
- * dlog_a and dstate0 may be NULL.  Asynchronous; workspace of heinsen_attention_workspace_bytes(p, 1) bytes.
+ * Nothing of the forward call is needed again.  Outputs, all contiguous: dq, dk, dv in the shapes of q, k, v (summed over the
+ * heads that share a head), 16-byte aligned; dlog_a float32 [batch, tokens, heads], or [heads] where the decay is fixed (batch
+ * and token stride 0); dstate0 float32.  dlog_a and dstate0 may be NULL.  Where d_state is given 1 / scale has to be finite.
+ * Without sequences or heads, gradients that have elements all the same are zeros.  Asynchronous; workspace of heinsen_attention_workspace_bytes(p, 1) bytes.
  */
 hs_status heinsen_attention_backward(const heinsen_attention_problem* p, const heinsen_attention_tensor* d_o,
                                      const float* d_state, void* dq, void* dk, void* dv, float* dlog_a,

@@ -579,6 +579,9 @@ hs_status heinsen_attention_backward(const heinsen_attention_problem* p, const h
     if (nothing(p)) return zero_gradients(p, dq, dk, dv, dlog_a, static_cast<cudaStream_t>(stream));
     if ((st = validate_inputs(p)) != HS_OK) return st;
     if (!d_o || (p->tokens && (!d_o->ptr || !dq || !dk || !dv))) return HS_ERR_INVALID_ARG;
+    if (d_state && !std::isfinite(1.0f / p->scale)) return HS_ERR_INVALID_ARG;  // the passes take d_state / scale
+    if (mma_fits(p) && ((reinterpret_cast<uintptr_t>(dq) | reinterpret_cast<uintptr_t>(dk) | reinterpret_cast<uintptr_t>(dv)) & 15u))
+        return HS_ERR_INVALID_ARG;  // TMA writes them
     if ((st = check_space(p, 1, workspace, workspace_bytes)) != HS_OK) return st;
     int sms;
     if ((st = hs_internal::current_device(&sms)) != HS_OK) return st;

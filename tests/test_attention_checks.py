@@ -64,3 +64,19 @@ def test_what_autograd_has_to_see(ha):
         ha._no_tangents("a call", x, leaf)
         with pytest.raises(NotImplementedError, match="a call"):
             ha._no_tangents("a call", x, dual)
+
+
+def test_gradients_that_cannot_be_written_are_refused(ha):
+    L = ha.lib()
+    buf = torch.empty(1 << 16, dtype=torch.uint8)
+    p = (buf.data_ptr() + 255) & ~255
+    t = ha._Tensor(p, 64, 32, 16)
+
+    def back(dq=p, dk=p, dv=p, d_state=None, scale=0.5, dtype=1):
+        problem = ha._Problem(2, 4, 2, 2, 2, 2, 16, 16, dtype, scale, t, t, t, t, None, None)
+        size = L.heinsen_attention_workspace_bytes(problem, 1)
+        return L.heinsen_attention_backward(problem, t, d_state, dq, dk, dv, None, None, p, size, None)
+    if not torch.cuda.is_available():  # what is accepted fails at the device
+        assert back() in (2, 4) and back(d_state=p) in (2, 4) and back(dq=p + 4, dtype=0) in (2, 4) and back(scale=1e-39) in (2, 4)
+    for bad in (dict(dq=p + 2), dict(dk=p + 8), dict(dv=p + 4), dict(scale=1e-39, d_state=p), dict(scale=-1e-40, d_state=p, dtype=0)):
+        assert back(**bad) == 1, bad
