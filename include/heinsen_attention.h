@@ -6,8 +6,8 @@
  *         S_t = exp(log_a_t) * S_{t-1} + k_t v_t^T ,     o_t = scale * S_t^T q_t ,        S_t : [k_dim, v_dim]
  *
  * (attention without a softmax; "attention with a decay for each head").  As in heinsen_scan.h the decays are given
- * as logarithms and are only ever summed and subtracted before one exponential is taken, so products of many decays
- * neither underflow early nor lose what is near them; log 0 = -inf is a legal decay and forgets the state.
+ * as logarithms and are only ever summed and subtracted before an exponential is taken, so products of many decays
+ * neither underflow early nor lose what is near them; log 0 = -inf is a legal decay and forgets the state, whatever it holds.
  *
  * Conventions beyond those of heinsen_scan.h
  *   - Tokens are rows: q [batch, tokens, q_heads, k_dim], k [batch, tokens, k_heads, k_dim],
@@ -19,7 +19,12 @@
  *     tokens < 2^31 - 2^20, batch * heads < 2^31.
  *   - lengths (optional, int32 [batch]): row b has lengths[b] tokens (clamped to 0..tokens).  What lies behind them is
  *     not part of the sequence: it is never used, whatever it holds; o and the gradients are zero there.
- *   - NaN and +inf inside a sequence give unspecified values from that token on in the heads that read them.
+ *   - Decays are meant to lie between 0 and 1.  A positive log decay is taken as it is, as long as every sum of consecutive log
+ *     decays within 128 tokens that holds no -inf lies between -40 and 40: factors of such a sum are formed by themselves.
+ *   - Tokens are worked on in chunks of up to 128, counted from a sequence's first.  A NaN or an infinity in q, k or v, or a NaN
+ *     or +inf in log_a, gives unspecified values in the heads that read it from the beginning of its chunk on: up to 127 tokens
+ *     before it, and behind it whatever decays follow, so in other sequences too where several are packed into one row with
+ *     decays of zero between them.  Other rows of the batch and other heads are not affected.
  */
 #ifndef HEINSEN_ATTENTION_H_
 #define HEINSEN_ATTENTION_H_

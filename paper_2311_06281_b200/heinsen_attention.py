@@ -301,7 +301,8 @@ def decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: to
     log_a: float32 [B, T, H], or [H] for fixed decays, H a multiple of Hq, Hk and Hv (head h reads head h * Hq // H of q);
     state0 [B, H, K, V] float32 continues earlier tokens; lengths [B] int32 ends row b after lengths[b] tokens.
     scale defaults to K ** -0.5.  o [B, T, H, V] has q's dtype, state [B, H, K, V] is float32 (what the next call or
-    ``decay_attention_step`` takes).  log_a = -inf forgets the state at that token: packed sequences start so.
+    ``decay_attention_step`` takes).  log_a = -inf forgets the state at that token: packed sequences start so.  Log decays are
+    meant to be <= 0.  A NaN or infinity in q, k or v spoils its row's heads from up to 127 tokens before it on.
     workspace: scratch from ``workspace()``, kept by the caller; ``heinsen_scan.check(workspace)`` then reports what the
     device recorded for the last call (a bounded wait that ran out).  Without it each call takes its own; ``check(device)``
     reports for all calls, backward ones too.
