@@ -56,7 +56,7 @@ struct MmaPass {
     float scale;
     const float* s_in;
     float* s_out;
-    int s_in_t, s_out_t;
+    int s_in_t;
     float s_in_mul, s_out_mul;
     void* out;
     long long ob, ot, oh;
@@ -869,11 +869,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
 #pragma unroll
         for (int k = 0; k < 64; k += 2)
             if (to && mine && k0 + k < p.dx) {
-                const bool turned = !kStateOnly && p.s_out_t;
                 float s0, s1;
                 parts(s[k / 2], s0, s1);
-                to[turned ? z * p.dx + k0 + k : (k0 + k) * p.dz + z] = s0 * out_mul;
-                to[turned ? z * p.dx + k0 + k + 1 : (k0 + k + 1) * p.dz + z] = s1 * out_mul;
+                to[(k0 + k) * p.dz + z] = s0 * out_mul;
+                to[(k0 + k + 1) * p.dz + z] = s1 * out_mul;
             }
     }
     tmem_before_sync();

@@ -52,8 +52,8 @@ struct Pass {
     int batch, tokens, heads, dx, dz;
     float scale;
     const float* s_in;   // [batch, heads, dx, dz], or [.., dz, dx] where s_in_t
-    float* s_out;        // likewise
-    int s_in_t, s_out_t;
+    float* s_out;        // [batch, heads, dx, dz]
+    int s_in_t;
     float s_in_mul, s_out_mul;
     void* out;           // [batch, tokens, heads, dz] through its strides
     long long ob, ot, oh;
@@ -297,7 +297,7 @@ __device__ __forceinline__ void simt_pass(const Pass& p) {
     } else if (p.s_out && segment == p.segments - 1) {
         for (int e = tid; e < p.dx * kCols; e += kSimtThreads) {
             const int k = e / kCols, z = z0 + e % kCols;
-            if (z < p.dz) p.s_out[plane + (p.s_out_t ? (long long)z * p.dx + k : (long long)k * p.dz + z)] = st[e] * p.s_out_mul;
+            if (z < p.dz) p.s_out[plane + (long long)k * p.dz + z] = st[e] * p.s_out_mul;
         }
     }
 }

@@ -248,7 +248,7 @@ hs_status mma_pass(const Pass& ps, const View& x, const View& y, const View& z, 
     mp.tokens = ps.tokens; mp.heads = ps.heads; mp.dx = ps.dx; mp.dz = ps.dz;
     mp.xdiv = ps.x.div; mp.ydiv = ps.y.div; mp.zdiv = ps.z.div;
     mp.scale = ps.scale;
-    mp.s_in = ps.s_in; mp.s_out = ps.s_out; mp.s_in_t = ps.s_in_t; mp.s_out_t = ps.s_out_t;
+    mp.s_in = ps.s_in; mp.s_out = ps.s_out; mp.s_in_t = ps.s_in_t;
     mp.s_in_mul = ps.s_in_mul; mp.s_out_mul = ps.s_out_mul;
     mp.out = ps.out; mp.ob = ps.ob; mp.ot = ps.ot; mp.oh = ps.oh;
     mp.fault = reinterpret_cast<ha::Fault*>(ws); mp.call_id = id;

@@ -18,13 +18,6 @@ from torch.autograd import forward_ad
 
 from .heinsen_scan import HeinsenScanError, _check, _dtype_code, _on_device, lib as _scan_lib  # noqa: F401
 
-EXPORTS = [
-    "heinsen_attention_forward", "heinsen_attention_backward", "heinsen_attention_workspace_bytes",
-    "heinsen_attention_step", "heinsen_attention_check", "heinsen_block_norms_forward", "heinsen_block_norms_backward",
-    "heinsen_block_norms_workspace_bytes", "heinsen_gated_norm_forward", "heinsen_gated_norm_backward",
-    "heinsen_gated_norm_workspace_bytes",
-]
-
 
 class _Tensor(ctypes.Structure):
     _fields_ = [("ptr", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
@@ -53,29 +46,49 @@ assert (_PROBLEM.size, _ROWS.size, _NORMS.size) == tuple(ctypes.sizeof(t) for t 
 _lib = None
 _calls = None
 
+_PTR, _SIZE, _INT, _I64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int64
+# Arguments (the problem first) and result of every function
+_SIGNATURES = {
+    "heinsen_attention_forward": ([_Problem, _Tensor, _PTR, _PTR, _SIZE, _PTR], _INT),
+    "heinsen_attention_backward": ([_Problem, _Tensor, _PTR, _PTR, _PTR, _PTR, _PTR, _PTR, _PTR, _SIZE, _PTR], _INT),
+    "heinsen_attention_workspace_bytes": ([_Problem, _INT], _SIZE),
+    "heinsen_attention_step": ([_Problem, _Tensor, _PTR, _I64, _PTR, _PTR], _INT),
+    "heinsen_attention_check": ([_PTR], _INT),
+    "heinsen_block_norms_forward": ([_Norms, _PTR, _PTR, _PTR], _INT),
+    "heinsen_block_norms_backward": ([_Norms, *[_PTR] * 8, _SIZE, _PTR], _INT),
+    "heinsen_block_norms_workspace_bytes": ([_Norms], _SIZE),
+    "heinsen_gated_norm_forward": ([_Norms, _PTR, _PTR], _INT),
+    "heinsen_gated_norm_backward": ([_Norms, *[_PTR] * 5, _SIZE, _PTR], _INT),
+    "heinsen_gated_norm_workspace_bytes": ([_Norms], _SIZE),
+}
+EXPORTS = list(_SIGNATURES)
+
+
+def _bind(function, name: str, structure):
+    """Gives a function its signature; `structure` maps a structure to the type that it is passed as."""
+    args, function.restype = _SIGNATURES[name]
+    function.argtypes = [structure(t) if issubclass(t, ctypes.Structure) else t for t in args]
+    return function
+
 
 class _Calls:
     """The functions once more, taking structures as packed bytes and pointers as integers: filling in ctypes structures
     field by field costs more than a small call does on the GPU."""
 
     def __init__(self, L):
-        vp, sz, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64
+        def of(name):
+            return _bind(L[name], name, lambda _: _PTR)
 
-        def of(name, args, res=ctypes.c_int):
-            f = L[name]
-            f.argtypes, f.restype = args, res
-            return f
-
-        self.forward = of("heinsen_attention_forward", [vp, vp, vp, vp, sz, vp])
-        self.backward = of("heinsen_attention_backward", [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])
-        self.space = of("heinsen_attention_workspace_bytes", [vp, ctypes.c_int], sz)
-        self.step = of("heinsen_attention_step", [vp, vp, vp, i64, vp, vp])
-        self.block_forward = of("heinsen_block_norms_forward", [vp, vp, vp, vp])
-        self.block_backward = of("heinsen_block_norms_backward", [vp] * 9 + [sz, vp])
-        self.block_space = of("heinsen_block_norms_workspace_bytes", [vp], sz)
-        self.gated_forward = of("heinsen_gated_norm_forward", [vp, vp, vp])
-        self.gated_backward = of("heinsen_gated_norm_backward", [vp] * 6 + [sz, vp])
-        self.gated_space = of("heinsen_gated_norm_workspace_bytes", [vp], sz)
+        self.forward = of("heinsen_attention_forward")
+        self.backward = of("heinsen_attention_backward")
+        self.space = of("heinsen_attention_workspace_bytes")
+        self.step = of("heinsen_attention_step")
+        self.block_forward = of("heinsen_block_norms_forward")
+        self.block_backward = of("heinsen_block_norms_backward")
+        self.block_space = of("heinsen_block_norms_workspace_bytes")
+        self.gated_forward = of("heinsen_gated_norm_forward")
+        self.gated_backward = of("heinsen_gated_norm_backward")
+        self.gated_space = of("heinsen_gated_norm_workspace_bytes")
 
 
 def _call() -> _Calls:
@@ -90,21 +103,8 @@ def lib() -> ctypes.CDLL:
     global _lib
     if _lib is None:
         L = _scan_lib()
-        vp, sz, ci, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int64
-        pr, te, no = ctypes.POINTER(_Problem), ctypes.POINTER(_Tensor), ctypes.POINTER(_Norms)
-        for name, args, res in (
-                ("heinsen_attention_forward", [pr, te, vp, vp, sz, vp], ci),
-                ("heinsen_attention_backward", [pr, te, vp, vp, vp, vp, vp, vp, vp, sz, vp], ci),
-                ("heinsen_attention_workspace_bytes", [pr, ci], sz),
-                ("heinsen_attention_step", [pr, te, vp, i64, vp, vp], ci),
-                ("heinsen_attention_check", [vp], ci),
-                ("heinsen_block_norms_forward", [no, vp, vp, vp], ci),
-                ("heinsen_block_norms_backward", [no, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp], ci),
-                ("heinsen_block_norms_workspace_bytes", [no], sz),
-                ("heinsen_gated_norm_forward", [no, vp, vp], ci),
-                ("heinsen_gated_norm_backward", [no, vp, vp, vp, vp, vp, sz, vp], ci),
-                ("heinsen_gated_norm_workspace_bytes", [no], sz)):
-            getattr(L, name).argtypes, getattr(L, name).restype = args, res
+        for name in EXPORTS:
+            _bind(getattr(L, name), name, ctypes.POINTER)
         _lib = L
     return _lib
 
@@ -170,12 +170,8 @@ def _space_ok(workspace: torch.Tensor, device):
         raise ValueError(f"workspace is on {workspace.device}, not on {device}")
 
 
-def _tensor(t: torch.Tensor, name: str) -> _Tensor:
-    """[batch, tokens, heads, dim] of any strides, the last dimension contiguous."""
-    return _Tensor(*_rows(t, name))
-
-
 def _rows(t: torch.Tensor, name: str):
+    """Address and strides of [batch, tokens, heads, dim], the last dimension contiguous."""
     s = t.stride()
     if s[3] != 1 and t.shape[3] > 1 and t.numel():  # an empty tensor counts as contiguous whatever its strides
         raise ValueError(f"{name}: the last dimension must be contiguous")
