@@ -159,8 +159,12 @@ __device__ __forceinline__ float norm_back(float d, float n, float mean, float r
     return dim == 1 ? rs * d * (eps * rs * rs) : rs * fmaf(-n, mean, d);
 }
 
-// one exponential and one reciprocal, each good to about an ulp
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+// float32 results take the exponential and the division that are good to an ulp over the whole range.  Beside bf16 the fast ones
+// do: the exponential's error grows with its argument, to 1e-5 at the largest that is not an infinity, and the result is rounded
+// to 2e-3.
+template <class T> __device__ __forceinline__ float sigmoid(float z);
+template <> __device__ __forceinline__ float sigmoid<float>(float z) { return 1.0f / (1.0f + expf(-z)); }
+template <> __device__ __forceinline__ float sigmoid<__nv_bfloat16>(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
 template <class T, int kVec, int kNv, int kRowThreads>
 __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) block_norms_forward_kernel(const Norms p) {
@@ -378,7 +382,7 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads) gated_n
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
         x[e] *= rs * w[e];
-        if (p.gate) x[e] *= g[e] * sigmoid(g[e]);
+        if (p.gate) x[e] *= g[e] * sigmoid<T>(g[e]);
     }
     if (live) S::store(x, static_cast<T*>(p.y) + row * p.dim, t, p.dim);
 }
@@ -407,7 +411,7 @@ __global__ void __launch_bounds__(kRowThreads < 128 ? 128 : kRowThreads, residen
         for (int e = 0; e < kE; ++e) {
             float d = dy[e];
             if (p.gate) {
-                const float sg = sigmoid(g[e]);
+                const float sg = sigmoid<T>(g[e]);
                 dz[e] = d * w[e] * sg * fmaf(g[e], 1.0f - sg, 1.0f);  // times the norm below
                 d *= g[e] * sg;
             }
