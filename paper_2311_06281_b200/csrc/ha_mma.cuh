@@ -25,10 +25,11 @@
 // kDots: the pass also forms what the decay gradients need of it, in float32: the row sums of W = P o (w Z^T), w the fourth
 // tensor, from the unrounded P, and the dots w_i . (X S)_i, for which X S has the state in three terms.  Each W_ij comes out of
 // the two passes that form it in the same bits (each exponential is taken of the same difference there, each product is rounded
-// once before it is added to anything) and is summed in 64 bits: what cancels between their sums leaves at most 2^-44 of the sum
-// of |W|, at tokens that forget everything too.  (Four products added in float32 first left 2^-28 there, 1e-5 to 1e-4 where
-// nothing belonged; 64 bits from the start cost 3% of a training step.)  Row sums from the outputs instead, w_i . out_i, were 1e-6 off in a common direction (the tensor
-// core's additions cut off), which sums over many tokens turn into 5e-5.
+// once before it is added to anything), and the sums keep what their additions round off: what cancels between them leaves at
+// most 2^-44 of the sum of |W|, at tokens that forget everything too.  (Four products added in float32 first left 1e-5 to 1e-4
+// where nothing belonged.  This costs 2% of a training step, sums in 64 bits cost 4%: conversions are slow.)  Row sums from the
+// outputs instead, w_i . out_i, were 1e-6 off in a common direction (the tensor core's additions cut off), which sums over many
+// tokens turn into 5e-5.
 #pragma once
 #include <cuda.h>
 
@@ -160,6 +161,13 @@ __device__ __forceinline__ pair add_dot(pair sum, const uint32_t (&v)[16], const
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum = fma2(make_pair2(w[i] << 16, w[i] & 0xffff0000u), make_pair2(v[2 * i], v[2 * i + 1]), sum);
     return sum;
+}
+// sum + rest + v with no rounding but that of rest: what the sum's addition rounds off, from the operands themselves (Knuth's
+// two-sum, for v of any size).
+__device__ __forceinline__ void add_exact(pair& sum, pair& rest, pair v) {
+    const pair minus = make_pair2(-1.0f, -1.0f), all = add2(sum, v), own = fma2(sum, minus, all), other = fma2(own, minus, all);
+    rest = add2(rest, add2(fma2(own, minus, v), fma2(other, minus, sum)));
+    sum = all;
 }
 // Sixteen columns of one row, or the n (a multiple of 8) that are left of it
 __device__ __forceinline__ void store16(float* to, const uint32_t (&v)[16], int n) {
@@ -570,7 +578,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 const bool forgotten = far1 == 0.0f;  // a decay of zero forgets the state whatever it holds: no 0 * inf
                 ok = ok && wait(kScores, it);
                 tmem_after_sync();
-                double sum = 0.0, sum_odd = 0.0;  // of W's row, in 64 bits, since two such sums will be subtracted
+                pair sum = 0, sum_rest = 0;  // of W's row, in two floats each, since two such sums will be subtracted
                 pair sum_far = 0;
                 const pair minus = make_pair2(-1.0f, -1.0f), scale2 = make_pair2(p.scale, p.scale);
                 const float to_late = kRev ? 1.0f : -1.0f;
@@ -631,12 +639,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                         for (int j = 0; j < 16; ++j)
                             if (j == own) t16[j] = 0u;
 #pragma unroll
-                        for (int j = 0; j < 16; j += 2) {  // each W_ij rounded once, the same way in both passes, before any addition
-                            float a, c;
-                            parts(mul2(make_pair2(v[j], v[j + 1]), make_pair2(t16[j], t16[j + 1])), a, c);
-                            sum += (double)a;
-                            sum_odd += (double)c;
-                        }
+                        for (int j = 0; j < 16; j += 2)  // each W_ij rounded once, the same way in both passes, before any addition
+                            add_exact(sum, sum_rest, mul2(make_pair2(v[j], v[j + 1]), make_pair2(t16[j], t16[j + 1])));
                     }
                 }
                 release_reads();
@@ -700,10 +704,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1) mma_pass_kernel(const __grid_c
                 if (ok) bar_arrive(bars + 8 * kOutRead);
                 if constexpr (kDots) {
                     const long long to = ((long long)side * gridDim.x / p.segments + bh) * p.tokens + t;
-                    float a, c;
+                    float a, c, s0, s1, r0, r1;
                     parts(sum_far, a, c);
+                    parts(sum, s0, s1);
+                    parts(sum_rest, r0, r1);
                     if (t < live) {
-                        p.dots[to] = sum + sum_odd;
+                        p.dots[to] = ((double)s0 + (double)s1) + ((double)r0 + (double)r1);
                         p.dots_far[to] = columns ? a + c : 0.0f;
                     }
                 }
