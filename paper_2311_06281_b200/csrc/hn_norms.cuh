@@ -159,11 +159,15 @@ __device__ __forceinline__ float norm_back(float d, float n, float mean, float r
     return dim == 1 ? rs * d * (eps * rs * rs) : rs * fmaf(-n, mean, d);
 }
 
-// float32 results take the exponential and the division that are good to an ulp over the whole range.  Beside bf16 the fast ones
-// do: the exponential's error grows with its argument, to 1e-5 at the largest that is not an infinity, and the result is rounded
-// to 2e-3.
+// float32 results take the exponential that is good to an ulp over the whole range, of -|z| so that the quotient's divisor lies
+// between 1 and 2 (16384 x 16 rows of 128: 70 and 132 us, with the fast one 66 and 130, with a division of any size 72 and 141).
+// Beside bf16 the fast one does: its error grows with its argument, to 1e-5 at the largest that is not an infinity, and the result
+// is rounded to 2e-3.
 template <class T> __device__ __forceinline__ float sigmoid(float z);
-template <> __device__ __forceinline__ float sigmoid<float>(float z) { return 1.0f / (1.0f + expf(-z)); }
+template <> __device__ __forceinline__ float sigmoid<float>(float z) {
+    const float e = expf(-fabsf(z)), r = __fdividef(1.0f, 1.0f + e);
+    return z < 0.0f ? e * r : r;
+}
 template <> __device__ __forceinline__ float sigmoid<__nv_bfloat16>(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
 template <class T, int kVec, int kNv, int kRowThreads>
