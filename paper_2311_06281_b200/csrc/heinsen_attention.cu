@@ -190,10 +190,11 @@ bool encode(CUtensorMap* m, const View& v, long long batch, long long tokens) {
 
 // Segments of a sequence.  Fewer (batch, head) pairs than SMs leave the rest of the GPU idle, so a sequence is cut into as many
 // segments as there are SMs for; their states are formed first, from keys and values alone, and joined.  Measured at dimension
-// 128: one pass 15 us + 3.7 us a chunk, segments 34 us + 6.2 us for each chunk of a segment, 8 us where all SMs read at once.
-// (The states' part of a chunk took 3.2 us then; it takes 2.7 us now.)
-// So they are taken from about where they pay: 64 pairs never (64 chunks: 248 us whole, 257 us in two), 49 pairs of 16 chunks
-// not (74 us, in three 83 us) and of 32 (131 us, 120 us), 8 pairs of 4 chunks not (27 us, 38 us) and of 8 (41 us, 38 us).
+// 128 (and 64), whole against cut: 12 us + 3.9 us a chunk (9 + 3.2) against 35 us + 7 us for each chunk of a segment (29 + 5.5),
+// so a cut pays from chunks > 2 each + 5 at either width.  On both sides of that: 64 pairs of 64 chunks 261 us whole, 257 us in two
+// (213, 208; not cut); 49 pairs of 16 chunks 75 us, in three 79 us (61, 64; not cut) and of 32 133 us, 116 us (111, 93); 37 pairs
+// of 12 chunks 58 us, in four 59 us (48, 48); 16 pairs of 8 chunks 42 us, in eight 40 us (35, 36); 8 pairs of 6 chunks 34 us, in
+// six 38 us (29, 34; not cut) and of 8 42 us, 38 us (35, 32); 8 pairs of 64 chunks 246 us, in sixteen 63 us (211, 50).
 int segments_for(long long pairs, long long tokens, int sms) {
     const long long chunks = (tokens + ha::kChunk - 1) / ha::kChunk;
     const long long most = std::max(1ll, std::min(sms / std::max(1ll, pairs), chunks));
