@@ -15,6 +15,7 @@ import struct
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.graph import increment_version as _increment_version
 
 from .heinsen_scan import HeinsenScanError, _check, _dtype_code, _on_device, lib as _scan_lib  # noqa: F401
 
@@ -148,11 +149,16 @@ def _seen_by_autograd(*tensors) -> bool:
         for t in tensors:
             if t is not None and t.requires_grad:
                 return True
+    return _dual_level()
+
+
+def _dual_level() -> bool:
+    """May tensors have tangents at all?  (Asking each of them costs a microsecond.)"""
     return getattr(forward_ad, "_current_level", 0) >= 0
 
 
 def _no_tangents(name, *tensors):
-    if getattr(forward_ad, "_current_level", 0) >= 0 and any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+    if any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
         raise NotImplementedError(f"{name} has no forward-mode derivative")
 
 
@@ -347,18 +353,22 @@ def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
         raise ValueError("slots must be a contiguous int32 tensor [batch]")
     dev = q.device
     _on_gpu(q, "q")
+    written = state
     if out is None:
         out = torch.empty((b, h, vd), dtype=q.dtype, device=dev)
     elif tuple(out.shape) != (b, h, vd) or out.dtype is not q.dtype or b and out.stride(2) != 1 and vd > 1:
         raise ValueError("out must be [batch, heads, v_dim] of q's dtype, the last dimension contiguous")
+    else:
+        written = (state, out)
     _cuda("decay_attention_step", dev, k=k, v=v, log_a=log_a, state=state, slots=slots, out=out)
-    _no_tangents("decay_attention_step", q, k, v, log_a, state, out)
+    if _dual_level():
+        _no_tangents("decay_attention_step", q, k, v, log_a, state, out)
     ob, oh, _ = out.stride()
     packed = _PROBLEM.pack(b, 1, h, hq, hk, hv, kd, vd, _dtype(q), float(kd ** -0.5 if scale is None else scale),
                            q.data_ptr(), qb, 0, qh, k.data_ptr(), kb, 0, kh, v.data_ptr(), vb, 0, vh, log_a.data_ptr(), ab, 0, ah, 0, 0)
     _launch(dev, _call().step, packed, _ROWS.pack(out.data_ptr(), ob, 0, oh), state.data_ptr(), n, _addr(slots))
-    # autograd sees no address being written to: a graph that kept either of them has to notice
-    torch.autograd.graph.increment_version((state, out))
+    # autograd sees no address being written to: a graph that kept what has been has to notice
+    _increment_version(written)
     return out
 
 
