@@ -14,13 +14,13 @@
 // 24 bits, exact to float32's own rounding; P and the state in X S as one, where only the bf16 output depends on them (its own
 // rounding is as large).
 //
-// Measured, [8 x 2048 tokens, 16 heads of 128] (128 CTAs): forward and dv 75 us each, 268 MB at 3.6 TB/s; with kDots 150 us (dk)
-// and 169 us (dq).  Neither memory (55% of a copy's rate) nor the tensor core (31% of its cycles) bounds it: a chunk's steps wait
-// for each other, 7000 to 8000 clocks of them, and shared memory holds one CTA.  Of those the output's chain has: scores 520, P
-// 2000, X S 1100, scaling its rows 600, P Z 900, the output 760; the state's: Z^T 500, its terms 2400, the update 2000, reading
-// it 500, publishing it 500.  What did not help: the output from registers straight to memory (2200 clocks for 760), one warp that
-// watches the barriers of both chains (600 clocks from a barrier to the last of eight products), fewer registers for the rows of
-// the state (spills).
+// Measured, [8 x 2048 tokens, 16 heads of 128] (128 CTAs): forward and dv 77 us each, 268 MB at 3.5 TB/s; with kDots 157 us
+// (dk) and 172 us (dq), of which some is spills (64 to 96 bytes a thread; the other passes have none).  Neither memory (55% of
+// a copy's rate) nor the tensor core (31% of its cycles) bounds it: a chunk's steps wait for each other, 7000 to 8000 clocks of
+// them, and shared memory holds one CTA.  Of those the output's chain has: scores 520, P 2000, X S 1100, scaling its rows 600,
+// P Z 900, the output 760; the state's: Z^T 500, its terms 2400, the update 2000, reading it 500, publishing it 500.  What did
+// not help: the output from registers straight to memory (2200 clocks for 760), one warp that watches the barriers of both
+// chains (600 clocks from a barrier to the last of eight products), fewer registers for the rows of the state (spills).
 //
 // kDots: the pass also forms what the decay gradients need of it, in float32: the row sums of W = P o (w Z^T), w the fourth
 // tensor, from the unrounded P, and the dots w_i . (X S)_i, for which X S has the state in three terms.  Each W_ij comes out of

@@ -121,7 +121,8 @@ __device__ __forceinline__ void add4(float4& acc, float w, const float4& v) {
 // they compute: a 16-byte read of a warp costs it four turns, whatever is read twice.  So a thread has four columns of kPer
 // output rows and of four state rows, which share those reads (24 sequences of up to 1000 tokens, dimension 64: 69 us with one
 // row for 32 columns, 43 us with two for 64; the sums of the states before it 25 us and 16 us).  The next chunk's first 64
-// columns travel meanwhile: waiting for them took half of a chunk's time.
+// columns travel meanwhile: waiting for them took half of a chunk's time.  With an output a thread spills 52 to 68 bytes at the 128
+// registers that two CTAs leave it.
 template <class T, bool kRev, class OutT, bool kStateOnly, int kCols>
 __device__ __forceinline__ void simt_pass(const Pass& p) {
     constexpr int kLanes = kCols / 4, kSweep = kSimtThreads / kLanes, kPer = kSimtChunk / kSweep;

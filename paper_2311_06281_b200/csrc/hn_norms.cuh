@@ -4,9 +4,11 @@
 // that own the same columns of every row they see.
 //
 // Measured, bf16, and the time of the same bytes at a copy's rate: block, 16384 rows of 2048: forward 69 us (51), backward 154 us
-// (82); gated, 16384 x 16 rows of 128: forward 43 us (31), backward 69 us (51).  Between its loads and its stores a row waits for
-// two sums over its threads (three on the way back), each some 500 clocks: other rows of the SM have to cover that, and how many
-// fit is up to registers.
+// (82); gated, 16384 x 16 rows of 128: forward 43 us (31), backward 69 us (51); in float32 66 us (61) and 117 us (102).  Between its
+// loads and its stores a row waits for two sums over its threads (three on the way back), each some 500 clocks: other rows of the
+// SM have to cover that, and how many fit is up to registers.  The backward kernels are short of those: threads with 8 elements of a
+// row spill 32 to 84 bytes, rows of 8192 float32 240 bytes (one CTA of 512 threads to an SM: 209 us for 82), the widest rows
+// up to 1.4 KB.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
