@@ -14,6 +14,7 @@
  *     v [batch, tokens, v_heads, v_dim], o [batch, tokens, heads, v_dim], with the last dimension contiguous and the
  *     strides of the other three given in elements (batch, token, head).
  *   - heads is a multiple of q_heads, k_heads and v_heads; head h reads head h * q_heads / heads of q, and so on.
+ *   - Outputs do not overlap inputs, nor each other, but where it is said that they may.
  *   - States are float32, contiguous [.., heads, k_dim, v_dim]; decays are float32.
  *   - 1 <= k_dim, v_dim <= 256; batch, tokens, heads >= 0 with batch * tokens * heads * max(k_dim, v_dim) < 2^62 and
  *     tokens < 2^31 - 2^20, batch * heads < 2^31.
@@ -67,7 +68,8 @@ hs_status heinsen_attention_forward(const heinsen_attention_problem* p, const he
  * Nothing of the forward call is needed again.  Outputs, all contiguous: dq, dk, dv in the shapes of q, k, v (summed over the
  * heads that share a head), 16-byte aligned; dlog_a float32 [batch, tokens, heads], or [heads] where the decay is fixed (batch
  * and token stride 0); dstate0 float32.  dlog_a and dstate0 may be NULL.  Where d_state is given 1 / scale has to be finite.
- * Without sequences or heads, gradients that have elements all the same are zeros.  Asynchronous; workspace of heinsen_attention_workspace_bytes(p, 1) bytes.
+ * Without sequences or heads, gradients that have elements all the same are zeros.  Asynchronous; workspace of
+ * heinsen_attention_workspace_bytes(p, 1) bytes, checked as above.
  */
 hs_status heinsen_attention_backward(const heinsen_attention_problem* p, const heinsen_attention_tensor* d_o,
                                      const float* d_state, void* dq, void* dk, void* dv, float* dlog_a,
