@@ -46,7 +46,6 @@ constexpr int kFeedRegs = 80;
 constexpr int kRowRegs = 64, kStateRegs = 136;
 constexpr uint32_t kTile = 128 * 256;        // 128 rows of 128 bf16: two blocks of 64 columns, 128-byte swizzle
 constexpr uint32_t kBlock = kTile / 2;
-constexpr uint32_t kDrainSpin = 1u << 16;    // polls for what is still in flight when a CTA leaves (0.15 us each, measured)
 
 struct MmaPass {
     const float* log_a;
@@ -120,40 +119,6 @@ enum Bar : int { kFullX = 0, kFullY = 2, kFullZ = 4, kFreeX = 6, kFreeY = 8, kFr
 static_assert(kBars <= 40, "barriers");
 
 template <int kValue> struct Int { static constexpr int value = kValue; };
-
-// A thread whose wait has given up runs on without waiting (its warp's loads and stores of tensor memory need every lane), but
-// never arrives on a barrier again: nobody takes what it did not do for done, no barrier gets more arrivals in a phase than it
-// expects (one too many makes a fault), and the others' waits find `stop` set.
-struct Waiter {
-    uint32_t bars;
-    volatile int* stop;  // in shared memory: some wait of this CTA gave up
-    uint32_t limit;
-    __device__ __forceinline__ bool operator()(int bar, int turn) const {
-#pragma unroll 1
-        for (uint32_t i = 0; i < limit; ++i) {
-            if (bar_try(bars + 8 * bar, turn & 1)) return true;
-            if (*stop) return false;
-        }
-        *stop = 1 + bar;
-        return false;
-    }
-    // What this thread has in flight on a barrier lands before it leaves, whoever has given up meanwhile.
-    __device__ __forceinline__ void drain(int bar, int turn) const {
-#pragma unroll 1
-        for (uint32_t i = 0; i < kDrainSpin && !bar_try(bars + 8 * bar, turn & 1); ++i) {}
-    }
-};
-
-// A pair of values as kTerms bf16 pairs whose sum is the pair.
-template <int kTerms>
-__device__ __forceinline__ void split(pair v, uint32_t (&t)[kTerms]) {
-    t[0] = pack_bf16(v);
-#pragma unroll
-    for (int i = 1; i < kTerms; ++i) {
-        v = minus_bf16(v, t[i - 1]);
-        t[i] = pack_bf16(v);
-    }
-}
 
 // sum + the products of sixteen float32 values and sixteen bf16
 __device__ __forceinline__ pair add_dot(pair sum, const uint32_t (&v)[16], const uint4& lo, const uint4& hi) {

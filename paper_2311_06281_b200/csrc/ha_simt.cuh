@@ -20,29 +20,12 @@
 //     j before, i behind         e^{c_C} <S, D>
 // No term cancels another.  The two passes leave S and D of every chunk behind for it.
 #pragma once
-#include <cuda_bf16.h>
-#include <cuda_runtime.h>
-#include <stdint.h>
+#include "ha_common.cuh"
 
 namespace ha {
 
-constexpr float kLog2e = 1.4426950408889634f;
-// A log decay below this is a reset: e^-10000 is zero in float32 by a wide margin, and clamping -inf to it keeps every
-// difference of sums finite.  (x < kReset keeps NaN.)
-constexpr float kReset = -1.0e4f;
 constexpr int kSimtChunk = 32;   // tokens of a chunk
 constexpr int kSimtThreads = 256;
-
-struct Rows {  // [batch, tokens, heads', dim] with a contiguous last dimension, strides in elements
-    const void* ptr;
-    long long sb, st, sh;
-    int div;  // head h reads head h / div
-};
-
-struct Fault {  // the header that heinsen_scan_check() reads
-    unsigned long long started_id, error_id;
-    int error_code, error_where;
-};
 
 struct Pass {
     Rows x, y, z;
@@ -70,26 +53,6 @@ struct Pass {
 struct Passes {
     Pass p[3];
 };
-
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float to_f(float v) { return v; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <class T> __device__ __forceinline__ T from_f(float v);
-template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-
-__device__ __forceinline__ int live_tokens(const int* lengths, int b, int tokens) {
-    if (!lengths) return tokens;
-    const int n = lengths[b];
-    return n < 0 ? 0 : (n > tokens ? tokens : n);
-}
-
-// d * s without 0 * inf: a decay of zero forgets the state whatever it holds
-__device__ __forceinline__ float decayed(float d, float s) { return d == 0.0f ? 0.0f : d * s; }
 
 // Columns c0 + lane + 32 u (u < kN) of a warp's four of the rows t0 .. t0 + 31, zeros where there is nothing; and their way to
 // shared memory.
