@@ -1,0 +1,144 @@
+// What the forward and the backward pass of the delta rule share on the host.
+#pragma once
+#include <cstring>
+
+#include "../../include/heinsen_delta.h"
+#include "ha_host.h"
+#include "hd_scan.cuh"
+
+#ifndef HD_MID
+#define HD_MID 3
+#endif
+namespace hd_host {
+
+using namespace ha_host;
+
+#pragma GCC visibility push(hidden)
+// The word of the current device that says where a bounded wait of any call ran out; NULL where CUDA fails.
+int* gave_up_word();
+size_t backward_bytes(const heinsen_delta_problem* p);
+#pragma GCC visibility pop
+
+constexpr int kSms = 148;  // B200; sizes the grid and workspaces the same wherever they are asked for
+
+inline int width_of(int dk) { return dk <= 64 ? 64 : dk <= 128 ? 128 : 256; }
+
+struct View {  // one [batch, tokens, heads', dim] tensor
+    Rows rows;
+    int own_heads, dim;
+};
+inline View view_of(const heinsen_attention_tensor& t, int heads, int own, int dim) { return {rows_of(t, heads, own), own, dim}; }
+
+// Can TMA address it?  bf16, 16-byte base and strides; a stride of a dimension of one is never used.
+inline bool tma_strides(const View& v, long long batch, long long tokens) {
+    const long long s[3] = {v.own_heads > 1 ? v.rows.sh : 8, tokens > 1 ? v.rows.st : 8, batch > 1 ? v.rows.sb : 8};
+    for (long long x : s)
+        if (x <= 0 || x % 8 || x >= (1ll << 38)) return false;
+    return v.dim % 8 == 0 && (reinterpret_cast<uintptr_t>(v.rows.ptr) & 15u) == 0;
+}
+inline bool encode(CUtensorMap* m, const View& v, long long batch, long long tokens, int columns, int rows) {
+    const EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)v.dim, (cuuint64_t)v.own_heads, (cuuint64_t)tokens, (cuuint64_t)batch};
+    const cuuint64_t any = 256;
+    const cuuint64_t strides[3] = {v.own_heads > 1 ? (cuuint64_t)v.rows.sh * 2 : any, tokens > 1 ? (cuuint64_t)v.rows.st * 2 : any,
+                                   batch > 1 ? (cuuint64_t)v.rows.sb * 2 : any};
+    const cuuint32_t box[4] = {(cuuint32_t)columns, 1, (cuuint32_t)rows, 1}, one[4] = {1, 1, 1, 1};
+    for (int again = 0;; ++again) {
+        const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(v.rows.ptr), dims, strides, box, one,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, columns == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_32B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r == CUDA_SUCCESS || again) return r == CUDA_SUCCESS;
+        cudaFree(nullptr);  // a thread that has made no runtime call yet has no context for the driver's
+    }
+}
+
+// Bytes of a tensor laid out as bf16 terms for TMA; 0 where it is loaded as it is.
+inline size_t terms_bytes(const heinsen_attention_problem* p, const View& v) {
+    if (p->tokens == 0 || (p->dtype == HS_BF16 && tma_strides(v, p->batch, p->tokens))) return 0;
+    return up256((size_t)(p->dtype == HS_F32 ? 3 : 1) * p->batch * p->tokens * v.own_heads * ((v.dim + 7) / 8 * 8) * 2);
+}
+// The tensor map of a tensor, through `space` where it has to be laid out anew.
+template <class T, int TI>
+hs_status map_of(CUtensorMap* m, const heinsen_attention_problem* p, const View& v, uint8_t* space, int columns, int rows, cudaStream_t stream) {
+    View w = v;
+    if (terms_bytes(p, v)) {
+        const int width = (v.dim + 7) / 8 * 8;
+        const long long total = p->batch * p->tokens * v.own_heads * width;
+        hd::terms_kernel<TI, T><<<(unsigned)std::min<long long>((total + 255) / 256, kSms * 16), 256, 0, stream>>>(
+            v.rows, reinterpret_cast<__nv_bfloat16*>(space), (int)p->tokens, v.own_heads, v.dim, width, total);
+        const hs_status st = launched("terms_kernel");
+        if (st != HS_OK) return st;
+        const long long sh = width, stk = sh * v.own_heads;
+        w = {{space, stk * p->tokens, stk, sh, 1}, v.own_heads, width};
+    }
+    if (!encode(m, w, p->batch * TI, p->tokens, columns, rows)) return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
+    return HS_OK;
+}
+
+inline hd::Params params_of(const heinsen_delta_problem* dp, int chunk, uint8_t* ws) {
+    const heinsen_attention_problem* p = &dp->a;
+    hd::Params q;
+    std::memset(&q, 0, sizeof q);
+    q.log_a = static_cast<const float*>(p->log_a.ptr);
+    q.ab = p->log_a.batch_stride; q.at = p->log_a.token_stride; q.ah = p->log_a.head_stride;
+    q.beta = static_cast<const float*>(dp->beta.ptr);
+    q.bb = dp->beta.batch_stride; q.bt = dp->beta.token_stride; q.bh = dp->beta.head_stride;
+    q.lengths = p->lengths;
+    q.batch = (int)p->batch; q.tokens = (int)p->tokens; q.heads = p->heads;
+    q.chunks = (int)((p->tokens + chunk - 1) / chunk);
+    q.qdiv = p->heads / p->q_heads; q.kdiv = p->heads / p->k_heads; q.vdiv = p->heads / p->v_heads;
+    q.dk = p->k_dim; q.dv = p->v_dim;
+    q.scale = p->scale;
+    q.fault = reinterpret_cast<ha::Fault*>(ws);
+    q.call_id = hs_internal::call_id();
+    q.spin = hs_internal::spin_limit();
+    q.mute = (int)std::min<long long>(hs_internal::mute_tile(), 0x7fffffff);
+    return q;
+}
+
+inline long long chunks_of(const heinsen_attention_problem* p) {
+    const int c = hd::chunk_tokens(width_of(p->k_dim));
+    return p->batch * p->heads * ((p->tokens + c - 1) / c);
+}
+template <int C, int TM, int TP> size_t image_bytes(const heinsen_attention_problem* p) { return up256((size_t)chunks_of(p) * hd::Image<C, TM, TP>::end); }
+
+// Warps of a CTA of the scans, sixteen columns each: as many as one SM can have while there are CTAs for all SMs, since a CTA
+// loads K, Q, N and P for all of its warps.
+inline int warps_for(long long pairs, int slices) {
+    int warps = hd::kMaxWarps;
+    while (warps > 1 && (warps >= 2 * slices || (pairs * ((slices + warps - 1) / warps) <= kSms / 2))) warps /= 2;
+    return warps;
+}
+
+template <int KP, int C, int TI, int TM, int TP>
+hs_status launch_chunks(const CUtensorMap& mq, const CUtensorMap& mk, const hd::Params& q, int* word, cudaStream_t stream) {
+    using L = hd::ChunkLayout<KP, C, TI, TM, TP>;
+    const auto fn = hd::chunk_kernel<KP, C, TI, TM, TP>;
+    static std::atomic<unsigned long long> done{0};
+    const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end, done);
+    if (st != HS_OK) return st;
+    fn<<<(unsigned)((long long)q.batch * q.heads * q.chunks), 2 * C, L::end, stream>>>(mq, mk, q, word);
+    return launched("chunk_kernel");
+}
+
+template <int KP, int C, int TI, int TM, int TP, bool kOut, class T>
+hs_status launch_scan(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo, const hd::Params& q, int* word,
+                      cudaStream_t stream) {
+    using L = hd::ScanLayout<KP, C, TI, TM, TP, kOut>;
+    static_assert(L::end(hd::kMaxWarps) <= 232448, "shared memory");
+    const auto fn = hd::scan_kernel<KP, C, TI, TM, TP, kOut, T>;
+    static std::atomic<unsigned long long> done{0};
+    const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end(hd::kMaxWarps), done);
+    if (st != HS_OK) return st;
+    const long long pairs = (long long)q.batch * q.heads;
+    const int slices = (q.dv + 15) / 16, warps = warps_for(pairs, slices);
+    const long long grid = pairs * ((slices + warps - 1) / warps);
+    if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
+    hd::Params w = q;
+    w.warps = warps;
+    fn<<<(unsigned)grid, 32 * (hd::loader_of(warps) + 4), L::end(warps), stream>>>(mq, mk, mv, mo, w, word);
+    return launched("scan_kernel");
+}
+
+}  // namespace hd_host

@@ -318,14 +318,8 @@ def decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: to
     return _attention_forward(_problem(q, k, v, log_a, state0, scale, lengths), q, workspace)
 
 
-def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: torch.Tensor, state: torch.Tensor, *,
-                         scale: float | None = None, slots: torch.Tensor | None = None,
-                         out: torch.Tensor | None = None) -> torch.Tensor:
-    """One token for each sequence: updates ``state`` in place and returns o [B, H, V].  Asynchronous, not differentiable.
-
-    q [B, Hq, K], k [B, Hk, K], v [B, Hv, V]; log_a float32 [B, H] or [H]; state float32 [N, H, K, V], of which sequence b
-    uses row slots[b] (int32; negative or >= N: no state, o is zero), or row b.  No two sequences may share a row.
-    """
+def _step_problem(name, q, k, v, log_a, state, scale, slots, out):
+    """The checks of a one-token call; returns the packed problem, the output, and what the call writes."""
     if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
         raise ValueError("q, k, v are [batch, heads, dim]")
     b, hq, kd = q.shape
@@ -363,13 +357,25 @@ def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_
         raise ValueError("out must be [batch, heads, v_dim] of q's dtype, the last dimension contiguous")
     else:
         written = (state, out)
-    _cuda("decay_attention_step", dev, k=k, v=v, log_a=log_a, state=state, slots=slots, out=out)
+    _cuda(name, dev, k=k, v=v, log_a=log_a, state=state, slots=slots, out=out)
+    packed = _PROBLEM.pack(b, 1, h, hq, hk, hv, kd, vd, _dtype(q), float(kd ** -0.5 if scale is None else scale),
+                           q.data_ptr(), qb, 0, qh, k.data_ptr(), kb, 0, kh, v.data_ptr(), vb, 0, vh, log_a.data_ptr(), ab, 0, ah, 0, 0)
+    return packed, out, written
+
+
+def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: torch.Tensor, state: torch.Tensor, *,
+                         scale: float | None = None, slots: torch.Tensor | None = None,
+                         out: torch.Tensor | None = None) -> torch.Tensor:
+    """One token for each sequence: updates ``state`` in place and returns o [B, H, V].  Asynchronous, not differentiable.
+
+    q [B, Hq, K], k [B, Hk, K], v [B, Hv, V]; log_a float32 [B, H] or [H]; state float32 [N, H, K, V], of which sequence b
+    uses row slots[b] (int32; negative or >= N: no state, o is zero), or row b.  No two sequences may share a row.
+    """
+    packed, out, written = _step_problem("decay_attention_step", q, k, v, log_a, state, scale, slots, out)
     if _dual_level():
         _no_tangents("decay_attention_step", q, k, v, log_a, state, out)
     ob, oh, _ = out.stride()
-    packed = _PROBLEM.pack(b, 1, h, hq, hk, hv, kd, vd, _dtype(q), float(kd ** -0.5 if scale is None else scale),
-                           q.data_ptr(), qb, 0, qh, k.data_ptr(), kb, 0, kh, v.data_ptr(), vb, 0, vh, log_a.data_ptr(), ab, 0, ah, 0, 0)
-    _launch(dev, _call().step, packed, _ROWS.pack(out.data_ptr(), ob, 0, oh), state.data_ptr(), n, _addr(slots))
+    _launch(q.device, _call().step, packed, _ROWS.pack(out.data_ptr(), ob, 0, oh), state.data_ptr(), state.shape[0], _addr(slots))
     # autograd sees no address being written to: a graph that kept what has been has to notice
     _increment_version(written)
     return out
