@@ -1,0 +1,394 @@
+// Beam search: the best continuations of a group of beams, and the states that follow them.
+//
+// Within a beam the candidates' order is that of its logits, so a row of logits is read once: a CTA has a part of a row in
+// registers, forms its largest value, the sum of the exponentials over that, and its `keep` largest logits; a CTA for each group
+// joins the parts' sums to the beams' log-sums and picks from the parts' lists.  Bound by reading the logits.
+#pragma once
+#include "ha_common.cuh"
+
+namespace hb {
+
+constexpr int kThreads = 256;
+constexpr int kMaxKeep = 64;
+constexpr int kList = 256;  // candidates of a part that are sorted at once
+
+struct Select {
+    const void* logits;
+    long long sb, sw;  // strides of batch and beam
+    long long vocabulary;
+    int beams, keep, parts;
+    const float* scores;
+    const uint8_t* ended;
+    long long end_token;
+    float* part_value;   // [rows][parts][keep]
+    int* part_token;
+    double2* part_sum;   // [rows][parts]: largest value, sum of the exponentials
+    float* out_scores;
+    int *out_parents, *out_tokens;
+};
+
+// Numbers in the order of their size as unsigned ones
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+
+// One part of one row; kPer logits a thread, in vectors of 16 bytes at addresses of 16 bytes: part 0 begins at the last such address
+// at or before the row's first logit.
+template <class T, int kPer>
+__global__ void __launch_bounds__(kThreads) part_kernel(const Select p) {
+    constexpr int kVec = 16 / sizeof(T), kVecs = kPer / kVec;
+    __shared__ float red_max[kThreads / 32];
+    __shared__ double red_sum[kThreads / 32];
+    __shared__ __align__(16) uint32_t tops[kThreads];
+    __shared__ uint32_t least;
+    __shared__ uint32_t list_key[kList];
+    __shared__ int list_token[kList];
+    __shared__ int found;
+    __shared__ unsigned long long best[kThreads / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int part = blockIdx.x % p.parts;
+    const long long row = blockIdx.x / p.parts, b = row / p.beams, w = row % p.beams;
+    const T* const from = static_cast<const T*>(p.logits) + b * p.sb + w * p.sw;
+    const int ahead = (int)((reinterpret_cast<uintptr_t>(from) & 15u) / sizeof(T));
+    const long long first = (long long)part * (kThreads * kPer) - ahead;
+    if (tid == 0) found = 0;
+    if (p.ended && p.ended[row]) return;  // nothing of it is asked for
+    float x[kPer];
+    auto token = [&](int i) { return first + ((long long)(i / kVec) * kThreads + tid) * kVec + i % kVec; };
+#pragma unroll
+    for (int u = 0; u < kVecs; ++u) {
+        const long long n = token(u * kVec);
+        if (n >= 0 && n + kVec <= p.vocabulary) {
+            const uint4 f = __ldcs(reinterpret_cast<const uint4*>(from + n));
+            const uint32_t r[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                if constexpr (sizeof(T) == 2) x[u * kVec + i] = __uint_as_float(i & 1 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
+                else x[u * kVec + i] = __uint_as_float(r[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) x[u * kVec + i] = n + i >= 0 && n + i < p.vocabulary ? ha::to_f(from[n + i]) : __int_as_float(0xff800000);
+        }
+    }
+    float top = x[0];
+    bool odd = x[0] != x[0];
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) {
+        top = fmaxf(top, x[i]);
+        odd |= x[i] != x[i];
+    }
+    // The keep-th largest of the maxima of disjoint groups (8 lanes each; single threads where more than 16 are asked for) bounds the
+    // keep-th best of the part from below, and few logits lie above it.
+    const bool few = p.keep <= 16;
+    float m = top;
+#pragma unroll
+    for (int o = 1; o < 8; o *= 2) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    if (!few) tops[tid] = ordered(top);
+    else if ((lane & 7) == 0) tops[warp * 4 + (lane >> 3)] = ordered(m);
+    m = fmaxf(m, __shfl_xor_sync(~0u, m, 8));
+    m = fmaxf(m, __shfl_xor_sync(~0u, m, 16));
+    if (lane == 0) red_max[warp] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, red_max[i]);
+    float part_sum = 0.0f;  // (m - m is NaN for an infinite m)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) part_sum += ha::ex2((x[i] - m) * ha::kLog2e);
+    double sum = (double)part_sum;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    if (lane == 0) red_sum[warp] = sum;
+    odd = __syncthreads_or(odd);
+    const long long at = row * p.parts + part;
+    if (tid == 0) {
+        sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kThreads / 32; ++i) sum += red_sum[i];
+        p.part_sum[at] = make_double2((double)m, odd ? (double)__int_as_float(0x7fc00000) : m == __int_as_float(0xff800000) ? 0.0 : sum);
+    }
+    float* const values = p.part_value + at * p.keep;
+    int* const tokens = p.part_token + at * p.keep;
+    if (few) {
+        const uint32_t own = tops[lane];
+        int above = 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const uint32_t other = __shfl_sync(~0u, own, i);
+            above += other > own || (other == own && i < lane);
+        }
+        if (warp == 0 && above == p.keep - 1) least = own;
+    } else {
+        const uint32_t own = tops[tid];
+        int above = 0;
+#pragma unroll 8
+        for (int i = 0; i < kThreads; i += 4) {
+            const uint4 other = *reinterpret_cast<const uint4*>(tops + i);
+            above += (other.x > own || (other.x == own && i < tid)) + (other.y > own || (other.y == own && i + 1 < tid)) +
+                     (other.z > own || (other.z == own && i + 2 < tid)) + (other.w > own || (other.w == own && i + 3 < tid));
+        }
+        if (above == p.keep - 1) least = own;
+    }
+    __syncthreads();
+    const float bound = from_ordered(least);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const long long n = token(i);
+        if (x[i] >= bound && n >= 0 && n < p.vocabulary) {
+            const int to = atomicAdd(&found, 1);
+            if (to < kList) {
+                list_key[to] = ordered(x[i]);
+                list_token[to] = (int)n;
+            }
+        }
+    }
+    __syncthreads();
+    const int count = found;
+    if (count <= kList) {  // sorted by value and place: the order in which they came does not matter
+        if (tid < count) {
+            const uint32_t key = list_key[tid];
+            const int n = list_token[tid];
+            int rank = 0;
+            for (int i = 0; i < count; ++i) rank += list_key[i] > key || (list_key[i] == key && list_token[i] < n);
+            if (rank < p.keep) {
+                values[rank] = from_ordered(key);
+                tokens[rank] = n;
+            }
+        }
+        for (int i = count + tid; i < p.keep; i += kThreads) tokens[i] = -1;  // the part holds fewer
+    } else {  // many equal ones
+        // one after the other: the best of those that come after the last one in the order (value, then place)
+        unsigned long long last = ~0ull;
+        for (int k = 0; k < p.keep; ++k) {
+            unsigned long long mine = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const long long n = token(i);
+                const unsigned long long key = (unsigned long long)ordered(x[i]) << 32 | (uint32_t)~(uint32_t)n;
+                if (n >= 0 && n < p.vocabulary && key < last && key > mine) mine = key;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                const unsigned long long other = __shfl_xor_sync(~0u, mine, o);
+                mine = other > mine ? other : mine;
+            }
+            __syncthreads();
+            if (lane == 0) best[warp] = mine;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kThreads / 32; ++i) mine = best[i] > mine ? best[i] : mine;
+            last = mine;
+            if (tid == 0) {
+                values[k] = from_ordered((uint32_t)(mine >> 32));
+                tokens[k] = mine ? (int)~(uint32_t)mine : -1;
+            }
+            if (!mine) last = 0;
+        }
+    }
+}
+
+// The best of a group.  Candidates are formed in 64 bits; as above, the keep-th best of the threads' own best bounds the keep-th best
+// of all, and those above it are sorted.
+constexpr int kJoinList = 512;
+__global__ void __launch_bounds__(kThreads) join_kernel(const Select p) {
+    __shared__ double logs[64];
+    __shared__ int state[64];  // 0: as its logits say; 1: ended; 2: out
+    __shared__ double value_of[kJoinList];
+    __shared__ long long place_of[kJoinList];
+    __shared__ double least_value;
+    __shared__ long long least_place;
+    __shared__ int found;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const long long b = blockIdx.x, nowhere = 0x7fffffffffffffffll;
+    const double lowest = -__longlong_as_double(0x7ff0000000000000ll);
+    if (tid == 0) found = 0;
+    for (int w = warp; w < p.beams; w += kThreads / 32) {
+        const long long row = b * p.beams + w;
+        const float score = p.scores[row];
+        const bool ended = p.ended && p.ended[row];
+        double m = lowest, s = 0.0;
+        if (!ended) {
+            for (int i = lane; i < p.parts; i += 32) m = fmax(m, p.part_sum[row * p.parts + i].x);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(~0u, m, o));
+            for (int i = lane; i < p.parts; i += 32) {
+                const double2 f = p.part_sum[row * p.parts + i];
+                s += f.x == m || f.x == lowest ? f.y : f.y * exp(f.x - m);
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+        }
+        const double l = m + log(s);
+        if (lane == 0) {
+            logs[w] = (double)score - l;
+            state[w] = !isfinite(score) ? 2 : ended ? 1 : isfinite(l) ? 0 : 2;
+        }
+    }
+    __syncthreads();
+    const int lists = p.parts * p.keep, each = lists + 2, total = p.beams * each;
+    // Of a beam without candidates of its own the first tokens count, at -inf, as many as could be needed.
+    auto candidate = [&](int c, double& value, long long& place) {
+        const int w = c / each, i = c - w * each;
+        value = lowest;
+        place = nowhere;
+        long long n = -1;
+        if (state[w] == 0) {
+            if (i < lists) {
+                const long long at = (b * p.beams + w) * lists + i;
+                n = p.part_token[at];
+                if (n >= 0) value = logs[w] + (double)p.part_value[at];
+            }
+        } else if (i == lists + 1) {
+            if (state[w] == 1) {
+                n = p.end_token;
+                value = (double)p.scores[b * p.beams + w];
+            }
+        } else if (i <= p.keep && i < p.vocabulary && !(state[w] == 1 && i == p.end_token)) {
+            n = i;
+        }
+        if (n >= 0) place = (long long)w * p.vocabulary + n;
+    };
+    auto before = [](double v, long long at, double u, long long other) { return v > u || (v == u && at < other); };
+    double value = lowest;
+    long long place = nowhere;
+    for (int c = tid; c < total; c += kThreads) {
+        double v;
+        long long at;
+        candidate(c, v, at);
+        if (before(v, at, value, place)) {
+            value = v;
+            place = at;
+        }
+    }
+    value_of[tid] = value;
+    place_of[tid] = place;
+    __syncthreads();
+    int rank = 0;
+    for (int i = 0; i < kThreads; ++i) rank += before(value_of[i], place_of[i], value, place) || (place_of[i] == place && i < tid);
+    if (rank == p.keep - 1) {
+        least_value = value;
+        least_place = place;
+    }
+    __syncthreads();
+    const double bound = least_value;
+    const long long bound_place = least_place;
+    for (int c = tid; c < total; c += kThreads) {
+        double v;
+        long long at;
+        candidate(c, v, at);
+        if (at != nowhere && !before(bound, bound_place, v, at)) {
+            const int to = atomicAdd(&found, 1);
+            if (to < kJoinList) {
+                value_of[to] = v;
+                place_of[to] = at;
+            }
+        }
+    }
+    __syncthreads();
+    const int count = found;
+    auto put = [&](int k, double v, long long at) {
+        const long long to = b * p.keep + k;
+        p.out_scores[to] = (float)v;
+        p.out_parents[to] = (int)(at / p.vocabulary);
+        p.out_tokens[to] = (int)(at % p.vocabulary);
+    };
+    if (count <= kJoinList) {
+        for (int c = tid; c < count; c += kThreads) {
+            const double v = value_of[c];
+            const long long at = place_of[c];
+            int r = 0;
+            for (int i = 0; i < count; ++i) r += before(value_of[i], place_of[i], v, at);
+            if (r < p.keep) put(r, v, at);
+        }
+        return;
+    }
+    // more than the list holds (places are all different, so this takes one thread with very many good ones): one after the other
+    double last_value = -lowest;
+    long long last_place = -1;
+    for (int k = 0; k < p.keep; ++k) {
+        value = lowest;
+        place = nowhere;
+        for (int c = tid; c < total; c += kThreads) {
+            double v;
+            long long at;
+            candidate(c, v, at);
+            if (at != nowhere && before(last_value, last_place, v, at) && before(v, at, value, place)) {
+                value = v;
+                place = at;
+            }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            const double v = __shfl_xor_sync(~0u, value, o);
+            const long long at = __shfl_xor_sync(~0u, place, o);
+            if (before(v, at, value, place)) {
+                value = v;
+                place = at;
+            }
+        }
+        __syncthreads();
+        if (lane == 0) {
+            value_of[warp] = value;
+            place_of[warp] = place;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kThreads / 32; ++i)
+            if (before(value_of[i], place_of[i], value, place)) {
+                value = value_of[i];
+                place = place_of[i];
+            }
+        last_value = value;
+        last_place = place;
+        if (tid == 0) put(k, value, place);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------- states
+
+struct Reorder {
+    uint8_t* state;
+    long long pool, row_bytes;
+    const int *parents, *slots;
+    int beams, tiles;
+};
+
+// A CTA has a piece of the rows of one group: every thread reads its unit of all rows that move before it writes any.  Bound by
+// the two trips of the rows that move.
+template <class Unit, int kBeams>
+__global__ void __launch_bounds__(kThreads) reorder_kernel(const Reorder p) {
+    __shared__ long long from[kBeams], to[kBeams];
+    const int tid = threadIdx.x, tile = blockIdx.x % p.tiles;
+    const long long b = blockIdx.x / p.tiles;
+    if (tid < kBeams) {
+        long long source = -1, target = -1;
+        if (tid < p.beams) {
+            auto slot = [&](int w) {
+                const long long s = p.slots ? (long long)p.slots[b * p.beams + w] : b * p.beams + w;
+                return s < 0 || s >= p.pool ? -1 : s;
+            };
+            const int parent = p.parents[b * p.beams + tid];
+            if (parent >= 0 && parent < p.beams) {
+                source = slot(parent);
+                target = slot(tid);
+            }
+            if (source < 0 || target < 0 || source == target) source = target = -1;
+        }
+        from[tid] = source < 0 ? -1 : source * p.row_bytes;
+        to[tid] = target * p.row_bytes;
+    }
+    __syncthreads();
+    const long long at = ((long long)tile * kThreads + tid) * sizeof(Unit);
+    if (at >= p.row_bytes) return;
+    Unit held[kBeams];
+#pragma unroll
+    for (int w = 0; w < kBeams; ++w)
+        if (from[w] >= 0) held[w] = *reinterpret_cast<const Unit*>(p.state + from[w] + at);
+#pragma unroll
+    for (int w = 0; w < kBeams; ++w)
+        if (from[w] >= 0) *reinterpret_cast<Unit*>(p.state + to[w] + at) = held[w];
+}
+
+}  // namespace hb
