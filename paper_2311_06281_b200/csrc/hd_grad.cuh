@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int u = 0; u < TP; ++u)
-                            if (g < pairs) load4_t(bf[g][u], P + u * I::plane + place<2 * C>(16 * jj + at.bt_row(), 2 * (np + g) + at.bt_piece()));
+                            if (g < pairs) load4_t(bf[g][u], P + u * I::plane + block_place(jj, np + g, at.bt_row(), at.bt_piece()));
                     sum<kRounded, kLevel>(y + 2 * np, a, bf, pairs);
                 }
             }
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int u = 0; u < TM; ++u)
-                            if (g < pairs) load4_t(bf[g][u], N + u * I::plane + place<2 * C>(16 * jj + at.bt_row(), 2 * (np + g) + at.bt_piece()));
+                            if (g < pairs) load4_t(bf[g][u], N + u * I::plane + block_place(jj, np + g, at.bt_row(), at.bt_piece()));
                     sum<kRounded, kLevel>(y + 2 * np, a, bf, pairs);
                 }
             }
@@ -247,9 +247,118 @@ struct GradLayout {
     static constexpr uint32_t slab = 2 * tile, g = slab, own = C * 32, v = g + SL / 16 * TI * own, z = v + TM * SL * C * 2, s = z + TM * SL * C * 2,
                               d = s + TM * SL * KP * 2, slab_end = d + TD * SL * KP * 2;
     static constexpr uint32_t plane = C * C * 2, hd = slab, hz = hd + TH * plane, w = hz + TH * plane, h_end = w + C * (C + 1) * 4;
-    static constexpr uint32_t vec = (slab_end > h_end ? slab_end : h_end), far = vec + 5 * C * 4 + 128, sums = far + 8 * C * 4, bars = sums + 64 * 4,
+    static constexpr uint32_t vec = (slab_end > h_end ? slab_end : h_end), far = vec + 6 * C * 4 + 128, sums = far + 8 * C * 4, bars = sums + 64 * 4,
                               end = bars + 64;
 };
+
+// Columns c and c + 1 of a row of a gradient, of which `left` are left; float32 where the heads' rows are summed later.
+template <class T>
+__device__ __forceinline__ void put_pair(void* to, int each, long long at, int left, float x, float y) {
+    if (each) {
+        float* g = static_cast<float*>(to) + at;
+        if (left > 0) g[0] = x;
+        if (left > 1) g[1] = y;
+    } else {
+        T* g = static_cast<T*>(to) + at;
+        if (left > 0) g[0] = ha::from_f<T>(x);
+        if (left > 1) g[1] = ha::from_f<T>(y);
+    }
+}
+
+// A chunk without a token of the sequence: zeros
+template <int C, class T, int kThreads>
+__device__ __forceinline__ void empty_chunk(const Params& p, long long row0, int t0, int chunk) {
+    const int tid = threadIdx.x, pairs = (p.dk + 1) / 2;
+    for (int e = tid; e < C * pairs; e += kThreads)
+        if (t0 + e / pairs < p.tokens) {
+            const int c = 2 * (e % pairs);
+            const long long to = (row0 + (long long)(e / pairs) * p.heads) * p.dk + c;
+            put_pair<T>(p.dq, p.each_q, to, p.dk - c, 0.0f, 0.0f);
+            put_pair<T>(p.dk_out, p.each_k, to, p.dk - c, 0.0f, 0.0f);
+        }
+    if (tid < C && t0 + tid < p.tokens) {
+        if (p.dlog_a) p.dlog_a[row0 + (long long)tid * p.heads] = 0.0f;
+        if (p.dbeta) p.dbeta[row0 + (long long)tid * p.heads] = 0.0f;
+    }
+    if (tid == 0 && p.part) p.part[chunk] = 0.0;
+}
+
+// The gradients of beta and log a of a chunk.  `far`: kParts parts of far_i for each token, then room for C / 16 of as many; `sums`: the
+// warps' parts of <S, D>; `wm`: W, C rows of C + 1.
+template <int C, class I, int kParts>
+__device__ __forceinline__ void gate_gradients(const Params& p, const float* vec, float* far, float* sums, float* wm, long long row0, int t0, int live, int slices) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const float* const dots = p.dots + (long long)blockIdx.x * 2 * slices * C;
+    float db = 0.0f, dl = 0.0f;
+    if (tid < C)
+        for (int v = 0; v < slices; ++v) {
+            db += dots[v * C + tid];
+            dl += dots[(slices + v) * C + tid];
+        }
+    if (tid < C && p.dbeta && t0 + tid < p.tokens) p.dbeta[row0 + (long long)tid * p.heads] = t0 + tid < live ? db : 0.0f;
+    if (!p.dlog_a && !p.part) return;
+    __syncthreads();  // W is there
+    // sum_{i>=t>j} W_ij: sums up each column by parts of 16 rows, then along the rows
+    float* const tops = far + kParts * C;  // of each part and column (the rest of `far`)
+    static_assert((kParts + C / 16) * C <= 8 * C, "scratch");
+    for (int e = tid; e < C * (C / 16); e += kGradThreads) {
+        const int j = e % C, part = e / C;
+        float x = 0.0f;
+#pragma unroll
+        for (int i = 15; i >= 0; --i) {
+            float& w = wm[(16 * part + i) * (C + 1) + j];
+            x += 16 * part + i > j ? w : 0.0f;
+            w = x;
+        }
+        tops[part * C + j] = x;
+    }
+    __syncthreads();
+    float g = 0.0f;
+    if (tid < 4 * C) {
+        const int t = tid >> 2, quarter = tid & 3;  // a quarter of the columns before t
+        for (int j = quarter; j < t; j += 4) {
+            float x = wm[t * (C + 1) + j];
+            for (int part = (t >> 4) + 1; part < C / 16; ++part) x += tops[part * C + j];
+            g += x;
+        }
+        g += __shfl_xor_sync(~0u, g, 1);
+        g += __shfl_xor_sync(~0u, g, 2);
+    }
+    __syncthreads();
+    if (tid < 4 * C && (tid & 3) == 0) wm[tid >> 2] = g;
+    if (tid < C) {
+        float f = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kParts; ++c) f += far[c * C + tid];
+        wm[C + tid] = f;       // far
+        wm[2 * C + tid] = dl;  // late
+    }
+    __syncthreads();
+    if (tid < C) {
+        float x = wm[tid], all = 0.0f;
+        for (int i = C - 1; i >= tid; --i) x += wm[C + i];
+        for (int j = 0; j < tid; ++j) x += wm[2 * C + j];
+        for (int w = 0; w < kGradThreads / 32; ++w) all += sums[w];
+        x += ha::decayed(vec[I::whole / 4], all);
+        const bool on = t0 + tid < live;
+        if (!on) x = 0.0f;
+        if (p.dlog_a && t0 + tid < p.tokens) p.dlog_a[row0 + (long long)tid * p.heads] = x;
+        if (p.part) {
+            double total = x;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
+            if (lane == 0) reinterpret_cast<double*>(sums + 16)[warp] = total;
+        }
+    }
+    if (p.part) {
+        __syncthreads();
+        if (tid == 0) {
+            double total = 0.0;
+            for (int w = 0; w < C / 32; ++w) total += reinterpret_cast<double*>(sums + 16)[w];
+            p.part[blockIdx.x] = total;
+        }
+    }
+}
 
 // Rows of `width` floats in global memory as bf16 terms in shared memory; `weight` (for each column) or NULL.
 template <int kTerms>
@@ -281,31 +390,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     const int n = blockIdx.x % p.chunks, bh = blockIdx.x / p.chunks, b = bh / p.heads, h = bh % p.heads;
     const int live = live_tokens(p.lengths, b, p.tokens), t0 = n * C, slices = (p.dv + 15) / 16;
     const long long row0 = ((long long)b * p.tokens + t0) * p.heads + h;  // of [batch, tokens, heads, ..]
-    auto put2 = [&](void* to, int each, long long where, int c, float x, float y) {  // columns c and c + 1 of a row
-        if (each) {
-            float* g = static_cast<float*>(to) + where;
-            if (c < p.dk) g[0] = x;
-            if (c + 1 < p.dk) g[1] = y;
-        } else {
-            T* g = static_cast<T*>(to) + where;
-            if (c < p.dk) g[0] = ha::from_f<T>(x);
-            if (c + 1 < p.dk) g[1] = ha::from_f<T>(y);
-        }
-    };
-    if (t0 >= live) {  // no token of the sequence: zeros
-        const int wide2 = (p.dk + 1) / 2;
-        for (int e = tid; e < C * wide2; e += kGradThreads)
-            if (t0 + e / wide2 < p.tokens) {
-                const int c = 2 * (e % wide2);
-                const long long to = (row0 + (long long)(e / wide2) * p.heads) * p.dk + c;
-                put2(p.dq, p.each_q, to, c, 0.0f, 0.0f);
-                put2(p.dk_out, p.each_k, to, c, 0.0f, 0.0f);
-            }
-        if (tid < C && t0 + tid < p.tokens) {
-            if (p.dlog_a) p.dlog_a[row0 + (long long)tid * p.heads] = 0.0f;
-            if (p.dbeta) p.dbeta[row0 + (long long)tid * p.heads] = 0.0f;
-        }
-        if (tid == 0 && p.part) p.part[blockIdx.x] = 0.0;
+    if (t0 >= live) {
+        empty_chunk<C, T, kGradThreads>(p, row0, t0, blockIdx.x);
         return;
     }
     const Waiter wait{bars, stop, p.spin};
@@ -561,79 +647,10 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             if (t0 + i >= p.tokens) continue;
             const long long to = (row0 + (long long)i * p.heads) * p.dk + c;
             const bool on = t0 + i < live;
-            put2(p.dq, p.each_q, to, c, on ? fq[nt][2 * r] : 0.0f, on ? fq[nt][2 * r + 1] : 0.0f);
-            put2(p.dk_out, p.each_k, to, c, on ? fz[nt][2 * r] : 0.0f, on ? fz[nt][2 * r + 1] : 0.0f);
+            put_pair<T>(p.dq, p.each_q, to, p.dk - c, on ? fq[nt][2 * r] : 0.0f, on ? fq[nt][2 * r + 1] : 0.0f);
+            put_pair<T>(p.dk_out, p.each_k, to, p.dk - c, on ? fz[nt][2 * r] : 0.0f, on ? fz[nt][2 * r + 1] : 0.0f);
         }
-    // the gates
-    const float* const dots = p.dots + (long long)blockIdx.x * 2 * slices * C;
-    float db = 0.0f, dl = 0.0f;
-    if (tid < C)
-        for (int v = 0; v < slices; ++v) {
-            db += dots[v * C + tid];
-            dl += dots[(slices + v) * C + tid];
-        }
-    if (tid < C && p.dbeta && t0 + tid < p.tokens) p.dbeta[row0 + (long long)tid * p.heads] = t0 + tid < live ? db : 0.0f;
-    if (!p.dlog_a && !p.part) return;
-    // sum_{i>=t>j} W_ij: sums up each column by parts of 16 rows, then along the rows
-    float* const tops = far + kColumnBlocks * C;  // of each part and column (the rest of `far`)
-    static_assert((kColumnBlocks + C / 16) * C <= 8 * C, "scratch");
-    for (int e = tid; e < C * (C / 16); e += kGradThreads) {
-        const int j = e % C, part = e / C;
-        float x = 0.0f;
-#pragma unroll
-        for (int i = 15; i >= 0; --i) {
-            float& w = wm[(16 * part + i) * (C + 1) + j];
-            x += 16 * part + i > j ? w : 0.0f;
-            w = x;
-        }
-        tops[part * C + j] = x;
-    }
-    __syncthreads();
-    float g = 0.0f;
-    if (tid < 4 * C) {
-        const int t = tid >> 2, quarter = tid & 3;  // a quarter of the columns before t
-        for (int j = quarter; j < t; j += 4) {
-            float x = wm[t * (C + 1) + j];
-            for (int part = (t >> 4) + 1; part < C / 16; ++part) x += tops[part * C + j];
-            g += x;
-        }
-        g += __shfl_xor_sync(~0u, g, 1);
-        g += __shfl_xor_sync(~0u, g, 2);
-    }
-    __syncthreads();
-    if (tid < 4 * C && (tid & 3) == 0) wm[tid >> 2] = g;
-    if (tid < C) {
-        float f = 0.0f;
-#pragma unroll
-        for (int c = 0; c < kColumnBlocks; ++c) f += far[c * C + tid];
-        wm[C + tid] = f;       // far
-        wm[2 * C + tid] = dl;  // late
-    }
-    __syncthreads();
-    if (tid < C) {
-        float x = wm[tid], all = 0.0f;
-        for (int i = C - 1; i >= tid; --i) x += wm[C + i];
-        for (int j = 0; j < tid; ++j) x += wm[2 * C + j];
-        for (int w = 0; w < kGradThreads / 32; ++w) all += sums[w];
-        x += ha::decayed(vec[I::whole / 4], all);
-        const bool on = t0 + tid < live;
-        if (!on) x = 0.0f;
-        if (p.dlog_a && t0 + tid < p.tokens) p.dlog_a[row0 + (long long)tid * p.heads] = x;
-        if (p.part) {
-            double total = x;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
-            if (lane == 0) reinterpret_cast<double*>(sums + 16)[warp] = total;
-        }
-    }
-    if (p.part) {
-        __syncthreads();
-        if (tid == 0) {
-            double total = 0.0;
-            for (int w = 0; w < C / 32; ++w) total += reinterpret_cast<double*>(sums + 16)[w];
-            p.part[blockIdx.x] = total;
-        }
-    }
+    gate_gradients<C, I, kColumnBlocks>(p, vec, far, sums, wm, row0, t0, live, slices);
 }
 
 // dlog_a[h]: the sum of the chunks' parts over the batch, in 64 bits and in a fixed order; a warp for each head.

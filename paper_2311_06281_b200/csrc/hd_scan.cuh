@@ -61,7 +61,7 @@ struct Params {
     float* gradients;      // the gradient of the state after every chunk, as `states`
     float* dots;           // [batch * heads][chunks][2][slices][C]: by slice of V, dbeta and e^{c_C-c_j} k_j^T D V'_j
     void *dq, *dk_out;       // contiguous [batch, tokens, heads, dk]; in float32 where each_ says so (heads to be summed)
-    int each_q, each_k;
+    int each_q, each_k, dq_tma, dk_tma;
     float *dlog_a, *dbeta; // [batch, tokens, heads], or NULL
     double* part;          // fixed decays: their gradients' sums over each chunk, [batch * heads][chunks]
     Fault* fault;
@@ -79,27 +79,35 @@ __device__ __forceinline__ void give_up(const Params& p, int* gave_up, int where
     p.fault->error_id = p.call_id;
 }
 
-// What chunk_kernel writes: five vectors over the tokens and the decay of the whole chunk; N; P.  N and P as bf16 terms in the
-// layout of a tile, blocks above the diagonal left as they were.
+template <int kValue> struct Int { static constexpr int value = kValue; };
+
+// The blocks of 16 x 16 on and below the diagonal of a C x C matrix, row by row, each 16 rows of 32 bytes.
+__host__ __device__ constexpr int block_of(int i, int j) { return i * (i + 1) / 2 + j; }
+__device__ __forceinline__ uint32_t block_place(int i, int j, int row, int piece) { return block_of(i, j) * 512 + place<32>(row, piece); }
+
+// What chunk_kernel writes: six vectors over the tokens and the decay of the whole chunk; the blocks of N; those of P; as bf16 terms.
 template <int C, int kTermsN, int kTermsP> struct Image {
-    static constexpr uint32_t early = 0, late = C * 4, beta = 2 * C * 4, hi = 3 * C * 4, lo = 4 * C * 4, whole = 5 * C * 4;  // whole, its logarithm
-    static constexpr uint32_t n = 5 * C * 4 + 128, plane = C * C * 2, p = n + kTermsN * plane, end = p + kTermsP * plane;
+    // e^{c}, e^{c_C-c}, beta, c in two parts, e^{c_m-c} with m the last of the token's sixteen; the whole chunk's decay and its logarithm
+    static constexpr uint32_t early = 0, late = C * 4, beta = 2 * C * 4, hi = 3 * C * 4, lo = 4 * C * 4, edge = 5 * C * 4, whole = 6 * C * 4;
+    static constexpr uint32_t n = 6 * C * 4 + 128, plane = block_of(C / 16, 0) * 512, p = n + kTermsN * plane, end = p + kTermsP * plane;
     static_assert(n % 128 == 0 && end % 128 == 0, "alignment");
 };
 
-constexpr int kChunkBars = 8;
-
 template <int KP, int C, int TI, int TM, int TP>
 struct ChunkLayout {
-    static constexpr uint32_t tile = KP * C * 2 * TI, k = 0, q = tile;
     using I = Image<C, TM, TP>;
-    static constexpr uint32_t big = 2 * tile > I::end - I::n ? 2 * tile : I::end - I::n;  // the planes go where K and Q were
-    // M in three terms; its diagonal blocks of 16 in float32; their inverses in three terms, rows of 32 bytes
-    static constexpr uint32_t m = big, diag = m + 3 * I::plane, inverse = diag + C * 64, vec = inverse + 3 * C * 32, bars = vec + I::n, end = bars + 64;
+    // for each term and block of 64 columns the rows of K, then those of Q; the tensor core reads 128 rows from the first of a block
+    static constexpr uint32_t block = 2 * C * 128, tile = TI * (KP / 64) * block, reads = tile + 128 * 128 - block;
+    // M in three terms, then N, where K and Q were
+    static constexpr uint32_t m = 0, n = 3 * I::plane, solved = n + TM * I::plane, region = (reads > solved ? reads : solved + 1023) / 1024 * 1024;
+    // M's diagonal blocks in float32; the inverses in three terms
+    static constexpr uint32_t diag = region, inverse = diag + C * 64, vec = inverse + 3 * C * 32, bars = vec + I::n, end = bars + 64;
+    static constexpr int columns = C * (TI == 1 ? 1 : 2);  // of tensor memory
 };
 
-// M, P and N of one chunk.  C / 16 warps; a warp has 16 rows of M and P and inverts the diagonal block of I + M beta there, then has
-// 16 columns of N, transposed, and solves for them block by block of rows,
+// M, P and N of one chunk.  [K; Q] K^T is one product of 128 rows on the tensor core (tcgen05; float32: the leading terms' product and
+// the sum of the small ones side by side); a thread has a row of it, the first C threads M's, the others P's.  Then each of C / 16 warps
+// inverts a diagonal block of I + M beta, and solves for 16 columns of N, transposed, block by block of rows,
 //     N_iw = (I + M_ii beta_i)^{-1} (M_iw - sum_{w<=s<i} M_is beta_s N_sw),
 // every N^T_sw the next product's factor in its registers.  24 bits in all of it: a wrong N is wrong for every column of V.
 template <int KP, int C, int TI, int TM, int TP>
@@ -107,11 +115,12 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
                                                       int* gave_up) {
     using L = ChunkLayout<KP, C, TI, TM, TP>;
     using I = Image<C, TM, TP>;
-    constexpr int kLevel = TI - 1;
+    constexpr int NB = C / 16;
     extern __shared__ __align__(1024) uint8_t sm8[];
     const uint32_t base = smem_addr(sm8), bars = base + L::bars;
     float* const vec = reinterpret_cast<float*>(sm8 + L::vec);
     volatile int* const stop = reinterpret_cast<int*>(sm8 + L::bars + 48);
+    uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(sm8 + L::bars + 56);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int n = blockIdx.x % p.chunks, bh = blockIdx.x / p.chunks, b = bh / p.heads, h = bh % p.heads;
     const int live = live_tokens(p.lengths, b, p.tokens), t0 = n * C;
@@ -119,19 +128,25 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
     if (t0 >= live) return;
     if (tid == 0) {
         ha::bar_init(bars, 1);
+        ha::bar_init(bars + 8, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *stop = 0;
         ha::fence_smem_to_async();
         if (n != p.mute) {
-            ha::bar_expect(bars, 2 * L::tile);
+            ha::bar_expect(bars, L::tile);
             for (int u = 0; u < TI; ++u)
                 for (int c = 0; c < KP / 64; ++c) {
-                    ha::tma_load_4d(base + L::k + (u * (KP / 64) + c) * C * 128, &mk, 64 * c, h / p.kdiv, t0, u * p.batch + b, bars);
-                    ha::tma_load_4d(base + L::q + (u * (KP / 64) + c) * C * 128, &mq, 64 * c, h / p.qdiv, t0, u * p.batch + b, bars);
+                    const uint32_t to = base + (u * (KP / 64) + c) * L::block;
+                    ha::tma_load_4d(to, &mk, 64 * c, h / p.kdiv, t0, u * p.batch + b, bars);
+                    ha::tma_load_4d(to + C * 128, &mq, 64 * c, h / p.qdiv, t0, u * p.batch + b, bars);
                 }
         }
     }
-    if (warp == (C == 64 ? 1 : 0)) {  // the decays: a lane has C / 32 tokens, sums in 64 bits
+    if (warp == 0) {
+        __syncwarp();
+        ha::tmem_alloc(smem_addr(s_tmem), L::columns);
+    }
+    if (warp == 1) {  // the decays: a lane has C / 32 tokens, sums in 64 bits
         constexpr int kOwn = C / 32;
         double c[kOwn];
         float be[kOwn];
@@ -158,70 +173,116 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
             vec[I::beta / 4 + t] = be[i];
             vec[I::hi / 4 + t] = (float)x;
             vec[I::lo / 4 + t] = (float)(x - (double)(float)x);
+            const double edge = __shfl_sync(~0u, c[kOwn - 1] + before, lane | (16 / kOwn - 1));
+            vec[I::edge / 4 + t] = ex2((float)(edge - x));
         }
-        if (lane < 32) vec[I::whole / 4 + lane] = lane == 0 ? ex2((float)all) : lane == 1 ? (float)all : 0.0f;
+        vec[I::whole / 4 + lane] = lane == 0 ? ex2((float)all) : lane == 1 ? (float)all : 0.0f;
     }
+    ha::tmem_before_sync();
     __syncthreads();
+    ha::tmem_after_sync();
+    const uint32_t tmem = *s_tmem;
     const Waiter wait{bars, stop, p.spin};
-    bool ok = wait(0, 0);
-    ok = __syncthreads_and(ok);
+    if (warp == 0) {
+        const bool loaded = __all_sync(~0u, wait(0, 0));
+        if (!loaded) wait.drain(0, 0);
+        if (loaded && ha::elect_one()) {
+            constexpr uint32_t shape = ha::mma_shape(C, 0);
+            const uint32_t at = ha::operand(base, 0);
+            auto term = [](int u, int kk) { return (uint32_t)((u * (KP / 64) + (kk >> 2)) * (L::block >> 4) + (kk & 3) * 2); };
+#pragma unroll
+            for (int level = TI - 1; level >= 0; --level)
+#pragma unroll
+                for (int u = 0; u < TI; ++u)
+                    if (level - u >= 0)
+#pragma unroll
+                        for (int kk = 0; kk < KP / 16; ++kk)
+                            ha::mma_ss(tmem + (level ? C : 0), at + term(u, kk), at + term(level - u, kk), shape, kk > 0 || (level && (level < TI - 1 || u > 0)));
+            ha::mma_commit(bars + 8);
+        }
+        __syncwarp();
+    }
+    const bool ok = __syncthreads_and(wait(1, 0));
     if (!ok) {  // outputs are not valid; nothing of this CTA's is in flight, or was not within the limit
-        wait.drain(0, 0);
+        if (warp == 0) {
+            wait.drain(1, 0);
+            ha::tmem_free(tmem, L::columns);
+        }
         if (tid == 0) give_up(p, gave_up, 1);
         return;
     }
-    const Lane at;
-    const int i0 = 16 * warp + (lane >> 2), j0 = 2 * (lane & 3);
-    float mm[C / 8][4] = {}, pp[C / 8][4] = {};
-#pragma unroll 2
-    for (int kk = 0; kk < KP / 16; ++kk) {
-        uint32_t ak[TI][4], aq[TI][4];
+    ha::tmem_after_sync();
+    uint8_t* const image = p.image + (long long)blockIdx.x * I::end;
+    {   // weights of a row
+        const bool mine_p = tid >= C;
+        const int i = tid & (C - 1), ib = i >> 4;
+        const float own_hi = vec[I::hi / 4 + i], own_lo = vec[I::lo / 4 + i];
+        float* const diag = reinterpret_cast<float*>(sm8 + L::diag) + ib * 256 + (i & 15);
+#pragma unroll 1
+        for (int jb = 0; jb <= ((tid | 31) & (C - 1)) >> 4; ++jb) {  // the warp's last row says how far
+            uint32_t v[16];
+            float x[16];
+            __syncwarp();
+            ha::tmem_ld16(v, tmem + ((uint32_t)(tid & ~31) << 16) + 16 * jb);
 #pragma unroll
-        for (int u = 0; u < TI; ++u) {
-            load4(ak[u], base + L::k + u * (KP * C * 2) + wide<C>(16 * warp + at.a_row(), 2 * kk + at.a_piece()));
-            load4(aq[u], base + L::q + u * (KP * C * 2) + wide<C>(16 * warp + at.a_row(), 2 * kk + at.a_piece()));
-        }
+            for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(v[e]);
+            if constexpr (TI > 1) {
+                ha::tmem_ld16(v, tmem + ((uint32_t)(tid & ~31) << 16) + C + 16 * jb);
 #pragma unroll
-        for (int np = 0; np < C / 16; ++np)
-            if (np <= warp) {
-                uint32_t bk[1][TI][4];
+                for (int e = 0; e < 16; ++e) x[e] += __uint_as_float(v[e]);
+            }
+            if (jb > ib) continue;
+            if (16 * jb + 15 < (tid & (C - 32))) {
+                // Sixteen columns before all rows of the warp: e^{c_i-c_j} = e^{c_i-c_m} e^{c_m-c_j} with m the last of them; both exponents
+                // keep their sign, and one exponential of the row serves them all.
+                const int m = 16 * jb + 15;
+                float f = t0 + i < live ? ex2((own_hi - vec[I::hi / 4 + m]) + (own_lo - vec[I::lo / 4 + m])) : 0.0f;
+                if (mine_p) f *= p.scale;
 #pragma unroll
-                for (int u = 0; u < TI; ++u) load4(bk[0][u], base + L::k + u * (KP * C * 2) + wide<C>(16 * np + at.b_row(), 2 * kk + at.b_piece()));
-                if constexpr (TI == 1) {
-                    products<kLevel>(mm + 2 * np, ak, bk);
-                    products<kLevel>(pp + 2 * np, aq, bk);
-                } else {
-                    rounded_products<kLevel>(mm + 2 * np, ak, bk);
-                    rounded_products<kLevel>(pp + 2 * np, aq, bk);
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 g = *reinterpret_cast<const float4*>(vec + I::edge / 4 + 16 * jb + e);
+                    x[e] = f == 0.0f ? 0.0f : f * g.x * x[e];
+                    x[e + 1] = f == 0.0f ? 0.0f : f * g.y * x[e + 1];
+                    x[e + 2] = f == 0.0f ? 0.0f : f * g.z * x[e + 2];
+                    x[e + 3] = f == 0.0f ? 0.0f : f * g.w * x[e + 3];
+                }
+            } else {
+                const int last = t0 + i < live ? (mine_p ? i : i - 1) - 16 * jb : -1;  // the last column that counts
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const float4 hi = *reinterpret_cast<const float4*>(vec + I::hi / 4 + 16 * jb + e), lo = *reinterpret_cast<const float4*>(vec + I::lo / 4 + 16 * jb + e);
+                    const float d[4] = {(own_hi - hi.x) + (own_lo - lo.x), (own_hi - hi.y) + (own_lo - lo.y), (own_hi - hi.z) + (own_lo - lo.z), (own_hi - hi.w) + (own_lo - lo.w)};
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const float w = e + u <= last ? ex2(d[u]) : 0.0f;
+                        x[e + u] = w != 0.0f ? (mine_p ? p.scale * w : w) * x[e + u] : 0.0f;
+                    }
+                    if (!mine_p && jb == ib)  // transposed: the inverse reads columns
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) diag[(e + u) * 16] = x[e + u];
                 }
             }
-    }
-    // weights
-    const float hi0 = vec[I::hi / 4 + i0], hi1 = vec[I::hi / 4 + i0 + 8], lo0 = vec[I::lo / 4 + i0], lo1 = vec[I::lo / 4 + i0 + 8];
-    const bool on0 = t0 + i0 < live, on1 = t0 + i0 + 8 < live;
-    float* const diag = reinterpret_cast<float*>(sm8 + L::diag) + warp * 256;
+            auto put = [&](auto terms, uint8_t* to) {
+                constexpr int kTerms = decltype(terms)::value;
 #pragma unroll
-    for (int nt = 0; nt < C / 8; ++nt)
-        if (nt <= 2 * warp + 1) {
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t t[4][kTerms];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = e < 2 ? i0 : i0 + 8, j = 8 * nt + j0 + (e & 1);
-                const float d = ((e < 2 ? hi0 : hi1) - vec[I::hi / 4 + j]) + ((e < 2 ? lo0 : lo1) - vec[I::lo / 4 + j]);
-                const float w = j <= i && (e < 2 ? on0 : on1) ? ex2(d) : 0.0f;
-                pp[nt][e] = w != 0.0f ? p.scale * w * pp[nt][e] : 0.0f;
-                mm[nt][e] = j < i && w != 0.0f ? w * mm[nt][e] : 0.0f;
-                if (nt >= 2 * warp) diag[(i & 15) * 16 + (j & 15)] = mm[nt][e];
-            }
+                    for (int u = 0; u < 4; ++u) ha::split<kTerms>(ha::make_pair2(x[8 * half + 2 * u], x[8 * half + 2 * u + 1]), t[u]);
 #pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                uint32_t t[3];
-                ha::split<3>(ha::make_pair2(mm[nt][e], mm[nt][e + 1]), t);
-#pragma unroll
-                for (int u = 0; u < 3; ++u) *reinterpret_cast<uint32_t*>(sm8 + L::m + u * I::plane + place<2 * C>(i0 + 4 * e, nt) + 2 * j0) = t[u];
-            }
+                    for (int u = 0; u < kTerms; ++u)
+                        *reinterpret_cast<uint4*>(to + u * I::plane + block_place(ib, jb, i & 15, half)) = make_uint4(t[0][u], t[1][u], t[2][u], t[3][u]);
+                }
+            };
+            if (mine_p) put(Int<TP>{}, image + I::p);
+            else put(Int<3>{}, sm8 + L::m);
         }
-    __syncwarp();
+    }
+    ha::tmem_before_sync();
+    __syncthreads();
+    if (warp == 0) ha::tmem_free(tmem, L::columns);
     {   // the inverse of the warp's diagonal block, a column for each lane of either half
+        const float* const diag = reinterpret_cast<const float*>(sm8 + L::diag) + warp * 256;
         const int c = lane & 15;
         float x[16];
 #pragma unroll
@@ -230,41 +291,40 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
         for (int i = 0; i < 15; ++i) {
             const float y = vec[I::beta / 4 + 16 * warp + i] * x[i];
 #pragma unroll
-            for (int r = i + 1; r < 16; ++r) x[r] = fmaf(-diag[r * 16 + i], y, x[r]);
-        }
+            for (int r = (i + 1) / 4 * 4; r < 16; r += 4) {
+                const float4 f = *reinterpret_cast<const float4*>(diag + i * 16 + r);
+                const float g[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            uint32_t t[3];
-            ha::split<3>(ha::make_pair2(x[r], 0.0f), t);
-            if (lane < 16)
-#pragma unroll
-                for (int u = 0; u < 3; ++u)
-                    *reinterpret_cast<uint16_t*>(sm8 + L::inverse + u * (C * 32) + place<32>(16 * warp + r, c >> 3) + 2 * (c & 7)) = (uint16_t)t[u];
-        }
-    }
-    __syncthreads();  // K and Q have been read, M and the inverses are there
-#pragma unroll
-    for (int nt = 0; nt < C / 8; ++nt)
-        if (nt <= 2 * warp + 1) {
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                uint32_t t[TP];
-                ha::split<TP>(ha::make_pair2(pp[nt][e], pp[nt][e + 1]), t);
-#pragma unroll
-                for (int u = 0; u < TP; ++u)
-                    *reinterpret_cast<uint32_t*>(sm8 + (I::p - I::n) + u * I::plane + place<2 * C>(i0 + 4 * e, nt) + 2 * j0) = t[u];
+                for (int u = 0; u < 4; ++u)
+                    if (r + u > i) x[r + u] = fmaf(-g[u], y, x[r + u]);
             }
         }
-    uint32_t done[C / 16][3][4];  // -(N^T_sw) beta_s as an operand
 #pragma unroll
-    for (int i = 0; i < C / 16; ++i)
+        for (int r = 0; r < 16; r += 2) {
+            uint32_t t[3];
+            ha::split<3>(ha::make_pair2(x[r], x[r + 1]), t);
+            if (lane < 16)
+#pragma unroll
+                for (int u = 0; u < 3; ++u) {
+                    uint8_t* const to = sm8 + L::inverse + u * (C * 32) + 2 * (c & 7);
+                    *reinterpret_cast<uint16_t*>(to + place<32>(16 * warp + r, c >> 3)) = (uint16_t)t[u];
+                    *reinterpret_cast<uint16_t*>(to + place<32>(16 * warp + r + 1, c >> 3)) = (uint16_t)(t[u] >> 16);
+                }
+        }
+    }
+    __syncthreads();
+    const Lane at;
+    const int j0 = 2 * (lane & 3);
+    uint32_t done[NB][3][4];  // -(N^T_sw) beta_s as an operand
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
         if (i >= warp) {
             float r[2][4] = {}, x[2][4] = {};
             {   // M^T_iw
                 uint32_t m[4];
 #pragma unroll
                 for (int u = 2; u >= 0; --u) {
-                    load4_t(m, base + L::m + u * I::plane + place<2 * C>(16 * i + at.b_row(), 2 * warp + at.b_piece()));
+                    load4_t(m, base + L::m + u * I::plane + block_place(i, warp, at.b_row(), at.b_piece()));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         r[e >> 1][2 * (e & 1)] += __uint_as_float(m[e] << 16);
@@ -272,18 +332,36 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
                     }
                 }
             }
-            uint32_t bf[1][3][4], a[3][4];
+            float t[NB][2][4] = {};  // products that do not wait for each other
+            uint32_t bf[NB][1][3][4], a[3][4];
 #pragma unroll
             for (int s = 0; s < i; ++s)
-                if (s >= warp) {
+                if (s >= warp)
 #pragma unroll
-                    for (int u = 0; u < 3; ++u) load4(bf[0][u], base + L::m + u * I::plane + place<2 * C>(16 * i + at.b_row(), 2 * s + at.b_piece()));
-                    rounded_products<2>(r, done[s], bf);
-                }
+                    for (int u = 0; u < 3; ++u) load4(bf[s][0][u], base + L::m + u * I::plane + block_place(i, s, at.b_row(), at.b_piece()));
+#pragma unroll
+            for (int level = 2; level >= 0; --level)
+#pragma unroll
+                for (int u = 0; u <= level; ++u)
+#pragma unroll
+                    for (int s = 0; s < i; ++s)
+                        if (s >= warp) {
+                            mma(t[s][0], done[s][u], bf[s][0][level - u][0], bf[s][0][level - u][1]);
+                            mma(t[s][1], done[s][u], bf[s][0][level - u][2], bf[s][0][level - u][3]);
+                        }
+#pragma unroll
+            for (int s = 0; s < i; ++s)
+                if (s >= warp)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        r[0][e] += t[s][0][e];
+                        r[1][e] += t[s][1][e];
+                    }
             as_operand<3>(a, r[0], r[1]);
+            uint32_t bi[1][3][4];
 #pragma unroll
-            for (int u = 0; u < 3; ++u) load4(bf[0][u], base + L::inverse + u * (C * 32) + place<32>(16 * i + at.b_row(), at.b_piece()));
-            rounded_products<2>(x, a, bf);
+            for (int u = 0; u < 3; ++u) load4(bi[0][u], base + L::inverse + u * (C * 32) + place<32>(16 * i + at.b_row(), at.b_piece()));
+            products<2>(x, a, bi);
             float w[2][4];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
@@ -291,18 +369,16 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
 #pragma unroll
                 for (int e = 0; e < 4; ++e) w[y][e] = -(e & 1 ? be.y : be.x) * x[y][e];
             }
-            if (i + 1 < C / 16) as_operand<3>(done[i], w[0], w[1]);
+            if (i + 1 < NB) as_operand<3>(done[i], w[0], w[1]);
             as_operand<3>(a, x[0], x[1]);
 #pragma unroll
-            for (int u = 0; u < TM; ++u) {
-                const uint32_t t[4] = {a[u][0], a[u][1], a[u][2], a[u][3]};  // in the order in which M^T was loaded
-                store4_t(base + u * I::plane + place<2 * C>(16 * i + at.b_row(), 2 * warp + at.b_piece()), t);
-            }
+            for (int u = 0; u < TM; ++u)  // in the order in which M^T was loaded
+                store4_t(base + L::n + u * I::plane + block_place(i, warp, at.b_row(), at.b_piece()), a[u]);
         }
     __syncthreads();
-    uint4* to = reinterpret_cast<uint4*>(p.image + (long long)blockIdx.x * I::end);
+    uint4* to = reinterpret_cast<uint4*>(image);
     for (uint32_t e = tid; e < I::n / 16; e += 2 * C) to[e] = reinterpret_cast<const uint4*>(sm8 + L::vec)[e];
-    for (uint32_t e = tid; e < (I::end - I::n) / 16; e += 2 * C) to[I::n / 16 + e] = reinterpret_cast<const uint4*>(sm8)[e];
+    for (uint32_t e = tid; e < (I::p - I::n) / 16; e += 2 * C) to[I::n / 16 + e] = reinterpret_cast<const uint4*>(sm8 + L::n)[e];
 }
 
 // ---------------------------------------------------------------------------------------------------------------- scan
@@ -588,7 +664,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int u = 0; u < TM; ++u)
-                            if (g < pairs) load4(bf[g][u], N + u * I::plane + place<2 * C>(16 * (np + g) + at.b_row(), 2 * jj + at.b_piece()));
+                            if (g < pairs) load4(bf[g][u], N + u * I::plane + block_place(np + g, jj, at.b_row(), at.b_piece()));
                     sum<kRounded, kLevel>(y + 2 * np, a, bf, pairs);
                 }
             }
@@ -613,7 +689,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
                         for (int g = 0; g < 2; ++g)
 #pragma unroll
                             for (int u = 0; u < TP; ++u)
-                                if (g < pairs) load4(bf[g][u], P + u * I::plane + place<2 * C>(16 * (np + g) + at.b_row(), 2 * jj + at.b_piece()));
+                                if (g < pairs) load4(bf[g][u], P + u * I::plane + block_place(np + g, jj, at.b_row(), at.b_piece()));
                         sum<kRounded, TO - 1>(o + 2 * np, a, bf, pairs);
                     }
                 }

@@ -1,5 +1,5 @@
 // C ABI of the delta rule with a decay: the gradients.
-#include "hd_grad.cuh"
+#include "hd_grad_mma.cuh"
 #include "hd_host.h"
 
 namespace {
@@ -63,16 +63,38 @@ hs_status launch_back(const CUtensorMap& mq, const CUtensorMap& mk, const CUtens
     return launched("back_kernel");
 }
 
+// The gradients of the chunks: tcgen05 for bf16 and keys up to 128 wide (8 x 2048 tokens, 16 heads of 128: see the figures in
+// hd_grad_mma.cuh), mma.sync for the rest, where all factors have three terms or the tiles of two CTAs would not fit.
 template <int KP, int TI, class T>
 hs_status launch_grad(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mg, const hd::Params& q, int* word, cudaStream_t stream) {
     constexpr int C = hd::chunk_tokens(KP), TM = terms_of(TI);
-    using L = hd::GradLayout<KP, C, TI, TM>;
-    static_assert(L::end <= 232448, "shared memory");
-    const auto fn = hd::grad_kernel<KP, C, TI, TM, T>;
     static std::atomic<unsigned long long> done{0};
-    const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end, done);
-    if (st != HS_OK) return st;
-    fn<<<(unsigned)((long long)q.batch * q.heads * q.chunks), hd::kGradThreads, L::end, stream>>>(mq, mk, mg, q, word);
+    const unsigned grid = (unsigned)((long long)q.batch * q.heads * q.chunks);
+    if constexpr (TI == 1 && KP <= 128) {
+        using L = hd::GradMmaLayout<KP>;
+        static_assert(L::end <= 232448, "shared memory");
+        const auto fn = hd::grad_mma_kernel<KP, T>;
+        const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end, done);
+        if (st != HS_OK) return st;
+        hd::Params g = q;
+        CUtensorMap mdq, mdk;
+        auto out = [&](CUtensorMap* m, void* to, int each) {  // the tensor map of a gradient that TMA can store
+            std::memset(m, 0, sizeof *m);
+            const long long sh = q.dk, stk = sh * q.heads;
+            const View v{{to, stk * q.tokens, stk, sh, 1}, q.heads, q.dk};
+            return !each && tma_strides(v, q.batch, q.tokens) && encode(m, v, q.batch, q.tokens, 64, C);
+        };
+        g.dq_tma = out(&mdq, q.dq, q.each_q);
+        g.dk_tma = out(&mdk, q.dk_out, q.each_k);
+        fn<<<std::min(grid, (unsigned)kSms), hd::kGradMmaThreads, L::end, stream>>>(mq, mk, mg, mdq, mdk, g, (int)grid, word);
+    } else {
+        using L = hd::GradLayout<KP, C, TI, TM>;
+        static_assert(L::end <= 232448, "shared memory");
+        const auto fn = hd::grad_kernel<KP, C, TI, TM, T>;
+        const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end, done);
+        if (st != HS_OK) return st;
+        fn<<<grid, hd::kGradThreads, L::end, stream>>>(mq, mk, mg, q, word);
+    }
     return launched("grad_kernel");
 }
 
