@@ -7,8 +7,8 @@
 //     R = [Q; K] K^T      (128 x 64)
 //     A += [Hd; -Hz] K + [0; Hd^T] Q + [0; -Hz^T] K       dQ = A above, dK = A + e^{c_C-c} L below
 // V', Z and S enter as three bf16 terms (24 bits: dlog a hangs on them), formed from the float32 dumps while the tensor core works on
-// the sixteen columns before; dO is exact, its lower terms zero.  A CTA stays and takes chunk after chunk; one warp loads ahead, the
-// others have a row of a product and a quarter of its columns each.
+// the sixteen columns before; dO is exact, its lower terms zero.  A CTA stays and takes chunk after chunk; one warp loads ahead, one
+// issues the products, the others have a row of a product and a quarter of its columns each.
 #pragma once
 #include "hd_grad.cuh"
 
@@ -22,7 +22,7 @@ __device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a, uint32_t b, uin
                  : "memory");
 }
 
-constexpr int kGradMmaThreads = 544;  // sixteen warps that compute, one that loads
+constexpr int kGradMmaThreads = 576;  // sixteen warps that compute, one that loads, one that issues the products
 constexpr int kTeam = 512;
 
 // The team's barrier; true where all of its threads say so.
@@ -47,7 +47,7 @@ template <int KP> struct GradMmaLayout {
     static constexpr uint32_t zero = ops, h = zero + C * 128, h_term = 2 * C * 128, w = h + 2 * h_term, w_end = w + C * (C + 1) * 4;
     static constexpr uint32_t out = ops + op;
     static constexpr uint32_t raw_at = raw > (w_end + 1023) / 1024 * 1024 ? raw : (w_end + 1023) / 1024 * 1024;
-    static constexpr uint32_t vec = raw_at + kRaw * raw_bytes, far = vec + kTiles * I::n, sums = far + 16 * C * 4, bars = sums + 256, end = bars + 160;
+    static constexpr uint32_t vec = raw_at + kRaw * raw_bytes, far = vec + kTiles * I::n, sums = far + 16 * C * 4, bars = sums + 256, end = bars + 192;
     static constexpr uint32_t ta = 0, tl = KP, tg = 2 * KP, tr = 2 * KP + C, columns = 512;
     static_assert(tr + C <= columns && s % 1024 == 0 && s_term % 1024 == 0 && raw_bytes % 1024 == 0 && I::n % 128 == 0, "layout");
     static_assert(out + KP / 64 * 2 * C * 128 <= raw_at, "the way out");
@@ -60,17 +60,17 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
     using L = GradMmaLayout<KP>;
     using I = typename L::I;
     constexpr int C = 64, TM = 3;
-    enum : int { kFullTiles = 0, kFreeTiles = 2, kFullRaw = 4, kFreeRaw = 7, kDone = 10, kStep = 12, kAll = 13 };
+    enum : int { kFullTiles = 0, kFreeTiles = 2, kFullRaw = 4, kFreeRaw = 7, kDone = 10, kReady = 12, kStep = 14, kNear, kOutFree, kAll };
     extern __shared__ __align__(1024) uint8_t sm8[];
     const uint32_t base = smem_addr(sm8), bars = base + L::bars;
     float* const far = reinterpret_cast<float*>(sm8 + L::far);
     float* const sums = reinterpret_cast<float*>(sm8 + L::sums);
-    volatile int* const stop = reinterpret_cast<int*>(sm8 + L::bars + 128);
-    uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(sm8 + L::bars + 136);
+    volatile int* const stop = reinterpret_cast<int*>(sm8 + L::bars + 160);
+    uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(sm8 + L::bars + 168);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, slices = (p.dv + 15) / 16;
     const Waiter wait{bars, stop, p.spin};
     if (tid == 0) {
-        for (int i = 0; i < kAll; ++i) ha::bar_init(bars + 8 * i, i >= kFreeRaw && i < kDone ? 16 : 1);
+        for (int i = 0; i < kAll; ++i) ha::bar_init(bars + 8 * i, (i >= kFreeRaw && i < kDone) || i == kReady || i == kReady + 1 || i == kNear ? 16 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *stop = 0;
     }
@@ -133,9 +133,71 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
             for (int i = max(0, raws - L::kRaw); i < raws; ++i) wait.drain(kFullRaw + i % L::kRaw, i / L::kRaw);
         }
         __syncwarp();
+    } else if (warp == 17) {
+        // ---------------------------------------------------------------------------------------------- products
+        if (ha::elect_one()) {
+            constexpr uint32_t wide_shape = ha::mma_shape(KP, ha::kColMajorB), near_shape = ha::mma_shape(C, 0);
+            constexpr uint32_t late_shape = ha::mma_shape(KP, ha::kColMajorA | ha::kColMajorB);
+            bool ok = true;
+            int tiles = 0, ready[2] = {0, 0};
+            for (int at = blockIdx.x; at < total && ok; at += gridDim.x) {
+                const Chunk c = chunk_at(at);
+                if (c.t0 >= c.live) continue;
+                const int ts = tiles % L::kTiles;
+                for (int slab = 0; slab < slices && ok; ++slab) {
+                    const int buf = slab & 1;
+                    ok = wait(kReady + buf, ready[buf]);  // (the team has waited for what arrived)
+                    if (!ok) break;
+                    ready[buf] += 1;
+                    const uint32_t from = base + L::ops + buf * L::op;
+                    ha::tmem_after_sync();
+                    const uint32_t az = ha::operand(from + L::az, 0), vo = ha::operand(from + L::v, 0), so = ha::operand(from + L::s, 2048),
+                                   dd = ha::operand(from + L::d, 2048);
+#pragma unroll
+                    for (int level = TM - 1; level >= 0; --level)
+#pragma unroll
+                        for (int u = 0; u <= level; ++u) {
+                            const bool more = slab > 0 || level < TM - 1 || u > 0;
+                            mma_tile<kRows32, ha::kSwizzled>(L::ta, az + u * (L::az_term >> 4), so + (level - u) * (L::s_term >> 4), wide_shape, more);
+                            mma_tile<kRows32, kRows32>(L::tg, az + u * (L::az_term >> 4), vo + (level - u) * (L::v_term >> 4), near_shape, more);
+                        }
+#pragma unroll
+                    for (int u = 1; u >= 0; --u)  // rows 64..127 are V' (above them is what lies before it: those sums are not used)
+                        mma_tile<kRows32, ha::kSwizzled>(L::tl, vo + u * (L::v_term >> 4) - (C * 32 >> 4), dd, wide_shape, slab > 0 || u == 0);
+                    if (slab == 0) {
+                        const uint32_t rows = ha::operand(base + ts * L::tiles_bytes, 0);
+#pragma unroll
+                        for (int kk = 0; kk < KP / 16; ++kk) {
+                            const uint32_t step = (kk >> 2) * (L::block >> 4) + (kk & 3) * 2;
+                            mma_tile<ha::kSwizzled, ha::kSwizzled>(L::tr, rows + step, rows + step + (C * 128 >> 4), near_shape, kk > 0);
+                        }
+                    }
+                    ha::mma_commit(bars + 8 * (kDone + buf));
+                }
+                if (!ok || !(ok = wait(kNear, tiles))) break;
+                ha::tmem_after_sync();
+                const uint32_t q = ha::operand(base + ts * L::tiles_bytes, L::block), k = ha::operand(base + ts * L::tiles_bytes + C * 128, L::block);
+#pragma unroll
+                for (int u = 1; u >= 0; --u)
+#pragma unroll
+                    for (int kk = 0; kk < C / 16; ++kk) {
+                        mma_tile<ha::kSwizzled, ha::kSwizzled>(L::ta, ha::operand(base + L::h + u * L::h_term, 0) + kk * 2, k + kk * 128, wide_shape, true);
+                        // [0; H^T]: from the zeros the second 64 rows lie as far as H does
+                        mma_tile<ha::kSwizzled, ha::kSwizzled>(L::ta, ha::operand(base + L::zero, L::h - L::zero + u * L::h_term) + kk * 128, q + kk * 128, late_shape, true);
+                        mma_tile<ha::kSwizzled, ha::kSwizzled>(L::ta, ha::operand(base + L::zero, L::h - L::zero + u * L::h_term + C * 128) + kk * 128, k + kk * 128, late_shape, true);
+                    }
+                ha::mma_commit(bars + 8 * kStep);
+                ++tiles;
+            }
+            // what was issued may still run
+            for (int buf = 0; buf < 2; ++buf)
+                if (ready[buf]) wait.drain(kDone + buf, ready[buf] - 1);
+            if (tiles) wait.drain(kStep, tiles - 1);
+        }
+        __syncwarp();
     } else {
         bool ok = true;
-        int tiles = 0, used = 0, steps = 0, issued[2] = {0, 0};  // chunks with tokens, slabs, separate products, slabs of each buffer so far
+        int tiles = 0, used = 0, issued[2] = {0, 0};  // chunks with tokens, slabs, slabs of each buffer so far
         const int quarter = warp >> 2, row = (warp & 3) * 32 + lane, i = row & (C - 1);  // a row of the products, a quarter of their columns
         const bool key = row >= C;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -165,6 +227,7 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                 const uint8_t* const raw = sm8 + L::raw_at + rs * L::raw_bytes;
                 // (the buffers held other things since the chunk before: its last products are done)
                 if (slab >= 2) ok = ok && wait(kDone + buf, issued[buf] - 1);
+                if (slab == 1 && tiles > 1) ok = ok && wait(kOutFree, tiles - 2);  // what the chunk before sent from there has left
                 ok = ok && wait(kFullRaw + rs, used / L::kRaw);
                 if (ok) {
                     const int token = tid & 63, quad = (tid >> 6) & 3;
@@ -190,37 +253,15 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                     ha::release_reads();
                     ha::fence_smem_to_async();
                 }
-                __syncwarp();
-                if (lane == 0 && ok) ha::bar_arrive(bars + 8 * (kFreeRaw + rs));
-                if (tid == 0 && slab == 0) ha::tma_store_wait_read();  // the chunk before has left the second buffer
-                ok = team_sync(ok);
-                if (!ok) break;
-                if (warp == 0 && ha::elect_one()) {
-                    constexpr uint32_t wide_shape = ha::mma_shape(KP, ha::kColMajorB), near_shape = ha::mma_shape(C, 0);
-                    const uint32_t from = base + L::ops + buf * L::op;
-                    ha::tmem_after_sync();
-                    if (slab == 0) {
-                        const uint32_t rows = ha::operand(base + ts * L::tiles_bytes, 0);
-#pragma unroll
-                        for (int kk = 0; kk < KP / 16; ++kk) {
-                            const uint32_t step = (kk >> 2) * (L::block >> 4) + (kk & 3) * 2;
-                            mma_tile<ha::kSwizzled, ha::kSwizzled>(L::tr, rows + step, rows + step + (C * 128 >> 4), near_shape, kk > 0);
-                        }
-                    }
-                    const uint32_t az = ha::operand(from + L::az, 0), vo = ha::operand(from + L::v, 0), so = ha::operand(from + L::s, 2048),
-                                   dd = ha::operand(from + L::d, 2048);
-#pragma unroll
-                    for (int level = TM - 1; level >= 0; --level)
-#pragma unroll
-                        for (int u = 0; u <= level; ++u) {
-                            const bool more = slab > 0 || level < TM - 1 || u > 0;
-                            mma_tile<kRows32, ha::kSwizzled>(L::ta, az + u * (L::az_term >> 4), so + (level - u) * (L::s_term >> 4), wide_shape, more);
-                            mma_tile<kRows32, kRows32>(L::tg, az + u * (L::az_term >> 4), vo + (level - u) * (L::v_term >> 4), near_shape, more);
-                        }
-#pragma unroll
-                    for (int u = 1; u >= 0; --u)  // rows 64..127 are V' (above them is what lies before it: those sums are not used)
-                        mma_tile<kRows32, ha::kSwizzled>(L::tl, vo + u * (L::v_term >> 4) - (C * 32 >> 4), dd, wide_shape, slab > 0 || u == 0);
-                    ha::mma_commit(bars + 8 * (kDone + buf));
+                ok = __all_sync(~0u, ok);
+                ha::tmem_before_sync();  // (slab 0: the chunk before has been read from tensor memory)
+                if (lane == 0 && ok) {
+                    ha::bar_arrive(bars + 8 * (kFreeRaw + rs));
+                    ha::bar_arrive(bars + 8 * (kReady + buf));
+                }
+                if (tid == 0 && slab == 0 && tiles > 1) {
+                    ha::tma_store_wait_read();
+                    if (ok) ha::bar_arrive(bars + 8 * kOutFree);
                 }
                 __syncwarp();
                 issued[buf] += 1;
@@ -268,8 +309,10 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                 for (int e = 0; e < 16; ++e) x[e] = own_w[e] = 0.0f;
                 if (col <= ((row & 32) | 31)) {  // as far as the warp's last row
                     uint32_t g[16], r[16];
-                    ha::tmem_ld16(g, lanes + L::tg + col);
-                    ha::tmem_ld16(r, lanes + L::tr + col);
+                    ha::tmem_ld16_early(g, lanes + L::tg + col);
+                    ha::tmem_ld16_early(r, lanes + L::tr + col);
+                    ha::tmem_ready(g);
+                    ha::tmem_ready(r);
                     if (col + 15 < (row & 32)) {  // before all rows of the warp: one exponential for a row (as in chunk_kernel)
                         const int m = col + 15;
                         const float f = on ? (key ? -1.0f : p.scale) * ex2((hi - vec[I::hi / 4 + m]) + (lo - vec[I::lo / 4 + m])) : 0.0f;
@@ -315,23 +358,9 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
             ha::tmem_wait_st();
             ha::fence_smem_to_async();
             ha::tmem_before_sync();
-            team_sync(true);
-            if (warp == 0 && ha::elect_one()) {
-                ha::tmem_after_sync();
-                constexpr uint32_t shape = ha::mma_shape(KP, ha::kColMajorB), shape_t = ha::mma_shape(KP, ha::kColMajorA | ha::kColMajorB);
-                const uint32_t q = ha::operand(base + ts * L::tiles_bytes, L::block), k = ha::operand(base + ts * L::tiles_bytes + C * 128, L::block);
-#pragma unroll
-                for (int u = 1; u >= 0; --u)
-#pragma unroll
-                    for (int kk = 0; kk < C / 16; ++kk) {
-                        mma_tile<ha::kSwizzled, ha::kSwizzled>(L::ta, ha::operand(base + L::h + u * L::h_term, 0) + kk * 2, k + kk * 128, shape, true);
-                        // [0; H^T]: from the zeros the second 64 rows lie as far as H does
-                        mma_tile<ha::kSwizzled, ha::kSwizzled>(L::ta, ha::operand(base + L::zero, L::h - L::zero + u * L::h_term) + kk * 128, q + kk * 128, shape_t, true);
-                        mma_tile<ha::kSwizzled, ha::kSwizzled>(L::ta, ha::operand(base + L::zero, L::h - L::zero + u * L::h_term + C * 128) + kk * 128, k + kk * 128, shape_t, true);
-                    }
-                ha::mma_commit(bars + 8 * kStep);
-            }
             __syncwarp();
+            if (lane == 0) ha::bar_arrive(bars + 8 * kNear);
+            team_sync(true);
             if (key)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) wm[i * (C + 1) + 16 * quarter + e] += own_w[e];
@@ -430,7 +459,7 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                     }
                 }
             }
-            ok = team_sync(wait(kStep, steps++));
+            ok = team_sync(wait(kStep, tiles - 1));
             if (!ok) break;
             ha::tmem_after_sync();
             {
@@ -443,8 +472,10 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                 for (int x = 0; x < KP / 64; ++x) {
                     const int col = quarter * (KP / 4) + 16 * x;
                     uint32_t v[16], l[16];
-                    ha::tmem_ld16(v, lanes + L::ta + col);
-                    ha::tmem_ld16(l, lanes + L::tl + col);
+                    ha::tmem_ld16_early(v, lanes + L::ta + col);
+                    if (key) ha::tmem_ld16_early(l, lanes + L::tl + col);
+                    ha::tmem_ready(v);
+                    if (key) ha::tmem_ready(l);
                     float y[16];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) y[e] = !on ? 0.0f : key && late != 0.0f ? fmaf(late, __uint_as_float(l[e]), __uint_as_float(v[e])) : __uint_as_float(v[e]);
@@ -481,11 +512,6 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
             }
         }
         if (tid == 0) ha::tma_store_wait_all();
-        if (!ok) {  // what was issued may still run
-            if (issued[0]) wait.drain(kDone, issued[0] - 1);
-            if (issued[1]) wait.drain(kDone + 1, issued[1] - 1);
-            if (steps) wait.drain(kStep, steps - 1);
-        }
     }
     ha::tmem_before_sync();
     __syncthreads();
