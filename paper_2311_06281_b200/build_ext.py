@@ -11,7 +11,7 @@ CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libheinsen_scan.so")
 SOURCES = ["heinsen_scan.cu", "heinsen_attention.cu", "heinsen_norms.cu", "heinsen_delta.cu", "heinsen_delta_backward.cu", "heinsen_beam.cu"]
 HEADERS = ["hs_device.cuh", "hs_kernels.cuh", "hs_pairs.cuh", "hs_internal.h", "ha_common.cuh", "ha_host.h", "ha_ptx.cuh", "ha_simt.cuh", "ha_mma.cuh", "hn_norms.cuh", "hd_warp.cuh",
-           "hd_scan.cuh", "hd_grad.cuh", "hd_grad_mma.cuh", "hd_step.cuh", "hb_beam.cuh", "hd_host.h",
+           "hd_scan.cuh", "hd_scan_mma.cuh", "hd_grad.cuh", "hd_grad_mma.cuh", "hd_step.cuh", "hb_beam.cuh", "hd_host.h",
            os.path.join("..", "..", "include", "heinsen_scan.h"), os.path.join("..", "..", "include", "heinsen_attention.h"),
            os.path.join("..", "..", "include", "heinsen_delta.h"),
            os.path.join("..", "..", "include", "heinsen_beam.h")]

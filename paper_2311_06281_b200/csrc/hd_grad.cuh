@@ -19,8 +19,8 @@ __global__ void __launch_bounds__(kScanThreads, 1)
     back_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mg,
                 const __grid_constant__ CUtensorMap mo, const Params p, int* gave_up) {
     constexpr int TP = TM;
-    using L = ScanLayout<KP, C, TI, TM, TP, true>;
-    using I = Image<C, TM, TP>;
+    using L = ScanLayout<KP, C, TI, TM, TP, true, true>;
+    using I = typename L::I;
     constexpr int kLevel = TM - 1, kGroup = TI == 1 && C == 64 ? 4 : 2;
     constexpr bool kRounded = TI == 3;
     extern __shared__ __align__(1024) uint8_t sm8[];
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int u = 0; u < TP; ++u)
-                            if (g < pairs) load4_t(bf[g][u], P + u * I::plane + block_place(jj, np + g, at.bt_row(), at.bt_piece()));
+                            if (g < pairs) load4_t(bf[g][u], P + u * I::plane + in_block(I::p_block(jj, np + g), at.bt_row(), at.bt_piece()));
                     sum<kRounded, kLevel>(y + 2 * np, a, bf, pairs);
                 }
             }
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int u = 0; u < TM; ++u)
-                            if (g < pairs) load4_t(bf[g][u], N + u * I::plane + block_place(jj, np + g, at.bt_row(), at.bt_piece()));
+                            if (g < pairs) load4_t(bf[g][u], N + u * I::plane + in_block(Blocks<C>::by_columns(jj, np + g), at.bt_row(), at.bt_piece()));
                     sum<kRounded, kLevel>(y + 2 * np, a, bf, pairs);
                 }
             }
@@ -247,7 +247,7 @@ struct GradLayout {
     static constexpr uint32_t slab = 2 * tile, g = slab, own = C * 32, v = g + SL / 16 * TI * own, z = v + TM * SL * C * 2, s = z + TM * SL * C * 2,
                               d = s + TM * SL * KP * 2, slab_end = d + TD * SL * KP * 2;
     static constexpr uint32_t plane = C * C * 2, hd = slab, hz = hd + TH * plane, w = hz + TH * plane, h_end = w + C * (C + 1) * 4;
-    static constexpr uint32_t vec = (slab_end > h_end ? slab_end : h_end), far = vec + 6 * C * 4 + 128, sums = far + 8 * C * 4, bars = sums + 64 * 4,
+    static constexpr uint32_t vec = (slab_end > h_end ? slab_end : h_end), far = vec + 6 * C * 4 + 256, sums = far + 8 * C * 4, bars = sums + 64 * 4,
                               end = bars + 64;
 };
 
@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     grad_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mg, const Params p,
                 int* gave_up) {
     using L = GradLayout<KP, C, TI, TM>;
-    using I = Image<C, TM, TM>;
+    using I = Image<C, TM, TM, true>;
     constexpr int kLevel = TM - 1, TD = L::TD, TH = L::TH, SL = L::SL;
     constexpr bool kRounded = TI == 3;
     constexpr int kRowBlocks = C / 16, kColumnBlocks = 8 / kRowBlocks, kCols = KP / kColumnBlocks, kPairs = kCols / 16;

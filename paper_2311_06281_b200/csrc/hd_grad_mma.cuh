@@ -11,16 +11,9 @@
 // issues the products, the others have a row of a product and a quarter of its columns each.
 #pragma once
 #include "hd_grad.cuh"
+#include "hd_scan_mma.cuh"
 
 namespace hd {
-
-constexpr uint32_t kRows32 = (256u >> 4) | (1u << 14) | (6u << 29);  // operands of 32-byte rows (16 bf16 along k), swizzled so
-template <uint32_t kA, uint32_t kB>
-__device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %6, 0;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}" ::"r"(d), "r"(a), "r"(kA), "r"(b), "r"(kB), "r"(shape), "r"((uint32_t)add)
-                 : "memory");
-}
 
 constexpr int kGradMmaThreads = 576;  // sixteen warps that compute, one that loads, one that issues the products
 constexpr int kTeam = 512;
@@ -34,7 +27,7 @@ __device__ __forceinline__ bool team_sync(bool mine) {
 
 template <int KP> struct GradMmaLayout {
     static constexpr int C = 64, kTiles = 2, kRaw = 3;
-    using I = Image<C, 3, 3>;
+    using I = Image<C, 3, 3, true>;
     static constexpr uint32_t block = 2 * C * 128, tiles_bytes = KP / 64 * block;  // blocks of 64 columns: rows of Q, then of K
     // two operand buffers, of sixteen columns of V each: three terms of [dO; Z] (the lower terms of dO zero), of V', of S; one of D
     static constexpr uint32_t ops = kTiles * tiles_bytes;
@@ -49,7 +42,7 @@ template <int KP> struct GradMmaLayout {
     static constexpr uint32_t raw_at = raw > (w_end + 1023) / 1024 * 1024 ? raw : (w_end + 1023) / 1024 * 1024;
     static constexpr uint32_t vec = raw_at + kRaw * raw_bytes, far = vec + kTiles * I::n, sums = far + 16 * C * 4, bars = sums + 256, end = bars + 192;
     static constexpr uint32_t ta = 0, tl = KP, tg = 2 * KP, tr = 2 * KP + C, columns = 512;
-    static_assert(tr + C <= columns && s % 1024 == 0 && s_term % 1024 == 0 && raw_bytes % 1024 == 0 && I::n % 128 == 0, "layout");
+    static_assert(tr + C <= columns && s % 1024 == 0 && s_term % 1024 == 0 && raw_bytes % 1024 == 0 && I::n % 256 == 0, "layout");
     static_assert(out + KP / 64 * 2 * C * 128 <= raw_at, "the way out");
 };
 
@@ -219,7 +212,7 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                     for (int e = tid; e < rows * 8; e += kTeam) *reinterpret_cast<uint4*>(kq + block + (c.live - c.t0) * 128 + e * 16) = make_uint4(0, 0, 0, 0);
             }
             // for the first 2 C threads: the slices' parts of dbeta, and of what crosses into later chunks
-            const float* const dots = p.dots + (long long)at * 2 * slices * C + (tid >> 6) * (slices * C) + (tid & 63);
+            const float* const dots = p.dots + (long long)at * 2 * p.parts * C + (tid >> 6) * (p.parts * C) + (tid & 63);
             float part[8], cross = 0.0f;
             for (int slab = 0; slab < slices; ++slab, ++used) {
                 const int buf = slab & 1, rs = used % L::kRaw;
@@ -230,15 +223,15 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                 if (slab == 1 && tiles > 1) ok = ok && wait(kOutFree, tiles - 2);  // what the chunk before sent from there has left
                 ok = ok && wait(kFullRaw + rs, used / L::kRaw);
                 if (ok) {
-                    const int token = tid & 63, quad = (tid >> 6) & 3;
+                    const int token = (tid >> 2) & 63, quad = tid & 3;
                     const uint32_t piece = place<32>(token, quad >> 1) + 8 * (quad & 1);
                     const float be = vec[I::beta / 4 + token];
-                    const float* const from = reinterpret_cast<const float*>(raw + (tid < 256 ? L::raw_f : L::raw_e)) + 4 * quad * C + token;
-                    const float4 x = make_float4(be * from[0], be * from[C], be * from[2 * C], be * from[3 * C]);
+                    const float4 f4 = *reinterpret_cast<const float4*>(raw + (tid < 256 ? L::raw_f : L::raw_e) + token * 64 + quad * 16);
+                    const float4 x = make_float4(be * f4.x, be * f4.y, be * f4.z, be * f4.w);
                     if (tid < 256) put_terms<TM>(to + L::az + C * 32, L::az_term, x, piece);
                     else put_terms<TM>(to + L::v, L::v_term, x, piece);
                     if (KP == 128 || tid < 256) {
-                        const int r = tid / (KP / 4), col = 4 * (tid % (KP / 4));
+                        const int r = tid & 15, col = tid >> 4 << 2;
                         const float4 s4 = reinterpret_cast<const float4*>(raw)[tid], d4 = reinterpret_cast<const float4*>(raw + L::raw_d)[tid];
                         const uint32_t sat = wide<16>(r, col >> 3) + 2 * (col & 7);
                         put_terms<TM>(to + L::s, L::s_term, s4, sat);
@@ -267,7 +260,7 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                 issued[buf] += 1;
                 if (slab == 0 && tid < 2 * C)
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) part[u] = u < slices ? dots[u * C] : 0.0f;
+                    for (int u = 0; u < 8; ++u) part[u] = u < p.parts ? dots[u * C] : 0.0f;
             }
             ok = ok && wait(kDone, issued[0] - 1) && (slices == 1 || wait(kDone + 1, issued[1] - 1));
             ok = team_sync(ok);
@@ -369,7 +362,7 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                 if (tid < 2 * C) {
 #pragma unroll
                     for (int u = 0; u < 8; ++u) sum += part[u];
-                    for (int u = 8; u < slices; ++u) sum += dots[u * C];
+                    for (int u = 8; u < p.parts; ++u) sum += dots[u * C];
                 }
                 if (tid < C && p.dbeta && c.t0 + tid < p.tokens) p.dbeta[row0 + (long long)tid * p.heads] = c.t0 + tid < c.live ? sum : 0.0f;
                 if (p.dlog_a || p.part) {

@@ -4,7 +4,7 @@
 
 #include "../../include/heinsen_delta.h"
 #include "ha_host.h"
-#include "hd_scan.cuh"
+#include "hd_scan_mma.cuh"
 
 #ifndef HD_MID
 #define HD_MID 3
@@ -101,7 +101,7 @@ inline long long chunks_of(const heinsen_attention_problem* p) {
     const int c = hd::chunk_tokens(width_of(p->k_dim));
     return p->batch * p->heads * ((p->tokens + c - 1) / c);
 }
-template <int C, int TM, int TP> size_t image_bytes(const heinsen_attention_problem* p) { return up256((size_t)chunks_of(p) * hd::Image<C, TM, TP>::end); }
+template <int C, int TM, int TP, bool kBack> size_t image_bytes(const heinsen_attention_problem* p) { return up256((size_t)chunks_of(p) * hd::Image<C, TM, TP, kBack>::end); }
 
 // Warps of a CTA of the scans, sixteen columns each: as many as one SM can have while there are CTAs for all SMs, since a CTA
 // loads K, Q, N and P for all of its warps.
@@ -111,10 +111,10 @@ inline int warps_for(long long pairs, int slices) {
     return warps;
 }
 
-template <int KP, int C, int TI, int TM, int TP>
+template <int KP, int C, int TI, int TM, int TP, bool kBack>
 hs_status launch_chunks(const CUtensorMap& mq, const CUtensorMap& mk, const hd::Params& q, int* word, cudaStream_t stream) {
-    using L = hd::ChunkLayout<KP, C, TI, TM, TP>;
-    const auto fn = hd::chunk_kernel<KP, C, TI, TM, TP>;
+    using L = hd::ChunkLayout<KP, C, TI, TM, TP, kBack>;
+    const auto fn = hd::chunk_kernel<KP, C, TI, TM, TP, kBack>;
     static std::atomic<unsigned long long> done{0};
     const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end, done);
     if (st != HS_OK) return st;
@@ -125,7 +125,7 @@ hs_status launch_chunks(const CUtensorMap& mq, const CUtensorMap& mk, const hd::
 template <int KP, int C, int TI, int TM, int TP, bool kOut, class T>
 hs_status launch_scan(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo, const hd::Params& q, int* word,
                       cudaStream_t stream) {
-    using L = hd::ScanLayout<KP, C, TI, TM, TP, kOut>;
+    using L = hd::ScanLayout<KP, C, TI, TM, TP, kOut, !kOut>;
     static_assert(L::end(hd::kMaxWarps) <= 232448, "shared memory");
     const auto fn = hd::scan_kernel<KP, C, TI, TM, TP, kOut, T>;
     static std::atomic<unsigned long long> done{0};
@@ -139,6 +139,23 @@ hs_status launch_scan(const CUtensorMap& mq, const CUtensorMap& mk, const CUtens
     w.warps = warps;
     fn<<<(unsigned)grid, 32 * (hd::loader_of(warps) + 4), L::end(warps), stream>>>(mq, mk, mv, mo, w, word);
     return launched("scan_kernel");
+}
+
+// Whether the passes run on tcgen05: bf16 and keys up to 128 wide.
+template <int KP, int TI> constexpr bool on_tcgen05() { return TI == 1 && KP <= 128; }
+
+template <int KP, int kMode, class T>
+hs_status launch_pass(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const hd::Params& q, int* word, cudaStream_t stream) {
+    using L = hd::PassLayout<KP, kMode>;
+    static_assert(L::end <= 232448, "shared memory");
+    const auto fn = hd::pass_kernel<KP, kMode, T>;
+    static std::atomic<unsigned long long> done{0};
+    const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end, done);
+    if (st != HS_OK) return st;
+    const long long grid = (long long)q.batch * q.heads * ((q.dv + 127) / 128);
+    if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
+    fn<<<(unsigned)grid, hd::kPassThreads, L::end, stream>>>(mq, mk, mv, q, word);
+    return launched("pass_kernel");
 }
 
 }  // namespace hd_host

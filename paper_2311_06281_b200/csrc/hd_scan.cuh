@@ -57,9 +57,10 @@ struct Params {
     int out_tma;
     float* states;         // backward: before every chunk the state (after it, its gradient), [batch * heads][chunks][16 slices][KP]
     float* errors;         // E (F) of every chunk, [batch * heads][chunks][16 slices][C]
-    float* errors_back;    // F likewise
+    float* errors_back;    // F likewise (layouts of the tensor-core passes: hd_scan_mma.cuh)
+    int parts;             // of the sums over V in `dots`
     float* gradients;      // the gradient of the state after every chunk, as `states`
-    float* dots;           // [batch * heads][chunks][2][slices][C]: by slice of V, dbeta and e^{c_C-c_j} k_j^T D V'_j
+    float* dots;           // [batch * heads][chunks][2][parts][C]: by part of V, dbeta and e^{c_C-c_j} k_j^T D V'_j
     void *dq, *dk_out;       // contiguous [batch, tokens, heads, dk]; in float32 where each_ says so (heads to be summed)
     int each_q, each_k, dq_tma, dk_tma;
     float *dlog_a, *dbeta; // [batch, tokens, heads], or NULL
@@ -81,21 +82,29 @@ __device__ __forceinline__ void give_up(const Params& p, int* gave_up, int where
 
 template <int kValue> struct Int { static constexpr int value = kValue; };
 
-// The blocks of 16 x 16 on and below the diagonal of a C x C matrix, row by row, each 16 rows of 32 bytes.
-__host__ __device__ constexpr int block_of(int i, int j) { return i * (i + 1) / 2 + j; }
-__device__ __forceinline__ uint32_t block_place(int i, int j, int row, int piece) { return block_of(i, j) * 512 + place<32>(row, piece); }
+// The blocks of 16 x 16 on and below the diagonal of a C x C matrix, each 16 rows of 32 bytes: row by row of them, or column by column
+// (an operand whose sums run along its rows takes a column of blocks at a time, one whose sums run along its columns a row).
+template <int C> struct Blocks {
+    static constexpr int kAlong = C / 16, kCount = kAlong * (kAlong + 1) / 2;
+    static __host__ __device__ constexpr int by_rows(int i, int j) { return i * (i + 1) / 2 + j; }
+    static __host__ __device__ constexpr int by_columns(int i, int j) { return j * kAlong - j * (j - 1) / 2 + (i - j); }
+};
+__device__ __forceinline__ uint32_t in_block(int block, int row, int piece) { return block * 512 + place<32>(row, piece); }
 
-// What chunk_kernel writes: six vectors over the tokens and the decay of the whole chunk; the blocks of N; those of P; as bf16 terms.
-template <int C, int kTermsN, int kTermsP> struct Image {
+// What chunk_kernel writes: six vectors over the tokens and the decay of the whole chunk; the blocks of N by columns, kBack by rows as
+// well; those of P, by columns, kBack by rows; as bf16 terms.
+template <int C, int kTermsN, int kTermsP, bool kBack> struct Image {
     // e^{c}, e^{c_C-c}, beta, c in two parts, e^{c_m-c} with m the last of the token's sixteen; the whole chunk's decay and its logarithm
     static constexpr uint32_t early = 0, late = C * 4, beta = 2 * C * 4, hi = 3 * C * 4, lo = 4 * C * 4, edge = 5 * C * 4, whole = 6 * C * 4;
-    static constexpr uint32_t n = 6 * C * 4 + 128, plane = block_of(C / 16, 0) * 512, p = n + kTermsN * plane, end = p + kTermsP * plane;
-    static_assert(n % 128 == 0 && end % 128 == 0, "alignment");
+    static constexpr uint32_t plane = Blocks<C>::kCount * 512, n = 6 * C * 4 + 256, rows = n + kTermsN * plane, p = rows + (kBack ? kTermsN * plane : 0),
+                              end = p + kTermsP * plane;
+    static_assert(n % 256 == 0 && plane % 256 == 0, "the swizzle of 32-byte rows repeats every 256 bytes");
+    static __device__ __forceinline__ int p_block(int i, int j) { return kBack ? Blocks<C>::by_rows(i, j) : Blocks<C>::by_columns(i, j); }
 };
 
-template <int KP, int C, int TI, int TM, int TP>
+template <int KP, int C, int TI, int TM, int TP, bool kBack>
 struct ChunkLayout {
-    using I = Image<C, TM, TP>;
+    using I = Image<C, TM, TP, kBack>;
     // for each term and block of 64 columns the rows of K, then those of Q; the tensor core reads 128 rows from the first of a block
     static constexpr uint32_t block = 2 * C * 128, tile = TI * (KP / 64) * block, reads = tile + 128 * 128 - block;
     // M in three terms, then N, where K and Q were
@@ -110,11 +119,11 @@ struct ChunkLayout {
 // inverts a diagonal block of I + M beta, and solves for 16 columns of N, transposed, block by block of rows,
 //     N_iw = (I + M_ii beta_i)^{-1} (M_iw - sum_{w<=s<i} M_is beta_s N_sw),
 // every N^T_sw the next product's factor in its registers.  24 bits in all of it: a wrong N is wrong for every column of V.
-template <int KP, int C, int TI, int TM, int TP>
+template <int KP, int C, int TI, int TM, int TP, bool kBack>
 __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const Params p,
                                                       int* gave_up) {
-    using L = ChunkLayout<KP, C, TI, TM, TP>;
-    using I = Image<C, TM, TP>;
+    using L = ChunkLayout<KP, C, TI, TM, TP, kBack>;
+    using I = Image<C, TM, TP, kBack>;
     constexpr int NB = C / 16;
     extern __shared__ __align__(1024) uint8_t sm8[];
     const uint32_t base = smem_addr(sm8), bars = base + L::bars;
@@ -262,7 +271,7 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
                         for (int u = 0; u < 4; ++u) diag[(e + u) * 16] = x[e + u];
                 }
             }
-            auto put = [&](auto terms, uint8_t* to) {
+            auto put = [&](auto terms, uint8_t* to, int block) {
                 constexpr int kTerms = decltype(terms)::value;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
@@ -271,11 +280,11 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
                     for (int u = 0; u < 4; ++u) ha::split<kTerms>(ha::make_pair2(x[8 * half + 2 * u], x[8 * half + 2 * u + 1]), t[u]);
 #pragma unroll
                     for (int u = 0; u < kTerms; ++u)
-                        *reinterpret_cast<uint4*>(to + u * I::plane + block_place(ib, jb, i & 15, half)) = make_uint4(t[0][u], t[1][u], t[2][u], t[3][u]);
+                        *reinterpret_cast<uint4*>(to + u * I::plane + in_block(block, i & 15, half)) = make_uint4(t[0][u], t[1][u], t[2][u], t[3][u]);
                 }
             };
-            if (mine_p) put(Int<TP>{}, image + I::p);
-            else put(Int<3>{}, sm8 + L::m);
+            if (mine_p) put(Int<TP>{}, image + I::p, I::p_block(ib, jb));
+            else put(Int<3>{}, sm8 + L::m, Blocks<C>::by_rows(ib, jb));
         }
     }
     ha::tmem_before_sync();
@@ -324,7 +333,7 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
                 uint32_t m[4];
 #pragma unroll
                 for (int u = 2; u >= 0; --u) {
-                    load4_t(m, base + L::m + u * I::plane + block_place(i, warp, at.b_row(), at.b_piece()));
+                    load4_t(m, base + L::m + u * I::plane + in_block(Blocks<C>::by_rows(i, warp), at.b_row(), at.b_piece()));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         r[e >> 1][2 * (e & 1)] += __uint_as_float(m[e] << 16);
@@ -338,7 +347,7 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
             for (int s = 0; s < i; ++s)
                 if (s >= warp)
 #pragma unroll
-                    for (int u = 0; u < 3; ++u) load4(bf[s][0][u], base + L::m + u * I::plane + block_place(i, s, at.b_row(), at.b_piece()));
+                    for (int u = 0; u < 3; ++u) load4(bf[s][0][u], base + L::m + u * I::plane + in_block(Blocks<C>::by_rows(i, s), at.b_row(), at.b_piece()));
 #pragma unroll
             for (int level = 2; level >= 0; --level)
 #pragma unroll
@@ -373,12 +382,22 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
             as_operand<3>(a, x[0], x[1]);
 #pragma unroll
             for (int u = 0; u < TM; ++u)  // in the order in which M^T was loaded
-                store4_t(base + L::n + u * I::plane + block_place(i, warp, at.b_row(), at.b_piece()), a[u]);
+                store4_t(base + L::n + u * I::plane + in_block(Blocks<C>::by_columns(i, warp), at.b_row(), at.b_piece()), a[u]);
         }
     __syncthreads();
     uint4* to = reinterpret_cast<uint4*>(image);
     for (uint32_t e = tid; e < I::n / 16; e += 2 * C) to[e] = reinterpret_cast<const uint4*>(sm8 + L::vec)[e];
-    for (uint32_t e = tid; e < (I::p - I::n) / 16; e += 2 * C) to[I::n / 16 + e] = reinterpret_cast<const uint4*>(sm8 + L::n)[e];
+    for (uint32_t e = tid; e < (I::rows - I::n) / 16; e += 2 * C) {
+        const uint4 f = reinterpret_cast<const uint4*>(sm8 + L::n)[e];
+        to[I::n / 16 + e] = f;
+        if constexpr (kBack) {
+            const int block = e / 32 % Blocks<C>::kCount;
+            int j = 0;
+            while (j + 1 < NB && block >= Blocks<C>::by_columns(j + 1, j + 1)) ++j;
+            const int i = block - Blocks<C>::by_columns(j, j) + j;
+            to[I::rows / 16 + e + (Blocks<C>::by_rows(i, j) - block) * 32] = f;
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------- scan
@@ -391,12 +410,12 @@ static_assert(2 * kColumnRegs + kLoadRegs <= 3 * 168 && kScanThreads * 168 <= 65
 __host__ __device__ constexpr int loader_of(int warps) { return (warps + 3) / 4 * 4; }
 
 // kQ: a tile of Q and the weights P
-template <int KP, int C, int TI, int TM, int TP, bool kQ>
+template <int KP, int C, int TI, int TM, int TP, bool kQ, bool kBack>
 struct ScanLayout {
-    using I = Image<C, TM, TP>;
+    using I = Image<C, TM, TP, kBack>;
     static constexpr int kStages = TI == 1 ? 2 : 1;
     static constexpr uint32_t tile = KP * C * 2 * TI, k = 0, q = tile, v = q + (kQ ? tile : 0), own = C * 32;  // V: 16 columns for each warp
-    static constexpr uint32_t image_bytes = kQ ? I::end : I::p;
+    static constexpr uint32_t image_bytes = kQ ? I::end : I::rows;
     static __host__ __device__ constexpr uint32_t image(int warps) { return v + warps * TI * own; }
     static __host__ __device__ constexpr uint32_t stage(int warps) { return (image(warps) + image_bytes + 1023) / 1024 * 1024; }
     // stages, the output's staging (16 columns for each warp, bf16), barriers
@@ -538,8 +557,8 @@ template <int KP, int C, int TI, int TM, int TP, bool kOut, class T>
 __global__ void __launch_bounds__(kScanThreads, 1)
     scan_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                 const __grid_constant__ CUtensorMap mo, const Params p, int* gave_up) {
-    using L = ScanLayout<KP, C, TI, TM, TP, kOut>;
-    using I = Image<C, TM, TP>;
+    using L = ScanLayout<KP, C, TI, TM, TP, kOut, !kOut>;
+    using I = typename L::I;
     constexpr int kLevel = TM - 1, TO = TI == 1 ? 2 : 3, kGroup = TI == 1 && C == 64 ? 4 : 2;
     constexpr bool kRounded = TI == 3;
     extern __shared__ __align__(1024) uint8_t sm8[];
@@ -664,7 +683,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
                     for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int u = 0; u < TM; ++u)
-                            if (g < pairs) load4(bf[g][u], N + u * I::plane + block_place(np + g, jj, at.b_row(), at.b_piece()));
+                            if (g < pairs) load4(bf[g][u], N + u * I::plane + in_block(Blocks<C>::by_columns(np + g, jj), at.b_row(), at.b_piece()));
                     sum<kRounded, kLevel>(y + 2 * np, a, bf, pairs);
                 }
             }
@@ -689,7 +708,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
                         for (int g = 0; g < 2; ++g)
 #pragma unroll
                             for (int u = 0; u < TP; ++u)
-                                if (g < pairs) load4(bf[g][u], P + u * I::plane + block_place(np + g, jj, at.b_row(), at.b_piece()));
+                                if (g < pairs) load4(bf[g][u], P + u * I::plane + in_block(I::p_block(np + g, jj), at.b_row(), at.b_piece()));
                         sum<kRounded, TO - 1>(o + 2 * np, a, bf, pairs);
                     }
                 }

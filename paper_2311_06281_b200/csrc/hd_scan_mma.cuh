@@ -1,0 +1,513 @@
+// scan_kernel and back_kernel (hd_scan.cuh, hd_grad.cuh) on tcgen05: bf16, keys up to 128 wide, chunks of 64 tokens.
+//
+// A CTA has 128 columns of the values and all of the state's rows for them, S^T in registers (two threads to a column of V), and
+// walks the chunks.  Everything is formed transposed, columns of V as rows of the tensor core's tiles:
+//     X = S^T K^T,   Y = V^T - X e^c,   E = Y + (-beta Y) N^T,   S^T <- e^{c_C} S^T + (e^{c_C-c} beta E) K
+// Left factors go from registers to tensor memory as bf16 terms, three for what the state hangs on (24 bits), sums come back from there;
+// V^T is brought there by products with an identity.  Backward likewise from D^T:
+//     X = D^T K^T,   dV'^T = X e^{c_C-c} + dO^T P,   F = dV'^T + (-beta dV'^T) N,   Z = beta F
+//     D^T <- e^{c_C} D^T + (-e^c Z) K + (scale e^c dO^T) Q
+// Warps 0-7 have the state and the chain of dependent steps; warps 8-11 what hangs on it without the chain waiting: the output
+// (backward: dV, F and the sums over V for the gates, and the terms of dO).  One warp loads, a chunk ahead, one issues the products.
+#pragma once
+#include "hd_scan.cuh"
+
+namespace hd {
+
+constexpr int kPassThreads = 512;
+// Registers: 128 a thread at launch; 2 * 152 + 128 + 80 = 4 * 128.
+constexpr int kPassState = 152, kPassSide = 128, kPassFeed = 80;
+static_assert(2 * kPassState + kPassSide + kPassFeed <= 4 * 128, "registers");
+
+constexpr uint32_t kRows32 = (256u >> 4) | (1u << 14) | (6u << 29);  // operands of 32-byte rows, swizzled so
+template <uint32_t kA, uint32_t kB>
+__device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %6, 0;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}" ::"r"(d), "r"(a), "r"(kA), "r"(b), "r"(kB), "r"(shape), "r"((uint32_t)add)
+                 : "memory");
+}
+// The same with the left factor in tensor memory
+template <uint32_t kB>
+__device__ __forceinline__ void mma_left(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(kB), "r"(shape), "r"((uint32_t)add)
+                 : "memory");
+}
+
+// Tensor memory, in columns.  The update shares columns with the state's terms, V' (backward: dO) with X, and the later of two
+// factors with the earlier: each is written when the products that read the other are done.
+struct PassColumns {
+    static constexpr uint32_t s = 0, x = 192, y = 256, o = 320, f = 384, g = 480, columns = 512;
+    // term t of sixteen rows q of a thread's half of the state: its first two terms lie where its own half of the update will
+    static __device__ __forceinline__ constexpr uint32_t state(int half, int q, int t) { return t < 2 ? s + half * 64 + q * 16 + t * 8 : s + 128 + half * 32 + q * 8; }
+    static __device__ __forceinline__ constexpr uint32_t factor(int jj, int t) { return f + 24 * jj + 8 * t; }
+    static __device__ __forceinline__ constexpr uint32_t value(int jj, int t) { return x + 16 * jj + 8 * t; }
+    static __device__ __forceinline__ constexpr uint32_t outer(int jj, int t) { return t < 2 ? value(jj, t) : g + 8 * jj; }
+};
+
+// kMode 0: the output; 1: the states before the chunks and E for the gradients; 2: backward
+template <int KP, int kMode>
+struct PassLayout {
+    static constexpr int C = 64, kStages = 2;
+    using I = Image<C, 3, kMode == 0 ? 1 : 3, kMode != 0>;
+    static constexpr uint32_t block = C * 128, tile = KP / 64 * block;
+    static constexpr uint32_t k = 0, q = tile, v = kMode == 1 ? tile : 2 * tile, image = v + 2 * block;  // V (backward: dO): 128 columns
+    // backward N is wanted by rows
+    static constexpr uint32_t n = image + I::n, p = n + 3 * I::plane, stage = (p + (kMode == 0 ? I::plane : kMode == 2 ? 3 * I::plane : 0) + 1023) / 1024 * 1024;
+    static constexpr uint32_t ident = kStages * stage, bars = ident + 512, end = bars + 256;
+    static constexpr uint32_t bytes = p + (kMode == 0 ? I::plane : kMode == 2 ? 3 * I::plane : 0);  // of a chunk
+};
+
+// Sixteen values as terms of a left factor
+template <int kTerms>
+__device__ __forceinline__ void put_left(const float (&x)[16], uint32_t (&t)[kTerms][8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        uint32_t w[kTerms];
+        ha::split<kTerms>(ha::make_pair2(x[2 * e], x[2 * e + 1]), w);
+#pragma unroll
+        for (int u = 0; u < kTerms; ++u) t[u][e] = w[u];
+    }
+}
+__device__ __forceinline__ void four(const float* from, float (&to)[16]) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(from + e);
+        to[e] = f.x; to[e + 1] = f.y; to[e + 2] = f.z; to[e + 3] = f.w;
+    }
+}
+// 32 values of each lane, summed over the warp's lanes: lane l gets the sum of the l-th ones.
+__device__ __forceinline__ float sum_across(float (&x)[32]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const bool upper = lane & o;
+#pragma unroll
+        for (int e = 0; e < o; ++e) {
+            const float keep = upper ? x[e + o] : x[e], give = upper ? x[e] : x[e + o];
+            x[e] = keep + __shfl_xor_sync(~0u, give, o);
+        }
+    }
+    return x[0];
+}
+
+enum PassBar : int { kStateReady = 5, kScores, kFactor, kSolved, kWrites, kUpdated, kFar, kFarScaled, kOut, kOutRead, kOuter = kFar, kSolvedRead = kFarScaled,
+                     kDrainPass = kOutRead + 1, kPassBars };
+
+template <int KP, int kMode, class T>
+__global__ void __launch_bounds__(kPassThreads, 1)
+    pass_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p,
+                int* gave_up) {
+    using L = PassLayout<KP, kMode>;
+    using I = typename L::I;
+    using M = PassColumns;
+    using B = Blocks<64>;
+    constexpr int C = 64, kOwn = KP / 2;
+    constexpr bool kOutput = kMode == 0, kBack = kMode == 2;
+    extern __shared__ __align__(1024) uint8_t sm8[];
+    const uint32_t base = smem_addr(sm8), bars = base + L::bars;
+    volatile int* const stop = reinterpret_cast<int*>(sm8 + L::bars + 192);
+    uint32_t* const s_tmem = reinterpret_cast<uint32_t*>(sm8 + L::bars + 200);
+    const Waiter wait{bars, stop, p.spin};
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int slabs = (p.dv + 127) / 128, bh = blockIdx.x / slabs, b = bh / p.heads, h = bh % p.heads, v0 = (blockIdx.x % slabs) * 128;
+    const int slices = (p.dv + 15) / 16, live = live_tokens(p.lengths, b, p.tokens), count = (live + C - 1) / C;
+    if (tid == 0) {
+        for (int i = 0; i < kPassBars; ++i) {
+            uint32_t arrivals = 1;
+            if (i >= kEmpty && i < kPatched) arrivals = kMode == 1 ? 9 : 13;  // the warps that read vectors, and the products
+            if (i == kStateReady || i == kFactor || i == kWrites) arrivals = 8;
+            if (i == kFarScaled || i == kOutRead || (kBack && i == kOuter)) arrivals = 4;
+            ha::bar_init(bars + 8 * i, arrivals);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        *stop = 0;
+    }
+    if (tid < 256) {  // the identity, two 8 x 8 core matrices along each of k and n
+        const int n = tid >> 4, k = tid & 15;
+        *reinterpret_cast<__nv_bfloat16*>(sm8 + L::ident + (k >> 3) * 256 + (n >> 3) * 128 + (n & 7) * 16 + (k & 7) * 2) = __float2bfloat16(n == k ? 1.0f : 0.0f);
+    }
+    ha::fence_smem_to_async();
+    if (warp == 12) ha::tmem_alloc(smem_addr(s_tmem), M::columns);
+    ha::tmem_before_sync();
+    __syncthreads();
+    ha::tmem_after_sync();
+    if (tid == 0 && *s_tmem != 0) *stop = 1 + kPassBars;  // all columns were asked for: they start at 0
+    auto chunk_at = [&](int it) { return kBack ? count - 1 - it : it; };
+    if (warp >= 12) {
+        ha::give_registers<kPassFeed>();
+        if (warp == 12) {
+            // ------------------------------------------------------------------------------------------ loads
+            load_chunks<C, L::kStages>(
+                wait, sm8, L::stage, L::image, 0, count, live, p.tokens, L::bytes, p.mute,
+                [&](int n, int s, uint32_t bar) {
+                    const uint32_t to = base + s * L::stage;
+                    const uint8_t* const image = p.image + ((long long)bh * p.chunks + n) * I::end;
+                    bulk_load(to + L::image, image, I::n, bar);
+                    bulk_load(to + L::n, image + (kBack ? I::rows : I::n), 3 * I::plane, bar);
+                    if (kMode != 1) bulk_load(to + L::p, image + I::p, (kBack ? 3 : 1) * I::plane, bar);
+                    for (int c = 0; c < KP / 64; ++c) {
+                        ha::tma_load_4d(to + L::k + c * L::block, &mk, 64 * c, h / p.kdiv, n * C, b, bar);
+                        if (kMode != 1) ha::tma_load_4d(to + L::q + c * L::block, &mq, 64 * c, h / p.qdiv, n * C, b, bar);
+                    }
+                    for (int c = 0; c < 2; ++c) ha::tma_load_4d(to + L::v + c * L::block, &mv, v0 + 64 * c, kBack ? h : h / p.vdiv, n * C, b, bar);
+                },
+                kBack);
+        } else if (warp == 13) {
+            // ------------------------------------------------------------------------------------------ products
+            if (ha::elect_one()) {
+                constexpr uint32_t shape64 = ha::mma_shape(C, 0), shape_t = ha::mma_shape(16, ha::kColMajorA), shape_u = ha::mma_shape(KP, ha::kColMajorB);
+                const uint32_t ident = ha::operand(base + L::ident, 256);
+                auto step = [](int kk) { return (uint32_t)((kk >> 2) * (L::block >> 4) + (kk & 3) * 2); };
+                // left factors of KP/16 steps, three terms of the state, with a tile of rows of tokens
+                auto with_state = [&](uint32_t d, uint32_t tile, int terms) {
+#pragma unroll
+                    for (int t = 2; t >= 0; --t)
+                        if (t < terms)
+#pragma unroll
+                            for (int kk = 0; kk < KP / 16; ++kk)
+                                mma_left<ha::kSwizzled>(d, M::state(kk / (KP / 32), kk % (KP / 32), t), tile + step(kk), shape64, !(t == terms - 1 && kk == 0));
+                };
+                auto update = [&](uint32_t tile, bool outer, bool add) {  // D += factor * tile of KP columns
+#pragma unroll
+                    for (int t = 2; t >= 0; --t)
+#pragma unroll
+                        for (int jj = 0; jj < 4; ++jj)
+                            mma_left<ha::kSwizzled>(M::s, outer ? M::outer(jj, t) : M::factor(jj, t), tile + jj * 128, shape_u, add || t < 2 || jj > 0);
+                };
+                bool ok = true;
+                for (int it = 0; it < count; ++it) {
+                    const int st = it % L::kStages;
+                    const uint32_t at = base + st * L::stage, K = ha::operand(at + L::k, L::block), Q = ha::operand(at + L::q, L::block),
+                                   V = ha::operand(at + L::v, L::block), N = ha::operand(at + L::n, 512), P = ha::operand(at + L::p, 512);
+                    if (!(ok = wait(kFull + st, it / L::kStages))) break;
+                    ha::tmem_after_sync();
+                    if constexpr (kBack) {  // dO^T P, while the state's terms are formed
+#pragma unroll
+                        for (int u = 2; u >= 0; --u)
+#pragma unroll
+                            for (int ii = 3; ii >= 0; --ii)
+                                mma_tile<ha::kSwizzled, kRows32>(M::o, V + ii * 128, P + ((u * I::plane + B::by_rows(ii, 0) * 512) >> 4),
+                                                                 ha::mma_shape(16 * (ii + 1), ha::kColMajorA | ha::kColMajorB), u < 2 || ii < 3);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) ha::mma_ss<ha::plain_layout(128)>(M::y + 16 * q, V + q * 128, ident, shape_t, false);
+                    }
+                    if (!(ok = wait(kStateReady, it))) break;
+                    ha::tmem_after_sync();
+                    with_state(M::x, K, 3);
+                    ha::mma_commit(bars + 8 * kScores);
+                    if constexpr (kOutput) {
+                        if (it > 0 && !(ok = wait(kOutRead, it - 1))) break;
+                        ha::tmem_after_sync();
+                        with_state(M::o, Q, 2);
+                        ha::mma_commit(bars + 8 * kFar);
+                    }
+                    if (!(ok = wait(kFactor, it))) break;
+                    ha::tmem_after_sync();
+#pragma unroll
+                    for (int level = 2; level >= 0; --level)
+#pragma unroll
+                        for (int u = 0; u <= level; ++u)
+#pragma unroll
+                            for (int jj = 0; jj < 4; ++jj) {
+                                if constexpr (kBack)
+                                    mma_left<kRows32>(M::y, M::factor(jj, u), N + (((level - u) * I::plane + B::by_rows(jj, 0) * 512) >> 4),
+                                                      ha::mma_shape(16 * (jj + 1), ha::kColMajorB), true);
+                                else
+                                    mma_left<kRows32>(M::y + 16 * jj, M::factor(jj, u), N + (((level - u) * I::plane + B::by_columns(jj, jj) * 512) >> 4),
+                                                      ha::mma_shape(C - 16 * jj, 0), true);
+                            }
+                    ha::mma_commit(bars + 8 * kSolved);
+                    if (!(ok = wait(kWrites, it))) break;
+                    ha::tmem_after_sync();
+                    update(K, false, false);
+                    if constexpr (kBack) {
+                        if (!(ok = wait(kOuter, it))) break;
+                        ha::tmem_after_sync();
+                        update(Q, true, true);
+                    }
+                    ha::mma_commit(bars + 8 * kUpdated);
+                    if constexpr (kOutput) {
+                        if (!(ok = wait(kFarScaled, it))) break;
+                        ha::tmem_after_sync();
+#pragma unroll
+                        for (int t = 1; t >= 0; --t)
+#pragma unroll
+                            for (int jj = 0; jj < 4; ++jj)
+                                mma_left<kRows32>(M::o + 16 * jj, M::value(jj, t), P + (B::by_columns(jj, jj) * 512 >> 4), ha::mma_shape(C - 16 * jj, 0), true);
+                        ha::mma_commit(bars + 8 * kOut);
+                    }
+                    ha::mma_commit(bars + 8 * (kEmpty + st));
+                }
+                ha::mma_commit(bars + 8 * kDrainPass);  // what was issued ends before the CTA does
+                wait.drain(kDrainPass, 0);
+            }
+            __syncwarp();
+        }
+    } else if (warp >= 8) {
+        ha::give_registers<kPassSide>();
+        // ---------------------------------------------------------------------------------------------- beside the chain
+        if constexpr (kMode != 1) {
+            const int row = (warp & 3) * 32 + lane, v = v0 + row;
+            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+            T* const out = static_cast<T*>(p.out) + b * p.ob + h * p.oh;
+            const bool mine = v < p.dv;
+            bool ok = true;
+            for (int it = 0; it < count; ++it) {
+                const int st = it % L::kStages, n = chunk_at(it), t0 = n * C;
+                const float* const vec = reinterpret_cast<const float*>(sm8 + st * L::stage + L::image);
+                ok = ok && wait(kFull + st, it / L::kStages);
+                if constexpr (kOutput) {
+                    ok = ok && wait(kFar, it);
+                    ha::tmem_after_sync();
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t x[16];
+                        float ea[16];
+                        four(vec + I::early / 4 + 16 * c, ea);
+                        ha::tmem_ld16(x, lanes + M::o + 16 * c);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(ha::decayed(ea[e], p.scale * __uint_as_float(x[e])));
+                        ha::tmem_st16(lanes + M::o + 16 * c, x);
+                    }
+                    ha::release_reads();
+                    ha::tmem_wait_st();
+                    ha::tmem_before_sync();
+                    ok = __all_sync(~0u, ok);
+                    if (lane == 0 && ok) {
+                        ha::bar_arrive(bars + 8 * kFarScaled);
+                        ha::bar_arrive(bars + 8 * (kEmpty + st));
+                    }
+                    ok = ok && wait(kOut, it);
+                    ha::tmem_after_sync();
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t x[16];
+                        ha::tmem_ld16(x, lanes + M::o + 16 * c);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int t = t0 + 16 * c + e;
+                            if (mine && t < p.tokens && ok) out[t * p.ot + v] = ha::from_f<T>(t < live ? __uint_as_float(x[e]) : 0.0f);
+                        }
+                    }
+                    ha::tmem_before_sync();
+                    ok = __all_sync(~0u, ok);
+                    if (lane == 0 && ok) ha::bar_arrive(bars + 8 * kOutRead);
+                } else {
+                    const long long chunk = (long long)bh * p.chunks + n;
+                    const long long at = ((chunk * slices + (v >> 4)) * C) * 16 + (v & 15);  // of E and F: [sixteen columns][token][16]
+                    float* const dots = p.dots + (chunk * 2 * p.parts + (v0 >> 5) + (warp & 3)) * C + lane;
+                    float e[C];
+#pragma unroll
+                    for (int t = 0; t < C; ++t) e[t] = mine ? __ldcs(p.errors + at + t * 16) : 0.0f;
+                    ok = ok && wait(kScores, it);
+                    ha::tmem_after_sync();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {  // e^{c_C-c} k^T D V', over this warp's columns
+                        float x[32];
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t w[16];
+                            float la[16], be[16];
+                            four(vec + I::late / 4 + 32 * half + 16 * c, la);
+                            four(vec + I::beta / 4 + 32 * half + 16 * c, be);
+                            ha::tmem_ld16(w, lanes + M::x + 32 * half + 16 * c);
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) x[16 * c + u] = ha::decayed(la[u], __uint_as_float(w[u])) * (be[u] * e[32 * half + 16 * c + u]);
+                        }
+                        const float sum = sum_across(x);
+                        if (ok && (v0 >> 5) + (warp & 3) < p.parts) dots[p.parts * C + 32 * half] = sum;
+                    }
+                    ok = ok && wait(kFactor, it);  // X and dO^T P have been read
+                    const uint8_t* const go = sm8 + st * L::stage + L::v + (row >> 6) * L::block;
+#pragma unroll 1
+                    for (int jj = 0; jj < 4; ++jj) {  // scale e^c dO^T
+                        float x[16], ea[16];
+                        four(vec + I::early / 4 + 16 * jj, ea);
+#pragma unroll
+                        for (int u = 0; u < 16; ++u)
+                            x[u] = p.scale * ea[u] * __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(go + place<128>(16 * jj + u, (row & 63) >> 3) + 2 * (row & 7)));
+                        uint32_t w[3][8];
+                        put_left<3>(x, w);
+#pragma unroll
+                        for (int u = 0; u < 3; ++u) ha::tmem_st8(lanes + M::outer(jj, u), w[u]);
+                    }
+                    ha::tmem_wait_st();
+                    ha::tmem_before_sync();
+                    ok = __all_sync(~0u, ok);
+                    if (lane == 0 && ok) ha::bar_arrive(bars + 8 * kOuter);
+                    ok = ok && wait(kSolved, it);
+                    ha::tmem_after_sync();
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        float x[32];
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t w[16];
+                            float be[16];
+                            four(vec + I::beta / 4 + 32 * half + 16 * c, be);
+                            ha::tmem_ld16(w, lanes + M::y + 32 * half + 16 * c);
+#pragma unroll
+                            for (int u = 0; u < 16; ++u) {
+                                const float f = __uint_as_float(w[u]);
+                                const int j = 32 * half + 16 * c + u, t = t0 + j;
+                                if (ok && (v >> 4) < slices) p.errors_back[at + j * 16] = f;
+                                if (ok && mine && t < p.tokens) out[t * p.ot + v] = ha::from_f<T>(t < live ? be[u] * f : 0.0f);
+                                x[16 * c + u] = f * e[j];
+                            }
+                        }
+                        const float sum = sum_across(x);
+                        if (ok && (v0 >> 5) + (warp & 3) < p.parts) dots[32 * half] = sum;
+                    }
+                    ha::release_reads();
+                    ha::tmem_before_sync();
+                    ok = __all_sync(~0u, ok);
+                    if (lane == 0 && ok) {
+                        ha::bar_arrive(bars + 8 * kSolvedRead);
+                        ha::bar_arrive(bars + 8 * (kEmpty + st));
+                    }
+                }
+            }
+            for (long long t = (long long)count * C; t < p.tokens; ++t)  // chunks without a token of the sequence
+                if (mine) out[t * p.ot + v] = ha::from_f<T>(0.0f);
+        }
+    } else {
+        ha::take_registers<kPassState>();
+        // ---------------------------------------------------------------------------------------------- the state
+        const int half = warp >> 2, row = (warp & 3) * 32 + lane, v = v0 + row, k0 = half * kOwn;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const bool mine = v < p.dv;
+        float s[kOwn];
+        {
+            const float* const from = p.s_in ? p.s_in + (long long)bh * p.dk * p.dv : nullptr;
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k) s[k] = from && mine && k0 + k < p.dk ? from[(long long)(k0 + k) * p.dv + v] : 0.0f;
+        }
+        bool ok = true;
+        auto arrive = [&](int bar) {
+            ok = __all_sync(~0u, ok);
+            if (lane == 0 && ok) ha::bar_arrive(bars + 8 * bar);
+        };
+        auto publish = [&]() {  // the state's terms
+#pragma unroll
+            for (int q = 0; q < kOwn / 16; ++q) {
+                float x[16];
+                uint32_t w[3][8];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = s[16 * q + e];
+                put_left<3>(x, w);
+#pragma unroll
+                for (int t = 0; t < 3; ++t) ha::tmem_st8(lanes + M::state(half, q, t), w[t]);
+            }
+            ha::tmem_wait_st();
+            ha::tmem_before_sync();
+            arrive(kStateReady);
+        };
+        if (count > 0) publish();
+        for (int it = 0; it < count; ++it) {
+            const int st = it % L::kStages, n = chunk_at(it), t0 = n * C;
+            const float* const vec = reinterpret_cast<const float*>(sm8 + st * L::stage + L::image);
+            const long long chunk = (long long)bh * p.chunks + n;
+            ok = ok && wait(kFull + st, it / L::kStages);
+            if (kBack && it > 0) ok = ok && wait(kSolvedRead, it - 1);  // F of the chunk before
+            ok = ok && wait(kScores, it);
+            ha::tmem_after_sync();
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int jj = 2 * half + g, j = 16 * jj;
+                uint32_t x[16], y[16];
+                float we[16], be[16], z[16];
+                ha::tmem_ld16_early(x, lanes + M::x + j);
+                ha::tmem_ld16_early(y, lanes + (kBack ? M::o : M::y) + j);
+                four(vec + (kBack ? I::late : I::early) / 4 + j, we);
+                four(vec + I::beta / 4 + j, be);
+                ha::tmem_ready(x);
+                ha::tmem_ready(y);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float far = ha::decayed(we[e], __uint_as_float(x[e])), near = __uint_as_float(y[e]);
+                    const float f = t0 + j + e < live ? (kBack ? near + far : near - far) : 0.0f;
+                    y[e] = __float_as_uint(f);
+                    z[e] = -be[e] * f;
+                }
+                ha::tmem_st16(lanes + M::y + j, y);
+                uint32_t w[3][8];
+                put_left<3>(z, w);
+#pragma unroll
+                for (int t = 0; t < 3; ++t) ha::tmem_st8(lanes + M::factor(jj, t), w[t]);
+            }
+            ha::tmem_wait_st();
+            ha::tmem_before_sync();
+            arrive(kFactor);
+            if constexpr (kMode != 0) {  // the state before the chunk (its gradient after it), while the system is solved: [sixteen columns][k / 4][16][4]
+                if (ok && (v >> 4) < slices) {
+                    float4* const to = reinterpret_cast<float4*>((kBack ? p.gradients : p.states) + (chunk * slices + (v >> 4)) * 16 * KP) + (k0 / 4) * 16 + (v & 15);
+#pragma unroll
+                    for (int k = 0; k < kOwn; k += 4) to[k * 4] = make_float4(s[k], s[k + 1], s[k + 2], s[k + 3]);
+                }
+            }
+            ok = ok && wait(kSolved, it);
+            ha::tmem_after_sync();
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const int jj = 2 * half + g, j = 16 * jj;
+                uint32_t x[16];
+                float we[16], be[16], z[16];
+                ha::tmem_ld16_early(x, lanes + M::y + j);
+                four(vec + I::beta / 4 + j, be);
+                four(vec + (kBack ? I::early : I::late) / 4 + j, we);
+                ha::tmem_ready(x);
+                if constexpr (kMode == 1) {
+                    if (ok && (v >> 4) < slices) {
+                        float* const to = p.errors + ((chunk * slices + (v >> 4)) * C + j) * 16 + (v & 15);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) to[e * 16] = __uint_as_float(x[e]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[e] = be[e] * __uint_as_float(x[e]);
+                if constexpr (kOutput) {
+                    uint32_t w[2][8];
+                    put_left<2>(z, w);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) ha::tmem_st8(lanes + M::value(jj, t), w[t]);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[e] *= kBack ? -we[e] : we[e];
+                uint32_t w[3][8];
+                put_left<3>(z, w);
+#pragma unroll
+                for (int t = 0; t < 3; ++t) ha::tmem_st8(lanes + M::factor(jj, t), w[t]);
+            }
+            const float whole = vec[I::whole / 4];
+            ha::release_reads();
+            ha::tmem_wait_st();
+            ha::tmem_before_sync();
+            arrive(kWrites);
+            if (lane == 0 && ok) ha::bar_arrive(bars + 8 * (kEmpty + st));
+            ok = ok && wait(kUpdated, it);
+            ha::tmem_after_sync();
+#pragma unroll
+            for (int k = 0; k < kOwn; k += 16) {
+                uint32_t x[16];
+                ha::tmem_ld16(x, lanes + M::s + k0 + k);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[k + e] = whole == 0.0f ? __uint_as_float(x[e]) : fmaf(whole, s[k + e], __uint_as_float(x[e]));
+            }
+            if (it + 1 < count) publish();
+        }
+        if (p.s_out && mine && ok) {
+            float* const to = p.s_out + (long long)bh * p.dk * p.dv;
+#pragma unroll
+            for (int k = 0; k < kOwn; ++k)
+                if (k0 + k < p.dk) to[(long long)(k0 + k) * p.dv + v] = s[k];
+        }
+    }
+    ha::tmem_before_sync();
+    __syncthreads();
+    if (warp == 12) ha::tmem_free(0, M::columns);
+    if (tid == 0 && *stop) give_up(p, gave_up, 200 + *stop);
+}
+
+}  // namespace hd

@@ -18,7 +18,7 @@ template <int KP, int TI> Space space_of(const heinsen_attention_problem* p) {
     const size_t rows = (size_t)p->batch * p->tokens * p->heads, chunks = (size_t)chunks_of(p), slices = (p->v_dim + 15) / 16;
     Space s;
     s.image = kHeaderBytes;
-    s.q = s.image + image_bytes<C, TM, TM>(p);
+    s.q = s.image + image_bytes<C, TM, TM, true>(p);
     s.k = s.q + terms_bytes(p, view_of(p->q, p->heads, p->q_heads, p->k_dim));
     s.v = s.k + terms_bytes(p, view_of(p->k, p->heads, p->k_heads, p->k_dim));
     s.g = s.v + terms_bytes(p, view_of(p->v, p->heads, p->v_heads, p->v_dim));
@@ -47,7 +47,7 @@ template <int KP, int TI, class T>
 hs_status launch_back(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mg, const CUtensorMap& mo, const hd::Params& q, int* word,
                       cudaStream_t stream) {
     constexpr int C = hd::chunk_tokens(KP), TM = terms_of(TI);
-    using L = hd::ScanLayout<KP, C, TI, TM, TM, true>;
+    using L = hd::ScanLayout<KP, C, TI, TM, TM, true, true>;
     static_assert(L::end(hd::kMaxWarps) <= 232448, "shared memory");
     const auto fn = hd::back_kernel<KP, C, TI, TM, T>;
     static std::atomic<unsigned long long> done{0};
@@ -116,13 +116,26 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
     hs_status st;
     if ((st = map_of<T, TI>(&mq, p, view_of(p->q, p->heads, p->q_heads, p->k_dim), ws + sp.q, 64, C, stream)) != HS_OK) return st;
     if ((st = map_of<T, TI>(&mk, p, view_of(p->k, p->heads, p->k_heads, p->k_dim), ws + sp.k, 64, C, stream)) != HS_OK) return st;
-    if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, 16, C, stream)) != HS_OK) return st;
+    constexpr bool kTcgen05 = on_tcgen05<KP, TI>();
+    q.parts = kTcgen05 ? (p->v_dim + 31) / 32 : (p->v_dim + 15) / 16;
+    if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, kTcgen05 ? 64 : 16, C, stream)) != HS_OK) return st;
     if ((st = map_of<T, TI>(&mg, p, view_of(*d_o, p->heads, p->heads, p->v_dim), ws + sp.g, 16, C, stream)) != HS_OK) return st;
-    if ((st = launch_chunks<KP, C, TI, TM, TM>(mq, mk, q, word, stream)) != HS_OK) return st;
+    CUtensorMap mg64 = mg;  // the same in tiles of 64 columns
+    if (kTcgen05) {
+        View g = view_of(*d_o, p->heads, p->heads, p->v_dim);
+        if (terms_bytes(p, g)) {
+            const long long sh = (p->v_dim + 7) / 8 * 8, stk = sh * p->heads;
+            g = {{ws + sp.g, stk * p->tokens, stk, sh, 1}, p->heads, (int)sh};
+        }
+        if (!encode(&mg64, g, p->batch, p->tokens, 64, C)) return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
+    }
+    if ((st = launch_chunks<KP, C, TI, TM, TM, true>(mq, mk, q, word, stream)) != HS_OK) return st;
     {
         hd::Params f = q;
         f.s_in = p->state0;
-        if ((st = launch_scan<KP, C, TI, TM, TM, false, T>(mq, mk, mv, mo, f, word, stream)) != HS_OK) return st;
+        if constexpr (kTcgen05) st = launch_pass<KP, 1, T>(mq, mk, mv, f, word, stream);
+        else st = launch_scan<KP, C, TI, TM, TM, false, T>(mq, mk, mv, mo, f, word, stream);
+        if (st != HS_OK) return st;
     }
     {
         hd::Params r = q;
@@ -131,9 +144,10 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
         r.out = each ? ws + sp.dv : dv;
         r.oh = p->v_dim; r.ot = (long long)p->heads * p->v_dim; r.ob = p->tokens * r.ot;
         const View out{{r.out, r.ob, r.ot, r.oh, 1}, p->heads, p->v_dim};
-        r.out_tma = !each && TI == 1 && tma_strides(out, p->batch, p->tokens);
+        r.out_tma = !kTcgen05 && !each && TI == 1 && tma_strides(out, p->batch, p->tokens);
         if (r.out_tma && !encode(&mo, out, p->batch, p->tokens, 16, C)) return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
-        st = each ? launch_back<KP, TI, float>(mq, mk, mg, mo, r, word, stream) : launch_back<KP, TI, T>(mq, mk, mg, mo, r, word, stream);
+        if constexpr (kTcgen05) st = each ? launch_pass<KP, 2, float>(mq, mk, mg64, r, word, stream) : launch_pass<KP, 2, T>(mq, mk, mg64, r, word, stream);
+        else st = each ? launch_back<KP, TI, float>(mq, mk, mg, mo, r, word, stream) : launch_back<KP, TI, T>(mq, mk, mg, mo, r, word, stream);
         if (st != HS_OK) return st;
         if (each && (st = shared_sum<T>(at(sp.dv), dv, p, p->v_heads, p->v_dim, stream)) != HS_OK) return st;
     }
