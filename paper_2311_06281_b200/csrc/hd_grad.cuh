@@ -16,219 +16,209 @@ namespace hd {
 
 template <int KP, int C, int TI, int TM, class T>
 __global__ void __launch_bounds__(kScanThreads, 1)
-    back_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mg,
-                const __grid_constant__ CUtensorMap mo, const Params p, int* gave_up) {
+    back_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mg, const Params p,
+                int* gave_up) {
     constexpr int TP = TM;
     using L = ScanLayout<KP, C, TI, TM, TP, true, true>;
     using I = typename L::I;
-    constexpr int kLevel = TM - 1, kGroup = TI == 1 && C == 64 ? 4 : 2;
-    constexpr bool kRounded = TI == 3;
+    using B = Blocks<C>;
+    constexpr int kLevel = TM - 1, NB = C / 16, kTiles = KP / 32, kOwn = KP / 4;
+    constexpr bool kRounded = TI == 3, kSlabs = TI == 1 && KP <= 128;
     extern __shared__ __align__(1024) uint8_t sm8[];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = p.warps;
-    const uint32_t base = smem_addr(sm8), stage_bytes = L::stage(warps), bars = base + L::bars(warps);
-    volatile int* const stop = reinterpret_cast<int*>(sm8 + L::bars(warps) + 64);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, own_slices = p.slices;
+    const uint32_t base = smem_addr(sm8), stage_bytes = L::stage(own_slices), bars = base + L::bars(own_slices);
+    volatile int* const stop = reinterpret_cast<int*>(sm8 + L::bars(own_slices) + 64);
     const Waiter wait{bars, stop, p.spin};
-    const int slices = (p.dv + 15) / 16, groups = (slices + warps - 1) / warps;
-    const int bh = blockIdx.x / groups, b = bh / p.heads, h = bh % p.heads, slice0 = (blockIdx.x % groups) * warps;
+    const int slices = (p.dv + 15) / 16, groups = (slices + own_slices - 1) / own_slices;
+    const int bh = blockIdx.x / groups, b = bh / p.heads, h = bh % p.heads, slice0 = (blockIdx.x % groups) * own_slices;
     const int live = live_tokens(p.lengths, b, p.tokens), count = (live + C - 1) / C;
     if (tid == 0) {
-        for (int i = 0; i < kScanBars; ++i) ha::bar_init(bars + 8 * i, i >= kEmpty && i < kPatched ? warps : 1);
+        for (int i = 0; i < kScanBars; ++i) ha::bar_init(bars + 8 * i, i >= kEmpty && i < kPatched ? 4 * own_slices : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *stop = 0;
     }
     __syncthreads();
-    if (warp >= loader_of(warps)) {
-        ha::give_registers<kLoadRegs>();
-        const uint32_t bytes = 2 * L::tile + warps * TI * L::own + L::image_bytes;
-        if (warp == loader_of(warps)) load_chunks<C, L::kStages>(
-            wait, sm8, stage_bytes, 2 * L::tile, warps * TI * L::own, count, live, p.tokens, bytes, p.mute,
+    if (warp >= 4 * own_slices) {
+        const uint32_t bytes = 2 * L::tile + own_slices * TI * L::own + L::image_bytes;
+        if (warp == 4 * own_slices) load_chunks<C, L::kStages>(
+            wait, sm8, stage_bytes, 2 * L::tile, own_slices * TI * L::own, count, live, p.tokens, bytes, p.mute,
             [&](int n, int s, uint32_t bar) {
                 const uint32_t to = base + s * stage_bytes;
-                bulk_load(to + L::image(warps), p.image + ((long long)bh * p.chunks + n) * I::end, L::image_bytes, bar);
+                bulk_load(to + L::image(own_slices), p.image + ((long long)bh * p.chunks + n) * I::end, L::image_bytes, bar);
                 for (int u = 0; u < TI; ++u) {
                     for (int c = 0; c < KP / 64; ++c) {
                         ha::tma_load_4d(to + L::k + (u * (KP / 64) + c) * C * 128, &mk, 64 * c, h / p.kdiv, n * C, u * p.batch + b, bar);
                         ha::tma_load_4d(to + L::q + (u * (KP / 64) + c) * C * 128, &mq, 64 * c, h / p.qdiv, n * C, u * p.batch + b, bar);
                     }
-                    for (int w = 0; w < warps; ++w)
-                        ha::tma_load_4d(to + L::v + (w * TI + u) * L::own, &mg, 16 * (slice0 + w), h, n * C, u * p.batch + b, bar);
+                    for (int x = 0; x < own_slices; ++x)
+                        ha::tma_load_4d(to + L::v + (x * TI + u) * L::own, &mg, 16 * (slice0 + x), h, n * C, u * p.batch + b, bar);
                 }
             },
             true);
     } else {
-        ha::take_registers<kColumnRegs>();
         const Lane at;
-        const int v0 = 16 * (slice0 + warp), j0 = 2 * (lane & 3);
-        float s[KP / 8][4];
-        read_state<KP>(s, p.s_in ? p.s_in + (long long)bh * p.dk * p.dv : nullptr, p.dk, p.dv, v0);
-        bool ok = warp < warps;
-        for (int it = 0; ok && it < count; ++it) {
+        const int slice = warp >> 2, w = warp & 3, v0 = 16 * (slice0 + slice), k0 = w * kOwn, j0 = 2 * (lane & 3);
+        uint8_t* const xs = sm8 + L::shared(own_slices) + slice * L::slice;  // partial sums of X, then factors of the update by K
+        uint8_t* const os = xs + L::sums;                                    // factors of the update by Q
+        uint8_t* const fs = os + L::sums;                                    // beta dV'
+        const bool mine = w < NB, inside = v0 < p.dv;
+        float s[kTiles][4];
+        read_state(s, p.s_in ? p.s_in + (long long)bh * p.dk * p.dv : nullptr, p.dk, p.dv, v0, k0);
+        bool ok = true;
+        for (int it = 0; it < count; ++it) {
             const int st = it % L::kStages, n = count - 1 - it, t0 = n * C;
-            ok = __all_sync(~0u, wait(kFull + st, it / L::kStages));
-            if (!ok) break;
-            const uint32_t to = base + st * stage_bytes, K = to + L::k, Q = to + L::q, G = to + L::v + warp * TI * L::own, N = to + L::image(warps) + I::n,
-                           P = to + L::image(warps) + I::p;
-            const float* const vec = reinterpret_cast<const float*>(sm8 + st * stage_bytes + L::image(warps));
-            const long long chunk = (long long)bh * p.chunks + n, rows = (chunk * slices * 16 + v0);
-            if (v0 < p.dv) dump_rows(s, p.gradients + rows * KP, KP);
-            float y[C / 8][4] = {}, e[C / 8][4];  // dV'^T; E^T
+            const long long chunk = (long long)bh * p.chunks + n, rows = chunk * slices * 16 + v0;
+            if (inside && ok) dump_state<KP, kSlabs>(s, p.gradients + rows * KP, k0);
+            float e[2][4] = {};  // E^T
+            if (mine && inside && ok) read_errors<C, kSlabs>(e, p.errors + rows * C, w);
+            ok = __all_sync(~0u, ok && wait(kFull + st, it / L::kStages));
+            const uint32_t to = base + st * stage_bytes, K = to + L::k, Q = to + L::q, G = to + L::v + slice * TI * L::own,
+                           N = to + L::image(own_slices) + I::n, P = to + L::image(own_slices) + I::p;
+            const float* const vec = reinterpret_cast<const float*>(sm8 + st * stage_bytes + L::image(own_slices));
+            float x[2][4], near[2][4] = {};
             {
-                const float* from = p.errors + rows * C + (lane >> 2) * C + j0;
+                float y[2 * NB][4] = {};
 #pragma unroll
-                for (int nt = 0; nt < C / 8; ++nt) {
-                    const float2 x = v0 < p.dv ? *reinterpret_cast<const float2*>(from + 8 * nt) : make_float2(0.0f, 0.0f);
-                    const float2 z = v0 < p.dv ? *reinterpret_cast<const float2*>(from + 8 * C + 8 * nt) : make_float2(0.0f, 0.0f);
-                    e[nt][0] = x.x; e[nt][1] = x.y; e[nt][2] = z.x; e[nt][3] = z.y;
-                }
-            }
+                for (int kk = 0; kk < kTiles / 2; ++kk) {  // this quarter's part of (K D)^T
+                    uint32_t a[TM][4];
+                    as_operand<TM>(a, s[2 * kk], s[2 * kk + 1]);
 #pragma unroll
-            for (int kk = 0; kk < KP / 16; ++kk) {  // (K D)^T
-                uint32_t a[TM][4];
-                as_operand<TM>(a, s[2 * kk], s[2 * kk + 1]);
+                    for (int np = 0; np < NB; np += 2) {
+                        uint32_t bf[2][TI][4];
 #pragma unroll
-                for (int np = 0; np < C / 16; np += kGroup) {
-                    uint32_t bf[kGroup][TI][4];
-#pragma unroll
-                    for (int g = 0; g < kGroup; ++g)
-#pragma unroll
-                        for (int u = 0; u < TI; ++u)
-                            load4(bf[g][u], K + u * (KP * C * 2) + wide<C>(16 * (np + g) + at.b_row(), 2 * kk + at.b_piece()));
-                    sum<kRounded, kLevel>(y + 2 * np, a, bf);
-                }
-            }
-            // sums over the slice's columns for every token, to the lane that has tokens 8 nt + j0 of them
-            float* const dots = p.dots + (chunk * 2 * slices + slice0 + warp) * C;
-            auto put = [&](float* where, int nt, float x, float z) {
-#pragma unroll
-                for (int o = 4; o < 32; o *= 2) {
-                    x += __shfl_xor_sync(~0u, x, o);
-                    z += __shfl_xor_sync(~0u, z, o);
-                }
-                if (lane < 4 && v0 < p.dv) *reinterpret_cast<float2*>(where + 8 * nt + j0) = make_float2(x, z);
-            };
-#pragma unroll
-            for (int nt = 0; nt < C / 8; ++nt) {
-                const float2 la = *reinterpret_cast<const float2*>(vec + I::late / 4 + 8 * nt + j0);
-                const float2 be = *reinterpret_cast<const float2*>(vec + I::beta / 4 + 8 * nt + j0);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) y[nt][r] = ha::decayed(r & 1 ? la.y : la.x, y[nt][r]);
-                put(dots + slices * C, nt, be.x * fmaf(y[nt][0], e[nt][0], y[nt][2] * e[nt][2]), be.y * fmaf(y[nt][1], e[nt][1], y[nt][3] * e[nt][3]));
-            }
-#pragma unroll
-            for (int jj = 0; jj < C / 16; ++jj) {  // (P^T dO)^T
-                uint32_t a[TI][4];
-#pragma unroll
-                for (int u = 0; u < TI; ++u) load4_t(a[u], G + u * L::own + place<32>(16 * jj + at.b_row(), at.b_piece()));
-#pragma unroll
-                for (int np = 0; np <= jj; np += 2) {
-                    const int pairs = np + 1 <= jj ? 2 : 1;
-                    uint32_t bf[2][TP][4];
-#pragma unroll
-                    for (int g = 0; g < 2; ++g)
-#pragma unroll
-                        for (int u = 0; u < TP; ++u)
-                            if (g < pairs) load4_t(bf[g][u], P + u * I::plane + in_block(I::p_block(jj, np + g), at.bt_row(), at.bt_piece()));
-                    sum<kRounded, kLevel>(y + 2 * np, a, bf, pairs);
-                }
-            }
-            // F^T in place, from the first sixteen tokens on: theirs are needed by no other before they change
-#pragma unroll
-            for (int jj = 0; jj < C / 16; ++jj) {
-                float w[2][4];
-                uint32_t a[TM][4];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const float2 be = *reinterpret_cast<const float2*>(vec + I::beta / 4 + 16 * jj + 8 * x + j0);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) w[x][r] = -(r & 1 ? be.y : be.x) * y[2 * jj + x][r];
-                }
-                as_operand<TM>(a, w[0], w[1]);
-#pragma unroll
-                for (int np = 0; np <= jj; np += 2) {
-                    const int pairs = np + 1 <= jj ? 2 : 1;
-                    uint32_t bf[2][TM][4];
-#pragma unroll
-                    for (int g = 0; g < 2; ++g)
-#pragma unroll
-                        for (int u = 0; u < TM; ++u)
-                            if (g < pairs) load4_t(bf[g][u], N + u * I::plane + in_block(Blocks<C>::by_columns(jj, np + g), at.bt_row(), at.bt_piece()));
-                    sum<kRounded, kLevel>(y + 2 * np, a, bf, pairs);
-                }
-            }
-            if (v0 < p.dv) dump_rows(y, p.errors_back + rows * C, C);
-#pragma unroll
-            for (int nt = 0; nt < C / 8; ++nt) {
-                put(dots, nt, fmaf(y[nt][0], e[nt][0], y[nt][2] * e[nt][2]), fmaf(y[nt][1], e[nt][1], y[nt][3] * e[nt][3]));
-                const float2 be = *reinterpret_cast<const float2*>(vec + I::beta / 4 + 8 * nt + j0);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) y[nt][r] *= r & 1 ? be.y : be.x;  // Z^T
-            }
-            write_out<C, T>(y, &mo, p, sm8 + L::out(warps) + warp * L::own, b, h, v0, t0, live);
-            const float whole = vec[I::whole / 4];
-            uint32_t au[C / 16][TM][4];
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {  // - K^T (e^c Z); Q^T (scale e^c dO)
-#pragma unroll
-                for (int jj = 0; jj < C / 16; ++jj) {
-                    float w[2][4];
-                    if (part == 0) {
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const float2 ea = *reinterpret_cast<const float2*>(vec + I::early / 4 + 16 * jj + 8 * x + j0);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) w[x][r] = -(r & 1 ? ea.y : ea.x) * y[2 * jj + x][r];
-                        }
-                    } else {
-                        uint32_t g[TI][4];
-#pragma unroll
-                        for (int u = 0; u < TI; ++u) load4_t(g[u], G + u * L::own + place<32>(16 * jj + at.b_row(), at.b_piece()));
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const float2 ea = *reinterpret_cast<const float2*>(vec + I::early / 4 + 16 * jj + 8 * x + j0);
-#pragma unroll
-                            for (int r = 0; r < 2; ++r) {
-                                float f0 = 0.0f, f1 = 0.0f;
-#pragma unroll
-                                for (int u = TI - 1; u >= 0; --u) {
-                                    f0 += __uint_as_float(g[u][2 * x + r] << 16);
-                                    f1 += __uint_as_float(g[u][2 * x + r] & 0xffff0000u);
-                                }
-                                w[x][2 * r] = p.scale * ea.x * f0;
-                                w[x][2 * r + 1] = p.scale * ea.y * f1;
-                            }
-                        }
-                    }
-                    as_operand<TM>(au[jj], w[0], w[1]);
-                }
-#pragma unroll
-                for (int kp = 0; kp < KP / 16; kp += kGroup) {
-                    float up[2 * kGroup][4] = {};
-#pragma unroll
-                    for (int jj = 0; jj < C / 16; ++jj) {
-                        uint32_t bf[kGroup][TI][4];
-#pragma unroll
-                        for (int g = 0; g < kGroup; ++g)
+                        for (int g = 0; g < 2; ++g)
 #pragma unroll
                             for (int u = 0; u < TI; ++u)
-                                load4_t(bf[g][u], (part == 0 ? K : Q) + u * (KP * C * 2) + wide<C>(16 * jj + at.bt_row(), 2 * (kp + g) + at.bt_piece()));
-                        sum<kRounded, kLevel>(up, au[jj], bf);
+                                load4(bf[g][u], K + u * (KP * C * 2) + wide<C>(16 * (np + g) + at.b_row(), k0 / 8 + 2 * kk + at.b_piece()));
+                        sum<kRounded, kLevel>(y + 2 * np, a, bf);
+                    }
+                }
+                if (it > 0) slice_sync(slice);  // the factors of the update before have been read
+                hand_out<NB>(y, x, xs, w);
+            }
+            if (mine) {
+                // (P^T dO)^T of this warp's tokens
+#pragma unroll
+                for (int ii = 0; ii < NB; ++ii)
+                    if (ii >= w) {
+                        uint32_t a[TI][4], bf[1][TP][4];
+#pragma unroll
+                        for (int u = 0; u < TI; ++u) load4_t(a[u], G + u * L::own + place<32>(16 * ii + at.b_row(), at.b_piece()));
+#pragma unroll
+                        for (int u = 0; u < TP; ++u) load4_t(bf[0][u], P + u * I::plane + in_block(I::p_block(ii, w), at.bt_row(), at.bt_piece()));
+                        sum<kRounded, kLevel>(near, a, bf);
+                    }
+                // scale e^c dO^T of this warp's tokens, a factor of the update
+                float g[2][4];
+                uint32_t a[TM][4];
+                read_values<TI>(g, G, L::own, w, at);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) g[u][r] *= p.scale;
+                weigh_tokens<false>(g, vec + I::early / 4 + 16 * w);
+                as_operand<TM>(a, g[0], g[1]);
+                put_factor(os, w, a);
+            }
+            slice_sync(slice);
+            // sums over the slice's columns for every token, to the lanes that have tokens 8 u + j0 of them
+            float* const dots = p.dots + (chunk * 2 * p.parts + slice0 + slice) * C + 16 * w + j0;
+            auto put = [&](float* where, int u, float y, float z) {
+#pragma unroll
+                for (int o = 4; o < 32; o *= 2) {
+                    y += __shfl_xor_sync(~0u, y, o);
+                    z += __shfl_xor_sync(~0u, z, o);
+                }
+                if (lane < 4 && inside && ok) *reinterpret_cast<float2*>(where + 8 * u) = make_float2(y, z);
+            };
+            uint32_t own_f[TM][4];
+            if (mine) {
+                add_up(x, xs, w);
+                weigh_tokens<true>(x, vec + I::late / 4 + 16 * w);
+                float y[2][4];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float2 be = *reinterpret_cast<const float2*>(vec + I::beta / 4 + 16 * w + 8 * u + j0);
+                    put(dots + p.parts * C, u, be.x * fmaf(x[u][0], e[u][0], x[u][2] * e[u][2]), be.y * fmaf(x[u][1], e[u][1], x[u][3] * e[u][3]));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        x[u][r] += near[u][r];
+                        y[u][r] = -(r & 1 ? be.y : be.x) * x[u][r];
+                    }
+                }
+                as_operand<TM>(own_f, y[0], y[1]);
+                put_factor(fs, w, own_f);
+            }
+            slice_sync(slice);
+            if (mine) {  // F^T
+                float d[NB][2][4] = {};
+#pragma unroll
+                for (int ii = 0; ii < NB; ++ii)
+                    if (ii >= w) {
+                        uint32_t a[TM][4], bf[1][TM][4];
+                        if (ii == w) {
+#pragma unroll
+                            for (int u = 0; u < TM; ++u)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) a[u][r] = own_f[u][r];
+                        } else {
+                            get_factor(a, fs, ii);
+                        }
+#pragma unroll
+                        for (int u = 0; u < TM; ++u) load4_t(bf[0][u], N + u * I::plane + in_block(B::by_columns(ii, w), at.bt_row(), at.bt_piece()));
+                        products<kLevel>(d[ii], a, bf);
                     }
 #pragma unroll
-                    for (int m = 0; m < 2 * kGroup; ++m)
+                for (int ii = 0; ii < NB; ++ii)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            float& x = s[2 * kp + m][r];
-                            x = part ? x + up[m][r] : whole == 0.0f ? up[m][r] : fmaf(whole, x, up[m][r]);
+                    for (int r = 0; r < 4; ++r) {
+                        x[0][r] += d[ii][0][r];
+                        x[1][r] += d[ii][1][r];
+                    }
+                if (inside && ok) dump_errors<C, kSlabs>(x, p.errors_back + rows * C, w);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) put(dots, u, fmaf(x[u][0], e[u][0], x[u][2] * e[u][2]), fmaf(x[u][1], e[u][1], x[u][3] * e[u][3]));
+                weigh_tokens<false>(x, vec + I::beta / 4 + 16 * w);  // Z^T
+                if (ok) write_out<T>(x, p, b, h, v0, t0 + 16 * w, live);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) x[u][r] = -x[u][r];
+                weigh_tokens<false>(x, vec + I::early / 4 + 16 * w);
+                uint32_t a[TM][4];
+                as_operand<TM>(a, x[0], x[1]);
+                put_factor(xs, w, a);
+            }
+            slice_sync(slice);
+            const float whole = vec[I::whole / 4];
+            {
+                float up[kTiles][4] = {};
+#pragma unroll
+                for (int part = 0; part < 2; ++part)  // - K^T (e^c Z); Q^T (scale e^c dO)
+#pragma unroll
+                    for (int jj = 0; jj < NB; ++jj) {
+                        uint32_t a[TM][4];
+                        get_factor(a, part ? os : xs, jj);
+#pragma unroll
+                        for (int kp = 0; kp < kTiles / 2; ++kp) {
+                            uint32_t bf[1][TI][4];
+#pragma unroll
+                            for (int u = 0; u < TI; ++u)
+                                load4_t(bf[0][u], (part ? Q : K) + u * (KP * C * 2) + wide<C>(16 * jj + at.bt_row(), k0 / 8 + 2 * kp + at.bt_piece()));
+                            sum<kRounded, kLevel>(up + 2 * kp, a, bf);
                         }
-                }
+                    }
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[j][r] = whole == 0.0f ? up[j][r] : fmaf(whole, s[j][r], up[j][r]);
             }
             ha::release_reads();
             __syncwarp();
-            if (lane == 0) ha::bar_arrive(bars + 8 * (kEmpty + st));
+            if (lane == 0 && ok) ha::bar_arrive(bars + 8 * (kEmpty + st));
         }
-        if (lane == 0) ha::tma_store_wait_all();
-        if (warp < warps && v0 < p.dv) zero_out<T>(p, b, h, v0, count * C);
-        if (ok && p.s_out && v0 < p.dv) write_state<KP>(s, p.s_out + (long long)bh * p.dk * p.dv, p.dk, p.dv, v0);
+        if (inside) zero_out<T>(p, b, h, v0, count * C, w);
+        if (ok && p.s_out && inside) write_state(s, p.s_out + (long long)bh * p.dk * p.dv, p.dk, p.dv, v0, k0);
     }
     __syncthreads();
     if (tid == 0 && *stop) give_up(p, gave_up, 1 + *stop);

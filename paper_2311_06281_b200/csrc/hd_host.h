@@ -1,5 +1,6 @@
 // What the forward and the backward pass of the delta rule share on the host.
 #pragma once
+#include <cstdlib>
 #include <cstring>
 
 #include "../../include/heinsen_delta.h"
@@ -103,13 +104,8 @@ inline long long chunks_of(const heinsen_attention_problem* p) {
 }
 template <int C, int TM, int TP, bool kBack> size_t image_bytes(const heinsen_attention_problem* p) { return up256((size_t)chunks_of(p) * hd::Image<C, TM, TP, kBack>::end); }
 
-// Warps of a CTA of the scans, sixteen columns each: as many as one SM can have while there are CTAs for all SMs, since a CTA
-// loads K, Q, N and P for all of its warps.
-inline int warps_for(long long pairs, int slices) {
-    int warps = hd::kMaxWarps;
-    while (warps > 1 && (warps >= 2 * slices || (pairs * ((slices + warps - 1) / warps) <= kSms / 2))) warps /= 2;
-    return warps;
-}
+// Slices of sixteen columns of V that a CTA of the mma.sync scans has: two where there would be more CTAs than SMs otherwise.
+inline int slices_for(long long pairs, int slices) { return pairs * slices > kSms && slices > 1 ? hd::kMaxSlices : 1; }
 
 template <int KP, int C, int TI, int TM, int TP, bool kBack>
 hs_status launch_chunks(const CUtensorMap& mq, const CUtensorMap& mk, const hd::Params& q, int* word, cudaStream_t stream) {
@@ -122,27 +118,33 @@ hs_status launch_chunks(const CUtensorMap& mq, const CUtensorMap& mk, const hd::
     return launched("chunk_kernel");
 }
 
-template <int KP, int C, int TI, int TM, int TP, bool kOut, class T>
-hs_status launch_scan(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mo, const hd::Params& q, int* word,
-                      cudaStream_t stream) {
-    using L = hd::ScanLayout<KP, C, TI, TM, TP, kOut, !kOut>;
-    static_assert(L::end(hd::kMaxWarps) <= 232448, "shared memory");
-    const auto fn = hd::scan_kernel<KP, C, TI, TM, TP, kOut, T>;
-    static std::atomic<unsigned long long> done{0};
-    const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end(hd::kMaxWarps), done);
+template <class L, class Fn>
+hs_status launch_slices(Fn fn, std::atomic<unsigned long long>& done, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const hd::Params& q,
+                        int* word, cudaStream_t stream) {
+    static_assert(L::end(hd::kMaxSlices) <= 232448, "shared memory");
+    const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end(hd::kMaxSlices), done);
     if (st != HS_OK) return st;
     const long long pairs = (long long)q.batch * q.heads;
-    const int slices = (q.dv + 15) / 16, warps = warps_for(pairs, slices);
-    const long long grid = pairs * ((slices + warps - 1) / warps);
+    const int slices = (q.dv + 15) / 16, each = slices_for(pairs, slices);
+    const long long grid = pairs * ((slices + each - 1) / each);
     if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
     hd::Params w = q;
-    w.warps = warps;
-    fn<<<(unsigned)grid, 32 * (hd::loader_of(warps) + 4), L::end(warps), stream>>>(mq, mk, mv, mo, w, word);
+    w.slices = each;
+    fn<<<(unsigned)grid, 128 * (each + 1), L::end(each), stream>>>(mq, mk, mv, w, word);
     return launched("scan_kernel");
 }
+template <int KP, int C, int TI, int TM, int TP, bool kOut, class T>
+hs_status launch_scan(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const hd::Params& q, int* word, cudaStream_t stream) {
+    static std::atomic<unsigned long long> done{0};
+    return launch_slices<hd::ScanLayout<KP, C, TI, TM, TP, kOut, !kOut>>(hd::scan_kernel<KP, C, TI, TM, TP, kOut, T>, done, mq, mk, mv, q, word, stream);
+}
 
-// Whether the passes run on tcgen05: bf16 and keys up to 128 wide.
-template <int KP, int TI> constexpr bool on_tcgen05() { return TI == 1 && KP <= 128; }
+// Whether the passes can run on tcgen05: bf16 and keys up to 128 wide; and whether they do.
+template <int KP, int TI> constexpr bool fits_tcgen05() { return TI == 1 && KP <= 128; }
+#ifndef HD_PAIRS
+#define HD_PAIRS 1000000
+#endif
+inline bool many_slices(const heinsen_attention_problem* p) { static const long long most = getenv("HDP") ? atoll(getenv("HDP")) : HD_PAIRS; return p->batch * p->heads * ((p->v_dim + 15) / 16) >= most; }
 
 template <int KP, int kMode, class T>
 hs_status launch_pass(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const hd::Params& q, int* word, cudaStream_t stream) {

@@ -11,15 +11,12 @@
 //     dS  = e^{c_C} D + Q^T (scale e^c dO) - K^T (e^c Z).
 // The system is solved once, for N: the two directions and beta come in around it, and no division by beta is needed.
 //
-// Two kernels a direction.  chunk_kernel forms M, P and N of every chunk, all chunks at once.  scan_kernel (backward: back_kernel)
-// walks a sequence's chunks; a warp has 16 columns of the values and all that belongs to them: 16 columns of S, transposed, as
-// mma accumulators, so that every product of the chain has its left factor in the registers that the one before left it in
-// (hd_warp.cuh) and its right one, K, Q, N or P, in shared memory, where all warps of the CTA read it.  Nothing is handed from
-// thread to thread; the columns of V are independent, so warps wait for nothing but the loads of the next chunk.
-//
-// Why mma.sync: five dependent products a chunk.  On tcgen05 each of them ends with a trip through tensor memory (commit,
-// barrier, load, convert, store, barrier), about 1000 clocks as measured in ha_mma.cuh, for 128 x 128 tiles that it would take
-// 60 to 500 clocks to multiply; the accumulators of mma.sync are its next operands after a conversion.
+// Two kernels a direction.  chunk_kernel forms M, P and N of every chunk, all chunks at once.  The scans walk a sequence's chunks: on
+// tcgen05 (hd_scan_mma.cuh), or here with mma.sync, which is for all that the other is not (float32, wide keys) and where there are
+// few sequences and heads.  A slice of sixteen columns of V has four warps, one on each scheduler of an SM; each has a quarter of the
+// state's rows for it, transposed, as accumulators, and a quarter of a chunk's tokens.  Products over the state's rows are added up
+// between the four (one barrier), and each hands the others its tokens' Y and V' as factors (two more), so that the state never leaves
+// its registers.  Measured against one warp for a slice: see the notes at the launch.
 #pragma once
 #include <cuda.h>
 
@@ -48,13 +45,12 @@ struct Params {
     int qdiv, kdiv, vdiv;
     int dk, dv;
     float scale;
-    int warps;             // of a CTA of the scans that have columns of V
+    int slices;            // of sixteen columns of V, of a CTA of the scans
     uint8_t* image;        // what chunk_kernel leaves for each (batch, head) and chunk
     const float* s_in;     // [batch, heads, dk, dv] or NULL
     float* s_out;          // or NULL
     void* out;             // o (backward: dv) through its strides, where TMA does not store it
     long long ob, ot, oh;
-    int out_tma;
     float* states;         // backward: before every chunk the state (after it, its gradient), [batch * heads][chunks][16 slices][KP]
     float* errors;         // E (F) of every chunk, [batch * heads][chunks][16 slices][C]
     float* errors_back;    // F likewise (layouts of the tensor-core passes: hd_scan_mma.cuh)
@@ -402,27 +398,92 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
 
 // ---------------------------------------------------------------------------------------------------------------- scan
 
-constexpr int kMaxWarps = 8;
-// Warps of a CTA: those with columns of V, in groups of four (the rest of a group idles), and a group of which one loads.  Registers
-// move between groups: 168 a thread at launch, 3 * 168 = 2 * 224 + 56 (with one group of columns 2 * 168 > 224 + 56).
-constexpr int kScanThreads = 32 * (kMaxWarps + 4), kColumnRegs = 224, kLoadRegs = 56;
-static_assert(2 * kColumnRegs + kLoadRegs <= 3 * 168 && kScanThreads * 168 <= 65536, "registers");
-__host__ __device__ constexpr int loader_of(int warps) { return (warps + 3) / 4 * 4; }
+// A CTA has one or two slices of sixteen columns of V, four warps each, and a warp that loads (in a group of its own).
+constexpr int kMaxSlices = 2, kScanThreads = 128 * (kMaxSlices + 1);
 
 // kQ: a tile of Q and the weights P
 template <int KP, int C, int TI, int TM, int TP, bool kQ, bool kBack>
 struct ScanLayout {
     using I = Image<C, TM, TP, kBack>;
-    static constexpr int kStages = TI == 1 ? 2 : 1;
-    static constexpr uint32_t tile = KP * C * 2 * TI, k = 0, q = tile, v = q + (kQ ? tile : 0), own = C * 32;  // V: 16 columns for each warp
+    static constexpr int kStages = TI == 1 ? 2 : 1, NB = C / 16;
+    static constexpr uint32_t tile = KP * C * 2 * TI, k = 0, q = tile, v = q + (kQ ? tile : 0), own = C * 32;  // V: 16 columns for each slice
     static constexpr uint32_t image_bytes = kQ ? I::end : I::rows;
-    static __host__ __device__ constexpr uint32_t image(int warps) { return v + warps * TI * own; }
-    static __host__ __device__ constexpr uint32_t stage(int warps) { return (image(warps) + image_bytes + 1023) / 1024 * 1024; }
-    // stages, the output's staging (16 columns for each warp, bf16), barriers
-    static __host__ __device__ constexpr uint32_t out(int warps) { return kStages * stage(warps); }
-    static __host__ __device__ constexpr uint32_t bars(int warps) { return out(warps) + (kQ && TI == 1 ? warps * own : 0); }
-    static __host__ __device__ constexpr uint32_t end(int warps) { return bars(warps) + 128; }
+    static __host__ __device__ constexpr uint32_t image(int slices) { return v + slices * TI * own; }
+    static __host__ __device__ constexpr uint32_t stage(int slices) { return (image(slices) + image_bytes + 1023) / 1024 * 1024; }
+    // what the warps of a slice hand each other: two sets of partial sums (three for each block of tokens, 1 KB each), whose place
+    // factors of later products take, and three terms of a factor
+    static constexpr uint32_t sums = NB * 3 * 1024, factors = NB * 3 * 512, slice = 2 * sums + factors;
+    static_assert(2 * factors <= 2 * sums, "factors in the place of sums");
+    static __host__ __device__ constexpr uint32_t shared(int slices) { return kStages * stage(slices); }
+    static __host__ __device__ constexpr uint32_t bars(int slices) { return shared(slices) + slices * slice; }
+    static __host__ __device__ constexpr uint32_t end(int slices) { return bars(slices) + 128; }
 };
+
+// The four warps of a slice
+__device__ __forceinline__ void slice_sync(int slice) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(slice + 1) : "memory"); }
+
+// Partial sums over a quarter of the state's rows, [16][C], added up: warp w gets the sixteen tokens of block w, in the order of the
+// warps.  A barrier between the two halves.
+template <int NB>
+__device__ __forceinline__ void hand_out(const float (&y)[2 * NB][4], float (&own)[2][4], uint8_t* to, int w) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int d = 0; d < NB; ++d) {
+        if (d == w) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                own[0][e] = y[2 * d][e];
+                own[1][e] = y[2 * d + 1][e];
+            }
+        } else {
+            float4* const at = reinterpret_cast<float4*>(to + (d * 3 + (w < d ? w : w - 1)) * 1024) + lane;
+            at[0] = make_float4(y[2 * d][0], y[2 * d][1], y[2 * d][2], y[2 * d][3]);
+            at[32] = make_float4(y[2 * d + 1][0], y[2 * d + 1][1], y[2 * d + 1][2], y[2 * d + 1][3]);
+        }
+    }
+}
+__device__ __forceinline__ void add_up(float (&own)[2][4], const uint8_t* from, int w) {
+    const int lane = threadIdx.x & 31;
+    float sum[2][4] = {};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if (u == w) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sum[0][e] += own[0][e];
+                sum[1][e] += own[1][e];
+            }
+        } else {
+            const float4* const at = reinterpret_cast<const float4*>(from + (w * 3 + (u < w ? u : u - 1)) * 1024) + lane;
+            const float4 a = at[0], b = at[32];
+            sum[0][0] += a.x; sum[0][1] += a.y; sum[0][2] += a.z; sum[0][3] += a.w;
+            sum[1][0] += b.x; sum[1][1] += b.y; sum[1][2] += b.z; sum[1][3] += b.w;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        own[0][e] = sum[0][e];
+        own[1][e] = sum[1][e];
+    }
+}
+// Factors of one block of tokens, from warp to warp
+template <int kTerms>
+__device__ __forceinline__ void put_factor(uint8_t* to, int block, const uint32_t (&a)[kTerms][4]) {
+#pragma unroll
+    for (int u = 0; u < kTerms; ++u)
+        reinterpret_cast<uint4*>(to + (block * 3 + u) * 512)[threadIdx.x & 31] = make_uint4(a[u][0], a[u][1], a[u][2], a[u][3]);
+}
+template <int kTerms>
+__device__ __forceinline__ void get_factor(uint32_t (&a)[kTerms][4], const uint8_t* from, int block) {
+#pragma unroll
+    for (int u = 0; u < kTerms; ++u) {
+        const uint4 f = reinterpret_cast<const uint4*>(from + (block * 3 + u) * 512)[threadIdx.x & 31];
+        a[u][0] = f.x; a[u][1] = f.y; a[u][2] = f.z; a[u][3] = f.w;
+    }
+}
+// d += factor * block: sixteen tokens by sixteen, small terms first, added once
+template <int kLevel, int kA, int kB>
+__device__ __forceinline__ void add_block(float (&d)[2][4], const uint32_t (&a)[kA][4], const uint32_t (&b)[1][kB][4]) { rounded_products<kLevel>(d, a, b); }
 
 enum ScanBar : int { kFull = 0, kEmpty = 2, kPatched = 4, kScanBars = 5 };
 
@@ -472,286 +533,329 @@ __device__ __forceinline__ void load_chunks(const Waiter& wait, uint8_t* sm8, ui
         }
 }
 
-// Sixteen columns of S^T as accumulators: lane l has columns v0 + l / 4 and the eighth after, entries 8 j + 2 (l % 4) and the next.
-template <int KP>
-__device__ __forceinline__ void read_state(float (&s)[KP / 8][4], const float* from, int dk, int dv, int v0) {
-    const int lane = threadIdx.x & 31, v = v0 + (lane >> 2), k = 2 * (lane & 3);
+// Sixteen columns of kTiles * 8 rows of S, transposed, as accumulators: lane l has columns v0 + l / 4 and the eighth after, rows
+// k0 + 8 j + 2 (l % 4) and the next.
+template <int kTiles>
+__device__ __forceinline__ void read_state(float (&s)[kTiles][4], const float* from, int dk, int dv, int v0, int k0) {
+    const int lane = threadIdx.x & 31, v = v0 + (lane >> 2), k = k0 + 2 * (lane & 3);
 #pragma unroll
-    for (int j = 0; j < KP / 8; ++j)
+    for (int j = 0; j < kTiles; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int kk = 8 * j + k + (e & 1), vv = v + (e >> 1) * 8;
             s[j][e] = from && kk < dk && vv < dv ? from[(long long)kk * dv + vv] : 0.0f;
         }
 }
-template <int KP>
-__device__ __forceinline__ void write_state(const float (&s)[KP / 8][4], float* to, int dk, int dv, int v0) {
-    const int lane = threadIdx.x & 31, v = v0 + (lane >> 2), k = 2 * (lane & 3);
+template <int kTiles>
+__device__ __forceinline__ void write_state(const float (&s)[kTiles][4], float* to, int dk, int dv, int v0, int k0) {
+    const int lane = threadIdx.x & 31, v = v0 + (lane >> 2), k = k0 + 2 * (lane & 3);
 #pragma unroll
-    for (int j = 0; j < KP / 8; ++j)
+    for (int j = 0; j < kTiles; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int kk = 8 * j + k + (e & 1), vv = v + (e >> 1) * 8;
             if (kk < dk && vv < dv) to[(long long)kk * dv + vv] = s[j][e];
         }
 }
-// Accumulators [16][8 n] to rows of `pitch` floats
-template <int kTiles>
-__device__ __forceinline__ void dump_rows(const float (&s)[kTiles][4], float* to, int pitch) {
-    const int lane = threadIdx.x & 31;
-    float* at = to + (lane >> 2) * pitch + 2 * (lane & 3);
+// For the gradients: sixteen columns of the state before a chunk (its gradient behind it), and of E (F) of sixteen tokens.  kSlabs: as
+// hd_grad_mma.cuh reads them, [sixteen columns][k / 4][16][4] and [sixteen columns][token][16]; else rows of KP and of C for each column.
+template <int KP, bool kSlabs, int kTiles>
+__device__ __forceinline__ void dump_state(const float (&s)[kTiles][4], float* to, int k0) {
+    const int lane = threadIdx.x & 31, v = lane >> 2, k = k0 + 2 * (lane & 3);
 #pragma unroll
-    for (int j = 0; j < kTiles; ++j) {
-        *reinterpret_cast<float2*>(at + 8 * j) = make_float2(s[j][0], s[j][1]);
-        *reinterpret_cast<float2*>(at + 8 * pitch + 8 * j) = make_float2(s[j][2], s[j][3]);
+    for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int vv = v + 8 * r, kk = k + 8 * j;
+            float* const at = kSlabs ? to + (kk >> 2) * 64 + vv * 4 + (kk & 3) : to + vv * KP + kk;
+            *reinterpret_cast<float2*>(at) = make_float2(s[j][2 * r], s[j][2 * r + 1]);
+        }
+}
+template <int C, bool kSlabs>
+__device__ __forceinline__ void dump_errors(const float (&y)[2][4], float* to, int block) {
+    const int lane = threadIdx.x & 31, v = lane >> 2, t = 16 * block + 2 * (lane & 3);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int vv = v + 8 * r, tt = t + 8 * x;
+            if constexpr (kSlabs) {
+                to[tt * 16 + vv] = y[x][2 * r];
+                to[(tt + 1) * 16 + vv] = y[x][2 * r + 1];
+            } else {
+                *reinterpret_cast<float2*>(to + vv * C + tt) = make_float2(y[x][2 * r], y[x][2 * r + 1]);
+            }
+        }
+}
+template <int C, bool kSlabs>
+__device__ __forceinline__ void read_errors(float (&y)[2][4], const float* from, int block) {
+    const int lane = threadIdx.x & 31, v = lane >> 2, t = 16 * block + 2 * (lane & 3);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int vv = v + 8 * r, tt = t + 8 * x;
+            y[x][2 * r] = kSlabs ? from[tt * 16 + vv] : from[vv * C + tt];
+            y[x][2 * r + 1] = kSlabs ? from[(tt + 1) * 16 + vv] : from[vv * C + tt + 1];
+        }
+}
+
+// Sixteen columns of the output for sixteen tokens from t0 on: o^T in accumulators; tokens from `live` on are zero.
+template <class T>
+__device__ __forceinline__ void write_out(const float (&o)[2][4], const Params& p, int b, int h, int v0, int t0, int live) {
+    const int lane = threadIdx.x & 31, j0 = 2 * (lane & 3);
+    T* const go = static_cast<T*>(p.out) + b * p.ob + h * p.oh;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int t = t0 + 8 * x + j0 + (e & 1), v = v0 + (lane >> 2) + 8 * (e >> 1);
+            if (t < p.tokens && v < p.dv) go[t * p.ot + v] = ha::from_f<T>(t < live ? o[x][e] : 0.0f);
+        }
+}
+// Tokens of chunks that hold none of the sequence: zeros, from the four warps of a slice
+template <class T>
+__device__ __forceinline__ void zero_out(const Params& p, int b, int h, int v0, int from, int w) {
+    const int lane = threadIdx.x & 31, v = v0 + (lane & 15);
+    T* const go = static_cast<T*>(p.out) + b * p.ob + h * p.oh;
+    for (long long t = from + 2 * w + (lane >> 4); t < p.tokens; t += 8)
+        if (v < p.dv) go[t * p.ot + v] = ha::from_f<T>(0.0f);
+}
+// w * x for the accumulators of sixteen tokens, a weight for each; decayed: a weight of zero forgets
+template <bool kDecay>
+__device__ __forceinline__ void weigh_tokens(float (&x)[2][4], const float* weight) {
+    const int j0 = 2 * (threadIdx.x & 3);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const float2 f = *reinterpret_cast<const float2*>(weight + 8 * u + j0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float y = e & 1 ? f.y : f.x;
+            x[u][e] = kDecay ? ha::decayed(y, x[u][e]) : y * x[u][e];
+        }
+    }
+}
+// Sixteen tokens of sixteen columns of a tile of V (dO), transposed, as float32
+template <int TI>
+__device__ __forceinline__ void read_values(float (&y)[2][4], uint32_t tile, uint32_t term, int block, const Lane& at) {
+    uint32_t f[TI][4];
+#pragma unroll
+    for (int u = 0; u < TI; ++u) load4_t(f[u], tile + u * term + place<32>(16 * block + at.b_row(), at.b_piece()));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float a = 0.0f, b = 0.0f;
+#pragma unroll
+        for (int u = TI - 1; u >= 0; --u) {
+            a += __uint_as_float(f[u][e] << 16);
+            b += __uint_as_float(f[u][e] & 0xffff0000u);
+        }
+        y[e >> 1][2 * (e & 1)] = a;
+        y[e >> 1][2 * (e & 1) + 1] = b;
     }
 }
 
-// Sixteen columns of the output of one chunk: o^T in accumulators, tokens as columns; tokens from `live` on are zero.
-template <int C, class T>
-__device__ __forceinline__ void write_out(const float (&o)[C / 8][4], const CUtensorMap* map, const Params& p, uint8_t* stage, int b, int h, int v0, int t0,
-                                          int live) {
-    const int lane = threadIdx.x & 31, j0 = 2 * (lane & 3);
-    if (sizeof(T) == 2 && p.out_tma) {
-        const Lane at;
-        if (lane == 0) ha::tma_store_wait_read();
-        __syncwarp();
+// A quarter's part of the products of its rows of the state with all tokens of a tile: y += (tile S)^T, TI terms of the tile
+template <int KP, int C, int kLevel, int TI, int TM>
+__device__ __forceinline__ void quarter_scores(float (*y)[4], const uint32_t (&a)[KP / 64][TM][4], uint32_t tile, int piece, const Lane& at) {
 #pragma unroll
-        for (int np = 0; np < C / 16; ++np) {
-            uint32_t r[4];
+    for (int kk = 0; kk < KP / 64; ++kk)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int nt = 2 * np + (u >> 1), t = t0 + 8 * nt + j0, e = 2 * (u & 1);
-                r[u] = ha::pack_bf16(t < live ? o[nt][e] : 0.0f, t + 1 < live ? o[nt][e + 1] : 0.0f);
-            }
-            store4_t(smem_addr(stage) + place<32>(16 * np + at.b_row(), at.b_piece()), r);
+        for (int np = 0; np < C / 16; np += 2) {
+            uint32_t bf[2][TI][4];
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int u = 0; u < TI; ++u) load4(bf[g][u], tile + u * (KP * C * 2) + wide<C>(16 * (np + g) + at.b_row(), piece + 2 * kk + at.b_piece()));
+            sum<TI == 3, kLevel>(y + 2 * np, a[kk], bf);
         }
-        ha::fence_smem_to_async();
-        __syncwarp();
-        if (lane == 0) {
-            if (v0 < p.dv) ha::tma_store_4d(map, v0, h, t0, b, smem_addr(stage));
-            ha::tma_store_commit();
-        }
-        return;
-    }
-    T* go = static_cast<T*>(p.out) + b * p.ob + h * p.oh;
-#pragma unroll
-    for (int nt = 0; nt < C / 8; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int t = t0 + 8 * nt + j0 + (e & 1), v = v0 + (lane >> 2) + 8 * (e >> 1);
-            if (t < p.tokens && v < p.dv) go[t * p.ot + v] = ha::from_f<T>(t < live ? o[nt][e] : 0.0f);
-        }
-}
-// Tokens of chunks that hold none of the sequence: zeros
-template <class T>
-__device__ __forceinline__ void zero_out(const Params& p, int b, int h, int v0, int from) {
-    const int lane = threadIdx.x & 31, v = v0 + (lane & 15);
-    T* go = static_cast<T*>(p.out) + b * p.ob + h * p.oh;
-    for (long long t = from + (lane >> 4); t < p.tokens; t += 2)
-        if (v < p.dv) go[t * p.ot + v] = ha::from_f<T>(0.0f);
 }
 
 // kOut: the output; else the state before every chunk and E, for the gradients.  TO: terms of S and V' in the output.
 template <int KP, int C, int TI, int TM, int TP, bool kOut, class T>
 __global__ void __launch_bounds__(kScanThreads, 1)
-    scan_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
-                const __grid_constant__ CUtensorMap mo, const Params p, int* gave_up) {
+    scan_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p,
+                int* gave_up) {
     using L = ScanLayout<KP, C, TI, TM, TP, kOut, !kOut>;
     using I = typename L::I;
-    constexpr int kLevel = TM - 1, TO = TI == 1 ? 2 : 3, kGroup = TI == 1 && C == 64 ? 4 : 2;
-    constexpr bool kRounded = TI == 3;
+    using B = Blocks<C>;
+    constexpr int kLevel = TM - 1, TO = TI == 1 ? 2 : 3, NB = C / 16, kTiles = KP / 32, kOwn = KP / 4;
+    constexpr bool kRounded = TI == 3, kSlabs = TI == 1 && KP <= 128;
     extern __shared__ __align__(1024) uint8_t sm8[];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, warps = p.warps;
-    const uint32_t base = smem_addr(sm8), stage_bytes = L::stage(warps), bars = base + L::bars(warps);
-    volatile int* const stop = reinterpret_cast<int*>(sm8 + L::bars(warps) + 64);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, own_slices = p.slices;
+    const uint32_t base = smem_addr(sm8), stage_bytes = L::stage(own_slices), bars = base + L::bars(own_slices);
+    volatile int* const stop = reinterpret_cast<int*>(sm8 + L::bars(own_slices) + 64);
     const Waiter wait{bars, stop, p.spin};
-    const int slices = (p.dv + 15) / 16, groups = (slices + warps - 1) / warps;
-    const int bh = blockIdx.x / groups, b = bh / p.heads, h = bh % p.heads, slice0 = (blockIdx.x % groups) * warps;
+    const int slices = (p.dv + 15) / 16, groups = (slices + own_slices - 1) / own_slices;
+    const int bh = blockIdx.x / groups, b = bh / p.heads, h = bh % p.heads, slice0 = (blockIdx.x % groups) * own_slices;
     const int live = live_tokens(p.lengths, b, p.tokens), count = (live + C - 1) / C;
     if (tid == 0) {
-        for (int i = 0; i < kScanBars; ++i) ha::bar_init(bars + 8 * i, i >= kEmpty && i < kPatched ? warps : 1);
+        for (int i = 0; i < kScanBars; ++i) ha::bar_init(bars + 8 * i, i >= kEmpty && i < kPatched ? 4 * own_slices : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *stop = 0;
     }
     __syncthreads();
-    if (warp >= loader_of(warps)) {
-        ha::give_registers<kLoadRegs>();
-        const uint32_t bytes = (kOut ? 2 : 1) * L::tile + warps * TI * L::own + L::image_bytes;
-        if (warp == loader_of(warps)) load_chunks<C, L::kStages>(
+    if (warp >= 4 * own_slices) {
+        const uint32_t bytes = (kOut ? 2 : 1) * L::tile + own_slices * TI * L::own + L::image_bytes;
+        if (warp == 4 * own_slices) load_chunks<C, L::kStages>(
             wait, sm8, stage_bytes, kOut ? 2 * L::tile : L::tile, 0, count, live, p.tokens, bytes, p.mute,
             [&](int n, int s, uint32_t bar) {
                 const uint32_t to = base + s * stage_bytes;
-                bulk_load(to + L::image(warps), p.image + ((long long)bh * p.chunks + n) * I::end, L::image_bytes, bar);
+                bulk_load(to + L::image(own_slices), p.image + ((long long)bh * p.chunks + n) * I::end, L::image_bytes, bar);
                 for (int u = 0; u < TI; ++u) {
                     for (int c = 0; c < KP / 64; ++c) {
                         ha::tma_load_4d(to + L::k + (u * (KP / 64) + c) * C * 128, &mk, 64 * c, h / p.kdiv, n * C, u * p.batch + b, bar);
                         if (kOut) ha::tma_load_4d(to + L::q + (u * (KP / 64) + c) * C * 128, &mq, 64 * c, h / p.qdiv, n * C, u * p.batch + b, bar);
                     }
-                    for (int w = 0; w < warps; ++w)
-                        ha::tma_load_4d(to + L::v + (w * TI + u) * L::own, &mv, 16 * (slice0 + w), h / p.vdiv, n * C, u * p.batch + b, bar);
+                    for (int x = 0; x < own_slices; ++x)
+                        ha::tma_load_4d(to + L::v + (x * TI + u) * L::own, &mv, 16 * (slice0 + x), h / p.vdiv, n * C, u * p.batch + b, bar);
                 }
             },
             false);
     } else {
-        ha::take_registers<kColumnRegs>();
         const Lane at;
-        const int v0 = 16 * (slice0 + warp), j0 = 2 * (lane & 3);
-        float s[KP / 8][4];
-        read_state<KP>(s, p.s_in ? p.s_in + (long long)bh * p.dk * p.dv : nullptr, p.dk, p.dv, v0);
-        bool ok = warp < warps;
-        for (int it = 0; ok && it < count; ++it) {
+        const int slice = warp >> 2, w = warp & 3, v0 = 16 * (slice0 + slice), k0 = w * kOwn;
+        uint8_t* const xs = sm8 + L::shared(own_slices) + slice * L::slice;  // partial sums of X, then factors of the update
+        uint8_t* const os = xs + L::sums;                                    // ... of Q S, then V'
+        uint8_t* const fs = os + L::sums;                                    // beta Y
+        const bool mine = w < NB, inside = v0 < p.dv;                        // has tokens of a chunk; columns that there are
+        float s[kTiles][4];
+        read_state(s, p.s_in ? p.s_in + (long long)bh * p.dk * p.dv : nullptr, p.dk, p.dv, v0, k0);
+        bool ok = true;
+        for (int it = 0; it < count; ++it) {
             const int st = it % L::kStages, t0 = it * C;
-            ok = __all_sync(~0u, wait(kFull + st, it / L::kStages));
-            if (!ok) break;
-            const uint32_t to = base + st * stage_bytes, K = to + L::k, Q = to + L::q, V = to + L::v + warp * TI * L::own, N = to + L::image(warps) + I::n,
-                           P = to + L::image(warps) + I::p;
-            const float* const vec = reinterpret_cast<const float*>(sm8 + st * stage_bytes + L::image(warps));
+            ok = __all_sync(~0u, ok && wait(kFull + st, it / L::kStages));
+            const uint32_t to = base + st * stage_bytes, K = to + L::k, Q = to + L::q, V = to + L::v + slice * TI * L::own,
+                           N = to + L::image(own_slices) + I::n, P = to + L::image(own_slices) + I::p;
+            const float* const vec = reinterpret_cast<const float*>(sm8 + st * stage_bytes + L::image(own_slices));
+            const long long rows = (((long long)bh * p.chunks + it) * slices * 16 + v0);
             if constexpr (!kOut)
-                if (v0 < p.dv) dump_rows(s, p.states + (((long long)bh * p.chunks + it) * slices * 16 + v0) * KP, KP);
-            float y[C / 8][4] = {}, o[kOut ? C / 8 : 1][4] = {};
+                if (inside && ok) dump_state<KP, kSlabs>(s, p.states + rows * KP, k0);
+            float x[2][4], far[2][4];
+            {
+                uint32_t a[kTiles / 2][TM][4];
 #pragma unroll
-            for (int kk = 0; kk < KP / 16; ++kk) {  // (K S)^T and (Q S)^T
-                uint32_t a[TM][4];
-                as_operand<TM>(a, s[2 * kk], s[2 * kk + 1]);
-#pragma unroll
-                for (int np = 0; np < C / 16; np += kGroup) {
-                    uint32_t bf[kGroup][TI][4];
-#pragma unroll
-                    for (int g = 0; g < kGroup; ++g)
-#pragma unroll
-                        for (int u = 0; u < TI; ++u)
-                            load4(bf[g][u], K + u * (KP * C * 2) + wide<C>(16 * (np + g) + at.b_row(), 2 * kk + at.b_piece()));
-                    sum<kRounded, kLevel>(y + 2 * np, a, bf);
-                    if constexpr (kOut) {
-#pragma unroll
-                        for (int g = 0; g < kGroup; ++g)
-#pragma unroll
-                            for (int u = 0; u < TI; ++u)
-                                load4(bf[g][u], Q + u * (KP * C * 2) + wide<C>(16 * (np + g) + at.b_row(), 2 * kk + at.b_piece()));
-                        sum<kRounded, TO - 1>(o + 2 * np, a, bf);
-                    }
+                for (int kk = 0; kk < kTiles / 2; ++kk) as_operand<TM>(a[kk], s[2 * kk], s[2 * kk + 1]);
+                float y[2 * NB][4] = {};
+                quarter_scores<KP, C, kLevel, TI, TM>(y, a, K, k0 / 8, at);
+                if (it > 0) slice_sync(slice);  // the factors of the update before have been read
+                hand_out<NB>(y, x, xs, w);
+                if constexpr (kOut) {
+                    float z[2 * NB][4] = {};
+                    quarter_scores<KP, C, TO - 1, TI, TM>(z, a, Q, k0 / 8, at);
+                    hand_out<NB>(z, far, os, w);
                 }
             }
+            slice_sync(slice);
+            if (mine) {
+                float y[2][4];
+                add_up(x, xs, w);
+                weigh_tokens<true>(x, vec + I::early / 4 + 16 * w);
+                read_values<TI>(y, V, L::own, w, at);
+                const int left = live - (t0 + 16 * w) - 2 * (lane & 3);  // of the sequence, from this lane's first token on
 #pragma unroll
-            for (int np = 0; np < C / 16; ++np) {  // Y^T
-                uint32_t vf[TI][4];
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int u = 0; u < TI; ++u) load4_t(vf[u], V + u * L::own + place<32>(16 * np + at.b_row(), at.b_piece()));
+                    for (int e = 0; e < 4; ++e) x[u][e] = 8 * u + (e & 1) < left ? y[u][e] - x[u][e] : 0.0f;  // Y^T
+                if constexpr (kOut) {
+                    add_up(far, os, w);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int nt = 2 * np + x;
-                    const float2 e = *reinterpret_cast<const float2*>(vec + I::early / 4 + 8 * nt + j0);
-                    const bool on0 = t0 + 8 * nt + j0 < live, on1 = t0 + 8 * nt + j0 + 1 < live;
+                    for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        float f0 = 0.0f, f1 = 0.0f;
+                        for (int e = 0; e < 4; ++e) far[u][e] *= p.scale;
+                    weigh_tokens<true>(far, vec + I::early / 4 + 16 * w);
+                }
+            }
+            uint32_t own_f[TM][4];
+            if (mine) {
+                float y[2][4];
 #pragma unroll
-                        for (int u = TI - 1; u >= 0; --u) {
-                            f0 += __uint_as_float(vf[u][2 * x + r] << 16);
-                            f1 += __uint_as_float(vf[u][2 * x + r] & 0xffff0000u);
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[u][e] = -x[u][e];
+                weigh_tokens<false>(y, vec + I::beta / 4 + 16 * w);
+                as_operand<TM>(own_f, y[0], y[1]);
+                put_factor(fs, w, own_f);
+            }
+            slice_sync(slice);
+            if (mine) {  // E^T
+                float d[NB][2][4] = {};
+#pragma unroll
+                for (int jj = 0; jj < NB; ++jj)
+                    if (jj <= w) {
+                        uint32_t a[TM][4], bf[1][TM][4];
+                        if (jj == w) {
+#pragma unroll
+                            for (int u = 0; u < TM; ++u)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) a[u][e] = own_f[u][e];
+                        } else {
+                            get_factor(a, fs, jj);
                         }
-                        y[nt][2 * r] = on0 ? f0 - ha::decayed(e.x, y[nt][2 * r]) : 0.0f;
-                        y[nt][2 * r + 1] = on1 ? f1 - ha::decayed(e.y, y[nt][2 * r + 1]) : 0.0f;
-                    }
-                    if constexpr (kOut) {
 #pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            o[nt][2 * r] = ha::decayed(e.x, p.scale * o[nt][2 * r]);
-                            o[nt][2 * r + 1] = ha::decayed(e.y, p.scale * o[nt][2 * r + 1]);
-                        }
+                        for (int u = 0; u < TM; ++u) load4(bf[0][u], N + u * I::plane + in_block(B::by_columns(w, jj), at.b_row(), at.b_piece()));
+                        products<kLevel>(d[jj], a, bf);
                     }
-                }
-            }
-            // E^T in place, from the last sixteen tokens on: theirs are needed by no other before they change
 #pragma unroll
-            for (int jj = C / 16 - 1; jj >= 0; --jj) {
-                float w[2][4];
+                for (int jj = 0; jj < NB; ++jj)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[0][e] += d[jj][0][e];
+                        x[1][e] += d[jj][1][e];
+                    }
+                if constexpr (!kOut)
+                    if (inside && ok) dump_errors<C, kSlabs>(x, p.errors + rows * C, w);
+                weigh_tokens<false>(x, vec + I::beta / 4 + 16 * w);  // V'^T
                 uint32_t a[TM][4];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const float2 be = *reinterpret_cast<const float2*>(vec + I::beta / 4 + 16 * jj + 8 * x + j0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[x][e] = -(e & 1 ? be.y : be.x) * y[2 * jj + x][e];
+                if constexpr (kOut) {
+                    uint32_t a2[TO][4];
+                    as_operand<TO>(a2, x[0], x[1]);
+                    put_factor(os, w, a2);
                 }
-                as_operand<TM>(a, w[0], w[1]);
-#pragma unroll
-                for (int np = jj; np < C / 16; np += 2) {
-                    const int pairs = np + 1 < C / 16 ? 2 : 1;
-                    uint32_t bf[2][TM][4];
-#pragma unroll
-                    for (int g = 0; g < 2; ++g)
-#pragma unroll
-                        for (int u = 0; u < TM; ++u)
-                            if (g < pairs) load4(bf[g][u], N + u * I::plane + in_block(Blocks<C>::by_columns(np + g, jj), at.b_row(), at.b_piece()));
-                    sum<kRounded, kLevel>(y + 2 * np, a, bf, pairs);
-                }
+                weigh_tokens<false>(x, vec + I::late / 4 + 16 * w);
+                as_operand<TM>(a, x[0], x[1]);
+                put_factor(xs, w, a);
             }
-            if constexpr (!kOut)
-                if (v0 < p.dv) dump_rows(y, p.errors + (((long long)bh * p.chunks + it) * slices * 16 + v0) * C, C);
-#pragma unroll
-            for (int nt = 0; nt < C / 8; ++nt) {  // V'^T
-                const float2 be = *reinterpret_cast<const float2*>(vec + I::beta / 4 + 8 * nt + j0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[nt][e] *= e & 1 ? be.y : be.x;
-            }
-            if constexpr (kOut) {
-#pragma unroll
-                for (int jj = 0; jj < C / 16; ++jj) {
-                    uint32_t a[TO][4];
-                    as_operand<TO>(a, y[2 * jj], y[2 * jj + 1]);
-#pragma unroll
-                    for (int np = jj; np < C / 16; np += 2) {
-                        const int pairs = np + 1 < C / 16 ? 2 : 1;
-                        uint32_t bf[2][TP][4];
-#pragma unroll
-                        for (int g = 0; g < 2; ++g)
-#pragma unroll
-                            for (int u = 0; u < TP; ++u)
-                                if (g < pairs) load4(bf[g][u], P + u * I::plane + in_block(I::p_block(np + g, jj), at.b_row(), at.b_piece()));
-                        sum<kRounded, TO - 1>(o + 2 * np, a, bf, pairs);
-                    }
-                }
-                write_out<C, T>(o, &mo, p, sm8 + L::out(warps) + warp * L::own, b, h, v0, t0, live);
-            }
+            slice_sync(slice);
             const float whole = vec[I::whole / 4];
-            uint32_t au[C / 16][TM][4];
+            {   // the update by itself, added once: the old state is rounded, not cut off
+                float up[kTiles][4] = {};
 #pragma unroll
-            for (int jj = 0; jj < C / 16; ++jj) {
-                float w[2][4];
+                for (int jj = 0; jj < NB; ++jj) {
+                    uint32_t a[TM][4];
+                    get_factor(a, xs, jj);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const float2 la = *reinterpret_cast<const float2*>(vec + I::late / 4 + 16 * jj + 8 * x + j0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[x][e] = (e & 1 ? la.y : la.x) * y[2 * jj + x][e];
-                }
-                as_operand<TM>(au[jj], w[0], w[1]);
-            }
-#pragma unroll
-            for (int kp = 0; kp < KP / 16; kp += kGroup) {  // the update by itself, added once: the old state is rounded, not cut off
-                float up[2 * kGroup][4] = {};
-#pragma unroll
-                for (int jj = 0; jj < C / 16; ++jj) {
-                    uint32_t bf[kGroup][TI][4];
-#pragma unroll
-                    for (int g = 0; g < kGroup; ++g)
+                    for (int kp = 0; kp < kTiles / 2; ++kp) {
+                        uint32_t bf[1][TI][4];
 #pragma unroll
                         for (int u = 0; u < TI; ++u)
-                            load4_t(bf[g][u], K + u * (KP * C * 2) + wide<C>(16 * jj + at.bt_row(), 2 * (kp + g) + at.bt_piece()));
-                    sum<kRounded, kLevel>(up, au[jj], bf);
+                            load4_t(bf[0][u], K + u * (KP * C * 2) + wide<C>(16 * jj + at.bt_row(), k0 / 8 + 2 * kp + at.bt_piece()));
+                        sum<kRounded, kLevel>(up + 2 * kp, a, bf);
+                    }
                 }
 #pragma unroll
-                for (int n = 0; n < 2 * kGroup; ++n)
+                for (int j = 0; j < kTiles; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[2 * kp + n][e] = whole == 0.0f ? up[n][e] : fmaf(whole, s[2 * kp + n][e], up[n][e]);
+                    for (int e = 0; e < 4; ++e) s[j][e] = whole == 0.0f ? up[j][e] : fmaf(whole, s[j][e], up[j][e]);
             }
+            if constexpr (kOut)
+                if (mine) {
+#pragma unroll
+                    for (int jj = 0; jj < NB; ++jj)
+                        if (jj <= w) {
+                            uint32_t a[TO][4], bf[1][TP][4];
+                            get_factor(a, os, jj);
+#pragma unroll
+                            for (int u = 0; u < TP; ++u) load4(bf[0][u], P + u * I::plane + in_block(I::p_block(w, jj), at.b_row(), at.b_piece()));
+                            sum<kRounded, TO - 1>(far, a, bf);
+                        }
+                    if (ok) write_out<T>(far, p, b, h, v0, t0 + 16 * w, live);
+                }
             ha::release_reads();
             __syncwarp();
-            if (lane == 0) ha::bar_arrive(bars + 8 * (kEmpty + st));
+            if (lane == 0 && ok) ha::bar_arrive(bars + 8 * (kEmpty + st));
         }
-        if (kOut && lane == 0) ha::tma_store_wait_all();
-        if (kOut && warp < warps && v0 < p.dv) zero_out<T>(p, b, h, v0, count * C);
-        if (ok && p.s_out && v0 < p.dv) write_state<KP>(s, p.s_out + (long long)bh * p.dk * p.dv, p.dk, p.dv, v0);
+        if (kOut && inside) zero_out<T>(p, b, h, v0, count * C, w);
+        if (ok && p.s_out && inside) write_state(s, p.s_out + (long long)bh * p.dk * p.dv, p.dk, p.dv, v0, k0);
     }
     __syncthreads();
     if (tid == 0 && *stop) give_up(p, gave_up, 1 + *stop);

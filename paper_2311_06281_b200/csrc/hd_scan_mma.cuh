@@ -7,17 +7,17 @@
 // V^T is brought there by products with an identity.  Backward likewise from D^T:
 //     X = D^T K^T,   dV'^T = X e^{c_C-c} + dO^T P,   F = dV'^T + (-beta dV'^T) N,   Z = beta F
 //     D^T <- e^{c_C} D^T + (-e^c Z) K + (scale e^c dO^T) Q
-// Warps 0-7 have the state and the chain of dependent steps; warps 8-11 what hangs on it without the chain waiting: the output
+// Warps 0-7 have the state and the chain of dependent steps; warps 8-15 what hangs on it without the chain waiting: the output
 // (backward: dV, F and the sums over V for the gates, and the terms of dO).  One warp loads, a chunk ahead, one issues the products.
 #pragma once
 #include "hd_scan.cuh"
 
 namespace hd {
 
-constexpr int kPassThreads = 512;
-// Registers: 128 a thread at launch; 2 * 152 + 128 + 80 = 4 * 128.
-constexpr int kPassState = 152, kPassSide = 128, kPassFeed = 80;
-static_assert(2 * kPassState + kPassSide + kPassFeed <= 4 * 128, "registers");
+constexpr int kPassThreads = 640;
+// Registers: 96 a thread at launch; 2 * 136 + 2 * 80 + 48 = 5 * 96.
+constexpr int kPassState = 136, kPassSide = 80, kPassFeed = 48;
+static_assert(2 * kPassState + 2 * kPassSide + kPassFeed <= 5 * 96, "registers");
 
 constexpr uint32_t kRows32 = (256u >> 4) | (1u << 14) | (6u << 29);  // operands of 32-byte rows, swizzled so
 template <uint32_t kA, uint32_t kB>
@@ -60,7 +60,7 @@ struct PassLayout {
 
 // Sixteen values as terms of a left factor
 template <int kTerms>
-__device__ __forceinline__ void put_left(const float (&x)[16], uint32_t (&t)[kTerms][8]) {
+__device__ __forceinline__ void put_left(const uint32_t (&x)[16], uint32_t (&t)[kTerms][8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         uint32_t w[kTerms];
@@ -69,11 +69,18 @@ __device__ __forceinline__ void put_left(const float (&x)[16], uint32_t (&t)[kTe
         for (int u = 0; u < kTerms; ++u) t[u][e] = w[u];
     }
 }
-__device__ __forceinline__ void four(const float* from, float (&to)[16]) {
+// x[e] = weight[e] * x[e] for sixteen of a chunk's tokens; kPlain: no weight is zero (a weight of zero forgets whatever it is that it weighs)
+template <bool kPlain>
+__device__ __forceinline__ void weigh(const float* weight, uint32_t (&x)[16]) {
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
-        const float4 f = *reinterpret_cast<const float4*>(from + e);
-        to[e] = f.x; to[e + 1] = f.y; to[e + 2] = f.z; to[e + 3] = f.w;
+        const float4 f = *reinterpret_cast<const float4*>(weight + e);
+        const float w[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float y = __uint_as_float(x[e + u]);
+            x[e + u] = __float_as_uint(kPlain ? w[u] * y : ha::decayed(w[u], y));
+        }
     }
 }
 // 32 values of each lane, summed over the warp's lanes: lane l gets the sum of the l-th ones.
@@ -115,9 +122,9 @@ __global__ void __launch_bounds__(kPassThreads, 1)
     if (tid == 0) {
         for (int i = 0; i < kPassBars; ++i) {
             uint32_t arrivals = 1;
-            if (i >= kEmpty && i < kPatched) arrivals = kMode == 1 ? 9 : 13;  // the warps that read vectors, and the products
+            if (i >= kEmpty && i < kPatched) arrivals = kMode == 1 ? 9 : 17;  // the warps that read vectors, and the products
             if (i == kStateReady || i == kFactor || i == kWrites) arrivals = 8;
-            if (i == kFarScaled || i == kOutRead || (kBack && i == kOuter)) arrivals = 4;
+            if (i == kFarScaled || i == kOutRead || (kBack && i == kOuter)) arrivals = 8;
             ha::bar_init(bars + 8 * i, arrivals);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -128,15 +135,15 @@ __global__ void __launch_bounds__(kPassThreads, 1)
         *reinterpret_cast<__nv_bfloat16*>(sm8 + L::ident + (k >> 3) * 256 + (n >> 3) * 128 + (n & 7) * 16 + (k & 7) * 2) = __float2bfloat16(n == k ? 1.0f : 0.0f);
     }
     ha::fence_smem_to_async();
-    if (warp == 12) ha::tmem_alloc(smem_addr(s_tmem), M::columns);
+    if (warp == 16) ha::tmem_alloc(smem_addr(s_tmem), M::columns);
     ha::tmem_before_sync();
     __syncthreads();
     ha::tmem_after_sync();
     if (tid == 0 && *s_tmem != 0) *stop = 1 + kPassBars;  // all columns were asked for: they start at 0
     auto chunk_at = [&](int it) { return kBack ? count - 1 - it : it; };
-    if (warp >= 12) {
+    if (warp >= 16) {
         ha::give_registers<kPassFeed>();
-        if (warp == 12) {
+        if (warp == 16) {
             // ------------------------------------------------------------------------------------------ loads
             load_chunks<C, L::kStages>(
                 wait, sm8, L::stage, L::image, 0, count, live, p.tokens, L::bytes, p.mute,
@@ -153,7 +160,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                     for (int c = 0; c < 2; ++c) ha::tma_load_4d(to + L::v + c * L::block, &mv, v0 + 64 * c, kBack ? h : h / p.vdiv, n * C, b, bar);
                 },
                 kBack);
-        } else if (warp == 13) {
+        } else if (warp == 17) {
             // ------------------------------------------------------------------------------------------ products
             if (ha::elect_one()) {
                 constexpr uint32_t shape64 = ha::mma_shape(C, 0), shape_t = ha::mma_shape(16, ha::kColMajorA), shape_u = ha::mma_shape(KP, ha::kColMajorB);
@@ -197,12 +204,6 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                     ha::tmem_after_sync();
                     with_state(M::x, K, 3);
                     ha::mma_commit(bars + 8 * kScores);
-                    if constexpr (kOutput) {
-                        if (it > 0 && !(ok = wait(kOutRead, it - 1))) break;
-                        ha::tmem_after_sync();
-                        with_state(M::o, Q, 2);
-                        ha::mma_commit(bars + 8 * kFar);
-                    }
                     if (!(ok = wait(kFactor, it))) break;
                     ha::tmem_after_sync();
 #pragma unroll
@@ -219,6 +220,12 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                                                       ha::mma_shape(C - 16 * jj, 0), true);
                             }
                     ha::mma_commit(bars + 8 * kSolved);
+                    if constexpr (kOutput) {  // while the threads work on E
+                        if (it > 0 && !(ok = wait(kOutRead, it - 1))) break;
+                        ha::tmem_after_sync();
+                        with_state(M::o, Q, 2);
+                        ha::mma_commit(bars + 8 * kFar);
+                    }
                     if (!(ok = wait(kWrites, it))) break;
                     ha::tmem_after_sync();
                     update(K, false, false);
@@ -249,27 +256,31 @@ __global__ void __launch_bounds__(kPassThreads, 1)
         ha::give_registers<kPassSide>();
         // ---------------------------------------------------------------------------------------------- beside the chain
         if constexpr (kMode != 1) {
-            const int row = (warp & 3) * 32 + lane, v = v0 + row;
+            // a column of V and half of the tokens
+            const int row = (warp & 3) * 32 + lane, v = v0 + row, j0 = ((warp - 8) >> 2) * 32;
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-            T* const out = static_cast<T*>(p.out) + b * p.ob + h * p.oh;
+            T* const out = static_cast<T*>(p.out) + b * p.ob + h * p.oh + v;
             const bool mine = v < p.dv;
             bool ok = true;
+            auto store = [&](int t, float x) {
+                if (mine && t < p.tokens && ok) out[t * p.ot] = ha::from_f<T>(t < live ? x : 0.0f);
+            };
             for (int it = 0; it < count; ++it) {
                 const int st = it % L::kStages, n = chunk_at(it), t0 = n * C;
-                const float* const vec = reinterpret_cast<const float*>(sm8 + st * L::stage + L::image);
-                ok = ok && wait(kFull + st, it / L::kStages);
+                const float* const vec = reinterpret_cast<const float*>(sm8 + st * L::stage + L::image) + j0;
+                uint32_t x[2][16];
                 if constexpr (kOutput) {
-                    ok = ok && wait(kFar, it);
+                    ok = ok && wait(kFull + st, it / L::kStages) && wait(kFar, it);
                     ha::tmem_after_sync();
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[16];
-                        float ea[16];
-                        four(vec + I::early / 4 + 16 * c, ea);
-                        ha::tmem_ld16(x, lanes + M::o + 16 * c);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(ha::decayed(ea[e], p.scale * __uint_as_float(x[e])));
-                        ha::tmem_st16(lanes + M::o + 16 * c, x);
+                    for (int c = 0; c < 2; ++c) ha::tmem_ld16_early(x[c], lanes + M::o + j0 + 16 * c);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        ha::tmem_ready(x[c]);
+                        weigh<false>(vec + I::early / 4 + 16 * c, x[c]);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[c][e] = __float_as_uint(p.scale * __uint_as_float(x[c][e]));
+                        ha::tmem_st16(lanes + M::o + j0 + 16 * c, x[c]);
                     }
                     ha::release_reads();
                     ha::tmem_wait_st();
@@ -281,96 +292,92 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                     }
                     ok = ok && wait(kOut, it);
                     ha::tmem_after_sync();
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[16];
-                        ha::tmem_ld16(x, lanes + M::o + 16 * c);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int t = t0 + 16 * c + e;
-                            if (mine && t < p.tokens && ok) out[t * p.ot + v] = ha::from_f<T>(t < live ? __uint_as_float(x[e]) : 0.0f);
-                        }
-                    }
+                    for (int c = 0; c < 2; ++c) ha::tmem_ld16_early(x[c], lanes + M::o + j0 + 16 * c);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) ha::tmem_ready(x[c]);
                     ha::tmem_before_sync();
                     ok = __all_sync(~0u, ok);
                     if (lane == 0 && ok) ha::bar_arrive(bars + 8 * kOutRead);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) store(t0 + j0 + 16 * c + e, __uint_as_float(x[c][e]));
                 } else {
                     const long long chunk = (long long)bh * p.chunks + n;
-                    const long long at = ((chunk * slices + (v >> 4)) * C) * 16 + (v & 15);  // of E and F: [sixteen columns][token][16]
-                    float* const dots = p.dots + (chunk * 2 * p.parts + (v0 >> 5) + (warp & 3)) * C + lane;
-                    float e[C];
+                    const long long at = ((chunk * slices + (v >> 4)) * C + j0) * 16 + (v & 15);  // of E and F: [sixteen columns][token][16]
+                    const bool counts = (v0 >> 5) + (warp & 3) < p.parts;
+                    float* const dots = p.dots + (chunk * 2 * p.parts + (v0 >> 5) + (warp & 3)) * C + j0 + lane;
+                    float e[32];
 #pragma unroll
-                    for (int t = 0; t < C; ++t) e[t] = mine ? __ldcs(p.errors + at + t * 16) : 0.0f;
+                    for (int t = 0; t < 32; ++t) e[t] = mine ? __ldcs(p.errors + at + t * 16) : 0.0f;
+                    ok = ok && wait(kFull + st, it / L::kStages);
+                    const uint8_t* const go = sm8 + st * L::stage + L::v + (row >> 6) * L::block + j0 * 128;
+                    // scale e^c dO^T as terms, where X was
+                    auto outer = [&](int c) {
+                        uint32_t w[3][8];
+#pragma unroll
+                        for (int u = 0; u < 16; ++u)
+                            x[c][u] = (uint32_t)*reinterpret_cast<const uint16_t*>(go + place<128>(16 * c + u, (row & 63) >> 3) + 2 * (row & 7)) << 16;
+                        weigh<true>(vec + I::early / 4 + 16 * c, x[c]);
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) x[c][u] = __float_as_uint(p.scale * __uint_as_float(x[c][u]));
+                        put_left<3>(x[c], w);
+#pragma unroll
+                        for (int u = 0; u < 3; ++u) ha::tmem_st8(lanes + M::outer(j0 / 16 + c, u), w[u]);
+                    };
                     ok = ok && wait(kScores, it);
                     ha::tmem_after_sync();
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {  // e^{c_C-c} k^T D V', over this warp's columns
-                        float x[32];
+                    for (int c = 0; c < 2; ++c) ha::tmem_ld16_early(x[c], lanes + M::x + j0 + 16 * c);
+                    float y[32];  // e^{c_C-c} k^T D V', over this warp's columns
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            uint32_t w[16];
-                            float la[16], be[16];
-                            four(vec + I::late / 4 + 32 * half + 16 * c, la);
-                            four(vec + I::beta / 4 + 32 * half + 16 * c, be);
-                            ha::tmem_ld16(w, lanes + M::x + 32 * half + 16 * c);
+                    for (int c = 0; c < 2; ++c) {
+                        ha::tmem_ready(x[c]);
+                        weigh<false>(vec + I::late / 4 + 16 * c, x[c]);
 #pragma unroll
-                            for (int u = 0; u < 16; ++u) x[16 * c + u] = ha::decayed(la[u], __uint_as_float(w[u])) * (be[u] * e[32 * half + 16 * c + u]);
-                        }
-                        const float sum = sum_across(x);
-                        if (ok && (v0 >> 5) + (warp & 3) < p.parts) dots[p.parts * C + 32 * half] = sum;
+                        for (int u = 0; u < 16; ++u) y[16 * c + u] = __uint_as_float(x[c][u]) * e[16 * c + u];
                     }
                     ok = ok && wait(kFactor, it);  // X and dO^T P have been read
-                    const uint8_t* const go = sm8 + st * L::stage + L::v + (row >> 6) * L::block;
-#pragma unroll 1
-                    for (int jj = 0; jj < 4; ++jj) {  // scale e^c dO^T
-                        float x[16], ea[16];
-                        four(vec + I::early / 4 + 16 * jj, ea);
 #pragma unroll
-                        for (int u = 0; u < 16; ++u)
-                            x[u] = p.scale * ea[u] * __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(go + place<128>(16 * jj + u, (row & 63) >> 3) + 2 * (row & 7)));
-                        uint32_t w[3][8];
-                        put_left<3>(x, w);
-#pragma unroll
-                        for (int u = 0; u < 3; ++u) ha::tmem_st8(lanes + M::outer(jj, u), w[u]);
-                    }
+                    for (int c = 0; c < 2; ++c) outer(c);
                     ha::tmem_wait_st();
                     ha::tmem_before_sync();
                     ok = __all_sync(~0u, ok);
                     if (lane == 0 && ok) ha::bar_arrive(bars + 8 * kOuter);
+                    const float beta = vec[I::beta / 4 + lane];
+                    const float sum = beta * sum_across(y);
+                    if (ok && counts) dots[p.parts * C] = sum;
                     ok = ok && wait(kSolved, it);
                     ha::tmem_after_sync();
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        float x[32];
+                    for (int c = 0; c < 2; ++c) ha::tmem_ld16_early(x[c], lanes + M::y + j0 + 16 * c);
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            uint32_t w[16];
-                            float be[16];
-                            four(vec + I::beta / 4 + 32 * half + 16 * c, be);
-                            ha::tmem_ld16(w, lanes + M::y + 32 * half + 16 * c);
-#pragma unroll
-                            for (int u = 0; u < 16; ++u) {
-                                const float f = __uint_as_float(w[u]);
-                                const int j = 32 * half + 16 * c + u, t = t0 + j;
-                                if (ok && (v >> 4) < slices) p.errors_back[at + j * 16] = f;
-                                if (ok && mine && t < p.tokens) out[t * p.ot + v] = ha::from_f<T>(t < live ? be[u] * f : 0.0f);
-                                x[16 * c + u] = f * e[j];
-                            }
-                        }
-                        const float sum = sum_across(x);
-                        if (ok && (v0 >> 5) + (warp & 3) < p.parts) dots[32 * half] = sum;
-                    }
-                    ha::release_reads();
+                    for (int c = 0; c < 2; ++c) ha::tmem_ready(x[c]);
                     ha::tmem_before_sync();
                     ok = __all_sync(~0u, ok);
-                    if (lane == 0 && ok) {
-                        ha::bar_arrive(bars + 8 * kSolvedRead);
-                        ha::bar_arrive(bars + 8 * (kEmpty + st));
+                    if (lane == 0 && ok) ha::bar_arrive(bars + 8 * kSolvedRead);
+#pragma unroll
+                    for (int t = 0; t < 32; ++t) {
+                        const float f = __uint_as_float(x[t >> 4][t & 15]);
+                        if (ok && (v >> 4) < slices) p.errors_back[at + t * 16] = f;
+                        e[t] *= f;
                     }
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        weigh<true>(vec + I::beta / 4 + 16 * c, x[c]);
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) store(t0 + j0 + 16 * c + u, __uint_as_float(x[c][u]));
+                    }
+                    ha::release_reads();
+                    __syncwarp();
+                    if (lane == 0 && ok) ha::bar_arrive(bars + 8 * (kEmpty + st));
+                    const float sum2 = sum_across(e);
+                    if (ok && counts) dots[0] = sum2;
                 }
             }
-            for (long long t = (long long)count * C; t < p.tokens; ++t)  // chunks without a token of the sequence
-                if (mine) out[t * p.ot + v] = ha::from_f<T>(0.0f);
+            for (long long t = (long long)count * C + (j0 ? 1 : 0); t < p.tokens; t += 2)  // chunks without a token of the sequence
+                if (mine) out[t * p.ot] = ha::from_f<T>(0.0f);
         }
     } else {
         ha::take_registers<kPassState>();
@@ -392,10 +399,9 @@ __global__ void __launch_bounds__(kPassThreads, 1)
         auto publish = [&]() {  // the state's terms
 #pragma unroll
             for (int q = 0; q < kOwn / 16; ++q) {
-                float x[16];
-                uint32_t w[3][8];
+                uint32_t x[16], w[3][8];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = s[16 * q + e];
+                for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(s[16 * q + e]);
                 put_left<3>(x, w);
 #pragma unroll
                 for (int t = 0; t < 3; ++t) ha::tmem_st8(lanes + M::state(half, q, t), w[t]);
@@ -413,30 +419,38 @@ __global__ void __launch_bounds__(kPassThreads, 1)
             if (kBack && it > 0) ok = ok && wait(kSolvedRead, it - 1);  // F of the chunk before
             ok = ok && wait(kScores, it);
             ha::tmem_after_sync();
+            const float whole = vec[I::whole / 4];
+            auto factors = [&](auto plain) {  // plain: no weight is zero, and all tokens are the sequence's
+                constexpr bool kPlain = decltype(plain)::value;
+                uint32_t x[2][16], y[2][16];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int jj = 2 * half + g, j = 16 * jj;
-                uint32_t x[16], y[16];
-                float we[16], be[16], z[16];
-                ha::tmem_ld16_early(x, lanes + M::x + j);
-                ha::tmem_ld16_early(y, lanes + (kBack ? M::o : M::y) + j);
-                four(vec + (kBack ? I::late : I::early) / 4 + j, we);
-                four(vec + I::beta / 4 + j, be);
-                ha::tmem_ready(x);
-                ha::tmem_ready(y);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float far = ha::decayed(we[e], __uint_as_float(x[e])), near = __uint_as_float(y[e]);
-                    const float f = t0 + j + e < live ? (kBack ? near + far : near - far) : 0.0f;
-                    y[e] = __float_as_uint(f);
-                    z[e] = -be[e] * f;
+                for (int g = 0; g < 2; ++g) {
+                    ha::tmem_ld16_early(x[g], lanes + M::x + 32 * half + 16 * g);
+                    ha::tmem_ld16_early(y[g], lanes + (kBack ? M::o : M::y) + 32 * half + 16 * g);
                 }
-                ha::tmem_st16(lanes + M::y + j, y);
-                uint32_t w[3][8];
-                put_left<3>(z, w);
 #pragma unroll
-                for (int t = 0; t < 3; ++t) ha::tmem_st8(lanes + M::factor(jj, t), w[t]);
-            }
+                for (int g = 0; g < 2; ++g) {
+                    const int jj = 2 * half + g, j = 16 * jj;
+                    ha::tmem_ready(x[g]);
+                    ha::tmem_ready(y[g]);
+                    weigh<kPlain>(vec + (kBack ? I::late : I::early) / 4 + j, x[g]);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float f = kBack ? __uint_as_float(y[g][e]) + __uint_as_float(x[g][e]) : __uint_as_float(y[g][e]) - __uint_as_float(x[g][e]);
+                        y[g][e] = __float_as_uint(kPlain || t0 + j + e < live ? f : 0.0f);
+                    }
+                    ha::tmem_st16(lanes + M::y + j, y[g]);
+                    weigh<true>(vec + I::beta / 4 + j, y[g]);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[g][e] ^= 0x80000000u;
+                    uint32_t w[3][8];
+                    put_left<3>(y[g], w);
+#pragma unroll
+                    for (int t = 0; t < 3; ++t) ha::tmem_st8(lanes + M::factor(jj, t), w[t]);
+                }
+            };
+            if (whole != 0.0f && t0 + C <= live) factors(Int<1>{});
+            else factors(Int<0>{});
             ha::tmem_wait_st();
             ha::tmem_before_sync();
             arrive(kFactor);
@@ -449,38 +463,38 @@ __global__ void __launch_bounds__(kPassThreads, 1)
             }
             ok = ok && wait(kSolved, it);
             ha::tmem_after_sync();
+            {
+                uint32_t x[2][16];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const int jj = 2 * half + g, j = 16 * jj;
-                uint32_t x[16];
-                float we[16], be[16], z[16];
-                ha::tmem_ld16_early(x, lanes + M::y + j);
-                four(vec + I::beta / 4 + j, be);
-                four(vec + (kBack ? I::early : I::late) / 4 + j, we);
-                ha::tmem_ready(x);
-                if constexpr (kMode == 1) {
-                    if (ok && (v >> 4) < slices) {
-                        float* const to = p.errors + ((chunk * slices + (v >> 4)) * C + j) * 16 + (v & 15);
+                for (int g = 0; g < 2; ++g) ha::tmem_ld16_early(x[g], lanes + M::y + 32 * half + 16 * g);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) to[e * 16] = __uint_as_float(x[e]);
+                for (int g = 0; g < 2; ++g) {
+                    const int jj = 2 * half + g, j = 16 * jj;
+                    ha::tmem_ready(x[g]);
+                    if constexpr (kMode == 1) {
+                        if (ok && (v >> 4) < slices) {
+                            float* const to = p.errors + ((chunk * slices + (v >> 4)) * C + j) * 16 + (v & 15);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) to[e * 16] = __uint_as_float(x[g][e]);
+                        }
                     }
+                    weigh<true>(vec + I::beta / 4 + j, x[g]);
+                    if constexpr (kOutput) {
+                        uint32_t w[2][8];
+                        put_left<2>(x[g], w);
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) ha::tmem_st8(lanes + M::value(jj, t), w[t]);
+                    }
+                    weigh<true>(vec + (kBack ? I::early : I::late) / 4 + j, x[g]);
+                    if constexpr (kBack)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[g][e] ^= 0x80000000u;
+                    uint32_t w[3][8];
+                    put_left<3>(x[g], w);
+#pragma unroll
+                    for (int t = 0; t < 3; ++t) ha::tmem_st8(lanes + M::factor(jj, t), w[t]);
                 }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) z[e] = be[e] * __uint_as_float(x[e]);
-                if constexpr (kOutput) {
-                    uint32_t w[2][8];
-                    put_left<2>(z, w);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) ha::tmem_st8(lanes + M::value(jj, t), w[t]);
-                }
-#pragma unroll
-                for (int e = 0; e < 16; ++e) z[e] *= kBack ? -we[e] : we[e];
-                uint32_t w[3][8];
-                put_left<3>(z, w);
-#pragma unroll
-                for (int t = 0; t < 3; ++t) ha::tmem_st8(lanes + M::factor(jj, t), w[t]);
             }
-            const float whole = vec[I::whole / 4];
             ha::release_reads();
             ha::tmem_wait_st();
             ha::tmem_before_sync();
@@ -506,7 +520,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
     }
     ha::tmem_before_sync();
     __syncthreads();
-    if (warp == 12) ha::tmem_free(0, M::columns);
+    if (warp == 16) ha::tmem_free(0, M::columns);
     if (tid == 0 && *stop) give_up(p, gave_up, 200 + *stop);
 }
 

@@ -51,23 +51,21 @@ hs_status forward(const heinsen_delta_problem* dp, const heinsen_attention_tenso
     q.image = ws + sp.image;
     q.s_in = p->state0; q.s_out = state;
     q.out = const_cast<void*>(o->ptr); q.ob = o->batch_stride; q.ot = o->token_stride; q.oh = o->head_stride;
-    const View out = view_of(*o, p->heads, p->heads, p->v_dim);
-    q.out_tma = !on_tcgen05<KP, TI>() && TI == 1 && p->tokens && tma_strides(out, p->batch, p->tokens);
-    CUtensorMap mq, mk, mv, mo;
-    std::memset(&mo, 0, sizeof mo);
+    const bool many = fits_tcgen05<KP, TI>() && many_slices(p);
+    CUtensorMap mq, mk, mv;
     hs_status st;
     if (p->tokens) {
         if ((st = map_of<T, TI>(&mq, p, view_of(p->q, p->heads, p->q_heads, p->k_dim), ws + sp.q, 64, C, stream)) != HS_OK) return st;
         if ((st = map_of<T, TI>(&mk, p, view_of(p->k, p->heads, p->k_heads, p->k_dim), ws + sp.k, 64, C, stream)) != HS_OK) return st;
-        if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, on_tcgen05<KP, TI>() ? 64 : 16, C, stream)) != HS_OK) return st;
-        if (q.out_tma && !encode(&mo, out, p->batch, p->tokens, 16, C)) return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
+        if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, many ? 64 : 16, C, stream)) != HS_OK) return st;
         if ((st = launch_chunks<KP, C, TI, TM, TP, false>(mq, mk, q, word, stream)) != HS_OK) return st;
     } else {
         std::memset(&mq, 0, sizeof mq);
         mk = mv = mq;  // no chunk is loaded
     }
-    if constexpr (on_tcgen05<KP, TI>()) return launch_pass<KP, 0, T>(mq, mk, mv, q, word, stream);
-    else return launch_scan<KP, C, TI, TM, TP, true, T>(mq, mk, mv, mo, q, word, stream);
+    if constexpr (fits_tcgen05<KP, TI>())
+        if (many) return launch_pass<KP, 0, T>(mq, mk, mv, q, word, stream);
+    return launch_scan<KP, C, TI, TM, TP, true, T>(mq, mk, mv, q, word, stream);
 }
 
 template <class T>

@@ -44,23 +44,10 @@ hs_status shared_sum(const float* from, void* to, const heinsen_attention_proble
 }
 
 template <int KP, int TI, class T>
-hs_status launch_back(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mg, const CUtensorMap& mo, const hd::Params& q, int* word,
-                      cudaStream_t stream) {
+hs_status launch_back(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mg, const hd::Params& q, int* word, cudaStream_t stream) {
     constexpr int C = hd::chunk_tokens(KP), TM = terms_of(TI);
-    using L = hd::ScanLayout<KP, C, TI, TM, TM, true, true>;
-    static_assert(L::end(hd::kMaxWarps) <= 232448, "shared memory");
-    const auto fn = hd::back_kernel<KP, C, TI, TM, T>;
     static std::atomic<unsigned long long> done{0};
-    const hs_status st = allow_smem(reinterpret_cast<const void*>(fn), (int)L::end(hd::kMaxWarps), done);
-    if (st != HS_OK) return st;
-    const long long pairs = (long long)q.batch * q.heads;
-    const int slices = (q.dv + 15) / 16, warps = warps_for(pairs, slices);
-    const long long grid = pairs * ((slices + warps - 1) / warps);
-    if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
-    hd::Params w = q;
-    w.warps = warps;
-    fn<<<(unsigned)grid, 32 * (hd::loader_of(warps) + 4), L::end(warps), stream>>>(mq, mk, mg, mo, w, word);
-    return launched("back_kernel");
+    return launch_slices<hd::ScanLayout<KP, C, TI, TM, TM, true, true>>(hd::back_kernel<KP, C, TI, TM, T>, done, mq, mk, mg, q, word, stream);
 }
 
 // The gradients of the chunks: tcgen05 for bf16 and keys up to 128 wide (8 x 2048 tokens, 16 heads of 128: see the figures in
@@ -111,17 +98,16 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
     hd::Params q = params_of(dp, C, ws);
     q.image = ws + sp.image;
     q.states = at(sp.states); q.gradients = at(sp.gradients); q.errors = at(sp.errors); q.errors_back = at(sp.back); q.dots = at(sp.dots);
-    CUtensorMap mq, mk, mv, mg, mo;
-    std::memset(&mo, 0, sizeof mo);
+    CUtensorMap mq, mk, mv, mg;
     hs_status st;
     if ((st = map_of<T, TI>(&mq, p, view_of(p->q, p->heads, p->q_heads, p->k_dim), ws + sp.q, 64, C, stream)) != HS_OK) return st;
     if ((st = map_of<T, TI>(&mk, p, view_of(p->k, p->heads, p->k_heads, p->k_dim), ws + sp.k, 64, C, stream)) != HS_OK) return st;
-    constexpr bool kTcgen05 = on_tcgen05<KP, TI>();
-    q.parts = kTcgen05 ? (p->v_dim + 31) / 32 : (p->v_dim + 15) / 16;
-    if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, kTcgen05 ? 64 : 16, C, stream)) != HS_OK) return st;
+    const bool many = fits_tcgen05<KP, TI>() && many_slices(p);
+    q.parts = many ? (p->v_dim + 31) / 32 : (p->v_dim + 15) / 16;
+    if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, many ? 64 : 16, C, stream)) != HS_OK) return st;
     if ((st = map_of<T, TI>(&mg, p, view_of(*d_o, p->heads, p->heads, p->v_dim), ws + sp.g, 16, C, stream)) != HS_OK) return st;
     CUtensorMap mg64 = mg;  // the same in tiles of 64 columns
-    if (kTcgen05) {
+    if (many) {
         View g = view_of(*d_o, p->heads, p->heads, p->v_dim);
         if (terms_bytes(p, g)) {
             const long long sh = (p->v_dim + 7) / 8 * 8, stk = sh * p->heads;
@@ -133,8 +119,8 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
     {
         hd::Params f = q;
         f.s_in = p->state0;
-        if constexpr (kTcgen05) st = launch_pass<KP, 1, T>(mq, mk, mv, f, word, stream);
-        else st = launch_scan<KP, C, TI, TM, TM, false, T>(mq, mk, mv, mo, f, word, stream);
+        if constexpr (fits_tcgen05<KP, TI>()) st = many ? launch_pass<KP, 1, T>(mq, mk, mv, f, word, stream) : launch_scan<KP, C, TI, TM, TM, false, T>(mq, mk, mv, f, word, stream);
+        else st = launch_scan<KP, C, TI, TM, TM, false, T>(mq, mk, mv, f, word, stream);
         if (st != HS_OK) return st;
     }
     {
@@ -143,11 +129,13 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
         const bool each = p->v_heads != p->heads;
         r.out = each ? ws + sp.dv : dv;
         r.oh = p->v_dim; r.ot = (long long)p->heads * p->v_dim; r.ob = p->tokens * r.ot;
-        const View out{{r.out, r.ob, r.ot, r.oh, 1}, p->heads, p->v_dim};
-        r.out_tma = !kTcgen05 && !each && TI == 1 && tma_strides(out, p->batch, p->tokens);
-        if (r.out_tma && !encode(&mo, out, p->batch, p->tokens, 16, C)) return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
-        if constexpr (kTcgen05) st = each ? launch_pass<KP, 2, float>(mq, mk, mg64, r, word, stream) : launch_pass<KP, 2, T>(mq, mk, mg64, r, word, stream);
-        else st = each ? launch_back<KP, TI, float>(mq, mk, mg, mo, r, word, stream) : launch_back<KP, TI, T>(mq, mk, mg, mo, r, word, stream);
+        auto back = [&](auto type) {
+            using Out = decltype(type);
+            if constexpr (fits_tcgen05<KP, TI>())
+                if (many) return launch_pass<KP, 2, Out>(mq, mk, mg64, r, word, stream);
+            return launch_back<KP, TI, Out>(mq, mk, mg, r, word, stream);
+        };
+        st = each ? back(float{}) : back(T{});
         if (st != HS_OK) return st;
         if (each && (st = shared_sum<T>(at(sp.dv), dv, p, p->v_heads, p->v_dim, stream)) != HS_OK) return st;
     }
