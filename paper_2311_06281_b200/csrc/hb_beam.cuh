@@ -227,65 +227,77 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Select p) {
         }
     }
     __syncthreads();
-    const int lists = p.parts * p.keep, each = lists + 2, total = p.beams * each;
+    const int lists = p.parts * p.keep;
     // Of a beam without candidates of its own the first tokens count, at -inf, as many as could be needed.
-    auto candidate = [&](int c, double& value, long long& place) {
-        const int w = c / each, i = c - w * each;
-        value = lowest;
-        place = nowhere;
-        long long n = -1;
-        if (state[w] == 0) {
-            if (i < lists) {
-                const long long at = (b * p.beams + w) * lists + i;
-                n = p.part_token[at];
-                if (n >= 0) value = logs[w] + (double)p.part_value[at];
+    auto each_candidate = [&](auto take) {
+        for (int w = warp; w < p.beams; w += kThreads / 32) {
+            const int how = state[w];
+            const long long row0 = (long long)w * p.vocabulary;
+            if (how == 0) {
+                const double base = logs[w];
+                const long long at = (b * p.beams + w) * lists;
+                for (int i = lane; i < lists; i += 32) {
+                    const int n = p.part_token[at + i];
+                    if (n >= 0) take(base + (double)p.part_value[at + i], row0 + n);
+                }
+            } else {
+                for (int i = lane; i <= p.keep && i < p.vocabulary; i += 32)
+                    if (!(how == 1 && i == p.end_token)) take(lowest, row0 + i);
+                if (how == 1 && lane == 0) take((double)p.scores[b * p.beams + w], row0 + p.end_token);
             }
-        } else if (i == lists + 1) {
-            if (state[w] == 1) {
-                n = p.end_token;
-                value = (double)p.scores[b * p.beams + w];
-            }
-        } else if (i <= p.keep && i < p.vocabulary && !(state[w] == 1 && i == p.end_token)) {
-            n = i;
         }
-        if (n >= 0) place = (long long)w * p.vocabulary + n;
     };
     auto before = [](double v, long long at, double u, long long other) { return v > u || (v == u && at < other); };
     double value = lowest;
     long long place = nowhere;
-    for (int c = tid; c < total; c += kThreads) {
-        double v;
-        long long at;
-        candidate(c, v, at);
+    each_candidate([&](double v, long long at) {
         if (before(v, at, value, place)) {
             value = v;
             place = at;
         }
+    });
+    double group_value = value;
+    long long group_place = place;
+    const bool few = p.keep <= 16;
+    if (few)  // the best of every eight threads
+#pragma unroll
+        for (int o = 1; o < 8; o *= 2) {
+            const double v = __shfl_xor_sync(~0u, group_value, o);
+            const long long at = __shfl_xor_sync(~0u, group_place, o);
+            if (before(v, at, group_value, group_place)) {
+                group_value = v;
+                group_place = at;
+            }
+        }
+    const int each = few ? 8 : 1, members = kThreads / each;
+    if (tid % each == 0) {
+        value_of[tid / each] = group_value;
+        place_of[tid / each] = group_place;
     }
-    value_of[tid] = value;
-    place_of[tid] = place;
     __syncthreads();
-    int rank = 0;
-    for (int i = 0; i < kThreads; ++i) rank += before(value_of[i], place_of[i], value, place) || (place_of[i] == place && i < tid);
-    if (rank == p.keep - 1) {
-        least_value = value;
-        least_place = place;
+    if (tid < members) {
+        const double v = value_of[tid];
+        const long long at = place_of[tid];
+        int rank = 0;
+#pragma unroll 4
+        for (int i = 0; i < members; ++i) rank += before(value_of[i], place_of[i], v, at) || (place_of[i] == at && i < tid);
+        if (rank == p.keep - 1) {
+            least_value = v;
+            least_place = at;
+        }
     }
     __syncthreads();
     const double bound = least_value;
     const long long bound_place = least_place;
-    for (int c = tid; c < total; c += kThreads) {
-        double v;
-        long long at;
-        candidate(c, v, at);
-        if (at != nowhere && !before(bound, bound_place, v, at)) {
+    each_candidate([&](double v, long long at) {
+        if (!before(bound, bound_place, v, at)) {
             const int to = atomicAdd(&found, 1);
             if (to < kJoinList) {
                 value_of[to] = v;
                 place_of[to] = at;
             }
         }
-    }
+    });
     __syncthreads();
     const int count = found;
     auto put = [&](int k, double v, long long at) {
@@ -310,15 +322,12 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Select p) {
     for (int k = 0; k < p.keep; ++k) {
         value = lowest;
         place = nowhere;
-        for (int c = tid; c < total; c += kThreads) {
-            double v;
-            long long at;
-            candidate(c, v, at);
-            if (at != nowhere && before(last_value, last_place, v, at) && before(v, at, value, place)) {
+        each_candidate([&](double v, long long at) {
+            if (before(last_value, last_place, v, at) && before(v, at, value, place)) {
                 value = v;
                 place = at;
             }
-        }
+        });
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             const double v = __shfl_xor_sync(~0u, value, o);

@@ -1,15 +1,11 @@
 // What the forward and the backward pass of the delta rule share on the host.
 #pragma once
-#include <cstdlib>
 #include <cstring>
 
 #include "../../include/heinsen_delta.h"
 #include "ha_host.h"
 #include "hd_scan_mma.cuh"
 
-#ifndef HD_MID
-#define HD_MID 3
-#endif
 namespace hd_host {
 
 using namespace ha_host;
@@ -65,9 +61,11 @@ hs_status map_of(CUtensorMap* m, const heinsen_attention_problem* p, const View&
     View w = v;
     if (terms_bytes(p, v)) {
         const int width = (v.dim + 7) / 8 * 8;
-        const long long total = p->batch * p->tokens * v.own_heads * width;
-        hd::terms_kernel<TI, T><<<(unsigned)std::min<long long>((total + 255) / 256, kSms * 16), 256, 0, stream>>>(
-            v.rows, reinterpret_cast<__nv_bfloat16*>(space), (int)p->tokens, v.own_heads, v.dim, width, total);
+        const long long pieces = p->batch * p->tokens * v.own_heads * (width / 8);
+        const bool whole = TI == 3 && v.dim % 8 == 0 && (v.rows.sb | v.rows.st | v.rows.sh) % 4 == 0 && (reinterpret_cast<uintptr_t>(v.rows.ptr) & 15u) == 0;
+        const auto fn = whole ? hd::terms_kernel<TI, T, true> : hd::terms_kernel<TI, T, false>;
+        fn<<<(unsigned)std::min<long long>((pieces + 255) / 256, kSms * 16), 256, 0, stream>>>(
+            v.rows, reinterpret_cast<__nv_bfloat16*>(space), (uint32_t)p->tokens, (uint32_t)v.own_heads, v.dim, width, pieces);
         const hs_status st = launched("terms_kernel");
         if (st != HS_OK) return st;
         const long long sh = width, stk = sh * v.own_heads;
@@ -141,10 +139,17 @@ hs_status launch_scan(const CUtensorMap& mq, const CUtensorMap& mk, const CUtens
 
 // Whether the passes can run on tcgen05: bf16 and keys up to 128 wide; and whether they do.
 template <int KP, int TI> constexpr bool fits_tcgen05() { return TI == 1 && KP <= 128; }
-#ifndef HD_PAIRS
-#define HD_PAIRS 1000000
-#endif
-inline bool many_slices(const heinsen_attention_problem* p) { static const long long most = getenv("HDP") ? atoll(getenv("HDP")) : HD_PAIRS; return p->batch * p->heads * ((p->v_dim + 15) / 16) >= most; }
+
+// Which of the two: a CTA with four warps for each of one or two slices of sixteen columns of V (mma.sync), or one with 128 columns
+// (tcgen05).  Measured for a chunk, keys and values 128 wide, with one CTA to an SM: one slice 2.3 us, two 3.4 us, 128 columns 5.1 us
+// forward; for the gradients (both passes) two slices 6.4 us, 128 columns 12.9 us.  So two slices as long as their waves over the SMs
+// are at most 3/2 (2) of the other's: 16 (batch, head) pairs of 16385 tokens are 590 us against 1180, 64 pairs of 2048 218 us against
+// 162, 128 pairs with their gradients 820 us against 414.
+inline bool many_slices(const heinsen_attention_problem* p, bool backward) {
+    const long long pairs = p->batch * p->heads, slices = (p->v_dim + 15) / 16, two = (pairs * ((slices + 1) / 2) + kSms - 1) / kSms,
+                    all = (pairs * ((p->v_dim + 127) / 128) + kSms - 1) / kSms;
+    return pairs * slices > kSms && (backward ? two > 2 * all : 2 * two > 3 * all);
+}
 
 template <int KP, int kMode, class T>
 hs_status launch_pass(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const hd::Params& q, int* word, cudaStream_t stream) {

@@ -864,20 +864,28 @@ __global__ void __launch_bounds__(kScanThreads, 1)
 // ------------------------------------------------------------------------------------------------- tensors for TMA
 
 // A [batch, tokens, heads, dim] tensor that TMA cannot load as it is (float32, odd sizes or strides) as bf16 terms,
-// [term][batch][tokens][heads][width], columns from dim on zero.
-template <int TI, class T>
-__global__ void __launch_bounds__(256) terms_kernel(const ha::Rows from, __nv_bfloat16* to, int tokens, int heads, int dim, int width, long long total) {
-    for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < total; e += (long long)gridDim.x * blockDim.x) {
-        const int d = (int)(e % width);
-        const long long row = e / width, bt = row / heads;
-        float x = 0.0f;
-        if (d < dim) x = ha::to_f(static_cast<const T*>(from.ptr)[bt / tokens * from.sb + bt % tokens * from.st + row % heads * from.sh + d]);
+// [term][batch][tokens][heads][width], columns from dim on zero.  A thread has eight columns of a row; kWhole: they are there, at
+// addresses of 16 bytes.
+template <int TI, class T, bool kWhole>
+__global__ void __launch_bounds__(256) terms_kernel(const ha::Rows from, __nv_bfloat16* to, uint32_t tokens, uint32_t heads, int dim, int width, long long pieces) {
+    for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < pieces; e += (long long)gridDim.x * blockDim.x) {
+        const uint32_t along = width / 8;
+        const long long row = e / along, bt = row / heads;
+        const int d = 8 * (int)(e - row * along);
+        const T* const at = static_cast<const T*>(from.ptr) + bt / tokens * from.sb + bt % tokens * from.st + row % heads * from.sh + d;
+        float x[8];
+        if constexpr (kWhole && sizeof(T) == 4) {
+            const float4 a = reinterpret_cast<const float4*>(at)[0], b = reinterpret_cast<const float4*>(at)[1];
+            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+        } else {
 #pragma unroll
-        for (int u = 0; u < TI; ++u) {
-            const __nv_bfloat16 t = __float2bfloat16_rn(x);
-            to[u * total + e] = t;
-            x -= __bfloat162float(t);
+            for (int i = 0; i < 8; ++i) x[i] = d + i < dim ? ha::to_f(at[i]) : 0.0f;
         }
+        uint32_t t[4][TI];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ha::split<TI>(ha::make_pair2(x[2 * i], x[2 * i + 1]), t[i]);
+#pragma unroll
+        for (int u = 0; u < TI; ++u) reinterpret_cast<uint4*>(to)[u * pieces + e] = make_uint4(t[0][u], t[1][u], t[2][u], t[3][u]);
     }
 }
 

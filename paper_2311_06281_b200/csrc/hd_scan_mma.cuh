@@ -54,7 +54,9 @@ struct PassLayout {
     static constexpr uint32_t k = 0, q = tile, v = kMode == 1 ? tile : 2 * tile, image = v + 2 * block;  // V (backward: dO): 128 columns
     // backward N is wanted by rows
     static constexpr uint32_t n = image + I::n, p = n + 3 * I::plane, stage = (p + (kMode == 0 ? I::plane : kMode == 2 ? 3 * I::plane : 0) + 1023) / 1024 * 1024;
-    static constexpr uint32_t ident = kStages * stage, bars = ident + 512, end = bars + 256;
+    // backward E^T as well, eight times [token][16]
+    static constexpr uint32_t errors = stage, whole = stage + (kMode == 2 ? 8 * C * 64 : 0);
+    static constexpr uint32_t ident = kStages * whole, bars = ident + 512, end = bars + 256;
     static constexpr uint32_t bytes = p + (kMode == 0 ? I::plane : kMode == 2 ? 3 * I::plane : 0);  // of a chunk
 };
 
@@ -118,7 +120,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
     const Waiter wait{bars, stop, p.spin};
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int slabs = (p.dv + 127) / 128, bh = blockIdx.x / slabs, b = bh / p.heads, h = bh % p.heads, v0 = (blockIdx.x % slabs) * 128;
-    const int slices = (p.dv + 15) / 16, live = live_tokens(p.lengths, b, p.tokens), count = (live + C - 1) / C;
+    const int slices = (p.dv + 15) / 16, here = min(8, slices - v0 / 16), live = live_tokens(p.lengths, b, p.tokens), count = (live + C - 1) / C;
     if (tid == 0) {
         for (int i = 0; i < kPassBars; ++i) {
             uint32_t arrivals = 1;
@@ -146,12 +148,13 @@ __global__ void __launch_bounds__(kPassThreads, 1)
         if (warp == 16) {
             // ------------------------------------------------------------------------------------------ loads
             load_chunks<C, L::kStages>(
-                wait, sm8, L::stage, L::image, 0, count, live, p.tokens, L::bytes, p.mute,
+                wait, sm8, L::whole, L::image, 0, count, live, p.tokens, L::bytes + (kBack ? here * C * 64 : 0), p.mute,
                 [&](int n, int s, uint32_t bar) {
-                    const uint32_t to = base + s * L::stage;
+                    const uint32_t to = base + s * L::whole;
                     const uint8_t* const image = p.image + ((long long)bh * p.chunks + n) * I::end;
                     bulk_load(to + L::image, image, I::n, bar);
                     bulk_load(to + L::n, image + (kBack ? I::rows : I::n), 3 * I::plane, bar);
+                    if (kBack) bulk_load(to + L::errors, p.errors + (((long long)bh * p.chunks + n) * slices + v0 / 16) * 16 * C, here * C * 64, bar);
                     if (kMode != 1) bulk_load(to + L::p, image + I::p, (kBack ? 3 : 1) * I::plane, bar);
                     for (int c = 0; c < KP / 64; ++c) {
                         ha::tma_load_4d(to + L::k + c * L::block, &mk, 64 * c, h / p.kdiv, n * C, b, bar);
@@ -185,7 +188,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                 bool ok = true;
                 for (int it = 0; it < count; ++it) {
                     const int st = it % L::kStages;
-                    const uint32_t at = base + st * L::stage, K = ha::operand(at + L::k, L::block), Q = ha::operand(at + L::q, L::block),
+                    const uint32_t at = base + st * L::whole, K = ha::operand(at + L::k, L::block), Q = ha::operand(at + L::q, L::block),
                                    V = ha::operand(at + L::v, L::block), N = ha::operand(at + L::n, 512), P = ha::operand(at + L::p, 512);
                     if (!(ok = wait(kFull + st, it / L::kStages))) break;
                     ha::tmem_after_sync();
@@ -267,7 +270,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
             };
             for (int it = 0; it < count; ++it) {
                 const int st = it % L::kStages, n = chunk_at(it), t0 = n * C;
-                const float* const vec = reinterpret_cast<const float*>(sm8 + st * L::stage + L::image) + j0;
+                const float* const vec = reinterpret_cast<const float*>(sm8 + st * L::whole + L::image) + j0;
                 uint32_t x[2][16];
                 if constexpr (kOutput) {
                     ok = ok && wait(kFull + st, it / L::kStages) && wait(kFar, it);
@@ -308,11 +311,9 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                     const long long at = ((chunk * slices + (v >> 4)) * C + j0) * 16 + (v & 15);  // of E and F: [sixteen columns][token][16]
                     const bool counts = (v0 >> 5) + (warp & 3) < p.parts;
                     float* const dots = p.dots + (chunk * 2 * p.parts + (v0 >> 5) + (warp & 3)) * C + j0 + lane;
-                    float e[32];
-#pragma unroll
-                    for (int t = 0; t < 32; ++t) e[t] = mine ? __ldcs(p.errors + at + t * 16) : 0.0f;
                     ok = ok && wait(kFull + st, it / L::kStages);
-                    const uint8_t* const go = sm8 + st * L::stage + L::v + (row >> 6) * L::block + j0 * 128;
+                    const float* const e = reinterpret_cast<const float*>(sm8 + st * L::whole + L::errors) + (row >> 4) * (C * 16) + j0 * 16 + (row & 15);
+                    const uint8_t* const go = sm8 + st * L::whole + L::v + (row >> 6) * L::block + j0 * 128;
                     // scale e^c dO^T as terms, where X was
                     auto outer = [&](int c) {
                         uint32_t w[3][8];
@@ -336,7 +337,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                         ha::tmem_ready(x[c]);
                         weigh<false>(vec + I::late / 4 + 16 * c, x[c]);
 #pragma unroll
-                        for (int u = 0; u < 16; ++u) y[16 * c + u] = __uint_as_float(x[c][u]) * e[16 * c + u];
+                        for (int u = 0; u < 16; ++u) y[16 * c + u] = (v >> 4) < slices ? __uint_as_float(x[c][u]) * e[(16 * c + u) * 16] : 0.0f;
                     }
                     ok = ok && wait(kFactor, it);  // X and dO^T P have been read
 #pragma unroll
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                     for (int t = 0; t < 32; ++t) {
                         const float f = __uint_as_float(x[t >> 4][t & 15]);
                         if (ok && (v >> 4) < slices) p.errors_back[at + t * 16] = f;
-                        e[t] *= f;
+                        y[t] = (v >> 4) < slices ? f * e[t * 16] : 0.0f;
                     }
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                     ha::release_reads();
                     __syncwarp();
                     if (lane == 0 && ok) ha::bar_arrive(bars + 8 * (kEmpty + st));
-                    const float sum2 = sum_across(e);
+                    const float sum2 = sum_across(y);
                     if (ok && counts) dots[0] = sum2;
                 }
             }
@@ -413,7 +414,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
         if (count > 0) publish();
         for (int it = 0; it < count; ++it) {
             const int st = it % L::kStages, n = chunk_at(it), t0 = n * C;
-            const float* const vec = reinterpret_cast<const float*>(sm8 + st * L::stage + L::image);
+            const float* const vec = reinterpret_cast<const float*>(sm8 + st * L::whole + L::image);
             const long long chunk = (long long)bh * p.chunks + n;
             ok = ok && wait(kFull + st, it / L::kStages);
             if (kBack && it > 0) ok = ok && wait(kSolvedRead, it - 1);  // F of the chunk before

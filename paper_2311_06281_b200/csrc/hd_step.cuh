@@ -26,7 +26,7 @@ struct Step {
 
 // kBatch: rows that a thread has, at least ceil(dk / (kStepThreads / (kCols / kVec)))
 template <class T, int kCols, int kVec, int kBatch>
-__global__ void __launch_bounds__(kStepThreads) step_kernel(const Step p) {
+__global__ void __launch_bounds__(kStepThreads, kBatch * kVec <= 32 ? 4 : 2) step_kernel(const Step p) {
     constexpr int kLanes = kCols / kVec, kRows = kStepThreads / kLanes;
     __shared__ float ks[256], qs[256], es[kCols];
     __shared__ float part[2][kRows][kCols];

@@ -29,7 +29,7 @@ struct Space {
     size_t image, q, k, v, total;
 };
 template <int KP, int TI> Space space_of(const heinsen_attention_problem* p) {
-    constexpr int C = hd::chunk_tokens(KP), TM = TI == 1 ? HD_MID : 3, TP = TI;
+    constexpr int C = hd::chunk_tokens(KP), TM = 3, TP = TI;
     Space s;
     s.image = kHeaderBytes;
     s.q = s.image + image_bytes<C, TM, TP, false>(p);
@@ -41,7 +41,7 @@ template <int KP, int TI> Space space_of(const heinsen_attention_problem* p) {
 
 template <int KP, class T>
 hs_status forward(const heinsen_delta_problem* dp, const heinsen_attention_tensor* o, float* state, uint8_t* ws, cudaStream_t stream) {
-    constexpr int C = hd::chunk_tokens(KP), TI = sizeof(T) == 2 ? 1 : 3, TM = TI == 1 ? HD_MID : 3, TP = TI;
+    constexpr int C = hd::chunk_tokens(KP), TI = sizeof(T) == 2 ? 1 : 3, TM = 3, TP = TI;
     const heinsen_attention_problem* p = &dp->a;
     const Space sp = space_of<KP, TI>(p);
     int* const word = gave_up_word();
@@ -51,7 +51,7 @@ hs_status forward(const heinsen_delta_problem* dp, const heinsen_attention_tenso
     q.image = ws + sp.image;
     q.s_in = p->state0; q.s_out = state;
     q.out = const_cast<void*>(o->ptr); q.ob = o->batch_stride; q.ot = o->token_stride; q.oh = o->head_stride;
-    const bool many = fits_tcgen05<KP, TI>() && many_slices(p);
+    const bool many = fits_tcgen05<KP, TI>() && many_slices(p, false);
     CUtensorMap mq, mk, mv;
     hs_status st;
     if (p->tokens) {

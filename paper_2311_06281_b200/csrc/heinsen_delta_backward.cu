@@ -6,15 +6,13 @@ namespace {
 
 using namespace hd_host;
 
-constexpr int terms_of(int ti) { return ti == 1 ? HD_MID : 3; }
-
 // Workspace of a backward call: header | images of the chunks | q, k, v, dO as terms where TMA cannot load them | gradients of each
 // head where heads are shared, float32 | states before, their gradients after every chunk | E, F | sums over V | of decay gradients
 struct Space {
     size_t image, q, k, v, g, dq, dk, dv, states, gradients, errors, back, dots, part, total;
 };
 template <int KP, int TI> Space space_of(const heinsen_attention_problem* p) {
-    constexpr int C = hd::chunk_tokens(KP), TM = terms_of(TI);
+    constexpr int C = hd::chunk_tokens(KP), TM = 3;
     const size_t rows = (size_t)p->batch * p->tokens * p->heads, chunks = (size_t)chunks_of(p), slices = (p->v_dim + 15) / 16;
     Space s;
     s.image = kHeaderBytes;
@@ -45,7 +43,7 @@ hs_status shared_sum(const float* from, void* to, const heinsen_attention_proble
 
 template <int KP, int TI, class T>
 hs_status launch_back(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mg, const hd::Params& q, int* word, cudaStream_t stream) {
-    constexpr int C = hd::chunk_tokens(KP), TM = terms_of(TI);
+    constexpr int C = hd::chunk_tokens(KP), TM = 3;
     static std::atomic<unsigned long long> done{0};
     return launch_slices<hd::ScanLayout<KP, C, TI, TM, TM, true, true>>(hd::back_kernel<KP, C, TI, TM, T>, done, mq, mk, mg, q, word, stream);
 }
@@ -54,7 +52,7 @@ hs_status launch_back(const CUtensorMap& mq, const CUtensorMap& mk, const CUtens
 // hd_grad_mma.cuh), mma.sync for the rest, where all factors have three terms or the tiles of two CTAs would not fit.
 template <int KP, int TI, class T>
 hs_status launch_grad(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mg, const hd::Params& q, int* word, cudaStream_t stream) {
-    constexpr int C = hd::chunk_tokens(KP), TM = terms_of(TI);
+    constexpr int C = hd::chunk_tokens(KP), TM = 3;
     static std::atomic<unsigned long long> done{0};
     const unsigned grid = (unsigned)((long long)q.batch * q.heads * q.chunks);
     if constexpr (TI == 1 && KP <= 128) {
@@ -88,7 +86,7 @@ hs_status launch_grad(const CUtensorMap& mq, const CUtensorMap& mk, const CUtens
 template <int KP, class T>
 hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tensor* d_o, const float* d_state, void* dq, void* dk, void* dv, float* dlog_a,
                    float* dbeta, float* dstate0, uint8_t* ws, cudaStream_t stream) {
-    constexpr int C = hd::chunk_tokens(KP), TI = sizeof(T) == 2 ? 1 : 3, TM = terms_of(TI);
+    constexpr int C = hd::chunk_tokens(KP), TI = sizeof(T) == 2 ? 1 : 3, TM = 3;
     const heinsen_attention_problem* p = &dp->a;
     const Space sp = space_of<KP, TI>(p);
     int* const word = gave_up_word();
@@ -102,7 +100,7 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
     hs_status st;
     if ((st = map_of<T, TI>(&mq, p, view_of(p->q, p->heads, p->q_heads, p->k_dim), ws + sp.q, 64, C, stream)) != HS_OK) return st;
     if ((st = map_of<T, TI>(&mk, p, view_of(p->k, p->heads, p->k_heads, p->k_dim), ws + sp.k, 64, C, stream)) != HS_OK) return st;
-    const bool many = fits_tcgen05<KP, TI>() && many_slices(p);
+    const bool many = fits_tcgen05<KP, TI>() && many_slices(p, true);
     q.parts = many ? (p->v_dim + 31) / 32 : (p->v_dim + 15) / 16;
     if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, many ? 64 : 16, C, stream)) != HS_OK) return st;
     if ((st = map_of<T, TI>(&mg, p, view_of(*d_o, p->heads, p->heads, p->v_dim), ws + sp.g, 16, C, stream)) != HS_OK) return st;
