@@ -22,7 +22,7 @@ extern "C" {
  *
  * logits: float32 or bf16 [batch, beams, vocabulary], the last dimension contiguous, strides of the others in elements; scores
  * float32 [batch, beams] and ended (1 byte each, or NULL) contiguous.  Outputs, contiguous [batch, keep]: out_scores float32, out_parents
- * (the beam w) and out_tokens (n) int32.  1 <= beams <= 64, 1 <= keep <= 64, keep <= beams * vocabulary, vocabulary < 2^31;
+ * (the beam w) and out_tokens (n) int32.  1 <= beams <= 64, 1 <= keep <= 64, keep <= beams * vocabulary, vocabulary <= 2^31 - 2^20;
  * 0 <= end_token < vocabulary where ended is given.  Values are formed and compared in 64 bits; the exponentials of a sum are float32's
  * own, summed in 64 bits.  workspace: 256-byte aligned scratch of heinsen_beam_workspace_bytes.  Asynchronous on `stream`.
  */

@@ -27,9 +27,9 @@ struct Select {
     int *out_parents, *out_tokens;
 };
 
-// Numbers in the order of their size as unsigned ones
+// Numbers in the order of their size as unsigned ones; both zeros are one
 __device__ __forceinline__ uint32_t ordered(float x) {
-    const uint32_t u = __float_as_uint(x);
+    const uint32_t u = __float_as_uint(x + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
@@ -37,7 +37,7 @@ __device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_flo
 // One part of one row; kPer logits a thread, in vectors of 16 bytes at addresses of 16 bytes: part 0 begins at the last such address
 // at or before the row's first logit.
 template <class T, int kPer>
-__global__ void __launch_bounds__(kThreads) part_kernel(const Select p) {
+__global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(const Select p) {
     constexpr int kVec = 16 / sizeof(T), kVecs = kPer / kVec;
     __shared__ float red_max[kThreads / 32];
     __shared__ double red_sum[kThreads / 32];
@@ -52,34 +52,34 @@ __global__ void __launch_bounds__(kThreads) part_kernel(const Select p) {
     const long long row = blockIdx.x / p.parts, b = row / p.beams, w = row % p.beams;
     const T* const from = static_cast<const T*>(p.logits) + b * p.sb + w * p.sw;
     const int ahead = (int)((reinterpret_cast<uintptr_t>(from) & 15u) / sizeof(T));
-    const long long first = (long long)part * (kThreads * kPer) - ahead;
+    const int first = part * (kThreads * kPer) - ahead, vocabulary = (int)p.vocabulary;
     if (tid == 0) found = 0;
     if (p.ended && p.ended[row]) return;  // nothing of it is asked for
     float x[kPer];
-    auto token = [&](int i) { return first + ((long long)(i / kVec) * kThreads + tid) * kVec + i % kVec; };
+    auto token = [&](int i) { return first + (i / kVec * kThreads + tid) * kVec + i % kVec; };
+    if (first >= 0 && first + kThreads * kPer <= vocabulary) {  // all of it is there: no load waits for another's test
+        uint4 f[kVecs];
 #pragma unroll
-    for (int u = 0; u < kVecs; ++u) {
-        const long long n = token(u * kVec);
-        if (n >= 0 && n + kVec <= p.vocabulary) {
-            const uint4 f = __ldcs(reinterpret_cast<const uint4*>(from + n));
-            const uint32_t r[4] = {f.x, f.y, f.z, f.w};
+        for (int u = 0; u < kVecs; ++u) f[u] = __ldcs(reinterpret_cast<const uint4*>(from + token(u * kVec)));
+#pragma unroll
+        for (int u = 0; u < kVecs; ++u) {
+            const uint32_t r[4] = {f[u].x, f[u].y, f[u].z, f[u].w};
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
                 if constexpr (sizeof(T) == 2) x[u * kVec + i] = __uint_as_float(i & 1 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
                 else x[u * kVec + i] = __uint_as_float(r[i]);
             }
-        } else {
+        }
+    } else {
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) x[u * kVec + i] = n + i >= 0 && n + i < p.vocabulary ? ha::to_f(from[n + i]) : __int_as_float(0xff800000);
+        for (int i = 0; i < kPer; ++i) {
+            const int n = token(i);
+            x[i] = n >= 0 && n < vocabulary ? ha::to_f(from[n]) : __int_as_float(0xff800000);
         }
     }
     float top = x[0];
-    bool odd = x[0] != x[0];
 #pragma unroll
-    for (int i = 1; i < kPer; ++i) {
-        top = fmaxf(top, x[i]);
-        odd |= x[i] != x[i];
-    }
+    for (int i = 1; i < kPer; ++i) top = fmaxf(top, x[i]);
     // The keep-th largest of the maxima of disjoint groups (8 lanes each; single threads where more than 16 are asked for) bounds the
     // keep-th best of the part from below, and few logits lie above it.
     const bool few = p.keep <= 16;
@@ -94,24 +94,28 @@ __global__ void __launch_bounds__(kThreads) part_kernel(const Select p) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, red_max[i]);
-    float part_sum = 0.0f;  // (m - m is NaN for an infinite m)
+    float part_sum;  // NaN where a logit is (the maximum passes it over), and for an infinite maximum, of which m - m is NaN
+    {
+        const ha::pair minus = ha::make_pair2(-m, -m), base = ha::make_pair2(ha::kLog2e, ha::kLog2e);
+        ha::pair sums = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) part_sum += ha::ex2((x[i] - m) * ha::kLog2e);
+        for (int i = 0; i < kPer; i += 2) {
+            float a, b;
+            ha::parts(ha::mul2(ha::add2(ha::make_pair2(x[i], x[i + 1]), minus), base), a, b);
+            sums = ha::add2(sums, ha::make_pair2(ha::ex2(a), ha::ex2(b)));
+        }
+        float a, b;
+        ha::parts(sums, a, b);
+        part_sum = a + b;
+    }
     double sum = (double)part_sum;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
     if (lane == 0) red_sum[warp] = sum;
-    odd = __syncthreads_or(odd);
     const long long at = row * p.parts + part;
-    if (tid == 0) {
-        sum = 0.0;
-#pragma unroll
-        for (int i = 0; i < kThreads / 32; ++i) sum += red_sum[i];
-        p.part_sum[at] = make_double2((double)m, odd ? (double)__int_as_float(0x7fc00000) : m == __int_as_float(0xff800000) ? 0.0 : sum);
-    }
     float* const values = p.part_value + at * p.keep;
     int* const tokens = p.part_token + at * p.keep;
-    if (few) {
+    if (few && warp == 0) {
         const uint32_t own = tops[lane];
         int above = 0;
 #pragma unroll
@@ -119,8 +123,8 @@ __global__ void __launch_bounds__(kThreads) part_kernel(const Select p) {
             const uint32_t other = __shfl_sync(~0u, own, i);
             above += other > own || (other == own && i < lane);
         }
-        if (warp == 0 && above == p.keep - 1) least = own;
-    } else {
+        if (above == p.keep - 1) least = own;
+    } else if (!few) {
         const uint32_t own = tops[tid];
         int above = 0;
 #pragma unroll 8
@@ -132,18 +136,27 @@ __global__ void __launch_bounds__(kThreads) part_kernel(const Select p) {
         if (above == p.keep - 1) least = own;
     }
     __syncthreads();
-    const float bound = from_ordered(least);
+    if (tid == 0) {
+        sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const long long n = token(i);
-        if (x[i] >= bound && n >= 0 && n < p.vocabulary) {
-            const int to = atomicAdd(&found, 1);
-            if (to < kList) {
-                list_key[to] = ordered(x[i]);
-                list_token[to] = (int)n;
+        for (int i = 0; i < kThreads / 32; ++i) sum += red_sum[i];
+        p.part_sum[at] = make_double2((double)m, m == __int_as_float(0xff800000) ? 0.0 : sum);
+    }
+    // A bound of -inf (few logits that are not): of those at -inf the first `keep` places are enough.
+    const float bound = from_ordered(least), lowest = __int_as_float(0xff800000);
+    const int places = bound == lowest ? max(first, 0) + p.keep : vocabulary;
+    if (top >= bound)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int n = token(i);
+            if (x[i] >= bound && n >= 0 && n < (x[i] > lowest ? vocabulary : min(places, vocabulary))) {
+                const int to = atomicAdd(&found, 1);
+                if (to < kList) {
+                    list_key[to] = ordered(x[i]);
+                    list_token[to] = (int)n;
+                }
             }
         }
-    }
     __syncthreads();
     const int count = found;
     if (count <= kList) {  // sorted by value and place: the order in which they came does not matter
@@ -165,9 +178,9 @@ __global__ void __launch_bounds__(kThreads) part_kernel(const Select p) {
             unsigned long long mine = 0;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                const long long n = token(i);
+                const int n = token(i);
                 const unsigned long long key = (unsigned long long)ordered(x[i]) << 32 | (uint32_t)~(uint32_t)n;
-                if (n >= 0 && n < p.vocabulary && key < last && key > mine) mine = key;
+                if (n >= 0 && n < vocabulary && key < last && key > mine) mine = key;
             }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) {

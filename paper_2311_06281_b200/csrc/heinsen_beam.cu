@@ -12,9 +12,10 @@ using namespace ha_host;
 
 constexpr int kSms = 148;  // B200; sizes workspaces the same wherever they are asked for
 constexpr int kMaxBeams = 64;
+constexpr long long kMaxVocabulary = (1ll << 31) - (1ll << 20);  // places in a row are 32 bits, past the end of its last part too
 
 hs_status validate(const heinsen_beam_problem* p) {
-    if (!p || p->batch < 0 || p->vocabulary < 1 || p->vocabulary > 0x7fffffffll) return HS_ERR_INVALID_ARG;
+    if (!p || p->batch < 0 || p->vocabulary < 1 || p->vocabulary > kMaxVocabulary) return HS_ERR_INVALID_ARG;
     if (p->beams < 1 || p->beams > kMaxBeams || p->keep < 1 || p->keep > hb::kMaxKeep) return HS_ERR_INVALID_ARG;
     if (p->keep > p->beams * p->vocabulary) return HS_ERR_INVALID_ARG;
     if (p->dtype != HS_F32 && p->dtype != HS_BF16) return HS_ERR_INVALID_ARG;
