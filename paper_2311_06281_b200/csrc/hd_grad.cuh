@@ -33,6 +33,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
     const int bh = blockIdx.x / groups, b = bh / p.heads, h = bh % p.heads, slice0 = (blockIdx.x % groups) * own_slices;
     const int live = live_tokens(p.lengths, b, p.tokens), count = (live + C - 1) / C;
     if (tid == 0) {
+        if (blockIdx.x == 0) p.fault->started_id = p.call_id;  // (without a token no chunk has said so)
         for (int i = 0; i < kScanBars; ++i) ha::bar_init(bars + 8 * i, i >= kEmpty && i < kPatched ? 4 * own_slices : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *stop = 0;
@@ -533,7 +534,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         for (int r = 0; r < 2; ++r) {
             f[r] += __shfl_xor_sync(~0u, f[r], 1);
             f[r] += __shfl_xor_sync(~0u, f[r], 2);
-            if ((lane & 3) == 0) far[cb * C + i0 + 8 * r] = f[r];
+            if ((lane & 3) == 0) far[cb * C + i0 + 8 * r] = t0 + i0 + 8 * r < live ? f[r] : 0.0f;
         }
     }
 #pragma unroll

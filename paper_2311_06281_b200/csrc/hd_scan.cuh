@@ -689,6 +689,7 @@ __global__ void __launch_bounds__(kScanThreads, 1)
     const int bh = blockIdx.x / groups, b = bh / p.heads, h = bh % p.heads, slice0 = (blockIdx.x % groups) * own_slices;
     const int live = live_tokens(p.lengths, b, p.tokens), count = (live + C - 1) / C;
     if (tid == 0) {
+        if (blockIdx.x == 0) p.fault->started_id = p.call_id;  // (without a token no chunk has said so)
         for (int i = 0; i < kScanBars; ++i) ha::bar_init(bars + 8 * i, i >= kEmpty && i < kPatched ? 4 * own_slices : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *stop = 0;

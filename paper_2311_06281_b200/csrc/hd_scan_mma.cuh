@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
     const int slabs = (p.dv + 127) / 128, bh = blockIdx.x / slabs, b = bh / p.heads, h = bh % p.heads, v0 = (blockIdx.x % slabs) * 128;
     const int slices = (p.dv + 15) / 16, here = min(8, slices - v0 / 16), live = live_tokens(p.lengths, b, p.tokens), count = (live + C - 1) / C;
     if (tid == 0) {
+        if (blockIdx.x == 0) p.fault->started_id = p.call_id;
         for (int i = 0; i < kPassBars; ++i) {
             uint32_t arrivals = 1;
             if (i >= kEmpty && i < kPatched) arrivals = kMode == 1 ? 9 : 17;  // the warps that read vectors, and the products
