@@ -2,12 +2,14 @@
 
 Every layer is: block_norms (the residual sum with the layer before and the norm) -> projections -> decay_attention (whole
 sequences; in generation decay_attention_step, one token of every sequence with the states updated in place) -> gated_norm
-of every head -> output projection.  The projections are plain matrix products and PyTorch's; the rest is the library's.
+of every head -> output projection.  With ``delta`` the recurrence is that of ``heinsen_delta``: every token takes out of the state
+what it already answers for its key.  The projections are plain matrix products and PyTorch's; the rest is the library's.
 
-    python examples/decay_model.py [--steps 60] [--batch 16] [--tokens 256] [--dim 256] [--layers 2] [--heads 4]
+    python examples/decay_model.py [--steps 60] [--batch 16] [--tokens 256] [--dim 256] [--layers 2] [--heads 4] [--delta] [--beams 4]
 
 trains on sequences in which one symbol, another for each, stands between random ones and has to be named every time, then
-reads a prompt and continues it token by token.  Needs a GPU.
+reads a prompt and continues it token by token, the likeliest one each time or, with ``--beams``, by a search over so many
+continuations (``heinsen_beam``: the states of a beam become those of its parent).  Needs a GPU.
 """
 import argparse
 import json
@@ -20,10 +22,12 @@ import torch  # noqa: E402
 import torch.nn.functional as F  # noqa: E402
 
 from paper_2311_06281_b200 import heinsen_attention as ha  # noqa: E402
+from paper_2311_06281_b200 import heinsen_beam as hb  # noqa: E402
+from paper_2311_06281_b200 import heinsen_delta as hd  # noqa: E402
 
 
 class Layer(torch.nn.Module):
-    def __init__(self, dim: int, heads: int):
+    def __init__(self, dim: int, heads: int, delta: bool = False):
         super().__init__()
         self.heads, self.head_dim = heads, dim // heads
         self.norm = torch.nn.Parameter(torch.ones(dim))
@@ -32,6 +36,7 @@ class Layer(torch.nn.Module):
         self.decay_bias = torch.nn.Parameter(torch.linspace(-2.0, -7.0, heads))
         self.head_norm = torch.nn.Parameter(torch.ones(self.head_dim))
         self.out = torch.nn.Parameter(torch.randn(dim, dim) * dim ** -0.5)
+        self.write = torch.nn.Parameter(torch.randn(heads, dim) * dim ** -0.5) if delta else None  # how much of an error is written
 
     def forward(self, x, branch, state=None, step=False):
         """The residual stream and what the layer before adds to it, [B, T, dim] (step: [B, dim]); returns the stream, this
@@ -40,7 +45,13 @@ class Layer(torch.nn.Module):
         q, k, v, gate = F.linear(y, self.project.to(y.dtype)).unflatten(-1, (4, self.heads, self.head_dim)).unbind(-3)
         k = F.normalize(k.float(), dim=-1).to(y.dtype)
         log_a = -F.softplus(F.linear(y.float(), self.decay) + self.decay_bias)
-        if step:
+        if self.write is not None:
+            beta = torch.sigmoid(F.linear(y.float(), self.write))
+            if step:
+                o = hd.delta_attention_step(q, k, v, log_a, beta, state)
+            else:
+                o, state = hd.delta_attention(q, k, v, log_a, beta, state)
+        elif step:
             o = ha.decay_attention_step(q, k, v, log_a, state)
         else:
             o, state = ha.decay_attention(q, k, v, log_a, state)
@@ -49,11 +60,11 @@ class Layer(torch.nn.Module):
 
 
 class Model(torch.nn.Module):
-    def __init__(self, vocabulary: int, dim: int, layers: int, heads: int, dtype=torch.bfloat16):
+    def __init__(self, vocabulary: int, dim: int, layers: int, heads: int, dtype=torch.bfloat16, delta: bool = False):
         super().__init__()
         self.dtype = dtype
         self.embed = torch.nn.Parameter(torch.randn(vocabulary, dim) * dim ** -0.5)
-        self.layers = torch.nn.ModuleList(Layer(dim, heads) for _ in range(layers))
+        self.layers = torch.nn.ModuleList(Layer(dim, heads, delta) for _ in range(layers))
         self.norm = torch.nn.Parameter(torch.ones(dim))
 
     def forward(self, tokens, states=None):
@@ -105,16 +116,41 @@ def generate(model: Model, prompt: torch.Tensor, count: int) -> torch.Tensor:
     return torch.stack(tokens, dim=1)
 
 
+@torch.no_grad()
+def search(model: Model, prompt: torch.Tensor, count: int, beams: int):
+    """The `beams` likeliest continuations of `count` tokens that a beam search finds, best first, [B, beams, count], and their log
+    probabilities: the prompt in one pass, then for each token a selection, the states moved after their beams, and a step."""
+    batch = prompt.shape[0]
+    logits, states = model(prompt)
+    states = [s.repeat_interleave(beams, 0) for s in states]
+    logits = logits[:, -1:].expand(-1, beams, -1)
+    scores = torch.full((batch, beams), -float("inf"), device=prompt.device)
+    scores[:, 0] = 0.0  # one beam so far
+    made = torch.empty(batch, beams, 0, dtype=torch.long, device=prompt.device)
+    for i in range(count):
+        scores, parents, tokens = hb.beam_select(logits, scores)
+        made = torch.cat([made.gather(1, parents.long()[..., None].expand(-1, -1, i)), tokens.long()[..., None]], -1)
+        if i + 1 < count:
+            for s in states:
+                hb.beam_reorder(s, parents)
+            logits, states = model(tokens.long().flatten(), states)
+            logits = logits.unflatten(0, (batch, beams))
+    return made, scores
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, value in (("steps", 60), ("batch", 16), ("tokens", 256), ("dim", 256), ("layers", 2), ("heads", 4), ("vocabulary", 64)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--delta", action="store_true")
+    ap.add_argument("--beams", type=int, default=0)
     a = ap.parse_args()
     torch.manual_seed(0)
-    model = Model(a.vocabulary, a.dim, a.layers, a.heads).cuda()
+    model = Model(a.vocabulary, a.dim, a.layers, a.heads, delta=a.delta).cuda()
     losses = train(model, a.steps, a.batch, a.tokens)
     t = sequences(a.batch, a.tokens, a.vocabulary, "cuda", torch.Generator("cuda").manual_seed(1))
-    made = generate(model, t[:, :a.tokens // 2], a.tokens // 2)
+    prompt, count = t[:, :a.tokens // 2], a.tokens // 2
+    made = search(model, prompt, count, a.beams)[0][:, 0] if a.beams else generate(model, prompt, count)
     print(json.dumps({"first_loss": losses[0], "last_loss": losses[-1], "named": float((made == t[:, :1]).float().mean())}))
 
 
