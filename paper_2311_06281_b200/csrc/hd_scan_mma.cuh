@@ -38,6 +38,9 @@ __device__ __forceinline__ void mma_left(uint32_t d, uint32_t a, uint32_t b, uin
 // factors with the earlier: each is written when the products that read the other are done.
 struct PassColumns {
     static constexpr uint32_t s = 0, x = 192, y = 256, o = 320, f = 384, g = 480, columns = 512;
+    // What the solution adds to Y (dV'), by itself: the tensor core cuts off what it adds, and Y is the larger.  Where the state's last
+    // terms were, which X alone reads.
+    static constexpr uint32_t solved = s + 128;
     // term t of sixteen rows q of a thread's half of the state: its first two terms lie where its own half of the update will
     static __device__ __forceinline__ constexpr uint32_t state(int half, int q, int t) { return t < 2 ? s + half * 64 + q * 16 + t * 8 : s + 128 + half * 32 + q * 8; }
     static __device__ __forceinline__ constexpr uint32_t factor(int jj, int t) { return f + 24 * jj + 8 * t; }
@@ -215,13 +218,15 @@ __global__ void __launch_bounds__(kPassThreads, 1)
 #pragma unroll
                         for (int u = 0; u <= level; ++u)
 #pragma unroll
-                            for (int jj = 0; jj < 4; ++jj) {
+                            for (int n = 0; n < 4; ++n) {
+                                const int jj = kBack ? 3 - n : n;  // (the first covers all tokens)
+                                const bool more = level < 2 || u > 0 || n > 0;
                                 if constexpr (kBack)
-                                    mma_left<kRows32>(M::y, M::factor(jj, u), N + (((level - u) * I::plane + B::by_rows(jj, 0) * 512) >> 4),
-                                                      ha::mma_shape(16 * (jj + 1), ha::kColMajorB), true);
+                                    mma_left<kRows32>(M::solved, M::factor(jj, u), N + (((level - u) * I::plane + B::by_rows(jj, 0) * 512) >> 4),
+                                                      ha::mma_shape(16 * (jj + 1), ha::kColMajorB), more);
                                 else
-                                    mma_left<kRows32>(M::y + 16 * jj, M::factor(jj, u), N + (((level - u) * I::plane + B::by_columns(jj, jj) * 512) >> 4),
-                                                      ha::mma_shape(C - 16 * jj, 0), true);
+                                    mma_left<kRows32>(M::solved + 16 * jj, M::factor(jj, u), N + (((level - u) * I::plane + B::by_columns(jj, jj) * 512) >> 4),
+                                                      ha::mma_shape(C - 16 * jj, 0), more);
                             }
                     ha::mma_commit(bars + 8 * kSolved);
                     if constexpr (kOutput) {  // while the threads work on E
@@ -350,7 +355,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                     const float beta = vec[I::beta / 4 + lane];
                     const float sum = beta * sum_across(y);
                     if (ok && counts) dots[p.parts * C] = sum;
-                    ok = ok && wait(kSolved, it);
+                    ok = ok && wait(kWrites, it);  // F is there
                     ha::tmem_after_sync();
 #pragma unroll
                     for (int c = 0; c < 2; ++c) ha::tmem_ld16_early(x[c], lanes + M::y + j0 + 16 * c);
@@ -466,13 +471,20 @@ __global__ void __launch_bounds__(kPassThreads, 1)
             ok = ok && wait(kSolved, it);
             ha::tmem_after_sync();
             {
-                uint32_t x[2][16];
+                uint32_t x[2][16], z[2][16];
 #pragma unroll
-                for (int g = 0; g < 2; ++g) ha::tmem_ld16_early(x[g], lanes + M::y + 32 * half + 16 * g);
+                for (int g = 0; g < 2; ++g) {
+                    ha::tmem_ld16_early(x[g], lanes + M::y + 32 * half + 16 * g);
+                    ha::tmem_ld16_early(z[g], lanes + M::solved + 32 * half + 16 * g);
+                }
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     const int jj = 2 * half + g, j = 16 * jj;
                     ha::tmem_ready(x[g]);
+                    ha::tmem_ready(z[g]);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[g][e] = __float_as_uint(__uint_as_float(x[g][e]) + __uint_as_float(z[g][e]));
+                    if constexpr (kBack) ha::tmem_st16(lanes + M::y + j, x[g]);  // F, for the warps beside
                     if constexpr (kMode == 1) {
                         if (ok && (v >> 4) < slices) {
                             float* const to = p.errors + ((chunk * slices + (v >> 4)) * C + j) * 16 + (v & 15);
