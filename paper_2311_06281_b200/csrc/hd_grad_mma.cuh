@@ -322,16 +322,10 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                     } else {
                         const int last = on ? (key ? i - 1 : i) - col : -1;
 #pragma unroll
-                        for (int e = 0; e < 16; e += 4) {
-                            const float4 h4 = *reinterpret_cast<const float4*>(vec + I::hi / 4 + col + e), l4 = *reinterpret_cast<const float4*>(vec + I::lo / 4 + col + e);
-                            const float d[4] = {(hi - h4.x) + (lo - l4.x), (hi - h4.y) + (lo - l4.y), (hi - h4.z) + (lo - l4.z), (hi - h4.w) + (lo - l4.w)};
+                        for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(g[e]);
+                        between_tokens(x, vec + I::hi / 4 + col, vec + I::lo / 4 + col, hi, lo, key ? -1.0f : p.scale, last);
 #pragma unroll
-                            for (int u = 0; u < 4; ++u) {
-                                const float w = e + u <= last ? ex2(d[u]) : 0.0f;
-                                x[e + u] = w != 0.0f ? (key ? -w : p.scale * w) * __uint_as_float(g[e + u]) : 0.0f;
-                                own_w[e + u] = col + e + u < i && w != 0.0f ? x[e + u] * __uint_as_float(r[e + u]) : 0.0f;
-                            }
-                        }
+                        for (int e = 0; e < 16; ++e) own_w[e] = e <= last && col + e < i ? x[e] * __uint_as_float(r[e]) : 0.0f;
                     }
                 }
                 __syncwarp();

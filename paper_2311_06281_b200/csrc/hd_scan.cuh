@@ -98,6 +98,25 @@ template <int C, int kTermsN, int kTermsP, bool kBack> struct Image {
     static __device__ __forceinline__ int p_block(int i, int j) { return kBack ? Blocks<C>::by_rows(i, j) : Blocks<C>::by_columns(i, j); }
 };
 
+// x[e] = factor e^{c_i-c_j} x[e] for sixteen tokens j up to the last one that counts, zero behind it (whatever x holds there)
+__device__ __forceinline__ void between_tokens(float (&x)[16], const float* hi, const float* lo, float own_hi, float own_lo, float factor, int last) {
+    const ha::pair minus = ha::make_pair2(-1.0f, -1.0f), h = ha::make_pair2(own_hi, own_hi), l = ha::make_pair2(own_lo, own_lo), f = ha::make_pair2(factor, factor);
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        const float4 h4 = *reinterpret_cast<const float4*>(hi + e), l4 = *reinterpret_cast<const float4*>(lo + e);
+#pragma unroll
+        for (int u = 0; u < 4; u += 2) {
+            float d0, d1;
+            ha::parts(ha::add2(ha::fma2(u ? ha::make_pair2(h4.z, h4.w) : ha::make_pair2(h4.x, h4.y), minus, h),
+                               ha::fma2(u ? ha::make_pair2(l4.z, l4.w) : ha::make_pair2(l4.x, l4.y), minus, l)), d0, d1);
+            d0 = e + u <= last ? ex2(d0) : 0.0f;
+            d1 = e + u + 1 <= last ? ex2(d1) : 0.0f;
+            const ha::pair y = ha::make_pair2(e + u <= last ? x[e + u] : 0.0f, e + u + 1 <= last ? x[e + u + 1] : 0.0f);
+            ha::parts(ha::mul2(ha::mul2(f, ha::make_pair2(d0, d1)), y), x[e + u], x[e + u + 1]);
+        }
+    }
+}
+
 template <int KP, int C, int TI, int TM, int TP, bool kBack>
 struct ChunkLayout {
     using I = Image<C, TM, TP, kBack>;
@@ -116,7 +135,7 @@ struct ChunkLayout {
 //     N_iw = (I + M_ii beta_i)^{-1} (M_iw - sum_{w<=s<i} M_is beta_s N_sw),
 // every N^T_sw the next product's factor in its registers.  24 bits in all of it: a wrong N is wrong for every column of V.
 template <int KP, int C, int TI, int TM, int TP, bool kBack>
-__global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const Params p,
+__global__ void __launch_bounds__(2 * C, C == 64 && TI == 1 ? 5 : 1) chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const Params p,
                                                       int* gave_up) {
     using L = ChunkLayout<KP, C, TI, TM, TP, kBack>;
     using I = Image<C, TM, TP, kBack>;
@@ -241,31 +260,24 @@ __global__ void __launch_bounds__(2 * C) chunk_kernel(const __grid_constant__ CU
                 // Sixteen columns before all rows of the warp: e^{c_i-c_j} = e^{c_i-c_m} e^{c_m-c_j} with m the last of them; both exponents
                 // keep their sign, and one exponential of the row serves them all.
                 const int m = 16 * jb + 15;
-                float f = t0 + i < live ? ex2((own_hi - vec[I::hi / 4 + m]) + (own_lo - vec[I::lo / 4 + m])) : 0.0f;
+                const bool on = t0 + i < live;
+                float f = on ? ex2((own_hi - vec[I::hi / 4 + m]) + (own_lo - vec[I::lo / 4 + m])) : 0.0f;
                 if (mine_p) f *= p.scale;
+                const ha::pair f2 = ha::make_pair2(f, f);
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
                     const float4 g = *reinterpret_cast<const float4*>(vec + I::edge / 4 + 16 * jb + e);
-                    x[e] = f == 0.0f ? 0.0f : f * g.x * x[e];
-                    x[e + 1] = f == 0.0f ? 0.0f : f * g.y * x[e + 1];
-                    x[e + 2] = f == 0.0f ? 0.0f : f * g.z * x[e + 2];
-                    x[e + 3] = f == 0.0f ? 0.0f : f * g.w * x[e + 3];
+#pragma unroll
+                    for (int u = 0; u < 4; u += 2)
+                        ha::parts(ha::mul2(ha::mul2(f2, u ? ha::make_pair2(g.z, g.w) : ha::make_pair2(g.x, g.y)),
+                                           ha::make_pair2(on ? x[e + u] : 0.0f, on ? x[e + u + 1] : 0.0f)), x[e + u], x[e + u + 1]);
                 }
             } else {
                 const int last = t0 + i < live ? (mine_p ? i : i - 1) - 16 * jb : -1;  // the last column that counts
+                between_tokens(x, vec + I::hi / 4 + 16 * jb, vec + I::lo / 4 + 16 * jb, own_hi, own_lo, mine_p ? p.scale : 1.0f, last);
+                if (!mine_p && jb == ib)  // transposed: the inverse reads columns
 #pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    const float4 hi = *reinterpret_cast<const float4*>(vec + I::hi / 4 + 16 * jb + e), lo = *reinterpret_cast<const float4*>(vec + I::lo / 4 + 16 * jb + e);
-                    const float d[4] = {(own_hi - hi.x) + (own_lo - lo.x), (own_hi - hi.y) + (own_lo - lo.y), (own_hi - hi.z) + (own_lo - lo.z), (own_hi - hi.w) + (own_lo - lo.w)};
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const float w = e + u <= last ? ex2(d[u]) : 0.0f;
-                        x[e + u] = w != 0.0f ? (mine_p ? p.scale * w : w) * x[e + u] : 0.0f;
-                    }
-                    if (!mine_p && jb == ib)  // transposed: the inverse reads columns
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) diag[(e + u) * 16] = x[e + u];
-                }
+                    for (int e = 0; e < 16; ++e) diag[e * 16] = x[e];
             }
             auto put = [&](auto terms, uint8_t* to, int block) {
                 constexpr int kTerms = decltype(terms)::value;
