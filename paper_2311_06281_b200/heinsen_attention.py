@@ -130,14 +130,18 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
+# The current stream's handle without an object around it: two microseconds of every call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _launch(device, fn, *args):
     """Calls fn(*args, stream) on `device` and its current stream."""
     index = device.index
     if index == torch.cuda.current_device():
-        status = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        status = fn(*args, _raw_stream(index))
     else:
         with _on_device(device):
-            status = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+            status = fn(*args, _raw_stream(index))
     if status:
         _check(status)
 
