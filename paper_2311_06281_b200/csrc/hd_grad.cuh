@@ -14,6 +14,8 @@
 
 namespace hd {
 
+// Bound as scan_kernel is, by a chunk's chain: 3.4 us for a chunk and two slices (keys 128 wide); 24 pairs of nine chunks, keys 96 and
+// values 64 wide: 26 us.
 template <int KP, int C, int TI, int TM, class T>
 __global__ void __launch_bounds__(kScanThreads, 1)
     back_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mg, const Params p,

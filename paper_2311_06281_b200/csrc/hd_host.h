@@ -143,8 +143,8 @@ template <int KP, int TI> constexpr bool fits_tcgen05() { return TI == 1 && KP <
 // Which of the two: a CTA with four warps for each of one or two slices of sixteen columns of V (mma.sync), or one with 128 columns
 // (tcgen05).  Measured for a chunk, keys and values 128 wide, with one CTA to an SM: one slice 2.3 us, two 3.4 us, 128 columns 5.1 us
 // forward; for the gradients (both passes) two slices 6.4 us, 128 columns 12.9 us.  So two slices as long as their waves over the SMs
-// are at most 3/2 (2) of the other's: 16 (batch, head) pairs of 16385 tokens are 590 us against 1180, 64 pairs of 2048 218 us against
-// 162, 128 pairs with their gradients 820 us against 414.
+// are at most 3/2 (2) of the other's: 8 (batch, head) pairs of 16385 tokens are 590 us against 1180, 64 pairs of 2048 218 us against
+// 162, 128 pairs with their gradients 820 us against 426.
 inline bool many_slices(const heinsen_attention_problem* p, bool backward) {
     const long long pairs = p->batch * p->heads, slices = (p->v_dim + 15) / 16, two = (pairs * ((slices + 1) / 2) + kSms - 1) / kSms,
                     all = (pairs * ((p->v_dim + 127) / 128) + kSms - 1) / kSms;

@@ -16,7 +16,11 @@
 // few sequences and heads.  A slice of sixteen columns of V has four warps, one on each scheduler of an SM; each has a quarter of the
 // state's rows for it, transposed, as accumulators, and a quarter of a chunk's tokens.  Products over the state's rows are added up
 // between the four (one barrier), and each hands the others its tokens' Y and V' as factors (two more), so that the state never leaves
-// its registers.  Measured against one warp for a slice: see the notes at the launch.
+// its registers.  Against one warp for a slice with all of the state: 16385 tokens, 8 heads of 128, 1.23 ms -> 0.64 ms.
+//
+// What bounds it: chunks follow each other, and in a chunk the sums, the solution and the update.  A chunk takes a slice 2.3 us (keys
+// 128 wide; four barriers, 120 to 250 products of a warp one behind the other's operands), with the tensor pipe busy 41% of the time
+// and two slices on an SM.
 #pragma once
 #include <cuda.h>
 
@@ -49,11 +53,11 @@ struct Params {
     uint8_t* image;        // what chunk_kernel leaves for each (batch, head) and chunk
     const float* s_in;     // [batch, heads, dk, dv] or NULL
     float* s_out;          // or NULL
-    void* out;             // o (backward: dv) through its strides, where TMA does not store it
+    void* out;             // o (backward: dv) through its strides
     long long ob, ot, oh;
     float* states;         // backward: before every chunk the state (after it, its gradient), [batch * heads][chunks][16 slices][KP]
     float* errors;         // E (F) of every chunk, [batch * heads][chunks][16 slices][C]
-    float* errors_back;    // F likewise (layouts of the tensor-core passes: hd_scan_mma.cuh)
+    float* errors_back;    // F likewise (both as slabs where grad_mma_kernel reads them: dump_state, dump_errors)
     int parts;             // of the sums over V in `dots`
     float* gradients;      // the gradient of the state after every chunk, as `states`
     float* dots;           // [batch * heads][chunks][2][parts][C]: by part of V, dbeta and e^{c_C-c_j} k_j^T D V'_j
@@ -134,6 +138,10 @@ struct ChunkLayout {
 // inverts a diagonal block of I + M beta, and solves for 16 columns of N, transposed, block by block of rows,
 //     N_iw = (I + M_ii beta_i)^{-1} (M_iw - sum_{w<=s<i} M_is beta_s N_sw),
 // every N^T_sw the next product's factor in its registers.  24 bits in all of it: a wrong N is wrong for every column of V.
+// Bound by the instructions around the products (issue slots 47%, tensor pipe 21%): the weights between tokens, two to an instruction
+// and with one exponential for a row of a block where the block lies before all of the warp's rows, the splitting into terms and the
+// solution's chain.  2048 chunks of 64 tokens, keys 128 wide: 39 us (64 MB of images written), with five CTAs to an SM for four 45 us,
+// with the weights one by one 54 us.
 template <int KP, int C, int TI, int TM, int TP, bool kBack>
 __global__ void __launch_bounds__(2 * C, C == 64 && TI == 1 ? 5 : 1) chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const Params p,
                                                       int* gave_up) {
@@ -493,9 +501,6 @@ __device__ __forceinline__ void get_factor(uint32_t (&a)[kTerms][4], const uint8
         a[u][0] = f.x; a[u][1] = f.y; a[u][2] = f.z; a[u][3] = f.w;
     }
 }
-// d += factor * block: sixteen tokens by sixteen, small terms first, added once
-template <int kLevel, int kA, int kB>
-__device__ __forceinline__ void add_block(float (&d)[2][4], const uint32_t (&a)[kA][4], const uint32_t (&b)[1][kB][4]) { rounded_products<kLevel>(d, a, b); }
 
 enum ScanBar : int { kFull = 0, kEmpty = 2, kPatched = 4, kScanBars = 5 };
 
@@ -682,7 +687,8 @@ __device__ __forceinline__ void quarter_scores(float (*y)[4], const uint32_t (&a
         }
 }
 
-// kOut: the output; else the state before every chunk and E, for the gradients.  TO: terms of S and V' in the output.
+// kOut: the output; else the state before every chunk and E, for the gradients.  TO: terms of S and V' in the output.  Of bf16 tensors
+// the state has three terms where a later state hangs on it and two (16 bits) where it meets a query: the output is rounded to 8.
 template <int KP, int C, int TI, int TM, int TP, bool kOut, class T>
 __global__ void __launch_bounds__(kScanThreads, 1)
     scan_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p,
