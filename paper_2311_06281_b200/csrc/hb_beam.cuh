@@ -35,7 +35,8 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 __device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
 
 // Bound by HBM and by the instructions for a logit (an exponential and a test): 256 rows of 100003 float32 logits, a fifth of them of
-// ended beams, 28 us for 82 MB; 8 logits a thread where there are few rows (4 rows of 32000 bf16: 3.6 us).
+// ended beams, 28 us for 82 MB; 8 logits a thread where there are few rows (4 rows of 32000 bf16: 3.3 us).
+// Parts of many tiles of 16 logits a thread, the next one's loads ahead, gave the part 31 to 38 us and the join 7.3: no gain.
 // One part of one row; kPer logits a thread, in vectors of 16 bytes at addresses of 16 bytes: part 0 begins at the last such address
 // at or before the row's first logit.
 template <class T, int kPer>
@@ -206,7 +207,8 @@ __global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(cons
 
 // The best of a group.  Candidates are formed in 64 bits; as above, the keep-th best of the threads' own best bounds the keep-th best
 // of all, and those above it are sorted.
-// Bound by latency, a CTA for a group: 8 beams of 13 parts with 8 candidates each 11 us, 4 beams of 16 parts with 4 each 7 us.
+// Bound by latency, a CTA for a group: 8 beams of 13 parts with 8 candidates each 8.6 us (11 us with one load of a lane at a time),
+// 4 beams of 16 parts with 4 each 7 us.
 constexpr int kJoinList = 512;
 __global__ void __launch_bounds__(kThreads) join_kernel(const Select p) {
     __shared__ double logs[64];
@@ -252,9 +254,18 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Select p) {
             if (how == 0) {
                 const double base = logs[w];
                 const long long at = (b * p.beams + w) * lists;
-                for (int i = lane; i < lists; i += 32) {
-                    const int n = p.part_token[at + i];
-                    if (n >= 0) take(base + (double)p.part_value[at + i], row0 + n);
+                for (int i = lane; i < lists; i += 128) {  // four of a lane's loads together
+                    int n[4];
+                    float v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const bool on = i + 32 * u < lists;
+                        n[u] = on ? p.part_token[at + i + 32 * u] : -1;
+                        v[u] = on ? p.part_value[at + i + 32 * u] : 0.0f;  // (that of no token is never used)
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (n[u] >= 0) take(base + (double)v[u], row0 + n[u]);
                 }
             } else {
                 for (int i = lane; i <= p.keep && i < p.vocabulary; i += 32)

@@ -24,8 +24,10 @@ hs_status validate(const heinsen_beam_problem* p) {
     return HS_OK;
 }
 
-// Logits of a thread: 32 of them (8192 a CTA), or 8 where there would be fewer CTAs than two for each SM.
-int per_thread(const heinsen_beam_problem* p) { return p->batch * p->beams * ((p->vocabulary + 8191) / 8192) >= 2 * kSms ? 32 : 8; }
+// Logits of a thread: 32 of them (8192 a CTA), or 8 where that would leave an SM in two without a CTA.  Both kernels together, with 8
+// and with 32 (bf16, keep 4 to 8): 16 CTAs of 8192 logits 10.1 us, 11.5 us; 64 of them 11.3, 12.4; 128 of them 13.3, 12.6; 256 of them
+// 16.5, 13.6; 1024 of them 27.6, 20.0.
+int per_thread(const heinsen_beam_problem* p) { return p->batch * p->beams * ((p->vocabulary + 8191) / 8192) > kSms / 2 ? 32 : 8; }
 long long parts_of(const heinsen_beam_problem* p) {
     const long long each = hb::kThreads * per_thread(p), ahead = 16 / (p->dtype == HS_F32 ? 4 : 2) - 1;  // the row may begin behind an address of 16 bytes
     return (p->vocabulary + ahead + each - 1) / each;

@@ -86,6 +86,40 @@ def test_ended_missing_and_broken_beams(hb, n, keep):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("b,w,n,keep", [(6, 64, 90001, 64), (6, 64, 90001, 3), (37, 8, 40007, 17)])
+def test_rows_that_a_thread_block_reads_in_many_steps(hb, b, w, n, keep, dtype):
+    """Rows of all kinds in one call: far larger logits late (or early), rising and falling ones, equal ones, a masked beginning,
+    a masked end, single logits that are not masked, an infinity and a NaN late in the row."""
+    logits, scores = make(b, w, n, dtype, seed=n + keep)
+    ramp = torch.linspace(-40, 40, n, device=DEV)
+    for g in range(b):  # one kind for each group, so that its best come from every row of it
+        x = logits[g].float()
+        kind = g % 9
+        if kind == 0:
+            x[:, n // 2:] += 500
+        elif kind == 1:
+            x[:, n // 2:] -= 500
+        elif kind == 2:
+            x = ramp.expand(w, n)
+        elif kind == 3:
+            x = (-ramp).expand(w, n)
+        elif kind == 4:
+            x = torch.ones_like(x)
+        elif kind == 5:
+            x[:, :n - 5000] = -INF
+        elif kind == 6:
+            x[:, 5000:] = -INF
+        elif kind == 7:
+            x = torch.full_like(x, -INF)
+            x[:, 31000:31003] = 2.0
+        else:
+            x[0, n - 9] = INF
+            x[1, n - 9] = float("nan")
+        logits[g] = x.to(dtype)
+    compare(hb, logits, scores, keep)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_strides_of_logits(hb, dtype):
     g = torch.Generator(device=DEV).manual_seed(1)
     big = torch.randn(4, 7, 3011, device=DEV, generator=g).to(dtype)
