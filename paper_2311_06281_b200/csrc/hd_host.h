@@ -55,24 +55,29 @@ inline size_t terms_bytes(const heinsen_attention_problem* p, const View& v) {
     if (p->tokens == 0 || (p->dtype == HS_BF16 && tma_strides(v, p->batch, p->tokens))) return 0;
     return up256((size_t)(p->dtype == HS_F32 ? 3 : 1) * p->batch * p->tokens * v.own_heads * ((v.dim + 7) / 8 * 8) * 2);
 }
-// The tensor map of a tensor, through `space` where it has to be laid out anew.
+// The tensor map of a tensor; where it has to be laid out anew, that of the place in `space` which `all` then says it goes to.
 template <class T, int TI>
-hs_status map_of(CUtensorMap* m, const heinsen_attention_problem* p, const View& v, uint8_t* space, int columns, int rows, cudaStream_t stream) {
+hs_status map_of(CUtensorMap* m, const heinsen_attention_problem* p, const View& v, uint8_t* space, int columns, int rows, hd::Terms* all) {
     View w = v;
     if (terms_bytes(p, v)) {
         const int width = (v.dim + 7) / 8 * 8;
-        const long long pieces = p->batch * p->tokens * v.own_heads * (width / 8);
-        const bool whole = TI == 3 && v.dim % 8 == 0 && (v.rows.sb | v.rows.st | v.rows.sh) % 4 == 0 && (reinterpret_cast<uintptr_t>(v.rows.ptr) & 15u) == 0;
-        const auto fn = whole ? hd::terms_kernel<TI, T, true> : hd::terms_kernel<TI, T, false>;
-        fn<<<(unsigned)std::min<long long>((pieces + 255) / 256, kSms * 16), 256, 0, stream>>>(
-            v.rows, reinterpret_cast<__nv_bfloat16*>(space), (uint32_t)p->tokens, (uint32_t)v.own_heads, v.dim, width, pieces);
-        const hs_status st = launched("terms_kernel");
-        if (st != HS_OK) return st;
         const long long sh = width, stk = sh * v.own_heads;
+        const bool whole = v.dim % 8 == 0 && (v.rows.sb | v.rows.st | v.rows.sh) % 4 == 0 && (reinterpret_cast<uintptr_t>(v.rows.ptr) & 15u) == 0;
+        all->tokens = (uint32_t)p->tokens;
+        all->tensors[all->count++] = {v.rows, reinterpret_cast<__nv_bfloat16*>(space), p->batch * p->tokens * v.own_heads * (width / 8), (uint32_t)v.own_heads,
+                                      v.dim, width, whole};
         w = {{space, stk * p->tokens, stk, sh, 1}, v.own_heads, width};
     }
     if (!encode(m, w, p->batch * TI, p->tokens, columns, rows)) return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
     return HS_OK;
+}
+template <class T, int TI> hs_status launch_terms(const hd::Terms& all, cudaStream_t stream) {
+    if (!all.count) return HS_OK;
+    long long most = 0;
+    for (int i = 0; i < all.count; ++i) most = std::max(most, all.tensors[i].pieces);
+    const dim3 grid((unsigned)std::min<long long>((most + 255) / 256, kSms * 16), all.count);
+    hd::terms_kernel<TI, T><<<grid, 256, 0, stream>>>(all);
+    return launched("terms_kernel");
 }
 
 inline hd::Params params_of(const heinsen_delta_problem* dp, int chunk, uint8_t* ws) {

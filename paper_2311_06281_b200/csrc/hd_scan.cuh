@@ -882,29 +882,42 @@ __global__ void __launch_bounds__(kScanThreads, 1)
 
 // ------------------------------------------------------------------------------------------------- tensors for TMA
 
-// A [batch, tokens, heads, dim] tensor that TMA cannot load as it is (float32, odd sizes or strides) as bf16 terms,
-// [term][batch][tokens][heads][width], columns from dim on zero.  A thread has eight columns of a row; kWhole: they are there, at
-// addresses of 16 bytes.
-template <int TI, class T, bool kWhole>
-__global__ void __launch_bounds__(256) terms_kernel(const ha::Rows from, __nv_bfloat16* to, uint32_t tokens, uint32_t heads, int dim, int width, long long pieces) {
-    for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < pieces; e += (long long)gridDim.x * blockDim.x) {
-        const uint32_t along = width / 8;
-        const long long row = e / along, bt = row / heads;
+// [batch, tokens, heads, dim] tensors that TMA cannot load as they are (float32, odd sizes or strides) as bf16 terms,
+// [term][batch][tokens][heads][width], columns from dim on zero: all of a call's in one launch, a row of the grid each.  A thread has
+// eight columns of a row; `whole`: they are there, at addresses of 16 bytes.
+struct Terms {
+    static constexpr int kMost = 4;
+    struct Tensor {
+        ha::Rows from;
+        __nv_bfloat16* to;
+        long long pieces;
+        uint32_t heads;
+        int dim, width, whole;
+    } tensors[kMost];
+    uint32_t tokens;
+    int count;
+};
+template <int TI, class T>
+__global__ void __launch_bounds__(256) terms_kernel(const Terms p) {
+    const Terms::Tensor& x = p.tensors[blockIdx.y];
+    for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < x.pieces; e += (long long)gridDim.x * blockDim.x) {
+        const uint32_t along = x.width / 8;
+        const long long row = e / along, bt = row / x.heads;
         const int d = 8 * (int)(e - row * along);
-        const T* const at = static_cast<const T*>(from.ptr) + bt / tokens * from.sb + bt % tokens * from.st + row % heads * from.sh + d;
-        float x[8];
-        if constexpr (kWhole && sizeof(T) == 4) {
+        const T* const at = static_cast<const T*>(x.from.ptr) + bt / p.tokens * x.from.sb + bt % p.tokens * x.from.st + row % x.heads * x.from.sh + d;
+        float f[8];
+        if (sizeof(T) == 4 && x.whole) {
             const float4 a = reinterpret_cast<const float4*>(at)[0], b = reinterpret_cast<const float4*>(at)[1];
-            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+            f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = d + i < dim ? ha::to_f(at[i]) : 0.0f;
+            for (int i = 0; i < 8; ++i) f[i] = d + i < x.dim ? ha::to_f(at[i]) : 0.0f;
         }
         uint32_t t[4][TI];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ha::split<TI>(ha::make_pair2(x[2 * i], x[2 * i + 1]), t[i]);
+        for (int i = 0; i < 4; ++i) ha::split<TI>(ha::make_pair2(f[2 * i], f[2 * i + 1]), t[i]);
 #pragma unroll
-        for (int u = 0; u < TI; ++u) reinterpret_cast<uint4*>(to)[u * pieces + e] = make_uint4(t[0][u], t[1][u], t[2][u], t[3][u]);
+        for (int u = 0; u < TI; ++u) reinterpret_cast<uint4*>(x.to)[u * x.pieces + e] = make_uint4(t[0][u], t[1][u], t[2][u], t[3][u]);
     }
 }
 

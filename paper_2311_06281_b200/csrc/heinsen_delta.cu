@@ -54,10 +54,12 @@ hs_status forward(const heinsen_delta_problem* dp, const heinsen_attention_tenso
     const bool many = fits_tcgen05<KP, TI>() && many_slices(p, false);
     CUtensorMap mq, mk, mv;
     hs_status st;
+    hd::Terms terms{};
     if (p->tokens) {
-        if ((st = map_of<T, TI>(&mq, p, view_of(p->q, p->heads, p->q_heads, p->k_dim), ws + sp.q, 64, C, stream)) != HS_OK) return st;
-        if ((st = map_of<T, TI>(&mk, p, view_of(p->k, p->heads, p->k_heads, p->k_dim), ws + sp.k, 64, C, stream)) != HS_OK) return st;
-        if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, many ? 64 : 16, C, stream)) != HS_OK) return st;
+        if ((st = map_of<T, TI>(&mq, p, view_of(p->q, p->heads, p->q_heads, p->k_dim), ws + sp.q, 64, C, &terms)) != HS_OK) return st;
+        if ((st = map_of<T, TI>(&mk, p, view_of(p->k, p->heads, p->k_heads, p->k_dim), ws + sp.k, 64, C, &terms)) != HS_OK) return st;
+        if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, many ? 64 : 16, C, &terms)) != HS_OK) return st;
+        if ((st = launch_terms<T, TI>(terms, stream)) != HS_OK) return st;
         if ((st = launch_chunks<KP, C, TI, TM, TP, false>(mq, mk, q, word, stream)) != HS_OK) return st;
     } else {
         std::memset(&mq, 0, sizeof mq);

@@ -98,12 +98,13 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
     q.states = at(sp.states); q.gradients = at(sp.gradients); q.errors = at(sp.errors); q.errors_back = at(sp.back); q.dots = at(sp.dots);
     CUtensorMap mq, mk, mv, mg;
     hs_status st;
-    if ((st = map_of<T, TI>(&mq, p, view_of(p->q, p->heads, p->q_heads, p->k_dim), ws + sp.q, 64, C, stream)) != HS_OK) return st;
-    if ((st = map_of<T, TI>(&mk, p, view_of(p->k, p->heads, p->k_heads, p->k_dim), ws + sp.k, 64, C, stream)) != HS_OK) return st;
+    hd::Terms terms{};
+    if ((st = map_of<T, TI>(&mq, p, view_of(p->q, p->heads, p->q_heads, p->k_dim), ws + sp.q, 64, C, &terms)) != HS_OK) return st;
+    if ((st = map_of<T, TI>(&mk, p, view_of(p->k, p->heads, p->k_heads, p->k_dim), ws + sp.k, 64, C, &terms)) != HS_OK) return st;
     const bool many = fits_tcgen05<KP, TI>() && many_slices(p, true);
     q.parts = many ? (p->v_dim + 31) / 32 : (p->v_dim + 15) / 16;
-    if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, many ? 64 : 16, C, stream)) != HS_OK) return st;
-    if ((st = map_of<T, TI>(&mg, p, view_of(*d_o, p->heads, p->heads, p->v_dim), ws + sp.g, 16, C, stream)) != HS_OK) return st;
+    if ((st = map_of<T, TI>(&mv, p, view_of(p->v, p->heads, p->v_heads, p->v_dim), ws + sp.v, many ? 64 : 16, C, &terms)) != HS_OK) return st;
+    if ((st = map_of<T, TI>(&mg, p, view_of(*d_o, p->heads, p->heads, p->v_dim), ws + sp.g, 16, C, &terms)) != HS_OK) return st;
     CUtensorMap mg64 = mg;  // the same in tiles of 64 columns
     if (many) {
         View g = view_of(*d_o, p->heads, p->heads, p->v_dim);
@@ -113,6 +114,7 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
         }
         if (!encode(&mg64, g, p->batch, p->tokens, 64, C)) return hs_internal::cuda_fail("cuTensorMapEncodeTiled", cudaErrorInvalidValue);
     }
+    if ((st = launch_terms<T, TI>(terms, stream)) != HS_OK) return st;
     if ((st = launch_chunks<KP, C, TI, TM, TM, true>(mq, mk, q, word, stream)) != HS_OK) return st;
     {
         hd::Params f = q;

@@ -2,8 +2,8 @@
 selection over sorted candidates.
 
 Tolerances of attention_testlib, for the same reasons: float32 results are sums whose operands count with 24 bits, in at most 256
-products each before they are joined (256 roundings of 2^-24 are 1.5e-5); a bfloat16 result is rounded once itself (2^-9) and hangs on
-at most two operands that are (2^-9 each).  The recurrence does not enlarge what is off as long as beta |k|^2 lies between 0 and 2 and
+products each before they are joined (256 roundings of 2^-24 are 1.5e-5); a bfloat16 result is rounded once itself (at most 2^-8 of an
+element, which is below 2^-9 in the 2-norm) and hangs on at most two operands that are.  The recurrence does not enlarge what is off as long as beta |k|^2 lies between 0 and 2 and
 decays between 0 and 1: (I - beta k k^T) has no singular value above one."""
 import torch
 

@@ -236,6 +236,29 @@ def test_steps_continue_a_prompt(hd, tokens, dtype):
     close(state, want_s, "state")
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_offsets_past_32_bits(hd, dtype):
+    """Batches and tokens more than 2^31 elements apart, and states behind 2^31 elements of a pool."""
+    far = torch.empty(((1 << 31) + (1 << 22)) * (2 if dtype is F32 else 1) + (1 << 22), device=DEV, dtype=BF16).view(dtype)
+    q, k, v, log_a, beta, state = make(2, 70, 2, 2, 2, 2, 64, 64, dtype, "token", True, seed=3)
+    wide = [far.as_strided(x.shape, ((1 << 31) + 8 * n, 192 * 2 * 64, 64, 1), 64 * 2 * 64 * n) for n, x in enumerate((q, k, v))]
+    for to, x in zip(wide, (q, k, v)):
+        to.copy_(x)
+    ins = [x.detach().requires_grad_() for x in (*wide, log_a, beta, state)]
+    plain = [x.detach().requires_grad_() for x in (q, k, v, log_a, beta, state)]
+    outs = []
+    for x in (ins, plain):
+        o, s = hd.delta_attention(*x)
+        outs.append([o, s, *torch.autograd.grad((o.float().sum() + s.sum()), x)])
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    pool = torch.empty((1 << 31) // (2 * 64 * 64) + 2, 2, 64, 64, device=DEV)
+    slots = torch.tensor([pool.shape[0] - 1, 0], dtype=torch.int32, device=DEV)
+    pool[slots.long()] = state
+    step = [x[:, 0] for x in (q, k, v, log_a, beta)]
+    got = hd.delta_attention_step(*(x[:, 0] for x in wide), *step[3:], pool, slots=slots)
+    assert torch.equal(got, hd.delta_attention_step(*step, state)) and torch.equal(pool[slots.long()], state)
+
+
 def test_a_kept_workspace_and_a_captured_call(hd):
     """Two graphs of the same call on one workspace, replayed in turn with new inputs, beside an eager call on another stream."""
     from paper_2311_06281_b200 import heinsen_scan as hs
