@@ -656,15 +656,39 @@ __global__ void __launch_bounds__(32) part_sum_kernel(const double* part, int ba
     if (lane == 0) dlog_a[h] = (float)s;
 }
 
-// [batch, tokens, heads, dim] float32, a row for each head, summed over the heads that share one
+// [batch, tokens, heads, dim] float32, a row for each head, summed over the `each` heads that share one; one or two tensors, a row of the
+// grid each.  A thread has a unit of four columns (`whole`: dim and the result's address allow it), or of one.
+struct Sums {
+    struct Tensor {
+        const float* from;
+        void* to;
+        long long units;
+        int each, dim, whole;
+    } tensors[2];
+    int count;
+};
 template <class T>
-__global__ void __launch_bounds__(256) shared_sum_kernel(const float* from, T* to, int heads, int groups, int dim, long long total) {
-    for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < total; e += (long long)gridDim.x * blockDim.x) {
-        const long long d = e % dim, g = e / dim % groups, row = e / dim / groups;
-        const int each = heads / groups;
-        float s = 0.0f;
-        for (int i = 0; i < each; ++i) s += from[(row * heads + g * each + i) * dim + d];
-        to[e] = ha::from_f<T>(s);
+__global__ void __launch_bounds__(256) shared_sum_kernel(const Sums p) {
+    const Sums::Tensor& x = p.tensors[blockIdx.y];
+    const uint32_t along = x.whole ? x.dim / 4 : x.dim;
+    for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < x.units; e += (long long)gridDim.x * blockDim.x) {
+        const long long row = e >> 32 ? e / along : (uint32_t)e / along;
+        const float* const from = x.from + row * x.each * x.dim;
+        const int d = (int)(e - row * along);
+        if (x.whole) {
+            float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+            for (int i = 0; i < x.each; ++i) {
+                const float4 f = *reinterpret_cast<const float4*>(from + (long long)i * x.dim + 4 * d);
+                s.x += f.x; s.y += f.y; s.z += f.z; s.w += f.w;
+            }
+            if constexpr (sizeof(T) == 2) static_cast<uint2*>(x.to)[e] = make_uint2(ha::pack_bf16(s.x, s.y), ha::pack_bf16(s.z, s.w));
+            else static_cast<float4*>(x.to)[e] = s;
+        } else {
+            float s = 0.0f;
+            for (int i = 0; i < x.each; ++i) s += from[(long long)i * x.dim + d];
+            static_cast<T*>(x.to)[e] = ha::from_f<T>(s);
+        }
     }
 }
 

@@ -33,11 +33,17 @@ template <int KP, int TI> Space space_of(const heinsen_attention_problem* p) {
     return s;
 }
 
-template <class T>
-hs_status shared_sum(const float* from, void* to, const heinsen_attention_problem* p, int groups, int dim, cudaStream_t stream) {
-    const long long total = p->batch * p->tokens * groups * dim;
-    hd::shared_sum_kernel<T><<<(unsigned)std::min<long long>((total + 255) / 256, kSms * 16), 256, 0, stream>>>(from, static_cast<T*>(to), p->heads, groups,
-                                                                                                         dim, total);
+// To sum the heads that share a gradient's row.
+template <class T> void add_sum(hd::Sums* all, const float* from, void* to, const heinsen_attention_problem* p, int groups, int dim) {
+    const bool whole = dim % 4 == 0 && (reinterpret_cast<uintptr_t>(to) & (4 * sizeof(T) - 1)) == 0;
+    all->tensors[all->count++] = {from, to, p->batch * p->tokens * groups * (whole ? dim / 4 : dim), p->heads / groups, dim, whole};
+}
+template <class T> hs_status launch_sums(const hd::Sums& all, cudaStream_t stream) {
+    if (!all.count) return HS_OK;
+    long long most = 0;
+    for (int i = 0; i < all.count; ++i) most = std::max(most, all.tensors[i].units);
+    const dim3 grid((unsigned)std::min<long long>((most + 255) / 256, kSms * 16), all.count);
+    hd::shared_sum_kernel<T><<<grid, 256, 0, stream>>>(all);
     return launched("shared_sum_kernel");
 }
 
@@ -137,7 +143,11 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
         };
         st = each ? back(float{}) : back(T{});
         if (st != HS_OK) return st;
-        if (each && (st = shared_sum<T>(at(sp.dv), dv, p, p->v_heads, p->v_dim, stream)) != HS_OK) return st;
+        if (each) {
+            hd::Sums sums{};
+            add_sum<T>(&sums, at(sp.dv), dv, p, p->v_heads, p->v_dim);
+            if ((st = launch_sums<T>(sums, stream)) != HS_OK) return st;
+        }
     }
     const bool fixed = p->log_a.batch_stride == 0 && p->log_a.token_stride == 0;
     double* const part = reinterpret_cast<double*>(ws + sp.part);
@@ -151,8 +161,10 @@ hs_status backward(const heinsen_delta_problem* dp, const heinsen_attention_tens
         g.dq = eq ? (void*)wq : dq; g.dk_out = ek ? (void*)wk : dk;
         g.each_q = eq; g.each_k = ek;
         if ((st = launch_grad<KP, TI, T>(mq, mk, mg, g, word, stream)) != HS_OK) return st;
-        if (eq && (st = shared_sum<T>(wq, dq, p, p->q_heads, p->k_dim, stream)) != HS_OK) return st;
-        if (ek && (st = shared_sum<T>(wk, dk, p, p->k_heads, p->k_dim, stream)) != HS_OK) return st;
+        hd::Sums sums{};
+        if (eq) add_sum<T>(&sums, wq, dq, p, p->q_heads, p->k_dim);
+        if (ek) add_sum<T>(&sums, wk, dk, p, p->k_heads, p->k_dim);
+        if ((st = launch_sums<T>(sums, stream)) != HS_OK) return st;
     } else {
         g.dq = dq; g.dk_out = dk;
         if ((st = launch_grad<KP, TI, T>(mq, mk, mg, g, word, stream)) != HS_OK) return st;
