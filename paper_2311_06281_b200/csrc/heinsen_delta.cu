@@ -93,7 +93,9 @@ hs_status step(const hd::Step& s, long long batch, cudaStream_t stream) {
         return launched("step_kernel");
     };
     if (!vec) return go(hd::step_kernel<T, 32, 1, 32>, 32);
-    const bool narrow = s.dv <= 32 || batch * s.heads * ((s.dv + 63) / 64) <= kSms / 2;
+    // 32 columns to a CTA where 64 would be two CTAs for each SM or fewer: states of 128 x 128, 32 CTAs of 64 columns 6.2 us, their columns in
+    // 32s 4.1; 128 CTAs 6.2, 5.1; 256 CTAs 6.2, 6.2; 512 CTAs 8.4, 8.3; 1024 CTAs 12.6, 14.4.
+    const bool narrow = s.dv <= 32 || batch * s.heads * ((s.dv + 63) / 64) <= 2 * kSms;
     if (narrow) return s.dk <= 128 ? go(hd::step_kernel<T, 32, 4, 4>, 32) : go(hd::step_kernel<T, 32, 4, 8>, 32);
     return s.dk <= 128 ? go(hd::step_kernel<T, 64, 4, 8>, 64) : go(hd::step_kernel<T, 64, 4, 16>, 64);
 }
