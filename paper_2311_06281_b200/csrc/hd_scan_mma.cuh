@@ -40,12 +40,17 @@ __device__ __forceinline__ void mma_left(uint32_t d, uint32_t a, uint32_t b, uin
 }
 
 // Tensor memory, in columns.  The update shares columns with the state's terms, V' (backward: dO) with X, and the later of two
-// factors with the earlier: each is written when the products that read the other are done.
-struct PassColumns {
+// factors with the earlier: each is written when the products that read the other are done, which a barrier says.  Products are in
+// the order in which they are issued only where accumulator and shape are the same: sums in the same columns all have one shape, or a
+// barrier between them.
+template <int kMode> struct PassColumns {
     static constexpr uint32_t s = 0, x = 192, y = 256, o = 320, f = 384, g = 480, columns = 512;
-    // What the solution adds to Y (dV'), by itself: the tensor core cuts off what it adds, and Y is the larger.  Where the state's last
-    // terms were, which X alone reads.
-    static constexpr uint32_t solved = s + 128;
+    // What the solution adds to Y (dV'), by itself: the tensor core cuts off what it adds, and Y is the larger.  N is triangular: the block
+    // of 16 factors that reaches all tokens adds to the 64 columns of `solved`, the next to 48 of `second` (from the block of
+    // tokens that it starts with on), the other two to two blocks of 16 in `third`.  The first is where the state's last terms were, which X
+    // alone reads; the others are where its first ones were, or, where those still meet Q, in X (each half of the warps then writes V'
+    // where it alone has read) and in columns that only the backward pass has another use for.
+    static constexpr uint32_t solved = s + 128, second = kMode == 0 ? x : s, third = kMode == 0 ? g : s + 64;
     // term t of sixteen rows q of a thread's half of the state: its first two terms lie where its own half of the update will
     static __device__ __forceinline__ constexpr uint32_t state(int half, int q, int t) { return t < 2 ? s + half * 64 + q * 16 + t * 8 : s + 128 + half * 32 + q * 8; }
     static __device__ __forceinline__ constexpr uint32_t factor(int jj, int t) { return f + 24 * jj + 8 * t; }
@@ -117,7 +122,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                 int* gave_up) {
     using L = PassLayout<KP, kMode>;
     using I = typename L::I;
-    using M = PassColumns;
+    using M = PassColumns<kMode>;
     using B = Blocks<64>;
     constexpr int C = 64, kOwn = KP / 2;
     constexpr bool kOutput = kMode == 0, kBack = kMode == 2;
@@ -176,6 +181,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
             // ------------------------------------------------------------------------------------------ products
             if (ha::elect_one()) {
                 constexpr uint32_t shape64 = ha::mma_shape(C, 0), shape_t = ha::mma_shape(16, ha::kColMajorA), shape_u = ha::mma_shape(KP, ha::kColMajorB);
+                constexpr uint32_t kN = kBack ? ha::kColMajorB : 0, shape48 = ha::mma_shape(48, kN), shape16 = ha::mma_shape(16, kN);
                 const uint32_t ident = ha::operand(base + L::ident, 256);
                 auto step = [](int kk) { return (uint32_t)((kk >> 2) * (L::block >> 4) + (kk & 3) * 2); };
                 // left factors of KP/16 steps, three terms of the state, with a tile of rows of tokens
@@ -201,18 +207,22 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                                    V = ha::operand(at + L::v, L::block), N = ha::operand(at + L::n, 512), P = ha::operand(at + L::p, 512);
                     if (!(ok = wait(kFull + st, it / L::kStages))) break;
                     ha::tmem_after_sync();
-                    if constexpr (kBack) {  // dO^T P, while the state's terms are formed
+                    if constexpr (kBack) {  // dO^T P, while the state's terms are formed: sixteen tokens j of all ii >= j
 #pragma unroll
                         for (int u = 2; u >= 0; --u)
 #pragma unroll
                             for (int ii = 3; ii >= 0; --ii)
-                                mma_tile<ha::kSwizzled, kRows32>(M::o, V + ii * 128, P + ((u * I::plane + B::by_rows(ii, 0) * 512) >> 4),
-                                                                 ha::mma_shape(16 * (ii + 1), ha::kColMajorA | ha::kColMajorB), u < 2 || ii < 3);
+#pragma unroll
+                                for (int j = 0; j <= ii; ++j)
+                                    mma_tile<ha::kSwizzled, kRows32>(M::o + 16 * j, V + ii * 128, P + ((u * I::plane + B::by_rows(ii, j) * 512) >> 4),
+                                                                     ha::mma_shape(16, ha::kColMajorA | ha::kColMajorB), u < 2 || ii < 3);
                     } else {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) ha::mma_ss<ha::plain_layout(128)>(M::y + 16 * q, V + q * 128, ident, shape_t, false);
                     }
                     if (!(ok = wait(kStateReady, it))) break;
+                    if constexpr (kOutput)
+                        if (it > 0 && !(ok = wait(kOut, it - 1))) break;  // P has met the V' in X's columns
                     ha::tmem_after_sync();
                     with_state(M::x, K, 3);
                     ha::mma_commit(bars + 8 * kScores);
@@ -221,18 +231,19 @@ __global__ void __launch_bounds__(kPassThreads, 1)
 #pragma unroll
                     for (int level = 2; level >= 0; --level)
 #pragma unroll
-                        for (int u = 0; u <= level; ++u)
+                        for (int u = 0; u <= level; ++u) {
+                            const bool more = level < 2 || u > 0;
+                            // block `n` of the factors, counted from the one that reaches all tokens, with block `i` of the tokens
+                            auto left = [&](int n) { return M::factor(kBack ? 3 - n : n, u); };
+                            auto block = [&](int i, int n) {
+                                return N + (((level - u) * I::plane + (kBack ? B::by_rows(3 - n, i) : B::by_columns(i, n)) * 512) >> 4);
+                            };
+                            mma_left<kRows32>(M::solved, left(0), block(0, 0), ha::mma_shape(C, kN), more);
+                            mma_left<kRows32>(M::second + (kBack ? 0 : 16), left(1), block(kBack ? 0 : 1, 1), shape48, more);
 #pragma unroll
-                            for (int n = 0; n < 4; ++n) {
-                                const int jj = kBack ? 3 - n : n;  // (the first covers all tokens)
-                                const bool more = level < 2 || u > 0 || n > 0;
-                                if constexpr (kBack)
-                                    mma_left<kRows32>(M::solved, M::factor(jj, u), N + (((level - u) * I::plane + B::by_rows(jj, 0) * 512) >> 4),
-                                                      ha::mma_shape(16 * (jj + 1), ha::kColMajorB), more);
-                                else
-                                    mma_left<kRows32>(M::solved + 16 * jj, M::factor(jj, u), N + (((level - u) * I::plane + B::by_columns(jj, jj) * 512) >> 4),
-                                                      ha::mma_shape(C - 16 * jj, 0), more);
-                            }
+                            for (int i = 0; i < 2; ++i) mma_left<kRows32>(M::third + 16 * i, left(2), block(kBack ? i : i + 2, 2), shape16, more);
+                            mma_left<kRows32>(M::third + (kBack ? 0 : 16), left(3), block(kBack ? 0 : 3, 3), shape16, true);
+                        }
                     ha::mma_commit(bars + 8 * kSolved);
                     if constexpr (kOutput) {  // while the threads work on E
                         if (it > 0 && !(ok = wait(kOutRead, it - 1))) break;
@@ -241,6 +252,8 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                         ha::mma_commit(bars + 8 * kFar);
                     }
                     if (!(ok = wait(kWrites, it))) break;
+                    if constexpr (kOutput)
+                        if (!(ok = wait(kFar, it))) break;  // Q has met the state's terms in the update's columns
                     ha::tmem_after_sync();
                     update(K, false, false);
                     if constexpr (kBack) {
@@ -256,7 +269,9 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                         for (int t = 1; t >= 0; --t)
 #pragma unroll
                             for (int jj = 0; jj < 4; ++jj)
-                                mma_left<kRows32>(M::o + 16 * jj, M::value(jj, t), P + (B::by_columns(jj, jj) * 512 >> 4), ha::mma_shape(C - 16 * jj, 0), true);
+#pragma unroll
+                                for (int i = jj; i < 4; ++i)
+                                    mma_left<kRows32>(M::o + 16 * i, M::value(jj, t), P + (B::by_columns(i, jj) * 512 >> 4), shape16, true);
                         ha::mma_commit(bars + 8 * kOut);
                     }
                     ha::mma_commit(bars + 8 * (kEmpty + st));
@@ -476,40 +491,51 @@ __global__ void __launch_bounds__(kPassThreads, 1)
             ok = ok && wait(kSolved, it);
             ha::tmem_after_sync();
             {
-                uint32_t x[2][16], z[2][16];
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    ha::tmem_ld16_early(x[g], lanes + M::y + 32 * half + 16 * g);
-                    ha::tmem_ld16_early(z[g], lanes + M::solved + 32 * half + 16 * g);
-                }
+                // whether `third` reaches this half's two blocks of tokens; `second` reaches those and one of the other half's
+                const bool far = half == (kBack ? 0 : 1);
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     const int jj = 2 * half + g, j = 16 * jj;
-                    ha::tmem_ready(x[g]);
-                    ha::tmem_ready(z[g]);
+                    uint32_t x[16], z[16], more[16];
+                    auto plus = [](uint32_t (&to)[16], const uint32_t (&y)[16]) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) x[g][e] = __float_as_uint(__uint_as_float(x[g][e]) + __uint_as_float(z[g][e]));
-                    if constexpr (kBack) ha::tmem_st16(lanes + M::y + j, x[g]);  // F, for the warps beside
+                        for (int e = 0; e < 16; ++e) to[e] = __float_as_uint(__uint_as_float(to[e]) + __uint_as_float(y[e]));
+                    };
+                    ha::tmem_ld16_early(z, lanes + M::solved + j);
+                    if (far || g == (kBack ? 0 : 1)) {
+                        ha::tmem_ld16(more, lanes + M::second + j);
+                        ha::tmem_ready(z);
+                        plus(z, more);
+                    }
+                    ha::tmem_ld16_early(x, lanes + M::y + j);
+                    if (far) {
+                        ha::tmem_ld16(more, lanes + M::third + 16 * g);
+                        plus(z, more);
+                    }
+                    ha::tmem_ready(z);
+                    ha::tmem_ready(x);
+                    plus(x, z);
+                    if constexpr (kBack) ha::tmem_st16(lanes + M::y + j, x);  // F, for the warps beside
                     if constexpr (kMode == 1) {
                         if (ok && (v >> 4) < slices) {
                             float* const to = p.errors + ((chunk * slices + (v >> 4)) * C + j) * 16 + (v & 15);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) to[e * 16] = __uint_as_float(x[g][e]);
+                            for (int e = 0; e < 16; ++e) to[e * 16] = __uint_as_float(x[e]);
                         }
                     }
-                    weigh<true>(vec + I::beta / 4 + j, x[g]);
+                    weigh<true>(vec + I::beta / 4 + j, x);
                     if constexpr (kOutput) {
                         uint32_t w[2][8];
-                        put_left<2>(x[g], w);
+                        put_left<2>(x, w);
 #pragma unroll
                         for (int t = 0; t < 2; ++t) ha::tmem_st8(lanes + M::value(jj, t), w[t]);
                     }
-                    weigh<true>(vec + (kBack ? I::early : I::late) / 4 + j, x[g]);
+                    weigh<true>(vec + (kBack ? I::early : I::late) / 4 + j, x);
                     if constexpr (kBack)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) x[g][e] ^= 0x80000000u;
+                        for (int e = 0; e < 16; ++e) x[e] ^= 0x80000000u;
                     uint32_t w[3][8];
-                    put_left<3>(x[g], w);
+                    put_left<3>(x, w);
 #pragma unroll
                     for (int t = 0; t < 3; ++t) ha::tmem_st8(lanes + M::factor(jj, t), w[t]);
                 }
