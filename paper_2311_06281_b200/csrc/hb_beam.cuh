@@ -97,8 +97,12 @@ __global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(cons
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) m = fmaxf(m, red_max[i]);
-    float part_sum;  // NaN where a logit is (the maximum passes it over), and for an infinite maximum, of which m - m is NaN
-    {
+    float part_sum = 0.0f;  // NaN where a logit is (the maximum passes it over), and for a maximum of +inf, of which m - m is NaN
+    if (m == __int_as_float(0xff800000)) {  // none but -inf, and NaN
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (x[i] != x[i]) part_sum = x[i];
+    } else {
         const ha::pair minus = ha::make_pair2(-m, -m), base = ha::make_pair2(ha::kLog2e, ha::kLog2e);
         ha::pair sums = 0;
 #pragma unroll
@@ -143,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(cons
         sum = 0.0;
 #pragma unroll
         for (int i = 0; i < kThreads / 32; ++i) sum += red_sum[i];
-        p.part_sum[at] = make_double2((double)m, m == __int_as_float(0xff800000) ? 0.0 : sum);
+        p.part_sum[at] = make_double2((double)m, sum);
     }
     // A bound of -inf (few logits that are not): of those at -inf the first `keep` places are enough.
     const float bound = from_ordered(least), lowest = __int_as_float(0xff800000);
