@@ -23,8 +23,10 @@ extern "C" {
  * logits: float32 or bf16 [batch, beams, vocabulary], the last dimension contiguous, strides of the others in elements; scores
  * float32 [batch, beams] and ended (1 byte each, or NULL) contiguous.  Outputs, contiguous [batch, keep]: out_scores float32, out_parents
  * (the beam w) and out_tokens (n) int32.  1 <= beams <= 64, 1 <= keep <= 64, keep <= beams * vocabulary, vocabulary <= 2^31 - 2^20;
- * 0 <= end_token < vocabulary where ended is given.  Values are formed and compared in 64 bits; the exponentials of a sum are float32's
- * own, summed in 64 bits.  workspace: 256-byte aligned scratch of heinsen_beam_workspace_bytes.  Asynchronous on `stream`.
+ * 0 <= end_token < vocabulary where ended is given.  Values are formed and compared in 64 bits, with log-sums whose exponentials are
+ * float32's own, up to 32 of them added in float32 and those sums in 64 bits: a log-sum is off by less than 2^-18, whatever the logits.
+ * Beams of a call that have the same logits have the same log-sum to the last bit, wherever their rows begin.
+ * workspace: 256-byte aligned scratch of heinsen_beam_workspace_bytes.  Asynchronous on `stream`.
  */
 typedef struct {
     int64_t batch, vocabulary;

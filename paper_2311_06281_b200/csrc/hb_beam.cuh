@@ -37,11 +37,12 @@ __device__ __forceinline__ float from_ordered(uint32_t u) { return __uint_as_flo
 // Bound by HBM and by the instructions for a logit (an exponential and a test): 256 rows of 100003 float32 logits, a fifth of them of
 // ended beams, 28 us for 82 MB; 8 logits a thread where there are few rows (4 rows of 32000 bf16: 3.3 us).
 // Parts of many tiles of 16 logits a thread, the next one's loads ahead, gave the part 31 to 38 us and the join 7.3: no gain.
-// One part of one row; kPer logits a thread, in vectors of 16 bytes at addresses of 16 bytes: part 0 begins at the last such address
-// at or before the row's first logit.
-template <class T, int kPer>
+// One part of one row; kPer logits a thread.  Which of a row's logits a thread has is the same for all rows of a call, wherever they
+// begin, so that beams with the same logits have the same sums to the last bit and their candidates come in the order of the beams.
+// kWhole: every row begins at an address of 16 bytes, and a thread has vectors of as many; else single logits, a warp's side by side.
+template <class T, int kPer, bool kWhole>
 __global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(const Select p) {
-    constexpr int kVec = 16 / sizeof(T), kVecs = kPer / kVec;
+    constexpr int kVec = kWhole ? 16 / sizeof(T) : 1, kVecs = kPer / kVec;
     __shared__ float red_max[kThreads / 32];
     __shared__ double red_sum[kThreads / 32];
     __shared__ __align__(16) uint32_t tops[kThreads];
@@ -54,30 +55,37 @@ __global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(cons
     const int part = blockIdx.x % p.parts;
     const long long row = blockIdx.x / p.parts, b = row / p.beams, w = row % p.beams;
     const T* const from = static_cast<const T*>(p.logits) + b * p.sb + w * p.sw;
-    const int ahead = (int)((reinterpret_cast<uintptr_t>(from) & 15u) / sizeof(T));
-    const int first = part * (kThreads * kPer) - ahead, vocabulary = (int)p.vocabulary;
+    const int first = part * (kThreads * kPer), vocabulary = (int)p.vocabulary;
     if (tid == 0) found = 0;
     if (p.ended && p.ended[row]) return;  // nothing of it is asked for
     float x[kPer];
     auto token = [&](int i) { return first + (i / kVec * kThreads + tid) * kVec + i % kVec; };
-    if (first >= 0 && first + kThreads * kPer <= vocabulary) {  // all of it is there: no load waits for another's test
-        uint4 f[kVecs];
+    if (first + kThreads * kPer <= vocabulary) {  // all of it is there: no load waits for another's test
+        if constexpr (kWhole) {
+            uint4 f[kVecs];
 #pragma unroll
-        for (int u = 0; u < kVecs; ++u) f[u] = __ldcs(reinterpret_cast<const uint4*>(from + token(u * kVec)));
+            for (int u = 0; u < kVecs; ++u) f[u] = __ldcs(reinterpret_cast<const uint4*>(from + token(u * kVec)));
 #pragma unroll
-        for (int u = 0; u < kVecs; ++u) {
-            const uint32_t r[4] = {f[u].x, f[u].y, f[u].z, f[u].w};
+            for (int u = 0; u < kVecs; ++u) {
+                const uint32_t r[4] = {f[u].x, f[u].y, f[u].z, f[u].w};
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                if constexpr (sizeof(T) == 2) x[u * kVec + i] = __uint_as_float(i & 1 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
-                else x[u * kVec + i] = __uint_as_float(r[i]);
+                for (int i = 0; i < kVec; ++i) {
+                    if constexpr (sizeof(T) == 2) x[u * kVec + i] = __uint_as_float(i & 1 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
+                    else x[u * kVec + i] = __uint_as_float(r[i]);
+                }
             }
+        } else {
+            T f[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) f[i] = __ldcs(from + token(i));
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) x[i] = ha::to_f(f[i]);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int n = token(i);
-            x[i] = n >= 0 && n < vocabulary ? ha::to_f(from[n]) : __int_as_float(0xff800000);
+            x[i] = n < vocabulary ? ha::to_f(from[n]) : __int_as_float(0xff800000);
         }
     }
     float top = x[0];
@@ -103,6 +111,8 @@ __global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(cons
         for (int i = 0; i < kPer; ++i)
             if (x[i] != x[i]) part_sum = x[i];
     } else {
+        // Off by 2^-20 from the 16 roundings of its two chains and their sum, 2^-22 from the exponentials, and 2.3 x 2^-24 from each exponent
+        // times its size, 17 in the mean at most for 2^31 logits: less than 2^-18 of the sum.
         const ha::pair minus = ha::make_pair2(-m, -m), base = ha::make_pair2(ha::kLog2e, ha::kLog2e);
         ha::pair sums = 0;
 #pragma unroll
@@ -151,12 +161,12 @@ __global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(cons
     }
     // A bound of -inf (few logits that are not): of those at -inf the first `keep` places are enough.
     const float bound = from_ordered(least), lowest = __int_as_float(0xff800000);
-    const int places = bound == lowest ? max(first, 0) + p.keep : vocabulary;
+    const int places = bound == lowest ? first + p.keep : vocabulary;
     if (top >= bound)
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int n = token(i);
-            if (x[i] >= bound && n >= 0 && n < (x[i] > lowest ? vocabulary : min(places, vocabulary))) {
+            if (x[i] >= bound && n < (x[i] > lowest ? vocabulary : min(places, vocabulary))) {
                 const int to = atomicAdd(&found, 1);
                 if (to < kList) {
                     list_key[to] = ordered(x[i]);
@@ -187,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(cons
             for (int i = 0; i < kPer; ++i) {
                 const int n = token(i);
                 const unsigned long long key = (unsigned long long)ordered(x[i]) << 32 | (uint32_t)~(uint32_t)n;
-                if (n >= 0 && n < vocabulary && key < last && key > mine) mine = key;
+                if (n < vocabulary && key < last && key > mine) mine = key;
             }
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) {

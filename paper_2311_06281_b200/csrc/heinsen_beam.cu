@@ -29,8 +29,13 @@ hs_status validate(const heinsen_beam_problem* p) {
 // 16.5, 13.6; 1024 of them 27.6, 20.0.
 int per_thread(const heinsen_beam_problem* p) { return p->batch * p->beams * ((p->vocabulary + 8191) / 8192) > kSms / 2 ? 32 : 8; }
 long long parts_of(const heinsen_beam_problem* p) {
-    const long long each = hb::kThreads * per_thread(p), ahead = 16 / (p->dtype == HS_F32 ? 4 : 2) - 1;  // the row may begin behind an address of 16 bytes
-    return (p->vocabulary + ahead + each - 1) / each;
+    const long long each = hb::kThreads * per_thread(p);
+    return (p->vocabulary + each - 1) / each;
+}
+// Does every row begin at an address of 16 bytes?
+bool whole_rows(const heinsen_beam_problem* p) {
+    const long long vec = p->dtype == HS_F32 ? 4 : 8;
+    return (reinterpret_cast<uintptr_t>(p->logits) & 15u) == 0 && (p->batch == 1 || p->batch_stride % vec == 0) && (p->beams == 1 || p->beam_stride % vec == 0);
 }
 
 struct Space {
@@ -48,8 +53,10 @@ Space space_of(const heinsen_beam_problem* p) {
 template <class T> hs_status select(const heinsen_beam_problem* p, const hb::Select& s, cudaStream_t stream) {
     const long long grid = p->batch * p->beams * s.parts;
     if (grid > 0x7fffffffll) return HS_ERR_INVALID_ARG;
-    if (per_thread(p) == 32) hb::part_kernel<T, 32><<<(unsigned)grid, hb::kThreads, 0, stream>>>(s);
-    else hb::part_kernel<T, 8><<<(unsigned)grid, hb::kThreads, 0, stream>>>(s);
+    auto go = [&](auto fn) { fn<<<(unsigned)grid, hb::kThreads, 0, stream>>>(s); };
+    const bool whole = whole_rows(p);
+    if (per_thread(p) == 32) go(whole ? hb::part_kernel<T, 32, true> : hb::part_kernel<T, 32, false>);
+    else go(whole ? hb::part_kernel<T, 8, true> : hb::part_kernel<T, 8, false>);
     const hs_status st = launched("part_kernel");
     if (st != HS_OK) return st;
     hb::join_kernel<<<(unsigned)p->batch, hb::kThreads, 0, stream>>>(s);

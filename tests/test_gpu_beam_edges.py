@@ -1,4 +1,4 @@
-"""Beam search's selection where few logits decide: a NaN beside masked logits."""
+"""Beam search's selection where few logits decide: a NaN beside masked logits, equal beams at every alignment."""
 import pytest
 import torch
 
@@ -29,3 +29,18 @@ def test_a_nan_beside_masked_logits(hb, b, w, n, aligned, dtype):  # noqa: F811
     logits[:, 0] = -INF  # and where nothing else is
     logits[:, 0, n // 2] = float("nan")
     compare(hb, rows(logits, aligned), scores, min(4, w * n))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("b,w,n,keep", [(1, 4, 5003, 4), (2, 8, 100003, 8), (3, 16, 50257, 16), (40, 8, 8193, 20), (2, 64, 3001, 64), (1, 7, 2050, 7)])
+def test_equal_beams_are_taken_in_order(hb, b, w, n, keep, dtype):  # noqa: F811
+    """The same logits in every beam, in rows that begin at every place within 16 bytes: candidates are equal to the last bit, so w * N + n
+    decides."""
+    logits, scores = make(b, 1, n, dtype, seed=n)
+    logits, scores = logits.expand(b, w, n).contiguous(), scores.expand(b, w).contiguous()
+    order = torch.sort(logits.double().flatten(1), dim=-1, descending=True, stable=True).indices[:, :keep]
+    values, parents, tokens = hb.beam_select(logits, scores, keep)
+    assert torch.equal(parents.long() * n + tokens.long(), order)
+    first = logits.flatten(1).gather(1, order)
+    same = first[:, 1:] == first[:, :-1]
+    assert torch.equal(values[:, 1:][same], values[:, :-1][same])
