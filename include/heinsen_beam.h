@@ -16,7 +16,7 @@ extern "C" {
  *
  *         value(w, n) = scores[w] + logits[w, n] - log sum_m exp(logits[w, m])
  *
- * best first, equal ones in the order of w * vocabulary + n.  A beam with ended[w] != 0 goes on with the token end_token alone, at
+ * best first, equal ones in the order of w * vocabulary + n (of one beam, larger logits first where only their values are equal).  A beam with ended[w] != 0 goes on with the token end_token alone, at
  * value scores[w]; its other candidates count as -inf.  So do all candidates of a beam whose score is not finite or whose
  * logits have no finite log-sum (a NaN or +inf among them, or nothing but -inf).  Candidates of -inf fill up where there are no others.
  *

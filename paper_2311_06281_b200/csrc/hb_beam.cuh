@@ -219,6 +219,22 @@ __global__ void __launch_bounds__(kThreads, kPer == 32 ? 4 : 6) part_kernel(cons
     }
 }
 
+// A candidate: its value, its logit, and beam and token as one number.
+struct Candidate {
+    double value;
+    float logit;
+    long long place;
+};
+// The order of candidates.  Equal values come by beam; those of one beam by logit, since two logits can have the same sum with a large
+// score or log-sum in 64 bits, and the parts' lists, of which no more than `keep` are at hand, are in the logits' order.
+__device__ __forceinline__ bool before(const Candidate& a, const Candidate& b) {  // no branches: loads of more than one go together
+    const bool by_place = ((int)(a.place >> 32) != (int)(b.place >> 32)) | (a.logit == b.logit);
+    return (a.value > b.value) | ((a.value == b.value) & ((by_place & (a.place < b.place)) | (!by_place & (a.logit > b.logit))));
+}
+__device__ __forceinline__ Candidate across(const Candidate& c, int lanes) {
+    return {__shfl_xor_sync(~0u, c.value, lanes), __shfl_xor_sync(~0u, c.logit, lanes), __shfl_xor_sync(~0u, c.place, lanes)};
+}
+
 // The best of a group.  Candidates are formed in 64 bits; as above, the keep-th best of the threads' own best bounds the keep-th best
 // of all, and those above it are sorted.
 // Bound by latency, a CTA for a group: 8 beams of 13 parts with 8 candidates each 8.6 us (11 us with one load of a lane at a time),
@@ -229,12 +245,15 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Select p) {
     __shared__ int state[64];  // 0: as its logits say; 1: ended; 2: out
     __shared__ double value_of[kJoinList];
     __shared__ long long place_of[kJoinList];
+    __shared__ float logit_of[kJoinList];
     __shared__ double least_value;
     __shared__ long long least_place;
+    __shared__ float least_logit;
     __shared__ int found;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const long long b = blockIdx.x, nowhere = 0x7fffffffffffffffll;
+    const long long b = blockIdx.x;
     const double lowest = -__longlong_as_double(0x7ff0000000000000ll);
+    const Candidate none{lowest, 0.0f, 0x7fffffffffffffffll};
     if (tid == 0) found = 0;
     for (int w = warp; w < p.beams; w += kThreads / 32) {
         const long long row = b * p.beams + w;
@@ -264,7 +283,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Select p) {
     auto each_candidate = [&](auto take) {
         for (int w = warp; w < p.beams; w += kThreads / 32) {
             const int how = state[w];
-            const long long row0 = (long long)w * p.vocabulary;
+            const long long row0 = (long long)w << 32;
             if (how == 0) {
                 const double base = logs[w];
                 const long long at = (b * p.beams + w) * lists;
@@ -279,120 +298,95 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Select p) {
                     }
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        if (n[u] >= 0) take(base + (double)v[u], row0 + n[u]);
+                        if (n[u] >= 0) take(Candidate{base + (double)v[u], v[u], row0 + n[u]});
                 }
             } else {
                 for (int i = lane; i <= p.keep && i < p.vocabulary; i += 32)
-                    if (!(how == 1 && i == p.end_token)) take(lowest, row0 + i);
-                if (how == 1 && lane == 0) take((double)p.scores[b * p.beams + w], row0 + p.end_token);
+                    if (!(how == 1 && i == p.end_token)) take(Candidate{lowest, 0.0f, row0 + i});
+                if (how == 1 && lane == 0) take(Candidate{(double)p.scores[b * p.beams + w], 0.0f, row0 + p.end_token});
             }
         }
     };
-    auto before = [](double v, long long at, double u, long long other) { return v > u || (v == u && at < other); };
-    double value = lowest;
-    long long place = nowhere;
-    each_candidate([&](double v, long long at) {
-        if (before(v, at, value, place)) {
-            value = v;
-            place = at;
-        }
+    auto put = [&](int at, const Candidate& c) {
+        value_of[at] = c.value;
+        logit_of[at] = c.logit;
+        place_of[at] = c.place;
+    };
+    auto get = [&](int at) { return Candidate{value_of[at], logit_of[at], place_of[at]}; };
+    Candidate own = none;
+    each_candidate([&](const Candidate& c) {
+        if (before(c, own)) own = c;
     });
-    double group_value = value;
-    long long group_place = place;
     const bool few = p.keep <= 16;
     if (few)  // the best of every eight threads
 #pragma unroll
         for (int o = 1; o < 8; o *= 2) {
-            const double v = __shfl_xor_sync(~0u, group_value, o);
-            const long long at = __shfl_xor_sync(~0u, group_place, o);
-            if (before(v, at, group_value, group_place)) {
-                group_value = v;
-                group_place = at;
-            }
+            const Candidate c = across(own, o);
+            if (before(c, own)) own = c;
         }
     const int each = few ? 8 : 1, members = kThreads / each;
-    if (tid % each == 0) {
-        value_of[tid / each] = group_value;
-        place_of[tid / each] = group_place;
-    }
+    if (tid % each == 0) put(tid / each, own);
     __syncthreads();
     if (tid < members) {
-        const double v = value_of[tid];
-        const long long at = place_of[tid];
+        own = get(tid);
         int rank = 0;
 #pragma unroll 4
-        for (int i = 0; i < members; ++i) rank += before(value_of[i], place_of[i], v, at) || (place_of[i] == at && i < tid);
+        for (int i = 0; i < members; ++i) {
+            const Candidate c = get(i);
+            rank += before(c, own) | ((c.place == own.place) & (i < tid));
+        }
         if (rank == p.keep - 1) {
-            least_value = v;
-            least_place = at;
+            least_value = own.value;
+            least_logit = own.logit;
+            least_place = own.place;
         }
     }
     __syncthreads();
-    const double bound = least_value;
-    const long long bound_place = least_place;
-    each_candidate([&](double v, long long at) {
-        if (!before(bound, bound_place, v, at)) {
+    const Candidate bound{least_value, least_logit, least_place};
+    each_candidate([&](const Candidate& c) {
+        if (!before(bound, c)) {
             const int to = atomicAdd(&found, 1);
-            if (to < kJoinList) {
-                value_of[to] = v;
-                place_of[to] = at;
-            }
+            if (to < kJoinList) put(to, c);
         }
     });
     __syncthreads();
     const int count = found;
-    auto put = [&](int k, double v, long long at) {
+    auto choose = [&](int k, const Candidate& c) {
         const long long to = b * p.keep + k;
-        p.out_scores[to] = (float)v;
-        p.out_parents[to] = (int)(at / p.vocabulary);
-        p.out_tokens[to] = (int)(at % p.vocabulary);
+        p.out_scores[to] = (float)c.value;
+        p.out_parents[to] = (int)(c.place >> 32);
+        p.out_tokens[to] = (int)c.place;
     };
     if (count <= kJoinList) {
-        for (int c = tid; c < count; c += kThreads) {
-            const double v = value_of[c];
-            const long long at = place_of[c];
+        for (int at = tid; at < count; at += kThreads) {
+            const Candidate c = get(at);
             int r = 0;
-            for (int i = 0; i < count; ++i) r += before(value_of[i], place_of[i], v, at);
-            if (r < p.keep) put(r, v, at);
+            for (int i = 0; i < count; ++i) r += before(get(i), c);
+            if (r < p.keep) choose(r, c);
         }
         return;
     }
-    // more than the list holds (places are all different, so this takes one thread with very many good ones): one after the other
-    double last_value = -lowest;
-    long long last_place = -1;
+    // More than the list holds, one after the other: where a few threads have very many of the best, or where fewer threads than `keep` asks
+    // for have any (few beams: a beam is one warp's), so that nothing bounds them.
+    Candidate last{-lowest, 0.0f, -1};
     for (int k = 0; k < p.keep; ++k) {
-        value = lowest;
-        place = nowhere;
-        each_candidate([&](double v, long long at) {
-            if (before(last_value, last_place, v, at) && before(v, at, value, place)) {
-                value = v;
-                place = at;
-            }
+        own = none;
+        each_candidate([&](const Candidate& c) {
+            if (before(last, c) && before(c, own)) own = c;
         });
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            const double v = __shfl_xor_sync(~0u, value, o);
-            const long long at = __shfl_xor_sync(~0u, place, o);
-            if (before(v, at, value, place)) {
-                value = v;
-                place = at;
-            }
+            const Candidate c = across(own, o);
+            if (before(c, own)) own = c;
         }
         __syncthreads();
-        if (lane == 0) {
-            value_of[warp] = value;
-            place_of[warp] = place;
-        }
+        if (lane == 0) put(warp, own);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kThreads / 32; ++i)
-            if (before(value_of[i], place_of[i], value, place)) {
-                value = value_of[i];
-                place = place_of[i];
-            }
-        last_value = value;
-        last_place = place;
-        if (tid == 0) put(k, value, place);
+            if (before(get(i), own)) own = get(i);
+        last = own;
+        if (tid == 0) choose(k, own);
     }
 }
 

@@ -107,7 +107,8 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int | None = 
 
     logits [B, W, N]: float32 or bfloat16, last dimension contiguous, any other strides; scores float32 [B, W]: the beams' log
     probabilities so far.  Of the W * N candidates scores[b, w] + log_softmax(logits[b, w])[n] the `beams` (default W) best are taken,
-    best first, equal ones in the order of w * N + n: their scores (float32), the beams w they continue and their tokens n (int32).
+    best first, equal ones in the order of w * N + n (values count in 64 bits, and logits of one beam that even so have the same value
+    stay in their order): their scores (float32), the beams w they continue and their tokens n (int32).
     ended [B, W] (bool or uint8): such a beam goes on with end_token alone, at its own score.  A beam that is not there has the score
     -inf; it, and one with a NaN or +inf among its logits, has candidates of -inf only, which come last.
     W and `beams` up to 64.  Logits are masked by -inf.  workspace: scratch from ``workspace()``, kept by the caller.

@@ -1,4 +1,5 @@
-"""Beam search's selection where few logits decide: a NaN beside masked logits, equal beams at every alignment."""
+"""Beam search's selection where few logits decide: a NaN beside masked logits, equal beams at every alignment, logits that differ by
+less than their sums with a score can say."""
 import pytest
 import torch
 
@@ -44,3 +45,17 @@ def test_equal_beams_are_taken_in_order(hb, b, w, n, keep, dtype):  # noqa: F811
     first = logits.flatten(1).gather(1, order)
     same = first[:, 1:] == first[:, :-1]
     assert torch.equal(values[:, 1:][same], values[:, :-1][same])
+
+
+@pytest.mark.parametrize("w,n", [(1, 3000), (3, 3000), (2, 70001)])
+def test_logits_nearer_than_their_sums_can_say(hb, w, n):  # noqa: F811
+    """Logits of a beam that a sum in 64 bits cannot tell apart stay in their order, however many are asked for; between beams the first
+    comes first."""
+    logits = torch.zeros(1, w, n, device=DEV)
+    places = [n - 1, 5, n // 2, 700]
+    for i, at in enumerate(places):
+        logits[:, :, at] = (4 - i) * 1e-25
+    want = (places + [i for i in range(n) if i not in places])[:64]
+    for keep in (1, 2, 3, 5, 16, 17, 64):
+        _, parents, tokens = hb.beam_select(logits, torch.zeros(1, w, device=DEV), keep)
+        assert tokens[0].tolist() == want[:keep] and not parents.any()
