@@ -1,5 +1,5 @@
 """Beam search's selection where few logits decide: a NaN beside masked logits, equal beams at every alignment, logits that differ by
-less than their sums with a score can say."""
+less than their sums with a score can say, one beam with a long list."""
 import pytest
 import torch
 
@@ -59,3 +59,9 @@ def test_logits_nearer_than_their_sums_can_say(hb, w, n):  # noqa: F811
     for keep in (1, 2, 3, 5, 16, 17, 64):
         _, parents, tokens = hb.beam_select(logits, torch.zeros(1, w, device=DEV), keep)
         assert tokens[0].tolist() == want[:keep] and not parents.any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("w,keep", [(1, 8), (1, 16), (1, 64), (2, 9), (3, 64)])
+def test_few_beams_with_a_large_vocabulary(hb, w, keep, dtype):  # noqa: F811
+    compare(hb, *make(2, w, 150000, dtype, seed=keep), keep)
