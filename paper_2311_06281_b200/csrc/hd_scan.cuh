@@ -652,6 +652,12 @@ __device__ __forceinline__ void weigh_tokens(float (&x)[2][4], const float* weig
         }
     }
 }
+// Is the state forgotten behind a token of its chunk, by a log decay of -inf (kReset) that follows?  What the state answers there then meets
+// nothing but weights of zero, and has to be a number: 0 * NaN must not reach the tokens behind.  (A chunk's log decays sum up to less
+// than kReset only where one of them is below -156, whose decay is zero too.)
+__device__ __forceinline__ bool forgotten(float whole_log, float token_log) { return whole_log - token_log < 0.99f * kReset * kLog2e; }
+__device__ __forceinline__ float number(float x) { return fabsf(x) < __int_as_float(0x7f800000) ? x : 0.0f; }
+
 // Sixteen tokens of sixteen columns of a tile of V (dO), transposed, as float32
 template <int TI>
 __device__ __forceinline__ void read_values(float (&y)[2][4], uint32_t tile, uint32_t term, int block, const Lane& at) {
@@ -769,6 +775,12 @@ __global__ void __launch_bounds__(kScanThreads, 1)
                 float y[2][4];
                 add_up(x, xs, w);
                 weigh_tokens<true>(x, vec + I::early / 4 + 16 * w);
+                if (vec[I::whole / 4] == 0.0f)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (forgotten(vec[I::whole / 4 + 1], vec[I::hi / 4 + 16 * w + 8 * u + 2 * (lane & 3) + (e & 1)])) x[u][e] = number(x[u][e]);
                 read_values<TI>(y, V, L::own, w, at);
                 const int left = live - (t0 + 16 * w) - 2 * (lane & 3);  // of the sequence, from this lane's first token on
 #pragma unroll

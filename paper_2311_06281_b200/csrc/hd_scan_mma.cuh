@@ -461,6 +461,10 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                     ha::tmem_ready(x[g]);
                     ha::tmem_ready(y[g]);
                     weigh<kPlain>(vec + (kBack ? I::late : I::early) / 4 + j, x[g]);
+                    if constexpr (!kPlain && !kBack)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (forgotten(vec[I::whole / 4 + 1], vec[I::hi / 4 + j + e])) x[g][e] = __float_as_uint(number(__uint_as_float(x[g][e])));
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const float f = kBack ? __uint_as_float(y[g][e]) + __uint_as_float(x[g][e]) : __uint_as_float(y[g][e]) - __uint_as_float(x[g][e]);

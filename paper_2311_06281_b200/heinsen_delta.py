@@ -159,7 +159,7 @@ def delta_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: to
     h * Hq // H of q); beta: float32 [B, T, H], the share of the error that is written, 0 to 1 (or 2) for keys of length one;
     keys are taken as they are.  state0 [B, H, K, V] float32 continues earlier tokens; lengths [B] int32 ends row b after
     lengths[b] tokens.  scale defaults to K ** -0.5.  o [B, T, H, V] has q's dtype, state [B, H, K, V] is float32 (what the next
-    call or ``delta_attention_step`` takes).  log_a = -inf forgets the state at that token: packed sequences start so.
+    call or ``delta_attention_step`` takes).  log_a = -inf forgets the state, whatever it holds, at that token: packed sequences start so.
     A NaN or infinity in q, k or v spoils its row's heads from up to 63 tokens before it on.
     The products run on the tensor cores.  float32 tensors count with 24 bits.  Of bfloat16 tensors the state and the gradients
     of log_a, beta and state0 do too (1e-7 to 8e-7 off); the state that meets a query counts with 16, a chunk's own weights with 8.

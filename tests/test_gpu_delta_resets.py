@@ -1,5 +1,5 @@
 """The delta rule where log decays are -inf: gradients over sequences that forget their state in the middle of chunks (packed
-sequences), and states that hold what is not a number where the first token forgets them."""
+sequences), and states that hold what is not a number where the first token or a later one forgets them."""
 import pytest
 import torch
 
@@ -41,3 +41,24 @@ def test_a_state_that_the_first_token_forgets(hd, shape, what, dtype):  # noqa: 
         runs.append([o.detach(), s.detach(), *torch.autograd.grad([o, s], leaves, [d_o, torch.ones_like(s)])])
     assert all(torch.isfinite(x).all() for x in runs[0])
     assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("what", [float("nan"), float("inf")])
+@pytest.mark.parametrize("at", [1, 15, 37, 63, 64, 70])
+@pytest.mark.parametrize("shape", [(2, 100, 2, 2, 2, 2, 64, 64), (1, 100, 2, 2, 2, 2, 256, 64), (5, 100, 16, 16, 16, 16, 64, 128)], ids=str)
+def test_a_state_that_a_later_token_forgets(hd, shape, at, what, dtype):  # noqa: F811
+    """Packed sequences behind one whose state is not a number: from the token that forgets it on, all is as with any other state."""
+    ins = list(make(*shape, dtype, "token", True, seed=8))
+    ins[3][:, at] = -float("inf")
+    d_o = torch.randn(*shape[:3], shape[7], device=DEV).to(dtype)
+    runs = []
+    for value in (0.0, what):
+        ins[5] = torch.full_like(ins[5], value)
+        leaves = [x.detach().requires_grad_() for x in ins]
+        o, s = hd.delta_attention(*leaves)
+        runs.append([s.detach(), *(x[:, at:] for x in (o.detach(), *torch.autograd.grad([o, s], leaves[:5], [d_o, torch.ones_like(s)])))])
+        assert value == 0.0 or not torch.isfinite(o[:, :at]).any()
+    assert all(torch.isfinite(x).all() for x in runs[0])
+    for a, b, n in zip(*runs, ("state", "o", "dq", "dk", "dv", "dlog_a", "dbeta")):
+        assert torch.equal(a, b), n
