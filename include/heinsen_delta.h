@@ -11,8 +11,8 @@
  *   - Tokens are worked on in chunks of up to 64: what is said there of 128 tokens (decays above one, what a NaN spoils) holds
  *     for 64.
  *   - Products are formed on the tensor cores from bf16 terms.  Float32 tensors count with 24 bits (three terms a factor).  Of
- *     bf16 tensors states, the writes v - a S^T k and the gradients of the gates and of state0 count with 24 bits, the state that meets
- *     a query with 16, the weights of a chunk's own tokens in o and the state's gradient in dk with 8.  A float32 number beyond 3.38e38 in magnitude counts as infinite, one below 2^-100 may count as zero.
+ *     bf16 tensors states, the writes v - a S^T k and the gradients of the gates, of v and of state0 count with 24 bits, what meets a
+ *     query or a key in o, dq and dk (the state, its gradient, the weights between a chunk's tokens) with 16.  A float32 number beyond 3.38e38 in magnitude counts as infinite, one below 2^-100 may count as zero.
  */
 #ifndef HEINSEN_DELTA_H_
 #define HEINSEN_DELTA_H_

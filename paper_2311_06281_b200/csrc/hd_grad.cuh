@@ -231,11 +231,12 @@ __global__ void __launch_bounds__(kScanThreads, 1)
 
 constexpr int kGradThreads = 256;
 
-// Terms of V', Z and S (TM), and of D and the H (TL), which only the gradients of the tensors' own type depend on.
+// Terms of V', Z and S (TM), and of D and the H (TD, TH), which only the gradients of the tensors' own type depend on: 16 bits for those
+// that are rounded to 8 themselves.
 template <int KP, int C, int TI, int TM>
 struct GradLayout {
     static constexpr int SL = TI == 1 ? 64 : 32;  // columns of V at a time
-    static constexpr int TD = TI == 1 ? 1 : 3, TH = TI == 1 ? 2 : 3;
+    static constexpr int TD = TI == 1 ? 2 : 3, TH = TD;
     static constexpr uint32_t tile = KP * C * 2 * TI, k = 0, q = tile;
     static constexpr uint32_t slab = 2 * tile, g = slab, own = C * 32, v = g + SL / 16 * TI * own, z = v + TM * SL * C * 2, s = z + TM * SL * C * 2,
                               d = s + TM * SL * KP * 2, slab_end = d + TD * SL * KP * 2;

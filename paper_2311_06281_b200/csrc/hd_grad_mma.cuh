@@ -12,8 +12,8 @@
 //
 // 4096 chunks, keys and values 128 wide: 396 us, 1.1 GB read and 0.14 GB written (HBM alone: 190 us).  A chunk's 27000 clocks are eight
 // steps over V (1200 to 1500 each, bound by the products of three terms) and what follows them, which waits for the last one and which
-// the next chunk's steps wait for: far_i, H and W, the last products, the gates' sums, dq and dk (10000).  D enters the product for dk
-// with one term and H with two, since dk is rounded to 8 bits.
+// the next chunk's steps wait for: far_i, H and W, the last products, the gates' sums, dq and dk (10000).  D and H enter the products for
+// dq and dk with two terms (16 bits), since those are rounded to 8.
 #pragma once
 #include "hd_grad.cuh"
 #include "hd_scan_mma.cuh"
@@ -34,10 +34,10 @@ template <int KP> struct GradMmaLayout {
     static constexpr int C = 64, kTiles = 2, kRaw = 3;
     using I = Image<C, 3, 3, true>;
     static constexpr uint32_t block = 2 * C * 128, tiles_bytes = KP / 64 * block;  // blocks of 64 columns: rows of Q, then of K
-    // two operand buffers, of sixteen columns of V each: three terms of [dO; Z] (the lower terms of dO zero), of V', of S; one of D
+    // two operand buffers, of sixteen columns of V each: three terms of [dO; Z] (the lower terms of dO zero), of V', of S; two of D
     static constexpr uint32_t ops = kTiles * tiles_bytes;
     static constexpr uint32_t az = 0, az_term = 2 * C * 32, v = 3 * az_term, v_term = C * 32, s = v + 3 * v_term, s_term = 16 * KP * 2, d = s + 3 * s_term,
-                              op = (d + s_term + 1023) / 1024 * 1024;
+                              op = (d + 2 * s_term + 1023) / 1024 * 1024;
     // what arrives for them: S, D (16 x KP), E^T, F^T (16 x C) in float32, dO
     static constexpr uint32_t raw = ops + 2 * op, raw_d = 16 * KP * 4, raw_e = 2 * raw_d, raw_f = raw_e + 16 * C * 4, raw_g = raw_f + 16 * C * 4,
                               raw_bytes = raw_g + C * 32;
@@ -160,8 +160,11 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                             mma_tile<kRows32, kRows32>(L::tg, az + u * (L::az_term >> 4), vo + (level - u) * (L::v_term >> 4), near_shape, more);
                         }
 #pragma unroll
-                    for (int u = 1; u >= 0; --u)  // rows 64..127 are V' (above them is what lies before it: those sums are not used)
-                        mma_tile<kRows32, ha::kSwizzled>(L::tl, vo + u * (L::v_term >> 4) - (C * 32 >> 4), dd, wide_shape, slab > 0 || u == 0);
+                    for (int level = 1; level >= 0; --level)  // rows 64..127 are V' (above them is what lies before it: those sums are not used)
+#pragma unroll
+                        for (int u = level; u >= 0; --u)
+                            mma_tile<kRows32, ha::kSwizzled>(L::tl, vo + u * (L::v_term >> 4) - (C * 32 >> 4), dd + (level - u) * (L::s_term >> 4), wide_shape,
+                                                             slab > 0 || level == 0 || u == 0);
                     if (slab == 0) {
                         const uint32_t rows = ha::operand(base + ts * L::tiles_bytes, 0);
 #pragma unroll
@@ -240,7 +243,7 @@ __global__ void __launch_bounds__(kGradMmaThreads, 1)
                         const float4 s4 = reinterpret_cast<const float4*>(raw)[tid], d4 = reinterpret_cast<const float4*>(raw + L::raw_d)[tid];
                         const uint32_t sat = wide<16>(r, col >> 3) + 2 * (col & 7);
                         put_terms<TM>(to + L::s, L::s_term, s4, sat);
-                        put_terms<1>(to + L::d, L::s_term, d4, sat);
+                        put_terms<2>(to + L::d, L::s_term, d4, sat);
                         cross = fmaf(s4.x, d4.x, fmaf(s4.y, d4.y, fmaf(s4.z, d4.z, fmaf(s4.w, d4.w, cross))));
                     }
                     if (tid < 128) reinterpret_cast<uint4*>(to + L::az)[tid] = reinterpret_cast<const uint4*>(raw + L::raw_g)[tid];

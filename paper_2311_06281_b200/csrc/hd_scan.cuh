@@ -693,8 +693,8 @@ __device__ __forceinline__ void quarter_scores(float (*y)[4], const uint32_t (&a
         }
 }
 
-// kOut: the output; else the state before every chunk and E, for the gradients.  TO: terms of S and V' in the output.  Of bf16 tensors
-// the state has three terms where a later state hangs on it and two (16 bits) where it meets a query: the output is rounded to 8.
+// kOut: the output; else the state before every chunk and E, for the gradients.  TO: terms of S, P and V' in the output.  Of bf16 tensors
+// the state has three terms where a later state hangs on it, and all three two (16 bits) in the output, which is rounded to 8 itself.
 template <int KP, int C, int TI, int TM, int TP, bool kOut, class T>
 __global__ void __launch_bounds__(kScanThreads, 1)
     scan_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const Params p,

@@ -62,15 +62,15 @@ template <int kMode> struct PassColumns {
 template <int KP, int kMode>
 struct PassLayout {
     static constexpr int C = 64, kStages = 2;
-    using I = Image<C, 3, kMode == 0 ? 1 : 3, kMode != 0>;
+    static constexpr int kTermsP = kMode == 0 ? 2 : 3;
+    using I = Image<C, 3, kTermsP, kMode != 0>;
     static constexpr uint32_t block = C * 128, tile = KP / 64 * block;
     static constexpr uint32_t k = 0, q = tile, v = kMode == 1 ? tile : 2 * tile, image = v + 2 * block;  // V (backward: dO): 128 columns
     // backward N is wanted by rows
-    static constexpr uint32_t n = image + I::n, p = n + 3 * I::plane, stage = (p + (kMode == 0 ? I::plane : kMode == 2 ? 3 * I::plane : 0) + 1023) / 1024 * 1024;
+    static constexpr uint32_t n = image + I::n, p = n + 3 * I::plane, bytes = p + (kMode == 1 ? 0 : kTermsP * I::plane), stage = (bytes + 1023) / 1024 * 1024;  // (bytes: of a chunk)
     // backward E^T as well, eight times [token][16]
     static constexpr uint32_t errors = stage, whole = stage + (kMode == 2 ? 8 * C * 64 : 0);
     static constexpr uint32_t ident = kStages * whole, bars = ident + 512, end = bars + 256;
-    static constexpr uint32_t bytes = p + (kMode == 0 ? I::plane : kMode == 2 ? 3 * I::plane : 0);  // of a chunk
 };
 
 // Sixteen values as terms of a left factor
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                     bulk_load(to + L::image, image, I::n, bar);
                     bulk_load(to + L::n, image + (kBack ? I::rows : I::n), 3 * I::plane, bar);
                     if (kBack) bulk_load(to + L::errors, p.errors + (((long long)bh * p.chunks + n) * slices + v0 / 16) * 16 * C, here * C * 64, bar);
-                    if (kMode != 1) bulk_load(to + L::p, image + I::p, (kBack ? 3 : 1) * I::plane, bar);
+                    if (kMode != 1) bulk_load(to + L::p, image + I::p, L::kTermsP * I::plane, bar);
                     for (int c = 0; c < KP / 64; ++c) {
                         ha::tma_load_4d(to + L::k + c * L::block, &mk, 64 * c, h / p.kdiv, n * C, b, bar);
                         if (kMode != 1) ha::tma_load_4d(to + L::q + c * L::block, &mq, 64 * c, h / p.qdiv, n * C, b, bar);
@@ -266,12 +266,14 @@ __global__ void __launch_bounds__(kPassThreads, 1)
                         if (!(ok = wait(kFarScaled, it))) break;
                         ha::tmem_after_sync();
 #pragma unroll
-                        for (int t = 1; t >= 0; --t)
+                        for (int level = 1; level >= 0; --level)
 #pragma unroll
-                            for (int jj = 0; jj < 4; ++jj)
+                            for (int t = level; t >= 0; --t)
 #pragma unroll
-                                for (int i = jj; i < 4; ++i)
-                                    mma_left<kRows32>(M::o + 16 * i, M::value(jj, t), P + (B::by_columns(i, jj) * 512 >> 4), shape16, true);
+                                for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+                                    for (int i = jj; i < 4; ++i)
+                                        mma_left<kRows32>(M::o + 16 * i, M::value(jj, t), P + (((level - t) * I::plane + B::by_columns(i, jj) * 512) >> 4), shape16, true);
                         ha::mma_commit(bars + 8 * kOut);
                     }
                     ha::mma_commit(bars + 8 * (kEmpty + st));

@@ -29,7 +29,7 @@ struct Space {
     size_t image, q, k, v, total;
 };
 template <int KP, int TI> Space space_of(const heinsen_attention_problem* p) {
-    constexpr int C = hd::chunk_tokens(KP), TM = 3, TP = TI;
+    constexpr int C = hd::chunk_tokens(KP), TM = 3, TP = TI == 1 ? 2 : 3;
     Space s;
     s.image = kHeaderBytes;
     s.q = s.image + image_bytes<C, TM, TP, false>(p);
@@ -41,7 +41,7 @@ template <int KP, int TI> Space space_of(const heinsen_attention_problem* p) {
 
 template <int KP, class T>
 hs_status forward(const heinsen_delta_problem* dp, const heinsen_attention_tensor* o, float* state, uint8_t* ws, cudaStream_t stream) {
-    constexpr int C = hd::chunk_tokens(KP), TI = sizeof(T) == 2 ? 1 : 3, TM = 3, TP = TI;
+    constexpr int C = hd::chunk_tokens(KP), TI = sizeof(T) == 2 ? 1 : 3, TM = 3, TP = TI == 1 ? 2 : 3;
     const heinsen_attention_problem* p = &dp->a;
     const Space sp = space_of<KP, TI>(p);
     int* const word = gave_up_word();

@@ -162,7 +162,8 @@ def delta_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_a: to
     call or ``delta_attention_step`` takes).  log_a = -inf forgets the state, whatever it holds, at that token: packed sequences start so.
     A NaN or infinity in q, k or v spoils its row's heads from up to 63 tokens before it on.
     The products run on the tensor cores.  float32 tensors count with 24 bits.  Of bfloat16 tensors the state and the gradients
-    of log_a, beta and state0 do too (1e-7 to 8e-7 off); the state that meets a query counts with 16, a chunk's own weights with 8.
+    of log_a, beta and state0 do too (1e-7 to 8e-7 off); what o, dq and dk are products with counts with 16, so that they are off by
+    their own rounding to bfloat16 alone (1.7e-3 in the mean).
     workspace: scratch from ``workspace()``, kept by the caller; ``heinsen_scan.check(workspace)`` then reports what the
     device recorded for the last call (a bounded wait that ran out).  Without it each call takes its own; ``check(device)``
     reports for all calls, backward ones too.
