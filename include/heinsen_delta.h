@@ -41,7 +41,9 @@ hs_status heinsen_delta_backward(const heinsen_delta_problem* p, const heinsen_a
                                  size_t workspace_bytes, void* stream);
 
 /* Scratch in bytes for either call on these very tensors (what TMA cannot load is laid out anew there); 0 for sizes the library
- * does not accept. */
+ * does not accept.  Of each (batch, head) pair a chunk of 64 tokens takes 27 KB forward and 243 KB backward where keys and values are 128
+ * wide and bf16 (47 KB of weights, the state before the chunk and its gradient after it 64 KB each, the errors and theirs 32 KB each, sums
+ * 4 KB), and a backward call room for a copy of dO: 1.06 GB for 8 x 2048 tokens of 16 heads.  Nothing is kept between the calls. */
 size_t heinsen_delta_workspace_bytes(const heinsen_delta_problem* p, int backward);
 
 /* As heinsen_attention_check, for the calls of this file. */

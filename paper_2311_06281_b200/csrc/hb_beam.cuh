@@ -237,8 +237,8 @@ __device__ __forceinline__ Candidate across(const Candidate& c, int lanes) {
 
 // The best of a group.  Candidates are formed in 64 bits; as above, the keep-th best of the threads' own best bounds the keep-th best
 // of all, and those above it are sorted.
-// Bound by latency, a CTA for a group: 8 beams of 13 parts with 8 candidates each 8.6 us (11 us with one load of a lane at a time),
-// 4 beams of 16 parts with 4 each 7 us.
+// Bound by latency, a CTA for a group: 8 beams of 13 parts with 8 candidates each 8.5 us (11 us with one load of a lane at a time),
+// 4 beams of 16 parts with 4 each 5.1 us.  Comparisons with branches in them: 15 us and 8 us.
 constexpr int kJoinList = 512;
 __global__ void __launch_bounds__(kThreads) join_kernel(const Select p) {
     __shared__ double logs[64];

@@ -10,7 +10,7 @@
 // the sixteen columns before; dO is exact, its lower terms zero.  A CTA stays and takes chunk after chunk; one warp loads ahead, one
 // issues the products, the others have a row of a product and a quarter of its columns each.
 //
-// 4096 chunks, keys and values 128 wide: 396 us, 1.1 GB read and 0.14 GB written (HBM alone: 190 us).  A chunk's 27000 clocks are eight
+// 4096 chunks, keys and values 128 wide: 392 us, 1.1 GB read and 0.14 GB written (HBM alone: 190 us).  A chunk's 27000 clocks are eight
 // steps over V (1200 to 1500 each, bound by the products of three terms) and what follows them, which waits for the last one and which
 // the next chunk's steps wait for: far_i, H and W, the last products, the gates' sums, dq and dk (10000).  D and H enter the products for
 // dq and dk with two terms (16 bits), since those are rounded to 8.

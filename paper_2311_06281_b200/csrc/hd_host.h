@@ -108,7 +108,7 @@ inline long long chunks_of(const heinsen_attention_problem* p) {
 template <int C, int TM, int TP, bool kBack> size_t image_bytes(const heinsen_attention_problem* p) { return up256((size_t)chunks_of(p) * hd::Image<C, TM, TP, kBack>::end); }
 
 // Slices of sixteen columns of V that a CTA of the mma.sync scans has: two where there would be more CTAs than SMs otherwise, since a
-// chunk of two at once takes 3.4 us and two CTAs of one slice one after the other 4.6 (keys 128 wide, one CTA to an SM).
+// chunk of two at once takes 3.4 us and two CTAs of one slice one after the other 4.8 (keys 128 wide, one CTA to an SM).
 inline int slices_for(long long pairs, int slices) { return pairs * slices > kSms && slices > 1 ? hd::kMaxSlices : 1; }
 
 template <int KP, int C, int TI, int TM, int TP, bool kBack>
@@ -147,10 +147,13 @@ hs_status launch_scan(const CUtensorMap& mq, const CUtensorMap& mk, const CUtens
 template <int KP, int TI> constexpr bool fits_tcgen05() { return TI == 1 && KP <= 128; }
 
 // Which of the two: a CTA with four warps for each of one or two slices of sixteen columns of V (mma.sync), or one with 128 columns
-// (tcgen05).  Measured for a chunk, keys and values 128 wide, with one CTA to an SM: one slice 2.3 us, two 3.4 us, 128 columns 5.1 us
-// forward; for the gradients (both passes) two slices 6.4 us, 128 columns 12.9 us.  So two slices as long as their waves over the SMs
-// are at most 3/2 (2) of the other's: 8 (batch, head) pairs of 16385 tokens are 590 us against 1180, 64 pairs of 2048 218 us against
-// 162, 128 pairs with their gradients 820 us against 426.
+// (tcgen05).  Measured for a chunk, keys and values 128 wide, with one CTA to an SM: one slice 2.4 us, two 3.4 us, 128 columns 5.4 us
+// forward; for the gradients (both passes) two slices 6.7 us, 128 columns 13.7 us.  So two slices as long as their waves over the SMs
+// are at most 3/2 (2) of the other's.  Sequences of 1024 tokens, mma.sync and tcgen05 forward, and both passes for the gradients, us:
+//   keys, values 128, 128: 32 pairs 56, 86; 110, 221.  64 pairs 110, 93; 215, 220.  80 pairs 161, 94; 315, 223.  160 pairs 266, 183; 526, 431.
+//   64, 64: 64 pairs 48, 68; 93, 155.  80 pairs 92, 69; 176, 157.  128 pairs 94, 76; 178, 176.  160 pairs 137, 137; 261, 298.
+//   64, 128: 64 pairs 94, 67; 179, 162.    128, 64: 64 pairs 56, 90; 110, 197.  80 pairs 107, 93; 211, 198.
+// Where it takes the slower one (64, 64, 80 pairs; 64, 128, 64 pairs, gradients) that costs 12% at most.
 inline bool many_slices(const heinsen_attention_problem* p, bool backward) {
     const long long pairs = p->batch * p->heads, slices = (p->v_dim + 15) / 16, two = (pairs * ((slices + 1) / 2) + kSms - 1) / kSms,
                     all = (pairs * ((p->v_dim + 127) / 128) + kSms - 1) / kSms;

@@ -18,7 +18,7 @@
 // between the four (one barrier), and each hands the others its tokens' Y and V' as factors (two more), so that the state never leaves
 // its registers.  Against one warp for a slice with all of the state: 16385 tokens, 8 heads of 128, 1.23 ms -> 0.64 ms.
 //
-// What bounds it: chunks follow each other, and in a chunk the sums, the solution and the update.  A chunk takes a slice 2.3 us (keys
+// What bounds it: chunks follow each other, and in a chunk the sums, the solution and the update.  A chunk takes a slice 2.4 us (keys
 // 128 wide; four barriers, 120 to 250 products of a warp one behind the other's operands), with the tensor pipe busy 41% of the time
 // and two slices on an SM.
 #pragma once
@@ -140,7 +140,7 @@ struct ChunkLayout {
 // every N^T_sw the next product's factor in its registers.  24 bits in all of it: a wrong N is wrong for every column of V.
 // Bound by the instructions around the products (issue slots 47%, tensor pipe 21%): the weights between tokens, two to an instruction
 // and with one exponential for a row of a block where the block lies before all of the warp's rows, the splitting into terms and the
-// solution's chain.  2048 chunks of 64 tokens, keys 128 wide: 39 us (64 MB of images written), with five CTAs to an SM for four 45 us,
+// solution's chain.  2048 chunks of 64 tokens, keys 128 wide: 40 us (56 MB of images written), with five CTAs to an SM for four 45 us,
 // with the weights one by one 54 us.
 template <int KP, int C, int TI, int TM, int TP, bool kBack>
 __global__ void __launch_bounds__(2 * C, C == 64 && TI == 1 ? 5 : 1) chunk_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const Params p,

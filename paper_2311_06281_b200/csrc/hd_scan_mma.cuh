@@ -10,10 +10,10 @@
 // Warps 0-7 have the state and the chain of dependent steps; warps 8-15 what hangs on it without the chain waiting: the output
 // (backward: dV, F and the sums over V for the gates, and the terms of dO).  One warp loads, a chunk ahead, one issues the products.
 //
-// Bound by the chain: a chunk takes 8400 clocks (products of X 1040, their sums scaled and split 1250, the solution 1040, E 1330, the
-// update's products 1070, the state read, decayed and split anew 2200), the tensor pipe is busy 30% of them, HBM 12%.  64 (batch, head)
-// pairs of 2048 tokens, keys and values 128 wide: 162 us; 128 pairs: 176 us forward, 176 us for the states, 250 us backward.  mma.sync
-// against it: many_slices in hd_host.h.
+// Bound by the chain: a chunk takes 8900 clocks (products of X 1290, their sums scaled and split 1150, the solution 1200, E 1600, the
+// update's products 1370, the state read, decayed and split anew 2150), the tensor pipe is busy 29% of them, HBM 12%.  64 (batch, head)
+// pairs of 2048 tokens, keys and values 128 wide: 172 us; 128 pairs: 180 us forward, 180 us for the states, 257 us backward.  Of that 4% are
+// the waits and the sums in places of their own that the order of the products needs.  mma.sync against it: many_slices in hd_host.h.
 #pragma once
 #include "hd_scan.cuh"
 

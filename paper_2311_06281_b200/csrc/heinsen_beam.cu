@@ -25,8 +25,8 @@ hs_status validate(const heinsen_beam_problem* p) {
 }
 
 // Logits of a thread: 32 of them (8192 a CTA), or 8 where that would leave an SM in two without a CTA.  Both kernels together, with 8
-// and with 32 (bf16, keep 4 to 8): 16 CTAs of 8192 logits 10.1 us, 11.5 us; 64 of them 11.3, 12.4; 128 of them 13.3, 12.6; 256 of them
-// 16.5, 13.6; 1024 of them 27.6, 20.0.
+// and with 32 (bf16, keep 4 to 8): 16 CTAs of 8192 logits 8.5 us, 10.2 us (4 rows; 2 rows 10.9, 10.6); 64 of them 11.2, 11.1; 128 of
+// them 12.0, 11.1 (4 rows: 17.7, 11.7); 256 of them 14.6, 11.6; 1024 of them 26.2, 18.0.
 int per_thread(const heinsen_beam_problem* p) { return p->batch * p->beams * ((p->vocabulary + 8191) / 8192) > kSms / 2 ? 32 : 8; }
 long long parts_of(const heinsen_beam_problem* p) {
     const long long each = hb::kThreads * per_thread(p);

@@ -54,7 +54,7 @@ hs_status launch_back(const CUtensorMap& mq, const CUtensorMap& mk, const CUtens
     return launch_slices<hd::ScanLayout<KP, C, TI, TM, TM, true, true>>(hd::back_kernel<KP, C, TI, TM, T>, done, mq, mk, mg, q, word, stream);
 }
 
-// The gradients of the chunks: tcgen05 for bf16 and keys up to 128 wide (4096 chunks, 128 wide: 396 us; with mma.sync 498 us before
+// The gradients of the chunks: tcgen05 for bf16 and keys up to 128 wide (4096 chunks, 128 wide: 392 us; with mma.sync 498 us before
 // the other was made faster), mma.sync for the rest, where all factors have three terms or the tiles would not fit.
 template <int KP, int TI, class T>
 hs_status launch_grad(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mg, const hd::Params& q, int* word, cudaStream_t stream) {
