@@ -16,9 +16,10 @@ extern "C" {
  *
  *         value(w, n) = scores[w] + logits[w, n] - log sum_m exp(logits[w, m])
  *
- * best first, equal ones in the order of w * vocabulary + n (of one beam, larger logits first where only their values are equal).  A beam with ended[w] != 0 goes on with the token end_token alone, at
- * value scores[w]; its other candidates count as -inf.  So do all candidates of a beam whose score is not finite or whose
- * logits have no finite log-sum (a NaN or +inf among them, or nothing but -inf).  Candidates of -inf fill up where there are no others.
+ * best first, equal ones in the order of w * vocabulary + n (of one beam, larger logits first where only their values are equal).
+ * A beam with ended[w] != 0 goes on with the token end_token alone, at value scores[w]; its other candidates count as -inf.  So do all
+ * candidates of a beam whose score is not finite or whose logits have no finite log-sum (a NaN or +inf among them, or nothing but
+ * -inf).  Candidates of -inf fill up where there are no others.
  *
  * logits: float32 or bf16 [batch, beams, vocabulary], the last dimension contiguous, strides of the others in elements; scores
  * float32 [batch, beams] and ended (1 byte each, or NULL) contiguous.  Outputs, contiguous [batch, keep]: out_scores float32, out_parents
